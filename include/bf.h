@@ -315,6 +315,136 @@ BF_API int bf_whatif(const bf_scenario* scn, uint64_t base_index, bf_probe* out,
 BF_API int bf_search_batch_noalloc(const bf_scenario_desc* descs, uint32_t count, bf_result* out,
                             void* cuda_stream);
 
+/* ---- Learning from makespans ----------------------------------------------
+ *
+ * The searches and evaluations above grade the mappings a scheduling model
+ * answers with; these entry points turn such grades into gradients.  The paper
+ * prompts its scheduler (§3.3) and trains nothing: they are this library's
+ * addition, for callers that fit a policy to the makespans of the mappings it
+ * samples.
+ *
+ * All of them are asynchronous on `cuda_stream`, allocate nothing and can be
+ * captured; a workspace is the caller's, of the size its *_workspace function
+ * gives and aligned to 256 bytes, holds nothing between calls, and must not be
+ * used by two calls whose work overlaps.  Values are computed in 32 bits
+ * whatever the matrices' types, sums in an order that does not depend on when
+ * blocks run (the same call gives the same bits), and rounded once.
+ *
+ * A row t of logits x (vocab columns) goes with token y = tokens[t].  With
+ * temperature tau, z = x / tau, p = softmax(z), lp = ln p_y, H = -sum p ln p.
+ * A token below 0 marks a row that is not scored (a prompt, padding): its
+ * logits are not read, its log-probability and entropy are 0 and its gradient
+ * is 0.  A token >= vocab makes its row's values NaN.  Logits may be -inf
+ * (banned tokens); a row with none above -inf has log-probability -inf,
+ * entropy 0, gradient 0, and terms of 0 in the policy loss.
+ */
+enum bf_dtype { BF_F32 = 0, BF_BF16 = 1, BF_F16 = 2 };
+
+/* A matrix in device memory: element (i, j) is data[i * row_stride + j].
+ * At most 2^31 - 1 rows and 2^30 columns, row_stride >= cols. */
+typedef struct bf_matrix {
+  void* data;
+  uint64_t rows, cols;
+  uint64_t row_stride;  /* in elements */
+  uint32_t dtype;       /* bf_dtype */
+  uint32_t pad;
+} bf_matrix;
+
+/* Log-probabilities d_logprob[t] = lp and, unless d_entropy is NULL, entropies
+ * d_entropy[t] = H of the rows of `logits`.  temperature > 0. */
+BF_API int bf_token_logprobs(const bf_matrix* logits, const int64_t* d_tokens, float temperature, float* d_logprob,
+                             float* d_entropy, void* cuda_stream);
+
+/* The gradient in the logits of sum_t d_grad_logprob[t] lp_t +
+ * d_grad_entropy[t] H_t (d_grad_entropy may be NULL):
+ *   dx_j = (g ([j = y] - p_j) - h p_j (ln p_j + H)) / tau.
+ * `grad` has the shape and type of `logits`; it may be `logits` itself (same
+ * data and stride), else the two must not overlap. */
+BF_API int bf_token_logprobs_grad(const bf_matrix* logits, const int64_t* d_tokens, float temperature,
+                                  const float* d_grad_logprob, const float* d_grad_entropy, const bf_matrix* grad,
+                                  void* cuda_stream);
+
+/* How the policy loss weighs its rows: w = 1 / (scored rows); w = 1 / (scored
+ * rows of the row's sequence * sequences with a scored row); w = 1. */
+enum bf_reduction { BF_MEAN_TOKENS = 0, BF_MEAN_SEQUENCES = 1, BF_SUM = 2 };
+
+/* Sequence s is rows [offsets[s], offsets[s+1]); offsets ascend.  Rows outside
+ * every sequence are not scored. */
+typedef struct bf_policy_args {
+  const int64_t* tokens;       /* device, one per row */
+  const int64_t* offsets;      /* device, sequences + 1 */
+  const float* old_logprob;    /* device, one per row: under the policy that sampled the tokens */
+  const float* ref_logprob;    /* device, one per row: under the reference policy; NULL without a KL term */
+  const float* advantage;      /* device, one per sequence, or per row with advantage_per_token */
+  uint64_t sequences;
+  uint32_t advantage_per_token;
+  uint32_t reduction;          /* bf_reduction */
+  float clip_low, clip_high;   /* the ratio is held to [1 - clip_low, 1 + clip_high]; >= 0 */
+  float kl_coef;               /* >= 0 */
+  float entropy_coef;
+  float temperature;           /* > 0 */
+  float grad_scale;            /* factor of the gradient (loss scaling), 1 for none */
+} bf_policy_args;
+
+#define BF_POLICY_STATS 6
+
+/* The clipped policy loss with a KL term and its gradient in the logits.  With
+ * r = e^(lp - old), advantage A and u = ref - lp, a scored row's term is
+ *   l = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A)
+ *       + kl_coef (e^u - u - 1) - entropy_coef H
+ * and the loss is sum w l.  d_stats: the loss, then the weighted sums of
+ * -min(...), of e^u - u - 1 (0 without ref_logprob), of H, of the rows whose
+ * clip stops the gradient, and of r.  d_logprob (may be NULL): lp of each row.
+ * `grad` (may be NULL: loss only) as for bf_token_logprobs_grad. */
+BF_API int bf_policy_loss(const bf_matrix* logits, const bf_policy_args* args, float* d_stats, float* d_logprob,
+                          const bf_matrix* grad, void* d_workspace, uint64_t workspace_bytes, void* cuda_stream);
+BF_API int bf_policy_loss_workspace(uint64_t rows, uint64_t sequences, uint64_t* bytes);
+
+/* Pair p: sequence 2p is the preferred answer (the faster mapping), 2p + 1 the
+ * other. */
+typedef struct bf_preference_args {
+  const int64_t* tokens;       /* device, one per row */
+  const int64_t* offsets;      /* device, 2 * pairs + 1 */
+  const float* ref_logprob;    /* device, one per row; NULL for no reference policy */
+  uint64_t pairs;
+  uint32_t average;            /* rewards from the mean over a sequence's scored rows instead of the sum */
+  float beta;                  /* > 0 */
+  float label_smoothing;       /* eps: in [0, 1) */
+  float margin;
+  float temperature;           /* > 0 */
+  float grad_scale;            /* factor of the gradient (loss scaling), 1 for none */
+} bf_preference_args;
+
+#define BF_PREFERENCE_STATS 4
+
+/* The preference loss and its gradient in the logits.  A sequence's reward is
+ * beta sum (lp - ref) over its scored rows (beta times their mean with
+ * `average`; 0 without scored rows); with h = reward_2p - reward_2p+1 - margin
+ * a pair's loss is -(1 - eps) ln sigma(h) - eps ln sigma(-h), and the loss the
+ * mean over the pairs.  d_stats: the loss, the share of pairs with reward_2p >
+ * reward_2p+1, the mean reward of the preferred and of the other answers.
+ * d_rewards: 2 * pairs.  d_logprob (may be NULL) and `grad` (may be NULL) as
+ * for bf_policy_loss. */
+BF_API int bf_preference_loss(const bf_matrix* logits, const bf_preference_args* args, float* d_stats,
+                              float* d_rewards, float* d_logprob, const bf_matrix* grad, void* d_workspace,
+                              uint64_t workspace_bytes, void* cuda_stream);
+BF_API int bf_preference_loss_workspace(uint64_t rows, uint64_t pairs, uint64_t* bytes);
+
+/* Token embedding: row t of `out` is scale * table[tokens[t]], 0 for a token
+ * below 0 and NaN for one >= table->rows.  `out` has one row per token and the
+ * table's width and type, and does not overlap it. */
+BF_API int bf_embed(const bf_matrix* table, const int64_t* d_tokens, float scale, const bf_matrix* out,
+                    void* cuda_stream);
+
+/* Its gradient: grad_table[v] = scale * sum over t with tokens[t] = v, in
+ * ascending t, of grad_out[t] (added to what grad_table holds with
+ * `accumulate`; else every row is written, 0 where no token occurs).  Tokens
+ * outside the table are left out.  The types may differ; the matrices do not
+ * overlap. */
+BF_API int bf_embed_grad(const bf_matrix* grad_out, const int64_t* d_tokens, float scale, uint32_t accumulate,
+                         const bf_matrix* grad_table, void* d_workspace, uint64_t workspace_bytes, void* cuda_stream);
+BF_API int bf_embed_grad_workspace(uint64_t rows, uint64_t width, uint64_t* bytes);
+
 /* Time limit of blocking waits, in milliseconds (default 600000; 0 = none).
  * Process-wide. */
 BF_API void bf_set_wait_timeout_ms(uint32_t ms);

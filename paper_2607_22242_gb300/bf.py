@@ -7,7 +7,9 @@ the C entry points without their ``bf_`` prefix: ``validate_desc``,
 ``create_scenario``, ``destroy_scenario``, ``eval_mappings``, ``search_best``,
 ``search_range``, ``search_batch``, ``search_batch_noalloc``, ``eval_indices``,
 ``whatif``, ``search_pruned``, ``set_wait_timeout_ms``, ``last_error``,
-``version``.
+``version``; and, for learning from the makespans of sampled mappings,
+``token_logprobs``, ``token_logprobs_grad``, ``policy_loss``,
+``preference_loss``, ``embed`` and ``embed_grad``.
 
 There is no CPU fallback: if ``libbf.so`` has not been built, or no CUDA
 device is present, these calls raise.
@@ -18,7 +20,7 @@ import ctypes
 import dataclasses
 import itertools
 import os
-from typing import List, Optional, Sequence, Tuple, Union
+from typing import List, NamedTuple, Optional, Sequence, Tuple, Union
 
 from .scenarios import MAX_TOOLS, Scenario
 
@@ -29,8 +31,10 @@ STATUS_NAMES = {0: "BF_OK", 1: "BF_EINVAL", 2: "BF_ERANGE", 3: "BF_ENOMEM", 4: "
 INFEASIBLE = 0xFFFFFFFF
 EXPORTED = ("bf_validate_desc", "bf_create_scenario", "bf_destroy_scenario", "bf_eval_mappings",
             "bf_search_best", "bf_search_range", "bf_search_batch", "bf_search_batch_noalloc",
-            "bf_eval_indices", "bf_whatif", "bf_search_pruned", "bf_search_tree", "bf_set_wait_timeout_ms",
-            "bf_last_error", "bf_version")
+            "bf_eval_indices", "bf_whatif", "bf_search_pruned", "bf_search_tree", "bf_token_logprobs",
+            "bf_token_logprobs_grad", "bf_policy_loss", "bf_policy_loss_workspace", "bf_preference_loss",
+            "bf_preference_loss_workspace", "bf_embed", "bf_embed_grad", "bf_embed_grad_workspace",
+            "bf_set_wait_timeout_ms", "bf_last_error", "bf_version")
 SPACE_BINARY, SPACE_FULL = 2, 3
 TREE_NO_PRUNE = 1
 MAX_PROBES = 2 * MAX_TOOLS + MAX_TOOLS * MAX_TOOLS
@@ -87,6 +91,29 @@ class CTreeStats(ctypes.Structure):
                 ("pad", ctypes.c_uint32)]
 
 
+class Matrix(ctypes.Structure):
+    """``bf_matrix``."""
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_uint64), ("cols", ctypes.c_uint64),
+                ("row_stride", ctypes.c_uint64), ("dtype", ctypes.c_uint32), ("pad", ctypes.c_uint32)]
+
+
+class PolicyArgs(ctypes.Structure):
+    """``bf_policy_args``."""
+    _fields_ = [("tokens", ctypes.c_void_p), ("offsets", ctypes.c_void_p), ("old_logprob", ctypes.c_void_p),
+                ("ref_logprob", ctypes.c_void_p), ("advantage", ctypes.c_void_p), ("sequences", ctypes.c_uint64),
+                ("advantage_per_token", ctypes.c_uint32), ("reduction", ctypes.c_uint32),
+                ("clip_low", ctypes.c_float), ("clip_high", ctypes.c_float), ("kl_coef", ctypes.c_float),
+                ("entropy_coef", ctypes.c_float), ("temperature", ctypes.c_float), ("grad_scale", ctypes.c_float)]
+
+
+class PreferenceArgs(ctypes.Structure):
+    """``bf_preference_args``."""
+    _fields_ = [("tokens", ctypes.c_void_p), ("offsets", ctypes.c_void_p), ("ref_logprob", ctypes.c_void_p),
+                ("pairs", ctypes.c_uint64), ("average", ctypes.c_uint32), ("beta", ctypes.c_float),
+                ("label_smoothing", ctypes.c_float), ("margin", ctypes.c_float), ("temperature", ctypes.c_float),
+                ("grad_scale", ctypes.c_float)]
+
+
 @dataclasses.dataclass
 class Result:
     index: int
@@ -119,9 +146,16 @@ def load(path: str = LIB_PATH):
     lib.bf_whatif.argtypes = [vp, u64, ctypes.POINTER(CProbe), u32, ctypes.POINTER(u32), vp]
     lib.bf_search_pruned.argtypes = [vp, u64, ctypes.POINTER(CResult), vp]
     lib.bf_search_tree.argtypes = [vp, u32, u32, u64, ctypes.POINTER(CResult), ctypes.POINTER(CTreeStats), vp]
-    for name in ("bf_validate_desc", "bf_create_scenario", "bf_destroy_scenario", "bf_eval_mappings",
-                 "bf_search_best", "bf_search_range", "bf_search_batch", "bf_search_batch_noalloc",
-                 "bf_eval_indices", "bf_whatif", "bf_search_pruned", "bf_search_tree"):
+    mat, f32 = ctypes.POINTER(Matrix), ctypes.c_float
+    lib.bf_token_logprobs.argtypes = [mat, vp, f32, vp, vp, vp]
+    lib.bf_token_logprobs_grad.argtypes = [mat, vp, f32, vp, vp, mat, vp]
+    lib.bf_policy_loss.argtypes = [mat, ctypes.POINTER(PolicyArgs), vp, vp, mat, vp, u64, vp]
+    lib.bf_preference_loss.argtypes = [mat, ctypes.POINTER(PreferenceArgs), vp, vp, vp, mat, vp, u64, vp]
+    lib.bf_embed.argtypes = [mat, vp, f32, mat, vp]
+    lib.bf_embed_grad.argtypes = [mat, vp, f32, u32, mat, vp, u64, vp]
+    for name in ("bf_policy_loss_workspace", "bf_preference_loss_workspace", "bf_embed_grad_workspace"):
+        getattr(lib, name).argtypes = [u64, u64, ctypes.POINTER(u64)]
+    for name in EXPORTED:
         getattr(lib, name).restype = ctypes.c_int
     lib.bf_set_wait_timeout_ms.argtypes = [u32]
     lib.bf_set_wait_timeout_ms.restype = None
@@ -420,3 +454,203 @@ def search_tree(h: Union[ScenarioHandle, Scenario], space: int = SPACE_FULL, pru
     finally:
         if owned:
             handle.close()
+
+
+# ---- learning from makespans ----------------------------------------------------------------------------------------
+
+REDUCTIONS = {"tokens": 0, "sequences": 1, "sum": 2}
+POLICY_STATS, PREFERENCE_STATS = 6, 4
+
+
+class PolicyLoss(NamedTuple):
+    """``stats`` (POLICY_STATS float32: loss, surrogate term, KL, entropy, clipped share, mean ratio), the tokens'
+    log-probabilities and the gradient in the logits (None when not wanted)."""
+    stats: object
+    logprob: object
+    grad: object
+
+
+class PreferenceLoss(NamedTuple):
+    """``stats`` (PREFERENCE_STATS float32: loss, share of pairs ranked right, mean reward of the preferred and of the
+    other answers), the answers' rewards, the tokens' log-probabilities and the gradient in the logits (or None)."""
+    stats: object
+    rewards: object
+    logprob: object
+    grad: object
+
+
+def _dtype_code(dtype) -> Optional[int]:
+    import torch
+    return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(dtype)
+
+
+def _matrix(t, name: str) -> Matrix:
+    """A 2-D CUDA tensor with contiguous rows (any row stride) on the current device as ``bf_matrix``."""
+    import torch
+    code = _dtype_code(t.dtype)
+    if code is None or not t.is_cuda or t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-D CUDA tensor of float32, bfloat16 or float16")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} is on device {t.get_device()} but device {torch.cuda.current_device()} is current")
+    rows, cols = t.shape
+    stride, inner = t.stride()
+    if inner != 1 and cols > 1 and rows:
+        raise ValueError(f"{name} must have contiguous rows")
+    return Matrix(t.data_ptr(), rows, cols, max(stride, cols) if rows <= 1 else stride, code, 0)
+
+
+def _vector(t, count: int, dtype, like, name: str) -> int:
+    """The address of a contiguous 1-D CUDA tensor of `count` elements beside `like`."""
+    if t.dtype != dtype or t.numel() != count or t.get_device() != like.get_device() or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {count} elements on {like.device}")
+    return t.data_ptr()
+
+
+def _allocate(stream):
+    """Context in which results and workspaces belong to `stream` for torch's allocator."""
+    import contextlib
+    import torch
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+
+
+def _workspace(query, rows: int, groups: int, device):
+    import torch
+    need = ctypes.c_uint64(0)
+    _check(query(rows, groups, ctypes.byref(need)))
+    return torch.empty(max(need.value, 1), dtype=torch.uint8, device=device)
+
+
+def _grad_like(logits, out, grad: bool):
+    """Where the gradient goes: nowhere, to `out` (it may be `logits`) or to a new tensor."""
+    import torch
+    if not grad:
+        return None
+    return torch.empty_like(logits, memory_format=torch.contiguous_format) if out is None else out
+
+
+def token_logprobs(logits, tokens, *, temperature: float = 1.0, entropy: bool = False, stream=None):
+    """Log-probabilities (float32) of `tokens` (int64, one per row; below 0: not scored) under `logits`
+    (rows x vocab; float32, bfloat16 or float16) -- with ``entropy``, the pair of them and the rows' entropies.
+    Asynchronous on ``stream``, as everything below."""
+    import torch
+    x = _matrix(logits, "logits")
+    y = _vector(tokens, x.rows, torch.int64, logits, "tokens")
+    with _allocate(stream):
+        logprob = torch.empty(x.rows, dtype=torch.float32, device=logits.device)
+        h = torch.empty_like(logprob) if entropy else None
+    _check(load().bf_token_logprobs(x, y, temperature, logprob.data_ptr(), h.data_ptr() if entropy else None,
+                                    _stream_handle(stream)))
+    return (logprob, h) if entropy else logprob
+
+
+def token_logprobs_grad(logits, tokens, grad_logprob, grad_entropy=None, *, temperature: float = 1.0, out=None,
+                        stream=None):
+    """The gradient in `logits` of sum(grad_logprob * logprob + grad_entropy * entropy).  `out` may be `logits`."""
+    import torch
+    x = _matrix(logits, "logits")
+    y = _vector(tokens, x.rows, torch.int64, logits, "tokens")
+    gl = _vector(grad_logprob, x.rows, torch.float32, logits, "grad_logprob")
+    gh = None if grad_entropy is None else _vector(grad_entropy, x.rows, torch.float32, logits, "grad_entropy")
+    with _allocate(stream):
+        grad = _grad_like(logits, out, True)
+    _check(load().bf_token_logprobs_grad(x, y, temperature, gl, gh, _matrix(grad, "out"), _stream_handle(stream)))
+    return grad
+
+
+def policy_loss(logits, tokens, offsets, old_logprob, advantage, ref_logprob=None, *, clip_low: float = 0.2,
+                clip_high: float = 0.2, kl_coef: float = 0.0, entropy_coef: float = 0.0, temperature: float = 1.0,
+                reduction: str = "tokens", advantage_per_token: bool = False, grad_scale: float = 1.0,
+                grad: bool = True, out=None, stream=None) -> PolicyLoss:
+    """The clipped policy loss with a KL term over the sequences that `offsets` (int64, sequences + 1) cuts the rows
+    into, and its gradient in the logits (times `grad_scale`).  `advantage` holds one value per sequence, or one per row
+    with `advantage_per_token`.  ``reduction``: "tokens", "sequences" or "sum".  `out` may be `logits`: the gradient
+    then replaces them."""
+    import torch
+    x = _matrix(logits, "logits")
+    rows, sequences = x.rows, offsets.numel() - 1
+    if sequences < 0:
+        raise ValueError("offsets must hold one element more than there are sequences")
+    if reduction not in REDUCTIONS:
+        raise ValueError(f"reduction must be one of {', '.join(REDUCTIONS)}")
+    f32 = torch.float32
+    args = PolicyArgs(_vector(tokens, rows, torch.int64, logits, "tokens"),
+                      _vector(offsets, sequences + 1, torch.int64, logits, "offsets"),
+                      _vector(old_logprob, rows, f32, logits, "old_logprob"),
+                      None if ref_logprob is None else _vector(ref_logprob, rows, f32, logits, "ref_logprob"),
+                      _vector(advantage, rows if advantage_per_token else sequences, f32, logits, "advantage"),
+                      sequences, bool(advantage_per_token), REDUCTIONS[reduction], clip_low, clip_high, kl_coef, entropy_coef, temperature,
+                      grad_scale)
+    lib = load()
+    with _allocate(stream):
+        g = _grad_like(logits, out, grad)
+        stats = torch.empty(POLICY_STATS, dtype=f32, device=logits.device)
+        logprob = torch.empty(rows, dtype=f32, device=logits.device)
+        work = _workspace(lib.bf_policy_loss_workspace, rows, sequences, logits.device)
+    _check(lib.bf_policy_loss(x, args, stats.data_ptr(), logprob.data_ptr(), None if g is None else _matrix(g, "out"),
+                              work.data_ptr(), work.numel(), _stream_handle(stream)))
+    return PolicyLoss(stats, logprob, g)
+
+
+def preference_loss(logits, tokens, offsets, ref_logprob=None, *, beta: float = 0.1, label_smoothing: float = 0.0,
+                    margin: float = 0.0, average: bool = False, temperature: float = 1.0, grad_scale: float = 1.0,
+                    grad: bool = True, out=None, stream=None) -> PreferenceLoss:
+    """The preference loss over pairs of answers (sequence 2p of `offsets` is preferred to 2p + 1) and its gradient in
+    the logits (times `grad_scale`).  `out` may be `logits`: the gradient then replaces them."""
+    import torch
+    x = _matrix(logits, "logits")
+    rows, pairs = x.rows, offsets.numel() // 2
+    if offsets.numel() % 2 == 0:
+        raise ValueError("offsets must hold 2 * pairs + 1 elements")
+    f32 = torch.float32
+    args = PreferenceArgs(_vector(tokens, rows, torch.int64, logits, "tokens"),
+                          _vector(offsets, 2 * pairs + 1, torch.int64, logits, "offsets"),
+                          None if ref_logprob is None else _vector(ref_logprob, rows, f32, logits, "ref_logprob"),
+                          pairs, bool(average), beta, label_smoothing, margin, temperature, grad_scale)
+    lib = load()
+    with _allocate(stream):
+        g = _grad_like(logits, out, grad)
+        stats = torch.empty(PREFERENCE_STATS, dtype=f32, device=logits.device)
+        rewards = torch.empty(2 * pairs, dtype=f32, device=logits.device)
+        logprob = torch.empty(rows, dtype=f32, device=logits.device)
+        work = _workspace(lib.bf_preference_loss_workspace, rows, pairs, logits.device)
+    _check(lib.bf_preference_loss(x, args, stats.data_ptr(), rewards.data_ptr(), logprob.data_ptr(),
+                                  None if g is None else _matrix(g, "out"), work.data_ptr(), work.numel(),
+                                  _stream_handle(stream)))
+    return PreferenceLoss(stats, rewards, logprob, g)
+
+
+def embed(table, tokens, *, scale: float = 1.0, out=None, stream=None):
+    """Rows scale * table[tokens] (zeros for a token below 0), one per token of the 1-D int64 tensor."""
+    import torch
+    w = _matrix(table, "table")
+    y = _vector(tokens, tokens.numel(), torch.int64, table, "tokens")
+    with _allocate(stream):
+        if out is None:
+            out = torch.empty(tokens.numel(), w.cols, dtype=table.dtype, device=table.device)
+    o = _matrix(out, "out")
+    if o.rows != tokens.numel():
+        raise ValueError("out must have one row per token")
+    _check(load().bf_embed(w, y, scale, o, _stream_handle(stream)))
+    return out
+
+
+def embed_grad(grad_out, tokens, vocab: int, *, scale: float = 1.0, out=None, accumulate: bool = False, stream=None):
+    """The gradient of :func:`embed` in its table (vocab x width): scale * the sums of `grad_out`'s rows by token, of
+    grad_out's type or in `out` (any of the types); with ``accumulate`` added to what `out` holds."""
+    import torch
+    g = _matrix(grad_out, "grad_out")
+    y = _vector(tokens, g.rows, torch.int64, grad_out, "tokens")
+    if accumulate and out is None:
+        raise ValueError("accumulate needs out")
+    lib = load()
+    with _allocate(stream):
+        if out is None:
+            out = torch.empty(vocab, g.cols, dtype=grad_out.dtype, device=grad_out.device)
+        work = _workspace(lib.bf_embed_grad_workspace, g.rows, g.cols, grad_out.device)
+    o = _matrix(out, "out")
+    if o.rows != vocab:
+        raise ValueError("out must have one row per token of the vocabulary")
+    _check(lib.bf_embed_grad(g, y, scale, accumulate, o, work.data_ptr(), work.numel(), _stream_handle(stream)))
+    return out

@@ -1,0 +1,163 @@
+// bf_rows.cuh -- the arithmetic of one row of logits, shared by the kernels in
+// bf_rows.cu.
+//
+// With x the row's logits, y its token and tau the temperature:
+//   m = max_j x_j,  t_j = (x_j - m) log2(e) / tau,  e_j = 2^t_j,  s = sum_j e_j,  q = sum_j e_j t_j
+//   log-probability  lp = (x_y - m) / tau - ln s
+//   entropy          H  = ln s - ln2 q / s
+// and for a loss with slopes A = dL/dlp and C = dL/dH of this row,
+//   dL/dx_j = e_j (B + D t_j) + [j = y] A / tau
+//   B = -(A + C (H - ln s)) / (tau s),  D = -C ln2 / (tau s).
+// x - m is taken before the product with log2(e)/tau: a row of the type's
+// lowest values would overflow in x log2(e)/tau, and here has m among them.
+#pragma once
+
+#include "bf_elem.cuh"
+#include "bf_learn.h"
+
+namespace bfk {
+
+constexpr float kLn2 = 0.693147180559945309f;
+constexpr float kMinusInf = -__builtin_huge_valf();
+
+__device__ __forceinline__ float exp2_fast(float t) {
+  float e;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
+  return e;
+}
+
+// Maximum, sum and first moment of the exponentials of some of a row's logits.
+// m is -inf, s and q are 0 where there is no logit above -inf.
+struct RowSums {
+  float m, s, q;
+};
+
+// t as a factor beside e = 2^t: where e is 0, a finite one (0 * -inf would be NaN).
+__device__ __forceinline__ float finite_t(float t) { return fmaxf(t, -160.0f); }
+
+// The max that exponents are taken against: 0 in a row without a logit above -inf.
+__device__ __forceinline__ float usable_max(float m) { return m == kMinusInf ? 0.0f : m; }
+
+__device__ __forceinline__ RowSums join(const RowSums& a, const RowSums& b, float c2) {
+  const float m = fmaxf(a.m, b.m), ref = usable_max(m);
+  const float ta = (a.m - ref) * c2, tb = (b.m - ref) * c2;
+  const float ea = exp2_fast(ta), eb = exp2_fast(tb);
+  return {m, ea * a.s + eb * b.s, ea * (a.q + finite_t(ta) * a.s) + eb * (b.q + finite_t(tb) * b.s)};
+}
+
+// What a row brings besides its logits.
+struct RowIn {
+  bool on;          // scored
+  bool known;       // its token is inside the vocabulary
+  uint32_t y;
+  float xy;         // its token's logit
+  float w;          // kPolicy: its weight in the loss
+  float old_lp, ref_lp, adv;
+  float slope_lp, slope_h;  // kScoreGrad; slope_lp also kPairGrad
+};
+
+// What its gradient is made from, and its terms of the loss.
+struct RowOut {
+  float m;          // usable max
+  float b, d, hit;  // dL/dx_j = e_j (b + d t_j), plus hit at the token
+  float sums[kPolicySums];
+};
+
+template <typename E, RowOp op>
+__device__ __forceinline__ RowIn load_row(const RowArgs& a, uint64_t row) {
+  RowIn in = {};
+  const int64_t y = a.tokens[row];
+  in.on = y >= 0;
+  in.known = y < (int64_t)a.vocab;
+  in.y = (uint32_t)y;
+  if constexpr (op == RowOp::kPolicy || op == RowOp::kPairScore || op == RowOp::kPairGrad) {
+    const uint32_t seq = a.row_seq[row];
+    in.on = seq != kNoSequence;
+    if constexpr (op == RowOp::kPolicy) {
+      if (in.on) {
+        const uint32_t n = a.seq_tokens[seq];
+        in.w = a.reduction == BF_MEAN_TOKENS ? 1.0f / (float)a.counts->tokens
+               : a.reduction == BF_MEAN_SEQUENCES ? 1.0f / ((float)n * (float)a.counts->sequences) : 1.0f;
+        in.old_lp = a.old_logprob[row];
+        in.adv = a.advantage[a.advantage_per_token ? row : seq];
+        if (a.ref_logprob) in.ref_lp = a.ref_logprob[row];
+      }
+    }
+    if constexpr (op == RowOp::kPairGrad) {
+      if (in.on) in.slope_lp = a.seq_slope[seq];
+    }
+  }
+  if constexpr (op == RowOp::kScoreGrad) {
+    in.slope_lp = a.grad_logprob[row];
+    if (a.grad_entropy) in.slope_h = a.grad_entropy[row];
+  }
+  if (in.on && in.known) in.xy = to_f32(static_cast<const E*>(a.x)[row * a.ldx + in.y]);
+  return in;
+}
+
+// The row's outputs from its sums (written by the caller's leading thread) and
+// its gradient's factors.  A row without a logit above -inf has log-probability
+// -inf, entropy 0, loss term 0 and gradient 0; a token outside the vocabulary
+// makes its row's values NaN.
+template <RowOp op>
+__device__ __forceinline__ RowOut finish_row(const RowArgs& a, uint64_t row, const RowIn& in, const RowSums& r,
+                                             bool leader) {
+  RowOut o = {};
+  if (!in.on) {
+    if (leader) {
+      if (a.logprob) a.logprob[row] = 0.0f;
+      if (a.entropy) a.entropy[row] = 0.0f;
+    }
+    return o;
+  }
+  const bool none = r.s == 0.0f;
+  o.m = usable_max(r.m);
+  const float ln_s = logf(r.s), inv_s = none ? 0.0f : 1.0f / r.s;
+  float lp = none ? kMinusInf : (in.xy - o.m) * a.inv_tau - ln_s;
+  const float h = none ? 0.0f : ln_s - kLn2 * r.q * inv_s;
+  if (!in.known) lp = __int_as_float(0x7FC00000);
+  if (leader) {
+    if (a.logprob) a.logprob[row] = lp;
+    if (a.entropy) a.entropy[row] = h;
+  }
+  if constexpr (op == RowOp::kPairScore) {
+    if (leader) a.row_softmax[row] = make_float2(o.m, inv_s);
+  }
+  if constexpr (op == RowOp::kScore || op == RowOp::kPairScore) return o;
+  if (none) return o;
+  float slope_lp = in.slope_lp, slope_h = in.slope_h;
+  if constexpr (op == RowOp::kPolicy) {
+    const float ratio = expf(lp - in.old_lp);
+    const bool clipped = in.adv >= 0.0f ? ratio > a.ratio_hi : ratio < a.ratio_lo;
+    const float held = clipped ? (in.adv >= 0.0f ? a.ratio_hi : a.ratio_lo) : ratio;
+    float kl = 0.0f;
+    slope_lp = clipped ? 0.0f : -in.adv * ratio;
+    if (a.ref_logprob) {
+      const float u = in.ref_lp - lp, em1 = expm1f(u);
+      kl = em1 - u;
+      slope_lp -= a.kl_coef * em1;
+    }
+    o.sums[0] = in.w * held * in.adv;
+    o.sums[1] = in.w * kl;
+    o.sums[2] = in.w * h;
+    o.sums[3] = clipped ? in.w : 0.0f;
+    o.sums[4] = in.w * ratio;
+    slope_lp *= in.w * a.grad_scale;
+    slope_h = -a.entropy_coef * in.w * a.grad_scale;
+  }
+  if constexpr (op == RowOp::kPairGrad) {
+    if (!in.known) slope_lp = lp;
+  }
+  o.b = -(slope_lp + slope_h * (h - ln_s)) * a.inv_tau * inv_s;
+  o.d = -slope_h * kLn2 * a.inv_tau * inv_s;
+  o.hit = slope_lp * a.inv_tau;
+  return o;
+}
+
+// A logit's gradient, without the token's own part.
+__device__ __forceinline__ float logit_grad(const RowOut& o, float x, float c2) {
+  const float t = (x - o.m) * c2;
+  return exp2_fast(t) * fmaf(o.d, finite_t(t), o.b);
+}
+
+}  // namespace bfk
