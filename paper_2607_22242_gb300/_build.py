@@ -2,8 +2,8 @@
 
 Each window-width bucket of ``csrc/bf_kernels.cu`` is its own translation unit
 (``-DBF_NW=<slots>``); the units compile in parallel and link with ``bf_tree.cu``
-(the tree search and 32-slot index lists), ``bf_rows.cu`` and ``bf_embed.cu`` (learning from
-makespans), ``bf_capi.cu``, ``bf_capi_tree.cu`` and ``bf_capi_learn.cu`` into
+(the tree search and 32-slot index lists), ``bf_rows.cu`` (once per element type),
+``bf_answers.cu`` and ``bf_embed.cu`` (learning from makespans), ``bf_capi.cu``, ``bf_capi_tree.cu`` and ``bf_capi_learn.cu`` into
 ``paper_2607_22242_gb300/_build/libbf.so`` (CUDA runtime linked statically, so
 the library carries no path to a toolkit; no undefined symbol is allowed).
 """
@@ -97,10 +97,13 @@ def build(force: bool = False, extra_flags=(), verbose: bool = False) -> str:
         obj = os.path.join(BUILD_DIR, f"bf_kernels_nw{nt}.o")
         jobs.append([cc, *ARCH, *NVCC_FLAGS, *extra_flags, f"-DBF_NW={nt}", "-c",
                      os.path.join(CSRC, "bf_kernels.cu"), "-o", obj])
-    for unit in ("bf_tree", "bf_lanetree", "bf_segments", "bf_rows", "bf_embed", "bf_capi", "bf_capi_tree",
+    for unit in ("bf_tree", "bf_lanetree", "bf_segments", "bf_answers", "bf_embed", "bf_capi", "bf_capi_tree",
                  "bf_capi_learn"):
         jobs.append([cc, *ARCH, *NVCC_FLAGS, *extra_flags, "-c", os.path.join(CSRC, unit + ".cu"), "-o",
                      os.path.join(BUILD_DIR, unit + ".o")])
+    for code in range(3):
+        jobs.append([cc, *ARCH, *NVCC_FLAGS, *extra_flags, f"-DBF_ROWS_TYPE={code}", "-c",
+                     os.path.join(CSRC, "bf_rows.cu"), "-o", os.path.join(BUILD_DIR, f"bf_rows_type{code}.o")])
 
     def run(cmd):
         res = subprocess.run(cmd, capture_output=True, text=True)

@@ -50,7 +50,7 @@ struct RowArgs {
   uint32_t advantage_per_token;
   uint32_t reduction;  // bf_reduction
   float ratio_lo, ratio_hi, kl_coef, entropy_coef, grad_scale;
-  float* partial;  // kPolicy: kPolicySums rows of `rows` sums
+  float* partial;  // kPolicy: kPolicySums rows of sums, one for each row of logits at most
   float* stats;
   // kPairScore writes and kPairGrad reads what a row's probabilities are made from; kPairGrad's slope of each sequence
   float2* row_softmax;  // (max, 1 / sum)
@@ -77,7 +77,14 @@ struct PairArgs {
 // Which sequence each scored row belongs to, and how many there are: zeroes and fills row_seq, seq_tokens and counts.
 cudaError_t launch_row_sequences(const int64_t* tokens, uint64_t rows, const int64_t* offsets, uint64_t sequences,
                                  uint32_t* row_seq, uint32_t* seq_tokens, RowCounts* counts, cudaStream_t st);
-cudaError_t launch_rows(RowOp op, const RowArgs& a, cudaStream_t st);
+// One pass over rows of each element type (bf_rows.cu, compiled once per type).
+cudaError_t launch_rows_type0(RowOp op, const RowArgs& a, cudaStream_t st);
+cudaError_t launch_rows_type1(RowOp op, const RowArgs& a, cudaStream_t st);
+cudaError_t launch_rows_type2(RowOp op, const RowArgs& a, cudaStream_t st);
+inline cudaError_t launch_rows(RowOp op, const RowArgs& a, cudaStream_t st) {
+  return a.dtype == BF_F32 ? launch_rows_type0(op, a, st)
+         : a.dtype == BF_BF16 ? launch_rows_type1(op, a, st) : launch_rows_type2(op, a, st);
+}
 cudaError_t launch_pairs(const PairArgs& a, cudaStream_t st);
 
 struct EmbedArgs {

@@ -110,6 +110,14 @@ __device__ __forceinline__ RowOut finish_row(const RowArgs& a, uint64_t row, con
     }
     return o;
   }
+  if constexpr (op == RowOp::kPairGrad) {  // from what its scoring pass kept
+    const float2 kept = a.row_softmax[row];
+    const float slope = in.known ? in.slope_lp * a.inv_tau : __int_as_float(0x7FC00000);
+    o.m = kept.x;
+    o.b = -slope * kept.y;
+    o.hit = kept.y == 0.0f ? 0.0f : slope;
+    return o;
+  }
   const bool none = r.s == 0.0f;
   o.m = usable_max(r.m);
   const float ln_s = logf(r.s), inv_s = none ? 0.0f : 1.0f / r.s;
@@ -145,9 +153,6 @@ __device__ __forceinline__ RowOut finish_row(const RowArgs& a, uint64_t row, con
     slope_lp *= in.w * a.grad_scale;
     slope_h = -a.entropy_coef * in.w * a.grad_scale;
   }
-  if constexpr (op == RowOp::kPairGrad) {
-    if (!in.known) slope_lp = lp;
-  }
   o.b = -(slope_lp + slope_h * (h - ln_s)) * a.inv_tau * inv_s;
   o.d = -slope_h * kLn2 * a.inv_tau * inv_s;
   o.hit = slope_lp * a.inv_tau;
@@ -158,6 +163,43 @@ __device__ __forceinline__ RowOut finish_row(const RowArgs& a, uint64_t row, con
 __device__ __forceinline__ float logit_grad(const RowOut& o, float x, float c2) {
   const float t = (x - o.m) * c2;
   return exp2_fast(t) * fmaf(o.d, finite_t(t), o.b);
+}
+
+// The sums of `lanes` neighbouring lanes (a power of two) joined, in all of them.
+__device__ __forceinline__ RowSums lanes_join(RowSums r, float c2, uint32_t lanes) {
+  float m = r.m;
+  for (uint32_t o = lanes / 2; o; o /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+  const float t = (r.m - usable_max(m)) * c2, e = exp2_fast(t);
+  r = {m, e * r.s, e * (r.q + finite_t(t) * r.s)};
+  for (uint32_t o = lanes / 2; o; o /= 2) {
+    r.s += __shfl_xor_sync(~0u, r.s, o);
+    r.q += __shfl_xor_sync(~0u, r.q, o);
+  }
+  return r;
+}
+
+// Sum over the block's threads, in thread 0; every thread of the block calls it.  buf: a float per warp.
+__device__ __forceinline__ float block_sum(float v, float* buf) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+  __syncthreads();
+  if (threadIdx.x % 32 == 0) buf[threadIdx.x / 32] = v;
+  __syncthreads();
+  float sum = 0.0f;
+  if (threadIdx.x == 0)
+    for (uint32_t w = 0; w < blockDim.x / 32; ++w) sum += buf[w];
+  return sum;
+}
+
+// Whether this block is the last of `blocks` to get here; what the others wrote before is then visible.
+__device__ __forceinline__ bool last_block(uint32_t* done, uint32_t blocks) {
+  __shared__ bool last;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) last = atomicAdd(done, 1u) == blocks - 1;
+  __syncthreads();
+  if (last) __threadfence();
+  return last;
 }
 
 }  // namespace bfk
