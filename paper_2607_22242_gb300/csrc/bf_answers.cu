@@ -6,62 +6,156 @@ namespace bfk {
 
 namespace {
 
-constexpr uint32_t kRowThreads = 256;
-
-// The sequence whose rows [offsets[s], offsets[s+1]) contain `row`, or
-// kNoSequence.  Offsets that do not ascend make rows miss their sequence; no
-// read leaves the array.
-__device__ __forceinline__ uint32_t sequence_of(uint64_t row, const int64_t* offsets, uint64_t sequences) {
-  uint64_t lo = 0, hi = sequences;  // the last s with offsets[s] <= row lies in [lo, hi)
+// The last s in [0, sequences) with offsets[s] <= row, by halving [lo, hi).
+template <typename T, typename I>
+__device__ __forceinline__ I last_at_or_before(const T* offsets, I lo, I hi, T row) {
   while (hi - lo > 1) {
-    const uint64_t mid = (lo + hi) / 2;
-    if (offsets[mid] <= (int64_t)row) lo = mid;
+    const I mid = (lo + hi) / 2;
+    if (offsets[mid] <= row) lo = mid;
     else hi = mid;
   }
-  return offsets[lo] <= (int64_t)row && (int64_t)row < offsets[lo + 1] ? (uint32_t)lo : kNoSequence;
+  return lo;
 }
 
-// Counts are sums of whole numbers: their order does not matter.
+// Offsets that do not ascend make rows miss their sequence; no read leaves the
+// array.  Counts are sums of whole numbers: their order does not matter.
+
+// Up to kSmallRows rows of up to kSmallSequences sequences: one block, with the
+// offsets and the counts in shared memory (no memory to clear first, 3.5 us
+// where the kernel below and its memset take 7).
+constexpr uint32_t kSmallRows = 16384, kSmallSequences = 4096, kSmallThreads = 1024;
+
+__global__ void __launch_bounds__(kSmallThreads) small_sequence_kernel(const int64_t* tokens, uint32_t rows,
+                                                                       const int64_t* offsets, uint32_t sequences,
+                                                                       uint32_t* row_seq, uint32_t* seq_tokens,
+                                                                       RowCounts* counts) {
+  __shared__ uint32_t begin[kSmallSequences + 1], count[kSmallSequences];
+  __shared__ uint32_t all;
+  let_next_start();
+  if (threadIdx.x == 0) all = 0;
+  for (uint32_t s = threadIdx.x; s <= sequences; s += kSmallThreads) {
+    const int64_t o = offsets[s];
+    begin[s] = o < 0 ? 0u : o > (int64_t)rows ? rows : (uint32_t)o;
+    if (s < sequences) count[s] = 0;
+  }
+  __syncthreads();
+  for (uint32_t first = 0; first < rows; first += kSmallThreads) {
+    const uint32_t row = first + threadIdx.x;
+    uint32_t seq = kNoSequence;
+    if (row < rows) {
+      if (sequences && tokens[row] >= 0) {
+        const uint32_t s = last_at_or_before(begin, 0u, sequences, row);
+        if (begin[s] <= row && row < begin[s + 1]) seq = s;
+      }
+      row_seq[row] = seq;
+    }
+    const uint32_t same = __match_any_sync(~0u, seq);
+    if (seq != kNoSequence && threadIdx.x % 32 == (uint32_t)__ffs(same) - 1) {
+      atomicAdd(&count[seq], (uint32_t)__popc(same));
+      atomicAdd(&all, (uint32_t)__popc(same));
+    }
+  }
+  __syncthreads();
+  uint32_t used = 0;
+  for (uint32_t first = 0; first < sequences; first += kSmallThreads) {
+    const uint32_t s = first + threadIdx.x, n = s < sequences ? count[s] : 0;
+    if (s < sequences) seq_tokens[s] = n;
+    used += __syncthreads_count(n != 0);
+  }
+  if (threadIdx.x == 0) *counts = RowCounts{all, used, 0, 0};
+}
+
+// Any number: counts and seq_tokens are zero at the start.  A block's rows are
+// neighbours, so their sequences are too: one search for its first row by a
+// warp (32 probes at a time), then the offsets from there on in shared memory.
+constexpr uint32_t kRowThreads = 256;
+constexpr uint32_t kOffsets = 2 * kRowThreads;
+
 __global__ void __launch_bounds__(kRowThreads) sequence_kernel(const int64_t* tokens, uint64_t rows,
                                                                const int64_t* offsets, uint64_t sequences,
                                                                uint32_t* row_seq, uint32_t* seq_tokens,
-                                                               RowCounts* counts) {
-  const uint64_t row = (uint64_t)blockIdx.x * kRowThreads + threadIdx.x;
+                                                               RowCounts* counts, uint32_t per_sequence) {
+  __shared__ uint64_t first_seq;
+  __shared__ int64_t begin[kOffsets + 1];
+  let_next_start();
+  const uint64_t first = (uint64_t)blockIdx.x * kRowThreads, row = first + threadIdx.x;
+  const uint32_t lane = threadIdx.x % 32;
+  if (threadIdx.x < 32) {
+    uint64_t lo = 0, hi = sequences ? sequences : 1;
+    while (hi - lo > 1) {
+      const uint64_t step = (hi - lo + 31) / 32, at = lo + lane * step;
+      const uint32_t before = __ballot_sync(~0u, lane == 0 || (at < hi && offsets[at] <= (int64_t)first));
+      lo += (31 - __clz(before)) * step;
+      hi = min(hi, lo + step);
+    }
+    if (lane == 0) first_seq = lo;
+  }
+  __syncthreads();
+  const uint64_t s0 = first_seq;
+  const uint32_t held = (uint32_t)min((uint64_t)kOffsets, sequences - (sequences ? s0 : 0));
+  for (uint32_t i = threadIdx.x; i <= held; i += kRowThreads) begin[i] = offsets[s0 + i];
+  __syncthreads();
   uint32_t seq = kNoSequence;
   if (row < rows) {
-    if (sequences && tokens[row] >= 0) seq = sequence_of(row, offsets, sequences);
+    if (sequences && tokens[row] >= 0) {
+      const uint32_t i = last_at_or_before(begin, 0u, held + 1, (int64_t)row);
+      if (i < held) {
+        if (begin[i] <= (int64_t)row) seq = (uint32_t)(s0 + i);
+      } else if (s0 + held < sequences) {  // many empty sequences: beyond those held
+        const uint64_t s = last_at_or_before(offsets, s0 + held, sequences, (int64_t)row);
+        if (offsets[s] <= (int64_t)row && (int64_t)row < offsets[s + 1]) seq = (uint32_t)s;
+      }
+    }
     row_seq[row] = seq;
   }
-  const uint32_t same = __match_any_sync(~0u, seq), scored = __ballot_sync(~0u, seq != kNoSequence);
-  const uint32_t lane = threadIdx.x % 32;
-  if (seq != kNoSequence && lane == (uint32_t)__ffs(same) - 1) {
-    if (atomicAdd(&seq_tokens[seq], (uint32_t)__popc(same)) == 0u) atomicAdd(&counts->sequences, 1u);
+  bool opens = false;
+  if (per_sequence) {
+    const uint32_t same = __match_any_sync(~0u, seq);
+    opens = seq != kNoSequence && lane == (uint32_t)__ffs(same) - 1 &&
+            atomicAdd(&seq_tokens[seq], (uint32_t)__popc(same)) == 0u;
   }
-  if (lane == 0 && scored) atomicAdd(&counts->tokens, (uint32_t)__popc(scored));
+  const uint32_t scored = __syncthreads_count(seq != kNoSequence), opened = __syncthreads_count(opens);
+  if (threadIdx.x == 0) {
+    if (scored) atomicAdd(&counts->tokens, scored);
+    if (opened) atomicAdd(&counts->sequences, opened);
+  }
 }
 
-// One block per pair: the rewards beta * sum (lp - ref) of both answers (or of
-// their means), the loss of their gap
+// One block per pair, half of it per answer: the rewards beta * sum (lp - ref)
+// of both answers (or of their means), the loss of their gap
 //   h = reward_0 - reward_1 - margin,  l = -(1 - eps) ln sigma(h) - eps ln sigma(-h)
 // and the slopes of the mean loss in each answer's log-probabilities.
-__global__ void __launch_bounds__(kRowThreads) pair_kernel(const PairArgs a) {
-  __shared__ float buf[kRowThreads / 32];
+constexpr uint32_t kPairThreads = 512;
+
+__global__ void __launch_bounds__(kPairThreads) pair_kernel(const PairArgs a) {
+  __shared__ float buf[kPairThreads / 32 * 4];
+  __shared__ float sum[2];
+  let_next_start();
+  wait_for_previous();
+  const uint32_t half = threadIdx.x / (kPairThreads / 2), lane = threadIdx.x % (kPairThreads / 2);
   for (uint64_t p = blockIdx.x; p < a.pairs; p += gridDim.x) {
-    float sum[2];
-    for (uint32_t k = 0; k < 2; ++k) {
-      const uint64_t seq = 2 * p + k;
-      const int64_t lo = a.offsets[seq], hi = a.offsets[seq + 1];
-      const uint64_t begin = lo > 0 ? (uint64_t)lo : 0, end = hi > 0 ? min((uint64_t)hi, a.rows) : 0;
-      float v = 0.0f;
-      for (uint64_t row = begin + threadIdx.x; row < end; row += kRowThreads)
-        if (a.row_seq[row] == (uint32_t)seq) v += a.logprob[row] - (a.ref_logprob ? a.ref_logprob[row] : 0.0f);
-      sum[k] = block_sum(v, buf);
+    const uint64_t seq = 2 * p + half;
+    const int64_t lo = a.offsets[seq], hi = a.offsets[seq + 1];
+    const uint64_t begin = lo > 0 ? (uint64_t)lo : 0, end = hi > 0 ? min((uint64_t)hi, a.rows) : 0;
+    float v = 0.0f;
+    for (uint64_t row = begin + lane; row < end; row += kPairThreads / 2)
+      if (a.row_seq[row] == (uint32_t)seq) v += a.logprob[row] - (a.ref_logprob ? a.ref_logprob[row] : 0.0f);
+#pragma unroll
+    for (int o = 16; o; o /= 2) v += __shfl_xor_sync(~0u, v, o);
+    __syncthreads();
+    if (threadIdx.x % 32 == 0) buf[threadIdx.x / 32] = v;
+    __syncthreads();
+    if (lane == 0) {
+      float total = 0.0f;
+      for (uint32_t w = 0; w < kPairThreads / 64; ++w) total += buf[half * (kPairThreads / 64) + w];
+      sum[half] = total;
     }
+    __syncthreads();
     if (threadIdx.x == 0) {
       float share[2], reward[2];
       for (uint32_t k = 0; k < 2; ++k) {
-        const uint32_t n = a.seq_tokens[2 * p + k];
-        share[k] = a.beta * (a.average && n ? 1.0f / (float)n : 1.0f);
+        const uint32_t n = a.average ? a.seq_tokens[2 * p + k] : 0;
+        share[k] = a.beta * (n ? 1.0f / (float)n : 1.0f);
         reward[k] = share[k] * sum[k];
         a.rewards[2 * p + k] = reward[k];
       }
@@ -74,38 +168,52 @@ __global__ void __launch_bounds__(kRowThreads) pair_kernel(const PairArgs a) {
       a.partial[p] = loss;
     }
   }
-  if (last_block(&a.counts->blocks_done, gridDim.x)) {
+  bool last = false;
+  if (threadIdx.x < 32) last = last_to_say(&a.counts->blocks_done, gridDim.x);
+  if (__syncthreads_or(last)) {
+    last_sees();
     float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (uint64_t p = threadIdx.x; p < a.pairs; p += kRowThreads) {
+    for (uint64_t p = threadIdx.x; p < a.pairs; p += kPairThreads) {
       const float r0 = __ldcg(a.rewards + 2 * p), r1 = __ldcg(a.rewards + 2 * p + 1);
       v[0] += __ldcg(a.partial + p);
       v[1] += r0 > r1 ? 1.0f : 0.0f;
       v[2] += r0;
       v[3] += r1;
     }
-    for (uint32_t k = 0; k < 4; ++k) {
-      const float total = block_sum(v[k], buf);
-      if (threadIdx.x == 0) a.stats[k] = total / (float)a.pairs;
-    }
+    const float total = block_sums(v, buf);
+    if (threadIdx.x < 4) a.stats[threadIdx.x] = total / (float)a.pairs;
   }
 }
 
 }  // namespace
 
 cudaError_t launch_row_sequences(const int64_t* tokens, uint64_t rows, const int64_t* offsets, uint64_t sequences,
-                                 uint32_t* row_seq, uint32_t* seq_tokens, RowCounts* counts, cudaStream_t st) {
+                                 bool per_sequence, uint32_t* row_seq, uint32_t* seq_tokens, RowCounts* counts,
+                                 cudaStream_t st) {
+  if (rows <= kSmallRows && sequences <= kSmallSequences) {
+    small_sequence_kernel<<<1, kSmallThreads, 0, st>>>(tokens, (uint32_t)rows, offsets, (uint32_t)sequences, row_seq,
+                                                      seq_tokens, counts);
+    return cudaGetLastError();
+  }
   // counts and seq_tokens stand side by side (bf_capi_learn.cu)
-  cudaError_t e = cudaMemsetAsync(counts, 0, sizeof(RowCounts) + sizeof(uint32_t) * sequences, st);
+  cudaError_t e = cudaMemsetAsync(counts, 0, sizeof(RowCounts) + (per_sequence ? sizeof(uint32_t) * sequences : 0), st);
   if (e != cudaSuccess) return e;
   sequence_kernel<<<(uint32_t)((rows + kRowThreads - 1) / kRowThreads), kRowThreads, 0, st>>>(
-      tokens, rows, offsets, sequences, row_seq, seq_tokens, counts);
+      tokens, rows, offsets, sequences, row_seq, seq_tokens, counts, per_sequence);
   return cudaGetLastError();
 }
 
 cudaError_t launch_pairs(const PairArgs& a, cudaStream_t st) {
-  const uint32_t grid = (uint32_t)(a.pairs < (1u << 30) ? a.pairs : (1u << 30));
-  pair_kernel<<<grid, kRowThreads, 0, st>>>(a);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((uint32_t)(a.pairs < (1u << 30) ? a.pairs : (1u << 30)));
+  cfg.blockDim = dim3(kPairThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, pair_kernel, a);
 }
 
 }  // namespace bfk

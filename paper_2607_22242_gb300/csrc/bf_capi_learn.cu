@@ -231,8 +231,8 @@ int bf_policy_loss(const bf_matrix* logits, const bf_policy_args* args, float* d
   a.grad_scale = args->grad_scale;
   a.partial = ws.partial;
   a.stats = d_stats;
-  cudaError_t e = bfk::launch_row_sequences(args->tokens, rows, args->offsets, sequences, ws.row_seq, ws.seq_tokens,
-                                            ws.counts, st);
+  cudaError_t e = bfk::launch_row_sequences(args->tokens, rows, args->offsets, sequences,
+                                            args->reduction == BF_MEAN_SEQUENCES, ws.row_seq, ws.seq_tokens, ws.counts, st);
   if (e == cudaSuccess) e = bfk::launch_rows(RowOp::kPolicy, a, st);
   return e == cudaSuccess ? BF_OK : cuda_fail(e, who);
 }
@@ -273,7 +273,8 @@ int bf_preference_loss(const bf_matrix* logits, const bf_preference_args* args, 
     a.logprob = d_logprob ? d_logprob : ws.logprob;
     a.row_seq = ws.row_seq;
     a.row_softmax = ws.row_softmax;
-    e = bfk::launch_row_sequences(args->tokens, rows, args->offsets, 2 * pairs, ws.row_seq, ws.seq_tokens, ws.counts, st);
+    e = bfk::launch_row_sequences(args->tokens, rows, args->offsets, 2 * pairs, args->average != 0, ws.row_seq,
+                                  ws.seq_tokens, ws.counts, st);
     if (e == cudaSuccess) e = bfk::launch_rows(RowOp::kPairScore, a, st);
   } else {
     e = cudaMemsetAsync(ws.counts, 0, sizeof(RowCounts) + 8 * pairs, st);

@@ -31,94 +31,135 @@ __device__ __forceinline__ uint32_t minus_inf_bits(float) { return 0xFF800000u; 
 __device__ __forceinline__ uint32_t minus_inf_bits(__nv_bfloat16) { return 0xFF80FF80u; }
 __device__ __forceinline__ uint32_t minus_inf_bits(__half) { return 0xFC00FC00u; }
 
-__device__ __forceinline__ void unpack(uint32_t u, float, float* f) { f[0] = __uint_as_float(u); }
-__device__ __forceinline__ void unpack(uint32_t u, __nv_bfloat16, float* f) {
-  f[0] = __uint_as_float(u << 16);
-  f[1] = __uint_as_float(u & 0xFFFF0000u);
+__device__ __forceinline__ float2 unpack2(uint32_t u, __nv_bfloat16) {
+  return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
 }
-__device__ __forceinline__ void unpack(uint32_t u, __half, float* f) {
-  const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&u));
-  f[0] = v.x;
-  f[1] = v.y;
+__device__ __forceinline__ float2 unpack2(uint32_t u, __half) {
+  return __half22float2(*reinterpret_cast<const __half2*>(&u));
 }
-
-__device__ __forceinline__ uint32_t pack(const float* f, float) { return __float_as_uint(f[0]); }
-__device__ __forceinline__ uint32_t pack(const float* f, __nv_bfloat16) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(f[0], f[1]);
+__device__ __forceinline__ uint32_t pack2(float2 f, __nv_bfloat16) {
+  const __nv_bfloat162 v = __float22bfloat162_rn(f);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ uint32_t pack(const float* f, __half) {
-  const __half2 v = __floats2half2_rn(f[0], f[1]);
+__device__ __forceinline__ uint32_t pack2(float2 f, __half) {
+  const __half2 v = __float22half2_rn(f);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
+// A vector's elements in pairs.
 template <typename E>
-__device__ __forceinline__ void unpack(const uint4& u, float* f) {
-  constexpr int n = 4 / sizeof(E);
-  unpack(u.x, E(), f);
-  unpack(u.y, E(), f + n);
-  unpack(u.z, E(), f + 2 * n);
-  unpack(u.w, E(), f + 3 * n);
+__device__ __forceinline__ void unpack(const uint4& u, float2* f) {
+  if constexpr (sizeof(E) == 4) {
+    f[0] = make_float2(__uint_as_float(u.x), __uint_as_float(u.y));
+    f[1] = make_float2(__uint_as_float(u.z), __uint_as_float(u.w));
+  } else {
+    f[0] = unpack2(u.x, E());
+    f[1] = unpack2(u.y, E());
+    f[2] = unpack2(u.z, E());
+    f[3] = unpack2(u.w, E());
+  }
 }
 template <typename E>
-__device__ __forceinline__ uint4 pack(const float* f) {
-  constexpr int n = 4 / sizeof(E);
-  return make_uint4(pack(f, E()), pack(f + n, E()), pack(f + 2 * n, E()), pack(f + 3 * n, E()));
+__device__ __forceinline__ uint4 pack(const float2* f) {
+  if constexpr (sizeof(E) == 4)
+    return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y));
+  else
+    return make_uint4(pack2(f[0], E()), pack2(f[1], E()), pack2(f[2], E()), pack2(f[3], E()));
+}
+
+// The largest element of N vectors that is a number (-inf if none is).
+__device__ __forceinline__ float max_words(const uint32_t* u, int n, float) {
+  float m = -__builtin_huge_valf();
+#pragma unroll
+  for (int i = 0; i < n; ++i) m = fmaxf(m, __uint_as_float(u[i]));
+  return m;
+}
+template <typename E2>
+__device__ __forceinline__ E2 max_pairs(const uint32_t* u, int n, uint32_t least) {
+  E2 m = *reinterpret_cast<const E2*>(&least);
+#pragma unroll
+  for (int i = 0; i < n; ++i) m = __hmax2(m, *reinterpret_cast<const E2*>(&u[i]));
+  return m;
+}
+__device__ __forceinline__ float max_words(const uint32_t* u, int n, __nv_bfloat16) {
+  const float2 m = __bfloat1622float2(max_pairs<__nv_bfloat162>(u, n, 0xFF80FF80u));
+  return fmaxf(m.x, m.y);
+}
+__device__ __forceinline__ float max_words(const uint32_t* u, int n, __half) {
+  const float2 m = __half22float2(max_pairs<__half2>(u, n, 0xFC00FC00u));
+  return fmaxf(m.x, m.y);
+}
+template <typename E, int N>
+__device__ __forceinline__ float max_of(const uint4* u) {
+  return max_words(reinterpret_cast<const uint32_t*>(u), 4 * N, E());
+}
+
+// The elements of one vector that lie inside [lo, hi), -inf elsewhere: for the
+// ends of a row, which are read and written element by element.  Kept out of
+// line: a row has two such vectors, and their code would be in every unrolled
+// load and store (the kernels stalled for instructions a fifth of the time).
+template <typename E>
+__device__ __noinline__ uint4 load_ends(const E* p, int32_t lo, int32_t hi) {
+  constexpr int n = Vec<E>::kWidth;
+  uint32_t b[n];
+#pragma unroll
+  for (int i = 0; i < n; ++i) {
+    b[i] = minus_inf_bits(E());
+    if (i >= lo && i < hi) {
+      if constexpr (sizeof(E) == 4) b[i] = reinterpret_cast<const uint32_t*>(p)[i];
+      else b[i] = reinterpret_cast<const uint16_t*>(p)[i];
+    }
+  }
+  if constexpr (sizeof(E) == 4) return make_uint4(b[0], b[1], b[2], b[3]);
+  else
+    return make_uint4(__byte_perm(b[0], b[1], 0x5410), __byte_perm(b[2], b[3], 0x5410), __byte_perm(b[4], b[5], 0x5410),
+                      __byte_perm(b[6], b[7], 0x5410));
+}
+template <typename E>
+__device__ __noinline__ void store_ends(E* p, uint4 u, int32_t lo, int32_t hi) {
+  constexpr int n = Vec<E>::kWidth;
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < n; ++i)
+    if (i >= lo && i < hi) {
+      if constexpr (sizeof(E) == 4) reinterpret_cast<uint32_t*>(p)[i] = w[i];
+      else reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(w[i / 2] >> (i % 2 * 16));
+    }
 }
 
 // A row of elements as 16-byte vectors: vector v holds elements v * kWidth -
 // shift and on, where shift is how far the row starts behind a 16-byte
-// boundary.  The first and the last vector may reach outside the row: those are
-// read and written element by element.
+// boundary; vectors [lo, hi) lie in the row as a whole.
 template <typename E>
 struct Window {
-  E* row;
-  uint32_t shift, width, vectors;
   static constexpr uint32_t kWidth = Vec<E>::kWidth;
+  E* row;
+  uint32_t shift, end, lo, whole, vectors;
 
   __device__ __forceinline__ Window(E* p, uint32_t n)
-      : row(p), shift((uint32_t)((uintptr_t)p % 16) / sizeof(E)), width(n), vectors((shift + n + kWidth - 1) / kWidth) {}
+      : row(p), shift((uint32_t)((uintptr_t)p % 16) / sizeof(E)), end(shift + n), lo(shift ? 1 : 0),
+        whole(end / kWidth > lo ? end / kWidth - lo : 0), vectors((end + kWidth - 1) / kWidth) {}
 
-  __device__ __forceinline__ bool whole(uint32_t v) const {
-    return v * kWidth >= shift && (v + 1) * kWidth <= shift + width;
-  }
-  __device__ __forceinline__ uint4* at(uint32_t v) const {
-    return reinterpret_cast<uint4*>(row + ((int64_t)v * kWidth - shift));
-  }
-  // Vector v, with -inf outside the row.
-  __device__ __forceinline__ uint4 load(uint32_t v) const {
-    if (whole(v)) return __ldcs(at(v));
+  // Where vector v starts; for a first vector that reaches before the row, before it.
+  __device__ __forceinline__ E* at(uint32_t v) const { return row + ((int64_t)v * kWidth - shift); }
+  // Vector v, with -inf outside the row; `last`: it will not be read again.
+  __device__ __forceinline__ uint4 load(uint32_t v, bool last) const {
+    const uint4* p = reinterpret_cast<const uint4*>(at(v));
+    if (v - lo < whole) return last ? __ldcs(p) : __ldcg(p);
     const uint32_t none = minus_inf_bits(E());
     uint4 u = make_uint4(none, none, none, none);
-    if (v < vectors) {
-      float f[kWidth];
-#pragma unroll
-      for (uint32_t i = 0; i < kWidth; ++i) {
-        const uint32_t j = v * kWidth + i;
-        f[i] = j >= shift && j < shift + width ? to_f32(row[j - shift]) : -__builtin_huge_valf();
-      }
-      u = pack<E>(f);
-    }
+    if (v < vectors) u = load_ends<E>(at(v), v ? 0 : (int32_t)shift, (int32_t)(end - v * kWidth));
     return u;
   }
-  __device__ __forceinline__ void store(uint32_t v, const float* f) const {
-    if (whole(v)) {
-      __stcs(at(v), pack<E>(f));
-    } else if (v < vectors) {
-#pragma unroll
-      for (uint32_t i = 0; i < kWidth; ++i) {
-        const uint32_t j = v * kWidth + i;
-        if (j >= shift && j < shift + width) row[j - shift] = from_f32<E>(f[i]);
-      }
-    }
+  __device__ __forceinline__ void store(uint32_t v, const uint4& u) const {
+    if (v - lo < whole) __stcs(reinterpret_cast<uint4*>(at(v)), u);
+    else if (v < vectors) store_ends<E>(at(v), u, v ? 0 : (int32_t)shift, (int32_t)(end - v * kWidth));
   }
   // As store, for values cut into vectors at another row's boundaries (`from` behind one).
-  __device__ __forceinline__ void store_cut(uint32_t v, uint32_t from, const float* f) const {
-#pragma unroll
-    for (uint32_t i = 0; i < kWidth; ++i) {
-      const uint32_t j = v * kWidth + i;
-      if (j >= from && j < from + width) row[j - from] = from_f32<E>(f[i]);
-    }
+  __device__ __forceinline__ void store_cut(uint32_t v, uint32_t from, const uint4& u) const {
+    const int64_t first = (int64_t)v * kWidth - from;
+    if (first < (int64_t)(end - shift))
+      store_ends<E>(row + first, u, v ? 0 : (int32_t)from, (int32_t)min((int64_t)kWidth, (int64_t)(end - shift) - first));
   }
 };
 

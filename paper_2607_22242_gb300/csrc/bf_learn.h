@@ -74,9 +74,11 @@ struct PairArgs {
   float* stats;
 };
 
-// Which sequence each scored row belongs to, and how many there are: zeroes and fills row_seq, seq_tokens and counts.
+// Which sequence each scored row belongs to, and how many there are: fills row_seq, counts and, with `per_sequence`,
+// seq_tokens.
 cudaError_t launch_row_sequences(const int64_t* tokens, uint64_t rows, const int64_t* offsets, uint64_t sequences,
-                                 uint32_t* row_seq, uint32_t* seq_tokens, RowCounts* counts, cudaStream_t st);
+                                 bool per_sequence, uint32_t* row_seq, uint32_t* seq_tokens, RowCounts* counts,
+                                 cudaStream_t st);
 // One pass over rows of each element type (bf_rows.cu, compiled once per type).
 cudaError_t launch_rows_type0(RowOp op, const RowArgs& a, cudaStream_t st);
 cudaError_t launch_rows_type1(RowOp op, const RowArgs& a, cudaStream_t st);

@@ -2,6 +2,8 @@
 // entropies, their gradient, the clipped policy loss and both passes of the
 // preference loss (arithmetic in bf_rows.cuh).  Compiled once per element type
 // (-DBF_ROWS_TYPE=<bf_dtype>).
+#include <type_traits>
+
 #include "bf_rows.cuh"
 
 #ifndef BF_ROWS_TYPE
@@ -21,162 +23,220 @@ using E = __half;
 #endif
 constexpr uint32_t kW = Vec<E>::kWidth;
 
+// `entropy` of a kernel: whether its scores need the rows' entropies, its
+// gradient a slope in them.  The policy loss always reports them.
+template <RowOp op, bool entropy>
+constexpr bool kMoment = op == RowOp::kPolicy || entropy;
+
 template <RowOp op>
 constexpr bool kScores = op == RowOp::kScore || op == RowOp::kPairScore;
 
 // The policy loss from its parts' sums, in an order that does not depend on when blocks ran.
 __device__ __forceinline__ void policy_stats(const RowArgs& a, uint64_t parts, float* buf) {
-  float total[kPolicySums];
-  for (uint32_t k = 0; k < kPolicySums; ++k) {
-    float v = 0.0f;
-    for (uint64_t i = threadIdx.x; i < parts; i += blockDim.x) v += __ldcg(a.partial + k * parts + i);
-    total[k] = block_sum(v, buf);
+  last_sees();
+  float v[kPolicySums] = {};
+  for (uint64_t i = threadIdx.x; i < parts; i += blockDim.x) {
+#pragma unroll
+    for (uint32_t k = 0; k < kPolicySums; ++k) v[k] += __ldcg(a.partial + k * parts + i);
   }
+  const float total = block_sums(v, buf);
+  const float surrogate = __shfl_sync(~0u, total, 0), kl = __shfl_sync(~0u, total, 1), h = __shfl_sync(~0u, total, 2);
   if (threadIdx.x == 0) {
-    a.stats[0] = -total[0] + a.kl_coef * total[1] - a.entropy_coef * total[2];
-    a.stats[1] = -total[0];
-    for (uint32_t k = 1; k < kPolicySums; ++k) a.stats[k + 1] = total[k];
+    a.stats[0] = -surrogate + a.kl_coef * kl - a.entropy_coef * h;
+    a.stats[1] = -surrogate;
+  } else if (threadIdx.x < kPolicySums) {
+    a.stats[threadIdx.x + 1] = total;
   }
 }
 
-// Sums of N values against their own maximum.
-template <int N>
-__device__ __forceinline__ RowSums sums_of(const float* x, float c2) {
-  RowSums r = {x[0], 0.0f, 0.0f};
-#pragma unroll
-  for (int i = 1; i < N; ++i) r.m = fmaxf(r.m, x[i]);
-  const float ref = usable_max(r.m);
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const float t = (x[i] - ref) * c2, e = exp2_fast(t);
-    r.s += e;
-    r.q = fmaf(e, finite_t(t), r.q);
-  }
-  return r;
-}
+// (x - m) c2 as (x - base) c2 - r: with base = 0 and r = m c2 rounded it is one
+// product and sum, and what r is off by (`rest`) goes into the factors once per
+// row; in rows whose m c2 leaves the 32-bit range (all masked by the type's
+// lowest value), base = m and r = 0.  f16 logits never get there.
+struct Exponent {
+  static constexpr bool kShifts = !std::is_same<E, __half>::value;
+  float2 c, base, r;
+  float rest;
 
-// NV vectors in registers: their sums against their own maximum.
-template <int NV>
+  __device__ __forceinline__ Exponent(float m, float c2) : c(make_float2(c2, c2)) {
+    const bool fits = !kShifts || fabsf(m) * c2 < 1e38f;
+    base = fits ? make_float2(0.0f, 0.0f) : make_float2(-m, -m);
+    r = fits ? make_float2(-m * c2, -m * c2) : make_float2(0.0f, 0.0f);
+    rest = fits ? fmaf(-m, c2, m * c2) : 0.0f;
+  }
+  __device__ __forceinline__ float2 of(float2 x) const {
+    return __ffma2_rn(kShifts ? __fadd2_rn(x, base) : x, c, r);
+  }
+};
+
+// NV vectors in registers: their sums against their own maximum (q only with `moment`).
+template <int NV, bool moment>
 __device__ __forceinline__ RowSums sums_of(const uint4* u, float c2) {
-  RowSums r = {kMinusInf, 0.0f, 0.0f};
+  const float m = max_of<E, NV>(u);
+  const Exponent ex(usable_max(m), c2);
+  float2 s = {}, q = {};
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    float x[kW];
+    float2 x[kW / 2];
     unpack<E>(u[k], x);
 #pragma unroll
-    for (uint32_t i = 0; i < kW; ++i) r.m = fmaxf(r.m, x[i]);
+    for (uint32_t i = 0; i < kW / 2; ++i) {
+      const float2 t = ex.of(x[i]), e = make_float2(exp2_fast(t.x), exp2_fast(t.y));
+      s = __fadd2_rn(s, e);
+      if (moment) q = __ffma2_rn(e, make_float2(finite_t(t.x), finite_t(t.y)), q);
+    }
   }
-  const float ref = usable_max(r.m);
+  const float s1 = s.x + s.y, f = fmaf(ex.rest, kLn2, 1.0f);  // 2^rest
+  return {m, f * s1, f * fmaf(ex.rest, s1, q.x + q.y)};
+}
+
+// The gradient of vectors of logits, from a row's factors (o.d only with `tilt`).
+template <bool tilt>
+struct Grads {
+  Exponent ex;
+  float2 b, d;
+
+  __device__ __forceinline__ Grads(const RowOut& o, float c2) : ex(o.m, c2) {
+    const float f = fmaf(ex.rest, kLn2, 1.0f), b1 = f * fmaf(o.d, ex.rest, o.b), d1 = f * o.d;
+    b = make_float2(b1, b1);
+    d = make_float2(d1, d1);
+  }
+  __device__ __forceinline__ uint4 of(const uint4& u) const {
+    float2 x[kW / 2];
+    unpack<E>(u, x);
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    float x[kW];
-    unpack<E>(u[k], x);
+    for (uint32_t i = 0; i < kW / 2; ++i) {
+      const float2 t = ex.of(x[i]), e = make_float2(exp2_fast(t.x), exp2_fast(t.y));
+      x[i] = __fmul2_rn(e, tilt ? __ffma2_rn(d, make_float2(finite_t(t.x), finite_t(t.y)), b) : b);
+    }
+    return pack<E>(x);
+  }
+};
+
+// The gradient of vector v of row x, to row g.
+__device__ __forceinline__ void put(const Window<E>& x, const Window<E>& g, uint32_t v, const uint4& d) {
+  if (x.shift == g.shift) g.store(v, d);
+  else g.store_cut(v, x.shift, d);
+}
+
+// ---- the shortest rows (three modes): a thread per row, N elements at most ----
+
+constexpr uint32_t kGroupThreads = 256;
+
+// The block's part of the policy loss.  Said before the gradient is stored, so
+// that the fence has only these few values to wait for: after the stores, it
+// cost a fifth of the kernel's time.  The last block sums up at its end.
+__device__ __forceinline__ bool say_policy_part(const RowArgs& a, const RowOut& o, bool mine, uint32_t lanes, float* buf) {
+  float v[kPolicySums];
 #pragma unroll
-    for (uint32_t i = 0; i < kW; ++i) {
-      const float t = (x[i] - ref) * c2, e = exp2_fast(t);
+  for (uint32_t k = 0; k < kPolicySums; ++k) v[k] = mine ? o.sums[k] : 0.0f;
+  const float sum = block_sums(v, buf, lanes);
+  if (threadIdx.x >= 32) return false;
+  if (threadIdx.x < kPolicySums) a.partial[(uint64_t)threadIdx.x * gridDim.x + blockIdx.x] = sum;
+  return last_to_say(&a.counts->blocks_done, gridDim.x);
+}
+
+template <RowOp op, int N>
+__global__ void __launch_bounds__(kGroupThreads) short_kernel(const RowArgs a, uint32_t) {
+  const uint64_t row = (uint64_t)blockIdx.x * kGroupThreads + threadIdx.x;
+  const bool here = row < a.rows;
+  if constexpr (kFollows<op>) let_next_start();
+  RowIn in = {};
+  if (here) in = load_row<E, op>(a, row);
+  const E* x = static_cast<const E*>(a.x) + row * a.ldx;
+  float v[N];
+#pragma unroll
+  for (uint32_t j = 0; j < N; ++j) v[j] = in.on && j < a.vocab ? to_f32(x[j]) : kMinusInf;
+  RowSums r = {};
+  if constexpr (op != RowOp::kPairGrad) {
+    r.m = v[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) r.m = fmaxf(r.m, v[i]);
+    const float ref = usable_max(r.m);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float t = (v[i] - ref) * a.c2, e = exp2_fast(t);
       r.s += e;
       r.q = fmaf(e, finite_t(t), r.q);
     }
   }
-  return r;
-}
-
-template <int NV>
-__device__ __forceinline__ void grad_of(const uint4& u, const RowOut& o, float c2, float* g) {
-  float x[kW];
-  unpack<E>(u, x);
-#pragma unroll
-  for (uint32_t i = 0; i < kW; ++i) g[i] = logit_grad(o, x[i], c2);
-}
-
-// ---- short rows: 1 to 32 lanes of a warp per row, kShort elements a lane ----
-
-constexpr uint32_t kGroupThreads = 256;
-constexpr uint32_t kShort = 4;
-
-// The block's part of the policy loss, once its rows are done.
-__device__ __forceinline__ void put_policy_block(const RowArgs& a, const RowOut& o, bool mine) {
-  __shared__ float buf[kGroupThreads / 32];
-  for (uint32_t k = 0; k < kPolicySums; ++k) {
-    const float v = block_sum(mine ? o.sums[k] : 0.0f, buf);
-    if (threadIdx.x == 0) a.partial[(uint64_t)k * gridDim.x + blockIdx.x] = v;
-  }
-  if (last_block(&a.counts->blocks_done, gridDim.x)) policy_stats(a, gridDim.x, buf);
-}
-
-template <RowOp op>
-__global__ void __launch_bounds__(kGroupThreads) short_kernel(const RowArgs a, uint32_t lanes) {
-  const uint64_t row = ((uint64_t)blockIdx.x * kGroupThreads + threadIdx.x) / lanes;
-  const uint32_t lane = threadIdx.x % lanes;
-  const bool here = row < a.rows;
-  RowIn in = {};
-  if (here) in = load_row<E, op>(a, row);
-  const E* x = static_cast<const E*>(a.x) + row * a.ldx;
-  float v[kShort];
-#pragma unroll
-  for (uint32_t i = 0; i < kShort; ++i) {
-    const uint32_t j = lane + i * lanes;
-    v[i] = in.on && j < a.vocab ? to_f32(x[j]) : kMinusInf;
-  }
-  RowSums r = {};
-  if constexpr (op != RowOp::kPairGrad) r = lanes_join(sums_of<kShort>(v, a.c2), a.c2, lanes);
   RowOut o = {};
-  if (here) o = finish_row<op>(a, row, in, r, lane == 0);
+  if constexpr (kFollows<op>) wait_for_previous();
+  if (here) {
+    load_row_late<op>(a, row, in);
+    o = finish_row<op>(a, row, in, r, true);
+  }
+  __shared__ float buf[kGroupThreads / 32 * kPolicySums];
+  bool last = false;
+  if constexpr (op == RowOp::kPolicy) last = say_policy_part(a, o, here, 1, buf);
   if constexpr (!kScores<op>) {
     if (here && a.g) {
       E* g = static_cast<E*>(a.g) + row * a.ldg;
 #pragma unroll
-      for (uint32_t i = 0; i < kShort; ++i) {
-        const uint32_t j = lane + i * lanes;
+      for (uint32_t j = 0; j < N; ++j) {
         if (j >= a.vocab) continue;
-        float d = in.on ? logit_grad(o, v[i], a.c2) : 0.0f;
+        float d = in.on ? logit_grad(o, v[j], a.c2) : 0.0f;
         if (in.on && j == in.y) d += o.hit;
         g[j] = from_f32<E>(d);
       }
     }
   }
-  if constexpr (op == RowOp::kPolicy) put_policy_block(a, o, here && lane == 0);
+  if constexpr (op == RowOp::kPolicy) {
+    if (__syncthreads_or(last)) policy_stats(a, gridDim.x, buf);
+  }
 }
 
-// ---- middling rows: 8 to 32 lanes of a warp per row, NV vectors a lane ----
+// ---- middling rows: 1 to 32 lanes of a warp per row, NV vectors a lane ----
 
-template <RowOp op, int NV>
-__global__ void __launch_bounds__(kGroupThreads) warp_kernel(const RowArgs a, uint32_t lanes) {
+template <RowOp op, bool entropy, int NV>
+__global__ void __launch_bounds__(kGroupThreads, op == RowOp::kPolicy ? 3 : 4) warp_kernel(const RowArgs a, uint32_t lanes) {
   const uint64_t row = ((uint64_t)blockIdx.x * kGroupThreads + threadIdx.x) / lanes;
   const uint32_t lane = threadIdx.x % lanes;
   const bool here = row < a.rows;
+  if constexpr (kFollows<op>) let_next_start();
   RowIn in = {};
   if (here) in = load_row<E, op>(a, row);
-  const Window<E> x(const_cast<E*>(static_cast<const E*>(a.x)) + row * a.ldx, in.on ? a.vocab : 0);
-  uint4 u[NV];
+  const Window<E> x(const_cast<E*>(static_cast<const E*>(a.x)) + row * a.ldx, a.vocab);
+  uint4 u[NV] = {};
+  if (in.on) {
 #pragma unroll
-  for (int k = 0; k < NV; ++k) u[k] = x.load(lane + k * lanes);
+    for (int k = 0; k < NV; ++k) u[k] = x.load(lane + k * lanes, true);
+  }
   RowSums r = {};
-  if constexpr (op != RowOp::kPairGrad) r = lanes_join(sums_of<NV>(u, a.c2), a.c2, lanes);
+  if constexpr (op != RowOp::kPairGrad) r = lanes_join(sums_of<NV, kMoment<op, entropy>>(u, a.c2), a.c2, lanes);
   RowOut o = {};
-  if (here) o = finish_row<op>(a, row, in, r, lane == 0);
+  if constexpr (kFollows<op>) wait_for_previous();
+  if (here) {
+    load_row_late<op>(a, row, in);
+    o = finish_row<op>(a, row, in, r, lane == 0);
+  }
+  __shared__ float buf[kGroupThreads / 32 * kPolicySums];
+  bool last = false;
+  if constexpr (op == RowOp::kPolicy) last = say_policy_part(a, o, here && lane == 0, lanes, buf);
   if constexpr (!kScores<op>) {
     if (here && a.g) {
       const Window<E> g(static_cast<E*>(a.g) + row * a.ldg, a.vocab);
-      const uint32_t shift = in.on ? x.shift : g.shift;
+      const Grads<entropy> grads(o, a.c2);
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
-        float d[kW] = {};
-        if (in.on) grad_of<NV>(u[k], o, a.c2, d);
-        if (shift == g.shift) g.store(lane + k * lanes, d);
-        else g.store_cut(lane + k * lanes, shift, d);
+        uint4 d = make_uint4(0, 0, 0, 0);
+        if (in.on) d = grads.of(u[k]);
+        put(x, g, lane + k * lanes, d);
       }
-      if (in.on && in.known && (in.y + shift) / kW % lanes == lane)
+      if (in.on && in.known && (in.y + x.shift) / kW % lanes == lane)
         g.row[in.y] = from_f32<E>(logit_grad(o, in.xy, a.c2) + o.hit);
     }
   }
-  if constexpr (op == RowOp::kPolicy) put_policy_block(a, o, here && lane == 0);
+  if constexpr (op == RowOp::kPolicy) {
+    if (__syncthreads_or(last)) policy_stats(a, gridDim.x, buf);
+  }
 }
 
 // ---- long rows: a block, or a cluster of blocks, per row ----
 
 constexpr uint32_t kWideThreads = 512;
 constexpr uint32_t kMaxCluster = 8;
+constexpr int kWideVectors = 8;  // a thread's vectors of a tile
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -187,28 +247,29 @@ __device__ __forceinline__ void cluster_store(float* p, uint32_t rank, float v) 
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(v) : "memory");
 }
 
-// `cluster` blocks per row, each with `tiles` tiles of NV vectors a thread;
+// `cluster` blocks per row, each with `tiles` tiles of kWideVectors vectors a thread;
 // the last tile stays in registers between the row's sums and its gradient.
-template <RowOp op, int NV>
+template <RowOp op, bool entropy>
 __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, uint32_t cluster, uint32_t tiles) {
+  constexpr int NV = kWideVectors;
   constexpr uint32_t kMost = kWideThreads / 32 * kMaxCluster;
   __shared__ float part[3][kMost];  // sums of the row's warps, all blocks'
   const uint64_t row = blockIdx.x / cluster;
   const uint32_t rank = blockIdx.x % cluster, tid = threadIdx.x, threads = blockDim.x;
-  const RowIn in = load_row<E, op>(a, row);
+  if constexpr (kFollows<op>) let_next_start();
+  RowIn in = load_row<E, op>(a, row);
   const Window<E> x(const_cast<E*>(static_cast<const E*>(a.x)) + row * a.ldx, a.vocab);
   const uint32_t first = rank * tiles * NV * threads + tid;
   uint4 u[NV];
-  RowOut o = {};
+  RowSums r = {kMinusInf, 0.0f, 0.0f};
   if (in.on) {
     if (cluster > 1 && op != RowOp::kPairGrad) cluster_arrive();  // seen below: the others run
-    RowSums r = {kMinusInf, 0.0f, 0.0f};
     for (uint32_t tile = 0; tile < tiles; ++tile) {
       if (op == RowOp::kPairGrad && tile + 1 < tiles) continue;
 #pragma unroll
-      for (int k = 0; k < NV; ++k) u[k] = x.load(first + (tile * NV + k) * threads);
+      for (int k = 0; k < NV; ++k) u[k] = x.load(first + (tile * NV + k) * threads, kScores<op> || tile + 1 == tiles);
       if constexpr (op != RowOp::kPairGrad) {
-        const RowSums now = sums_of<NV>(u, a.c2);
+        const RowSums now = sums_of<NV, kMoment<op, entropy>>(u, a.c2);
         r = tiles > 1 ? join(r, now, a.c2) : now;
       }
     }
@@ -240,33 +301,36 @@ __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, 
       }
       r = lanes_join(r, a.c2, 32);
     }
-    o = finish_row<op>(a, row, in, r, rank == 0 && tid == 0);
-  } else {
-    o = finish_row<op>(a, row, in, {}, rank == 0 && tid == 0);
   }
+  if constexpr (kFollows<op>) wait_for_previous();
+  load_row_late<op>(a, row, in);
+  const RowOut o = finish_row<op>(a, row, in, r, rank == 0 && tid == 0);
+  bool last = false;
   if constexpr (op == RowOp::kPolicy) {
-    if (rank == 0 && tid == 0)
-      for (uint32_t k = 0; k < kPolicySums; ++k) a.partial[k * a.rows + row] = o.sums[k];
+    if (rank == 0 && tid < 32) {
+      if (tid == 0)
+        for (uint32_t k = 0; k < kPolicySums; ++k) a.partial[k * a.rows + row] = o.sums[k];
+      last = last_to_say(&a.counts->blocks_done, (uint32_t)a.rows);
+    }
   }
   if constexpr (!kScores<op>) {
     if (a.g) {
       const Window<E> g(static_cast<E*>(a.g) + row * a.ldg, a.vocab);
       if (!in.on) {
-        const float zero[kW] = {};
-        for (uint32_t k = 0; k < NV * tiles; ++k) g.store(first + k * threads, zero);
+        const uint4 zero = make_uint4(0, 0, 0, 0);
+        for (uint32_t k = 0; k < NV * tiles; ++k) put(x, g, first + k * threads, zero);
       } else {
+        const Grads<entropy> grads(o, a.c2);
         for (uint32_t tile = tiles; tile-- > 0;) {
           if (tile + 1 < tiles) {
 #pragma unroll
-            for (int k = 0; k < NV; ++k) u[k] = x.load(first + (tile * NV + k) * threads);
+            for (int k = 0; k < NV; ++k) u[k] = x.load(first + (tile * NV + k) * threads, true);
           }
 #pragma unroll
           for (int k = 0; k < NV; ++k) {
             const uint32_t v = first + (tile * NV + k) * threads;
-            float d[kW];
-            grad_of<NV>(u[k], o, a.c2, d);
-            if (x.shift == g.shift) g.store(v, d);
-            else g.store_cut(v, x.shift, d);
+            const uint4 d = grads.of(u[k]);
+            put(x, g, v, d);
           }
         }
         const uint32_t at = (in.y + x.shift) / kW - rank * tiles * NV * threads;  // the vector with the token
@@ -276,69 +340,70 @@ __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, 
     }
   }
   if constexpr (op == RowOp::kPolicy) {
-    __shared__ float sums[kWideThreads / 32];
-    if (rank == 0 && last_block(&a.counts->blocks_done, (uint32_t)a.rows)) policy_stats(a, a.rows, sums);
+    __shared__ float sums[kWideThreads / 32 * kPolicySums];
+    if (rank == 0 && __syncthreads_or(last)) policy_stats(a, a.rows, sums);
   }
 }
 
 struct WideShape {
-  uint32_t cluster, threads, vectors, tiles;
+  uint32_t cluster, threads, tiles;
 };
 
 uint32_t div_up(uint32_t a, uint32_t b) { return (a + b - 1) / b; }
 
-WideShape wide_shape(uint64_t rows, uint32_t vectors) {
-  WideShape s = {1, 0, 8, 1};
-  while (s.cluster < kMaxCluster && div_up(vectors, s.cluster) > 256 * 8) s.cluster *= 2;
-  while (s.cluster < kMaxCluster && rows * s.cluster < 304 && div_up(vectors, s.cluster) > 256) s.cluster *= 2;
-  const uint32_t each = div_up(vectors, s.cluster);
-  s.vectors = each <= 256 * 2 ? 2 : each <= 256 * 4 ? 4 : 8;
-  const uint32_t lanes = div_up(each, s.vectors);
-  s.tiles = div_up(lanes, kWideThreads);
+WideShape wide_shape(uint64_t rows, uint32_t vectors, bool scores) {
+  WideShape s = {1, 0, 1};
+  while (s.cluster < kMaxCluster && rows * s.cluster <= 400 && div_up(vectors, s.cluster) > 256) s.cluster *= 2;
+  const uint32_t lanes = div_up(div_up(vectors, s.cluster), kWideVectors);
+  const uint32_t most = scores ? 128 : lanes / 2 < 128 ? 128 : lanes / 2 < kWideThreads ? div_up(lanes / 2, 32) * 32 : kWideThreads;
+  s.tiles = div_up(lanes, most);
   s.threads = div_up(div_up(lanes, s.tiles), 32) * 32;
   return s;
 }
 
-template <RowOp op, int NV>
-cudaError_t launch_wide(const RowArgs& a, const WideShape& s, cudaStream_t st) {
-  if (a.rows > 0x7FFFFFFFu / s.cluster) return cudaErrorInvalidValue;
+// A launch that may start before the call's previous kernel ends (kFollows), with clusters of `cluster` blocks.
+template <RowOp op, typename K, typename... Args>
+cudaError_t launch(K kernel, uint64_t blocks, uint32_t threads, uint32_t cluster, cudaStream_t st, Args... args) {
+  if (blocks > 0x7FFFFFFFu) return cudaErrorInvalidValue;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((uint32_t)a.rows * s.cluster);
-  cfg.blockDim = dim3(s.threads);
+  cfg.gridDim = dim3((uint32_t)blocks);
+  cfg.blockDim = dim3(threads);
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = s.cluster;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cudaLaunchAttribute attr[2];
   cfg.attrs = attr;
-  cfg.numAttrs = s.cluster > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, wide_kernel<op, NV>, a, s.cluster, s.tiles);
+  if (kFollows<op>) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (cluster > 1) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+    attr[cfg.numAttrs].val.clusterDim.x = cluster;
+    attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
+    ++cfg.numAttrs;
+  }
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <RowOp op>
+uint32_t pow2_up(uint32_t n) {
+  uint32_t p = 1;
+  while (p < n) p *= 2;
+  return p;
+}
+
+template <RowOp op, bool entropy>
 cudaError_t launch_op(const RowArgs& a, cudaStream_t st) {
-  const auto blocks = [&](uint32_t lanes) { return (uint32_t)((a.rows * lanes + kGroupThreads - 1) / kGroupThreads); };
-  if (a.vocab <= 32 * kShort) {
-    uint32_t lanes = 1;
-    while (lanes * kShort < a.vocab) lanes *= 2;
-    short_kernel<op><<<blocks(lanes), kGroupThreads, 0, st>>>(a, lanes);
-    return cudaGetLastError();
-  }
-  const uint32_t vectors = div_up(a.vocab + kW - 1, kW);  // at the worst alignment
-  if (vectors <= 128) {
-    uint32_t lanes = 8;
-    while (lanes < 32 && lanes < vectors) lanes *= 2;
-    if (vectors <= lanes) warp_kernel<op, 1><<<blocks(lanes), kGroupThreads, 0, st>>>(a, lanes);
-    else if (vectors <= 64) warp_kernel<op, 2><<<blocks(lanes), kGroupThreads, 0, st>>>(a, lanes);
-    else warp_kernel<op, 4><<<blocks(lanes), kGroupThreads, 0, st>>>(a, lanes);
-    return cudaGetLastError();
-  }
-  const WideShape s = wide_shape(a.rows, vectors);
-  switch (s.vectors) {
-    case 2: return launch_wide<op, 2>(a, s, st);
-    case 4: return launch_wide<op, 4>(a, s, st);
-    default: return launch_wide<op, 8>(a, s, st);
-  }
+  const auto group = [&](auto kernel, uint32_t lanes) {
+    return launch<op>(kernel, (a.rows * lanes + kGroupThreads - 1) / kGroupThreads, kGroupThreads, 1, st, a, lanes);
+  };
+  // Vectors that a row touches: one more where rows may start inside one.
+  const bool aligned = ((uintptr_t)a.x | (uintptr_t)(a.ldx * sizeof(E))) % 16 == 0;
+  const uint32_t vectors = div_up(a.vocab + (aligned ? 0 : kW - 1), kW);
+  if (a.vocab <= 4) return group(short_kernel<op, 4>, 1);
+  if (vectors <= 2) return group(warp_kernel<op, entropy, 2>, 1);
+  if (vectors <= 8) return group(warp_kernel<op, entropy, 4>, pow2_up(div_up(vectors, 4)));
+  if (vectors <= 256) return group(warp_kernel<op, entropy, 8>, pow2_up(div_up(vectors, 8)));
+  const WideShape s = wide_shape(a.rows, vectors, kScores<op>);
+  return launch<op>(wide_kernel<op, entropy>, a.rows * s.cluster, s.threads, s.cluster, st, a, s.cluster, s.tiles);
 }
 
 }  // namespace
@@ -347,11 +412,13 @@ cudaError_t launch_op(const RowArgs& a, cudaStream_t st) {
 #define BF_ROWS_NAME(t) BF_ROWS_NAME2(t)
 cudaError_t BF_ROWS_NAME(BF_ROWS_TYPE)(RowOp op, const RowArgs& a, cudaStream_t st) {
   switch (op) {
-    case RowOp::kScore: return launch_op<RowOp::kScore>(a, st);
-    case RowOp::kScoreGrad: return launch_op<RowOp::kScoreGrad>(a, st);
-    case RowOp::kPolicy: return launch_op<RowOp::kPolicy>(a, st);
-    case RowOp::kPairScore: return launch_op<RowOp::kPairScore>(a, st);
-    default: return launch_op<RowOp::kPairGrad>(a, st);
+    case RowOp::kScore: return a.entropy ? launch_op<RowOp::kScore, true>(a, st) : launch_op<RowOp::kScore, false>(a, st);
+    case RowOp::kScoreGrad:
+      return a.grad_entropy ? launch_op<RowOp::kScoreGrad, true>(a, st) : launch_op<RowOp::kScoreGrad, false>(a, st);
+    case RowOp::kPolicy:
+      return a.entropy_coef != 0.0f ? launch_op<RowOp::kPolicy, true>(a, st) : launch_op<RowOp::kPolicy, false>(a, st);
+    case RowOp::kPairScore: return launch_op<RowOp::kPairScore, false>(a, st);
+    default: return launch_op<RowOp::kPairGrad, false>(a, st);
   }
 }
 

@@ -63,6 +63,16 @@ struct RowOut {
   float sums[kPolicySums];
 };
 
+// Whether an op's rows depend on work that its own launch may overlap: what the
+// kernels before it in the call write is read after wait_for_previous().
+template <RowOp op>
+constexpr bool kFollows = op == RowOp::kPolicy || op == RowOp::kPairScore || op == RowOp::kPairGrad;
+
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// The next kernel of the call may start: it waits for this one's end where it has to.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// The part of a row that the caller's arrays give.
 template <typename E, RowOp op>
 __device__ __forceinline__ RowIn load_row(const RowArgs& a, uint64_t row) {
   RowIn in = {};
@@ -70,29 +80,33 @@ __device__ __forceinline__ RowIn load_row(const RowArgs& a, uint64_t row) {
   in.on = y >= 0;
   in.known = y < (int64_t)a.vocab;
   in.y = (uint32_t)y;
-  if constexpr (op == RowOp::kPolicy || op == RowOp::kPairScore || op == RowOp::kPairGrad) {
-    const uint32_t seq = a.row_seq[row];
-    in.on = seq != kNoSequence;
-    if constexpr (op == RowOp::kPolicy) {
-      if (in.on) {
-        const uint32_t n = a.seq_tokens[seq];
-        in.w = a.reduction == BF_MEAN_TOKENS ? 1.0f / (float)a.counts->tokens
-               : a.reduction == BF_MEAN_SEQUENCES ? 1.0f / ((float)n * (float)a.counts->sequences) : 1.0f;
-        in.old_lp = a.old_logprob[row];
-        in.adv = a.advantage[a.advantage_per_token ? row : seq];
-        if (a.ref_logprob) in.ref_lp = a.ref_logprob[row];
-      }
-    }
-    if constexpr (op == RowOp::kPairGrad) {
-      if (in.on) in.slope_lp = a.seq_slope[seq];
-    }
-  }
   if constexpr (op == RowOp::kScoreGrad) {
     in.slope_lp = a.grad_logprob[row];
     if (a.grad_entropy) in.slope_h = a.grad_entropy[row];
   }
+  if constexpr (op == RowOp::kPolicy) {
+    in.old_lp = a.old_logprob[row];
+    if (a.ref_logprob) in.ref_lp = a.ref_logprob[row];
+    if (a.advantage_per_token) in.adv = a.advantage[row];
+  }
   if (in.on && in.known) in.xy = to_f32(static_cast<const E*>(a.x)[row * a.ldx + in.y]);
   return in;
+}
+
+// The part that the call's earlier kernels give; a row of no sequence is not scored.
+template <RowOp op>
+__device__ __forceinline__ void load_row_late(const RowArgs& a, uint64_t row, RowIn& in) {
+  if constexpr (kFollows<op>) {
+    const uint32_t seq = a.row_seq[row];
+    in.on = seq != kNoSequence;
+    if (!in.on) return;
+    if constexpr (op == RowOp::kPolicy) {
+      in.w = a.reduction == BF_MEAN_TOKENS ? 1.0f / (float)a.counts->tokens
+             : a.reduction == BF_MEAN_SEQUENCES ? 1.0f / ((float)a.seq_tokens[seq] * (float)a.counts->sequences) : 1.0f;
+      if (!a.advantage_per_token) in.adv = a.advantage[seq];
+    }
+    if constexpr (op == RowOp::kPairGrad) in.slope_lp = a.seq_slope[seq];
+  }
 }
 
 // The row's outputs from its sums (written by the caller's leading thread) and
@@ -178,28 +192,35 @@ __device__ __forceinline__ RowSums lanes_join(RowSums r, float c2, uint32_t lane
   return r;
 }
 
-// Sum over the block's threads, in thread 0; every thread of the block calls it.  buf: a float per warp.
-__device__ __forceinline__ float block_sum(float v, float* buf) {
+// Sums of N values over the block's threads: the k-th in thread k.  Every thread of the block calls it with the same
+// `lanes`: only every lanes-th one (a power of two, at most 32) brings values.  buf: N floats per warp, not in use.
+template <uint32_t N>
+__device__ __forceinline__ float block_sums(float (&v)[N], float* buf, uint32_t lanes = 1) {
 #pragma unroll
-  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
-  __syncthreads();
-  if (threadIdx.x % 32 == 0) buf[threadIdx.x / 32] = v;
+  for (uint32_t k = 0; k < N; ++k)
+    for (uint32_t o = 16; o >= lanes && o; o /= 2) v[k] += __shfl_down_sync(~0u, v[k], o);
+  if (threadIdx.x % 32 == 0) {
+#pragma unroll
+    for (uint32_t k = 0; k < N; ++k) buf[threadIdx.x / 32 * N + k] = v[k];
+  }
   __syncthreads();
   float sum = 0.0f;
-  if (threadIdx.x == 0)
-    for (uint32_t w = 0; w < blockDim.x / 32; ++w) sum += buf[w];
+  if (threadIdx.x < N)
+    for (uint32_t w = 0; w < blockDim.x / 32; ++w) sum += buf[w * N + threadIdx.x];
   return sum;
 }
 
-// Whether this block is the last of `blocks` to get here; what the others wrote before is then visible.
-__device__ __forceinline__ bool last_block(uint32_t* done, uint32_t blocks) {
-  __shared__ bool last;
-  __threadfence();
-  __syncthreads();
-  if (threadIdx.x == 0) last = atomicAdd(done, 1u) == blocks - 1;
-  __syncthreads();
-  if (last) __threadfence();
-  return last;
+// Whether this block is the last of `blocks` to say so; called by the warp whose
+// lanes wrote what the last one reads (last_sees() there).
+__device__ __forceinline__ bool last_to_say(uint32_t* done, uint32_t blocks) {
+  __syncwarp();
+  uint32_t before = 0;
+  if (threadIdx.x % 32 == 0) {
+    __threadfence();
+    before = atomicAdd(done, 1u);
+  }
+  return __shfl_sync(~0u, before, 0) == blocks - 1;
 }
+__device__ __forceinline__ void last_sees() { __threadfence(); }
 
 }  // namespace bfk
