@@ -204,16 +204,7 @@ cudaError_t launch_row_sequences(const int64_t* tokens, uint64_t rows, const int
 }
 
 cudaError_t launch_pairs(const PairArgs& a, cudaStream_t st) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((uint32_t)(a.pairs < (1u << 30) ? a.pairs : (1u << 30)));
-  cfg.blockDim = dim3(kPairThreads);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, pair_kernel, a);
+  return launch_after(pair_kernel, a.pairs < (1u << 30) ? a.pairs : (1u << 30), kPairThreads, st, a);
 }
 
 }  // namespace bfk

@@ -4,9 +4,12 @@
 // The gradient sorts the positions by token (stable: by token, then position)
 // and sums each token's rows in that order, so its result does not depend on
 // when blocks run, and a token that fills half of the batch costs no more than
-// others: a block sums kTile sorted positions, writes the tokens that lie
-// within its tile and leaves a partial row for one that goes on in the next.
+// others: tiles of kTile sorted positions are summed apart, the tokens that lie
+// within one tile are written, and one that goes on in the next leaves a
+// partial row, which the last kernel adds up.  Both directions are bound by
+// memory: every thread moves 16 bytes at a time where the rows allow it.
 #include "bf_elem.cuh"
+#include "bf_launches.cuh"
 #include "bf_learn.h"
 
 namespace bfk {
@@ -14,31 +17,115 @@ namespace bfk {
 namespace {
 
 constexpr uint32_t kThreads = 256;
-constexpr uint32_t kTile = 32;        // sorted positions summed by a block
-constexpr uint32_t kSortTile = 1024;  // positions counted and placed by a block
-constexpr uint32_t kBins = 256;       // 8 bits of the token a pass
+constexpr uint32_t kTile = 32;  // sorted positions summed by one group of lanes
 
-template <typename S, typename D>
-__global__ void __launch_bounds__(kThreads) embed_kernel(const EmbedArgs a) {
-  for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const int64_t id = a.tokens[row];
-    D* out = static_cast<D*>(a.dst) + row * a.ldd;
-    const bool in = id >= 0 && id < (int64_t)a.vocab;
-    const float other = id < 0 ? 0.0f : __int_as_float(0x7FC00000);
-    const S* w = static_cast<const S*>(a.src) + (in ? (uint64_t)id : 0) * a.lds;
-    for (uint32_t c = threadIdx.x; c < a.width; c += kThreads)
-      out[c] = from_f32<D>(in ? to_f32(w[c]) * a.scale : other);
+__device__ __forceinline__ float nan_value() { return __int_as_float(0x7FC00000); }
+
+// N neighbouring elements (N = 1, or the 16 bytes of the row's own type) as 32-bit values and back.
+template <typename E, int N>
+__device__ __forceinline__ void read_n(const E* p, float* f) {
+  if constexpr (N * sizeof(E) == 16) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    float2 v[N / 2];
+    unpack<E>(u, v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = i % 2 ? v[i / 2].y : v[i / 2].x;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = to_f32(p[i]);
+  }
+}
+// The same, still as read: 16 bytes or one element.
+template <typename E, int N>
+struct Piece {
+  uint4 u;
+  __device__ __forceinline__ void load(const E* p) { u = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void add_to(float* sum) const {
+    float2 v[N / 2];
+    unpack<E>(u, v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] += i % 2 ? v[i / 2].y : v[i / 2].x;
+  }
+};
+template <typename E>
+struct Piece<E, 1> {
+  E v;
+  __device__ __forceinline__ void load(const E* p) { v = *p; }
+  __device__ __forceinline__ void add_to(float* sum) const { sum[0] += to_f32(v); }
+};
+template <int N>
+__device__ __forceinline__ void read_floats(const float* p, float* f) {
+  if constexpr (N % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) read_n<float, 4>(p + i, f + i);
+  } else {
+    f[0] = *p;
+  }
+}
+template <typename E, int N>
+__device__ __forceinline__ void write_n(E* p, const float* f) {
+  if constexpr (N * sizeof(E) == 16) {
+    float2 v[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) v[i] = make_float2(f[2 * i], f[2 * i + 1]);
+    *reinterpret_cast<uint4*>(p) = pack<E>(v);
+  } else if constexpr (N * sizeof(E) == 32) {
+    write_n<E, N / 2>(p, f);
+    write_n<E, N / 2>(p + N / 2, f + N / 2);
+  } else if constexpr (N * sizeof(E) == 8) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack2(make_float2(f[0], f[1]), E()), pack2(make_float2(f[2], f[3]), E()));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) p[i] = from_f32<E>(f[i]);
   }
 }
 
-// ---- sort by token ----
+// ---- forward: kPieces pieces of N elements a thread, all read before the first is written ----
+
+constexpr uint32_t kPieces = 4;
+
+template <typename E, int N, typename I>
+__global__ void __launch_bounds__(kThreads) embed_kernel(const EmbedArgs a, I pieces, uint32_t per_row) {
+  const I first = (I)blockIdx.x * (kThreads * kPieces) + threadIdx.x;
+  I row[kPieces];
+  int64_t id[kPieces];
+  float f[kPieces][N] = {};
+#pragma unroll
+  for (uint32_t k = 0; k < kPieces; ++k) {
+    row[k] = (first + k * kThreads) / per_row;
+    id[k] = first + k * kThreads < pieces ? a.tokens[row[k]] : -1;
+  }
+#pragma unroll
+  for (uint32_t k = 0; k < kPieces; ++k) {
+    const uint32_t c = (uint32_t)(first + k * kThreads - row[k] * per_row) * N;
+    if (id[k] >= 0 && id[k] < (int64_t)a.vocab) read_n<E, N>(static_cast<const E*>(a.src) + (uint64_t)id[k] * a.lds + c, f[k]);
+  }
+#pragma unroll
+  for (uint32_t k = 0; k < kPieces; ++k) {
+    if (first + k * kThreads >= pieces) continue;
+    const uint32_t c = (uint32_t)(first + k * kThreads - row[k] * per_row) * N;
+#pragma unroll
+    for (int j = 0; j < N; ++j) f[k][j] = id[k] >= (int64_t)a.vocab ? nan_value() : id[k] < 0 ? 0.0f : f[k][j] * a.scale;
+    write_n<E, N>(static_cast<E*>(a.dst) + (uint64_t)row[k] * a.ldd + c, f[k]);
+  }
+}
+
+// ---- sort by token: 9 bits a pass, a count and a placing kernel each ----
+
+constexpr uint32_t kBits = 9, kBins = 1u << kBits, kSortThreads = kBins;
+constexpr uint32_t kMaxSortTiles = 128;
 
 struct SortArgs {
   const int64_t* tokens;  // first pass: keys are made from these
   const uint32_t *key_in, *pos_in;
   uint32_t *key_out, *pos_out;
-  uint32_t* hist;  // kBins rows of `tiles`
-  uint32_t rows, tiles, shift, vocab;
+  uint32_t* hist;  // a row of kBins counts per tile
+  uint32_t* runs;  // first pass clears it: number of runs over several tiles
+  uint32_t rows, tiles, tile, shift, vocab;
+  // rows of the table's gradient that this launch's other blocks clear
+  void* fill;
+  uint64_t ld;
+  uint32_t fill_first, fill_end, width;
 };
 
 // Tokens outside the vocabulary sort behind it, as `vocab`.
@@ -48,72 +135,164 @@ __device__ __forceinline__ uint32_t key_of(const SortArgs& a, uint32_t i) {
   return id >= 0 && id < (int64_t)a.vocab ? (uint32_t)id : a.vocab;
 }
 
-__global__ void __launch_bounds__(kThreads) sort_count(const SortArgs a) {
+// Clearing the gradient takes longer than sorting the positions, and the sort
+// fills a few blocks only: its launches' other blocks clear, a warp per row.
+template <typename D>
+__device__ __forceinline__ void fill_rows(const SortArgs& a) {
+  const uint32_t warps = (gridDim.x - a.tiles) * (kSortThreads / 32), lane = threadIdx.x % 32;
+  for (uint64_t row = a.fill_first + (blockIdx.x - a.tiles) * (kSortThreads / 32) + threadIdx.x / 32; row < a.fill_end;
+       row += warps) {
+    const Window<D> w(static_cast<D*>(a.fill) + row * a.ld, a.width);
+    for (uint32_t v = lane; v < w.vectors; v += 32) w.store(v, make_uint4(0, 0, 0, 0));
+  }
+}
+
+template <typename D>
+__global__ void __launch_bounds__(kSortThreads) sort_count(const SortArgs a) {
+  let_next_start();
+  if (blockIdx.x >= a.tiles) {
+    fill_rows<D>(a);
+    return;
+  }
   __shared__ uint32_t bins[kBins];
   bins[threadIdx.x] = 0;
+  wait_for_previous();
+  if (a.tokens && blockIdx.x == 0 && threadIdx.x == 0) *a.runs = 0;
   __syncthreads();
-  for (uint32_t k = threadIdx.x; k < kSortTile; k += kThreads) {
-    const uint32_t i = blockIdx.x * kSortTile + k;
-    if (i < a.rows) atomicAdd(&bins[(key_of(a, i) >> a.shift) % kBins], 1u);
-  }
+  const uint32_t first = blockIdx.x * a.tile, end = min(a.rows, first + a.tile);
+  for (uint32_t i = first + threadIdx.x; i < end; i += kSortThreads) atomicAdd(&bins[(key_of(a, i) >> a.shift) % kBins], 1u);
   __syncthreads();
-  a.hist[threadIdx.x * a.tiles + blockIdx.x] = bins[threadIdx.x];
+  a.hist[blockIdx.x * kBins + threadIdx.x] = bins[threadIdx.x];
 }
 
-// Exclusive sums of the counts in place, digit by digit and tile by tile; one block.
-__global__ void __launch_bounds__(1024) sort_scan(uint32_t* hist, uint32_t n) {
-  __shared__ uint32_t warp_sum[32];
-  uint32_t before = 0;
-  for (uint32_t base = 0; base < n; base += 1024) {
-    const uint32_t i = base + threadIdx.x, lane = threadIdx.x % 32;
-    const uint32_t v = i < n ? hist[i] : 0;
-    uint32_t sum = v;
-#pragma unroll
-    for (int o = 1; o < 32; o *= 2) {
-      const uint32_t up = __shfl_up_sync(~0u, sum, o);
-      if (lane >= (uint32_t)o) sum += up;
-    }
-    if (lane == 31) warp_sum[threadIdx.x / 32] = sum;
-    __syncthreads();
-    uint32_t ahead = 0, total = 0;
-    for (uint32_t w = 0; w < 32; ++w) {
-      if (w < threadIdx.x / 32) ahead += warp_sum[w];
-      total += warp_sum[w];
-    }
-    if (i < n) hist[i] = before + ahead + sum - v;
-    before += total;
-    __syncthreads();
+template <typename D>
+__global__ void __launch_bounds__(kSortThreads) sort_place(const SortArgs a) {
+  constexpr uint32_t kWarps = kSortThreads / 32;
+  let_next_start();
+  if (blockIdx.x >= a.tiles) {
+    fill_rows<D>(a);
+    return;
   }
-}
-
-__global__ void __launch_bounds__(kThreads) sort_place(const SortArgs a) {
-  __shared__ uint32_t next[kBins];                   // where the tile's next item of each digit goes
-  __shared__ uint32_t ahead[kThreads / 32][kBins];   // items of a digit in the round's earlier warps
+  __shared__ uint32_t next[kBins];           // where the tile's next item of each digit goes
+  __shared__ uint16_t ahead[kWarps][kBins];  // items of a digit in the round's earlier warps
+  __shared__ uint32_t warp_sum[kWarps];
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  next[threadIdx.x] = a.hist[threadIdx.x * a.tiles + blockIdx.x];
-  for (uint32_t k = 0; k < kSortTile; k += kThreads) {
-    const uint32_t i = blockIdx.x * kSortTile + k + threadIdx.x;
-    for (uint32_t w = 0; w < kThreads / 32; ++w) ahead[w][threadIdx.x] = 0;
+  wait_for_previous();
+  // Thread d: the digit's items in all tiles and in those before this one.
+  uint32_t all = 0, before = 0;
+#pragma unroll 8
+  for (uint32_t t = 0; t < a.tiles; ++t) {
+    const uint32_t n = a.hist[t * kBins + threadIdx.x];
+    all += n;
+    before += t < blockIdx.x ? n : 0;
+  }
+  uint32_t sum = all;
+#pragma unroll
+  for (uint32_t o = 1; o < 32; o *= 2) {
+    const uint32_t up = __shfl_up_sync(~0u, sum, o);
+    if (lane >= o) sum += up;
+  }
+  if (lane == 31) warp_sum[warp] = sum;
+  __syncthreads();
+  for (uint32_t w = 0; w < warp; ++w) sum += warp_sum[w];
+  next[threadIdx.x] = sum - all + before;
+  const uint32_t first = blockIdx.x * a.tile, end = min(a.rows, first + a.tile);
+  for (uint32_t base = first; base < end; base += kSortThreads) {
+    const uint32_t i = base + threadIdx.x;
+#pragma unroll
+    for (uint32_t w = 0; w < kWarps; ++w) ahead[w][threadIdx.x] = 0;
     __syncthreads();
-    const bool in = i < a.rows;
+    const bool in = i < end;
     const uint32_t key = in ? key_of(a, i) : 0, digit = in ? (key >> a.shift) % kBins : kBins;
+    const uint32_t pos = in && !a.tokens ? a.pos_in[i] : i;
     const uint32_t same = __match_any_sync(~0u, digit), rank = __popc(same & ((1u << lane) - 1));
-    if (in && rank == 0) ahead[warp][digit] = __popc(same);
+    if (in && rank == 0) ahead[warp][digit] = (uint16_t)__popc(same);
     __syncthreads();
-    uint32_t sum = 0;
-    for (uint32_t w = 0; w < kThreads / 32; ++w) {  // thread d: digit d over the warps
+    uint32_t count = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < kWarps; ++w) {  // thread d: digit d over the warps
       const uint32_t n = ahead[w][threadIdx.x];
-      ahead[w][threadIdx.x] = sum;
-      sum += n;
+      ahead[w][threadIdx.x] = (uint16_t)count;
+      count += n;
     }
     __syncthreads();
     if (in) {
       const uint32_t to = next[digit] + ahead[warp][digit] + rank;
       a.key_out[to] = key;
-      a.pos_out[to] = a.tokens ? i : a.pos_in[i];
+      a.pos_out[to] = pos;
     }
     __syncthreads();
-    next[threadIdx.x] += sum;
+    next[threadIdx.x] += count;
+  }
+}
+
+// Up to kSmallSort positions: all passes in one block, the keys in shared memory.
+constexpr uint32_t kSmallSort = 2 * kSortThreads;
+
+template <typename D>
+__global__ void __launch_bounds__(kSortThreads) sort_small(const SortArgs a) {
+  constexpr uint32_t kWarps = kSortThreads / 32;
+  let_next_start();
+  if (blockIdx.x >= a.tiles) {
+    fill_rows<D>(a);
+    return;
+  }
+  __shared__ uint32_t key[2][kSmallSort], next[kBins], warp_sum[kWarps];
+  __shared__ uint16_t pos[2][kSmallSort], ahead[kWarps][kBins];
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  if (threadIdx.x == 0) *a.runs = 0;
+  for (uint32_t i = threadIdx.x; i < a.rows; i += kSortThreads) {
+    key[0][i] = key_of(a, i);
+    pos[0][i] = (uint16_t)i;
+  }
+  uint32_t from = 0;
+  for (uint32_t shift = 0; shift == 0 || (shift < 32 && (a.vocab >> shift)); shift += kBits, from = 1 - from) {
+    next[threadIdx.x] = 0;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < a.rows; i += kSortThreads) atomicAdd(&next[(key[from][i] >> shift) % kBins], 1u);
+    __syncthreads();
+    const uint32_t all = next[threadIdx.x];
+    uint32_t sum = all;
+#pragma unroll
+    for (uint32_t o = 1; o < 32; o *= 2) {
+      const uint32_t up = __shfl_up_sync(~0u, sum, o);
+      if (lane >= o) sum += up;
+    }
+    if (lane == 31) warp_sum[warp] = sum;
+    __syncthreads();
+    for (uint32_t w = 0; w < warp; ++w) sum += warp_sum[w];
+    next[threadIdx.x] = sum - all;
+    for (uint32_t base = 0; base < a.rows; base += kSortThreads) {
+      const uint32_t i = base + threadIdx.x;
+#pragma unroll
+      for (uint32_t w = 0; w < kWarps; ++w) ahead[w][threadIdx.x] = 0;
+      __syncthreads();
+      const bool in = i < a.rows;
+      const uint32_t k = in ? key[from][i] : 0, digit = in ? (k >> shift) % kBins : kBins;
+      const uint32_t same = __match_any_sync(~0u, digit), rank = __popc(same & ((1u << lane) - 1));
+      if (in && rank == 0) ahead[warp][digit] = (uint16_t)__popc(same);
+      __syncthreads();
+      uint32_t count = 0;
+#pragma unroll
+      for (uint32_t w = 0; w < kWarps; ++w) {
+        const uint32_t n = ahead[w][threadIdx.x];
+        ahead[w][threadIdx.x] = (uint16_t)count;
+        count += n;
+      }
+      __syncthreads();
+      if (in) {
+        const uint32_t to = next[digit] + ahead[warp][digit] + rank;
+        key[1 - from][to] = k;
+        pos[1 - from][to] = pos[from][i];
+      }
+      __syncthreads();
+      next[threadIdx.x] += count;
+    }
+    __syncthreads();
+  }
+  for (uint32_t i = threadIdx.x; i < a.rows; i += kSortThreads) {
+    a.key_out[i] = key[from][i];
+    a.pos_out[i] = pos[from][i];
   }
 }
 
@@ -122,91 +301,224 @@ __global__ void __launch_bounds__(kThreads) sort_place(const SortArgs a) {
 struct SumArgs {
   EmbedArgs e;
   const uint32_t *key, *pos;
-  float* partial;  // per tile: the part of a token that began before it, and of one that goes on after it
+  float* partial;   // per tile: the part of a token that began before it, and of one that goes on after it
+  uint32_t* runs;   // number of tokens that go on after the tile they began in, then their tiles, in any order
   uint32_t tiles;
 };
 
-template <typename D>
-__device__ __forceinline__ void put_sum(const SumArgs& a, uint32_t key, uint32_t c, float sum) {
+template <typename D, int N>
+__device__ __forceinline__ void put_sum(const SumArgs& a, uint32_t key, uint32_t c, float* sum) {
   D* out = static_cast<D*>(a.e.dst) + (uint64_t)key * a.e.ldd + c;
-  sum *= a.e.scale;
-  *out = from_f32<D>(a.e.accumulate ? to_f32(*out) + sum : sum);
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    sum[j] *= a.e.scale;
+    if (a.e.accumulate) sum[j] += to_f32(out[j]);
+  }
+  write_n<D, N>(out, sum);
 }
 
-template <typename S, typename D>
-__global__ void __launch_bounds__(kThreads) sum_kernel(const SumArgs a) {
-  __shared__ uint32_t key[kTile + 2];  // with the neighbours on both sides
-  __shared__ uint32_t pos[kTile];
-  const uint32_t rows = (uint32_t)a.e.rows, first = blockIdx.x * kTile, count = min(kTile, rows - first);
-  for (uint32_t k = threadIdx.x; k < kTile + 2; k += kThreads) {
-    const int64_t i = (int64_t)first + k - 1;
-    key[k] = i >= 0 && i < rows && k < count + 2 ? a.key[i] : 0xFFFFFFFFu;
-    if (k < count) pos[k] = a.pos[first + k];
+// `lanes` threads per tile, N columns a thread at a time; kAhead rows are read
+// before they are added, whatever tokens they belong to.
+template <typename S, typename D, int N>
+__global__ void __launch_bounds__(kThreads) sum_kernel(const SumArgs a, uint32_t lanes) {
+  constexpr uint32_t kAhead = 8;
+  __shared__ uint32_t keys[kThreads / 32 * (kTile + 2)];  // with the neighbours on both sides
+  __shared__ uint32_t poss[kThreads / 32 * kTile];
+  let_next_start();
+  wait_for_previous();
+  const uint32_t groups = kThreads / lanes, group = threadIdx.x / lanes, lane = threadIdx.x % lanes;
+  const uint32_t rows = (uint32_t)a.e.rows, tile0 = blockIdx.x * groups;
+  for (uint32_t i = threadIdx.x; i < groups * (kTile + 2); i += kThreads) {
+    const int64_t at = (int64_t)(tile0 + i / (kTile + 2)) * kTile + i % (kTile + 2) - 1;
+    keys[i] = at >= 0 && at < rows ? a.key[at] : 0xFFFFFFFFu;
+  }
+  for (uint32_t i = threadIdx.x; i < groups * kTile; i += kThreads) {
+    const uint64_t at = (uint64_t)tile0 * kTile + i;
+    poss[i] = at < rows ? a.pos[at] : 0;
   }
   __syncthreads();
-  float* part = a.partial + (uint64_t)blockIdx.x * 2 * a.e.width;
-  for (uint32_t c = threadIdx.x; c < a.e.width; c += kThreads) {
-    float sum = 0.0f;
-    bool began = key[0] != key[1];  // the token's first row lies in this tile
-    for (uint32_t k = 0; k < count; ++k) {
-      const uint32_t now = key[k + 1];
-      if (now >= a.e.vocab) break;  // sorted behind all tokens
-      sum += to_f32(static_cast<const S*>(a.e.src)[(uint64_t)pos[k] * a.e.lds + c]);
-      if (now == key[k + 2]) {
-        if (k + 1 == count) part[began ? a.e.width + c : c] = sum;
-        continue;
+  const uint32_t tile = tile0 + group;
+  if (tile >= a.tiles) return;
+  const uint32_t *key = keys + group * (kTile + 2) + 1, *pos = poss + group * kTile;
+  const uint32_t count = min(kTile, rows - tile * kTile), last = key[count - 1];
+  if (lane == 0 && last < a.e.vocab && key[count] == last && (key[0] != last || key[-1] != last))
+    a.runs[1 + atomicAdd(a.runs, 1u)] = tile;
+  float* part = a.partial + (uint64_t)tile * 2 * a.e.width;
+  for (uint32_t c = lane * N; c < a.e.width; c += lanes * N) {
+    float sum[N] = {};
+    bool began = key[-1] != key[0];  // the token's first row lies in this tile
+    for (uint32_t k = 0; k < count; k += kAhead) {
+      Piece<S, N> piece[kAhead];
+#pragma unroll
+      for (uint32_t i = 0; i < kAhead; ++i)
+        if (k + i < count && key[k + i] < a.e.vocab)
+          piece[i].load(static_cast<const S*>(a.e.src) + (uint64_t)pos[k + i] * a.e.lds + c);
+#pragma unroll
+      for (uint32_t i = 0; i < kAhead; ++i) {
+        if (k + i >= count || key[k + i] >= a.e.vocab) break;
+        piece[i].add_to(sum);
+        if (key[k + i] == key[k + i + 1]) {
+          if (k + i + 1 == count) write_n<float, N>(part + (began ? a.e.width : 0) + c, sum);
+          continue;
+        }
+        if (began) put_sum<D, N>(a, key[k + i], c, sum);
+        else write_n<float, N>(part + c, sum);
+#pragma unroll
+        for (int j = 0; j < N; ++j) sum[j] = 0.0f;
+        began = true;
       }
-      if (began) put_sum<D>(a, now, c, sum);
-      else part[c] = sum;
-      sum = 0.0f;
-      began = true;
     }
   }
 }
 
-// Tokens over several tiles: the block of the tile where one begins adds up its partial rows, in the tiles' order.
-template <typename D>
-__global__ void __launch_bounds__(kThreads) join_kernel(const SumArgs a) {
-  const uint32_t rows = (uint32_t)a.e.rows, last = min(rows, (blockIdx.x + 1) * kTile) - 1, first = blockIdx.x * kTile;
-  const uint32_t key = a.key[last];
-  if (key >= a.e.vocab || last + 1 >= rows || a.key[last + 1] != key) return;       // ends here
-  if (a.key[first] == key && first > 0 && a.key[first - 1] == key) return;          // began before
-  for (uint32_t c = threadIdx.x; c < a.e.width; c += kThreads) {
-    float sum = a.partial[((uint64_t)blockIdx.x * 2 + 1) * a.e.width + c];
-    for (uint32_t t = blockIdx.x + 1; t < a.tiles && a.key[t * kTile] == key; ++t)
-      sum += a.partial[(uint64_t)t * 2 * a.e.width + c];
-    put_sum<D>(a, key, c, sum);
+// Tokens over several tiles: a block adds up one's partial rows, in the tiles'
+// order: each of its groups of `lanes` threads a stretch of them, then the stretches.
+constexpr uint32_t kJoinThreads = 512;
+
+template <typename D, int N>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const SumArgs a, uint32_t lanes) {
+  __shared__ float stretch[kJoinThreads * N];
+  wait_for_previous();
+  const uint32_t groups = kJoinThreads / lanes, group = threadIdx.x / lanes, lane = threadIdx.x % lanes;
+  const uint32_t runs = *a.runs;
+  for (uint32_t r = blockIdx.x; r < runs; r += gridDim.x) {
+    const uint32_t tile = a.runs[1 + r], key = a.key[(uint64_t)tile * kTile + kTile - 1];
+    uint32_t lo = tile, hi = a.tiles;  // the last tile that begins with this token: 32 probes at a time
+    while (hi - lo > 1) {
+      const uint32_t step = (hi - lo + 31) / 32, probe = lo + threadIdx.x % 32 * step;
+      const uint32_t at_most = __ballot_sync(~0u, probe == lo || (probe < hi && a.key[(uint64_t)probe * kTile] <= key));
+      lo += (31 - __clz(at_most)) * step;
+      hi = min(hi, lo + step);
+    }
+    const uint32_t each = (lo - tile + groups - 1) / groups, first = tile + 1 + group * each, end = min(lo + 1, first + each);
+    for (uint32_t c0 = 0; c0 < a.e.width; c0 += lanes * N) {
+      const uint32_t c = c0 + lane * N;
+      float sum[N] = {};
+      if (c < a.e.width) {
+#pragma unroll 4
+        for (uint32_t t = first; t < end; ++t) {
+          float f[N];
+          read_floats<N>(a.partial + (uint64_t)t * 2 * a.e.width + c, f);
+#pragma unroll
+          for (int j = 0; j < N; ++j) sum[j] += f[j];
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < N; ++j) stretch[j * kJoinThreads + threadIdx.x] = sum[j];
+      __syncthreads();
+      if (group == 0 && c < a.e.width) {
+        read_floats<N>(a.partial + ((uint64_t)tile * 2 + 1) * a.e.width + c, sum);
+        for (uint32_t g = 0; g < groups; ++g)
+#pragma unroll
+          for (int j = 0; j < N; ++j) sum[j] += stretch[j * kJoinThreads + g * lanes + lane];
+        put_sum<D, N>(a, key, c, sum);
+      }
+    }
   }
 }
 
 uint64_t align256(uint64_t x) { return (x + 255) / 256 * 256; }
+uint32_t div_up(uint64_t a, uint32_t b) { return (uint32_t)((a + b - 1) / b); }
+
+// Whether every row of a matrix allows pieces of 16 bytes of type size `size`.
+bool rows_of_16(const void* p, uint64_t ld, uint32_t width, uint32_t size) {
+  return ((uintptr_t)p | (ld * size) | (uint64_t)width * size) % 16 == 0;
+}
+
+template <typename S, typename D, int N>
+cudaError_t launch_sums(const SumArgs& a, cudaStream_t st) {
+  uint32_t lanes = 32;
+  while (lanes < kThreads && lanes * N < a.e.width) lanes *= 2;
+  cudaError_t e = launch_after(sum_kernel<S, D, N>, div_up(a.tiles, kThreads / lanes), kThreads, st, a, lanes);
+  if (e != cudaSuccess) return e;
+  const uint32_t blocks = a.tiles < 608 ? a.tiles : 608;
+  return launch_after(join_kernel<D, N>, blocks, kJoinThreads, st, a, lanes);
+}
 
 template <typename S, typename D>
-cudaError_t launch_sums(const SumArgs& a, cudaStream_t st) {
-  if (!a.e.accumulate) {
-    cudaError_t e = cudaMemset2DAsync(a.e.dst, a.e.ldd * sizeof(D), 0, a.e.width * sizeof(D), a.e.vocab, st);
+cudaError_t launch_grad(const EmbedArgs& a, void* workspace, cudaStream_t st) {
+  char* at = static_cast<char*>(workspace);
+  const auto take = [&](uint64_t bytes) {
+    char* p = at;
+    at += align256(bytes);
+    return p;
+  };
+  const uint32_t rows = (uint32_t)a.rows, tiles = div_up(rows, kTile);
+  SortArgs s = {};
+  s.rows = rows;
+  s.vocab = a.vocab;
+  s.tile = div_up(div_up(rows, kMaxSortTiles), kSortThreads) * kSortThreads;
+  if (s.tile < 2 * kSortThreads) s.tile = 2 * kSortThreads;
+  s.tiles = div_up(rows, s.tile);
+  s.fill = a.dst;
+  s.ld = a.ldd;
+  s.width = a.width;
+  uint32_t *key[2] = {}, *pos[2] = {};
+  if (rows) {
+    for (uint32_t k = 0; k < 2; ++k) {
+      key[k] = (uint32_t*)take(4 * a.rows);
+      pos[k] = (uint32_t*)take(4 * a.rows);
+    }
+    s.hist = (uint32_t*)take(4ull * kBins * kMaxSortTiles);
+    s.runs = (uint32_t*)take(4ull * (tiles + 1));
+  }
+  uint32_t passes = rows ? 1 : 0;
+  while (passes && passes * kBits < 32 && (a.vocab >> (passes * kBits))) ++passes;
+  const bool small = rows && rows <= kSmallSort;
+  const uint32_t launches = passes && !small ? 2 * passes : 1;
+  const uint64_t fill_bytes = a.accumulate ? 0 : (uint64_t)a.vocab * a.width * sizeof(D);
+  const uint64_t most = fill_bytes / launches / (16 * kSortThreads) + 1;  // blocks with 16 bytes a thread to clear
+  const uint32_t fillers = a.accumulate ? 0 : most < 456 ? (uint32_t)most : 456;
+  uint32_t from = 0;
+  for (uint32_t l = 0; l < launches; ++l) {
+    s.tokens = l < 2 ? a.tokens : nullptr;
+    s.shift = l / 2 * kBits;
+    s.key_in = key[from];
+    s.pos_in = pos[from];
+    s.key_out = key[1 - from];
+    s.pos_out = pos[1 - from];
+    s.fill_first = (uint32_t)((uint64_t)a.vocab * l / launches);
+    s.fill_end = (uint32_t)((uint64_t)a.vocab * (l + 1) / launches);
+    if (s.tiles + fillers == 0) continue;
+    // The first launch waits for all earlier work: the gradient may be in use.
+    const cudaError_t e = small  ? launch_plain(sort_small<D>, s.tiles + fillers, kSortThreads, st, s)
+                          : l == 0 ? launch_plain(sort_count<D>, s.tiles + fillers, kSortThreads, st, s)
+                          : l % 2 ? launch_after(sort_place<D>, s.tiles + fillers, kSortThreads, st, s)
+                                  : launch_after(sort_count<D>, s.tiles + fillers, kSortThreads, st, s);
     if (e != cudaSuccess) return e;
+    if (small || l % 2) from = 1 - from;
   }
-  if (a.e.rows == 0) return cudaSuccess;
-  sum_kernel<S, D><<<a.tiles, kThreads, 0, st>>>(a);
-  join_kernel<D><<<a.tiles, kThreads, 0, st>>>(a);
-  return cudaGetLastError();
+  if (rows == 0) return cudaSuccess;
+  const SumArgs m = {a, key[from], pos[from], (float*)at, s.runs, tiles};
+  constexpr int kN = Vec<S>::kWidth;
+  const bool wide = rows_of_16(a.src, a.lds, a.width, sizeof(S)) && rows_of_16(a.dst, a.ldd, a.width, sizeof(D));
+  return wide ? launch_sums<S, D, kN>(m, st) : launch_sums<S, D, 1>(m, st);
 }
 
 template <typename S>
-cudaError_t launch_sums_from(const SumArgs& a, cudaStream_t st) {
-  switch (a.e.dst_dtype) {
-    case BF_BF16: return launch_sums<S, __nv_bfloat16>(a, st);
-    case BF_F16: return launch_sums<S, __half>(a, st);
-    default: return launch_sums<S, float>(a, st);
+cudaError_t launch_grad_from(const EmbedArgs& a, void* workspace, cudaStream_t st) {
+  switch (a.dst_dtype) {
+    case BF_BF16: return launch_grad<S, __nv_bfloat16>(a, workspace, st);
+    case BF_F16: return launch_grad<S, __half>(a, workspace, st);
+    default: return launch_grad<S, float>(a, workspace, st);
   }
 }
 
-template <typename S>
+template <typename E, int N>
+cudaError_t launch_embed_pieces(const EmbedArgs& a, cudaStream_t st) {
+  const uint32_t per_row = div_up(a.width, N);
+  const uint64_t pieces = a.rows * per_row, blocks = (pieces + kThreads * kPieces - 1) / (kThreads * kPieces);
+  if (blocks > 0x7FFFFFFFu) return cudaErrorInvalidValue;
+  if (pieces + kThreads * kPieces < (1ull << 32))
+    return launch_plain(embed_kernel<E, N, uint32_t>, (uint32_t)blocks, kThreads, st, a, (uint32_t)pieces, per_row);
+  return launch_plain(embed_kernel<E, N, uint64_t>, (uint32_t)blocks, kThreads, st, a, pieces, per_row);
+}
+
+template <typename E>
 cudaError_t launch_embed_typed(const EmbedArgs& a, cudaStream_t st) {
-  const uint32_t grid = (uint32_t)(a.rows < (1u << 30) ? a.rows : (1u << 30));
-  embed_kernel<S, S><<<grid, kThreads, 0, st>>>(a);
-  return cudaGetLastError();
+  return rows_of_16(a.src, a.lds, a.width, sizeof(E)) && rows_of_16(a.dst, a.ldd, a.width, sizeof(E))
+             ? launch_embed_pieces<E, Vec<E>::kWidth>(a, st) : launch_embed_pieces<E, 1>(a, st);
 }
 
 }  // namespace
@@ -220,35 +532,17 @@ cudaError_t launch_embed(const EmbedArgs& a, cudaStream_t st) {
 }
 
 uint64_t embed_grad_bytes(uint64_t rows, uint32_t width) {
-  const uint64_t sort_tiles = (rows + kSortTile - 1) / kSortTile, tiles = (rows + kTile - 1) / kTile;
-  return 4 * align256(4 * rows) + align256(4 * kBins * sort_tiles) + align256(4 * 2 * tiles * width);
+  if (rows == 0) return 0;
+  const uint64_t tiles = (rows + kTile - 1) / kTile;
+  return 4 * align256(4 * rows) + align256(4ull * kBins * kMaxSortTiles) + align256(4 * (tiles + 1)) +
+         align256(4 * 2 * tiles * width);
 }
 
 cudaError_t launch_embed_grad(const EmbedArgs& a, void* workspace, cudaStream_t st) {
-  char* at = static_cast<char*>(workspace);
-  const auto take = [&](uint64_t bytes) {
-    char* p = at;
-    at += align256(bytes);
-    return p;
-  };
-  const uint32_t rows = (uint32_t)a.rows, sort_tiles = (rows + kSortTile - 1) / kSortTile;
-  uint32_t* key[2] = {(uint32_t*)take(4 * a.rows), (uint32_t*)take(4 * a.rows)};
-  uint32_t* pos[2] = {(uint32_t*)take(4 * a.rows), (uint32_t*)take(4 * a.rows)};
-  uint32_t* hist = (uint32_t*)take(4ull * kBins * sort_tiles);
-  uint32_t from = 0;
-  for (uint32_t shift = 0; rows && (shift == 0 || (shift < 32 && (a.vocab >> shift))); shift += 8) {
-    const SortArgs s = {shift == 0 ? a.tokens : nullptr, key[from], pos[from], key[1 - from], pos[1 - from], hist, rows,
-                        sort_tiles, shift, a.vocab};
-    sort_count<<<sort_tiles, kThreads, 0, st>>>(s);
-    sort_scan<<<1, 1024, 0, st>>>(hist, kBins * sort_tiles);
-    sort_place<<<sort_tiles, kThreads, 0, st>>>(s);
-    from = 1 - from;
-  }
-  const SumArgs s = {a, key[from], pos[from], (float*)at, (rows + kTile - 1) / kTile};
   switch (a.src_dtype) {
-    case BF_BF16: return launch_sums_from<__nv_bfloat16>(s, st);
-    case BF_F16: return launch_sums_from<__half>(s, st);
-    default: return launch_sums_from<float>(s, st);
+    case BF_BF16: return launch_grad_from<__nv_bfloat16>(a, workspace, st);
+    case BF_F16: return launch_grad_from<__half>(a, workspace, st);
+    default: return launch_grad_from<float>(a, workspace, st);
   }
 }
 

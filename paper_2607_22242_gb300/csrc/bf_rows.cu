@@ -361,29 +361,6 @@ WideShape wide_shape(uint64_t rows, uint32_t vectors, bool scores) {
   return s;
 }
 
-// A launch that may start before the call's previous kernel ends (kFollows), with clusters of `cluster` blocks.
-template <RowOp op, typename K, typename... Args>
-cudaError_t launch(K kernel, uint64_t blocks, uint32_t threads, uint32_t cluster, cudaStream_t st, Args... args) {
-  if (blocks > 0x7FFFFFFFu) return cudaErrorInvalidValue;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((uint32_t)blocks);
-  cfg.blockDim = dim3(threads);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  cfg.attrs = attr;
-  if (kFollows<op>) {
-    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
-  }
-  if (cluster > 1) {
-    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
-    attr[cfg.numAttrs].val.clusterDim.x = cluster;
-    attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
-    ++cfg.numAttrs;
-  }
-  return cudaLaunchKernelEx(&cfg, kernel, args...);
-}
-
 uint32_t pow2_up(uint32_t n) {
   uint32_t p = 1;
   while (p < n) p *= 2;
@@ -393,7 +370,7 @@ uint32_t pow2_up(uint32_t n) {
 template <RowOp op, bool entropy>
 cudaError_t launch_op(const RowArgs& a, cudaStream_t st) {
   const auto group = [&](auto kernel, uint32_t lanes) {
-    return launch<op>(kernel, (a.rows * lanes + kGroupThreads - 1) / kGroupThreads, kGroupThreads, 1, st, a, lanes);
+    return launch_shaped(kernel, (a.rows * lanes + kGroupThreads - 1) / kGroupThreads, kGroupThreads, 1, kFollows<op>, st, a, lanes);
   };
   // Vectors that a row touches: one more where rows may start inside one.
   const bool aligned = ((uintptr_t)a.x | (uintptr_t)(a.ldx * sizeof(E))) % 16 == 0;
@@ -403,7 +380,8 @@ cudaError_t launch_op(const RowArgs& a, cudaStream_t st) {
   if (vectors <= 8) return group(warp_kernel<op, entropy, 4>, pow2_up(div_up(vectors, 4)));
   if (vectors <= 256) return group(warp_kernel<op, entropy, 8>, pow2_up(div_up(vectors, 8)));
   const WideShape s = wide_shape(a.rows, vectors, kScores<op>);
-  return launch<op>(wide_kernel<op, entropy>, a.rows * s.cluster, s.threads, s.cluster, st, a, s.cluster, s.tiles);
+  return launch_shaped(wide_kernel<op, entropy>, a.rows * s.cluster, s.threads, s.cluster, kFollows<op>, st, a, s.cluster,
+                       s.tiles);
 }
 
 }  // namespace

@@ -13,6 +13,7 @@
 #pragma once
 
 #include "bf_elem.cuh"
+#include "bf_launches.cuh"
 #include "bf_learn.h"
 
 namespace bfk {
@@ -67,10 +68,6 @@ struct RowOut {
 // kernels before it in the call write is read after wait_for_previous().
 template <RowOp op>
 constexpr bool kFollows = op == RowOp::kPolicy || op == RowOp::kPairScore || op == RowOp::kPairGrad;
-
-__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-// The next kernel of the call may start: it waits for this one's end where it has to.
-__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // The part of a row that the caller's arrays give.
 template <typename E, RowOp op>
