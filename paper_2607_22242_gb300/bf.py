@@ -16,8 +16,10 @@ device is present, these calls raise.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import dataclasses
+import functools
 import itertools
 import os
 from typing import List, NamedTuple, Optional, Sequence, Tuple, Union
@@ -479,9 +481,14 @@ class PreferenceLoss(NamedTuple):
     grad: object
 
 
+_DTYPE_CODES = {}
+
+
 def _dtype_code(dtype) -> Optional[int]:
-    import torch
-    return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(dtype)
+    if not _DTYPE_CODES:
+        import torch
+        _DTYPE_CODES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    return _DTYPE_CODES.get(dtype)
 
 
 def _matrix(t, name: str) -> Matrix:
@@ -490,7 +497,7 @@ def _matrix(t, name: str) -> Matrix:
     code = _dtype_code(t.dtype)
     if code is None or not t.is_cuda or t.dim() != 2:
         raise ValueError(f"{name} must be a 2-D CUDA tensor of float32, bfloat16 or float16")
-    if t.get_device() != torch.cuda.current_device():
+    if t.get_device() != torch._C._cuda_getDevice():
         raise ValueError(f"{name} is on device {t.get_device()} but device {torch.cuda.current_device()} is current")
     rows, cols = t.shape
     stride, inner = t.stride()
@@ -506,20 +513,35 @@ def _vector(t, count: int, dtype, like, name: str) -> int:
     return t.data_ptr()
 
 
+_SAME = contextlib.nullcontext()
+
+
 def _allocate(stream):
     """Context in which results and workspaces belong to `stream` for torch's allocator."""
-    import contextlib
-    import torch
     if stream is None:
-        return contextlib.nullcontext()
+        return _SAME
+    import torch
     return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
 
 
-def _workspace(query, rows: int, groups: int, device):
+def _stream_of(stream, like) -> int:
+    """As _stream_handle, without the object that torch.cuda.current_stream makes (3 us of a call of 20)."""
+    if stream is not None:
+        return _stream_handle(stream)
     import torch
+    return torch._C._cuda_getCurrentRawStream(like.get_device())
+
+
+@functools.lru_cache(maxsize=256)
+def _workspace_bytes(name: str, rows: int, groups: int) -> int:
     need = ctypes.c_uint64(0)
-    _check(query(rows, groups, ctypes.byref(need)))
-    return torch.empty(max(need.value, 1), dtype=torch.uint8, device=device)
+    _check(getattr(load(), name)(rows, groups, ctypes.byref(need)))
+    return max(need.value, 1)
+
+
+def _workspace(name: str, rows: int, groups: int, device):
+    import torch
+    return torch.empty(_workspace_bytes(name, rows, groups), dtype=torch.uint8, device=device)
 
 
 def _grad_like(logits, out, grad: bool):
@@ -541,7 +563,7 @@ def token_logprobs(logits, tokens, *, temperature: float = 1.0, entropy: bool = 
         logprob = torch.empty(x.rows, dtype=torch.float32, device=logits.device)
         h = torch.empty_like(logprob) if entropy else None
     _check(load().bf_token_logprobs(x, y, temperature, logprob.data_ptr(), h.data_ptr() if entropy else None,
-                                    _stream_handle(stream)))
+                                    _stream_of(stream, logits)))
     return (logprob, h) if entropy else logprob
 
 
@@ -555,7 +577,7 @@ def token_logprobs_grad(logits, tokens, grad_logprob, grad_entropy=None, *, temp
     gh = None if grad_entropy is None else _vector(grad_entropy, x.rows, torch.float32, logits, "grad_entropy")
     with _allocate(stream):
         grad = _grad_like(logits, out, True)
-    _check(load().bf_token_logprobs_grad(x, y, temperature, gl, gh, _matrix(grad, "out"), _stream_handle(stream)))
+    _check(load().bf_token_logprobs_grad(x, y, temperature, gl, gh, _matrix(grad, "out"), _stream_of(stream, logits)))
     return grad
 
 
@@ -580,16 +602,16 @@ def policy_loss(logits, tokens, offsets, old_logprob, advantage, ref_logprob=Non
                       _vector(old_logprob, rows, f32, logits, "old_logprob"),
                       None if ref_logprob is None else _vector(ref_logprob, rows, f32, logits, "ref_logprob"),
                       _vector(advantage, rows if advantage_per_token else sequences, f32, logits, "advantage"),
-                      sequences, bool(advantage_per_token), REDUCTIONS[reduction], clip_low, clip_high, kl_coef, entropy_coef, temperature,
-                      grad_scale)
+                      sequences, bool(advantage_per_token), REDUCTIONS[reduction], clip_low, clip_high, kl_coef,
+                      entropy_coef, temperature, grad_scale)
     lib = load()
     with _allocate(stream):
         g = _grad_like(logits, out, grad)
         stats = torch.empty(POLICY_STATS, dtype=f32, device=logits.device)
         logprob = torch.empty(rows, dtype=f32, device=logits.device)
-        work = _workspace(lib.bf_policy_loss_workspace, rows, sequences, logits.device)
+        work = _workspace("bf_policy_loss_workspace", rows, sequences, logits.device)
     _check(lib.bf_policy_loss(x, args, stats.data_ptr(), logprob.data_ptr(), None if g is None else _matrix(g, "out"),
-                              work.data_ptr(), work.numel(), _stream_handle(stream)))
+                              work.data_ptr(), work.numel(), _stream_of(stream, logits)))
     return PolicyLoss(stats, logprob, g)
 
 
@@ -614,10 +636,10 @@ def preference_loss(logits, tokens, offsets, ref_logprob=None, *, beta: float = 
         stats = torch.empty(PREFERENCE_STATS, dtype=f32, device=logits.device)
         rewards = torch.empty(2 * pairs, dtype=f32, device=logits.device)
         logprob = torch.empty(rows, dtype=f32, device=logits.device)
-        work = _workspace(lib.bf_preference_loss_workspace, rows, pairs, logits.device)
+        work = _workspace("bf_preference_loss_workspace", rows, pairs, logits.device)
     _check(lib.bf_preference_loss(x, args, stats.data_ptr(), rewards.data_ptr(), logprob.data_ptr(),
                                   None if g is None else _matrix(g, "out"), work.data_ptr(), work.numel(),
-                                  _stream_handle(stream)))
+                                  _stream_of(stream, logits)))
     return PreferenceLoss(stats, rewards, logprob, g)
 
 
@@ -632,7 +654,7 @@ def embed(table, tokens, *, scale: float = 1.0, out=None, stream=None):
     o = _matrix(out, "out")
     if o.rows != tokens.numel():
         raise ValueError("out must have one row per token")
-    _check(load().bf_embed(w, y, scale, o, _stream_handle(stream)))
+    _check(load().bf_embed(w, y, scale, o, _stream_of(stream, table)))
     return out
 
 
@@ -648,9 +670,9 @@ def embed_grad(grad_out, tokens, vocab: int, *, scale: float = 1.0, out=None, ac
     with _allocate(stream):
         if out is None:
             out = torch.empty(vocab, g.cols, dtype=grad_out.dtype, device=grad_out.device)
-        work = _workspace(lib.bf_embed_grad_workspace, g.rows, g.cols, grad_out.device)
+        work = _workspace("bf_embed_grad_workspace", g.rows, g.cols, grad_out.device)
     o = _matrix(out, "out")
     if o.rows != vocab:
         raise ValueError("out must have one row per token of the vocabulary")
-    _check(lib.bf_embed_grad(g, y, scale, accumulate, o, work.data_ptr(), work.numel(), _stream_handle(stream)))
+    _check(lib.bf_embed_grad(g, y, scale, accumulate, o, work.data_ptr(), work.numel(), _stream_of(stream, grad_out)))
     return out

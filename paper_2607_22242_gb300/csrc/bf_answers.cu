@@ -6,17 +6,6 @@ namespace bfk {
 
 namespace {
 
-// The last s in [0, sequences) with offsets[s] <= row, by halving [lo, hi).
-template <typename T, typename I>
-__device__ __forceinline__ I last_at_or_before(const T* offsets, I lo, I hi, T row) {
-  while (hi - lo > 1) {
-    const I mid = (lo + hi) / 2;
-    if (offsets[mid] <= row) lo = mid;
-    else hi = mid;
-  }
-  return lo;
-}
-
 // Offsets that do not ascend make rows miss their sequence; no read leaves the
 // array.  Counts are sums of whole numbers: their order does not matter.
 
@@ -34,8 +23,7 @@ __global__ void __launch_bounds__(kSmallThreads) small_sequence_kernel(const int
   let_next_start();
   if (threadIdx.x == 0) all = 0;
   for (uint32_t s = threadIdx.x; s <= sequences; s += kSmallThreads) {
-    const int64_t o = offsets[s];
-    begin[s] = o < 0 ? 0u : o > (int64_t)rows ? rows : (uint32_t)o;
+    begin[s] = clamp_offset(offsets[s], rows);
     if (s < sequences) count[s] = 0;
   }
   __syncthreads();
@@ -43,10 +31,7 @@ __global__ void __launch_bounds__(kSmallThreads) small_sequence_kernel(const int
     const uint32_t row = first + threadIdx.x;
     uint32_t seq = kNoSequence;
     if (row < rows) {
-      if (sequences && tokens[row] >= 0) {
-        const uint32_t s = last_at_or_before(begin, 0u, sequences, row);
-        if (begin[s] <= row && row < begin[s + 1]) seq = s;
-      }
+      if (tokens[row] >= 0) seq = sequence_at(begin, sequences, row);
       row_seq[row] = seq;
     }
     const uint32_t same = __match_any_sync(~0u, seq);
@@ -68,8 +53,8 @@ __global__ void __launch_bounds__(kSmallThreads) small_sequence_kernel(const int
 // Any number: counts and seq_tokens are zero at the start.  A block's rows are
 // neighbours, so their sequences are too: one search for its first row by a
 // warp (32 probes at a time), then the offsets from there on in shared memory.
-constexpr uint32_t kRowThreads = 256;
-constexpr uint32_t kOffsets = 2 * kRowThreads;
+constexpr uint32_t kRowThreads = 256, kRowsEach = 4, kBlockRows = kRowThreads * kRowsEach;
+constexpr uint32_t kOffsets = kBlockRows;
 
 __global__ void __launch_bounds__(kRowThreads) sequence_kernel(const int64_t* tokens, uint64_t rows,
                                                                const int64_t* offsets, uint64_t sequences,
@@ -78,8 +63,14 @@ __global__ void __launch_bounds__(kRowThreads) sequence_kernel(const int64_t* to
   __shared__ uint64_t first_seq;
   __shared__ int64_t begin[kOffsets + 1];
   let_next_start();
-  const uint64_t first = (uint64_t)blockIdx.x * kRowThreads, row = first + threadIdx.x;
+  const uint64_t first = (uint64_t)blockIdx.x * kBlockRows;
   const uint32_t lane = threadIdx.x % 32;
+  bool on[kRowsEach];
+#pragma unroll
+  for (uint32_t k = 0; k < kRowsEach; ++k) {
+    const uint64_t row = first + k * kRowThreads + threadIdx.x;
+    on[k] = row < rows && sequences && tokens[row] >= 0;
+  }
   if (threadIdx.x < 32) {
     uint64_t lo = 0, hi = sequences ? sequences : 1;
     while (hi - lo > 1) {
@@ -92,12 +83,15 @@ __global__ void __launch_bounds__(kRowThreads) sequence_kernel(const int64_t* to
   }
   __syncthreads();
   const uint64_t s0 = first_seq;
-  const uint32_t held = (uint32_t)min((uint64_t)kOffsets, sequences - (sequences ? s0 : 0));
+  const uint32_t held = sequences ? (uint32_t)min((uint64_t)kOffsets, sequences - s0) : 0;
   for (uint32_t i = threadIdx.x; i <= held; i += kRowThreads) begin[i] = offsets[s0 + i];
   __syncthreads();
-  uint32_t seq = kNoSequence;
-  if (row < rows) {
-    if (sequences && tokens[row] >= 0) {
+  uint32_t scored = 0, opened = 0;
+#pragma unroll
+  for (uint32_t k = 0; k < kRowsEach; ++k) {
+    const uint64_t row = first + k * kRowThreads + threadIdx.x;
+    uint32_t seq = kNoSequence;
+    if (on[k]) {
       const uint32_t i = last_at_or_before(begin, 0u, held + 1, (int64_t)row);
       if (i < held) {
         if (begin[i] <= (int64_t)row) seq = (uint32_t)(s0 + i);
@@ -106,25 +100,30 @@ __global__ void __launch_bounds__(kRowThreads) sequence_kernel(const int64_t* to
         if (offsets[s] <= (int64_t)row && (int64_t)row < offsets[s + 1]) seq = (uint32_t)s;
       }
     }
-    row_seq[row] = seq;
+    if (row < rows) row_seq[row] = seq;
+    scored += __popc(__ballot_sync(~0u, seq != kNoSequence));
+    if (per_sequence) {
+      const uint32_t same = __match_any_sync(~0u, seq);
+      const bool opens = seq != kNoSequence && lane == (uint32_t)__ffs(same) - 1 &&
+                         atomicAdd(&seq_tokens[seq], (uint32_t)__popc(same)) == 0u;
+      opened += __popc(__ballot_sync(~0u, opens));
+    }
   }
-  bool opens = false;
-  if (per_sequence) {
-    const uint32_t same = __match_any_sync(~0u, seq);
-    opens = seq != kNoSequence && lane == (uint32_t)__ffs(same) - 1 &&
-            atomicAdd(&seq_tokens[seq], (uint32_t)__popc(same)) == 0u;
+  __shared__ uint32_t sums[2];
+  if (threadIdx.x < 2) sums[threadIdx.x] = 0;
+  __syncthreads();
+  if (lane == 0) {
+    atomicAdd(&sums[0], scored);
+    atomicAdd(&sums[1], opened);
   }
-  const uint32_t scored = __syncthreads_count(seq != kNoSequence), opened = __syncthreads_count(opens);
+  __syncthreads();
   if (threadIdx.x == 0) {
-    if (scored) atomicAdd(&counts->tokens, scored);
-    if (opened) atomicAdd(&counts->sequences, opened);
+    if (sums[0]) atomicAdd(&counts->tokens, sums[0]);
+    if (sums[1]) atomicAdd(&counts->sequences, sums[1]);
   }
 }
 
-// One block per pair, half of it per answer: the rewards beta * sum (lp - ref)
-// of both answers (or of their means), the loss of their gap
-//   h = reward_0 - reward_1 - margin,  l = -(1 - eps) ln sigma(h) - eps ln sigma(-h)
-// and the slopes of the mean loss in each answer's log-probabilities.
+// One block per pair, half of it per answer.
 constexpr uint32_t kPairThreads = 512;
 
 __global__ void __launch_bounds__(kPairThreads) pair_kernel(const PairArgs a) {
@@ -152,36 +151,15 @@ __global__ void __launch_bounds__(kPairThreads) pair_kernel(const PairArgs a) {
     }
     __syncthreads();
     if (threadIdx.x == 0) {
-      float share[2], reward[2];
-      for (uint32_t k = 0; k < 2; ++k) {
-        const uint32_t n = a.average ? a.seq_tokens[2 * p + k] : 0;
-        share[k] = a.beta * (n ? 1.0f / (float)n : 1.0f);
-        reward[k] = share[k] * sum[k];
-        a.rewards[2 * p + k] = reward[k];
-      }
-      const float h = reward[0] - reward[1] - a.margin, eps = a.label_smoothing;
-      const float tail = log1pf(expf(-fabsf(h)));  // ln(1 + e^-|h|)
-      const float loss = (1.0f - eps) * (fmaxf(-h, 0.0f) + tail) + eps * (fmaxf(h, 0.0f) + tail);
-      const float slope = (eps / (1.0f + expf(-h)) - (1.0f - eps) / (1.0f + expf(h))) * a.grad_scale / (float)a.pairs;
-      a.seq_slope[2 * p] = slope * share[0];
-      a.seq_slope[2 * p + 1] = -slope * share[1];
-      a.partial[p] = loss;
+      const uint32_t n[2] = {a.average ? a.seq_tokens[2 * p] : 0, a.average ? a.seq_tokens[2 * p + 1] : 0};
+      finish_pair(a, p, sum, n);
     }
   }
   bool last = false;
   if (threadIdx.x < 32) last = last_to_say(&a.counts->blocks_done, gridDim.x);
   if (__syncthreads_or(last)) {
     last_sees();
-    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (uint64_t p = threadIdx.x; p < a.pairs; p += kPairThreads) {
-      const float r0 = __ldcg(a.rewards + 2 * p), r1 = __ldcg(a.rewards + 2 * p + 1);
-      v[0] += __ldcg(a.partial + p);
-      v[1] += r0 > r1 ? 1.0f : 0.0f;
-      v[2] += r0;
-      v[3] += r1;
-    }
-    const float total = block_sums(v, buf);
-    if (threadIdx.x < 4) a.stats[threadIdx.x] = total / (float)a.pairs;
+    preference_stats(a, buf);
   }
 }
 
@@ -198,7 +176,7 @@ cudaError_t launch_row_sequences(const int64_t* tokens, uint64_t rows, const int
   // counts and seq_tokens stand side by side (bf_capi_learn.cu)
   cudaError_t e = cudaMemsetAsync(counts, 0, sizeof(RowCounts) + (per_sequence ? sizeof(uint32_t) * sequences : 0), st);
   if (e != cudaSuccess) return e;
-  sequence_kernel<<<(uint32_t)((rows + kRowThreads - 1) / kRowThreads), kRowThreads, 0, st>>>(
+  sequence_kernel<<<(uint32_t)((rows + kBlockRows - 1) / kBlockRows), kRowThreads, 0, st>>>(
       tokens, rows, offsets, sequences, row_seq, seq_tokens, counts, per_sequence);
   return cudaGetLastError();
 }

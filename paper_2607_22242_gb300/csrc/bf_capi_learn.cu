@@ -231,8 +231,11 @@ int bf_policy_loss(const bf_matrix* logits, const bf_policy_args* args, float* d
   a.grad_scale = args->grad_scale;
   a.partial = ws.partial;
   a.stats = d_stats;
-  cudaError_t e = bfk::launch_row_sequences(args->tokens, rows, args->offsets, sequences,
-                                            args->reduction == BF_MEAN_SEQUENCES, ws.row_seq, ws.seq_tokens, ws.counts, st);
+  bool done = false;
+  cudaError_t e = bfk::launch_few(a, nullptr, args->offsets, sequences, &done, st);
+  if (done || e != cudaSuccess) return e == cudaSuccess ? BF_OK : cuda_fail(e, who);
+  e = bfk::launch_row_sequences(args->tokens, rows, args->offsets, sequences,
+                                args->reduction == BF_MEAN_SEQUENCES, ws.row_seq, ws.seq_tokens, ws.counts, st);
   if (e == cudaSuccess) e = bfk::launch_rows(RowOp::kPolicy, a, st);
   return e == cudaSuccess ? BF_OK : cuda_fail(e, who);
 }
@@ -267,10 +270,33 @@ int bf_preference_loss(const bf_matrix* logits, const bf_preference_args* args, 
   const Layout ws(d_workspace, rows, 2 * pairs, true);
   BF_TRY(check_workspace(d_workspace, workspace_bytes, ws.bytes, who));
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  RowArgs a = row_args(logits, args->tokens, args->temperature, grad);
+  a.logprob = d_logprob ? d_logprob : ws.logprob;
+  PairArgs p = {};
+  p.offsets = args->offsets;
+  p.pairs = pairs;
+  p.rows = rows;
+  p.row_seq = ws.row_seq;
+  p.seq_tokens = ws.seq_tokens;
+  p.counts = ws.counts;
+  p.logprob = a.logprob;
+  p.ref_logprob = args->ref_logprob;
+  p.beta = args->beta;
+  p.label_smoothing = args->label_smoothing;
+  p.margin = args->margin;
+  p.grad_scale = args->grad_scale;
+  p.average = args->average;
+  p.seq_slope = ws.seq_slope;
+  p.rewards = d_rewards;
+  p.partial = ws.partial;
+  p.stats = d_stats;
   cudaError_t e = cudaSuccess;
-  RowArgs a = row_args(logits, args->tokens, args->temperature, nullptr);
+  if (rows && pairs) {
+    bool done = false;
+    e = bfk::launch_few(a, &p, args->offsets, 2 * pairs, &done, st);
+    if (done || e != cudaSuccess) return e == cudaSuccess ? BF_OK : cuda_fail(e, who);
+  }
   if (rows) {
-    a.logprob = d_logprob ? d_logprob : ws.logprob;
     a.row_seq = ws.row_seq;
     a.row_softmax = ws.row_softmax;
     e = bfk::launch_row_sequences(args->tokens, rows, args->offsets, 2 * pairs, args->average != 0, ws.row_seq,
@@ -280,31 +306,9 @@ int bf_preference_loss(const bf_matrix* logits, const bf_preference_args* args, 
     e = cudaMemsetAsync(ws.counts, 0, sizeof(RowCounts) + 8 * pairs, st);
   }
   if (e == cudaSuccess && pairs == 0) e = cudaMemsetAsync(d_stats, 0, sizeof(float) * BF_PREFERENCE_STATS, st);
-  if (e == cudaSuccess && pairs) {
-    PairArgs p = {};
-    p.offsets = args->offsets;
-    p.pairs = pairs;
-    p.rows = rows;
-    p.row_seq = ws.row_seq;
-    p.seq_tokens = ws.seq_tokens;
-    p.counts = ws.counts;
-    p.logprob = a.logprob;
-    p.ref_logprob = args->ref_logprob;
-    p.beta = args->beta;
-    p.label_smoothing = args->label_smoothing;
-    p.margin = args->margin;
-    p.grad_scale = args->grad_scale;
-    p.average = args->average;
-    p.seq_slope = ws.seq_slope;
-    p.rewards = d_rewards;
-    p.partial = ws.partial;
-    p.stats = d_stats;
-    e = bfk::launch_pairs(p, st);
-  }
+  if (e == cudaSuccess && pairs) e = bfk::launch_pairs(p, st);
   if (e == cudaSuccess && grad && rows) {
     a.logprob = nullptr;
-    a.g = grad->data;
-    a.ldg = grad->row_stride;
     a.seq_slope = ws.seq_slope;
     e = bfk::launch_rows(RowOp::kPairGrad, a, st);
   }

@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place(const SortArgs a) {
   wait_for_previous();
   // Thread d: the digit's items in all tiles and in those before this one.
   uint32_t all = 0, before = 0;
-#pragma unroll 8
+#pragma unroll 16
   for (uint32_t t = 0; t < a.tiles; ++t) {
     const uint32_t n = a.hist[t * kBins + threadIdx.x];
     all += n;
@@ -320,7 +320,7 @@ __device__ __forceinline__ void put_sum(const SumArgs& a, uint32_t key, uint32_t
 // `lanes` threads per tile, N columns a thread at a time; kAhead rows are read
 // before they are added, whatever tokens they belong to.
 template <typename S, typename D, int N>
-__global__ void __launch_bounds__(kThreads) sum_kernel(const SumArgs a, uint32_t lanes) {
+__global__ void __launch_bounds__(kThreads, N == 8 ? 3 : 4) sum_kernel(const SumArgs a, uint32_t lanes) {
   constexpr uint32_t kAhead = 8;
   __shared__ uint32_t keys[kThreads / 32 * (kTile + 2)];  // with the neighbours on both sides
   __shared__ uint32_t poss[kThreads / 32 * kTile];

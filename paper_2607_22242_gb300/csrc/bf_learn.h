@@ -89,6 +89,21 @@ inline cudaError_t launch_rows(RowOp op, const RowArgs& a, cudaStream_t st) {
 }
 cudaError_t launch_pairs(const PairArgs& a, cudaStream_t st);
 
+// A whole loss (the preference loss with `p`, else the policy loss) in one
+// launch, where its rows are few and short; *done tells whether they were.
+cudaError_t launch_few_type0(const RowArgs& a, const PairArgs* p, const int64_t* offsets, uint64_t sequences, bool* done,
+                             cudaStream_t st);
+cudaError_t launch_few_type1(const RowArgs& a, const PairArgs* p, const int64_t* offsets, uint64_t sequences, bool* done,
+                             cudaStream_t st);
+cudaError_t launch_few_type2(const RowArgs& a, const PairArgs* p, const int64_t* offsets, uint64_t sequences, bool* done,
+                             cudaStream_t st);
+inline cudaError_t launch_few(const RowArgs& a, const PairArgs* p, const int64_t* offsets, uint64_t sequences, bool* done,
+                              cudaStream_t st) {
+  return a.dtype == BF_F32 ? launch_few_type0(a, p, offsets, sequences, done, st)
+         : a.dtype == BF_BF16 ? launch_few_type1(a, p, offsets, sequences, done, st)
+                              : launch_few_type2(a, p, offsets, sequences, done, st);
+}
+
 struct EmbedArgs {
   const void* src;  // embed: the table; gradient: the gradient of the output rows
   void* dst;        // embed: the output rows; gradient: the table's gradient

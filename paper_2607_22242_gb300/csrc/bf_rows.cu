@@ -31,7 +31,18 @@ constexpr bool kMoment = op == RowOp::kPolicy || entropy;
 template <RowOp op>
 constexpr bool kScores = op == RowOp::kScore || op == RowOp::kPairScore;
 
-// The policy loss from its parts' sums, in an order that does not depend on when blocks ran.
+// The policy loss from its sums, the k-th in lane k of the calling warp.
+__device__ __forceinline__ void put_policy_stats(const RowArgs& a, float total) {
+  const float surrogate = __shfl_sync(~0u, total, 0), kl = __shfl_sync(~0u, total, 1), h = __shfl_sync(~0u, total, 2);
+  if (threadIdx.x == 0) {
+    a.stats[0] = -surrogate + a.kl_coef * kl - a.entropy_coef * h;
+    a.stats[1] = -surrogate;
+  } else if (threadIdx.x < kPolicySums) {
+    a.stats[threadIdx.x + 1] = total;
+  }
+}
+
+// The same from its parts' sums, in an order that does not depend on when blocks ran.
 __device__ __forceinline__ void policy_stats(const RowArgs& a, uint64_t parts, float* buf) {
   last_sees();
   float v[kPolicySums] = {};
@@ -40,13 +51,7 @@ __device__ __forceinline__ void policy_stats(const RowArgs& a, uint64_t parts, f
     for (uint32_t k = 0; k < kPolicySums; ++k) v[k] += __ldcg(a.partial + k * parts + i);
   }
   const float total = block_sums(v, buf);
-  const float surrogate = __shfl_sync(~0u, total, 0), kl = __shfl_sync(~0u, total, 1), h = __shfl_sync(~0u, total, 2);
-  if (threadIdx.x == 0) {
-    a.stats[0] = -surrogate + a.kl_coef * kl - a.entropy_coef * h;
-    a.stats[1] = -surrogate;
-  } else if (threadIdx.x < kPolicySums) {
-    a.stats[threadIdx.x + 1] = total;
-  }
+  if (threadIdx.x < 32) put_policy_stats(a, total);
 }
 
 // (x - m) c2 as (x - base) c2 - r: with base = 0 and r = m c2 rounded it is one
@@ -119,7 +124,7 @@ __device__ __forceinline__ void put(const Window<E>& x, const Window<E>& g, uint
   else g.store_cut(v, x.shift, d);
 }
 
-// ---- the shortest rows (three modes): a thread per row, N elements at most ----
+// ---- the shortest rows (three modes): a thread for each, N elements at most ----
 
 constexpr uint32_t kGroupThreads = 256;
 
@@ -137,25 +142,24 @@ __device__ __forceinline__ bool say_policy_part(const RowArgs& a, const RowOut& 
 }
 
 template <RowOp op, int N>
-__global__ void __launch_bounds__(kGroupThreads) short_kernel(const RowArgs a, uint32_t) {
+__global__ void __launch_bounds__(kGroupThreads) short_kernel(const RowArgs a) {
   const uint64_t row = (uint64_t)blockIdx.x * kGroupThreads + threadIdx.x;
   const bool here = row < a.rows;
   if constexpr (kFollows<op>) let_next_start();
   RowIn in = {};
-  if (here) in = load_row<E, op>(a, row);
-  const E* x = static_cast<const E*>(a.x) + row * a.ldx;
   float v[N];
+  const E* x = static_cast<const E*>(a.x) + row * a.ldx;
 #pragma unroll
-  for (uint32_t j = 0; j < N; ++j) v[j] = in.on && j < a.vocab ? to_f32(x[j]) : kMinusInf;
-  RowSums r = {};
+  for (uint32_t j = 0; j < N; ++j) v[j] = here && j < a.vocab ? to_f32(x[j]) : kMinusInf;
+  if (here) in = load_row<E, op>(a, row);
+  RowSums r = {v[0], 0.0f, 0.0f};
   if constexpr (op != RowOp::kPairGrad) {
-    r.m = v[0];
 #pragma unroll
-    for (int i = 1; i < N; ++i) r.m = fmaxf(r.m, v[i]);
+    for (int j = 1; j < N; ++j) r.m = fmaxf(r.m, v[j]);
     const float ref = usable_max(r.m);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float t = (v[i] - ref) * a.c2, e = exp2_fast(t);
+    for (int j = 0; j < N; ++j) {
+      const float t = (v[j] - ref) * a.c2, e = exp2_fast(t);
       r.s += e;
       r.q = fmaf(e, finite_t(t), r.q);
     }
@@ -238,8 +242,14 @@ constexpr uint32_t kWideThreads = 512;
 constexpr uint32_t kMaxCluster = 8;
 constexpr int kWideVectors = 8;  // a thread's vectors of a tile
 
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  __syncwarp();
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 // Store to the same shared variable of the cluster's block `rank`.
 __device__ __forceinline__ void cluster_store(float* p, uint32_t rank, float v) {
   uint32_t here = (uint32_t)__cvta_generic_to_shared(p), there;
@@ -267,7 +277,7 @@ __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, 
     for (uint32_t tile = 0; tile < tiles; ++tile) {
       if (op == RowOp::kPairGrad && tile + 1 < tiles) continue;
 #pragma unroll
-      for (int k = 0; k < NV; ++k) u[k] = x.load(first + (tile * NV + k) * threads, kScores<op> || tile + 1 == tiles);
+      for (int k = 0; k < NV; ++k) u[k] = x.load(first + (tile * NV + k) * threads, op == RowOp::kScore || (op != RowOp::kPairScore && tile + 1 == tiles));
       if constexpr (op != RowOp::kPairGrad) {
         const RowSums now = sums_of<NV, kMoment<op, entropy>>(u, a.c2);
         r = tiles > 1 ? join(r, now, a.c2) : now;
@@ -345,6 +355,119 @@ __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, 
   }
 }
 
+// ---- few rows of short answers: a loss in one launch, by one cluster ----
+
+// Up to 8 blocks hold all rows in registers, as the warp kernel does, from
+// their sums to their gradient; each block counts the sequences' scored rows for
+// itself, and the blocks meet at cluster barriers instead of kernel ends.  Where
+// it fits, it takes one launch instead of two (policy) or four (preference).
+constexpr uint32_t kFewThreads = 512, kFewSequences = 1024, kFewRows = 1024;
+
+struct FewShape {
+  uint32_t sequences, lanes, cluster;
+};
+
+template <bool pairs, bool entropy, int NV>
+__global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const RowArgs a, const PairArgs p, const int64_t* offsets,
+                                                             const FewShape f) {
+  constexpr uint32_t kWarps = kFewThreads / 32;
+  __shared__ uint32_t begin[kFewSequences + 1], count[kFewSequences];
+  __shared__ uint32_t all, used;
+  __shared__ float buf[kWarps * kPolicySums], part[kMaxCluster * kPolicySums];
+  const uint32_t rank = blockIdx.x, tid = threadIdx.x, rows = (uint32_t)a.rows;
+  const uint32_t row = (rank * kFewThreads + tid) / f.lanes, lane = tid % f.lanes;
+  const bool here = row < rows;
+  cluster_arrive();
+  RowIn in = {};
+  if (here) in = load_row<E, pairs ? RowOp::kPairScore : RowOp::kPolicy>(a, row);
+  const Window<E> x(const_cast<E*>(static_cast<const E*>(a.x)) + row * a.ldx, a.vocab);
+  uint4 u[NV] = {};
+  if (in.on) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) u[k] = x.load(lane + k * f.lanes, true);
+  }
+  if (tid == 0) all = used = 0;
+  for (uint32_t s = tid; s <= f.sequences; s += kFewThreads) {
+    begin[s] = clamp_offset(offsets[s], rows);
+    if (s < f.sequences) count[s] = 0;
+  }
+  __syncthreads();
+  for (uint32_t first = 0; first < rows; first += kFewThreads) {
+    const uint32_t r = first + tid;
+    const uint32_t seq = r < rows && a.tokens[r] >= 0 ? sequence_at(begin, f.sequences, r) : kNoSequence;
+    const uint32_t same = __match_any_sync(~0u, seq), n = (uint32_t)__popc(same);
+    if (seq != kNoSequence && tid % 32 == (uint32_t)__ffs(same) - 1) {
+      atomicAdd(&all, n);
+      if (atomicAdd(&count[seq], n) == 0) atomicAdd(&used, 1u);
+    }
+  }
+  const uint32_t seq = in.on ? sequence_at(begin, f.sequences, row) : kNoSequence;
+  in.on = seq != kNoSequence;
+  const RowSums r = lanes_join(sums_of<NV, !pairs || entropy>(u, a.c2), a.c2, f.lanes);
+  __syncthreads();
+  RowOut o = {};
+  if constexpr (pairs) {
+    if (here) finish_row<RowOp::kScore>(a, row, in, r, lane == 0);
+    cluster_wait();
+    cluster_arrive();  // the rows' log-probabilities are written
+    cluster_wait();
+    for (uint32_t pair = rank * kWarps + tid / 32; pair < (uint32_t)p.pairs; pair += f.cluster * kWarps) {
+      float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+      for (uint32_t k = 0; k < 2; ++k) {
+        for (uint32_t i = begin[2 * pair + k] + tid % 32; i < begin[2 * pair + k + 1]; i += 32)
+          if (a.tokens[i] >= 0) sum[k] += __ldcg(a.logprob + i) - (p.ref_logprob ? p.ref_logprob[i] : 0.0f);
+#pragma unroll
+        for (int d = 16; d; d /= 2) sum[k] += __shfl_xor_sync(~0u, sum[k], d);
+      }
+      const uint32_t n[2] = {count[2 * pair], count[2 * pair + 1]};
+      if (tid % 32 == 0) finish_pair(p, pair, sum, n);
+    }
+    cluster_arrive();  // the pairs' slopes are written
+    cluster_wait();
+    if (rank == 0) preference_stats(p, buf);
+    if (here && a.g) {
+      if (in.on) in.slope_lp = __ldcg(p.seq_slope + seq);
+      o = finish_row<RowOp::kScoreGrad>(a, row, in, r, false);
+    }
+  } else {
+    if (in.on) {
+      in.w = a.reduction == BF_MEAN_TOKENS ? 1.0f / (float)all
+             : a.reduction == BF_MEAN_SEQUENCES ? 1.0f / ((float)count[seq] * (float)used) : 1.0f;
+      if (!a.advantage_per_token) in.adv = a.advantage[seq];
+    }
+    if (here) o = finish_row<RowOp::kPolicy>(a, row, in, r, lane == 0);
+    float v[kPolicySums];
+#pragma unroll
+    for (uint32_t k = 0; k < kPolicySums; ++k) v[k] = lane == 0 ? o.sums[k] : 0.0f;
+    const float sum = block_sums(v, buf, f.lanes);
+    cluster_wait();
+    if (tid < kPolicySums) cluster_store(&part[rank * kPolicySums + tid], 0, sum);
+    cluster_arrive();
+  }
+  if (here && a.g) {
+    const Window<E> g(static_cast<E*>(a.g) + row * a.ldg, a.vocab);
+    const Grads<entropy> grads(o, a.c2);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      uint4 d = make_uint4(0, 0, 0, 0);
+      if (in.on) d = grads.of(u[k]);
+      put(x, g, lane + k * f.lanes, d);
+    }
+    if (in.on && in.known && (in.y + x.shift) / kW % f.lanes == lane)
+      g.row[in.y] = from_f32<E>(logit_grad(o, in.xy, a.c2) + o.hit);
+  }
+  if constexpr (!pairs) {
+    cluster_wait();  // the blocks' sums are in the first one
+    if (rank == 0 && tid < 32) {
+      float total = 0.0f;
+      if (tid < kPolicySums)
+        for (uint32_t b = 0; b < f.cluster; ++b) total += part[b * kPolicySums + tid];
+      put_policy_stats(a, total);
+    }
+  }
+}
+
 struct WideShape {
   uint32_t cluster, threads, tiles;
 };
@@ -367,15 +490,21 @@ uint32_t pow2_up(uint32_t n) {
   return p;
 }
 
+// Vectors that a row touches: one more where rows may start inside one.
+uint32_t vectors_of(const RowArgs& a) {
+  const bool aligned = ((uintptr_t)a.x | (uintptr_t)(a.ldx * sizeof(E))) % 16 == 0;
+  return div_up(a.vocab + (aligned ? 0 : kW - 1), kW);
+}
+
 template <RowOp op, bool entropy>
 cudaError_t launch_op(const RowArgs& a, cudaStream_t st) {
   const auto group = [&](auto kernel, uint32_t lanes) {
     return launch_shaped(kernel, (a.rows * lanes + kGroupThreads - 1) / kGroupThreads, kGroupThreads, 1, kFollows<op>, st, a, lanes);
   };
-  // Vectors that a row touches: one more where rows may start inside one.
-  const bool aligned = ((uintptr_t)a.x | (uintptr_t)(a.ldx * sizeof(E))) % 16 == 0;
-  const uint32_t vectors = div_up(a.vocab + (aligned ? 0 : kW - 1), kW);
-  if (a.vocab <= 4) return group(short_kernel<op, 4>, 1);
+  const uint32_t vectors = vectors_of(a);
+  if (a.vocab <= 4)
+    return launch_shaped(short_kernel<op, 4>, (a.rows + kGroupThreads - 1) / kGroupThreads, kGroupThreads, 1, kFollows<op>,
+                         st, a);
   if (vectors <= 2) return group(warp_kernel<op, entropy, 2>, 1);
   if (vectors <= 8) return group(warp_kernel<op, entropy, 4>, pow2_up(div_up(vectors, 4)));
   if (vectors <= 256) return group(warp_kernel<op, entropy, 8>, pow2_up(div_up(vectors, 8)));
@@ -384,11 +513,37 @@ cudaError_t launch_op(const RowArgs& a, cudaStream_t st) {
                        s.tiles);
 }
 
+template <bool pairs, bool entropy>
+cudaError_t launch_few(const RowArgs& a, const PairArgs& p, const int64_t* offsets, FewShape f, bool two, cudaStream_t st) {
+  const auto kernel = two ? few_kernel<pairs, entropy, 2> : few_kernel<pairs, entropy, 8>;
+  return launch_shaped(kernel, f.cluster, kFewThreads, f.cluster, false, st, a, p, offsets, f);
+}
+
 }  // namespace
 
-#define BF_ROWS_NAME2(t) launch_rows_type##t
-#define BF_ROWS_NAME(t) BF_ROWS_NAME2(t)
-cudaError_t BF_ROWS_NAME(BF_ROWS_TYPE)(RowOp op, const RowArgs& a, cudaStream_t st) {
+#define BF_ROWS_JOIN2(name, t) name##t
+#define BF_ROWS_JOIN(name, t) BF_ROWS_JOIN2(name, t)
+#define BF_ROWS_NAME(name) BF_ROWS_JOIN(name, BF_ROWS_TYPE)
+
+cudaError_t BF_ROWS_NAME(launch_few_type)(const RowArgs& a, const PairArgs* p, const int64_t* offsets, uint64_t sequences,
+                                          bool* done, cudaStream_t st) {
+  const uint32_t vectors = vectors_of(a);
+  FewShape f = {};
+  *done = false;
+  if (vectors > 256 || a.rows > kFewRows || sequences > kFewSequences) return cudaSuccess;
+  f.lanes = vectors <= 2 ? 1 : pow2_up(div_up(vectors, 8));
+  f.sequences = (uint32_t)sequences;
+  const uint32_t blocks = div_up((uint32_t)a.rows * f.lanes, kFewThreads);
+  if (blocks > kMaxCluster) return cudaSuccess;
+  f.cluster = pow2_up(blocks);
+  *done = true;
+  const bool two = vectors <= 2;
+  if (p) return launch_few<true, false>(a, *p, offsets, f, two, st);
+  return a.entropy_coef != 0.0f ? launch_few<false, true>(a, PairArgs{}, offsets, f, two, st)
+                                : launch_few<false, false>(a, PairArgs{}, offsets, f, two, st);
+}
+
+cudaError_t BF_ROWS_NAME(launch_rows_type)(RowOp op, const RowArgs& a, cudaStream_t st) {
   switch (op) {
     case RowOp::kScore: return a.entropy ? launch_op<RowOp::kScore, true>(a, st) : launch_op<RowOp::kScore, false>(a, st);
     case RowOp::kScoreGrad:

@@ -189,6 +189,26 @@ __device__ __forceinline__ RowSums lanes_join(RowSums r, float c2, uint32_t lane
   return r;
 }
 
+// One pair, from both answers' sums of lp - ref and numbers of scored rows: the
+// rewards beta * sum (or beta * mean), the loss of their gap
+//   h = reward_0 - reward_1 - margin,  l = -(1 - eps) ln sigma(h) - eps ln sigma(-h)
+// and the slopes of the mean loss in each answer's log-probabilities.
+__device__ __forceinline__ void finish_pair(const PairArgs& a, uint64_t p, const float (&sum)[2], const uint32_t (&n)[2]) {
+  float share[2], reward[2];
+#pragma unroll
+  for (uint32_t k = 0; k < 2; ++k) {
+    share[k] = a.beta * (a.average && n[k] ? 1.0f / (float)n[k] : 1.0f);
+    reward[k] = share[k] * sum[k];
+    a.rewards[2 * p + k] = reward[k];
+  }
+  const float h = reward[0] - reward[1] - a.margin, eps = a.label_smoothing;
+  const float tail = log1pf(expf(-fabsf(h)));  // ln(1 + e^-|h|)
+  const float slope = (eps / (1.0f + expf(-h)) - (1.0f - eps) / (1.0f + expf(h))) * a.grad_scale / (float)a.pairs;
+  a.seq_slope[2 * p] = slope * share[0];
+  a.seq_slope[2 * p + 1] = -slope * share[1];
+  a.partial[p] = (1.0f - eps) * (fmaxf(-h, 0.0f) + tail) + eps * (fmaxf(h, 0.0f) + tail);
+}
+
 // Sums of N values over the block's threads: the k-th in thread k.  Every thread of the block calls it with the same
 // `lanes`: only every lanes-th one (a power of two, at most 32) brings values.  buf: N floats per warp, not in use.
 template <uint32_t N>
@@ -205,6 +225,43 @@ __device__ __forceinline__ float block_sums(float (&v)[N], float* buf, uint32_t 
   if (threadIdx.x < N)
     for (uint32_t w = 0; w < blockDim.x / 32; ++w) sum += buf[w * N + threadIdx.x];
   return sum;
+}
+
+// The preference loss from its pairs, once all are visible; every thread of the block calls it.  buf: 4 floats per warp.
+__device__ __forceinline__ void preference_stats(const PairArgs& a, float* buf) {
+  float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (uint64_t p = threadIdx.x; p < a.pairs; p += blockDim.x) {
+    const float r0 = __ldcg(a.rewards + 2 * p), r1 = __ldcg(a.rewards + 2 * p + 1);
+    v[0] += __ldcg(a.partial + p);
+    v[1] += r0 > r1 ? 1.0f : 0.0f;
+    v[2] += r0;
+    v[3] += r1;
+  }
+  const float total = block_sums(v, buf);
+  if (threadIdx.x < 4) a.stats[threadIdx.x] = total / (float)a.pairs;
+}
+
+// The last s in [0, sequences) with offsets[s] <= row, by halving [lo, hi).
+template <typename T, typename I>
+__device__ __forceinline__ I last_at_or_before(const T* offsets, I lo, I hi, T row) {
+  while (hi - lo > 1) {
+    const I mid = (lo + hi) / 2;
+    if (offsets[mid] <= row) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// Offsets as 32-bit rows, those outside [0, rows] moved to its ends: a row is before the same ones.
+__device__ __forceinline__ uint32_t clamp_offset(int64_t o, uint32_t rows) {
+  return o < 0 ? 0u : o > (int64_t)rows ? rows : (uint32_t)o;
+}
+
+// The sequence of a row, from clamped offsets in shared memory.
+__device__ __forceinline__ uint32_t sequence_at(const uint32_t* begin, uint32_t sequences, uint32_t row) {
+  if (!sequences) return kNoSequence;
+  const uint32_t s = last_at_or_before(begin, 0u, sequences, row);
+  return begin[s] <= row && row < begin[s + 1] ? s : kNoSequence;
 }
 
 // Whether this block is the last of `blocks` to say so; called by the warp whose
