@@ -151,6 +151,25 @@ struct Window {
     if (v < vectors) u = load_ends<E>(at(v), v ? 0 : (int32_t)shift, (int32_t)(end - v * kWidth));
     return u;
   }
+  // Whether vectors v, v + step, ... (N of them) all lie in the row as a whole.
+  template <int N>
+  __device__ __forceinline__ bool all_whole(uint32_t v, uint32_t step) const {
+    return v - lo < whole && v - lo + (N - 1) * step < whole;
+  }
+  // Those vectors: read by one address and a step where they lie in the row (the
+  // tests and addresses of single ones took more instructions than the
+  // arithmetic of their elements).
+  template <int N>
+  __device__ __forceinline__ void load_many(uint4 (&u)[N], uint32_t v, uint32_t step, bool last) const {
+    if (all_whole<N>(v, step)) {
+      const uint4* p = reinterpret_cast<const uint4*>(at(v));
+#pragma unroll
+      for (int k = 0; k < N; ++k, p += step) u[k] = last ? __ldcs(p) : __ldcg(p);
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k) u[k] = load(v + k * step, last);
+    }
+  }
   __device__ __forceinline__ void store(uint32_t v, const uint4& u) const {
     if (v - lo < whole) __stcs(reinterpret_cast<uint4*>(at(v)), u);
     else if (v < vectors) store_ends<E>(at(v), u, v ? 0 : (int32_t)shift, (int32_t)(end - v * kWidth));

@@ -46,9 +46,25 @@ __device__ __forceinline__ void put_policy_stats(const RowArgs& a, float total) 
 __device__ __forceinline__ void policy_stats(const RowArgs& a, uint64_t parts, float* buf) {
   last_sees();
   float v[kPolicySums] = {};
-  for (uint64_t i = threadIdx.x; i < parts; i += blockDim.x) {
+  const float4* part = reinterpret_cast<const float4*>(a.partial);  // kPolicyPart floats each
+  constexpr uint32_t kAhead = 8;  // one block reads them all: at one a time it took a fifth of a short call
+  for (uint64_t i = threadIdx.x; i < parts; i += kAhead * blockDim.x) {
+    float4 lo[kAhead];
+    float hi[kAhead];
 #pragma unroll
-    for (uint32_t k = 0; k < kPolicySums; ++k) v[k] += __ldcg(a.partial + k * parts + i);
+    for (uint32_t j = 0; j < kAhead; ++j) {
+      const uint64_t at = i + j * blockDim.x;
+      lo[j] = at < parts ? __ldcg(part + 2 * at) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      hi[j] = at < parts ? __ldcg(a.partial + kPolicyPart * at + 4) : 0.0f;
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < kAhead; ++j) {
+      v[0] += lo[j].x;
+      v[1] += lo[j].y;
+      v[2] += lo[j].z;
+      v[3] += lo[j].w;
+      v[4] += hi[j];
+    }
   }
   const float total = block_sums(v, buf);
   if (threadIdx.x < 32) put_policy_stats(a, total);
@@ -124,6 +140,26 @@ __device__ __forceinline__ void put(const Window<E>& x, const Window<E>& g, uint
   else g.store_cut(v, x.shift, d);
 }
 
+// The gradients of N vectors of row x, to row g (zeros with `zero`).
+template <int N, bool tilt>
+__device__ __forceinline__ void put_many(const Window<E>& x, const Window<E>& g, const uint4 (&u)[N], uint32_t v,
+                                         uint32_t step, const Grads<tilt>& grads, bool zero) {
+  const uint4 none = make_uint4(0, 0, 0, 0);
+  if (x.shift == g.shift && g.template all_whole<N>(v, step)) {
+    uint4* p = reinterpret_cast<uint4*>(g.at(v));
+    if (zero) {
+#pragma unroll
+      for (int k = 0; k < N; ++k, p += step) __stcs(p, none);
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k, p += step) __stcs(p, grads.of(u[k]));
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k) put(x, g, v + k * step, zero ? none : grads.of(u[k]));
+  }
+}
+
 // ---- the shortest rows (three modes): a thread for each, N elements at most ----
 
 constexpr uint32_t kGroupThreads = 256;
@@ -137,7 +173,7 @@ __device__ __forceinline__ bool say_policy_part(const RowArgs& a, const RowOut& 
   for (uint32_t k = 0; k < kPolicySums; ++k) v[k] = mine ? o.sums[k] : 0.0f;
   const float sum = block_sums(v, buf, lanes);
   if (threadIdx.x >= 32) return false;
-  if (threadIdx.x < kPolicySums) a.partial[(uint64_t)threadIdx.x * gridDim.x + blockIdx.x] = sum;
+  if (threadIdx.x < kPolicySums) a.partial[(uint64_t)blockIdx.x * kPolicyPart + threadIdx.x] = sum;
   return last_to_say(&a.counts->blocks_done, gridDim.x);
 }
 
@@ -152,6 +188,8 @@ __global__ void __launch_bounds__(kGroupThreads) short_kernel(const RowArgs a) {
 #pragma unroll
   for (uint32_t j = 0; j < N; ++j) v[j] = here && j < a.vocab ? to_f32(x[j]) : kMinusInf;
   if (here) in = load_row<E, op>(a, row);
+  if constexpr (kFollows<op>) wait_for_previous();
+  if (here) load_row_late<op>(a, row, in);
   RowSums r = {v[0], 0.0f, 0.0f};
   if constexpr (op != RowOp::kPairGrad) {
 #pragma unroll
@@ -165,11 +203,7 @@ __global__ void __launch_bounds__(kGroupThreads) short_kernel(const RowArgs a) {
     }
   }
   RowOut o = {};
-  if constexpr (kFollows<op>) wait_for_previous();
-  if (here) {
-    load_row_late<op>(a, row, in);
-    o = finish_row<op>(a, row, in, r, true);
-  }
+  if (here) o = finish_row<op>(a, row, in, r, true);
   __shared__ float buf[kGroupThreads / 32 * kPolicySums];
   bool last = false;
   if constexpr (op == RowOp::kPolicy) last = say_policy_part(a, o, here, 1, buf);
@@ -203,17 +237,14 @@ __global__ void __launch_bounds__(kGroupThreads, op == RowOp::kPolicy ? 3 : 4) w
   const Window<E> x(const_cast<E*>(static_cast<const E*>(a.x)) + row * a.ldx, a.vocab);
   uint4 u[NV] = {};
   if (in.on) {
-#pragma unroll
-    for (int k = 0; k < NV; ++k) u[k] = x.load(lane + k * lanes, true);
+    x.load_many(u, lane, lanes, true);
   }
+  if constexpr (kFollows<op>) wait_for_previous();
+  if (here) load_row_late<op>(a, row, in);
   RowSums r = {};
   if constexpr (op != RowOp::kPairGrad) r = lanes_join(sums_of<NV, kMoment<op, entropy>>(u, a.c2), a.c2, lanes);
   RowOut o = {};
-  if constexpr (kFollows<op>) wait_for_previous();
-  if (here) {
-    load_row_late<op>(a, row, in);
-    o = finish_row<op>(a, row, in, r, lane == 0);
-  }
+  if (here) o = finish_row<op>(a, row, in, r, lane == 0);
   __shared__ float buf[kGroupThreads / 32 * kPolicySums];
   bool last = false;
   if constexpr (op == RowOp::kPolicy) last = say_policy_part(a, o, here && lane == 0, lanes, buf);
@@ -221,12 +252,7 @@ __global__ void __launch_bounds__(kGroupThreads, op == RowOp::kPolicy ? 3 : 4) w
     if (here && a.g) {
       const Window<E> g(static_cast<E*>(a.g) + row * a.ldg, a.vocab);
       const Grads<entropy> grads(o, a.c2);
-#pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        uint4 d = make_uint4(0, 0, 0, 0);
-        if (in.on) d = grads.of(u[k]);
-        put(x, g, lane + k * lanes, d);
-      }
+      put_many(x, g, u, lane, lanes, grads, !in.on);
       if (in.on && in.known && (in.y + x.shift) / kW % lanes == lane)
         g.row[in.y] = from_f32<E>(logit_grad(o, in.xy, a.c2) + o.hit);
     }
@@ -272,12 +298,18 @@ __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, 
   const uint32_t first = rank * tiles * NV * threads + tid;
   uint4 u[NV];
   RowSums r = {kMinusInf, 0.0f, 0.0f};
-  if (in.on) {
+  const bool read = in.on;
+  if (read) {
     if (cluster > 1 && op != RowOp::kPairGrad) cluster_arrive();  // seen below: the others run
     for (uint32_t tile = 0; tile < tiles; ++tile) {
       if (op == RowOp::kPairGrad && tile + 1 < tiles) continue;
-#pragma unroll
-      for (int k = 0; k < NV; ++k) u[k] = x.load(first + (tile * NV + k) * threads, op == RowOp::kScore || (op != RowOp::kPairScore && tile + 1 == tiles));
+      x.load_many(u, first + tile * NV * threads, threads,
+                  op == RowOp::kScore || (op != RowOp::kPairScore && tile + 1 == tiles));
+      // Only the first blocks find the kernel ahead still running; what it wrote arrives beside the logits.
+      if (kFollows<op> && (tile == 0 || op == RowOp::kPairGrad)) {
+        wait_for_previous();
+        load_row_late<op>(a, row, in);
+      }
       if constexpr (op != RowOp::kPairGrad) {
         const RowSums now = sums_of<NV, kMoment<op, entropy>>(u, a.c2);
         r = tiles > 1 ? join(r, now, a.c2) : now;
@@ -312,37 +344,29 @@ __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, 
       r = lanes_join(r, a.c2, 32);
     }
   }
-  if constexpr (kFollows<op>) wait_for_previous();
-  load_row_late<op>(a, row, in);
+  if (kFollows<op> && !read) {
+    wait_for_previous();
+    load_row_late<op>(a, row, in);
+  }
   const RowOut o = finish_row<op>(a, row, in, r, rank == 0 && tid == 0);
   bool last = false;
   if constexpr (op == RowOp::kPolicy) {
     if (rank == 0 && tid < 32) {
       if (tid == 0)
-        for (uint32_t k = 0; k < kPolicySums; ++k) a.partial[k * a.rows + row] = o.sums[k];
+        for (uint32_t k = 0; k < kPolicySums; ++k) a.partial[row * kPolicyPart + k] = o.sums[k];
       last = last_to_say(&a.counts->blocks_done, (uint32_t)a.rows);
     }
   }
   if constexpr (!kScores<op>) {
     if (a.g) {
       const Window<E> g(static_cast<E*>(a.g) + row * a.ldg, a.vocab);
-      if (!in.on) {
-        const uint4 zero = make_uint4(0, 0, 0, 0);
-        for (uint32_t k = 0; k < NV * tiles; ++k) put(x, g, first + k * threads, zero);
-      } else {
-        const Grads<entropy> grads(o, a.c2);
-        for (uint32_t tile = tiles; tile-- > 0;) {
-          if (tile + 1 < tiles) {
-#pragma unroll
-            for (int k = 0; k < NV; ++k) u[k] = x.load(first + (tile * NV + k) * threads, true);
-          }
-#pragma unroll
-          for (int k = 0; k < NV; ++k) {
-            const uint32_t v = first + (tile * NV + k) * threads;
-            const uint4 d = grads.of(u[k]);
-            put(x, g, v, d);
-          }
-        }
+      const Grads<entropy> grads(o, a.c2);
+      for (uint32_t tile = tiles; tile-- > 0;) {
+        const uint32_t v = first + tile * NV * threads;
+        if (in.on && tile + 1 < tiles) x.load_many(u, v, threads, true);
+        put_many(x, g, u, v, threads, grads, !in.on);
+      }
+      if (in.on) {
         const uint32_t at = (in.y + x.shift) / kW - rank * tiles * NV * threads;  // the vector with the token
         if (in.known && at < tiles * NV * threads && at % threads == tid)
           g.row[in.y] = from_f32<E>(logit_grad(o, in.xy, a.c2) + o.hit);
@@ -383,8 +407,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const RowArgs a, co
   const Window<E> x(const_cast<E*>(static_cast<const E*>(a.x)) + row * a.ldx, a.vocab);
   uint4 u[NV] = {};
   if (in.on) {
-#pragma unroll
-    for (int k = 0; k < NV; ++k) u[k] = x.load(lane + k * f.lanes, true);
+    x.load_many(u, lane, f.lanes, true);
   }
   if (tid == 0) all = used = 0;
   for (uint32_t s = tid; s <= f.sequences; s += kFewThreads) {
@@ -448,12 +471,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const RowArgs a, co
   if (here && a.g) {
     const Window<E> g(static_cast<E*>(a.g) + row * a.ldg, a.vocab);
     const Grads<entropy> grads(o, a.c2);
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      uint4 d = make_uint4(0, 0, 0, 0);
-      if (in.on) d = grads.of(u[k]);
-      put(x, g, lane + k * f.lanes, d);
-    }
+    put_many(x, g, u, lane, f.lanes, grads, !in.on);
     if (in.on && in.known && (in.y + x.shift) / kW % f.lanes == lane)
       g.row[in.y] = from_f32<E>(logit_grad(o, in.xy, a.c2) + o.hit);
   }
