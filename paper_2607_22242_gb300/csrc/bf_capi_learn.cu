@@ -77,7 +77,11 @@ RowArgs row_args(const bf_matrix* logits, const int64_t* tokens, float temperatu
   a.dtype = logits->dtype;
   a.tokens = tokens;
   a.inv_tau = 1.0f / temperature;
-  a.c2 = (float)(1.44269504088896340736 / (double)temperature);
+  a.tau = temperature;
+  const double c2 = 1.44269504088896340736 / (double)temperature;
+  a.c2_hi = (float)c2;
+  if ((double)a.c2_hi >= c2) a.c2_hi = std::nextafterf(a.c2_hi, 0.0f);
+  a.c2_lo = (float)(c2 - (double)a.c2_hi);
   if (grad) {
     a.g = grad->data;
     a.ldg = grad->row_stride;

@@ -34,8 +34,8 @@ struct RowArgs {
   uint32_t vocab;
   uint32_t dtype;     // bf_dtype
   const int64_t* tokens;
-  float inv_tau;      // 1 / temperature
-  float c2;           // log2(e) / temperature
+  float tau, inv_tau;      // temperature, and its reciprocal
+  float c2_hi, c2_lo;      // log2(e) / temperature in two parts, the second above 0
   float* logprob;     // nullptr: not wanted
   float* entropy;     // nullptr: not wanted
   // kScoreGrad

@@ -70,31 +70,40 @@ __device__ __forceinline__ void policy_stats(const RowArgs& a, uint64_t parts, f
   if (threadIdx.x < 32) put_policy_stats(a, total);
 }
 
-// (x - m) c2 as (x - base) c2 - r: with base = 0 and r = m c2 rounded it is one
-// product and sum, and what r is off by (`rest`) goes into the factors once per
-// row; in rows whose m c2 leaves the 32-bit range (all masked by the type's
-// lowest value), base = m and r = 0.  f16 logits never get there.
+// (x - m) (hi + lo) as (x - base) hi - r + (x - base) lo: with base = 0 and r =
+// m hi rounded it is two products and sums, the small part last, and what r is
+// off by (`rest`) goes into the factors once per row; in rows whose m hi leaves
+// the 32-bit range (all masked by the type's lowest value), base = m and r = 0.
+// f16 logits never get there.
+//
+// Without `exact` the small part is left out, for gradients of 16 bits: 1e-6 of
+// a probability of e^-14.
+template <bool exact>
 struct Exponent {
   static constexpr bool kShifts = !std::is_same<E, __half>::value;
-  float2 c, base, r;
+  float2 hi, lo, base, r;
   float rest;
 
-  __device__ __forceinline__ Exponent(float m, float c2) : c(make_float2(c2, c2)) {
-    const bool fits = !kShifts || fabsf(m) * c2 < 1e38f;
+  __device__ __forceinline__ Exponent(float m, Scale c) : hi(make_float2(c.hi, c.hi)), lo(make_float2(c.lo, c.lo)) {
+    const bool fits = !kShifts || fabsf(m) * c.hi < 1e38f;
     base = fits ? make_float2(0.0f, 0.0f) : make_float2(-m, -m);
-    r = fits ? make_float2(-m * c2, -m * c2) : make_float2(0.0f, 0.0f);
-    rest = fits ? fmaf(-m, c2, m * c2) : 0.0f;
+    r = fits ? make_float2(-m * c.hi, -m * c.hi) : make_float2(0.0f, 0.0f);
+    rest = fits ? fmaf(exact ? -m : 0.0f, c.lo, fmaf(-m, c.hi, m * c.hi)) : 0.0f;
   }
+  // v 2^rest; 2^rest itself, rounded, would be off the same way in every row with this m.
+  __device__ __forceinline__ float put_back(float v) const { return fmaf(v, rest * kLn2, v); }
   __device__ __forceinline__ float2 of(float2 x) const {
-    return __ffma2_rn(kShifts ? __fadd2_rn(x, base) : x, c, r);
+    if (kShifts) x = __fadd2_rn(x, base);
+    const float2 t = __ffma2_rn(x, hi, r);
+    return exact ? __ffma2_rn(x, lo, t) : t;
   }
 };
 
 // NV vectors in registers: their sums against their own maximum (q only with `moment`).
 template <int NV, bool moment>
-__device__ __forceinline__ RowSums sums_of(const uint4* u, float c2) {
+__device__ __forceinline__ RowSums sums_of(const uint4* u, Scale c) {
   const float m = max_of<E, NV>(u);
-  const Exponent ex(usable_max(m), c2);
+  const Exponent<true> ex(usable_max(m), c);
   float2 s = {}, q = {};
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
@@ -107,18 +116,18 @@ __device__ __forceinline__ RowSums sums_of(const uint4* u, float c2) {
       if (moment) q = __ffma2_rn(e, make_float2(finite_t(t.x), finite_t(t.y)), q);
     }
   }
-  const float s1 = s.x + s.y, f = fmaf(ex.rest, kLn2, 1.0f);  // 2^rest
-  return {m, f * s1, f * fmaf(ex.rest, s1, q.x + q.y)};
+  const float s1 = s.x + s.y, q1 = fmaf(ex.rest, s1, q.x + q.y);
+  return {m, ex.put_back(s1), ex.put_back(q1), m == kMinusInf ? 0.0f : 1.0f};
 }
 
 // The gradient of vectors of logits, from a row's factors (o.d only with `tilt`).
 template <bool tilt>
 struct Grads {
-  Exponent ex;
+  Exponent<sizeof(E) == 4> ex;
   float2 b, d;
 
-  __device__ __forceinline__ Grads(const RowOut& o, float c2) : ex(o.m, c2) {
-    const float f = fmaf(ex.rest, kLn2, 1.0f), b1 = f * fmaf(o.d, ex.rest, o.b), d1 = f * o.d;
+  __device__ __forceinline__ Grads(const RowOut& o, Scale c) : ex(o.m, c) {
+    const float b1 = ex.put_back(fmaf(o.d, ex.rest, o.b)), d1 = ex.put_back(o.d);
     b = make_float2(b1, b1);
     d = make_float2(d1, d1);
   }
@@ -190,14 +199,14 @@ __global__ void __launch_bounds__(kGroupThreads) short_kernel(const RowArgs a) {
   if (here) in = load_row<E, op>(a, row);
   if constexpr (kFollows<op>) wait_for_previous();
   if (here) load_row_late<op>(a, row, in);
-  RowSums r = {v[0], 0.0f, 0.0f};
+  RowSums r = {v[0], 0.0f, 0.0f, 1.0f};
   if constexpr (op != RowOp::kPairGrad) {
 #pragma unroll
     for (int j = 1; j < N; ++j) r.m = fmaxf(r.m, v[j]);
     const float ref = usable_max(r.m);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const float t = (v[j] - ref) * a.c2, e = exp2_fast(t);
+      const float t = scale_of(a).of(v[j] - ref), e = exp2_fast(t);
       r.s += e;
       r.q = fmaf(e, finite_t(t), r.q);
     }
@@ -213,7 +222,7 @@ __global__ void __launch_bounds__(kGroupThreads) short_kernel(const RowArgs a) {
 #pragma unroll
       for (uint32_t j = 0; j < N; ++j) {
         if (j >= a.vocab) continue;
-        float d = in.on ? logit_grad(o, v[j], a.c2) : 0.0f;
+        float d = in.on ? logit_grad(o, v[j], scale_of(a)) : 0.0f;
         if (in.on && j == in.y) d += o.hit;
         g[j] = from_f32<E>(d);
       }
@@ -242,7 +251,7 @@ __global__ void __launch_bounds__(kGroupThreads, op == RowOp::kPolicy ? 3 : 4) w
   if constexpr (kFollows<op>) wait_for_previous();
   if (here) load_row_late<op>(a, row, in);
   RowSums r = {};
-  if constexpr (op != RowOp::kPairGrad) r = lanes_join(sums_of<NV, kMoment<op, entropy>>(u, a.c2), a.c2, lanes);
+  if constexpr (op != RowOp::kPairGrad) r = lanes_join(sums_of<NV, kMoment<op, entropy>>(u, scale_of(a)), scale_of(a), lanes);
   RowOut o = {};
   if (here) o = finish_row<op>(a, row, in, r, lane == 0);
   __shared__ float buf[kGroupThreads / 32 * kPolicySums];
@@ -251,10 +260,10 @@ __global__ void __launch_bounds__(kGroupThreads, op == RowOp::kPolicy ? 3 : 4) w
   if constexpr (!kScores<op>) {
     if (here && a.g) {
       const Window<E> g(static_cast<E*>(a.g) + row * a.ldg, a.vocab);
-      const Grads<entropy> grads(o, a.c2);
+      const Grads<entropy> grads(o, scale_of(a));
       put_many(x, g, u, lane, lanes, grads, !in.on);
       if (in.on && in.known && (in.y + x.shift) / kW % lanes == lane)
-        g.row[in.y] = from_f32<E>(logit_grad(o, in.xy, a.c2) + o.hit);
+        g.row[in.y] = from_f32<E>(logit_grad(o, in.xy, scale_of(a)) + o.hit);
     }
   }
   if constexpr (op == RowOp::kPolicy) {
@@ -289,7 +298,7 @@ template <RowOp op, bool entropy>
 __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, uint32_t cluster, uint32_t tiles) {
   constexpr int NV = kWideVectors;
   constexpr uint32_t kMost = kWideThreads / 32 * kMaxCluster;
-  __shared__ float part[3][kMost];  // sums of the row's warps, all blocks'
+  __shared__ float part[4][kMost];  // sums of the row's warps, all blocks'
   const uint64_t row = blockIdx.x / cluster;
   const uint32_t rank = blockIdx.x % cluster, tid = threadIdx.x, threads = blockDim.x;
   if constexpr (kFollows<op>) let_next_start();
@@ -297,7 +306,7 @@ __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, 
   const Window<E> x(const_cast<E*>(static_cast<const E*>(a.x)) + row * a.ldx, a.vocab);
   const uint32_t first = rank * tiles * NV * threads + tid;
   uint4 u[NV];
-  RowSums r = {kMinusInf, 0.0f, 0.0f};
+  RowSums r = {kMinusInf, 0.0f, 0.0f, 0.0f};
   const bool read = in.on;
   if (read) {
     if (cluster > 1 && op != RowOp::kPairGrad) cluster_arrive();  // seen below: the others run
@@ -311,12 +320,12 @@ __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, 
         load_row_late<op>(a, row, in);
       }
       if constexpr (op != RowOp::kPairGrad) {
-        const RowSums now = sums_of<NV, kMoment<op, entropy>>(u, a.c2);
-        r = tiles > 1 ? join(r, now, a.c2) : now;
+        const RowSums now = sums_of<NV, kMoment<op, entropy>>(u, scale_of(a));
+        r = tiles > 1 ? join(r, now, scale_of(a)) : now;
       }
     }
     if constexpr (op != RowOp::kPairGrad) {
-      r = lanes_join(r, a.c2, 32);
+      r = lanes_join(r, scale_of(a), 32);
       const uint32_t warps = threads / 32, at = rank * warps + tid / 32;
       if (cluster > 1) {
         cluster_wait();
@@ -324,6 +333,7 @@ __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, 
           cluster_store(&part[0][at], tid % 32, r.m);
           cluster_store(&part[1][at], tid % 32, r.s);
           cluster_store(&part[2][at], tid % 32, r.q);
+          cluster_store(&part[3][at], tid % 32, r.one);
         }
         __syncwarp();
         cluster_arrive();
@@ -333,15 +343,16 @@ __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, 
           part[0][at] = r.m;
           part[1][at] = r.s;
           part[2][at] = r.q;
+          part[3][at] = r.one;
         }
         __syncthreads();
       }
-      r = {kMinusInf, 0.0f, 0.0f};
+      r = {kMinusInf, 0.0f, 0.0f, 0.0f};
       for (uint32_t w = tid % 32; w < warps * cluster; w += 32) {
-        const RowSums other = {part[0][w], part[1][w], part[2][w]};
-        r = w < 32 ? other : join(r, other, a.c2);
+        const RowSums other = {part[0][w], part[1][w], part[2][w], part[3][w]};
+        r = w < 32 ? other : join(r, other, scale_of(a));
       }
-      r = lanes_join(r, a.c2, 32);
+      r = lanes_join(r, scale_of(a), 32);
     }
   }
   if (kFollows<op> && !read) {
@@ -360,7 +371,7 @@ __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, 
   if constexpr (!kScores<op>) {
     if (a.g) {
       const Window<E> g(static_cast<E*>(a.g) + row * a.ldg, a.vocab);
-      const Grads<entropy> grads(o, a.c2);
+      const Grads<entropy> grads(o, scale_of(a));
       for (uint32_t tile = tiles; tile-- > 0;) {
         const uint32_t v = first + tile * NV * threads;
         if (in.on && tile + 1 < tiles) x.load_many(u, v, threads, true);
@@ -369,7 +380,7 @@ __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, 
       if (in.on) {
         const uint32_t at = (in.y + x.shift) / kW - rank * tiles * NV * threads;  // the vector with the token
         if (in.known && at < tiles * NV * threads && at % threads == tid)
-          g.row[in.y] = from_f32<E>(logit_grad(o, in.xy, a.c2) + o.hit);
+          g.row[in.y] = from_f32<E>(logit_grad(o, in.xy, scale_of(a)) + o.hit);
       }
     }
   }
@@ -426,7 +437,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const RowArgs a, co
   }
   const uint32_t seq = in.on ? sequence_at(begin, f.sequences, row) : kNoSequence;
   in.on = seq != kNoSequence;
-  const RowSums r = lanes_join(sums_of<NV, !pairs || entropy>(u, a.c2), a.c2, f.lanes);
+  const RowSums r = lanes_join(sums_of<NV, !pairs || entropy>(u, scale_of(a)), scale_of(a), f.lanes);
   __syncthreads();
   RowOut o = {};
   if constexpr (pairs) {
@@ -470,10 +481,10 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(const RowArgs a, co
   }
   if (here && a.g) {
     const Window<E> g(static_cast<E*>(a.g) + row * a.ldg, a.vocab);
-    const Grads<entropy> grads(o, a.c2);
+    const Grads<entropy> grads(o, scale_of(a));
     put_many(x, g, u, lane, f.lanes, grads, !in.on);
     if (in.on && in.known && (in.y + x.shift) / kW % f.lanes == lane)
-      g.row[in.y] = from_f32<E>(logit_grad(o, in.xy, a.c2) + o.hit);
+      g.row[in.y] = from_f32<E>(logit_grad(o, in.xy, scale_of(a)) + o.hit);
   }
   if constexpr (!pairs) {
     cluster_wait();  // the blocks' sums are in the first one

@@ -10,6 +10,9 @@
 //   B = -(A + C (H - ln s)) / (tau s),  D = -C ln2 / (tau s).
 // x - m is taken before the product with log2(e)/tau: a row of the type's
 // lowest values would overflow in x log2(e)/tau, and here has m among them.
+// log2(e)/tau is held in two parts: its rounding alone shifts every ln s of a
+// batch the same way (by up to 6e-8 |t|), and a preference loss adds some
+// hundred of them up to a reward.
 #pragma once
 
 #include "bf_elem.cuh"
@@ -27,10 +30,25 @@ __device__ __forceinline__ float exp2_fast(float t) {
   return e;
 }
 
-// Maximum, sum and first moment of the exponentials of some of a row's logits.
-// m is -inf, s and q are 0 where there is no logit above -inf.
+// log2(e) / tau = hi + lo with lo > 0, so that an infinite product has one sign.
+struct Scale {
+  float hi, lo, inv_tau;
+  // A difference of logits as an exponent of 2, and its exponential.
+  __device__ __forceinline__ float of(float d) const { return fmaf(d, lo, d * hi); }
+  __device__ __forceinline__ float exp_of(float d) const { return expf(d * inv_tau); }
+};
+
+// ex2.approx cuts its result off: over any octave its values are 5.0e-8 too
+// small on average (measured in 2^20 points of each of 12), except at 0.  The
+// probabilities do not mind, their sum being as much too small; ln s does, as
+// above, so s is put right before the logarithm, and sums are joined by expf.
+constexpr float kExp2Short = 5.0e-8f;
+
+// Maximum, sum and first moment of the exponentials of some of a row's logits,
+// and how much of the sum came from exponents of 0.
+// m is -inf, the others 0 where there is no logit above -inf.
 struct RowSums {
-  float m, s, q;
+  float m, s, q, one;
 };
 
 // t as a factor beside e = 2^t: where e is 0, a finite one (0 * -inf would be NaN).
@@ -39,12 +57,19 @@ __device__ __forceinline__ float finite_t(float t) { return fmaxf(t, -160.0f); }
 // The max that exponents are taken against: 0 in a row without a logit above -inf.
 __device__ __forceinline__ float usable_max(float m) { return m == kMinusInf ? 0.0f : m; }
 
-__device__ __forceinline__ RowSums join(const RowSums& a, const RowSums& b, float c2) {
-  const float m = fmaxf(a.m, b.m), ref = usable_max(m);
-  const float ta = (a.m - ref) * c2, tb = (b.m - ref) * c2;
-  const float ea = exp2_fast(ta), eb = exp2_fast(tb);
-  return {m, ea * a.s + eb * b.s, ea * (a.q + finite_t(ta) * a.s) + eb * (b.q + finite_t(tb) * b.s)};
+// r's sums against the maximum m (>= r.m).
+__device__ __forceinline__ RowSums against(const RowSums& r, float m, const Scale& c) {
+  const float d = r.m - usable_max(m), e = c.exp_of(d);
+  return {m, e * r.s, e * (r.q + finite_t(c.of(d)) * r.s), e * r.one};
 }
+
+__device__ __forceinline__ RowSums join(const RowSums& a, const RowSums& b, const Scale& c) {
+  const float m = fmaxf(a.m, b.m);
+  const RowSums x = against(a, m, c), y = against(b, m, c);
+  return {m, x.s + y.s, x.q + y.q, x.one + y.one};
+}
+
+__device__ __forceinline__ Scale scale_of(const RowArgs& a) { return {a.c2_hi, a.c2_lo, a.inv_tau}; }
 
 // What a row brings besides its logits.
 struct RowIn {
@@ -131,8 +156,8 @@ __device__ __forceinline__ RowOut finish_row(const RowArgs& a, uint64_t row, con
   }
   const bool none = r.s == 0.0f;
   o.m = usable_max(r.m);
-  const float ln_s = logf(r.s), inv_s = none ? 0.0f : 1.0f / r.s;
-  float lp = none ? kMinusInf : (in.xy - o.m) * a.inv_tau - ln_s;
+  const float ln_s = logf(fmaf(r.s - r.one, kExp2Short, r.s)), inv_s = none ? 0.0f : 1.0f / r.s;
+  float lp = none ? kMinusInf : (in.xy - o.m) / a.tau - ln_s;
   const float h = none ? 0.0f : ln_s - kLn2 * r.q * inv_s;
   if (!in.known) lp = __int_as_float(0x7FC00000);
   if (leader) {
@@ -171,20 +196,20 @@ __device__ __forceinline__ RowOut finish_row(const RowArgs& a, uint64_t row, con
 }
 
 // A logit's gradient, without the token's own part.
-__device__ __forceinline__ float logit_grad(const RowOut& o, float x, float c2) {
-  const float t = (x - o.m) * c2;
+__device__ __forceinline__ float logit_grad(const RowOut& o, float x, Scale c) {
+  const float t = c.of(x - o.m);
   return exp2_fast(t) * fmaf(o.d, finite_t(t), o.b);
 }
 
 // The sums of `lanes` neighbouring lanes (a power of two) joined, in all of them.
-__device__ __forceinline__ RowSums lanes_join(RowSums r, float c2, uint32_t lanes) {
+__device__ __forceinline__ RowSums lanes_join(RowSums r, const Scale& c, uint32_t lanes) {
   float m = r.m;
   for (uint32_t o = lanes / 2; o; o /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
-  const float t = (r.m - usable_max(m)) * c2, e = exp2_fast(t);
-  r = {m, e * r.s, e * (r.q + finite_t(t) * r.s)};
+  r = against(r, m, c);
   for (uint32_t o = lanes / 2; o; o /= 2) {
     r.s += __shfl_xor_sync(~0u, r.s, o);
     r.q += __shfl_xor_sync(~0u, r.q, o);
+    r.one += __shfl_xor_sync(~0u, r.one, o);
   }
   return r;
 }

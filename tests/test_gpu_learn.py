@@ -102,6 +102,20 @@ def test_scores_and_gradient(rows, vocab, stride, shift, dtype):
     assert torch.equal(x, g) and torch.isnan(buf).sum() == around
 
 
+@pytest.mark.parametrize("vocab,rows", [(3, 60000), (390, 8000), (6000, 4000), (50001, 1000)])
+def test_scores_are_not_off_the_same_way(vocab, rows):
+    """A preference loss adds hundreds of log-probabilities up, so what they are all off by counts.  Their errors are
+    roundings to 32 bits (below 2^-21 each, of either sign: 4 standard deviations of their mean are allowed), and half a
+    unit of the sum of exponentials where its last bit decides: 3e-8."""
+    gen = torch.Generator(device="cuda").manual_seed(vocab)
+    x = torch.randn(rows, vocab, generator=gen, device="cuda") * 2
+    y = torch.randint(vocab, (rows,), generator=gen, device="cuda")
+    for tau in (1.0, 0.7):
+        want = torch.log_softmax(x.double() / float(np.float32(tau)), 1).gather(1, y[:, None])[:, 0]
+        off = (bf.token_logprobs(x, y, temperature=tau).double() - want).mean().item()
+        assert abs(off) < 3e-8 + 4 * 2.0 ** -21 / np.sqrt(12 * rows), off
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("vocab", [5, 40, 1500, 9000, 40000])
 def test_masked_logits(dtype, vocab):
