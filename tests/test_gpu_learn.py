@@ -315,6 +315,74 @@ def test_preference(vocab, lengths, eps, margin, average, reference, tau, dtype)
     assert torch.equal(c["x"], got.grad)
 
 
+@pytest.mark.parametrize("dtype,vocab,lengths,unscored", [
+    ("bf16", 16384, [300, 280, 1, 0, 0, 0, 700, 3, 20, 900, 33, 34, 2, 500, 400, 401], 0.2),
+    ("f32", 9001, [1500, 1400, 5, 6, 900, 800, 0, 700], 0.0),
+    ("f16", 20000, [2000, 1], 0.5), ("bf16", 2500, [40] * 400, 0.3), ("bf16", 131072, [30, 31, 32, 33, 1, 2], 0.1)])
+def test_preference_sizes(dtype, vocab, lengths, unscored):
+    """Rows enough for several stretches of L2's size, pairs of every length among them, in 64 bits on the GPU."""
+    gen = torch.Generator(device="cuda").manual_seed(vocab)
+    rows, before, after = sum(lengths), 3, 5
+    total = rows + before + after
+    x = (torch.randn(total, vocab, generator=gen, device="cuda") * 2).to(TYPES[dtype])
+    y = torch.randint(vocab, (total,), generator=gen, device="cuda")
+    y[torch.rand(total, generator=gen, device="cuda") < unscored] = -1
+    cuts = (np.cumsum([0] + lengths) + before).tolist()
+    offsets = torch.tensor(cuts, device="cuda")
+    seq = torch.full((total,), -1, device="cuda")
+    for k, (a, b) in enumerate(zip(cuts, cuts[1:])):
+        seq[a:b] = k
+    on = (seq >= 0) & (y >= 0)
+    lp = torch.zeros(total, dtype=torch.float64, device="cuda")
+    for a in range(0, total, 512):
+        z = torch.log_softmax(x[a:a + 512].double(), 1)
+        lp[a:a + 512] = z.gather(1, y[a:a + 512].clamp(min=0)[:, None])[:, 0]
+    lp = torch.where(on, lp, 0.0)
+    ref = (lp + 0.3 * torch.randn(total, generator=gen, device="cuda")).float()
+    got = bf.preference_loss(x, y, offsets, ref, beta=0.2, label_smoothing=0.1, margin=0.1)
+    close_scores(got.logprob, lp.cpu().numpy())
+    reward = torch.zeros(len(lengths), dtype=torch.float64, device="cuda")
+    reward.index_add_(0, seq[on], 0.2 * (lp - ref.double())[on])
+    # a row's error is a rounding of at most 2^-21 (32-bit values near 16) and as much of the sum it is added to
+    reach = 0.2 * 2.0 ** -21 * max(lengths) + 1e-6
+    assert torch.all((got.rewards.double() - reward).abs() <= reach)
+    h = reward[0::2] - reward[1::2] - 0.1
+    pairs = len(lengths) // 2
+    up, down = torch.sigmoid(h), torch.sigmoid(-h)
+    loss = -(0.9 * torch.nn.functional.logsigmoid(h) + 0.1 * torch.nn.functional.logsigmoid(-h)).mean()
+    want = torch.stack([loss, (reward[0::2] > reward[1::2]).double().mean(), reward[0::2].mean(), reward[1::2].mean()])
+    assert torch.all((got.stats.double() - want).abs() <= 2 * reach + 1e-5 * want.abs())
+    slope = 0.2 * (0.1 * up - 0.9 * down) / pairs
+    parts = 0.2 * (0.1 * up + 0.9 * down) / pairs
+    both = lambda v, s: torch.stack([v, s * v], 1).reshape(-1)
+    a, size = both(slope, -1.0), both(parts, 1.0)
+    for r in range(0, total, 512):
+        t, q = y[r:r + 512], seq[r:r + 512]
+        p = torch.softmax(x[r:r + 512].double(), 1)
+        hit = torch.zeros_like(p).scatter_(1, t.clamp(min=0)[:, None], 1.0)
+        live = on[r:r + 512, None]
+        w = torch.where(live, a[q.clamp(min=0)][:, None] * (hit - p), 0.0)
+        far = torch.where(live, size[q.clamp(min=0)][:, None] * (hit + p), 0.0)
+        bound = (5e-5 + 2 * reach) * far + ROUND[dtype] * w.abs() + LEAST[dtype]
+        assert torch.all((got.grad[r:r + 512].double() - w).abs() <= bound)
+    again = bf.preference_loss(x, y, offsets, ref, beta=0.2, label_smoothing=0.1, margin=0.1)
+    assert all(torch.equal(u, v) for u, v in zip(got, again))
+    only = bf.preference_loss(x, y, offsets, ref, beta=0.2, label_smoothing=0.1, margin=0.1, grad=False)
+    assert torch.all((only.rewards.double() - reward).abs() <= reach)
+    bf.preference_loss(x, y, offsets, ref, beta=0.2, label_smoothing=0.1, margin=0.1, out=x)
+    assert torch.equal(x, got.grad)
+
+
+def test_preference_offsets_that_do_not_ascend():
+    x = torch.randn(40, 6000, device="cuda")
+    y = torch.randint(6000, (40,), device="cuda")
+    for offsets in ([-7, 20, 900], [30, 10, 0], [1 << 40, 5, 1 << 41], [20, 30, 0, 10, 40], [0, 40, 0, 40, 0]):
+        r = bf.preference_loss(x, y, torch.tensor(offsets, device="cuda"))
+        assert torch.isfinite(r.stats).all() and torch.isfinite(r.grad).all()
+    r = bf.preference_loss(x, y * 0 - 1, torch.tensor([0, 10, 40], device="cuda"))
+    assert r.stats[0].item() == pytest.approx(np.log(2)) and not r.grad.any()
+
+
 def test_preference_edges():
     x = torch.randn(4, 6, device="cuda")
     y = torch.tensor([0, 1, 2, 3], device="cuda")
