@@ -110,7 +110,7 @@ struct Layout {
     counts = reinterpret_cast<RowCounts*>(head);
     seq_tokens = reinterpret_cast<uint32_t*>(head + sizeof(RowCounts));
     row_seq = reinterpret_cast<uint32_t*>(take(4 * rows));
-    partial = reinterpret_cast<float*>(take(4 * (pairs ? sequences / 2 : bfk::kPolicyPart * rows)));
+    partial = reinterpret_cast<float*>(take(4 * (pairs ? sequences / 2 : bfk::kPolicyPart * (rows + bfk::kPolicyMoreParts))));
     logprob = nullptr;
     row_softmax = nullptr;
     seq_slope = nullptr;

@@ -82,7 +82,7 @@ __device__ __forceinline__ void write_n(E* p, const float* f) {
 
 // ---- forward: kPieces pieces of N elements a thread, all read before the first is written ----
 
-constexpr uint32_t kPieces = 4;
+constexpr uint32_t kPieces = 2;
 
 template <typename E, int N, typename I>
 __global__ void __launch_bounds__(kThreads) embed_kernel(const EmbedArgs a, I pieces, uint32_t per_row) {

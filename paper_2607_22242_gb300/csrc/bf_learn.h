@@ -16,6 +16,7 @@ enum class RowOp { kScore, kScoreGrad, kPolicy, kPairScore, kPairGrad };
 constexpr uint32_t kNoSequence = 0xFFFFFFFFu;
 constexpr uint32_t kPolicySums = 5;  // surrogate, KL, entropy, clipped share, ratio: weighted sums over the rows
 constexpr uint32_t kPolicyPart = 8;  // floats that a part of them takes
+constexpr uint32_t kPolicyMoreParts = 256;
 
 // Counts of a call's scored tokens, in its workspace.
 struct RowCounts {
@@ -51,7 +52,8 @@ struct RowArgs {
   uint32_t advantage_per_token;
   uint32_t reduction;  // bf_reduction
   float ratio_lo, ratio_hi, kl_coef, entropy_coef, grad_scale;
-  float* partial;  // kPolicy: kPolicyPart floats (the sums) for each block, or each row of logits at most
+  float* partial;  // kPolicy: kPolicyPart floats (the sums) a part; as many as rows, and kPolicyMoreParts more
+  bool sums_behind;  // kPolicy: a kernel behind sums the parts up
   float* stats;
   // kPairScore writes and kPairGrad reads what a row's probabilities are made from; kPairGrad's slope of each sequence
   float2* row_softmax;  // (max, 1 / sum)

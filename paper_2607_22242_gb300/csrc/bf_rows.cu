@@ -42,11 +42,10 @@ __device__ __forceinline__ void put_policy_stats(const RowArgs& a, float total) 
   }
 }
 
-// The same from its parts' sums, in an order that does not depend on when blocks ran.
-__device__ __forceinline__ void policy_stats(const RowArgs& a, uint64_t parts, float* buf) {
-  last_sees();
+// The sums of `parts` parts from `from` on, the k-th in thread k.
+__device__ __forceinline__ float sum_parts(const float* from, uint64_t parts, float* buf) {
   float v[kPolicySums] = {};
-  const float4* part = reinterpret_cast<const float4*>(a.partial);  // kPolicyPart floats each
+  const float4* part = reinterpret_cast<const float4*>(from);  // kPolicyPart floats each
   constexpr uint32_t kAhead = 8;  // one block reads them all: at one a time it took a fifth of a short call
   for (uint64_t i = threadIdx.x; i < parts; i += kAhead * blockDim.x) {
     float4 lo[kAhead];
@@ -55,7 +54,7 @@ __device__ __forceinline__ void policy_stats(const RowArgs& a, uint64_t parts, f
     for (uint32_t j = 0; j < kAhead; ++j) {
       const uint64_t at = i + j * blockDim.x;
       lo[j] = at < parts ? __ldcg(part + 2 * at) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      hi[j] = at < parts ? __ldcg(a.partial + kPolicyPart * at + 4) : 0.0f;
+      hi[j] = at < parts ? __ldcg(from + kPolicyPart * at + 4) : 0.0f;
     }
 #pragma unroll
     for (uint32_t j = 0; j < kAhead; ++j) {
@@ -66,7 +65,13 @@ __device__ __forceinline__ void policy_stats(const RowArgs& a, uint64_t parts, f
       v[4] += hi[j];
     }
   }
-  const float total = block_sums(v, buf);
+  return block_sums(v, buf);
+}
+
+// The loss from its parts' sums, in an order that does not depend on when blocks ran.
+__device__ __forceinline__ void policy_stats(const RowArgs& a, uint64_t parts, float* buf) {
+  last_sees();
+  const float total = sum_parts(a.partial, parts, buf);
   if (threadIdx.x < 32) put_policy_stats(a, total);
 }
 
@@ -173,13 +178,26 @@ __device__ __forceinline__ void put_many(const Window<E>& x, const Window<E>& g,
 
 constexpr uint32_t kGroupThreads = 256;
 
-// The block's part of the policy loss.  Said before the gradient is stored, so
-// that the fence has only these few values to wait for: after the stores, it
-// cost a fifth of the kernel's time.  The last block sums up at its end.
+// The part of the policy loss that a block's rows have.  Said before the
+// gradient is stored, so that the fence has only these few values to wait for:
+// after the stores, it cost a fifth of the kernel's time.  The last block sums
+// up at its end.  Above kMostSaying blocks, each warp leaves its part without
+// waiting for others and a kernel behind sums up.
 __device__ __forceinline__ bool say_policy_part(const RowArgs& a, const RowOut& o, bool mine, uint32_t lanes, float* buf) {
   float v[kPolicySums];
 #pragma unroll
   for (uint32_t k = 0; k < kPolicySums; ++k) v[k] = mine ? o.sums[k] : 0.0f;
+  if (a.sums_behind) {
+#pragma unroll
+    for (uint32_t k = 0; k < kPolicySums; ++k)
+      for (uint32_t d = 16; d >= lanes && d; d /= 2) v[k] += __shfl_down_sync(~0u, v[k], d);
+    if (threadIdx.x % 32 == 0) {
+      float* part = a.partial + ((uint64_t)blockIdx.x * (kGroupThreads / 32) + threadIdx.x / 32) * kPolicyPart;
+      *reinterpret_cast<float4*>(part) = make_float4(v[0], v[1], v[2], v[3]);
+      part[4] = v[4];
+    }
+    return false;
+  }
   const float sum = block_sums(v, buf, lanes);
   if (threadIdx.x >= 32) return false;
   if (threadIdx.x < kPolicySums) a.partial[(uint64_t)blockIdx.x * kPolicyPart + threadIdx.x] = sum;
@@ -187,7 +205,7 @@ __device__ __forceinline__ bool say_policy_part(const RowArgs& a, const RowOut& 
 }
 
 template <RowOp op, int N>
-__global__ void __launch_bounds__(kGroupThreads) short_kernel(const RowArgs a) {
+__global__ void __launch_bounds__(kGroupThreads) short_kernel(const RowArgs a, uint32_t) {
   const uint64_t row = (uint64_t)blockIdx.x * kGroupThreads + threadIdx.x;
   const bool here = row < a.rows;
   if constexpr (kFollows<op>) let_next_start();
@@ -229,7 +247,28 @@ __global__ void __launch_bounds__(kGroupThreads) short_kernel(const RowArgs a) {
     }
   }
   if constexpr (op == RowOp::kPolicy) {
-    if (__syncthreads_or(last)) policy_stats(a, gridDim.x, buf);
+    if (!a.sums_behind && __syncthreads_or(last)) policy_stats(a, gridDim.x, buf);
+  }
+}
+
+// Behind a grid of many blocks: each of these sums up a stretch of the warps' parts into its own, the last one those.
+constexpr uint32_t kMostSaying = 608, kSumBlocks = 128;
+
+__global__ void __launch_bounds__(kGroupThreads) policy_sum_kernel(const RowArgs a, uint32_t parts) {
+  __shared__ float buf[kGroupThreads / 32 * kPolicySums];
+  wait_for_previous();
+  const uint32_t each = (parts + kSumBlocks - 1) / kSumBlocks, first = min(parts, blockIdx.x * each);
+  const float sum = sum_parts(a.partial + (uint64_t)first * kPolicyPart, min(parts, first + each) - first, buf);
+  bool last = false;
+  float* mine = a.partial + (uint64_t)parts * kPolicyPart;
+  if (threadIdx.x < 32) {
+    if (threadIdx.x < kPolicySums) mine[blockIdx.x * kPolicyPart + threadIdx.x] = sum;
+    last = last_to_say(&a.counts->blocks_done, kSumBlocks);
+  }
+  if (__syncthreads_or(last)) {
+    last_sees();
+    const float total = sum_parts(mine, kSumBlocks, buf);
+    if (threadIdx.x < 32) put_policy_stats(a, total);
   }
 }
 
@@ -267,7 +306,7 @@ __global__ void __launch_bounds__(kGroupThreads, op == RowOp::kPolicy ? 3 : 4) w
     }
   }
   if constexpr (op == RowOp::kPolicy) {
-    if (__syncthreads_or(last)) policy_stats(a, gridDim.x, buf);
+    if (!a.sums_behind && __syncthreads_or(last)) policy_stats(a, gridDim.x, buf);
   }
 }
 
@@ -528,12 +567,15 @@ uint32_t vectors_of(const RowArgs& a) {
 template <RowOp op, bool entropy>
 cudaError_t launch_op(const RowArgs& a, cudaStream_t st) {
   const auto group = [&](auto kernel, uint32_t lanes) {
-    return launch_shaped(kernel, (a.rows * lanes + kGroupThreads - 1) / kGroupThreads, kGroupThreads, 1, kFollows<op>, st, a, lanes);
+    const uint64_t blocks = (a.rows * lanes + kGroupThreads - 1) / kGroupThreads;
+    RowArgs b = a;
+    b.sums_behind = op == RowOp::kPolicy && blocks > kMostSaying;
+    const cudaError_t e = launch_shaped(kernel, blocks, kGroupThreads, 1, kFollows<op>, st, b, lanes);
+    if (e != cudaSuccess || !b.sums_behind) return e;
+    return launch_after(policy_sum_kernel, kSumBlocks, kGroupThreads, st, b, (uint32_t)blocks * (kGroupThreads / 32));
   };
   const uint32_t vectors = vectors_of(a);
-  if (a.vocab <= 4)
-    return launch_shaped(short_kernel<op, 4>, (a.rows + kGroupThreads - 1) / kGroupThreads, kGroupThreads, 1, kFollows<op>,
-                         st, a);
+  if (a.vocab <= 4) return group(short_kernel<op, 4>, 1);
   if (vectors <= 2) return group(warp_kernel<op, entropy, 2>, 1);
   if (vectors <= 8) return group(warp_kernel<op, entropy, 4>, pow2_up(div_up(vectors, 4)));
   if (vectors <= 256) return group(warp_kernel<op, entropy, 8>, pow2_up(div_up(vectors, 8)));
