@@ -377,13 +377,17 @@ constexpr uint32_t kJoinThreads = 512;
 
 template <typename D, int N>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const SumArgs a, uint32_t lanes) {
+  constexpr uint32_t kAhead = 8;  // partial rows read before they are added
   __shared__ float stretch[kJoinThreads * N];
   wait_for_previous();
   const uint32_t groups = kJoinThreads / lanes, group = threadIdx.x / lanes, lane = threadIdx.x % lanes;
   const uint32_t runs = *a.runs;
   for (uint32_t r = blockIdx.x; r < runs; r += gridDim.x) {
     const uint32_t tile = a.runs[1 + r], key = a.key[(uint64_t)tile * kTile + kTile - 1];
-    uint32_t lo = tile, hi = a.tiles;  // the last tile that begins with this token: 32 probes at a time
+    // The last tile that begins with this token: among the next 32, or by 32 probes at a time.
+    const uint32_t near = tile + 1 + threadIdx.x % 32;
+    const uint32_t other = __ballot_sync(~0u, near >= a.tiles || a.key[(uint64_t)near * kTile] != key);
+    uint32_t lo = tile + (other ? __ffs(other) - 1 : 32), hi = other ? lo + 1 : a.tiles;
     while (hi - lo > 1) {
       const uint32_t step = (hi - lo + 31) / 32, probe = lo + threadIdx.x % 32 * step;
       const uint32_t at_most = __ballot_sync(~0u, probe == lo || (probe < hi && a.key[(uint64_t)probe * kTile] <= key));
@@ -395,12 +399,15 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const SumArgs a, uin
       const uint32_t c = c0 + lane * N;
       float sum[N] = {};
       if (c < a.e.width) {
-#pragma unroll 4
-        for (uint32_t t = first; t < end; ++t) {
-          float f[N];
-          read_floats<N>(a.partial + (uint64_t)t * 2 * a.e.width + c, f);
+        for (uint32_t t = first; t < end; t += kAhead) {
+          float f[kAhead][N] = {};
 #pragma unroll
-          for (int j = 0; j < N; ++j) sum[j] += f[j];
+          for (uint32_t i = 0; i < kAhead; ++i)
+            if (t + i < end) read_floats<N>(a.partial + (uint64_t)(t + i) * 2 * a.e.width + c, f[i]);
+#pragma unroll
+          for (uint32_t i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j) sum[j] += f[i][j];
         }
       }
       __syncthreads();
