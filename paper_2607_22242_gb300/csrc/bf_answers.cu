@@ -10,8 +10,8 @@ namespace {
 // array.  Counts are sums of whole numbers: their order does not matter.
 
 // Up to kSmallRows rows of up to kSmallSequences sequences: one block, with the
-// offsets and the counts in shared memory (no memory to clear first, 3.5 us
-// where the kernel below and its memset take 7).
+// offsets and the counts in shared memory, no memory to clear first (1,024 rows
+// 3.8 us, 8,000 rows 11 us, beside which the rows' kernel reads its logits).
 constexpr uint32_t kSmallRows = 16384, kSmallSequences = 4096, kSmallThreads = 1024;
 
 __global__ void __launch_bounds__(kSmallThreads) small_sequence_kernel(const int64_t* tokens, uint32_t rows,
@@ -53,6 +53,7 @@ __global__ void __launch_bounds__(kSmallThreads) small_sequence_kernel(const int
 // Any number: counts and seq_tokens are zero at the start.  A block's rows are
 // neighbours, so their sequences are too: one search for its first row by a
 // warp (32 probes at a time), then the offsets from there on in shared memory.
+// 655,360 rows of 65,536 sequences 10 us; a search of all offsets for each row 38 us.
 constexpr uint32_t kRowThreads = 256, kRowsEach = 4, kBlockRows = kRowThreads * kRowsEach;
 constexpr uint32_t kOffsets = kBlockRows;
 

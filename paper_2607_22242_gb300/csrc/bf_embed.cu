@@ -81,6 +81,8 @@ __device__ __forceinline__ void write_n(E* p, const float* f) {
 }
 
 // ---- forward: kPieces pieces of N elements a thread, all read before the first is written ----
+//
+// Bound by memory: 16,384 rows of 2,048 bf16 21 us, 6.4 TB/s (1 piece a thread 27 us, 4 27, 8 39).
 
 constexpr uint32_t kPieces = 2;
 
@@ -111,6 +113,10 @@ __global__ void __launch_bounds__(kThreads) embed_kernel(const EmbedArgs a, I pi
 }
 
 // ---- sort by token: 9 bits a pass, a count and a placing kernel each ----
+//
+// Bound by waiting (16,384 tokens of 131,072: two passes), so it runs beside the
+// clearing of the gradient, which takes 80 us there; a pass of 81,920 tokens of
+// 500 takes 4 + 10 us.
 
 constexpr uint32_t kBits = 9, kBins = 1u << kBits, kSortThreads = kBins;
 constexpr uint32_t kMaxSortTiles = 128;
@@ -318,7 +324,9 @@ __device__ __forceinline__ void put_sum(const SumArgs& a, uint32_t key, uint32_t
 }
 
 // `lanes` threads per tile, N columns a thread at a time; kAhead rows are read
-// before they are added, whatever tokens they belong to.
+// before they are added, whatever tokens they belong to.  81,920 rows of 256 f32
+// 17 us, 4.9 TB/s; 16,384 rows of 2,048 bf16 23 us beside 8,500 rows written.
+// Tiles of 16 or 64 positions: the same within 2 us.
 template <typename S, typename D, int N>
 __global__ void __launch_bounds__(kThreads, N == 8 ? 3 : 4) sum_kernel(const SumArgs a, uint32_t lanes) {
   constexpr uint32_t kAhead = 8;

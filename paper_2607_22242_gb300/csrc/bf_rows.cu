@@ -175,6 +175,10 @@ __device__ __forceinline__ void put_many(const Window<E>& x, const Window<E>& g,
 }
 
 // ---- the shortest rows (three modes): a thread for each, N elements at most ----
+//
+// Bound by waiting, not by its bytes: token and logits, then the sequence, then
+// the advantage arrive one after the other.  655,360 rows of 3 (f32): 13.5 us of
+// a policy loss of 29 us, the counts before it 10 us.
 
 constexpr uint32_t kGroupThreads = 256;
 
@@ -251,8 +255,11 @@ __global__ void __launch_bounds__(kGroupThreads) short_kernel(const RowArgs a, u
   }
 }
 
-// Behind a grid of many blocks: each of these sums up a stretch of the warps' parts into its own, the last one those.
-constexpr uint32_t kMostSaying = 608, kSumBlocks = 128;
+// Behind a grid of many blocks: each of these sums up a stretch of the warps'
+// parts into its own, the last one those.  1,000,000 rows of 3 (3,907 blocks) 43
+// -> 33 us; 655,360 rows (2,560 blocks) 29 -> 27 us, but the launch makes the
+// call 33 us on the host: hence the limit.
+constexpr uint32_t kMostSaying = 3072, kSumBlocks = 128;
 
 __global__ void __launch_bounds__(kGroupThreads) policy_sum_kernel(const RowArgs a, uint32_t parts) {
   __shared__ float buf[kGroupThreads / 32 * kPolicySums];
@@ -273,6 +280,11 @@ __global__ void __launch_bounds__(kGroupThreads) policy_sum_kernel(const RowArgs
 }
 
 // ---- middling rows: 1 to 32 lanes of a warp per row, NV vectors a lane ----
+//
+// All of a row is read at once and stays in registers; lanes join by shuffles.
+// As few lanes as hold the row: what a row costs besides its logits (its loss,
+// two exponentials and a logarithm) is paid once per warp, for 32 / lanes rows.
+// 65,536 rows of 2,048 bf16, gradient: 101 us, 5.3 TB/s; 200,000 rows of 512 88 us.
 
 template <RowOp op, bool entropy, int NV>
 __global__ void __launch_bounds__(kGroupThreads, op == RowOp::kPolicy ? 3 : 4) warp_kernel(const RowArgs a, uint32_t lanes) {
@@ -331,8 +343,13 @@ __device__ __forceinline__ void cluster_store(float* p, uint32_t rank, float v) 
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(v) : "memory");
 }
 
-// `cluster` blocks per row, each with `tiles` tiles of kWideVectors vectors a thread;
-// the last tile stays in registers between the row's sums and its gradient.
+// `cluster` blocks per row, each with `tiles` tiles of kWideVectors vectors a
+// thread; the last tile stays in registers between the row's sums and its
+// gradient, the others are read again from L2 (608 or fewer rows are on their way,
+// 78 MB of the longest).  Bound by memory: 8,192 rows of 131,072 bf16, policy loss
+// 0.62 ms, 6.1 of 6.67 TB/s measured; 2,048 rows of 32,768 f32, gradient with
+// entropies 85 us, 6.0 TB/s; 4,096 rows of 50,001 f16, scores with entropies 62 us,
+// 5.3 TB/s (rows at any alignment).
 template <RowOp op, bool entropy>
 __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, uint32_t cluster, uint32_t tiles) {
   constexpr int NV = kWideVectors;
@@ -434,7 +451,11 @@ __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, 
 // Up to 8 blocks hold all rows in registers, as the warp kernel does, from
 // their sums to their gradient; each block counts the sequences' scored rows for
 // itself, and the blocks meet at cluster barriers instead of kernel ends.  Where
-// it fits, it takes one launch instead of two (policy) or four (preference).
+// it fits, it takes one launch instead of two (policy) or four (preference):
+// 4 pairs, 130 rows of 1,009 f16, 12.6 us against 14.3 and 26 against 33 us on the
+// host; 64 mappings, 1,024 rows of 3, 9.4 us against 8.5 and 24 against 26 us on
+// the host.  From 2,000 rows on the blocks' counting loses (4,096 rows of 3 14.4
+// against 12.4 us).
 constexpr uint32_t kFewThreads = 512, kFewSequences = 1024, kFewRows = 1024;
 
 struct FewShape {
@@ -542,6 +563,14 @@ struct WideShape {
 
 uint32_t div_up(uint32_t a, uint32_t b) { return (a + b - 1) / b; }
 
+// A cluster only where there are few rows (131,072 bf16 columns, gradient, 1 / 2 /
+// 4 / 8 blocks a row: 20 rows 18.6 / 12.4 / 11.3 / 10.4 us, 80 rows 20.4 / 18.4 /
+// 14.8 / 14.4, 300 rows 35.9 / 36.8 / 41.2 / 39.5): its blocks have to start together.
+// Scores read their rows once: 128 threads, with many rows beside each other
+// (4,096 rows of 50,001 f16: 128 / 256 / 512 threads 62 / 66 / 80 us).  A gradient
+// reads its row again from L2, so fewer rows at a time: two tiles a thread, up to 512
+// threads (2,048 rows of 32,768 f32: 128 / 256 / 512 threads 112 / 96 / 90 us; 8,192 rows
+// of 131,072 bf16 920 / 803 / 738 us).
 WideShape wide_shape(uint64_t rows, uint32_t vectors, bool scores) {
   WideShape s = {1, 0, 1};
   while (s.cluster < kMaxCluster && rows * s.cluster <= 400 && div_up(vectors, s.cluster) > 256) s.cluster *= 2;
@@ -575,6 +604,11 @@ cudaError_t launch_op(const RowArgs& a, cudaStream_t st) {
     return launch_after(policy_sum_kernel, kSumBlocks, kGroupThreads, st, b, (uint32_t)blocks * (kGroupThreads / 32));
   };
   const uint32_t vectors = vectors_of(a);
+  // Vectors a lane, then lanes: 655,360 rows of 16 bf16 (2 vectors) 45 us with 2,
+  // 50 with 4; 400,000 of 64 (8 vectors) 56 us with 2 lanes of 4, 66 with 1 of 8;
+  // 200,000 of 512 (64 vectors) 119 us with 8 lanes of 8, 169 with 16 of 4, 283 with
+  // 32 of 2; policy losses.  Up to 4 KB a row: 131,072 rows of 1,024 bf16 123 us here,
+  // 195 with a block a row; 65,536 of 2,048 105 against 111.
   if (a.vocab <= 4) return group(short_kernel<op, 4>, 1);
   if (vectors <= 2) return group(warp_kernel<op, entropy, 2>, 1);
   if (vectors <= 8) return group(warp_kernel<op, entropy, 4>, pow2_up(div_up(vectors, 4)));
