@@ -336,7 +336,8 @@ BF_API int bf_search_batch_noalloc(const bf_scenario_desc* descs, uint32_t count
  * logits are not read, its log-probability and entropy are 0 and its gradient
  * is 0.  A token >= vocab makes its row's values NaN.  Logits may be -inf
  * (banned tokens); a row with none above -inf has log-probability -inf,
- * entropy 0, gradient 0, and terms of 0 in the policy loss.
+ * entropy 0, gradient 0, and terms of 0 in the policy loss.  A probability
+ * below 2^-126 of its row's largest counts as 0.
  */
 enum bf_dtype { BF_F32 = 0, BF_BF16 = 1, BF_F16 = 2 };
 
@@ -351,7 +352,7 @@ typedef struct bf_matrix {
 } bf_matrix;
 
 /* Log-probabilities d_logprob[t] = lp and, unless d_entropy is NULL, entropies
- * d_entropy[t] = H of the rows of `logits`.  temperature > 0. */
+ * d_entropy[t] = H of the rows of `logits`.  1e-18 <= temperature <= 1e18. */
 BF_API int bf_token_logprobs(const bf_matrix* logits, const int64_t* d_tokens, float temperature, float* d_logprob,
                              float* d_entropy, void* cuda_stream);
 
@@ -382,7 +383,7 @@ typedef struct bf_policy_args {
   float clip_low, clip_high;   /* the ratio is held to [1 - clip_low, 1 + clip_high]; >= 0 */
   float kl_coef;               /* >= 0 */
   float entropy_coef;
-  float temperature;           /* > 0 */
+  float temperature;           /* 1e-18 to 1e18 */
   float grad_scale;            /* factor of the gradient (loss scaling), 1 for none */
 } bf_policy_args;
 
@@ -411,7 +412,7 @@ typedef struct bf_preference_args {
   float beta;                  /* > 0 */
   float label_smoothing;       /* eps: in [0, 1) */
   float margin;
-  float temperature;           /* > 0 */
+  float temperature;           /* 1e-18 to 1e18 */
   float grad_scale;            /* factor of the gradient (loss scaling), 1 for none */
 } bf_preference_args;
 

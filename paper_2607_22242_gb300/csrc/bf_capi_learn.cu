@@ -63,6 +63,9 @@ int check_number(float v, bool ok, const char* name, const char* who) {
   return std::isfinite(v) && ok ? BF_OK : fail(BF_EINVAL, "%s: %s = %g is out of its range", who, name, (double)v);
 }
 
+// A temperature whose reciprocals, in two parts, are normal 32-bit numbers.
+int check_temperature(float v, const char* who) { return check_number(v, v >= 1e-18f && v <= 1e18f, "temperature", who); }
+
 #define BF_TRY(call)                         \
   do {                                       \
     if ((call) != BF_OK) return BF_EINVAL;   \
@@ -153,7 +156,7 @@ int bf_token_logprobs(const bf_matrix* logits, const int64_t* d_tokens, float te
   BF_TRY(check_array(d_tokens, logits->rows, 8, "tokens", who));
   BF_TRY(check_array(d_logprob, logits->rows, 4, "logprob", who));
   BF_TRY(check_array(d_entropy, 0, 4, "entropy", who));
-  BF_TRY(check_number(temperature, temperature > 0.0f, "temperature", who));
+  BF_TRY(check_temperature(temperature, who));
   if (logits->rows == 0) return BF_OK;
   RowArgs a = row_args(logits, d_tokens, temperature, nullptr);
   a.logprob = d_logprob;
@@ -171,7 +174,7 @@ int bf_token_logprobs_grad(const bf_matrix* logits, const int64_t* d_tokens, flo
   BF_TRY(check_array(d_tokens, logits->rows, 8, "tokens", who));
   BF_TRY(check_array(d_grad_logprob, logits->rows, 4, "grad_logprob", who));
   BF_TRY(check_array(d_grad_entropy, 0, 4, "grad_entropy", who));
-  BF_TRY(check_number(temperature, temperature > 0.0f, "temperature", who));
+  BF_TRY(check_temperature(temperature, who));
   if (logits->rows == 0) return BF_OK;
   RowArgs a = row_args(logits, d_tokens, temperature, grad);
   a.grad_logprob = d_grad_logprob;
@@ -202,7 +205,7 @@ int bf_policy_loss(const bf_matrix* logits, const bf_policy_args* args, float* d
   BF_TRY(check_array(args->advantage, args->advantage_per_token ? rows : sequences, 4, "advantage", who));
   BF_TRY(check_array(d_stats, 1, 4, "stats", who));
   BF_TRY(check_array(d_logprob, 0, 4, "logprob", who));
-  BF_TRY(check_number(args->temperature, args->temperature > 0.0f, "temperature", who));
+  BF_TRY(check_temperature(args->temperature, who));
   BF_TRY(check_number(args->clip_low, args->clip_low >= 0.0f, "clip_low", who));
   BF_TRY(check_number(args->clip_high, args->clip_high >= 0.0f, "clip_high", who));
   BF_TRY(check_number(args->kl_coef, args->kl_coef >= 0.0f, "kl_coef", who));
@@ -265,7 +268,7 @@ int bf_preference_loss(const bf_matrix* logits, const bf_preference_args* args, 
   BF_TRY(check_array(d_stats, 1, 4, "stats", who));
   BF_TRY(check_array(d_rewards, pairs, 4, "rewards", who));
   BF_TRY(check_array(d_logprob, 0, 4, "logprob", who));
-  BF_TRY(check_number(args->temperature, args->temperature > 0.0f, "temperature", who));
+  BF_TRY(check_temperature(args->temperature, who));
   BF_TRY(check_number(args->beta, args->beta > 0.0f, "beta", who));
   BF_TRY(check_number(args->label_smoothing, args->label_smoothing >= 0.0f && args->label_smoothing < 1.0f,
                       "label_smoothing", who));

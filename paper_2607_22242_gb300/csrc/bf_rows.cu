@@ -2,8 +2,6 @@
 // entropies, their gradient, the clipped policy loss and both passes of the
 // preference loss (arithmetic in bf_rows.cuh).  Compiled once per element type
 // (-DBF_ROWS_TYPE=<bf_dtype>).
-#include <type_traits>
-
 #include "bf_rows.cuh"
 
 #ifndef BF_ROWS_TYPE
@@ -77,20 +75,19 @@ __device__ __forceinline__ void policy_stats(const RowArgs& a, uint64_t parts, f
 
 // (x - m) (hi + lo) as (x - base) hi - r + (x - base) lo: with base = 0 and r =
 // m hi rounded it is two products and sums, the small part last, and what r is
-// off by (`rest`) goes into the factors once per row; in rows whose m hi leaves
-// the 32-bit range (all masked by the type's lowest value), base = m and r = 0.
-// f16 logits never get there.
+// off by (`rest`) goes into the factors once per row, as 1 + rest ln2: below 1e-9
+// off where m hi is below 1,024.  Rows of larger logits (or all masked by the
+// type's lowest value, where m hi leaves the 32-bit range) take base = m, r = 0.
 //
 // Without `exact` the small part is left out, for gradients of 16 bits: 1e-6 of
 // a probability of e^-14.
 template <bool exact>
 struct Exponent {
-  static constexpr bool kShifts = !std::is_same<E, __half>::value;
   float2 hi, lo, base, r;
   float rest;
 
   __device__ __forceinline__ Exponent(float m, Scale c) : hi(make_float2(c.hi, c.hi)), lo(make_float2(c.lo, c.lo)) {
-    const bool fits = !kShifts || fabsf(m) * c.hi < 1e38f;
+    const bool fits = fabsf(m) * c.hi < 1024.0f;
     base = fits ? make_float2(0.0f, 0.0f) : make_float2(-m, -m);
     r = fits ? make_float2(-m * c.hi, -m * c.hi) : make_float2(0.0f, 0.0f);
     rest = fits ? fmaf(exact ? -m : 0.0f, c.lo, fmaf(-m, c.hi, m * c.hi)) : 0.0f;
@@ -98,7 +95,7 @@ struct Exponent {
   // v 2^rest; 2^rest itself, rounded, would be off the same way in every row with this m.
   __device__ __forceinline__ float put_back(float v) const { return fmaf(v, rest * kLn2, v); }
   __device__ __forceinline__ float2 of(float2 x) const {
-    if (kShifts) x = __fadd2_rn(x, base);
+    x = __fadd2_rn(x, base);
     const float2 t = __ffma2_rn(x, hi, r);
     return exact ? __ffma2_rn(x, lo, t) : t;
   }
@@ -348,8 +345,8 @@ __device__ __forceinline__ void cluster_store(float* p, uint32_t rank, float v) 
 // gradient, the others are read again from L2 (608 or fewer rows are on their way,
 // 78 MB of the longest).  Bound by memory: 8,192 rows of 131,072 bf16, policy loss
 // 0.62 ms, 6.1 of 6.67 TB/s measured; 2,048 rows of 32,768 f32, gradient with
-// entropies 85 us, 6.0 TB/s; 4,096 rows of 50,001 f16, scores with entropies 62 us,
-// 5.3 TB/s (rows at any alignment).
+// entropies 85 us, 6.0 TB/s; 4,096 rows of 50,001 f16, scores with entropies 66 us,
+// 5.0 TB/s (rows at any alignment).
 template <RowOp op, bool entropy>
 __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, uint32_t cluster, uint32_t tiles) {
   constexpr int NV = kWideVectors;

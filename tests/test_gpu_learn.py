@@ -102,6 +102,36 @@ def test_scores_and_gradient(rows, vocab, stride, shift, dtype):
     assert torch.equal(x, g) and torch.isnan(buf).sum() == around
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [3, 40, 700, 3000, 20000])
+@pytest.mark.parametrize("level,tau", [(0.0, 1e-3), (0.0, 1e3), (3e4, 1.0), (-3e4, 0.01), (900.0, 0.5), (0.0, 1e-18),
+                                       (0.0, 1e18)])
+def test_large_logits_and_temperatures(vocab, dtype, level, tau):
+    """Logits far from 0 or divided by little: the exponents' differences are exact where their terms are large.  An
+    exponent t is off by 2^-23 |t| and a log-probability as much as its own size, 1e-6 of it.  An exponential below 2^-126
+    is taken as 0: its part of the gradient, (|a| + 100 |c|) 2^-126 / tau at most, is missing."""
+    rng = np.random.default_rng(vocab)
+    buf, x, _ = make_logits(rng, 9, vocab, dtype)
+    x.add_(level)
+    xd = host(x)
+    y = make_tokens(rng, 9, vocab)
+    tau = float(np.float32(tau))
+    lp, h = bf.token_logprobs(x, gpu(y, torch.int64), temperature=tau, entropy=True)
+    want_lp, want_h = R.scores(xd, y, tau)
+    close_scores(lp, want_lp)
+    close_scores(h, want_h)
+    a, c = rng.normal(0, 1, 9).astype(np.float32), rng.normal(0, 0.1, 9).astype(np.float32)
+    g = bf.token_logprobs_grad(x, gpu(y, torch.int64), gpu(a), gpu(c), temperature=tau)
+    want, size = R.scores_grad(xd, y, a.astype(np.float64), c.astype(np.float64), tau)
+    big = np.abs(want) > 65504 if dtype == "f16" else np.abs(want) > 3e38  # beyond the type's range: infinite
+    got = host(g)
+    assert np.all(np.isinf(got[big]) | (np.abs(got[big]) > 6e4))
+    flushed = (np.abs(a) + 100 * np.abs(c)).astype(np.float64)[:, None] * 2.0 ** -126 / tau
+    bound = 5e-5 * size + ROUND[dtype] * np.abs(want) + LEAST[dtype] + flushed
+    fine = ~big & (np.abs(want) + bound < (65504 if dtype == "f16" else 3e38))
+    assert np.all(np.abs(got[fine] - want[fine]) <= bound[fine])
+
+
 @pytest.mark.parametrize("vocab,rows", [(3, 60000), (390, 8000), (6000, 4000), (50001, 1000)])
 def test_scores_are_not_off_the_same_way(vocab, rows):
     """A preference loss adds hundreds of log-probabilities up, so what they are all off by counts.  Their errors are

@@ -55,7 +55,7 @@ BAD_POLICY = [dict(tokens=None), dict(offsets=None), dict(old_logprob=None), dic
               dict(offsets=SOME + 4), dict(old_logprob=SOME + 2), dict(ref_logprob=SOME + 1), dict(advantage=SOME + 1),
               dict(sequences=1 << 31), dict(reduction=3), dict(clip_low=-0.1), dict(clip_high=NAN), dict(kl_coef=-1.0),
               dict(kl_coef=0.1), dict(entropy_coef=INF), dict(temperature=0.0), dict(temperature=-1.0),
-              dict(temperature=INF), dict(grad_scale=NAN)]
+              dict(temperature=INF), dict(temperature=1e-19), dict(temperature=1e19), dict(grad_scale=NAN)]
 
 
 @pytest.mark.parametrize("kw", BAD_POLICY, ids=str)
@@ -101,6 +101,14 @@ def test_bad_buffers(lib):
     assert lib.bf_embed_grad(x, SOME, 1.0, 0, mat(data=SOME + 64), SOME, 1 << 30, None) == bf.BF_EINVAL
     assert lib.bf_embed_grad(x, SOME, 1.0, 0, mat(rows=0, data=1 << 24), SOME, 1 << 30, None) == bf.BF_EINVAL
     assert lib.bf_embed_grad(x, SOME, 1.0, 0, far, SOME, 8, None) == bf.BF_EINVAL
+
+
+@pytest.mark.parametrize("temperature", [0.0, -1.0, 1e-40, 1e-19, 1e19, INF, NAN])
+def test_bad_temperature(lib, temperature):
+    assert lib.bf_token_logprobs(mat(), SOME, temperature, SOME, None, None) == bf.BF_EINVAL
+    assert lib.bf_token_logprobs_grad(mat(), SOME, temperature, SOME, None, mat(), None) == bf.BF_EINVAL
+    assert lib.bf_preference_loss(mat(), preference(temperature=temperature), SOME, SOME, None, None, SOME, 1 << 30,
+                                  None) == bf.BF_EINVAL
 
 
 def test_no_rows_is_a_call_without_work(lib):
