@@ -94,17 +94,17 @@ __device__ __forceinline__ float max_of(const uint4* u) {
   return max_words(reinterpret_cast<const uint32_t*>(u), 4 * N, E());
 }
 
-// The elements of one vector that lie inside [lo, hi), -inf elsewhere: for the
+// The elements of one vector that lie inside [lo, hi), `none` elsewhere: for the
 // ends of a row, which are read and written element by element.  Kept out of
 // line: a row has two such vectors, and their code would be in every unrolled
 // load and store (the kernels stalled for instructions a fifth of the time).
 template <typename E>
-__device__ __noinline__ uint4 load_ends(const E* p, int32_t lo, int32_t hi) {
+__device__ __noinline__ uint4 load_ends(const E* p, int32_t lo, int32_t hi, uint32_t none) {
   constexpr int n = Vec<E>::kWidth;
   uint32_t b[n];
 #pragma unroll
   for (int i = 0; i < n; ++i) {
-    b[i] = minus_inf_bits(E());
+    b[i] = none;
     if (i >= lo && i < hi) {
       if constexpr (sizeof(E) == 4) b[i] = reinterpret_cast<const uint32_t*>(p)[i];
       else b[i] = reinterpret_cast<const uint16_t*>(p)[i];
@@ -127,6 +127,47 @@ __device__ __noinline__ void store_ends(E* p, uint4 u, int32_t lo, int32_t hi) {
     }
 }
 
+// A matrix's bytes.
+struct Extent {
+  uintptr_t begin, end;
+  template <typename E>
+  __device__ __forceinline__ Extent(const E* p, uint64_t rows, uint64_t ld, uint32_t width)
+      : begin((uintptr_t)p), end((uintptr_t)(p + (rows - 1) * ld + width)) {}
+};
+
+// Sixteen bytes of a row from any element j on: the one or two aligned vectors
+// that hold them, to be shifted by take().  Outside the row they are the
+// neighbouring rows' and not used; at the matrix's own ends the row's elements are
+// read one by one.
+template <typename E>
+struct Unaligned {
+  uint4 lo, hi;
+  uint32_t off;  // bytes of lo ahead of them
+
+  __device__ __forceinline__ void load(const E* row, uint32_t width, int64_t j, const Extent& m) {
+    const uintptr_t at = (uintptr_t)row + (uintptr_t)(j * (int64_t)sizeof(E)), base = at & ~(uintptr_t)15;
+    off = (uint32_t)(at & 15);
+    if (base >= m.begin && base + (off ? 32 : 16) <= m.end) {
+      lo = *reinterpret_cast<const uint4*>(base);
+      if (off) hi = *reinterpret_cast<const uint4*>(base + 16);
+    } else {
+      off = 0;
+      lo = load_ends<E>(reinterpret_cast<const E*>(at), j < 0 ? (int32_t)-j : 0,
+                        (int32_t)min((int64_t)Vec<E>::kWidth, (int64_t)width - j), 0);
+    }
+  }
+  __device__ __forceinline__ uint4 take() const {
+    if (off == 0) return lo;
+    const bool two = off & 8, one = off & 4;
+    const uint32_t a0 = two ? lo.z : lo.x, a1 = two ? lo.w : lo.y, a2 = two ? hi.x : lo.z, a3 = two ? hi.y : lo.w,
+                   a4 = two ? hi.z : hi.x, a5 = two ? hi.w : hi.y;
+    const uint32_t b0 = one ? a1 : a0, b1 = one ? a2 : a1, b2 = one ? a3 : a2, b3 = one ? a4 : a3, b4 = one ? a5 : a4;
+    const uint32_t r = off % 4 * 8;
+    return make_uint4(__funnelshift_r(b0, b1, r), __funnelshift_r(b1, b2, r), __funnelshift_r(b2, b3, r),
+                      __funnelshift_r(b3, b4, r));
+  }
+};
+
 // A row of elements as 16-byte vectors: vector v holds elements v * kWidth -
 // shift and on, where shift is how far the row starts behind a 16-byte
 // boundary; vectors [lo, hi) lie in the row as a whole.
@@ -148,7 +189,7 @@ struct Window {
     if (v - lo < whole) return last ? __ldcs(p) : __ldcg(p);
     const uint32_t none = minus_inf_bits(E());
     uint4 u = make_uint4(none, none, none, none);
-    if (v < vectors) u = load_ends<E>(at(v), v ? 0 : (int32_t)shift, (int32_t)(end - v * kWidth));
+    if (v < vectors) u = load_ends<E>(at(v), v ? 0 : (int32_t)shift, (int32_t)(end - v * kWidth), none);
     return u;
   }
   // Whether vectors v, v + step, ... (N of them) all lie in the row as a whole.
@@ -172,6 +213,11 @@ struct Window {
   }
   __device__ __forceinline__ void store(uint32_t v, const uint4& u) const {
     if (v - lo < whole) __stcs(reinterpret_cast<uint4*>(at(v)), u);
+    else if (v < vectors) store_ends<E>(at(v), u, v ? 0 : (int32_t)shift, (int32_t)(end - v * kWidth));
+  }
+  // As store, for what is read again soon.
+  __device__ __forceinline__ void put(uint32_t v, const uint4& u) const {
+    if (v - lo < whole) *reinterpret_cast<uint4*>(at(v)) = u;
     else if (v < vectors) store_ends<E>(at(v), u, v ? 0 : (int32_t)shift, (int32_t)(end - v * kWidth));
   }
   // As store, for values cut into vectors at another row's boundaries (`from` behind one).

@@ -19,49 +19,26 @@ namespace {
 constexpr uint32_t kThreads = 256;
 constexpr uint32_t kTile = 32;  // sorted positions summed by one group of lanes
 
-__device__ __forceinline__ float nan_value() { return __int_as_float(0x7FC00000); }
-
-// N neighbouring elements (N = 1, or the 16 bytes of the row's own type) as 32-bit values and back.
-template <typename E, int N>
-__device__ __forceinline__ void read_n(const E* p, float* f) {
-  if constexpr (N * sizeof(E) == 16) {
-    const uint4 u = *reinterpret_cast<const uint4*>(p);
-    float2 v[N / 2];
-    unpack<E>(u, v);
-#pragma unroll
-    for (int i = 0; i < N; ++i) f[i] = i % 2 ? v[i / 2].y : v[i / 2].x;
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) f[i] = to_f32(p[i]);
-  }
-}
-// The same, still as read: 16 bytes or one element.
-template <typename E, int N>
-struct Piece {
-  uint4 u;
-  __device__ __forceinline__ void load(const E* p) { u = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void add_to(float* sum) const {
-    float2 v[N / 2];
-    unpack<E>(u, v);
-#pragma unroll
-    for (int i = 0; i < N; ++i) sum[i] += i % 2 ? v[i / 2].y : v[i / 2].x;
-  }
-};
+// Sixteen bytes, still as read.
 template <typename E>
-struct Piece<E, 1> {
-  E v;
-  __device__ __forceinline__ void load(const E* p) { v = *p; }
-  __device__ __forceinline__ void add_to(float* sum) const { sum[0] += to_f32(v); }
-};
+__device__ __forceinline__ void add_to(float* sum, const uint4& u) {
+  float2 v[Vec<E>::kWidth / 2];
+  unpack<E>(u, v);
+#pragma unroll
+  for (uint32_t i = 0; i < Vec<E>::kWidth; ++i) sum[i] += i % 2 ? v[i / 2].y : v[i / 2].x;
+}
 template <int N>
 __device__ __forceinline__ void read_floats(const float* p, float* f) {
-  if constexpr (N % 4 == 0) {
 #pragma unroll
-    for (int i = 0; i < N; i += 4) read_n<float, 4>(p + i, f + i);
-  } else {
-    f[0] = *p;
+  for (int i = 0; i < N; i += 4) {
+    const float4 v = *reinterpret_cast<const float4*>(p + i);
+    f[i] = v.x;
+    f[i + 1] = v.y;
+    f[i + 2] = v.z;
+    f[i + 3] = v.w;
   }
 }
+// N neighbouring elements from 32-bit values, where they make up whole vectors or half of one.
 template <typename E, int N>
 __device__ __forceinline__ void write_n(E* p, const float* f) {
   if constexpr (N * sizeof(E) == 16) {
@@ -72,26 +49,37 @@ __device__ __forceinline__ void write_n(E* p, const float* f) {
   } else if constexpr (N * sizeof(E) == 32) {
     write_n<E, N / 2>(p, f);
     write_n<E, N / 2>(p + N / 2, f + N / 2);
-  } else if constexpr (N * sizeof(E) == 8) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(pack2(make_float2(f[0], f[1]), E()), pack2(make_float2(f[2], f[3]), E()));
   } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) p[i] = from_f32<E>(f[i]);
+    static_assert(N * sizeof(E) == 8, "a half, one or two vectors");
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack2(make_float2(f[0], f[1]), E()), pack2(make_float2(f[2], f[3]), E()));
   }
 }
 
 // ---- forward: kPieces pieces of N elements a thread, all read before the first is written ----
 //
-// Bound by memory: 16,384 rows of 2,048 bf16 21 us, 6.4 TB/s (1 piece a thread 27 us, 4 27, 8 39).
+// Bound by memory: 16,384 rows of 2,048 bf16 21 us, 6.4 TB/s (1 piece a thread 27 us, 4 27, 8 39);
+// rows of 2,047, which start at any element, 35 us (75 us element by element).
 
 constexpr uint32_t kPieces = 2;
 
-template <typename E, int N, typename I>
+template <typename E>
+__device__ __forceinline__ uint4 scaled(const uint4& u, float scale) {
+  float2 f[Vec<E>::kWidth / 2];
+  unpack<E>(u, f);
+#pragma unroll
+  for (uint32_t i = 0; i < Vec<E>::kWidth / 2; ++i) f[i] = make_float2(f[i].x * scale, f[i].y * scale);
+  return pack<E>(f);
+}
+
+// `aligned`: every row of both matrices is a row of 16-byte vectors; else a piece
+// is one of the output row's vectors, wherever its elements lie in the table's row.
+template <typename E, bool aligned, typename I>
 __global__ void __launch_bounds__(kThreads) embed_kernel(const EmbedArgs a, I pieces, uint32_t per_row) {
   const I first = (I)blockIdx.x * (kThreads * kPieces) + threadIdx.x;
   I row[kPieces];
   int64_t id[kPieces];
-  float f[kPieces][N] = {};
+  Unaligned<E> u[kPieces] = {};
+  const Extent all(static_cast<const E*>(a.src), a.vocab, a.lds, a.width);
 #pragma unroll
   for (uint32_t k = 0; k < kPieces; ++k) {
     row[k] = (first + k * kThreads) / per_row;
@@ -99,16 +87,25 @@ __global__ void __launch_bounds__(kThreads) embed_kernel(const EmbedArgs a, I pi
   }
 #pragma unroll
   for (uint32_t k = 0; k < kPieces; ++k) {
-    const uint32_t c = (uint32_t)(first + k * kThreads - row[k] * per_row) * N;
-    if (id[k] >= 0 && id[k] < (int64_t)a.vocab) read_n<E, N>(static_cast<const E*>(a.src) + (uint64_t)id[k] * a.lds + c, f[k]);
+    const uint32_t v = (uint32_t)(first + k * kThreads - row[k] * per_row);
+    if (id[k] < 0 || id[k] >= (int64_t)a.vocab) continue;
+    const E* w = static_cast<const E*>(a.src) + (uint64_t)id[k] * a.lds;
+    if constexpr (aligned) {
+      u[k].lo = *reinterpret_cast<const uint4*>(w + (uint64_t)v * Vec<E>::kWidth);
+    } else {
+      const Window<E> o(static_cast<E*>(a.dst) + (uint64_t)row[k] * a.ldd, a.width);
+      if (v < o.vectors) u[k].load(w, a.width, (int64_t)v * Vec<E>::kWidth - o.shift, all);
+    }
   }
 #pragma unroll
   for (uint32_t k = 0; k < kPieces; ++k) {
     if (first + k * kThreads >= pieces) continue;
-    const uint32_t c = (uint32_t)(first + k * kThreads - row[k] * per_row) * N;
-#pragma unroll
-    for (int j = 0; j < N; ++j) f[k][j] = id[k] >= (int64_t)a.vocab ? nan_value() : id[k] < 0 ? 0.0f : f[k][j] * a.scale;
-    write_n<E, N>(static_cast<E*>(a.dst) + (uint64_t)row[k] * a.ldd + c, f[k]);
+    const uint32_t v = (uint32_t)(first + k * kThreads - row[k] * per_row);
+    E* out = static_cast<E*>(a.dst) + (uint64_t)row[k] * a.ldd;
+    const uint32_t nan = sizeof(E) == 4 ? 0x7FC00000u : 0x7FFF7FFFu;  // a NaN in each 16-bit type too
+    const uint4 f = id[k] >= (int64_t)a.vocab ? make_uint4(nan, nan, nan, nan) : scaled<E>(u[k].take(), a.scale);
+    if constexpr (aligned) *reinterpret_cast<uint4*>(out + (uint64_t)v * Vec<E>::kWidth) = f;
+    else Window<E>(out, a.width).put(v, f);
   }
 }
 
@@ -310,26 +307,54 @@ struct SumArgs {
   float* partial;   // per tile: the part of a token that began before it, and of one that goes on after it
   uint32_t* runs;   // number of tokens that go on after the tile they began in, then their tiles, in any order
   uint32_t tiles;
+  uint32_t part_width;  // the width, up to whole vectors
 };
 
+// N values to columns of a row that starts anywhere, the first `count` of them: two 16-bit ones a store where they share a word.
+template <typename D, int N, int first>
+__device__ __forceinline__ void write_pairs(D* p, const float* f, uint32_t count) {
+  if (first == 1 && count > 0) p[0] = from_f32<D>(f[0]);
+#pragma unroll
+  for (int j = first; j < N; j += 2) {
+    if (j + 1 < N && j + 1 < (int)count) *reinterpret_cast<uint32_t*>(p + j) = pack2(make_float2(f[j], f[j + 1]), D());
+    else if (j < (int)count) p[j] = from_f32<D>(f[j]);
+  }
+}
 template <typename D, int N>
+__device__ __forceinline__ void write_some(D* p, const float* f, uint32_t count) {
+  if constexpr (sizeof(D) == 4) {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (j < (int)count) p[j] = f[j];
+  } else {
+    if ((uintptr_t)p % 4) write_pairs<D, N, 1>(p, f, count);
+    else write_pairs<D, N, 0>(p, f, count);
+  }
+}
+
+template <typename D, int N, bool aligned>
 __device__ __forceinline__ void put_sum(const SumArgs& a, uint32_t key, uint32_t c, float* sum) {
   D* out = static_cast<D*>(a.e.dst) + (uint64_t)key * a.e.ldd + c;
 #pragma unroll
   for (int j = 0; j < N; ++j) {
     sum[j] *= a.e.scale;
-    if (a.e.accumulate) sum[j] += to_f32(out[j]);
+    if (a.e.accumulate && (aligned || c + j < a.e.width)) sum[j] += to_f32(out[j]);
   }
-  write_n<D, N>(out, sum);
+  if constexpr (aligned) write_n<D, N>(out, sum);
+  else write_some<D, N>(out, sum, a.e.width - c);
 }
 
 // `lanes` threads per tile, N columns a thread at a time; kAhead rows are read
 // before they are added, whatever tokens they belong to.  81,920 rows of 256 f32
 // 17 us, 4.9 TB/s; 16,384 rows of 2,048 bf16 23 us beside 8,500 rows written.
-// Tiles of 16 or 64 positions: the same within 2 us.
-template <typename S, typename D, int N>
-__global__ void __launch_bounds__(kThreads, N == 8 ? 3 : 4) sum_kernel(const SumArgs a, uint32_t lanes) {
-  constexpr uint32_t kAhead = 8;
+// Tiles of 16 or 64 positions: the same within 2 us.  Rows that start anywhere
+// (not `aligned`): 16,384 rows of 2,047 bf16 into 131,072, whole gradient 139 us (169 us
+// element by element, 107 us aligned).
+template <typename S, typename D, bool aligned>
+__global__ void __launch_bounds__(kThreads, sizeof(S) == 2 ? 3 : 4) sum_kernel(const SumArgs a, uint32_t lanes) {
+  constexpr int N = Vec<S>::kWidth;
+  constexpr uint32_t kAhead = aligned ? 8 : 4;
+  const Extent all(static_cast<const S*>(a.e.src), a.e.rows, a.e.lds, a.e.width);
   __shared__ uint32_t keys[kThreads / 32 * (kTile + 2)];  // with the neighbours on both sides
   __shared__ uint32_t poss[kThreads / 32 * kTile];
   let_next_start();
@@ -351,25 +376,29 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 3 : 4) sum_kernel(const Sum
   const uint32_t count = min(kTile, rows - tile * kTile), last = key[count - 1];
   if (lane == 0 && last < a.e.vocab && key[count] == last && (key[0] != last || key[-1] != last))
     a.runs[1 + atomicAdd(a.runs, 1u)] = tile;
-  float* part = a.partial + (uint64_t)tile * 2 * a.e.width;
+  float* part = a.partial + (uint64_t)tile * 2 * a.part_width;
   for (uint32_t c = lane * N; c < a.e.width; c += lanes * N) {
     float sum[N] = {};
     bool began = key[-1] != key[0];  // the token's first row lies in this tile
     for (uint32_t k = 0; k < count; k += kAhead) {
-      Piece<S, N> piece[kAhead];
+      Unaligned<S> piece[kAhead];
 #pragma unroll
-      for (uint32_t i = 0; i < kAhead; ++i)
-        if (k + i < count && key[k + i] < a.e.vocab)
-          piece[i].load(static_cast<const S*>(a.e.src) + (uint64_t)pos[k + i] * a.e.lds + c);
+      for (uint32_t i = 0; i < kAhead; ++i) {
+        piece[i].off = 0;
+        if (k + i >= count || key[k + i] >= a.e.vocab) continue;
+        const S* row = static_cast<const S*>(a.e.src) + (uint64_t)pos[k + i] * a.e.lds;
+        if constexpr (aligned) piece[i].lo = *reinterpret_cast<const uint4*>(row + c);
+        else piece[i].load(row, a.e.width, c, all);
+      }
 #pragma unroll
       for (uint32_t i = 0; i < kAhead; ++i) {
         if (k + i >= count || key[k + i] >= a.e.vocab) break;
-        piece[i].add_to(sum);
+        add_to<S>(sum, piece[i].take());
         if (key[k + i] == key[k + i + 1]) {
-          if (k + i + 1 == count) write_n<float, N>(part + (began ? a.e.width : 0) + c, sum);
+          if (k + i + 1 == count) write_n<float, N>(part + (began ? a.part_width : 0) + c, sum);
           continue;
         }
-        if (began) put_sum<D, N>(a, key[k + i], c, sum);
+        if (began) put_sum<D, N, aligned>(a, key[k + i], c, sum);
         else write_n<float, N>(part + c, sum);
 #pragma unroll
         for (int j = 0; j < N; ++j) sum[j] = 0.0f;
@@ -383,7 +412,7 @@ __global__ void __launch_bounds__(kThreads, N == 8 ? 3 : 4) sum_kernel(const Sum
 // order: each of its groups of `lanes` threads a stretch of them, then the stretches.
 constexpr uint32_t kJoinThreads = 512;
 
-template <typename D, int N>
+template <typename D, int N, bool aligned>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const SumArgs a, uint32_t lanes) {
   constexpr uint32_t kAhead = 8;  // partial rows read before they are added
   __shared__ float stretch[kJoinThreads * N];
@@ -411,7 +440,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const SumArgs a, uin
           float f[kAhead][N] = {};
 #pragma unroll
           for (uint32_t i = 0; i < kAhead; ++i)
-            if (t + i < end) read_floats<N>(a.partial + (uint64_t)(t + i) * 2 * a.e.width + c, f[i]);
+            if (t + i < end) read_floats<N>(a.partial + (uint64_t)(t + i) * 2 * a.part_width + c, f[i]);
 #pragma unroll
           for (uint32_t i = 0; i < kAhead; ++i)
 #pragma unroll
@@ -423,11 +452,11 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const SumArgs a, uin
       for (int j = 0; j < N; ++j) stretch[j * kJoinThreads + threadIdx.x] = sum[j];
       __syncthreads();
       if (group == 0 && c < a.e.width) {
-        read_floats<N>(a.partial + ((uint64_t)tile * 2 + 1) * a.e.width + c, sum);
+        read_floats<N>(a.partial + ((uint64_t)tile * 2 + 1) * a.part_width + c, sum);
         for (uint32_t g = 0; g < groups; ++g)
 #pragma unroll
           for (int j = 0; j < N; ++j) sum[j] += stretch[j * kJoinThreads + g * lanes + lane];
-        put_sum<D, N>(a, key, c, sum);
+        put_sum<D, N, aligned>(a, key, c, sum);
       }
     }
   }
@@ -441,15 +470,19 @@ bool rows_of_16(const void* p, uint64_t ld, uint32_t width, uint32_t size) {
   return ((uintptr_t)p | (ld * size) | (uint64_t)width * size) % 16 == 0;
 }
 
-template <typename S, typename D, int N>
+template <typename S, typename D, bool aligned>
 cudaError_t launch_sums(const SumArgs& a, cudaStream_t st) {
+  constexpr int N = Vec<S>::kWidth;
   uint32_t lanes = 32;
   while (lanes < kThreads && lanes * N < a.e.width) lanes *= 2;
-  cudaError_t e = launch_after(sum_kernel<S, D, N>, div_up(a.tiles, kThreads / lanes), kThreads, st, a, lanes);
+  cudaError_t e = launch_after(sum_kernel<S, D, aligned>, div_up(a.tiles, kThreads / lanes), kThreads, st, a, lanes);
   if (e != cudaSuccess) return e;
   const uint32_t blocks = a.tiles < 608 ? a.tiles : 608;
-  return launch_after(join_kernel<D, N>, blocks, kJoinThreads, st, a, lanes);
+  return launch_after(join_kernel<D, N, aligned>, blocks, kJoinThreads, st, a, lanes);
 }
+
+// Columns of a partial row: whole vectors of 16-bit elements.
+uint32_t part_width(uint32_t width) { return div_up(width, 8) * 8; }
 
 template <typename S, typename D>
 cudaError_t launch_grad(const EmbedArgs& a, void* workspace, cudaStream_t st) {
@@ -505,10 +538,9 @@ cudaError_t launch_grad(const EmbedArgs& a, void* workspace, cudaStream_t st) {
     if (small || l % 2) from = 1 - from;
   }
   if (rows == 0) return cudaSuccess;
-  const SumArgs m = {a, key[from], pos[from], (float*)at, s.runs, tiles};
-  constexpr int kN = Vec<S>::kWidth;
-  const bool wide = rows_of_16(a.src, a.lds, a.width, sizeof(S)) && rows_of_16(a.dst, a.ldd, a.width, sizeof(D));
-  return wide ? launch_sums<S, D, kN>(m, st) : launch_sums<S, D, 1>(m, st);
+  const SumArgs m = {a, key[from], pos[from], (float*)at, s.runs, tiles, part_width(a.width)};
+  const bool aligned = rows_of_16(a.src, a.lds, a.width, sizeof(S)) && rows_of_16(a.dst, a.ldd, a.width, sizeof(D));
+  return aligned ? launch_sums<S, D, true>(m, st) : launch_sums<S, D, false>(m, st);
 }
 
 template <typename S>
@@ -520,20 +552,20 @@ cudaError_t launch_grad_from(const EmbedArgs& a, void* workspace, cudaStream_t s
   }
 }
 
-template <typename E, int N>
+template <typename E, bool aligned>
 cudaError_t launch_embed_pieces(const EmbedArgs& a, cudaStream_t st) {
-  const uint32_t per_row = div_up(a.width, N);
+  const uint32_t per_row = div_up(a.width + (aligned ? 0 : Vec<E>::kWidth - 1), Vec<E>::kWidth);
   const uint64_t pieces = a.rows * per_row, blocks = (pieces + kThreads * kPieces - 1) / (kThreads * kPieces);
   if (blocks > 0x7FFFFFFFu) return cudaErrorInvalidValue;
   if (pieces + kThreads * kPieces < (1ull << 32))
-    return launch_plain(embed_kernel<E, N, uint32_t>, (uint32_t)blocks, kThreads, st, a, (uint32_t)pieces, per_row);
-  return launch_plain(embed_kernel<E, N, uint64_t>, (uint32_t)blocks, kThreads, st, a, pieces, per_row);
+    return launch_plain(embed_kernel<E, aligned, uint32_t>, (uint32_t)blocks, kThreads, st, a, (uint32_t)pieces, per_row);
+  return launch_plain(embed_kernel<E, aligned, uint64_t>, (uint32_t)blocks, kThreads, st, a, pieces, per_row);
 }
 
 template <typename E>
 cudaError_t launch_embed_typed(const EmbedArgs& a, cudaStream_t st) {
   return rows_of_16(a.src, a.lds, a.width, sizeof(E)) && rows_of_16(a.dst, a.ldd, a.width, sizeof(E))
-             ? launch_embed_pieces<E, Vec<E>::kWidth>(a, st) : launch_embed_pieces<E, 1>(a, st);
+             ? launch_embed_pieces<E, true>(a, st) : launch_embed_pieces<E, false>(a, st);
 }
 
 }  // namespace
@@ -550,7 +582,7 @@ uint64_t embed_grad_bytes(uint64_t rows, uint32_t width) {
   if (rows == 0) return 0;
   const uint64_t tiles = (rows + kTile - 1) / kTile;
   return 4 * align256(4 * rows) + align256(4ull * kBins * kMaxSortTiles) + align256(4 * (tiles + 1)) +
-         align256(4 * 2 * tiles * width);
+         align256(4 * 2 * tiles * part_width(width));
 }
 
 cudaError_t launch_embed_grad(const EmbedArgs& a, void* workspace, cudaStream_t st) {

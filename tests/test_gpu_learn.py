@@ -447,7 +447,8 @@ def test_long_sequences_of_pairs():
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,vocab,width,stride", [(1, 1, 1, 0), (5, 3, 7, 0), (33, 10, 64, 0), (100, 7, 130, 3),
                                                      (64, 500, 256, 0), (1000, 20, 33, 0), (3000, 2, 16, 0),
-                                                     (2100, 70000, 12, 0), (40, 300, 2048, 8), (4500, 4099, 40, 1)])
+                                                     (2100, 70000, 12, 0), (40, 300, 2048, 8), (4500, 4099, 40, 1),
+                                                     (70, 9, 2047, 0), (300, 50, 513, 0), (90, 11, 66, 6), (50, 7, 15, 2)])
 def test_embed(rows, vocab, width, stride, dtype):
     rng = np.random.default_rng([rows, vocab, width])
     _, table, td = make_logits(rng, vocab, width, dtype, stride, stride % 2)
