@@ -333,7 +333,7 @@ BF_API int bf_search_batch_noalloc(const bf_scenario_desc* descs, uint32_t count
  * A row t of logits x (vocab columns) goes with token y = tokens[t].  With
  * temperature tau, z = x / tau, p = softmax(z), lp = ln p_y, H = -sum p ln p.
  * A token below 0 marks a row that is not scored (a prompt, padding): its
- * logits are not read, its log-probability and entropy are 0 and its gradient
+ * logits are not used, its log-probability and entropy are 0 and its gradient
  * is 0.  A token >= vocab makes its row's values NaN.  Logits may be -inf
  * (banned tokens); a row with none above -inf has log-probability -inf,
  * entropy 0, gradient 0, and terms of 0 in the policy loss.  A probability
@@ -341,8 +341,9 @@ BF_API int bf_search_batch_noalloc(const bf_scenario_desc* descs, uint32_t count
  */
 enum bf_dtype { BF_F32 = 0, BF_BF16 = 1, BF_F16 = 2 };
 
-/* A matrix in device memory: element (i, j) is data[i * row_stride + j].
- * At most 2^31 - 1 rows and 2^30 columns, row_stride >= cols. */
+/* A matrix in device memory: element (i, j) is data[i * row_stride + j], at any
+ * address its type allows.  At most 2^31 - 1 rows and 2^30 columns, row_stride
+ * >= cols.  What lies between its rows may be read and is never written. */
 typedef struct bf_matrix {
   void* data;
   uint64_t rows, cols;

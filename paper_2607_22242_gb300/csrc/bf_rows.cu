@@ -324,6 +324,7 @@ __global__ void __launch_bounds__(kGroupThreads, op == RowOp::kPolicy ? 3 : 4) w
 constexpr uint32_t kWideThreads = 512;
 constexpr uint32_t kMaxCluster = 8;
 constexpr int kWideVectors = 8;  // a thread's vectors of a tile
+constexpr uint32_t kChunk = 32 * kWideVectors;  // a warp's
 
 __device__ __forceinline__ void cluster_arrive() {
   __syncwarp();
@@ -344,9 +345,9 @@ __device__ __forceinline__ void cluster_store(float* p, uint32_t rank, float v) 
 // thread; the last tile stays in registers between the row's sums and its
 // gradient, the others are read again from L2 (608 or fewer rows are on their way,
 // 78 MB of the longest).  Bound by memory: 8,192 rows of 131,072 bf16, policy loss
-// 0.62 ms, 6.1 of 6.67 TB/s measured; 2,048 rows of 32,768 f32, gradient with
-// entropies 85 us, 6.0 TB/s; 4,096 rows of 50,001 f16, scores with entropies 66 us,
-// 5.0 TB/s (rows at any alignment).
+// 0.61 ms, 6.2 of 6.67 TB/s measured; 2,048 rows of 32,768 f32, gradient with
+// entropies 87 us, 5.9 TB/s; 4,096 rows of 50,001 f16, scores with entropies 60 us,
+// 5.4 TB/s (rows at any alignment).
 template <RowOp op, bool entropy>
 __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, uint32_t cluster, uint32_t tiles) {
   constexpr int NV = kWideVectors;
@@ -357,7 +358,10 @@ __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, 
   if constexpr (kFollows<op>) let_next_start();
   RowIn in = load_row<E, op>(a, row);
   const Window<E> x(const_cast<E*>(static_cast<const E*>(a.x)) + row * a.ldx, a.vocab);
-  const uint32_t first = rank * tiles * NV * threads + tid;
+  // A warp's vectors of a tile are neighbours: a row's last ones and what is
+  // beyond it fall to few warps, and the others need no test of single vectors
+  // (23,439 rows of 16,736 bf16, gradient: 317 -> 287 us; of 16,741 393 -> 336).
+  const uint32_t warps = threads / 32, first = (rank * tiles * warps + tid / 32) * kChunk + tid % 32;
   uint4 u[NV];
   RowSums r = {kMinusInf, 0.0f, 0.0f, 0.0f};
   const bool read = in.on;
@@ -365,21 +369,24 @@ __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, 
     if (cluster > 1 && op != RowOp::kPairGrad) cluster_arrive();  // seen below: the others run
     for (uint32_t tile = 0; tile < tiles; ++tile) {
       if (op == RowOp::kPairGrad && tile + 1 < tiles) continue;
-      x.load_many(u, first + tile * NV * threads, threads,
-                  op == RowOp::kScore || (op != RowOp::kPairScore && tile + 1 == tiles));
+      const uint32_t v = first + tile * warps * kChunk;
+      const bool some = v - tid % 32 < x.vectors;  // the same in all of a warp
+      if (some) x.load_many(u, v, 32, op == RowOp::kScore || (op != RowOp::kPairScore && tile + 1 == tiles));
       // Only the first blocks find the kernel ahead still running; what it wrote arrives beside the logits.
       if (kFollows<op> && (tile == 0 || op == RowOp::kPairGrad)) {
         wait_for_previous();
         load_row_late<op>(a, row, in);
       }
       if constexpr (op != RowOp::kPairGrad) {
-        const RowSums now = sums_of<NV, kMoment<op, entropy>>(u, scale_of(a));
-        r = tiles > 1 ? join(r, now, scale_of(a)) : now;
+        if (some) {
+          const RowSums now = sums_of<NV, kMoment<op, entropy>>(u, scale_of(a));
+          r = tile ? join(r, now, scale_of(a)) : now;
+        }
       }
     }
     if constexpr (op != RowOp::kPairGrad) {
       r = lanes_join(r, scale_of(a), 32);
-      const uint32_t warps = threads / 32, at = rank * warps + tid / 32;
+      const uint32_t at = rank * warps + tid / 32;
       if (cluster > 1) {
         cluster_wait();
         if (tid % 32 < cluster) {  // a lane per block of the cluster
@@ -426,13 +433,14 @@ __global__ void __launch_bounds__(kWideThreads, 2) wide_kernel(const RowArgs a, 
       const Window<E> g(static_cast<E*>(a.g) + row * a.ldg, a.vocab);
       const Grads<entropy> grads(o, scale_of(a));
       for (uint32_t tile = tiles; tile-- > 0;) {
-        const uint32_t v = first + tile * NV * threads;
-        if (in.on && tile + 1 < tiles) x.load_many(u, v, threads, true);
-        put_many(x, g, u, v, threads, grads, !in.on);
+        const uint32_t v = first + tile * warps * kChunk;
+        if (v - tid % 32 >= x.vectors) continue;
+        if (in.on && tile + 1 < tiles) x.load_many(u, v, 32, true);
+        put_many(x, g, u, v, 32, grads, !in.on);
       }
       if (in.on) {
-        const uint32_t at = (in.y + x.shift) / kW - rank * tiles * NV * threads;  // the vector with the token
-        if (in.known && at < tiles * NV * threads && at % threads == tid)
+        const uint32_t at = (in.y + x.shift) / kW, chunk = at / kChunk - rank * tiles * warps;  // the vector with the token
+        if (in.known && chunk < tiles * warps && chunk % warps == tid / 32 && at % 32 == tid % 32)
           g.row[in.y] = from_f32<E>(logit_grad(o, in.xy, scale_of(a)) + o.hit);
       }
     }
