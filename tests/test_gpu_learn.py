@@ -430,6 +430,42 @@ def test_preference_edges():
     assert r.stats[0].item() == pytest.approx(1e4, rel=1e-3) and torch.isfinite(r.grad).all()
 
 
+@pytest.mark.parametrize("pairs,longest", [(1003, 25), (1, 256), (5, 300), (9, 700), (3, 1500), (2, 3000), (7, 9000),
+                                           (2048, 3)])
+@pytest.mark.parametrize("average", [False, True])
+def test_pairs_of_any_length(pairs, longest, average):
+    """Few threads per answer and many, several pairs together and an odd one behind, in 64 bits on the GPU."""
+    gen = torch.Generator(device="cuda").manual_seed(pairs)
+    lengths = torch.randint(longest // 2, longest + 1, (2 * pairs,), generator=gen, device="cuda")
+    lengths[1::7] = 0
+    offsets = torch.nn.functional.pad(lengths.cumsum(0), (1, 0)) + 2
+    rows, vocab = int(offsets[-1]) + 3, 5
+    x = torch.randn(rows, vocab, generator=gen, device="cuda")
+    y = torch.randint(vocab, (rows,), generator=gen, device="cuda")
+    y[torch.rand(rows, generator=gen, device="cuda") < 0.2] = -1
+    seq = torch.full((rows,), -1, device="cuda")
+    seq[2:rows - 3] = torch.arange(2 * pairs, device="cuda").repeat_interleave(lengths)
+    on = (seq >= 0) & (y >= 0)
+    lp = torch.log_softmax(x.double(), 1).gather(1, y.clamp(min=0)[:, None])[:, 0]
+    ref = (lp + 0.3 * torch.randn(rows, generator=gen, device="cuda")).float()
+    got = bf.preference_loss(x, y, offsets, ref, beta=0.2, average=average)
+    sums = torch.zeros(2 * pairs, dtype=torch.float64, device="cuda")
+    sums.index_add_(0, seq[on], (lp - ref.double())[on])
+    counted = torch.bincount(seq[on], minlength=2 * pairs)
+    reward = 0.2 * sums / (counted.clamp(min=1) if average else 1)
+    # a row's error is a rounding of at most 2^-21 (32-bit values near 16) and as much of the sum it is added to
+    reach = 0.2 * 2.0 ** -21 * longest + 1e-6
+    assert torch.all((got.rewards.double() - reward).abs() <= reach)
+    loss = torch.nn.functional.softplus(reward[1::2] - reward[0::2])
+    assert abs(got.stats[0].item() - loss.mean().item()) <= 2 * reach + 1e-6 * loss.mean().item()
+    mean = torch.stack([(reward[0::2] > reward[1::2]).double().mean(), reward[0::2].mean(), reward[1::2].mean()])
+    close = (reward[0::2] - reward[1::2]).abs() <= 2 * reach  # either answer of such a pair may come out ahead
+    slack = torch.tensor([close.double().mean().item(), reach, reach], dtype=torch.float64, device="cuda") + 1e-6
+    assert torch.all((got.stats[1:].double() - mean).abs() <= slack + 1e-6 * mean.abs())
+    again = bf.preference_loss(x, y, offsets, ref, beta=0.2, average=average)
+    assert all(torch.equal(u, v) for u, v in zip(got, again))
+
+
 def test_long_sequences_of_pairs():
     gen = torch.Generator(device="cuda").manual_seed(5)
     rows, vocab = 60000, 5
