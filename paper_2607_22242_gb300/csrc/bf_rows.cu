@@ -345,7 +345,7 @@ __device__ __forceinline__ void cluster_store(float* p, uint32_t rank, float v) 
 // thread; the last tile stays in registers between the row's sums and its
 // gradient, the others are read again from L2 (608 or fewer rows are on their way,
 // 78 MB of the longest).  Bound by memory: 8,192 rows of 131,072 bf16, policy loss
-// 0.61 ms, 6.2 of 6.67 TB/s measured; 2,048 rows of 32,768 f32, gradient with
+// 0.617 ms, 6.1 of 6.67 TB/s measured; 2,048 rows of 32,768 f32, gradient with
 // entropies 87 us, 5.9 TB/s; 4,096 rows of 50,001 f16, scores with entropies 60 us,
 // 5.4 TB/s (rows at any alignment).
 template <RowOp op, bool entropy>

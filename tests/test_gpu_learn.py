@@ -314,6 +314,27 @@ def test_policy_ratio_beyond_range():
     assert r.stats[1].item() == pytest.approx(-0.6) and not r.grad.any()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab", [(1000000, 3), (900, 3), (1000000, 7), (500000, 46), (200000, 455), (40000, 2500)])
+def test_log_probabilities_are_not_off_to_one_side(rows, vocab, dtype):
+    """A preference loss adds many up: their mean error is far below a rounding."""
+    gen = torch.Generator(device="cuda").manual_seed(vocab)
+    errors = []
+    for _ in range(max(1, 200000 // rows)):
+        x = (torch.randn(rows, vocab, generator=gen, device="cuda") * 2).to(TYPES[dtype])
+        y = torch.randint(vocab, (rows,), generator=gen, device="cuda")
+        x[torch.arange(rows, device="cuda"), y] += (torch.rand(rows, generator=gen, device="cuda") * 4).to(TYPES[dtype])
+        want = torch.cat([torch.log_softmax(x[a:a + 50000].double(), 1).gather(1, y[a:a + 50000, None])[:, 0]
+                          for a in range(0, rows, 50000)])
+        # a pair of half the rows each takes the way of few rows where there are few
+        got = bf.preference_loss(x, y, torch.tensor([0, rows // 2, rows], device="cuda"), grad=False).logprob
+        errors.append(got.double() - want)
+    errors = torch.cat(errors)
+    # A value's own roundings, of either sign, are a few 2^-24 of sizes up to 8, so their mean over n rows is within 4
+    # standard errors of 0; what is left is held to 1e-8, a fifth of ex2.approx's shortfall of 5e-8.
+    assert abs(errors.mean().item()) <= 1e-8 + 4 * errors.std().item() / len(errors) ** 0.5
+
+
 # ---- preference loss ----
 
 @pytest.mark.parametrize("dtype", TYPES)
