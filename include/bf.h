@@ -334,9 +334,10 @@ BF_API int bf_search_batch_noalloc(const bf_scenario_desc* descs, uint32_t count
  * temperature tau, z = x / tau, p = softmax(z), lp = ln p_y, H = -sum p ln p.
  * A token below 0 marks a row that is not scored (a prompt, padding): its
  * logits are not used, its log-probability and entropy are 0 and its gradient
- * is 0.  A token >= vocab makes its row's values NaN.  Logits may be -inf
- * (banned tokens); a row with none above -inf has log-probability -inf,
- * entropy 0, gradient 0, and terms of 0 in the policy loss.  A probability
+ * is 0.  A token >= vocab makes its row's values NaN (log-probability,
+ * entropy, gradient, terms of a loss), whatever the row's logits.  Logits may
+ * be -inf (banned tokens); a row with none above -inf has log-probability
+ * -inf, entropy 0, gradient 0, and terms of 0 in the policy loss.  A probability
  * below 2^-126 of its row's largest counts as 0.
  */
 enum bf_dtype { BF_F32 = 0, BF_BF16 = 1, BF_F16 = 2 };

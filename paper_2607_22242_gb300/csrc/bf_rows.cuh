@@ -152,9 +152,9 @@ __device__ __forceinline__ void load_row_late(const RowArgs& a, uint64_t row, Ro
 }
 
 // The row's outputs from its sums (written by the caller's leading thread) and
-// its gradient's factors.  A row without a logit above -inf has log-probability
-// -inf, entropy 0, loss term 0 and gradient 0; a token outside the vocabulary
-// makes its row's values NaN.
+// its gradient's factors.  A token outside the vocabulary makes its row's values
+// NaN, whatever its logits; else a row without a logit above -inf has
+// log-probability -inf, entropy 0, loss term 0 and gradient 0.
 template <RowOp op>
 __device__ __forceinline__ RowOut finish_row(const RowArgs& a, uint64_t row, const RowIn& in, const RowSums& r,
                                              bool leader) {
@@ -180,8 +180,8 @@ __device__ __forceinline__ RowOut finish_row(const RowArgs& a, uint64_t row, con
   const Log log_s = log_of(r.s, kExp2Short * (r.s - r.one) * inv_s);
   const float ln_s = log_s.big + log_s.low;
   float lp = none ? kMinusInf : less((in.xy - o.m) / a.tau, log_s);
-  const float h = none ? 0.0f : ln_s - kLn2 * r.q * inv_s;
-  if (!in.known) lp = __int_as_float(0x7FC00000);
+  float h = none ? 0.0f : ln_s - kLn2 * r.q * inv_s;
+  if (!in.known) lp = h = __int_as_float(0x7FC00000);
   if (leader) {
     if (a.logprob) a.logprob[row] = lp;
     if (a.entropy) a.entropy[row] = h;
@@ -190,8 +190,8 @@ __device__ __forceinline__ RowOut finish_row(const RowArgs& a, uint64_t row, con
     if (leader) a.row_softmax[row] = make_float2(o.m, inv_s);
   }
   if constexpr (op == RowOp::kScore || op == RowOp::kPairScore) return o;
-  if (none) return o;
-  float slope_lp = in.slope_lp, slope_h = in.slope_h;
+  if (none && in.known) return o;
+  float slope_lp = in.known ? in.slope_lp : lp, slope_h = in.slope_h;
   if constexpr (op == RowOp::kPolicy) {
     const float ratio = expf(lp - in.old_lp);
     const bool clipped = in.adv >= 0.0f ? ratio > a.ratio_hi : ratio < a.ratio_lo;

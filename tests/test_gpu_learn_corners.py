@@ -1,0 +1,78 @@
+"""Corners of the operators that learn from makespans: tokens outside the vocabulary, infinite terms beside coefficients
+of 0, rows whose mask leaves nothing, sums of many blocks, and what autograd is told."""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from paper_2607_22242_gb300 import bf  # noqa: E402
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+ROUND = {"f32": 2.0 ** -23, "bf16": 2.0 ** -8, "f16": 2.0 ** -10}     # twice half a unit in the last place
+INF = float("inf")
+
+# Rows x vocabulary: a thread, some lanes and a block or cluster per row; the losses of the first three run in one launch.
+SHAPES = [(8, 3), (8, 50), (8, 700), (1100, 3), (1100, 50), (1100, 700), (8, 6000), (500, 6000), (4, 131073)]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    assert torch.cuda.is_available()
+    bf.load()
+
+
+def draw(rows, vocab, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(rows + vocab)
+    x = (torch.randn(rows, vocab, generator=gen, device="cuda") * 2).to(TYPES[dtype])
+    return gen, x, torch.randint(vocab, (rows,), generator=gen, device="cuda")
+
+
+def cuts(rows, parts):
+    return torch.tensor([rows * k // parts for k in range(parts + 1)], device="cuda")
+
+
+# ---- a token outside the vocabulary makes its row's values NaN, and no other's ----
+
+def with_unknown(y, vocab):
+    """The tokens with the first and last outside the vocabulary, the last by its high bits alone."""
+    y = y.clone()
+    y[0], y[-1] = vocab, (1 << 32) + 1
+    return y, y >= vocab
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab", SHAPES)
+def test_unknown_token_in_scores(rows, vocab, dtype):
+    gen, x, y = draw(rows, vocab, dtype)
+    y, out = with_unknown(y, vocab)
+    x[0] = -INF  # a mask that leaves nothing does not hide it
+    lp, h = bf.token_logprobs(x, y, entropy=True)
+    assert torch.equal(torch.isnan(lp), out) and torch.equal(torch.isnan(h), out)
+    a, c = torch.randn(rows, generator=gen, device="cuda"), torch.randn(rows, generator=gen, device="cuda")
+    known = torch.where(out, -1, y)
+    for slopes in ((a, c), (a, None), (torch.zeros_like(a), c), (torch.zeros_like(a), None)):
+        g = bf.token_logprobs_grad(x, y, *slopes)
+        assert torch.isnan(g[out]).all()
+        assert torch.equal(g[~out], bf.token_logprobs_grad(x, known, *slopes)[~out])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab", SHAPES)
+def test_unknown_token_in_losses(rows, vocab, dtype):
+    gen, x, y = draw(rows, vocab, dtype)
+    y, out = with_unknown(y, vocab)
+    x[0] = -INF
+    old, adv = torch.full((rows,), -2.0, device="cuda"), torch.tensor([1.0, -1.0], device="cuda")
+    for entropy_coef in (0.0, 0.01):
+        got = bf.policy_loss(x, y, cuts(rows, 2), old, adv, entropy_coef=entropy_coef)
+        known = bf.policy_loss(x, y.clamp(max=vocab - 1), cuts(rows, 2), old, adv, entropy_coef=entropy_coef)
+        assert torch.isnan(got.stats[0]) and torch.equal(torch.isnan(got.logprob), out)
+        assert torch.isnan(got.grad[out]).all() and torch.equal(got.grad[~out], known.grad[~out])
+    # the first of two pairs has it: its gap has no value
+    y[-1] = 0
+    out[-1] = False
+    got = bf.preference_loss(x, y, cuts(rows, 4))
+    known = bf.preference_loss(x, torch.where(out, -1, y), cuts(rows, 4))
+    assert torch.equal(torch.isnan(got.logprob), out) and torch.isnan(got.rewards).tolist() == [True, False, False, False]
+    assert torch.isnan(got.grad[0]).all()
+    assert torch.equal(got.grad[rows // 2:], known.grad[rows // 2:]) and torch.isfinite(known.grad).all()
