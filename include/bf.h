@@ -395,9 +395,11 @@ typedef struct bf_policy_args {
  * r = e^(lp - old), advantage A and u = ref - lp, a scored row's term is
  *   l = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A)
  *       + kl_coef (e^u - u - 1) - entropy_coef H
- * and the loss is sum w l.  d_stats: the loss, then the weighted sums of
- * -min(...), of e^u - u - 1 (0 without ref_logprob), of H, of the rows whose
- * clip stops the gradient, and of r.  d_logprob (may be NULL): lp of each row.
+ * and the loss is sum w l; with kl_coef = 0 a reference is only watched, and
+ * nothing of it gets into the loss or the gradient.  d_stats: the loss, then
+ * the weighted sums of -min(...), of e^u - u - 1 (0 without ref_logprob), of H,
+ * of the rows whose clip stops the gradient, and of r.  d_logprob (may be
+ * NULL): lp of each row.
  * `grad` (may be NULL: loss only) as for bf_token_logprobs_grad. */
 BF_API int bf_policy_loss(const bf_matrix* logits, const bf_policy_args* args, float* d_stats, float* d_logprob,
                           const bf_matrix* grad, void* d_workspace, uint64_t workspace_bytes, void* cuda_stream);

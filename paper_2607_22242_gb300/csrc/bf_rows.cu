@@ -33,7 +33,7 @@ constexpr bool kScores = op == RowOp::kScore || op == RowOp::kPairScore;
 __device__ __forceinline__ void put_policy_stats(const RowArgs& a, float total) {
   const float surrogate = __shfl_sync(~0u, total, 0), kl = __shfl_sync(~0u, total, 1), h = __shfl_sync(~0u, total, 2);
   if (threadIdx.x == 0) {
-    a.stats[0] = -surrogate + a.kl_coef * kl - a.entropy_coef * h;
+    a.stats[0] = -surrogate + (a.kl_coef != 0.0f ? a.kl_coef * kl : 0.0f) - a.entropy_coef * h;
     a.stats[1] = -surrogate;
   } else if (threadIdx.x < kPolicySums) {
     a.stats[threadIdx.x + 1] = total;

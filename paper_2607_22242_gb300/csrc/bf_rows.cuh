@@ -201,7 +201,7 @@ __device__ __forceinline__ RowOut finish_row(const RowArgs& a, uint64_t row, con
     if (a.ref_logprob) {
       const float u = in.ref_lp - lp, em1 = expm1f(u);
       kl = em1 - u;
-      slope_lp -= a.kl_coef * em1;
+      if (a.kl_coef != 0.0f) slope_lp -= a.kl_coef * em1;  // e^u may be infinite, and 0 of it is nothing
     }
     o.sums[0] = in.w * held * in.adv;
     o.sums[1] = in.w * kl;

@@ -76,3 +76,32 @@ def test_unknown_token_in_losses(rows, vocab, dtype):
     assert torch.equal(torch.isnan(got.logprob), out) and torch.isnan(got.rewards).tolist() == [True, False, False, False]
     assert torch.isnan(got.grad[0]).all()
     assert torch.equal(got.grad[rows // 2:], known.grad[rows // 2:]) and torch.isfinite(known.grad).all()
+
+
+# ---- infinite terms beside coefficients of 0 ----
+
+def with_far_reference(rows, vocab, dtype):
+    """Rows of which the second's ratio to the reference overflows and the third's token is banned though drawn."""
+    gen, x, y = draw(rows, vocab, dtype)
+    y[2] = 1
+    x[2, 1] = -INF
+    lp = bf.token_logprobs(x, y)
+    assert lp[2] == -INF
+    ref = torch.where(torch.isinf(lp), -3.0, lp + 0.1)
+    ref[1] += 100.0
+    old = torch.where(torch.isinf(lp), -3.0, lp - 0.05)
+    return x, y, old, ref, torch.randn(2, generator=gen, device="cuda")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab", SHAPES)
+def test_reference_that_is_only_watched(rows, vocab, dtype):
+    """kl_coef = 0: the KL is reported, and neither the loss nor the gradient has anything of it."""
+    x, y, old, ref, adv = with_far_reference(rows, vocab, dtype)
+    for entropy_coef in (0.0, 0.02):
+        kw = dict(entropy_coef=entropy_coef)
+        got = bf.policy_loss(x, y, cuts(rows, 2), old, adv, ref, **kw)
+        want = bf.policy_loss(x, y, cuts(rows, 2), old, adv, **kw)
+        others = [0, 1, 3, 4, 5]
+        assert torch.equal(got.stats[others], want.stats[others]) and torch.isfinite(want.stats).all()
+        assert torch.equal(got.grad, want.grad) and torch.isfinite(want.grad).all()
