@@ -200,7 +200,7 @@ __device__ __forceinline__ RowOut finish_row(const RowArgs& a, uint64_t row, con
     slope_lp = clipped ? 0.0f : -in.adv * ratio;
     if (a.ref_logprob) {
       const float u = in.ref_lp - lp, em1 = expm1f(u);
-      kl = em1 - u;
+      kl = u == -kMinusInf ? u : em1 - u;
       if (a.kl_coef != 0.0f) slope_lp -= a.kl_coef * em1;  // e^u may be infinite, and 0 of it is nothing
     }
     o.sums[0] = in.w * held * in.adv;

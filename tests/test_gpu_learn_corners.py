@@ -105,3 +105,14 @@ def test_reference_that_is_only_watched(rows, vocab, dtype):
         others = [0, 1, 3, 4, 5]
         assert torch.equal(got.stats[others], want.stats[others]) and torch.isfinite(want.stats).all()
         assert torch.equal(got.grad, want.grad) and torch.isfinite(want.grad).all()
+
+
+@pytest.mark.parametrize("rows,vocab", SHAPES)
+def test_kl_of_a_banned_token_is_infinite(rows, vocab):
+    """e^u - u - 1 with u = ref - lp = inf, alone and in the loss."""
+    x, y, old, ref, adv = with_far_reference(rows, vocab, "f32")
+    ref[1] -= 100.0
+    for kl_coef in (0.0, 0.1):
+        got = bf.policy_loss(x, y, cuts(rows, 2), old, adv, ref, kl_coef=kl_coef)
+        assert got.stats[2] == INF and (got.stats[0] == INF) == (kl_coef > 0.0)
+        assert torch.isfinite(got.grad[[0, 1, 3]]).all()
