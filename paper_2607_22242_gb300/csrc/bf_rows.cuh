@@ -253,7 +253,8 @@ __device__ __forceinline__ void finish_pair(const PairArgs& a, uint64_t p, const
   const float slope = (eps / (1.0f + expf(-h)) - (1.0f - eps) / (1.0f + expf(h))) * a.grad_scale / (float)a.pairs;
   a.seq_slope[2 * p] = slope * share[0];
   a.seq_slope[2 * p + 1] = -slope * share[1];
-  a.partial[p] = (1.0f - eps) * (fmaxf(-h, 0.0f) + tail) + eps * (fmaxf(h, 0.0f) + tail);
+  const float smooth = eps > 0.0f ? eps * (fmaxf(h, 0.0f) + tail) : 0.0f;  // the gap may be infinite: a banned token
+  a.partial[p] = (1.0f - eps) * (fmaxf(-h, 0.0f) + tail) + smooth;
 }
 
 // Sums of N values over the block's threads: the k-th in thread k.  Every thread of the block calls it with the same

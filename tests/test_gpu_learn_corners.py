@@ -116,3 +116,26 @@ def test_kl_of_a_banned_token_is_infinite(rows, vocab):
         got = bf.policy_loss(x, y, cuts(rows, 2), old, adv, ref, kl_coef=kl_coef)
         assert got.stats[2] == INF and (got.stats[0] == INF) == (kl_coef > 0.0)
         assert torch.isfinite(got.grad[[0, 1, 3]]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab", [s for s in SHAPES if s[0] >= 8])
+def test_pair_with_a_banned_token(rows, vocab, dtype):
+    """A gap of +inf costs nothing without smoothing, one of -inf everything; slopes are finite either way."""
+    _, x, y = draw(rows, vocab, dtype)
+    offsets = cuts(rows, 4)
+    for answer, loss, smoothed in ((1, 0.0, INF), (0, INF, INF)):
+        z, t = x.clone(), y.clamp(min=1)
+        at = rows * answer // 4
+        t[at] = 0
+        z[at, 0] = -INF
+        got = bf.preference_loss(z, t, offsets)
+        assert got.rewards[answer] == -INF and torch.isfinite(got.grad).all()
+        if loss == 0.0:  # the mean has the other pair's loss alone: some roundings of it, 2^-24 each
+            gap = (got.rewards[2] - got.rewards[3]).double()
+            assert got.stats[0].item() == pytest.approx(0.5 * torch.nn.functional.softplus(-gap).item(), rel=2.0 ** -19)
+            assert not got.grad[:rows // 2].any()
+        else:
+            assert got.stats[0] == INF and got.grad[:rows // 2].any()
+        got = bf.preference_loss(z, t, offsets, label_smoothing=0.1)
+        assert got.stats[0] == smoothed and torch.isfinite(got.grad).all()
