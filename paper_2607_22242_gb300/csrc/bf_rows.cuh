@@ -170,8 +170,9 @@ __device__ __forceinline__ RowOut finish_row(const RowArgs& a, uint64_t row, con
     const float2 kept = a.row_softmax[row];
     const float slope = in.known ? in.slope_lp * a.inv_tau : __int_as_float(0x7FC00000);
     o.m = kept.x;
+    if (kept.y == 0.0f && in.known) return o;  // no logit above -inf: 0 whatever the pair's slope
     o.b = -slope * kept.y;
-    o.hit = kept.y == 0.0f ? 0.0f : slope;
+    o.hit = slope;
     return o;
   }
   const bool none = r.s == 0.0f;

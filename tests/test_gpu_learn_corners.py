@@ -139,3 +139,19 @@ def test_pair_with_a_banned_token(rows, vocab, dtype):
             assert got.stats[0] == INF and got.grad[:rows // 2].any()
         got = bf.preference_loss(z, t, offsets, label_smoothing=0.1)
         assert got.stats[0] == smoothed and torch.isfinite(got.grad).all()
+
+
+# ---- rows whose mask leaves nothing ----
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab", [s for s in SHAPES if s[0] >= 8])
+def test_pair_with_masked_rows_in_both_answers(rows, vocab, dtype):
+    """The pair's gap has no value, but a row with no logit above -inf has a gradient of 0 all the same."""
+    _, x, y = draw(rows, vocab, dtype)
+    masked = [0, rows // 4]
+    x[masked] = -INF
+    got = bf.preference_loss(x, y, cuts(rows, 4))
+    assert got.rewards[:2].tolist() == [-INF, -INF] and not got.grad[masked].any()
+    y[masked] = -1
+    want = bf.preference_loss(x, y, cuts(rows, 4))
+    assert torch.equal(got.grad[rows // 2:], want.grad[rows // 2:]) and torch.isfinite(want.grad).all()
