@@ -248,6 +248,7 @@ int bf_policy_loss(const bf_matrix* logits, const bf_policy_args* args, float* d
 }
 
 int bf_preference_loss_workspace(uint64_t rows, uint64_t pairs, uint64_t* bytes) {
+  if (pairs > kMaxRows / 2) return fail(BF_EINVAL, "bf_preference_loss_workspace: more than 2^30 - 1 pairs");
   BF_TRY(check_counts(rows, 2 * pairs, bytes, "bf_preference_loss_workspace"));
   *bytes = Layout(nullptr, rows, 2 * pairs, true).bytes;
   return BF_OK;
