@@ -102,6 +102,8 @@ def train(scns: Sequence[Scenario], method: str = "policy", steps: int = 60, sam
     """Fit a policy; the mean over the workflows of (makespan of the policy's likeliest mapping / optimum), before the
     first step and after every one (a mapping beyond the budget counts as the all-cpu one)."""
     import torch
+    if samples < 2:
+        raise ValueError("samples must be at least 2: a workflow's samples are measured against each other")
     torch.manual_seed(seed)
     policy = Policy(scns, seed=seed)
     best = torch.tensor([r.makespan_us for r in bf.search_batch(list(scns))], device="cuda", dtype=torch.float64)
