@@ -9,7 +9,10 @@ the C entry points without their ``bf_`` prefix: ``validate_desc``,
 ``whatif``, ``search_pruned``, ``set_wait_timeout_ms``, ``last_error``,
 ``version``; and, for learning from the makespans of sampled mappings,
 ``token_logprobs``, ``token_logprobs_grad``, ``policy_loss``,
-``preference_loss``, ``embed`` and ``embed_grad``.
+``preference_loss``, ``embed`` and ``embed_grad``.  Those six are outside
+autograd: what they return has no graph, also where an argument requires a
+gradient.  A loss's ``grad`` is the gradient in the logits, to hand to torch
+(``logits.backward(loss.grad)``); an ``out`` is marked as written over.
 
 There is no CPU fallback: if ``libbf.so`` has not been built, or no CUDA
 device is present, these calls raise.
@@ -544,6 +547,14 @@ def _workspace(name: str, rows: int, groups: int, device):
     return torch.empty(_workspace_bytes(name, rows, groups), dtype=torch.uint8, device=device)
 
 
+def _written(t) -> None:
+    """Tell autograd that a call wrote over a caller's tensor, as torch's own in-place operations do: it then refuses a
+    backward pass that needs what the tensor held."""
+    import torch
+    if t is not None and not t.is_inference():
+        torch.autograd.graph.increment_version(t)
+
+
 def _grad_like(logits, out, grad: bool):
     """Where the gradient goes: nowhere, to `out` (it may be `logits`) or to a new tensor."""
     import torch
@@ -578,6 +589,7 @@ def token_logprobs_grad(logits, tokens, grad_logprob, grad_entropy=None, *, temp
     with _allocate(stream):
         grad = _grad_like(logits, out, True)
     _check(load().bf_token_logprobs_grad(x, y, temperature, gl, gh, _matrix(grad, "out"), _stream_of(stream, logits)))
+    _written(out)
     return grad
 
 
@@ -612,6 +624,7 @@ def policy_loss(logits, tokens, offsets, old_logprob, advantage, ref_logprob=Non
         work = _workspace("bf_policy_loss_workspace", rows, sequences, logits.device)
     _check(lib.bf_policy_loss(x, args, stats.data_ptr(), logprob.data_ptr(), None if g is None else _matrix(g, "out"),
                               work.data_ptr(), work.numel(), _stream_of(stream, logits)))
+    _written(out if grad else None)
     return PolicyLoss(stats, logprob, g)
 
 
@@ -640,6 +653,7 @@ def preference_loss(logits, tokens, offsets, ref_logprob=None, *, beta: float = 
     _check(lib.bf_preference_loss(x, args, stats.data_ptr(), rewards.data_ptr(), logprob.data_ptr(),
                                   None if g is None else _matrix(g, "out"), work.data_ptr(), work.numel(),
                                   _stream_of(stream, logits)))
+    _written(out if grad else None)
     return PreferenceLoss(stats, rewards, logprob, g)
 
 
@@ -648,6 +662,7 @@ def embed(table, tokens, *, scale: float = 1.0, out=None, stream=None):
     import torch
     w = _matrix(table, "table")
     y = _vector(tokens, tokens.numel(), torch.int64, table, "tokens")
+    given = out
     with _allocate(stream):
         if out is None:
             out = torch.empty(tokens.numel(), w.cols, dtype=table.dtype, device=table.device)
@@ -655,6 +670,7 @@ def embed(table, tokens, *, scale: float = 1.0, out=None, stream=None):
     if o.rows != tokens.numel():
         raise ValueError("out must have one row per token")
     _check(load().bf_embed(w, y, scale, o, _stream_of(stream, table)))
+    _written(given)
     return out
 
 
@@ -666,7 +682,7 @@ def embed_grad(grad_out, tokens, vocab: int, *, scale: float = 1.0, out=None, ac
     y = _vector(tokens, g.rows, torch.int64, grad_out, "tokens")
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
-    lib = load()
+    lib, given = load(), out
     with _allocate(stream):
         if out is None:
             out = torch.empty(vocab, g.cols, dtype=grad_out.dtype, device=grad_out.device)
@@ -675,4 +691,5 @@ def embed_grad(grad_out, tokens, vocab: int, *, scale: float = 1.0, out=None, ac
     if o.rows != vocab:
         raise ValueError("out must have one row per token of the vocabulary")
     _check(lib.bf_embed_grad(g, y, scale, accumulate, o, work.data_ptr(), work.numel(), _stream_of(stream, grad_out)))
+    _written(given)
     return out

@@ -155,3 +155,35 @@ def test_pair_with_masked_rows_in_both_answers(rows, vocab, dtype):
     y[masked] = -1
     want = bf.preference_loss(x, y, cuts(rows, 4))
     assert torch.equal(got.grad[rows // 2:], want.grad[rows // 2:]) and torch.isfinite(want.grad).all()
+
+
+# ---- autograd ----
+
+def test_autograd_sees_what_is_written():
+    """A tensor that autograd keeps and a call writes over is refused in the backward pass, as after torch's own in-place
+    operations, instead of giving a wrong gradient."""
+    y, f = torch.tensor([0, 1, 2, 3], device="cuda"), torch.zeros(4, device="cuda")
+    offsets, table = torch.tensor([0, 2, 4], device="cuda"), torch.randn(4, 8, device="cuda")
+    calls = [lambda t: bf.token_logprobs_grad(t, y, f + 1, out=t),
+             lambda t: bf.policy_loss(t, y, offsets, f, f[:2] + 1, out=t),
+             lambda t: bf.preference_loss(t, y, offsets, out=t),
+             lambda t: bf.embed(table, y, out=t),
+             lambda t: bf.embed_grad(table, y, 4, out=t),
+             lambda t: bf.embed_grad(table, y, 4, out=t, accumulate=True)]
+    for call in calls:
+        for over in (lambda t: t, lambda t: t.detach()):
+            leaf = torch.randn(4, 8, device="cuda", requires_grad=True)
+            kept = leaf.exp()  # its backward pass multiplies by what exp gave
+            call(over(kept))
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                kept.sum().backward()
+    # what is not written over stays usable, and tensors without a version are written as before
+    leaf = torch.randn(4, 8, device="cuda", requires_grad=True)
+    kept = leaf.exp()
+    bf.policy_loss(kept, y, offsets, f, f[:2] + 1)
+    kept.sum().backward()
+    assert torch.equal(leaf.grad, kept.detach())
+    with torch.inference_mode():
+        t = torch.randn(4, 8, device="cuda")
+        want = bf.token_logprobs_grad(t, y, f + 1)
+        assert torch.equal(bf.token_logprobs_grad(t, y, f + 1, out=t), want)
