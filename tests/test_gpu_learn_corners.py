@@ -187,3 +187,121 @@ def test_autograd_sees_what_is_written():
         t = torch.randn(4, 8, device="cuda")
         want = bf.token_logprobs_grad(t, y, f + 1)
         assert torch.equal(bf.token_logprobs_grad(t, y, f + 1, out=t), want)
+
+
+# ---- sums of many blocks ----
+
+@pytest.mark.parametrize("rows,vocab,dtype,reduction", [(1000003, 3, "f32", "tokens"), (1000003, 7, "bf16", "sequences"),
+                                                        (200001, 512, "bf16", "sum"), (820001, 4, "f16", "sum")])
+def test_policy_of_many_blocks(rows, vocab, dtype, reduction):
+    """More blocks than sum up in one launch.  A term is made of a log-probability given to 32 bits: its ratio is off by
+    2^-22 of itself (a difference's rounding and expf's), its KL term by as much of e^u + |u| + 1, and is weighed and added
+    in fewer than 40 roundings of 2^-24: 3e-6 of the sum of magnitudes, far below what one warp's part weighs (4 rows:
+    2e-5).  An entropy is within 1e-5."""
+    gen, x, y = draw(rows, vocab, dtype)
+    y[torch.rand(rows, generator=gen, device="cuda") < 0.1] = -1
+    sequences = rows // 13
+    offsets = torch.sort(torch.randint(rows + 1, (sequences + 1,), generator=gen, device="cuda")).values
+    seq = torch.searchsorted(offsets, torch.arange(rows, device="cuda"), right=True) - 1
+    on = (y >= 0) & (seq >= 0) & (seq < sequences)
+    at = seq.clamp(0, sequences - 1)
+    parts = [torch.log_softmax(x[a:a + 50000].double(), 1) for a in range(0, rows, 50000)]
+    lp = torch.cat([z.gather(1, y[50000 * k:50000 * k + 50000].clamp(min=0)[:, None])[:, 0] for k, z in enumerate(parts)])
+    h = torch.cat([-(z.exp() * z).sum(1) for z in parts])
+    del parts
+    d = 0.25 * torch.randn(rows, generator=gen, device="cuda").double()
+    for edge in (0.8, 1.2):  # no ratio within 1e-3 of a clip edge
+        d = torch.where((d.exp() - edge).abs() < 1e-3, d + 4e-3, d)
+    old, ref = (lp - d).float(), (lp + 0.4 * torch.randn(rows, generator=gen, device="cuda")).float()
+    adv = torch.randn(sequences, generator=gen, device="cuda")
+    kw = dict(kl_coef=0.05, entropy_coef=0.01, reduction=reduction)
+    got = bf.policy_loss(x, y, offsets, old, adv, ref, **kw)
+    assert torch.all((got.logprob.double() - torch.where(on, lp, 0.0)).abs() <= 1e-5 + 1e-6 * lp.abs())
+    lp = got.logprob.double()
+    n = torch.bincount(at[on], minlength=sequences).double()
+    w = {"tokens": 1.0 / n.sum(), "sequences": 1.0 / (n[at].clamp(min=1) * (n > 0).sum()), "sum": 1.0}[reduction]
+    w = torch.where(on, w, 0.0)
+    A, r = adv.double()[at], torch.exp(torch.where(on, lp - old.double(), 0.0))
+    low, high = 1.0 - float(torch.tensor(0.2)), 1.0 + float(torch.tensor(0.2))
+    stopped = ((A >= 0) & (r > high)) | ((A < 0) & (r < low))
+    held = torch.where(stopped, torch.where(A >= 0, high, low), r)
+    u = torch.where(on, ref.double() - lp, 0.0)
+    k = torch.expm1(u) - u
+    terms = {1: -held * A, 2: k, 4: stopped.double(), 5: r}
+    size = {1: (held * A).abs(), 2: u.exp() + u.abs() + 1, 4: stopped.double(), 5: r}
+    for i, v in terms.items():
+        assert abs(got.stats[i].item() - (w * v).sum().item()) <= 3e-6 * (w * size[i]).sum().item(), i
+    assert abs(got.stats[3].item() - (w * h).sum().item()) <= 1e-5 * w.sum().item() + 3e-6 * (w * h).sum().item()
+    s = got.stats.double()
+    made = s[1] + 0.05 * s[2] - 0.01 * s[3]
+    assert abs(s[0] - made) <= 2.0 ** -21 * (s[1].abs() + 0.05 * s[2] + 0.01 * s[3])
+    a = w * (torch.where(stopped, 0.0, -A * r) - 0.05 * torch.expm1(u))
+    part = w * (torch.where(stopped, 0.0, (A * r).abs()) + 0.05 * (u.exp() + 1))
+    for f in range(0, rows, 50000):
+        z, t = torch.log_softmax(x[f:f + 50000].double(), 1), slice(f, f + 50000)
+        p = z.exp()
+        hit = torch.zeros_like(p).scatter_(1, y[t].clamp(min=0)[:, None], 1.0)
+        tilt = p * (z + h[t][:, None])
+        want = a[t][:, None] * (hit - p) + 0.01 * w[t][:, None] * tilt
+        far = part[t][:, None] * (hit + p) + 0.01 * w[t][:, None] * (tilt.abs() + p)
+        least = 2.0 ** -24 if dtype == "f16" else 1e-37
+        assert torch.all((got.grad[t].double() - want).abs() <= 5e-5 * far + ROUND[dtype] * want.abs() + least)
+    # the same bits again; without the gradient; in place
+    again = bf.policy_loss(x, y, offsets, old, adv, ref, **kw)
+    assert all(torch.equal(i, j) for i, j in zip(got, again))
+    assert torch.equal(bf.policy_loss(x, y, offsets, old, adv, ref, grad=False, **kw).stats, got.stats)
+    same = bf.policy_loss(x, y, offsets, old, adv, ref, out=x, **kw)
+    assert torch.equal(x, got.grad) and torch.equal(same.stats, got.stats)
+
+
+@pytest.mark.parametrize("reduction", bf.REDUCTIONS)
+@pytest.mark.parametrize("answers,longest,empty", [(40, 900, 3000), (200, 12, 5000), (2000, 40, 30), (3, 40000, 1025)])
+def test_many_empty_sequences(answers, longest, empty, reduction):
+    """Thousands of empty sequences between others change nothing for those: more than a block's rows have offsets."""
+    gen = torch.Generator(device="cuda").manual_seed(answers)
+    lengths = torch.randint(1, longest + 1, (answers,), generator=gen, device="cuda")
+    wide = torch.zeros(answers, empty + 1, dtype=torch.int64, device="cuda")
+    wide[:, empty // 2] = lengths
+    close = torch.nn.functional.pad(lengths.cumsum(0), (1, 0)) + 1
+    far = torch.nn.functional.pad(wide.flatten().cumsum(0), (1, 0)) + 1
+    rows = int(close[-1]) + 2
+    x = torch.randn(rows, 5, generator=gen, device="cuda")
+    y = torch.randint(-1, 5, (rows,), generator=gen, device="cuda")
+    old = torch.full((rows,), -1.6, device="cuda")
+    adv = torch.randn(answers, generator=gen, device="cuda")
+    spread = torch.zeros_like(wide, dtype=torch.float32)
+    spread[:, empty // 2] = adv
+    got = bf.policy_loss(x, y, far, old, spread.flatten(), reduction=reduction)
+    want = bf.policy_loss(x, y, close, old, adv, reduction=reduction)
+    on = (y >= 0) & (torch.arange(rows, device="cuda") >= 1) & (torch.arange(rows, device="cuda") < rows - 2)
+    assert torch.equal(want.logprob != 0, on)
+    assert torch.equal(got.logprob, want.logprob) and torch.equal(got.grad, want.grad)
+    # 32-bit sums of weighed terms whose blocks may differ: under 40 roundings of 2^-24 on either side
+    size = torch.tensor([max(1.0, adv.abs().max().item()) * 8] * 6, device="cuda") * (on.sum() if reduction == "sum" else 1)
+    assert torch.all((got.stats - want.stats).abs() <= 80 * 2.0 ** -24 * size)
+
+
+def test_many_empty_pairs():
+    """Pairs without rows between others: rewards by the rows that are there, a loss of ln 2 for the empty ones."""
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    pairs, empty = 30, 1500
+    lengths = torch.randint(300, 900, (pairs, 2), generator=gen, device="cuda")
+    wide = torch.zeros(pairs, empty + 1, 2, dtype=torch.int64, device="cuda")
+    wide[:, empty // 3] = lengths
+    offsets = torch.nn.functional.pad(wide.flatten().cumsum(0), (1, 0))
+    rows = int(offsets[-1])
+    x = torch.randn(rows, 5, generator=gen, device="cuda")
+    y = torch.randint(-1, 5, (rows,), generator=gen, device="cuda")
+    got = bf.preference_loss(x, y, offsets, average=True, beta=1.0)
+    seq = torch.arange(2 * pairs, device="cuda").repeat_interleave(lengths.flatten())
+    on = y >= 0
+    sums = torch.zeros(2 * pairs, dtype=torch.float64, device="cuda").index_add_(0, seq[on], got.logprob.double()[on])
+    want = sums / torch.bincount(seq[on], minlength=2 * pairs)
+    rewards = got.rewards.view(pairs, empty + 1, 2)
+    # at most 900 terms of one sign by 32 threads, then over those, divided and multiplied: under 40 roundings of 2^-24
+    assert torch.all((rewards[:, empty // 3].flatten().double() / want - 1).abs() <= 40 * 2.0 ** -24)
+    rest = torch.cat([rewards[:, :empty // 3], rewards[:, empty // 3 + 1:]], 1)
+    assert not rest.any()
+    gap = want.view(pairs, 2)
+    loss = (torch.nn.functional.softplus(gap[:, 1] - gap[:, 0]).sum() + pairs * empty * 0.6931471805599453) / (pairs * (empty + 1))
+    assert got.stats[0].item() == pytest.approx(loss.item(), rel=1.5e-5)  # 90 terms a thread, then over 512: 110 roundings and the gaps' own
