@@ -73,7 +73,7 @@ struct PairArgs {
   uint32_t average;
   float* seq_slope;  // 2 * pairs
   float* rewards;    // 2 * pairs
-  float* partial;    // 2 rows of `pairs` sums: loss, correct
+  float* partial;    // the loss of each pair
   float* stats;
 };
 

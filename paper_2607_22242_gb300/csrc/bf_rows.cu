@@ -75,9 +75,11 @@ __device__ __forceinline__ void policy_stats(const RowArgs& a, uint64_t parts, f
 
 // (x - m) (hi + lo) as (x - base) hi - r + (x - base) lo: with base = 0 and r =
 // m hi rounded it is two products and sums, the small part last, and what r is
-// off by (`rest`) goes into the factors once per row, as 1 + rest ln2: below 1e-9
-// off where m hi is below 1,024.  Rows of larger logits (or all masked by the
-// type's lowest value, where m hi leaves the 32-bit range) take base = m, r = 0.
+// off by (`rest`) goes into the factors once per row, as 1 + rest ln2.  With m hi
+// below 1,024 rest is at most 1.5e-4 (m lo, and half a last place of r), so that is
+// below 6e-9 off, always short; 1e-12 where m hi is around 10.  Rows of larger logits
+// (or all masked by the type's lowest value, where m hi leaves the 32-bit range) take
+// base = m, r = 0.
 //
 // Without `exact` the small part is left out, for gradients of 16 bits: 1e-6 of
 // a probability of e^-14.
@@ -343,9 +345,12 @@ __device__ __forceinline__ void cluster_store(float* p, uint32_t rank, float v) 
 
 // `cluster` blocks per row, each with `tiles` tiles of kWideVectors vectors a
 // thread; the last tile stays in registers between the row's sums and its
-// gradient, the others are read again from L2 (608 or fewer rows are on their way,
-// 78 MB of the longest).  Bound by memory: 8,192 rows of 131,072 bf16, policy loss
-// 0.617 ms, 6.1 of 6.67 TB/s measured; 2,048 rows of 32,768 f32, gradient with
+// gradient, the others are read again, from L2 as far as the rows on their way fit
+// it: two blocks an SM, so 304 rows, 80 MB of 131,072 bf16 (93 % of the second reads
+// hit), but 159 MB of 131,072 f32 (44 %: a policy loss of 1,024 rows reads 799 MB from
+// memory for 537 MB of logits) and 319 MB of 262,144 f32 (26 %, 910 MB).
+// Bound by memory: 8,192 rows of 131,072 bf16, policy loss
+// 0.611 ms, 6.2 of 6.67 TB/s measured; 2,048 rows of 32,768 f32, gradient with
 // entropies 87 us, 5.9 TB/s; 4,096 rows of 50,001 f16, scores with entropies 60 us,
 // 5.4 TB/s (rows at any alignment).
 template <RowOp op, bool entropy>
@@ -575,7 +580,8 @@ uint32_t div_up(uint32_t a, uint32_t b) { return (a + b - 1) / b; }
 // (4,096 rows of 50,001 f16: 128 / 256 / 512 threads 62 / 66 / 80 us).  A gradient
 // reads its row again from L2, so fewer rows at a time: two tiles a thread, up to 512
 // threads (2,048 rows of 32,768 f32: 128 / 256 / 512 threads 112 / 96 / 90 us; 8,192 rows
-// of 131,072 bf16 920 / 803 / 738 us).
+// of 131,072 bf16 920 / 803 / 738 us).  The rule goes by the operation: a policy loss
+// without its gradient keeps the gradient's shape (those rows 427 us, their scores 315 us).
 WideShape wide_shape(uint64_t rows, uint32_t vectors, bool scores) {
   WideShape s = {1, 0, 1};
   while (s.cluster < kMaxCluster && rows * s.cluster <= 400 && div_up(vectors, s.cluster) > 256) s.cluster *= 2;
@@ -613,7 +619,9 @@ cudaError_t launch_op(const RowArgs& a, cudaStream_t st) {
   // 50 with 4; 400,000 of 64 (8 vectors) 56 us with 2 lanes of 4, 66 with 1 of 8;
   // 200,000 of 512 (64 vectors) 119 us with 8 lanes of 8, 169 with 16 of 4, 283 with
   // 32 of 2; policy losses.  Up to 4 KB a row: 131,072 rows of 1,024 bf16 123 us here,
-  // 195 with a block a row; 65,536 of 2,048 105 against 111.
+  // 195 with a block a row; 65,536 of 2,048 105 against 111.  Their bytes alone take 9, 17,
+  // 62, 81 and 81 us: the shorter the rows, the more the loss's arithmetic and values of
+  // each row weigh.
   if (a.vocab <= 4) return group(short_kernel<op, 4>, 1);
   if (vectors <= 2) return group(warp_kernel<op, entropy, 2>, 1);
   if (vectors <= 8) return group(warp_kernel<op, entropy, 4>, pow2_up(div_up(vectors, 4)));

@@ -44,7 +44,8 @@ struct Scale {
 // above, so ln s is put right by the share of s that is short, and sums are joined
 // by expf.  With 4.0e-8 log-probabilities of normal logits are off by 5e-9 on
 // average at 3 to 10,000 of them, 1.2e-8 at 100,000 (torch's in 32 bits: 3e-9 at 3,
-// 1.2e-8 at 1,000, 1.8e-8 at 100,000); with 5.0e-8 by 7e-9 and 2.0e-8.
+// 1.2e-8 at 1,000, 1.8e-8 at 100,000); with 5.0e-8 by 7e-9 and 2.0e-8.  Logits of
+// another distribution, whose exponents fill their octaves otherwise, have another mean.
 constexpr float kExp2Short = 4.0e-8f;
 
 // ln v + more = big + low for a v that is 0 (any value then), NaN or normal.  `more` is below half a last place of v and
