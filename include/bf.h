@@ -450,6 +450,114 @@ BF_API int bf_embed_grad(const bf_matrix* grad_out, const int64_t* d_tokens, flo
                          const bf_matrix* grad_table, void* d_workspace, uint64_t workspace_bytes, void* cuda_stream);
 BF_API int bf_embed_grad_workspace(uint64_t rows, uint64_t width, uint64_t* bytes);
 
+/* ---- Answering --------------------------------------------------------------
+ *
+ * A decoding step of a scheduling model that answers a workflow's prompt with
+ * many candidate mappings: beams, or samples that are graded against each
+ * other.  The paper's scheduler (§3.3) answers once and by a prompted model;
+ * these entry points are this library's addition, beside the learning ones and
+ * under the same conventions: asynchronous on `cuda_stream`, no allocation, can be
+ * captured, a workspace (aligned to 256 bytes) that holds nothing between
+ * calls and serves one call at a time, values in 32 bits or more, the same
+ * bits for the same call.
+ */
+
+/* Vectors of many sequences in device memory: element (b, t, h, d) is
+ * data[b * batch_stride + t * token_stride + h * head_stride + d] (strides in
+ * elements), at any address its type allows.  At most 2^31 - 1 sequences and
+ * tokens, 65,536 heads, 256 dimensions, 2^42 elements from first to last. */
+typedef struct bf_cache {
+  void* data;
+  uint64_t batch, tokens, heads, dim;
+  uint64_t batch_stride, token_stride, head_stride;
+  uint32_t dtype;  /* bf_dtype */
+  uint32_t pad;
+} bf_cache;
+
+typedef struct bf_attention_args {
+  const int64_t* prefix_lengths;  /* device, one per prompt; NULL: prefix_k->tokens each */
+  const int64_t* suffix_lengths;  /* device, one per answer; NULL: suffix_k->tokens each */
+  float scale;                    /* of the scores, 1 / sqrt(dim) as a rule; finite */
+  uint32_t pad;
+} bf_attention_args;
+
+/* Attention of one token of each answer to its prompt, whose keys the answers
+ * share and which is read once for all of them, and to the answer's own keys.
+ * With `prompts` = prefix_k->batch prompts and w = q->batch / prompts answers to
+ * each, answer a belongs to prompt a / w; query head h reads key head
+ * h / (q->heads / prefix_k->heads).  Over the prompt's first
+ * prefix_lengths[a / w] tokens and the answer's first suffix_lengths[a]:
+ *   s_t = scale q . k_t, out = sum e^(s_t) v_t / sum e^(s_t), lse = ln sum e^(s_t).
+ * q and out have one token per answer; all types are the same.  suffix_k and
+ * suffix_v may both be NULL (the prompt alone); d_lse (answers x heads) may be
+ * NULL.  What lies behind a length is not used, whatever it holds.  With nothing
+ * to attend to (lengths 0, or every score -inf) out is 0 and lse -inf; a length
+ * outside 0..tokens makes its answers' out and lse NaN.  For 16-bit types the
+ * weights e^(s_t - max) are rounded to the type before the second product.  out
+ * overlaps no input. */
+BF_API int bf_prefix_attention(const bf_cache* q, const bf_cache* prefix_k, const bf_cache* prefix_v,
+                               const bf_cache* suffix_k, const bf_cache* suffix_v, const bf_attention_args* args,
+                               const bf_cache* out, float* d_lse, void* d_workspace, uint64_t workspace_bytes,
+                               void* cuda_stream);
+BF_API int bf_prefix_attention_workspace(const bf_cache* q, const bf_cache* prefix_k, const bf_cache* suffix_k,
+                                         uint64_t* bytes);
+
+#define BF_MAX_BEAMS 256
+
+typedef struct bf_beam_args {
+  const float* scores;      /* device, one per beam: log-probability so far; -inf for a beam that is not alive */
+  const uint8_t* finished;  /* device, one per beam, 0 or 1; NULL: none is */
+  const int64_t* lengths;   /* device, one per beam: tokens so far; NULL without a length penalty */
+  uint64_t groups;          /* prompts; the logits have groups * beams rows */
+  uint32_t beams;           /* per group, 1 to BF_MAX_BEAMS */
+  uint32_t keep;            /* continuations kept per group, 1 to BF_MAX_BEAMS */
+  int64_t end_token;        /* the token that finishes a beam; -1: none */
+  float length_penalty;     /* >= 0 */
+  float temperature;        /* 1e-18 to 1e18 */
+} bf_beam_args;
+
+/* The best continuations of each group's beams.  A beam that is alive continues
+ * with every token v of its row of logits, at the total score + ln softmax(logits
+ * / temperature)_v; one that is finished stays as it is, as the one continuation
+ * end_token at its own score (its logits are not used).  A continuation of n
+ * tokens has rank total / max(1, n)^length_penalty.  The `keep` of highest rank
+ * of each group, ties to the lower beam, then the lower token, are written in
+ * that order: d_scores (the total), d_tokens, d_parents (the row of the beam
+ * continued), d_finished (may be NULL: 1 where the beam was finished or the
+ * token is end_token) and d_lengths (may be NULL: n), groups * keep of each.
+ * Tokens of logit -inf are no continuations.  Where a group has fewer than
+ * `keep`, the rest has score -inf, token -1, finished 0, length 0 and as parent j
+ * the group's beam j modulo beams.  A logit of NaN or +inf, a score of NaN or
+ * +inf makes its group's scores NaN and the rest as if nothing could continue
+ * (a finished beam's logits do not matter).  At most 2^23 - 1 groups and a
+ * vocabulary of 2^24. */
+BF_API int bf_beam_step(const bf_matrix* logits, const bf_beam_args* args, float* d_scores, int64_t* d_tokens,
+                        int64_t* d_parents, uint8_t* d_finished, int64_t* d_lengths, void* d_workspace,
+                        uint64_t workspace_bytes, void* cuda_stream);
+BF_API int bf_beam_step_workspace(uint64_t groups, uint32_t beams, uint64_t vocab, uint32_t keep, uint64_t* bytes);
+
+/* The states of beams: `count` arrays of the same layout, `rows` rows of up to
+ * `tokens` tokens of `heads` runs of `width` bytes. */
+typedef struct bf_states {
+  uint64_t rows, tokens, heads, width;
+  uint64_t row_stride, token_stride, head_stride;  /* in bytes */
+} bf_states;
+
+#define BF_MAX_STATES 128
+
+/* Row i of each array takes row d_parents[i]'s first d_lengths[d_parents[i]]
+ * tokens (all of them where d_lengths is NULL); what is behind them in row i
+ * stays as it was.  Groups are runs of `beams` rows, and a parent is in its
+ * row's group: a row whose parent is not stays as it was, and so does one whose
+ * parent's length is negative; a length above `tokens` counts as `tokens`.
+ * `from` and `to` are host arrays of `count` (at most BF_MAX_STATES) device
+ * addresses; to[k] == from[k] with the same layout reorders in place (rows that
+ * are their own parent cost nothing), otherwise no array overlaps another.  d_lengths is not
+ * reordered. */
+BF_API int bf_beam_reorder(void* const* from, const bf_states* from_layout, void* const* to,
+                           const bf_states* to_layout, uint32_t count, const int64_t* d_parents, uint32_t beams,
+                           const int64_t* d_lengths, void* cuda_stream);
+
 /* Time limit of blocking waits, in milliseconds (default 600000; 0 = none).
  * Process-wide. */
 BF_API void bf_set_wait_timeout_ms(uint32_t ms);

@@ -9,8 +9,9 @@ the C entry points without their ``bf_`` prefix: ``validate_desc``,
 ``whatif``, ``search_pruned``, ``set_wait_timeout_ms``, ``last_error``,
 ``version``; and, for learning from the makespans of sampled mappings,
 ``token_logprobs``, ``token_logprobs_grad``, ``policy_loss``,
-``preference_loss``, ``embed`` and ``embed_grad``.  Those six are outside
-autograd: what they return has no graph, also where an argument requires a
+``preference_loss``, ``embed`` and ``embed_grad``; and, for a decoding step of
+the model that samples them, ``prefix_attention``, ``beam_step`` and
+``beam_reorder``.  Those nine are outside autograd: what they return has no graph, also where an argument requires a
 gradient.  A loss's ``grad`` is the gradient in the logits, to hand to torch
 (``logits.backward(loss.grad)``); an ``out`` is marked as written over.
 
@@ -39,7 +40,8 @@ EXPORTED = ("bf_validate_desc", "bf_create_scenario", "bf_destroy_scenario", "bf
             "bf_eval_indices", "bf_whatif", "bf_search_pruned", "bf_search_tree", "bf_token_logprobs",
             "bf_token_logprobs_grad", "bf_policy_loss", "bf_policy_loss_workspace", "bf_preference_loss",
             "bf_preference_loss_workspace", "bf_embed", "bf_embed_grad", "bf_embed_grad_workspace",
-            "bf_set_wait_timeout_ms", "bf_last_error", "bf_version")
+            "bf_prefix_attention", "bf_prefix_attention_workspace", "bf_beam_step", "bf_beam_step_workspace",
+            "bf_beam_reorder", "bf_set_wait_timeout_ms", "bf_last_error", "bf_version")
 SPACE_BINARY, SPACE_FULL = 2, 3
 TREE_NO_PRUNE = 1
 MAX_PROBES = 2 * MAX_TOOLS + MAX_TOOLS * MAX_TOOLS
@@ -119,6 +121,34 @@ class PreferenceArgs(ctypes.Structure):
                 ("grad_scale", ctypes.c_float)]
 
 
+class Cache(ctypes.Structure):
+    """``bf_cache``."""
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_uint64), ("tokens", ctypes.c_uint64),
+                ("heads", ctypes.c_uint64), ("dim", ctypes.c_uint64), ("batch_stride", ctypes.c_uint64),
+                ("token_stride", ctypes.c_uint64), ("head_stride", ctypes.c_uint64), ("dtype", ctypes.c_uint32),
+                ("pad", ctypes.c_uint32)]
+
+
+class AttentionArgs(ctypes.Structure):
+    """``bf_attention_args``."""
+    _fields_ = [("prefix_lengths", ctypes.c_void_p), ("suffix_lengths", ctypes.c_void_p), ("scale", ctypes.c_float),
+                ("pad", ctypes.c_uint32)]
+
+
+class BeamArgs(ctypes.Structure):
+    """``bf_beam_args``."""
+    _fields_ = [("scores", ctypes.c_void_p), ("finished", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+                ("groups", ctypes.c_uint64), ("beams", ctypes.c_uint32), ("keep", ctypes.c_uint32),
+                ("end_token", ctypes.c_int64), ("length_penalty", ctypes.c_float), ("temperature", ctypes.c_float)]
+
+
+class States(ctypes.Structure):
+    """``bf_states``."""
+    _fields_ = [("rows", ctypes.c_uint64), ("tokens", ctypes.c_uint64), ("heads", ctypes.c_uint64),
+                ("width", ctypes.c_uint64), ("row_stride", ctypes.c_uint64), ("token_stride", ctypes.c_uint64),
+                ("head_stride", ctypes.c_uint64)]
+
+
 @dataclasses.dataclass
 class Result:
     index: int
@@ -158,6 +188,13 @@ def load(path: str = LIB_PATH):
     lib.bf_preference_loss.argtypes = [mat, ctypes.POINTER(PreferenceArgs), vp, vp, vp, mat, vp, u64, vp]
     lib.bf_embed.argtypes = [mat, vp, f32, mat, vp]
     lib.bf_embed_grad.argtypes = [mat, vp, f32, u32, mat, vp, u64, vp]
+    cache, states, table = ctypes.POINTER(Cache), ctypes.POINTER(States), ctypes.POINTER(vp)
+    lib.bf_prefix_attention.argtypes = [cache, cache, cache, cache, cache, ctypes.POINTER(AttentionArgs), cache, vp, vp, u64,
+                                        vp]
+    lib.bf_prefix_attention_workspace.argtypes = [cache, cache, cache, ctypes.POINTER(u64)]
+    lib.bf_beam_step.argtypes = [mat, ctypes.POINTER(BeamArgs), vp, vp, vp, vp, vp, vp, u64, vp]
+    lib.bf_beam_step_workspace.argtypes = [u64, u32, u64, u32, ctypes.POINTER(u64)]
+    lib.bf_beam_reorder.argtypes = [table, states, table, states, u32, vp, u32, vp, vp]
     for name in ("bf_policy_loss_workspace", "bf_preference_loss_workspace", "bf_embed_grad_workspace"):
         getattr(lib, name).argtypes = [u64, u64, ctypes.POINTER(u64)]
     for name in EXPORTED:
@@ -693,3 +730,175 @@ def embed_grad(grad_out, tokens, vocab: int, *, scale: float = 1.0, out=None, ac
     _check(lib.bf_embed_grad(g, y, scale, accumulate, o, work.data_ptr(), work.numel(), _stream_of(stream, grad_out)))
     _written(given)
     return out
+
+
+# ---- answering ------------------------------------------------------------------------------------------------------
+
+MAX_BEAMS, MAX_STATES = 256, 128
+
+
+class BeamStep(NamedTuple):
+    """The continuations kept, the best first (each groups x keep): ``scores`` (float32), ``tokens`` and ``parents``
+    (int64; a parent is a row of the logits), ``finished`` (bool) and, where lengths were given, ``lengths`` (int64)."""
+    scores: object
+    tokens: object
+    parents: object
+    finished: object
+    lengths: object
+
+
+def _cache(t, name: str, like=None) -> Cache:
+    """A CUDA tensor (batch x tokens x heads x dim, or batch x heads x dim) on the current device as ``bf_cache``."""
+    import torch
+    code, n = _dtype_code(t.dtype), t.dim()
+    if code is None or not t.is_cuda or n != (3 if like is None else 4):
+        raise ValueError(f"{name} must be a {3 if like is None else 4}-D CUDA tensor of float32, bfloat16 or float16")
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} is on device {t.get_device()} but device {torch.cuda.current_device()} is current")
+    shape, stride = t.shape, t.stride()
+    if stride[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{name} must have contiguous vectors")
+    if n == 3:
+        return Cache(t.data_ptr(), shape[0], 1, shape[1], shape[2], stride[0], 0, stride[1], code, 0)
+    return Cache(t.data_ptr(), *shape, *stride[:3], code, 0)
+
+
+@functools.lru_cache(maxsize=256)
+def _attention_bytes(answers: int, heads: int, dim: int, prompts: int, prefix: int, kv_heads: int, suffix: int,
+                     code: int) -> int:
+    need = ctypes.c_uint64(0)
+    make = lambda batch, tokens, h: Cache(256, batch, tokens, h, dim, 0, 0, 0, code, 0)
+    own = None if suffix < 0 else make(answers, suffix, kv_heads)
+    _check(load().bf_prefix_attention_workspace(make(answers, 1, heads), make(prompts, prefix, kv_heads), own,
+                                                ctypes.byref(need)))
+    return need.value
+
+
+def prefix_attention(q, prefix_k, prefix_v, suffix_k=None, suffix_v=None, *, prefix_lengths=None, suffix_lengths=None,
+                     scale: Optional[float] = None, lse: bool = False, out=None, stream=None):
+    """Attention of one token of each answer, `q` (answers x heads x dim), to its prompt's keys and values, `prefix_k`
+    and `prefix_v` (prompts x tokens x key heads x dim; the answers of a prompt follow one another and share it), and to
+    its own, `suffix_k` and `suffix_v` (answers x tokens x key heads x dim, or None).  Lengths (int64, one per prompt and
+    per answer) say how many tokens hold something, all of them by default.  ``scale``: 1 / sqrt(dim) by default.
+    Returns the outputs, of q's shape and type -- with ``lse``, the pair of them and the float32 logarithms of the sums
+    of exponentials (answers x heads), by which a caller joins them with attention to other keys."""
+    import torch
+    x, pk, pv = _cache(q, "q"), _cache(prefix_k, "prefix_k", q), _cache(prefix_v, "prefix_v", q)
+    sk = None if suffix_k is None else _cache(suffix_k, "suffix_k", q)
+    sv = None if suffix_v is None else _cache(suffix_v, "suffix_v", q)
+    i64 = torch.int64
+    pl = None if prefix_lengths is None else _vector(prefix_lengths, pk.batch, i64, q, "prefix_lengths")
+    sl = None if suffix_lengths is None else _vector(suffix_lengths, x.batch, i64, q, "suffix_lengths")
+    if sl is not None and sk is None:
+        raise ValueError("suffix_lengths needs suffix_k")
+    need = _attention_bytes(x.batch, x.heads, x.dim, pk.batch, pk.tokens, pk.heads, -1 if sk is None else sk.tokens, x.dtype)
+    given = out
+    with _allocate(stream):
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        sums = torch.empty(x.batch, x.heads, dtype=torch.float32, device=q.device) if lse else None
+        work = torch.empty(need, dtype=torch.uint8, device=q.device)
+    args = AttentionArgs(pl, sl, x.dim ** -0.5 if scale is None else scale, 0)
+    _check(load().bf_prefix_attention(x, pk, pv, sk, sv, args, _cache(out, "out"), sums.data_ptr() if lse else None,
+                                      work.data_ptr(), need, _stream_of(stream, q)))
+    _written(given)
+    return (out, sums) if lse else out
+
+
+@functools.lru_cache(maxsize=256)
+def _beam_bytes(groups: int, beams: int, vocab: int, keep: int) -> int:
+    need = ctypes.c_uint64(0)
+    _check(load().bf_beam_step_workspace(groups, beams, vocab, keep, ctypes.byref(need)))
+    return need.value
+
+
+def beam_step(logits, scores, beams: int, *, keep: Optional[int] = None, finished=None, lengths=None,
+              length_penalty: float = 0.0, end_token: int = -1, temperature: float = 1.0, stream=None) -> BeamStep:
+    """The best `keep` (by default `beams`) continuations of every group of `beams` rows of `logits` (rows x vocab),
+    by the beams' `scores` (float32, one per row; -inf: not alive) plus the tokens' log-probabilities.  A beam that is
+    `finished` (bool, one per row) stays, with `end_token`.  With ``length_penalty`` continuations are ranked by score /
+    length ** length_penalty, from the beams' `lengths` (int64, one per row).  Places without a continuation have score
+    -inf and token -1."""
+    import torch
+    x = _matrix(logits, "logits")
+    if not 1 <= beams <= MAX_BEAMS or x.rows % beams:
+        raise ValueError(f"beams must be 1 to {MAX_BEAMS} and a divisor of the rows")
+    keep = beams if keep is None else keep
+    groups = x.rows // beams
+    args = BeamArgs(_vector(scores, x.rows, torch.float32, logits, "scores"),
+                    None if finished is None else _vector(finished, x.rows, torch.bool, logits, "finished"),
+                    None if lengths is None else _vector(lengths, x.rows, torch.int64, logits, "lengths"),
+                    groups, beams, keep, end_token, length_penalty, temperature)
+    need = _beam_bytes(groups, beams, x.cols, keep)
+    device, i64 = logits.device, torch.int64
+    with _allocate(stream):
+        best = torch.empty(groups, keep, dtype=torch.float32, device=device)
+        whole = torch.empty(2 if lengths is None else 3, groups, keep, dtype=i64, device=device)
+        ended = torch.empty(groups, keep, dtype=torch.bool, device=device)
+        work = torch.empty(need, dtype=torch.uint8, device=device)
+    at, step = whole.data_ptr(), 8 * groups * keep
+    _check(load().bf_beam_step(x, args, best.data_ptr(), at, at + step, ended.data_ptr(),
+                               None if lengths is None else at + 2 * step, work.data_ptr(), need,
+                               _stream_of(stream, logits)))
+    return BeamStep(best, whole[0], whole[1], ended, None if lengths is None else whole[2])
+
+
+def _addresses(tensors, name: str):
+    """The addresses of tensors of one layout (rows x tokens x ...) on the current device."""
+    import torch
+    first = tensors[0]
+    shape, stride, dtype, current = first.shape, first.stride(), first.dtype, torch._C._cuda_getDevice()
+    if len(shape) < 2:
+        raise ValueError(f"{name} must have rows and tokens")
+    for t in tensors:
+        if t.shape != shape or t.stride() != stride or t.dtype != dtype or not t.is_cuda:
+            raise ValueError(f"{name} must be CUDA tensors of one shape, layout and type")
+        if t.get_device() != current:
+            raise ValueError(f"{name} is on device {t.get_device()} but device {current} is current")
+    return (ctypes.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors])
+
+
+def _layouts(source, target):
+    """``bf_states`` of two tensors of one shape: what follows a token is runs that are contiguous in both, and at most
+    one dimension that is apart."""
+    shape, size = source.shape, source.element_size()
+    strides = source.stride(), target.stride()
+    dims = [(n, s, t) for n, s, t in zip(shape[2:], strides[0][2:], strides[1][2:]) if n != 1]
+    width = 1
+    while dims and dims[-1][1] == width == dims[-1][2]:
+        width *= dims.pop()[0]
+    heads, apart = 1, (0, 0)
+    if dims and width:
+        heads, *apart = dims.pop()
+        while dims and dims[-1][1] == heads * apart[0] and dims[-1][2] == heads * apart[1]:
+            heads *= dims.pop()[0]
+        if dims:
+            raise ValueError("states and out have more than one dimension apart behind their tokens")
+    return [States(shape[0], shape[1], heads, width * size, s[0] * size, s[1] * size, a * size) for s, a in zip(strides, apart)]
+
+
+def beam_reorder(states, parents, beams: int, *, lengths=None, out=None, stream=None):
+    """Row i of each of `states` (a tensor rows x tokens x ..., or a list of up to MAX_STATES of one layout: caches,
+    histories) takes row parents[i] (int64, within its group of `beams` rows), in place or in `out`.  `lengths` (int64,
+    one per row): how many tokens a parent's row holds, of which the others are not written; all of them by default.
+    Returns `states` or `out`."""
+    import torch
+    one = not isinstance(states, (list, tuple))
+    source = [states] if one else states
+    target = source if out is None else [out] if one else out
+    if not source:
+        return states if out is None else out
+    if len(source) > MAX_STATES or len(target) != len(source) or target[0].dtype != source[0].dtype:
+        raise ValueError(f"states must be up to {MAX_STATES} tensors, and out as many of their type")
+    like = source[0]
+    from_ = _addresses(source, "states")
+    to = from_ if out is None else _addresses(target, "out")
+    if target[0].shape != like.shape:
+        raise ValueError("out must have the shape of states")
+    layout, to_layout = _layouts(like, target[0])
+    y = _vector(parents, layout.rows, torch.int64, like, "parents")
+    n = None if lengths is None else _vector(lengths, layout.rows, torch.int64, like, "lengths")
+    _check(load().bf_beam_reorder(from_, layout, to, to_layout, len(source), y, beams, n, _stream_of(stream, like)))
+    for t in target:
+        _written(t)
+    return states if out is None else out

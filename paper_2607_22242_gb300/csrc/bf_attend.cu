@@ -1,0 +1,365 @@
+// bf_attend.cu -- attention of one token of many answers to a shared prompt and
+// to their own tokens: any type, layout and dimension (general_kernel), and the
+// joining of all pieces (join_kernel).
+#include "bf_attend.cuh"
+
+namespace bfk {
+
+namespace {
+
+// ---- pieces, for any type and layout ----------------------------------------
+
+// A piece: R query vectors against keys [k0, k1), 64 at a time, on 256 threads.
+// Everything is staged in shared memory in 32 bits; a thread makes 4 rows by
+// R / 16 (scores) or dim / (1024 / R) (outputs) values, so that a value read from
+// shared memory is used four times or more.
+constexpr uint32_t kThreads = 256, kKeys = 64, kMaxDim = 256;
+
+template <uint32_t R>
+struct Shape {
+  static constexpr uint32_t kRowGroups = R / 4, kCols = kThreads / kRowGroups;  // threads by rows and by columns
+  static constexpr uint32_t kScores = kKeys / kCols;                            // scores of a thread and row
+  static constexpr uint32_t kOuts = kMaxDim / kCols;                            // outputs, at most
+  static constexpr uint32_t kRowThreads = kThreads / R;                         // threads of a row's softmax
+};
+
+__host__ __device__ constexpr uint32_t pitch_of(uint32_t dim) { return (dim + 3) / 4 * 4 + 4; }
+template <uint32_t R>
+constexpr uint32_t shared_of(uint32_t dim) {
+  return 4 * ((R + kKeys) * pitch_of(dim) + R * (kKeys + 4) + 3 * R);
+}
+
+struct Piece {
+  const void *k, *v;
+  int64_t k_token, v_token;
+  uint32_t k0, k1;
+  float* record;
+};
+
+template <typename E>
+__device__ __forceinline__ void stage(float* to, uint32_t pitch, const E* from, int64_t step, uint32_t rows, uint32_t most,
+                                      uint32_t dim) {
+  const uint32_t wide = pitch - 4;
+  for (uint32_t i = threadIdx.x; i < most * wide; i += kThreads) {
+    const uint32_t r = i / wide, d = i % wide;
+    to[r * pitch + d] = r < rows && d < dim ? to_f32(from[(int64_t)r * step + d]) : 0.0f;
+  }
+}
+
+// Rows [0, rows) of Q, scaled, are in qs.
+template <typename E, uint32_t R>
+__device__ void piece(const Piece& p, uint32_t rows, uint32_t dim, float* sm) {
+  using S = Shape<R>;
+  const uint32_t pitch = pitch_of(dim), t = threadIdx.x, rg = t / S::kCols, cg = t % S::kCols;
+  float *qs = sm, *kv = qs + R * pitch, *ps = kv + kKeys * pitch, *ms = ps + R * (kKeys + 4), *ls = ms + R, *as = ls + R;
+  float o[4][S::kOuts] = {};
+  if (t < R) {
+    ms[t] = kNone;
+    ls[t] = 0.0f;
+  }
+  for (uint32_t k = p.k0; k < p.k1; k += kKeys) {
+    const uint32_t n = min(kKeys, p.k1 - k);
+    stage<E>(kv, pitch, static_cast<const E*>(p.k) + (int64_t)k * p.k_token, p.k_token, n, kKeys, dim);
+    __syncthreads();
+    float s[4][S::kScores] = {};
+    for (uint32_t d = 0; d < pitch - 4; d += 4) {
+      float4 q[4], c[S::kScores];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q[i] = *reinterpret_cast<const float4*>(qs + (rg * 4 + i) * pitch + d);
+#pragma unroll
+      for (uint32_t j = 0; j < S::kScores; ++j) c[j] = *reinterpret_cast<const float4*>(kv + (cg + j * S::kCols) * pitch + d);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (uint32_t j = 0; j < S::kScores; ++j)
+          s[i][j] = fmaf(q[i].w, c[j].w, fmaf(q[i].z, c[j].z, fmaf(q[i].y, c[j].y, fmaf(q[i].x, c[j].x, s[i][j]))));
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (uint32_t j = 0; j < S::kScores; ++j) {
+        const uint32_t at = cg + j * S::kCols;
+        ps[(rg * 4 + i) * (kKeys + 4) + at] = at < n ? s[i][j] : kNone;
+      }
+    __syncthreads();
+    stage<E>(kv, pitch, static_cast<const E*>(p.v) + (int64_t)k * p.v_token, p.v_token, n, kKeys, dim);
+    {
+      const uint32_t row = t / S::kRowThreads, mine = t % S::kRowThreads;
+      float* x = ps + row * (kKeys + 4);
+      float m = kNone;
+      for (uint32_t j = mine; j < kKeys; j += S::kRowThreads) m = fmaxf(m, x[j]);
+#pragma unroll
+      for (uint32_t w = S::kRowThreads / 2; w; w /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, w));
+      const float old = ms[row], now = fmaxf(old, m), base = now == kNone ? 0.0f : now;
+      float l = 0.0f;
+      for (uint32_t j = mine; j < kKeys; j += S::kRowThreads) {
+        const float e = exp2_of(x[j] - base);
+        x[j] = j < n ? e : 0.0f;
+        l += j < n ? e : 0.0f;
+      }
+#pragma unroll
+      for (uint32_t w = S::kRowThreads / 2; w; w /= 2) l += __shfl_xor_sync(~0u, l, w);
+      if (mine == 0) {
+        const float shrink = exp2_of(old - base);
+        ms[row] = now;
+        as[row] = shrink;
+        ls[row] = fmaf(ls[row], shrink, l);
+      }
+    }
+    __syncthreads();
+    float shrink[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) shrink[i] = as[rg * 4 + i];
+#pragma unroll
+    for (uint32_t c = 0; c < S::kOuts; ++c) {
+      const uint32_t d = cg + c * S::kCols;
+      if (d >= dim) break;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i][c] *= shrink[i];
+    }
+    for (uint32_t j = 0; j < n; ++j) {
+      float w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = ps[(rg * 4 + i) * (kKeys + 4) + j];
+#pragma unroll
+      for (uint32_t c = 0; c < S::kOuts; ++c) {
+        const uint32_t d = cg + c * S::kCols;
+        if (d >= dim) break;
+        const float v = kv[j * pitch + d];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i][c] = fmaf(w[i], v, o[i][c]);
+      }
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t row = rg * 4 + i;
+    if (row >= rows) break;
+#pragma unroll
+    for (uint32_t c = 0; c < S::kOuts; ++c) {
+      const uint32_t d = cg + c * S::kCols;
+      if (d >= dim) break;
+      p.record[row * dim + d] = o[i][c];
+    }
+  }
+  if (t < rows) {
+    float2* ml = reinterpret_cast<float2*>(p.record + R * dim);
+    ml[t] = make_float2(ms[t], ls[t]);
+  }
+  __syncthreads();
+}
+
+// Query vectors [first, first + rows) of a prompt's (or an answer's) for a key head, scaled.
+template <typename E>
+__device__ __forceinline__ void stage_q(const AttendArgs& a, float* to, uint64_t answer0, uint32_t head, uint32_t first,
+                                        uint32_t rows, uint32_t most) {
+  const uint32_t pitch = pitch_of(a.dim), wide = pitch - 4;
+  const E* q = static_cast<const E*>(a.q.data);
+  for (uint32_t i = threadIdx.x; i < most * wide; i += kThreads) {
+    const uint32_t r = i / wide, d = i % wide, at = first + r;
+    float v = 0.0f;
+    if (r < rows && d < a.dim)
+      v = to_f32(q[(int64_t)(answer0 + at / a.share) * a.q.batch + (int64_t)(head * a.share + at % a.share) * a.q.head + d]);
+    to[r * pitch + d] = v * a.scale2;
+  }
+  __syncthreads();
+}
+
+template <typename E, uint32_t R>
+__global__ void __launch_bounds__(kThreads) general_kernel(const __grid_constant__ AttendArgs a,
+                                                           const __grid_constant__ AttendPlan plan) {
+  extern __shared__ float sm[];
+  let_next_start();
+  if (blockIdx.x < plan.parts) {
+    const uint32_t inners = a.kv_heads * plan.row_tiles, rows_all = a.per_prompt * a.share;
+    const uint64_t total = tiles_before(a, kKeys, a.prompts) * inners;
+    const uint64_t parts = parts_of(plan, total);
+    if (blockIdx.x >= parts) return;
+    const uint64_t t0 = total * blockIdx.x / parts, t1 = total * (blockIdx.x + 1) / parts;
+    Place at = place_of(a, kKeys, inners, t0);
+    for (uint64_t left = t1 - t0; left;) {
+      const uint32_t len = length_of(a.prefix_len, a.prefix_cap, at.prompt), tiles = (len + kKeys - 1) / kKeys;
+      if (tiles == 0) {
+        ++at.prompt;
+        continue;
+      }
+      const uint32_t n = (uint32_t)min((uint64_t)(tiles - at.tile), left);
+      const uint32_t head = at.inner / plan.row_tiles, first = at.inner % plan.row_tiles * R, rows = min(R, rows_all - first);
+      stage_q<E>(a, sm, (uint64_t)at.prompt * a.per_prompt, head, first, rows, R);
+      const Piece p = {static_cast<const E*>(a.pk.data) + at.prompt * a.pk.batch + head * a.pk.head,
+                       static_cast<const E*>(a.pv.data) + at.prompt * a.pv.batch + head * a.pv.head,
+                       a.pk.token, a.pv.token, at.tile * kKeys, min(len, (at.tile + n) * kKeys),
+                       plan.prefix + (uint64_t)(blockIdx.x + (uint64_t)at.prompt * inners + at.inner) * plan.record};
+      piece<E, R>(p, rows, a.dim, sm);
+      left -= n;
+      at.tile = 0;
+      if (++at.inner == inners) {
+        at.inner = 0;
+        ++at.prompt;
+      }
+    }
+  } else {
+    uint64_t i = blockIdx.x - plan.parts;
+    const uint64_t slot = i;
+    const uint32_t split = i % plan.suffix_splits;
+    i /= plan.suffix_splits;
+    const uint32_t first = i % plan.suffix_row_tiles * R;
+    i /= plan.suffix_row_tiles;
+    const uint32_t head = i % a.kv_heads;
+    const uint64_t answer = i / a.kv_heads;
+    const uint32_t len = length_of(a.suffix_len, a.suffix_cap, answer), rows = min(R, a.share - first);
+    stage_q<E>(a, sm, answer, head, first, rows, R);
+    const Piece p = {static_cast<const E*>(a.sk.data) + answer * a.sk.batch + head * a.sk.head,
+                     static_cast<const E*>(a.sv.data) + answer * a.sv.batch + head * a.sv.head, a.sk.token, a.sv.token,
+                     (uint32_t)((uint64_t)len * split / plan.suffix_splits),
+                     (uint32_t)((uint64_t)len * (split + 1) / plan.suffix_splits), plan.suffix + slot * plan.suffix_record};
+    piece<E, R>(p, rows, a.dim, sm);
+  }
+}
+
+// ---- joining ----------------------------------------------------------------
+
+// A warp per query vector: its pieces' maxima and sums, then its outputs, a lane to a dimension.
+template <typename E>
+__global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ AttendArgs a,
+                                                        const __grid_constant__ AttendPlan plan) {
+  const uint32_t lane = threadIdx.x % 32, heads = a.kv_heads * a.share;
+  const uint64_t vec = (uint64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+  if (vec >= (uint64_t)a.prompts * a.per_prompt * heads) return;
+  const uint64_t answer = vec / heads;
+  const uint32_t h = vec % heads, head = h / a.share, prompt = answer / a.per_prompt;
+  const uint32_t row = (answer % a.per_prompt) * a.share + h % a.share;
+  const uint32_t inners = a.kv_heads * plan.row_tiles, inner = head * plan.row_tiles + row / plan.rows;
+  // The blocks that have a piece of the row's segment.
+  const uint64_t total = tiles_before(a, plan.keys, a.prompts) * inners;
+  const uint32_t tiles = (length_of(a.prefix_len, a.prefix_cap, prompt) + plan.keys - 1) / plan.keys;
+  const uint64_t at = tiles_before(a, plan.keys, prompt) * inners + (uint64_t)inner * tiles;
+  uint32_t c0 = 0, c1 = 0;
+  if (tiles) {
+    const uint64_t parts = parts_of(plan, total);
+    c0 = (uint32_t)(((at + 1) * parts - 1) / total);
+    c1 = (uint32_t)(((at + tiles) * parts - 1) / total) + 1;
+  }
+  const uint64_t segment = (uint64_t)prompt * inners + inner;
+  const uint32_t splits = a.suffix_cap ? plan.suffix_splits : 0, pieces = c1 - c0 + splits;
+  const uint32_t srow = h % a.share;
+  const uint64_t sslot = ((answer * a.kv_heads + head) * plan.suffix_row_tiles + srow / plan.suffix_rows) * plan.suffix_splits;
+  const auto record = [&](uint32_t i, uint32_t& rows, uint32_t& r) -> const float* {
+    if (i < c1 - c0) {
+      rows = plan.rows;
+      r = row % plan.rows;
+      return plan.prefix + (c0 + i + segment) * plan.record;
+    }
+    rows = plan.suffix_rows;
+    r = srow % plan.suffix_rows;
+    return plan.suffix + (sslot + (i - (c1 - c0))) * plan.suffix_record;
+  };
+  const bool bad = bad_length(a.prefix_len, a.prefix_cap, prompt) || (a.suffix_cap && bad_length(a.suffix_len, a.suffix_cap, answer)) ||
+                   (!a.suffix_cap && a.suffix_len && __ldg(a.suffix_len + answer) != 0);
+  wait_for_previous();
+  float m = kNone;
+  bool odd = bad;
+  for (uint32_t i = lane; i < pieces; i += 32) {
+    uint32_t rows, r;
+    const float* p = record(i, rows, r);
+    const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + (uint64_t)rows * a.dim) + r);
+    m = fmaxf(m, ml.x);
+    odd |= ml.y != ml.y;
+  }
+#pragma unroll
+  for (int d = 16; d; d /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+  odd = __any_sync(~0u, odd);
+  const float base = m == kNone ? 0.0f : m;
+  float l = 0.0f, o[kMaxDim / 32] = {};
+  for (uint32_t i = 0; i < pieces; ++i) {
+    uint32_t rows, r;
+    const float* p = record(i, rows, r);
+    const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + (uint64_t)rows * a.dim) + r);
+    const float w = exp2_of(ml.x - base);
+    if (!(ml.y > 0.0f)) continue;  // nothing to attend to in this piece: its outputs are 0
+    l = fmaf(w, ml.y, l);
+#pragma unroll
+    for (uint32_t c = 0; c < kMaxDim / 32; ++c)
+      if (lane + 32 * c < a.dim) o[c] = fmaf(w, __ldcg(p + r * a.dim + lane + 32 * c), o[c]);
+  }
+  const float nan = __int_as_float(0x7FC00000), inv = odd ? nan : l > 0.0f ? 1.0f / l : 0.0f;
+  E* out = static_cast<E*>(const_cast<void*>(a.out.data)) + (int64_t)answer * a.out.batch + (int64_t)h * a.out.head;
+#pragma unroll
+  for (uint32_t c = 0; c < kMaxDim / 32; ++c)
+    if (lane + 32 * c < a.dim) out[lane + 32 * c] = from_f32<E>(o[c] * inv);
+  if (a.lse && lane == 0) a.lse[vec] = odd ? nan : l > 0.0f ? (m + log2f(l)) * 0.693147180559945309f : kNone;
+}
+
+// ---- the host's part --------------------------------------------------------
+
+constexpr uint32_t kParts = 304;  // two blocks of each of 152 SMs
+
+AttendPlan plan_of(const AttendArgs& a, void* workspace, uint64_t* bytes) {
+  AttendPlan p = {};
+  const uint64_t rows = (uint64_t)a.per_prompt * a.share;
+  p.rows = rows <= 16 ? 16 : 64;
+  p.row_tiles = (uint32_t)((rows + p.rows - 1) / p.rows);
+  p.keys = kKeys;
+  p.parts = kParts;
+  p.suffix_rows = p.rows;
+  p.suffix_row_tiles = (a.share + p.suffix_rows - 1) / p.suffix_rows;
+  const uint64_t pieces = (uint64_t)a.prompts * a.per_prompt * a.kv_heads * p.suffix_row_tiles;
+  uint64_t splits = pieces ? kParts / pieces : 1;
+  splits = splits < a.suffix_cap / 128 ? splits : a.suffix_cap / 128;
+  p.suffix_splits = splits < 1 ? 1 : (uint32_t)splits;
+  p.record = p.rows * a.dim + 2 * p.rows;
+  p.record += p.record % 2;
+  p.suffix_record = p.record;
+  const uint64_t slots = kParts + (uint64_t)a.prompts * a.kv_heads * p.row_tiles;
+  const uint64_t prefix = (4 * slots * p.record + 255) / 256 * 256;
+  const uint64_t suffix = a.suffix_cap ? (4 * pieces * p.suffix_splits * p.suffix_record + 255) / 256 * 256 : 0;
+  p.prefix = static_cast<float*>(workspace);
+  p.suffix = reinterpret_cast<float*>(static_cast<char*>(workspace) + prefix);
+  *bytes = prefix + suffix;
+  return p;
+}
+
+template <typename K>
+cudaError_t launch_sized(K kernel, uint64_t blocks, uint32_t shared, cudaStream_t st, const AttendArgs& a, const AttendPlan& p) {
+  if (blocks > 0x7FFFFFFFu) return cudaErrorInvalidValue;
+  if (shared > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+    if (e != cudaSuccess) return e;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((uint32_t)blocks);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = shared;
+  cfg.stream = st;
+  return cudaLaunchKernelEx(&cfg, kernel, a, p);
+}
+
+template <typename E>
+cudaError_t launch_type(const AttendArgs& a, void* workspace, cudaStream_t st) {
+  uint64_t bytes = 0;
+  const AttendPlan p = plan_of(a, workspace, &bytes);
+  const uint64_t answers = (uint64_t)a.prompts * a.per_prompt;
+  const uint64_t suffix = a.suffix_cap ? answers * a.kv_heads * p.suffix_row_tiles * p.suffix_splits : 0;
+  cudaError_t e = p.rows == 16 ? launch_sized(general_kernel<E, 16>, p.parts + suffix, shared_of<16>(a.dim), st, a, p)
+                               : launch_sized(general_kernel<E, 64>, p.parts + suffix, shared_of<64>(a.dim), st, a, p);
+  if (e != cudaSuccess) return e;
+  const uint64_t vectors = answers * a.kv_heads * a.share;
+  return launch_after(join_kernel<E>, (vectors + kThreads / 32 - 1) / (kThreads / 32), kThreads, st, a, p);
+}
+
+}  // namespace
+
+uint64_t attend_bytes(const AttendArgs& a) {
+  uint64_t bytes = 0;
+  plan_of(a, nullptr, &bytes);
+  return bytes ? bytes : 256;
+}
+
+cudaError_t launch_attend(const AttendArgs& a, void* workspace, cudaStream_t st) {
+  return a.dtype == BF_F32    ? launch_type<float>(a, workspace, st)
+         : a.dtype == BF_BF16 ? launch_type<__nv_bfloat16>(a, workspace, st)
+                              : launch_type<__half>(a, workspace, st);
+}
+
+}  // namespace bfk

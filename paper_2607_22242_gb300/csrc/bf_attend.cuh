@@ -1,0 +1,98 @@
+// bf_attend.cuh -- what the attention kernels share: how a call's keys are cut
+// into pieces, and the record that a piece leaves.
+//
+// With s_t = scale q . k_t over a piece's keys, in units of log2(e):
+//   m = max s_t, l = sum 2^(s_t - m), o = sum 2^(s_t - m) v_t,
+// and pieces join by their sums weighted with 2^(m_i - max m): out = o / l, lse =
+// ln2 (m + log2 l).  All of it is held in 32 bits.
+//
+// The prompts' keys.  A segment is a prompt, a key head and a tile of up to `rows`
+// query vectors (the prompt's answers times the query heads that share the key
+// head); it has ceil(length / keys) tiles of keys.  The tiles of all segments, in
+// order, are dealt to `parts` blocks in runs of equal length, so that prompts of
+// uneven lengths, one long prompt and many short ones all keep every SM busy to
+// the end.  A run may begin and end inside a segment; block c's piece of segment
+// s leaves its record in slot c + s, which no two pieces share.  Lengths are in
+// device memory: blocks find their runs themselves.
+#pragma once
+
+#include "bf_answer.h"
+#include "bf_elem.cuh"
+#include "bf_launches.cuh"
+
+namespace bfk {
+
+// How a call is cut; chosen on the host from the sizes alone.
+struct AttendPlan {
+  uint32_t rows, row_tiles;      // query vectors of a prefix segment, segments of a prompt and key head
+  uint32_t keys;                 // of a tile
+  uint32_t parts;                // blocks that share the prefix tiles out
+  uint32_t suffix_rows, suffix_row_tiles, suffix_splits;  // the answers' own keys: pieces of an answer and key head
+  float *prefix, *suffix;        // records
+  uint32_t record, suffix_record;  // floats of a record: rows * dim, then rows (m, l) pairs
+};
+
+constexpr float kNone = -__builtin_huge_valf();
+__device__ __forceinline__ float exp2_of(float t) {
+  float e;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
+  return e;
+}
+
+// A length as given; 0 where it is outside 0..cap (the answers are NaN: bad_length).
+__device__ __forceinline__ uint32_t length_of(const int64_t* lengths, uint64_t cap, uint64_t i) {
+  if (!lengths) return (uint32_t)cap;
+  const int64_t n = __ldg(lengths + i);
+  return n < 0 || (uint64_t)n > cap ? 0u : (uint32_t)n;
+}
+__device__ __forceinline__ bool bad_length(const int64_t* lengths, uint64_t cap, uint64_t i) {
+  if (!lengths) return false;
+  const int64_t n = __ldg(lengths + i);
+  return n < 0 || (uint64_t)n > cap;
+}
+
+__device__ __forceinline__ uint64_t sum_lanes(uint64_t v) {
+#pragma unroll
+  for (int d = 16; d; d /= 2) v += __shfl_xor_sync(~0u, v, d);
+  return v;
+}
+
+// Key tiles of prompts [0, p) in one segment each; by a whole warp.
+__device__ __forceinline__ uint64_t tiles_before(const AttendArgs& a, uint32_t keys, uint32_t p) {
+  uint64_t n = 0;
+  for (uint32_t i = threadIdx.x % 32; i < p; i += 32) n += (length_of(a.prefix_len, a.prefix_cap, i) + keys - 1) / keys;
+  return sum_lanes(n);
+}
+
+// The blocks that share `total` tiles out: none is without a tile, so that between a
+// segment's first and last block each one has a piece of it.
+__device__ __forceinline__ uint64_t parts_of(const AttendPlan& plan, uint64_t total) { return min((uint64_t)plan.parts, total); }
+
+// A place in the run of all tiles: prompt, segment in it (key head and row tile), tile in that.
+struct Place {
+  uint32_t prompt, inner, tile;
+};
+// The place of tile t (below the total); by a whole warp.
+__device__ __forceinline__ Place place_of(const AttendArgs& a, uint32_t keys, uint32_t inners, uint64_t t) {
+  uint64_t before = 0;
+  for (uint32_t first = 0; first < a.prompts; first += 32) {
+    const uint32_t i = first + threadIdx.x % 32;
+    const uint64_t n = i < a.prompts ? (uint64_t)((length_of(a.prefix_len, a.prefix_cap, i) + keys - 1) / keys) * inners : 0;
+    uint64_t upto = n;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const uint64_t o = __shfl_up_sync(~0u, upto, d);
+      if (threadIdx.x % 32 >= d) upto += o;
+    }
+    const uint32_t past = __ballot_sync(~0u, before + upto > t);
+    if (past) {
+      const int lane = __ffs(past) - 1;
+      const uint64_t at = __shfl_sync(~0u, before + upto - n, lane), mine = __shfl_sync(~0u, n, lane) / inners;
+      return {first + lane, (uint32_t)((t - at) / mine), (uint32_t)((t - at) % mine)};
+    }
+    before += __shfl_sync(~0u, upto, 31);
+  }
+  return {a.prompts, 0, 0};
+}
+
+}  // namespace bfk
