@@ -260,6 +260,8 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
   wait_for_previous();
   float m = kNone;
   bool odd = bad;
+  if (plan.gave_up)
+    for (uint32_t c = c0 + lane; c < c1; c += 32) odd |= __ldcg(plan.gave_up + c) != 0;
   for (uint32_t i = lane; i < pieces; i += 32) {
     uint32_t rows, r;
     const float* p = record(i, rows, r);
@@ -295,28 +297,33 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
 
 constexpr uint32_t kParts = 304;  // two blocks of each of 152 SMs
 
-AttendPlan plan_of(const AttendArgs& a, void* workspace, uint64_t* bytes) {
+// `tile`: the prompts' keys go to the tiled kernel.
+AttendPlan plan_of(const AttendArgs& a, bool tile, void* workspace, uint64_t* bytes) {
   AttendPlan p = {};
   const uint64_t rows = (uint64_t)a.per_prompt * a.share;
-  p.rows = rows <= 16 ? 16 : 64;
+  p.rows = tile ? (rows <= 128 ? 128 : 256) : rows <= 16 ? 16 : 64;
   p.row_tiles = (uint32_t)((rows + p.rows - 1) / p.rows);
-  p.keys = kKeys;
-  p.parts = kParts;
-  p.suffix_rows = p.rows;
+  p.keys = tile ? kTileKeys : kKeys;
+  p.parts = tile ? kTileParts : kParts;
+  p.suffix_rows = tile ? (a.share <= 16 ? 16 : 64) : p.rows;
   p.suffix_row_tiles = (a.share + p.suffix_rows - 1) / p.suffix_rows;
   const uint64_t pieces = (uint64_t)a.prompts * a.per_prompt * a.kv_heads * p.suffix_row_tiles;
   uint64_t splits = pieces ? kParts / pieces : 1;
   splits = splits < a.suffix_cap / 128 ? splits : a.suffix_cap / 128;
   p.suffix_splits = splits < 1 ? 1 : (uint32_t)splits;
   p.record = p.rows * a.dim + 2 * p.rows;
-  p.record += p.record % 2;
-  p.suffix_record = p.record;
-  const uint64_t slots = kParts + (uint64_t)a.prompts * a.kv_heads * p.row_tiles;
-  const uint64_t prefix = (4 * slots * p.record + 255) / 256 * 256;
-  const uint64_t suffix = a.suffix_cap ? (4 * pieces * p.suffix_splits * p.suffix_record + 255) / 256 * 256 : 0;
-  p.prefix = static_cast<float*>(workspace);
-  p.suffix = reinterpret_cast<float*>(static_cast<char*>(workspace) + prefix);
-  *bytes = prefix + suffix;
+  p.suffix_record = p.suffix_rows * a.dim + 2 * p.suffix_rows;
+  char* at = static_cast<char*>(workspace);
+  const auto take = [&](uint64_t n) {
+    char* q = at;
+    at += (n + 255) / 256 * 256;
+    return q;
+  };
+  p.gave_up = reinterpret_cast<uint32_t*>(take(4 * kTileParts));
+  if (!tile) p.gave_up = nullptr;
+  p.prefix = reinterpret_cast<float*>(take(4 * (p.parts + (uint64_t)a.prompts * a.kv_heads * p.row_tiles) * p.record));
+  p.suffix = reinterpret_cast<float*>(take(a.suffix_cap ? 4 * pieces * p.suffix_splits * p.suffix_record : 0));
+  *bytes = (uint64_t)(at - static_cast<char*>(workspace));
   return p;
 }
 
@@ -338,11 +345,19 @@ cudaError_t launch_sized(K kernel, uint64_t blocks, uint32_t shared, cudaStream_
 template <typename E>
 cudaError_t launch_type(const AttendArgs& a, void* workspace, cudaStream_t st) {
   uint64_t bytes = 0;
-  const AttendPlan p = plan_of(a, workspace, &bytes);
+  const bool tile = tile_takes(a);
+  const AttendPlan p = plan_of(a, tile, workspace, &bytes);
   const uint64_t answers = (uint64_t)a.prompts * a.per_prompt;
   const uint64_t suffix = a.suffix_cap ? answers * a.kv_heads * p.suffix_row_tiles * p.suffix_splits : 0;
-  cudaError_t e = p.rows == 16 ? launch_sized(general_kernel<E, 16>, p.parts + suffix, shared_of<16>(a.dim), st, a, p)
-                               : launch_sized(general_kernel<E, 64>, p.parts + suffix, shared_of<64>(a.dim), st, a, p);
+  cudaError_t e = cudaSuccess;
+  AttendPlan general = p;
+  if (tile) {
+    e = launch_tile(a, p, st);
+    general.parts = 0;
+  }
+  if (e == cudaSuccess && general.parts + suffix)
+    e = p.suffix_rows == 16 ? launch_sized(general_kernel<E, 16>, general.parts + suffix, shared_of<16>(a.dim), st, a, general)
+                            : launch_sized(general_kernel<E, 64>, general.parts + suffix, shared_of<64>(a.dim), st, a, general);
   if (e != cudaSuccess) return e;
   const uint64_t vectors = answers * a.kv_heads * a.share;
   return launch_after(join_kernel<E>, (vectors + kThreads / 32 - 1) / (kThreads / 32), kThreads, st, a, p);
@@ -352,8 +367,13 @@ cudaError_t launch_type(const AttendArgs& a, void* workspace, cudaStream_t st) {
 
 uint64_t attend_bytes(const AttendArgs& a) {
   uint64_t bytes = 0;
-  plan_of(a, nullptr, &bytes);
-  return bytes ? bytes : 256;
+  plan_of(a, false, nullptr, &bytes);
+  if (tile_might_take(a)) {
+    uint64_t more = 0;
+    plan_of(a, true, nullptr, &more);
+    bytes = more > bytes ? more : bytes;
+  }
+  return bytes;
 }
 
 cudaError_t launch_attend(const AttendArgs& a, void* workspace, cudaStream_t st) {

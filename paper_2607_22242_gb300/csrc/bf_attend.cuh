@@ -29,6 +29,7 @@ struct AttendPlan {
   uint32_t parts;                // blocks that share the prefix tiles out
   uint32_t suffix_rows, suffix_row_tiles, suffix_splits;  // the answers' own keys: pieces of an answer and key head
   float *prefix, *suffix;        // records
+  uint32_t* gave_up;             // of the tiled kernel's blocks; nullptr: it does not run
   uint32_t record, suffix_record;  // floats of a record: rows * dim, then rows (m, l) pairs
 };
 
@@ -94,5 +95,12 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a, uint32_t keys, ui
   }
   return {a.prompts, 0, 0};
 }
+
+// The prompts' keys on the tensor cores (bf_attend_tile.cu): what of a call says that it may take them, and, with
+// the addresses and strides, does.
+inline bool tile_might_take(const AttendArgs& a) { return a.dtype != BF_F32 && a.dim % 8 == 0 && a.dim <= 128 && a.prefix_cap > 0; }
+bool tile_takes(const AttendArgs& a);
+constexpr uint32_t kTileKeys = 128, kTileParts = 152;  // a block on each SM
+cudaError_t launch_tile(const AttendArgs& a, const AttendPlan& plan, cudaStream_t st);
 
 }  // namespace bfk

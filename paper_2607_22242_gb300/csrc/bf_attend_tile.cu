@@ -1,0 +1,488 @@
+// bf_attend_tile.cu -- the prompts' keys on the tensor cores: 128 query vectors
+// (the answers of a prompt times the query heads that share a key head) against
+// tiles of 128 keys, 16-bit types, up to 128 dimensions.
+//
+// S = Q K^T and O += P V are tcgen05 products with S, P and O in tensor memory; K
+// and V come by TMA.  A block has two streams of tiles: of the same queries, even and
+// odd tiles of keys (whose sums it joins at a piece's end), or of 256 queries, each
+// half with all tiles.  While one stream's weights are made (a thread to a query, 128
+// threads), the other's products run: a prompt's keys are read once at the memory's
+// rate.  Queries that no thread has are skipped by whole warps.
+//
+// The maximum that weights are taken against is raised only where a score is above
+// it by more than 8 (in log2): weights are at most 2^8, and O in tensor memory is
+// rescaled a few times at the beginning of a piece instead of at every tile.
+// Weights are rounded to the keys' type, a relative 2^-9 (bf16) or 2^-12, as the
+// output is at the end; their sum is of the unrounded ones, in 32 bits.
+#include <cuda.h>
+
+#include "bf_attend.cuh"
+#include "bf_blackwell.cuh"
+
+namespace bfk {
+
+namespace {
+
+constexpr uint32_t kKeys = 128, kRows = 128;
+constexpr uint32_t kSoft = 256, kThreads = kSoft + 64;  // softmax threads; then a warp that copies, a warp that multiplies
+constexpr uint32_t kColumns = 512;                      // of tensor memory: S and P of both streams, O of both
+constexpr uint32_t kMaxStages = 12;
+constexpr float kRaise = 8.0f;
+
+struct TileArgs {
+  TensorMap k, v;
+  uint32_t stages, chunks;  // of the ring of K and V tiles; columns of 64 elements
+  uint32_t columns;         // dimensions, to a multiple of 16
+  uint32_t pair;            // 256 queries a block
+  uint32_t* gave_up;        // one word a block
+};
+
+struct Shared {
+  uint64_t full[kMaxStages], empty[kMaxStages];
+  uint64_t q_full, s_full[2], p_full[2], o_done[2];
+  uint32_t tensor, gave_up;
+  float2 sums[2][kRows];  // (maximum, sum) of the streams
+};
+
+// A block's pieces, in order; the same for all its warps.
+struct Pieces {
+  const AttendArgs& a;
+  const AttendPlan& plan;
+  uint32_t inners;
+  uint64_t left;
+  Place at;
+  uint32_t len, tiles;  // the piece's prompt, and its tiles
+
+  __device__ __forceinline__ Pieces(const AttendArgs& args, const AttendPlan& p)
+      : a(args), plan(p), inners(args.kv_heads * p.row_tiles), left(0), at{0, 0, 0}, len(0), tiles(0) {
+    const uint64_t total = tiles_before(a, kKeys, a.prompts) * inners, parts = parts_of(plan, total);
+    if (blockIdx.x >= parts) return;
+    const uint64_t t0 = total * blockIdx.x / parts, t1 = total * (blockIdx.x + 1) / parts;
+    at = place_of(a, kKeys, inners, t0);
+    left = t1 - t0;
+    find();
+  }
+  __device__ __forceinline__ void find() {
+    for (;; ++at.prompt) {
+      if (left == 0) return;
+      len = length_of(a.prefix_len, a.prefix_cap, at.prompt);
+      if (len) break;
+    }
+    tiles = (uint32_t)min((uint64_t)((len + kKeys - 1) / kKeys - at.tile), left);
+  }
+  __device__ __forceinline__ bool more() const { return left != 0; }
+  __device__ __forceinline__ void next() {
+    left -= tiles;
+    at.tile = 0;
+    if (++at.inner == inners) {
+      at.inner = 0;
+      ++at.prompt;
+    }
+    find();
+  }
+  __device__ __forceinline__ uint32_t head() const { return at.inner / plan.row_tiles; }
+  __device__ __forceinline__ uint32_t first_row() const { return at.inner % plan.row_tiles * plan.rows; }
+};
+
+// The ring of K and V tiles: how many were taken, and so the place and phase of the next.
+struct Ring {
+  uint32_t stage = 0, phase = 0;
+  __device__ __forceinline__ void step(uint32_t stages) {
+    if (++stage == stages) {
+      stage = 0;
+      phase ^= 1;
+    }
+  }
+};
+
+// Tiles in the order in which they are first used: with `lead` steps of scores
+// ahead (2 tiles, or 1 of both streams), K_0 .. K_lead-1, V_0, K_lead, V_1, ...
+__device__ void copy_tiles(const AttendArgs& a, const AttendPlan& plan, const TileArgs& t, Shared& sh, unsigned char* ring) {
+  const uint32_t bytes = t.chunks * kKeys * 128;
+  Ring r;
+  const auto load = [&](const TensorMap& map, uint32_t tile, const Pieces& p) {
+    if (!barrier_wait(&sh.empty[r.stage], r.phase ^ 1, &sh.gave_up)) return false;
+    if (threadIdx.x % 32 == 0) {
+      barrier_expect(&sh.full[r.stage], bytes);
+      for (uint32_t c = 0; c < t.chunks; ++c)
+        copy_box(ring + r.stage * bytes + c * kKeys * 128, &map, (int32_t)(c * 64), (int32_t)p.head(),
+                 (int32_t)((p.at.tile + tile) * kKeys), (int32_t)p.at.prompt, &sh.full[r.stage]);
+    }
+    __syncwarp();
+    r.step(t.stages);
+    return true;
+  };
+  const uint32_t lead = t.pair ? 1 : 2;
+  uint32_t loads = 0;
+  bool ok = true;
+  for (Pieces p(a, plan); ok && p.more(); p.next()) {
+    for (uint32_t i = 0; ok && i < min(lead, p.tiles); ++i) loads += ok = load(t.k, i, p);
+    for (uint32_t i = 0; ok && i < p.tiles; ++i) {
+      loads += ok = load(t.v, i, p);
+      if (ok && i + lead < p.tiles) loads += ok = load(t.k, i + lead, p);
+    }
+  }
+  // No copy is in flight when the block ends: the last `stages` loads have arrived.
+  Ring w;
+  for (uint32_t i = 0; i < loads; ++i, w.step(t.stages))
+    if (i + t.stages >= loads)
+      for (uint32_t n = 0; n < 1u << 22 && !barrier_try(&sh.full[w.stage], w.phase); ++n) {
+      }
+}
+
+template <bool bf16>
+__device__ void multiply_tiles(const AttendArgs& a, const AttendPlan& plan, const TileArgs& t, Shared& sh, uint32_t q_at,
+                               unsigned char* ring_base) {
+  const uint32_t bytes = t.chunks * kKeys * 128, tensor = sh.tensor, lane = threadIdx.x % 32;
+  const uint32_t ring_at = shared_address(ring_base);
+  const uint32_t scores = product_of(bf16, kKeys, false), outputs = product_of(bf16, t.columns, true);
+  Ring r;
+  uint32_t q_phase = 0, p_phase[2] = {0, 0}, o_phase[2] = {0, 0};
+  bool ok = true;
+  for (Pieces p(a, plan); ok && p.more(); p.next()) {
+    if (!(ok = barrier_wait(&sh.q_full, q_phase, &sh.gave_up))) break;
+    q_phase ^= 1;
+    tensor_fence_after();
+    const uint32_t steps = t.pair ? 2 * p.tiles : p.tiles;
+    uint32_t k_stage = 0, v_stage = 0;
+    // Takes the next tile from the ring.
+    const auto take = [&](uint32_t& stage) {
+      stage = r.stage;
+      const bool got = barrier_wait(&sh.full[r.stage], r.phase, &sh.gave_up);
+      r.step(t.stages);
+      return got;
+    };
+    const auto score = [&](uint32_t i) {
+      const uint32_t s = i & 1;
+      if (i >= 2) {  // the weights that lie where the scores will have been used
+        if (!barrier_wait(&sh.o_done[s], o_phase[s], &sh.gave_up)) return false;
+        o_phase[s] ^= 1;
+        tensor_fence_after();
+      }
+      if ((!t.pair || s == 0) && !take(k_stage)) return false;
+      if (lane == 0) {
+        const uint32_t q = q_at + (t.pair ? s * t.chunks * kRows * 128 : 0), k = ring_at + k_stage * bytes;
+        for (uint32_t d = 0; d < t.columns; d += 16) {
+          const uint32_t off = d / 64 * (kKeys * 128) + d % 64 * 2;
+          multiply(tensor + s * 128, matrix_at(q + off, 16), matrix_at(k + off, 16), scores, d != 0);
+        }
+        tensor_commit(&sh.s_full[s]);
+        if (!t.pair || s == 1) tensor_commit(&sh.empty[k_stage]);
+      }
+      __syncwarp();
+      return true;
+    };
+    for (uint32_t i = 0; ok && i < min(steps, 2u); ++i) ok = score(i);
+    for (uint32_t i = 0; ok && i < steps; ++i) {
+      const uint32_t s = i & 1, tile = t.pair ? i / 2 : i;
+      const bool fresh = !t.pair || s == 0;
+      if (fresh && !(ok = take(v_stage))) break;
+      const uint32_t valid = min(kKeys, p.len - (p.at.tile + tile) * kKeys), deep = (valid + 15) / 16 * 16;
+      if (fresh && valid < deep) {  // whatever lies behind the prompt's end is not multiplied, not even by 0
+        const uint32_t row = t.chunks * 8;  // pieces of 16 bytes
+        for (uint32_t n = lane; n < (deep - valid) * row; n += 32) {
+          const uint32_t key = valid + n / row, c = n % row;
+          *reinterpret_cast<uint4*>(ring_base + v_stage * bytes + c / 8 * (kKeys * 128) + key * 128 + c % 8 * 16) =
+              make_uint4(0, 0, 0, 0);
+        }
+        fence_to_async();
+        __syncwarp();
+      }
+      if (!(ok = barrier_wait(&sh.p_full[s], p_phase[s], &sh.gave_up))) break;
+      p_phase[s] ^= 1;
+      tensor_fence_after();
+      if (lane == 0) {
+        const uint32_t v = ring_at + v_stage * bytes;
+        for (uint32_t n = 0; n < deep; n += 16)
+          multiply_held(tensor + 256 + s * 128, tensor + s * 128 + n / 2, matrix_at(v + n * 128, kKeys * 128), outputs,
+                        n != 0 || i >= 2);
+        tensor_commit(&sh.o_done[s]);
+        if (!t.pair || s == 1) tensor_commit(&sh.empty[v_stage]);
+      }
+      __syncwarp();
+      if (i + 2 < steps) ok = score(i + 2);
+    }
+    // The last outputs of each stream are the softmax threads' to wait for: these phases pass.
+    for (uint32_t s = 0; s < min(steps, 2u); ++s) o_phase[s] ^= 1;
+  }
+  // No product is in flight when the block ends; where a wait gave up, one has milliseconds to end.
+  if (!ok)
+    for (uint32_t n = 0; n < 1u << 16; ++n) __nanosleep(100);
+}
+
+// A query vector to a thread: rows [first, first + rows) of the prompt's, pieces of 16 bytes where they are aligned.
+template <typename E>
+__device__ __forceinline__ void stage_q(const AttendArgs& a, const Pieces& p, const TileArgs& t, unsigned char* to) {
+  const uint32_t rows_all = a.per_prompt * a.share, first = p.first_row(), tile_rows = t.pair ? 2 * kRows : kRows;
+  const uint32_t row_pieces = t.chunks * 8;
+  const bool aligned = ((uintptr_t)a.q.data | (uint64_t)a.q.batch * 2 | (uint64_t)a.q.head * 2) % 16 == 0;
+  const uint32_t flip = a.scale2 < 0.0f ? 0x80008000u : 0u;
+  for (uint32_t n = threadIdx.x; n < tile_rows * row_pieces; n += kSoft) {
+    const uint32_t row = n / row_pieces, c = n % row_pieces, at = first + row;
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (at < rows_all && c * 8 < a.dim) {
+      const E* q = static_cast<const E*>(a.q.data) + (int64_t)((uint64_t)p.at.prompt * a.per_prompt + at / a.share) * a.q.batch +
+                   (int64_t)(p.head() * a.share + at % a.share) * a.q.head + c * 8;
+      if (aligned) {
+        u = __ldg(reinterpret_cast<const uint4*>(q));
+      } else {
+        const uint16_t* h = reinterpret_cast<const uint16_t*>(q);
+        u = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16,
+                       h[6] | (uint32_t)h[7] << 16);
+      }
+      u = make_uint4(u.x ^ flip, u.y ^ flip, u.z ^ flip, u.w ^ flip);
+    }
+    const uint32_t r = row % kRows;
+    *reinterpret_cast<uint4*>(to + (row / kRows * t.chunks + c / 8) * (kRows * 128) + r * 128 + (c % 8 ^ r % 8) * 16) = u;
+  }
+}
+
+// A barrier of the softmax threads that tells all of them whether any of them says so.
+__device__ __forceinline__ bool any_of_streams(bool say) {
+  uint32_t any;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.aligned.pred q, 1, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(any)
+      : "r"((uint32_t)say)
+      : "memory");
+  return any;
+}
+
+template <typename E>
+__device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const TileArgs& t, Shared& sh, unsigned char* q_to) {
+  const uint32_t s = threadIdx.x / kRows, row = threadIdx.x % kRows, lane = threadIdx.x % 32;
+  const uint32_t mine = sh.tensor + (row / 32 * 32 << 16), s_at = mine + s * 128;
+  const float scale = fmaxf(fabsf(a.scale2), 1e-37f);  // 0 would make NaN of masked scores
+  const uint32_t rows_all = a.per_prompt * a.share;
+  uint32_t s_phase = 0, o_phase = 0;
+  for (Pieces p(a, plan); p.more(); p.next()) {
+    stage_q<E>(a, p, t, q_to);
+    fence_to_async();
+    tensor_fence_before();
+    barrier_arrive(&sh.q_full);
+    const uint32_t rows = min(plan.rows, rows_all - p.first_row());
+    const uint32_t my_row = t.pair ? s * kRows + row : row;
+    const bool warp_on = my_row - lane < rows;  // some of the warp's rows are there
+    const uint32_t steps = t.pair ? p.tiles : s < p.tiles ? (p.tiles - s + 1) / 2 : 0;
+    float m = kNone, l = 0.0f;
+    bool ok = true;
+    for (uint32_t i = 0; i < steps; ++i) {
+      if (!(ok = barrier_wait(&sh.s_full[s], s_phase, &sh.gave_up))) break;
+      s_phase ^= 1;
+      tensor_fence_after();
+      if (warp_on) {
+        const uint32_t tile = p.at.tile + (t.pair ? i : 2 * i + s), valid = min(kKeys, p.len - tile * kKeys);
+        uint32_t raw[kKeys];
+        float x[kKeys];
+#pragma unroll
+        for (uint32_t c = 0; c < kKeys; c += 32) tensor_load32(s_at + c, raw + c);
+        tensor_wait_load(raw);
+#pragma unroll
+        for (uint32_t c = 0; c < kKeys; ++c) x[c] = __uint_as_float(raw[c]);
+        if (valid < kKeys) {
+#pragma unroll
+          for (uint32_t c = 0; c < kKeys; ++c) x[c] = c < valid ? x[c] : kNone;
+        }
+        float top[4] = {kNone, kNone, kNone, kNone};
+#pragma unroll
+        for (uint32_t c = 0; c < kKeys; ++c) top[c % 4] = fmaxf(top[c % 4], x[c]);
+        const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        float base = m == kNone ? 0.0f : m;
+        const bool raise = (now - base) * scale > kRaise || m == kNone;
+        if (i == 0) {
+          m = now;
+        } else if (__any_sync(~0u, raise)) {
+          const float to = raise ? fmaxf(m, now) : m, shrink = m == kNone ? 0.0f : exp2_of((m - to) * scale);
+          m = to;
+          l *= shrink;
+          for (uint32_t c = 0; c < t.columns; c += 8) {
+            uint32_t o[8];
+            tensor_load8(mine + 256 + s * 128 + c, o);
+            tensor_wait_load(o);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[k] = __float_as_uint(m == kNone || shrink == 0.0f ? 0.0f : __uint_as_float(o[k]) * shrink);
+            tensor_store8(mine + 256 + s * 128 + c, o);
+          }
+          tensor_wait_store();
+        }
+        base = m == kNone ? 0.0f : m;
+        const float2 scale_2 = make_float2(scale, scale), less = make_float2(-base * scale, -base * scale);
+        float2 sum = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (uint32_t half = 0; half < 2; ++half) {
+          uint32_t w[32];
+#pragma unroll
+          for (uint32_t c = 0; c < 32; ++c) {
+            const float2 e = __ffma2_rn(make_float2(x[half * 64 + 2 * c], x[half * 64 + 2 * c + 1]), scale_2, less);
+            const float2 v = make_float2(exp2_of(e.x), exp2_of(e.y));
+            sum = __fadd2_rn(sum, v);
+            w[c] = pack2(v, E());
+          }
+          tensor_store32(s_at + half * 32, w);
+        }
+        l += sum.x + sum.y;
+        tensor_wait_store();
+      }
+      tensor_fence_before();
+      __syncwarp();
+      if (lane == 0) barrier_arrive(&sh.p_full[s]);
+    }
+    // The piece's outputs: all of this stream's products are done.
+    if (ok && steps) ok = barrier_wait(&sh.o_done[s], (o_phase + steps - 1) & 1, &sh.gave_up);
+    o_phase = (o_phase + steps) & 1;
+    float* record = plan.prefix + (uint64_t)(blockIdx.x + (uint64_t)p.at.prompt * p.inners + p.at.inner) * plan.record;
+    sh.sums[s][row] = make_float2(m == kNone ? kNone : m * scale, l);
+    tensor_fence_before();
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    tensor_fence_after();
+    if (t.pair) {
+      if (warp_on)
+        for (uint32_t c = 0; c < a.dim; c += 8) {
+          uint32_t o[8];
+          tensor_load8(mine + 256 + s * 128 + c, o);
+          tensor_wait_load(o);
+          if (my_row < rows) {
+            float4* to = reinterpret_cast<float4*>(record + (uint64_t)my_row * a.dim + c);
+            to[0] = *reinterpret_cast<float4*>(o);
+            to[1] = *reinterpret_cast<float4*>(o + 4);
+          }
+        }
+      if (my_row < rows) reinterpret_cast<float2*>(record + (uint64_t)plan.rows * a.dim)[my_row] = sh.sums[s][row];
+    } else if (warp_on) {
+      // Both streams' sums of the same queries: each stream's threads join half of the dimensions.
+      const float2 s0 = sh.sums[0][row], s1 = sh.sums[1][row];
+      const bool two = p.tiles > 1;
+      const float most = two ? fmaxf(s0.x, s1.x) : s0.x, base = most == kNone ? 0.0f : most;
+      const float w0 = exp2_of(s0.x - base), w1 = two ? exp2_of(s1.x - base) : 0.0f;
+      const uint32_t cut = (a.dim / 16 + 1) / 2 * 16 < a.dim ? (a.dim / 16 + 1) / 2 * 16 : a.dim;
+      for (uint32_t c = s ? cut : 0; c < (s ? a.dim : cut); c += 8) {
+        uint32_t o0[8], o1[8] = {};
+        tensor_load8(mine + 256 + c, o0);
+        if (two) tensor_load8(mine + 384 + c, o1);
+        tensor_wait_load(o0);
+        tensor_wait_load(o1);
+        float o[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o[k] = fmaf(w1, __uint_as_float(o1[k]), w0 * __uint_as_float(o0[k]));
+        if (row < rows) {
+          float4* to = reinterpret_cast<float4*>(record + (uint64_t)row * a.dim + c);
+          to[0] = *reinterpret_cast<float4*>(o);
+          to[1] = *reinterpret_cast<float4*>(o + 4);
+        }
+      }
+      if (s == 0 && row < rows)
+        reinterpret_cast<float2*>(record + (uint64_t)plan.rows * a.dim)[row] = make_float2(most, fmaf(w1, two ? s1.y : 0.0f, w0 * s0.y));
+    }
+    tensor_fence_before();
+    // Both streams have read what the next piece writes over; all of their threads go on, or none.
+    if (any_of_streams(!ok || *static_cast<volatile uint32_t*>(&sh.gave_up))) break;
+  }
+}
+
+template <typename E>
+__global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ AttendPlan plan,
+                                                           const __grid_constant__ TileArgs t) {
+  extern __shared__ __align__(1024) unsigned char base[];  // queries, ring, barriers
+  unsigned char* ring = base + (t.pair ? 2 : 1) * t.chunks * kRows * 128;
+  Shared& sh = *reinterpret_cast<Shared*>(ring + t.stages * t.chunks * kKeys * 128);
+  const uint32_t warp = threadIdx.x / 32;
+  let_next_start();
+  if (shared_address(base) % 1024) {  // the swizzle goes by addresses
+    if (threadIdx.x == 0) t.gave_up[blockIdx.x] = 1;
+    return;
+  }
+  if (threadIdx.x == 0) {
+    for (uint32_t i = 0; i < t.stages; ++i) {
+      barrier_init(&sh.full[i], 1);
+      barrier_init(&sh.empty[i], 1);
+    }
+    barrier_init(&sh.q_full, kSoft);
+    for (uint32_t i = 0; i < 2; ++i) {
+      barrier_init(&sh.s_full[i], 1);
+      barrier_init(&sh.p_full[i], kRows / 32);
+      barrier_init(&sh.o_done[i], 1);
+    }
+    sh.gave_up = 0;
+    fence_barriers();
+  }
+  if (warp == 9) tensor_alloc(&sh.tensor, kColumns);
+  if (warp == 8 && threadIdx.x % 32 == 0) {
+    prefetch_map(&t.k);
+    prefetch_map(&t.v);
+  }
+  tensor_fence_before();
+  __syncthreads();
+  tensor_fence_after();
+  if (warp < 8) weigh_tiles<E>(a, plan, t, sh, base);
+  else if (warp == 8) copy_tiles(a, plan, t, sh, ring);
+  else multiply_tiles<sizeof(E) == 2 && __is_same(E, __nv_bfloat16)>(a, plan, t, sh, shared_address(base), ring);
+  tensor_fence_before();
+  __syncthreads();
+  tensor_fence_after();
+  if (warp == 9) tensor_free(sh.tensor, kColumns);
+  if (threadIdx.x == 0) t.gave_up[blockIdx.x] = sh.gave_up;
+}
+
+using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                            const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                            CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+Encode encoder() {
+  static const Encode found = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult how;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &how) != cudaSuccess) p = nullptr;
+    return reinterpret_cast<Encode>(p);
+  }();
+  return found;
+}
+
+bool make_map(TensorMap* map, const Vectors& x, const AttendArgs& a) {
+  static_assert(sizeof(TensorMap) == sizeof(CUtensorMap), "a tensor map");
+  const Encode encode = encoder();
+  if (!encode) return false;
+  const auto stride = [&](uint64_t count, int64_t s) { return count > 1 ? (cuuint64_t)s * 2 : (cuuint64_t)(a.dim * 2 + 15) / 16 * 16; };
+  const cuuint64_t size[4] = {a.dim, a.kv_heads, a.prefix_cap, a.prompts};
+  const cuuint64_t strides[3] = {stride(a.kv_heads, x.head), stride(a.prefix_cap, x.token), stride(a.prompts, x.batch)};
+  const cuuint32_t box[4] = {64, 1, kKeys, 1}, step[4] = {1, 1, 1, 1};
+  return encode(reinterpret_cast<CUtensorMap*>(map), a.dtype == BF_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                4, const_cast<void*>(x.data), size, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool copyable(const Vectors& x, const AttendArgs& a) {
+  const auto fits = [](uint64_t count, int64_t s) { return count < 2 || (s > 0 && s % 8 == 0 && s < (1ll << 38)); };
+  return (uintptr_t)x.data % 16 == 0 && fits(a.kv_heads, x.head) && fits(a.prefix_cap, x.token) && fits(a.prompts, x.batch);
+}
+
+}  // namespace
+
+bool tile_takes(const AttendArgs& a) {
+  return tile_might_take(a) && copyable(a.pk, a) && copyable(a.pv, a);
+}
+
+cudaError_t launch_tile(const AttendArgs& a, const AttendPlan& plan, cudaStream_t st) {
+  TileArgs t = {};
+  if (!make_map(&t.k, a.pk, a) || !make_map(&t.v, a.pv, a)) return cudaErrorInvalidValue;
+  t.pair = plan.rows == 2 * kRows;
+  t.chunks = (a.dim + 63) / 64;
+  t.columns = (a.dim + 15) / 16 * 16;
+  t.gave_up = plan.gave_up;
+  const uint32_t tile = t.chunks * kKeys * 128, queries = t.pair ? 2 : 1;
+  t.stages = (227 * 1024 - sizeof(Shared)) / tile - queries;
+  if (t.stages > kMaxStages) t.stages = kMaxStages;
+  const uint32_t shared = (queries + t.stages) * tile + sizeof(Shared);
+  const auto launch = [&](auto kernel) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(plan.parts);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = st;
+    return cudaLaunchKernelEx(&cfg, kernel, a, plan, t);
+  };
+  return a.dtype == BF_BF16 ? launch(tile_kernel<__nv_bfloat16>) : launch(tile_kernel<__half>);
+}
+
+}  // namespace bfk
