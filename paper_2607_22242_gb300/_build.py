@@ -3,7 +3,7 @@
 Each window-width bucket of ``csrc/bf_kernels.cu`` is its own translation unit
 (``-DBF_NW=<slots>``); the units compile in parallel and link with ``bf_tree.cu``
 (the tree search and 32-slot index lists), ``bf_rows.cu`` (once per element type),
-``bf_answers.cu`` and ``bf_embed.cu`` (learning from makespans), ``bf_attend.cu``, ``bf_attend_tile.cu`` and ``bf_beams.cu`` (answering),
+``bf_answers.cu`` and ``bf_embed.cu`` (learning from makespans), ``bf_attend.cu``, ``bf_attend_tile.cu``, ``bf_attend_few.cu`` and ``bf_beams.cu`` (answering),
 ``bf_capi.cu``, ``bf_capi_tree.cu``, ``bf_capi_learn.cu`` and ``bf_capi_answer.cu`` into
 ``paper_2607_22242_gb300/_build/libbf.so`` (CUDA runtime linked statically, so
 the library carries no path to a toolkit; no undefined symbol is allowed).
@@ -98,7 +98,7 @@ def build(force: bool = False, extra_flags=(), verbose: bool = False) -> str:
         obj = os.path.join(BUILD_DIR, f"bf_kernels_nw{nt}.o")
         jobs.append([cc, *ARCH, *NVCC_FLAGS, *extra_flags, f"-DBF_NW={nt}", "-c",
                      os.path.join(CSRC, "bf_kernels.cu"), "-o", obj])
-    for unit in ("bf_tree", "bf_lanetree", "bf_segments", "bf_answers", "bf_embed", "bf_attend", "bf_attend_tile",
+    for unit in ("bf_tree", "bf_lanetree", "bf_segments", "bf_answers", "bf_embed", "bf_attend", "bf_attend_tile", "bf_attend_few",
                  "bf_beams",
                  "bf_capi", "bf_capi_tree", "bf_capi_learn", "bf_capi_answer"):
         jobs.append([cc, *ARCH, *NVCC_FLAGS, *extra_flags, "-c", os.path.join(CSRC, unit + ".cu"), "-o",

@@ -140,11 +140,11 @@ __device__ void piece(const Piece& p, uint32_t rows, uint32_t dim, float* sm) {
     for (uint32_t c = 0; c < S::kOuts; ++c) {
       const uint32_t d = cg + c * S::kCols;
       if (d >= dim) break;
-      p.record[row * dim + d] = o[i][c];
+      p.record[record_place(R, row, d)] = o[i][c];
     }
   }
   if (t < rows) {
-    float2* ml = reinterpret_cast<float2*>(p.record + R * dim);
+    float2* ml = reinterpret_cast<float2*>(p.record + record_sums(R, dim));
     ml[t] = make_float2(ms[t], ls[t]);
   }
   __syncthreads();
@@ -230,18 +230,9 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
   const uint64_t answer = vec / heads;
   const uint32_t h = vec % heads, head = h / a.share, prompt = answer / a.per_prompt;
   const uint32_t row = (answer % a.per_prompt) * a.share + h % a.share;
-  const uint32_t inners = a.kv_heads * plan.row_tiles, inner = head * plan.row_tiles + row / plan.rows;
-  // The blocks that have a piece of the row's segment.
-  const uint64_t total = tiles_before(a, plan.keys, a.prompts) * inners;
-  const uint32_t tiles = (length_of(a.prefix_len, a.prefix_cap, prompt) + plan.keys - 1) / plan.keys;
-  const uint64_t at = tiles_before(a, plan.keys, prompt) * inners + (uint64_t)inner * tiles;
-  uint32_t c0 = 0, c1 = 0;
-  if (tiles) {
-    const uint64_t parts = parts_of(plan, total);
-    c0 = (uint32_t)(((at + 1) * parts - 1) / total);
-    c1 = (uint32_t)(((at + tiles) * parts - 1) / total) + 1;
-  }
-  const uint64_t segment = (uint64_t)prompt * inners + inner;
+  const Owners own = owners_of(a, plan, prompt, head * plan.row_tiles + row / plan.rows);
+  const uint32_t c0 = own.first, c1 = own.last;
+  const uint64_t segment = own.segment;
   const uint32_t splits = a.suffix_cap ? plan.suffix_splits : 0, pieces = c1 - c0 + splits;
   const uint32_t srow = h % a.share;
   const uint64_t sslot = ((answer * a.kv_heads + head) * plan.suffix_row_tiles + srow / plan.suffix_rows) * plan.suffix_splits;
@@ -255,8 +246,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
     r = srow % plan.suffix_rows;
     return plan.suffix + (sslot + (i - (c1 - c0))) * plan.suffix_record;
   };
-  const bool bad = bad_length(a.prefix_len, a.prefix_cap, prompt) || (a.suffix_cap && bad_length(a.suffix_len, a.suffix_cap, answer)) ||
-                   (!a.suffix_cap && a.suffix_len && __ldg(a.suffix_len + answer) != 0);
+  const bool bad = bad_answer(a, prompt, answer);
   wait_for_previous();
   float m = kNone;
   bool odd = bad;
@@ -265,7 +255,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
   for (uint32_t i = lane; i < pieces; i += 32) {
     uint32_t rows, r;
     const float* p = record(i, rows, r);
-    const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + (uint64_t)rows * a.dim) + r);
+    const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + record_sums(rows, a.dim)) + r);
     m = fmaxf(m, ml.x);
     odd |= ml.y != ml.y;
   }
@@ -277,13 +267,13 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
   for (uint32_t i = 0; i < pieces; ++i) {
     uint32_t rows, r;
     const float* p = record(i, rows, r);
-    const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + (uint64_t)rows * a.dim) + r);
+    const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + record_sums(rows, a.dim)) + r);
     const float w = exp2_of(ml.x - base);
     if (!(ml.y > 0.0f)) continue;  // nothing to attend to in this piece: its outputs are 0
     l = fmaf(w, ml.y, l);
 #pragma unroll
     for (uint32_t c = 0; c < kMaxDim / 32; ++c)
-      if (lane + 32 * c < a.dim) o[c] = fmaf(w, __ldcg(p + r * a.dim + lane + 32 * c), o[c]);
+      if (lane + 32 * c < a.dim) o[c] = fmaf(w, __ldcg(p + record_place(rows, r, lane + 32 * c)), o[c]);
   }
   const float nan = __int_as_float(0x7FC00000), inv = odd ? nan : l > 0.0f ? 1.0f / l : 0.0f;
   E* out = static_cast<E*>(const_cast<void*>(a.out.data)) + (int64_t)answer * a.out.batch + (int64_t)h * a.out.head;
@@ -311,8 +301,8 @@ AttendPlan plan_of(const AttendArgs& a, bool tile, void* workspace, uint64_t* by
   uint64_t splits = pieces ? kParts / pieces : 1;
   splits = splits < a.suffix_cap / 128 ? splits : a.suffix_cap / 128;
   p.suffix_splits = splits < 1 ? 1 : (uint32_t)splits;
-  p.record = p.rows * a.dim + 2 * p.rows;
-  p.suffix_record = p.suffix_rows * a.dim + 2 * p.suffix_rows;
+  p.record = record_floats(p.rows, a.dim);
+  p.suffix_record = record_floats(p.suffix_rows, a.dim);
   char* at = static_cast<char*>(workspace);
   const auto take = [&](uint64_t n) {
     char* q = at;
@@ -353,6 +343,7 @@ cudaError_t launch_type(const AttendArgs& a, void* workspace, cudaStream_t st) {
   AttendPlan general = p;
   if (tile) {
     e = launch_tile(a, p, st);
+    if (e == cudaSuccess && few_takes(a)) return launch_few_queries(a, p, st);
     general.parts = 0;
   }
   if (e == cudaSuccess && general.parts + suffix)

@@ -30,8 +30,14 @@ struct AttendPlan {
   uint32_t suffix_rows, suffix_row_tiles, suffix_splits;  // the answers' own keys: pieces of an answer and key head
   float *prefix, *suffix;        // records
   uint32_t* gave_up;             // of the tiled kernel's blocks; nullptr: it does not run
-  uint32_t record, suffix_record;  // floats of a record: rows * dim, then rows (m, l) pairs
+  uint32_t record, suffix_record;  // floats of a record
 };
+
+// A record: the outputs of its rows, four dimensions of all rows after four others (so
+// that a thread to a row writes, and neighbouring rows are read, whole lines), then (m, l) of each row.
+__host__ __device__ __forceinline__ uint32_t record_place(uint32_t rows, uint32_t row, uint32_t d) { return (d / 4 * rows + row) * 4 + d % 4; }
+__host__ __device__ __forceinline__ uint32_t record_sums(uint32_t rows, uint32_t dim) { return (dim + 3) / 4 * 4 * rows; }
+__host__ __device__ __forceinline__ uint32_t record_floats(uint32_t rows, uint32_t dim) { return record_sums(rows, dim) + 2 * rows; }
 
 constexpr float kNone = -__builtin_huge_valf();
 __device__ __forceinline__ float exp2_of(float t) {
@@ -102,5 +108,31 @@ inline bool tile_might_take(const AttendArgs& a) { return a.dtype != BF_F32 && a
 bool tile_takes(const AttendArgs& a);
 constexpr uint32_t kTileKeys = 128, kTileParts = 152;  // a block on each SM
 cudaError_t launch_tile(const AttendArgs& a, const AttendPlan& plan, cudaStream_t st);
+
+// The answers' own keys on few queries each, and the joining of all (bf_attend_few.cu).
+bool few_takes(const AttendArgs& a);
+cudaError_t launch_few_queries(const AttendArgs& a, const AttendPlan& plan, cudaStream_t st);
+
+// The blocks [first, last) that have a piece of a row's prefix segment; by a whole warp.
+struct Owners {
+  uint32_t first, last;
+  uint64_t segment;
+};
+__device__ __forceinline__ Owners owners_of(const AttendArgs& a, const AttendPlan& plan, uint32_t prompt, uint32_t inner) {
+  const uint32_t inners = a.kv_heads * plan.row_tiles;
+  const uint64_t total = tiles_before(a, plan.keys, a.prompts) * inners;
+  const uint32_t tiles = (length_of(a.prefix_len, a.prefix_cap, prompt) + plan.keys - 1) / plan.keys;
+  Owners o = {0, 0, (uint64_t)prompt * inners + inner};
+  if (tiles) {
+    const uint64_t at = tiles_before(a, plan.keys, prompt) * inners + (uint64_t)inner * tiles, parts = parts_of(plan, total);
+    o.first = (uint32_t)(((at + 1) * parts - 1) / total);
+    o.last = (uint32_t)(((at + tiles) * parts - 1) / total) + 1;
+  }
+  return o;
+}
+// Whether an answer's lengths make it NaN.
+__device__ __forceinline__ bool bad_answer(const AttendArgs& a, uint32_t prompt, uint64_t answer) {
+  return bad_length(a.prefix_len, a.prefix_cap, prompt) || bad_length(a.suffix_len, a.suffix_cap, answer);
+}
 
 }  // namespace bfk

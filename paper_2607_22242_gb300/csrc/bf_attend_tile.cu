@@ -24,16 +24,18 @@ namespace bfk {
 namespace {
 
 constexpr uint32_t kKeys = 128, kRows = 128;
-constexpr uint32_t kSoft = 256, kThreads = kSoft + 64;  // softmax threads; then a warp that copies, a warp that multiplies
-constexpr uint32_t kColumns = 512;                      // of tensor memory: S and P of both streams, O of both
+constexpr uint32_t kSoft = 256, kThreads = kSoft + 96;  // softmax threads; a warp that copies, a warp of products for each stream
+// Tensor memory: S of both streams, O of both; with up to 64 dimensions P of both, which otherwise lies where S was.
+constexpr uint32_t kColumns = 512, kOutputs = 256, kWeights = 384;
 constexpr uint32_t kMaxStages = 12;
 constexpr float kRaise = 8.0f;
 
 struct TileArgs {
   TensorMap k, v;
-  uint32_t stages, chunks;  // of the ring of K and V tiles; columns of 64 elements
+  uint32_t stages, chunks;  // of a ring of K and V tiles; columns of 64 elements
   uint32_t columns;         // dimensions, to a multiple of 16
   uint32_t pair;            // 256 queries a block
+  uint32_t apart;           // P has columns of its own
   uint32_t* gave_up;        // one word a block
 };
 
@@ -84,23 +86,22 @@ struct Pieces {
   __device__ __forceinline__ uint32_t first_row() const { return at.inner % plan.row_tiles * plan.rows; }
 };
 
-// The ring of K and V tiles: how many were taken, and so the place and phase of the next.
+// The rings of K and V tiles: one that both streams use whole (256 queries), or one
+// for each stream, in the order K, V, K, V of its tiles.  A barrier tells a phase only
+// from the one before it, so whoever waits for a place's filling must have waited for
+// every filling of that place before: a stream that passed over the other's tiles in a common ring could be a
+// round ahead of a copy that is late, and take what was there before.
 struct Ring {
-  uint32_t stage = 0, phase = 0;
-  __device__ __forceinline__ void step(uint32_t stages) {
-    if (++stage == stages) {
-      stage = 0;
-      phase ^= 1;
-    }
-  }
+  uint32_t stage, phase;
+  // The n-th tile of a ring that begins at place `first`.
+  __device__ __forceinline__ Ring(uint32_t n, uint32_t first, uint32_t stages) : stage(first + n % stages), phase(n / stages & 1) {}
 };
 
-// Tiles in the order in which they are first used: with `lead` steps of scores
-// ahead (2 tiles, or 1 of both streams), K_0 .. K_lead-1, V_0, K_lead, V_1, ...
 __device__ void copy_tiles(const AttendArgs& a, const AttendPlan& plan, const TileArgs& t, Shared& sh, unsigned char* ring) {
-  const uint32_t bytes = t.chunks * kKeys * 128;
-  Ring r;
-  const auto load = [&](const TensorMap& map, uint32_t tile, const Pieces& p) {
+  const uint32_t bytes = t.chunks * kKeys * 128, streams = t.pair ? 1 : 2;
+  uint32_t loads[2] = {0, 0};
+  const auto load = [&](const TensorMap& map, uint32_t tile, uint32_t s, const Pieces& p) {
+    const Ring r(s ? loads[1] : loads[0], s * t.stages, t.stages);
     if (!barrier_wait(&sh.empty[r.stage], r.phase ^ 1, &sh.gave_up)) return false;
     if (threadIdx.x % 32 == 0) {
       barrier_expect(&sh.full[r.stage], bytes);
@@ -109,101 +110,94 @@ __device__ void copy_tiles(const AttendArgs& a, const AttendPlan& plan, const Ti
                  (int32_t)((p.at.tile + tile) * kKeys), (int32_t)p.at.prompt, &sh.full[r.stage]);
     }
     __syncwarp();
-    r.step(t.stages);
+    if (s) ++loads[1];
+    else ++loads[0];
     return true;
   };
-  const uint32_t lead = t.pair ? 1 : 2;
-  uint32_t loads = 0;
   bool ok = true;
-  for (Pieces p(a, plan); ok && p.more(); p.next()) {
-    for (uint32_t i = 0; ok && i < min(lead, p.tiles); ++i) loads += ok = load(t.k, i, p);
-    for (uint32_t i = 0; ok && i < p.tiles; ++i) {
-      loads += ok = load(t.v, i, p);
-      if (ok && i + lead < p.tiles) loads += ok = load(t.k, i + lead, p);
+  for (Pieces p(a, plan); ok && p.more(); p.next())
+    for (uint32_t i = 0; ok && i < p.tiles; i += streams) {
+      for (uint32_t s = 0; ok && s < streams && i + s < p.tiles; ++s) ok = load(t.k, i + s, s, p);
+      for (uint32_t s = 0; ok && s < streams && i + s < p.tiles; ++s) ok = load(t.v, i + s, s, p);
+    }
+  // No copy is in flight when the block ends: the last ones of each ring have arrived.
+  for (uint32_t s = 0; s < streams; ++s) {
+    const uint32_t all = s ? loads[1] : loads[0];
+    for (uint32_t i = all > t.stages ? all - t.stages : 0; i < all; ++i) {
+      const Ring r(i, s * t.stages, t.stages);
+      for (uint32_t n = 0; n < 1u << 22 && !barrier_try(&sh.full[r.stage], r.phase); ++n) {
+      }
     }
   }
-  // No copy is in flight when the block ends: the last `stages` loads have arrived.
-  Ring w;
-  for (uint32_t i = 0; i < loads; ++i, w.step(t.stages))
-    if (i + t.stages >= loads)
-      for (uint32_t n = 0; n < 1u << 22 && !barrier_try(&sh.full[w.stage], w.phase); ++n) {
-      }
 }
 
+// The products of stream s.
 template <bool bf16>
 __device__ void multiply_tiles(const AttendArgs& a, const AttendPlan& plan, const TileArgs& t, Shared& sh, uint32_t q_at,
-                               unsigned char* ring_base) {
-  const uint32_t bytes = t.chunks * kKeys * 128, tensor = sh.tensor, lane = threadIdx.x % 32;
+                               unsigned char* ring_base, uint32_t s) {
+  const uint32_t bytes = t.chunks * kKeys * 128, tensor = uniform(sh.tensor), lane = threadIdx.x % 32;
   const uint32_t ring_at = shared_address(ring_base);
   const uint32_t scores = product_of(bf16, kKeys, false), outputs = product_of(bf16, t.columns, true);
-  Ring r;
-  uint32_t q_phase = 0, p_phase[2] = {0, 0}, o_phase[2] = {0, 0};
+  const uint32_t s_at = tensor + s * 128, o_at = tensor + kOutputs + s * (t.apart ? 64 : 128), p_at = t.apart ? tensor + kWeights + s * 64 : s_at;
+  const uint64_t q = matrix_at(uniform(q_at + (t.pair ? s * t.chunks * kRows * 128 : 0)), 16);
+  uint32_t q_phase = 0, p_phase = 0, o_phase = 0, taken = 0;  // taken: tiles from the stream's ring
+  const uint32_t ring_first = t.pair ? 0 : s * t.stages;
   bool ok = true;
   for (Pieces p(a, plan); ok && p.more(); p.next()) {
     if (!(ok = barrier_wait(&sh.q_full, q_phase, &sh.gave_up))) break;
     q_phase ^= 1;
     tensor_fence_after();
-    const uint32_t steps = t.pair ? 2 * p.tiles : p.tiles;
-    uint32_t k_stage = 0, v_stage = 0;
-    // Takes the next tile from the ring.
-    const auto take = [&](uint32_t& stage) {
-      stage = r.stage;
-      const bool got = barrier_wait(&sh.full[r.stage], r.phase, &sh.gave_up);
-      r.step(t.stages);
-      return got;
-    };
-    const auto score = [&](uint32_t i) {
-      const uint32_t s = i & 1;
-      if (i >= 2) {  // the weights that lie where the scores will have been used
-        if (!barrier_wait(&sh.o_done[s], o_phase[s], &sh.gave_up)) return false;
-        o_phase[s] ^= 1;
-        tensor_fence_after();
+    const uint32_t first = t.pair ? 0 : s, step = t.pair ? 1 : 2;
+    const auto score = [&](bool behind) {
+      const Ring r(taken++, ring_first, t.stages);
+      const uint64_t k = matrix_at(uniform(ring_at + r.stage * bytes), 16);
+      if (!barrier_wait(&sh.full[r.stage], r.phase, &sh.gave_up)) return false;
+      if (behind && !t.apart) {  // the weights that lie where the scores will have been used
+        if (!barrier_wait(&sh.o_done[s], o_phase, &sh.gave_up)) return false;
+        o_phase ^= 1;
       }
-      if ((!t.pair || s == 0) && !take(k_stage)) return false;
-      if (lane == 0) {
-        const uint32_t q = q_at + (t.pair ? s * t.chunks * kRows * 128 : 0), k = ring_at + k_stage * bytes;
-        for (uint32_t d = 0; d < t.columns; d += 16) {
-          const uint32_t off = d / 64 * (kKeys * 128) + d % 64 * 2;
-          multiply(tensor + s * 128, matrix_at(q + off, 16), matrix_at(k + off, 16), scores, d != 0);
-        }
-        tensor_commit(&sh.s_full[s]);
-        if (!t.pair || s == 1) tensor_commit(&sh.empty[k_stage]);
+      tensor_fence_after();
+      for (uint32_t c = 0; c < t.columns; c += 64) {
+        const uint64_t off = c / 64 * (kKeys * 128) / 16;  // of matrix_at's addresses
+        if (t.columns - c >= 64) multiply4(s_at, q + off, k + off, scores, c != 0, 2);
+        else
+          for (uint32_t d = 0; d < t.columns - c; d += 16) multiply(s_at, q + off + d / 8, k + off + d / 8, scores, (c | d) != 0);
       }
-      __syncwarp();
+      tensor_commit(&sh.s_full[s]);
+      tensor_commit(&sh.empty[r.stage]);
       return true;
     };
-    for (uint32_t i = 0; ok && i < min(steps, 2u); ++i) ok = score(i);
-    for (uint32_t i = 0; ok && i < steps; ++i) {
-      const uint32_t s = i & 1, tile = t.pair ? i / 2 : i;
-      const bool fresh = !t.pair || s == 0;
-      if (fresh && !(ok = take(v_stage))) break;
+    if (first < p.tiles) ok = score(false);
+    for (uint32_t tile = first; ok && tile < p.tiles; tile += step) {
+      const Ring r(taken++, ring_first, t.stages);
+      const uint64_t v = matrix_at(uniform(ring_at + r.stage * bytes), kKeys * 128);
+      if (!(ok = barrier_wait(&sh.full[r.stage], r.phase, &sh.gave_up))) break;
       const uint32_t valid = min(kKeys, p.len - (p.at.tile + tile) * kKeys), deep = (valid + 15) / 16 * 16;
-      if (fresh && valid < deep) {  // whatever lies behind the prompt's end is not multiplied, not even by 0
+      if (valid < deep) {  // whatever lies behind the prompt's end is not multiplied, not even by 0 (both streams see to it)
         const uint32_t row = t.chunks * 8;  // pieces of 16 bytes
         for (uint32_t n = lane; n < (deep - valid) * row; n += 32) {
           const uint32_t key = valid + n / row, c = n % row;
-          *reinterpret_cast<uint4*>(ring_base + v_stage * bytes + c / 8 * (kKeys * 128) + key * 128 + c % 8 * 16) =
+          *reinterpret_cast<uint4*>(ring_base + r.stage * bytes + c / 8 * (kKeys * 128) + key * 128 + c % 8 * 16) =
               make_uint4(0, 0, 0, 0);
         }
         fence_to_async();
         __syncwarp();
       }
-      if (!(ok = barrier_wait(&sh.p_full[s], p_phase[s], &sh.gave_up))) break;
-      p_phase[s] ^= 1;
+      if (!(ok = barrier_wait(&sh.p_full[s], p_phase, &sh.gave_up))) break;
+      p_phase ^= 1;
       tensor_fence_after();
-      if (lane == 0) {
-        const uint32_t v = ring_at + v_stage * bytes;
-        for (uint32_t n = 0; n < deep; n += 16)
-          multiply_held(tensor + 256 + s * 128, tensor + s * 128 + n / 2, matrix_at(v + n * 128, kKeys * 128), outputs,
-                        n != 0 || i >= 2);
-        tensor_commit(&sh.o_done[s]);
-        if (!t.pair || s == 1) tensor_commit(&sh.empty[v_stage]);
+      const bool more = tile != first;
+      if (deep == kKeys) {
+        multiply4_held(o_at, p_at, v, outputs, more, 8, 128);
+        multiply4_held(o_at, p_at + 32, v + 512, outputs, true, 8, 128);
+      } else {
+        for (uint32_t n = 0; n < deep; n += 16) multiply_held(o_at, p_at + n / 2, v + n * 8, outputs, n != 0 || more);
       }
-      __syncwarp();
-      if (i + 2 < steps) ok = score(i + 2);
+      tensor_commit(&sh.o_done[s]);
+      tensor_commit(&sh.empty[r.stage]);
+      if (tile + step < p.tiles) ok = score(true);
+      else o_phase ^= 1;  // the last outputs are the softmax threads' to wait for
     }
-    // The last outputs of each stream are the softmax threads' to wait for: these phases pass.
-    for (uint32_t s = 0; s < min(steps, 2u); ++s) o_phase[s] ^= 1;
   }
   // No product is in flight when the block ends; where a wait gave up, one has milliseconds to end.
   if (!ok)
@@ -248,10 +242,34 @@ __device__ __forceinline__ bool any_of_streams(bool say) {
   return any;
 }
 
+// A row's 32 columns from c on of a record, from the row's outputs in tensor memory (two parts of them, weighted).
+template <bool two>
+__device__ __forceinline__ void put_outputs(float* record, uint32_t rows, uint32_t row, bool on, uint32_t dim, uint32_t c, uint32_t at0,
+                                            uint32_t at1, float w0, float w1) {
+  uint32_t o0[32], o1[two ? 32 : 1];
+  tensor_load32(at0 + c, o0);
+  if constexpr (two) {
+    tensor_load32(at1 + c, o1);
+    tensor_wait_load(o1);
+  }
+  tensor_wait_load(o0);
+  if (!on) return;
+#pragma unroll
+  for (uint32_t k = 0; k < 32; k += 4) {
+    if (c + k >= dim) break;
+    float4 v = make_float4(__uint_as_float(o0[k]), __uint_as_float(o0[k + 1]), __uint_as_float(o0[k + 2]), __uint_as_float(o0[k + 3]));
+    if constexpr (two)
+      v = make_float4(fmaf(w1, __uint_as_float(o1[k]), w0 * v.x), fmaf(w1, __uint_as_float(o1[k + 1]), w0 * v.y),
+                      fmaf(w1, __uint_as_float(o1[k + 2]), w0 * v.z), fmaf(w1, __uint_as_float(o1[k + 3]), w0 * v.w));
+    *reinterpret_cast<float4*>(record + record_place(rows, row, c + k)) = v;
+  }
+}
+
 template <typename E>
 __device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const TileArgs& t, Shared& sh, unsigned char* q_to) {
   const uint32_t s = threadIdx.x / kRows, row = threadIdx.x % kRows, lane = threadIdx.x % 32;
-  const uint32_t mine = sh.tensor + (row / 32 * 32 << 16), s_at = mine + s * 128;
+  const uint32_t mine = sh.tensor + (row / 32 * 32 << 16), s_at = mine + s * 128, o_step = t.apart ? 64 : 128;
+  const uint32_t o_at = mine + kOutputs + s * o_step, p_at = t.apart ? mine + kWeights + s * 64 : s_at;
   const float scale = fmaxf(fabsf(a.scale2), 1e-37f);  // 0 would make NaN of masked scores
   const uint32_t rows_all = a.per_prompt * a.share;
   uint32_t s_phase = 0, o_phase = 0;
@@ -269,11 +287,15 @@ __device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const T
     for (uint32_t i = 0; i < steps; ++i) {
       if (!(ok = barrier_wait(&sh.s_full[s], s_phase, &sh.gave_up))) break;
       s_phase ^= 1;
+      if (i) {  // the outputs so far, and the weights' place, are free
+        if (!(ok = barrier_wait(&sh.o_done[s], o_phase, &sh.gave_up))) break;
+        o_phase ^= 1;
+      }
       tensor_fence_after();
       if (warp_on) {
+        float x[kKeys];
         const uint32_t tile = p.at.tile + (t.pair ? i : 2 * i + s), valid = min(kKeys, p.len - tile * kKeys);
         uint32_t raw[kKeys];
-        float x[kKeys];
 #pragma unroll
         for (uint32_t c = 0; c < kKeys; c += 32) tensor_load32(s_at + c, raw + c);
         tensor_wait_load(raw);
@@ -285,7 +307,9 @@ __device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const T
         }
         float top[4] = {kNone, kNone, kNone, kNone};
 #pragma unroll
-        for (uint32_t c = 0; c < kKeys; ++c) top[c % 4] = fmaxf(top[c % 4], x[c]);
+        for (uint32_t c = 0; c < kKeys; c += 8)
+#pragma unroll
+          for (uint32_t k = 0; k < 4; ++k) top[k] = fmaxf(top[k], fmaxf(x[c + k], x[c + k + 4]));
         const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
         float base = m == kNone ? 0.0f : m;
         const bool raise = (now - base) * scale > kRaise || m == kNone;
@@ -297,17 +321,17 @@ __device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const T
           l *= shrink;
           for (uint32_t c = 0; c < t.columns; c += 8) {
             uint32_t o[8];
-            tensor_load8(mine + 256 + s * 128 + c, o);
+            tensor_load8(o_at + c, o);
             tensor_wait_load(o);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) o[k] = __float_as_uint(m == kNone || shrink == 0.0f ? 0.0f : __uint_as_float(o[k]) * shrink);
-            tensor_store8(mine + 256 + s * 128 + c, o);
+            for (int k = 0; k < 8; ++k) o[k] = __float_as_uint(shrink == 0.0f ? 0.0f : __uint_as_float(o[k]) * shrink);
+            tensor_store8(o_at + c, o);
           }
           tensor_wait_store();
         }
         base = m == kNone ? 0.0f : m;
         const float2 scale_2 = make_float2(scale, scale), less = make_float2(-base * scale, -base * scale);
-        float2 sum = make_float2(0.0f, 0.0f);
+        float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
         for (uint32_t half = 0; half < 2; ++half) {
           uint32_t w[32];
@@ -315,12 +339,12 @@ __device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const T
           for (uint32_t c = 0; c < 32; ++c) {
             const float2 e = __ffma2_rn(make_float2(x[half * 64 + 2 * c], x[half * 64 + 2 * c + 1]), scale_2, less);
             const float2 v = make_float2(exp2_of(e.x), exp2_of(e.y));
-            sum = __fadd2_rn(sum, v);
+            sum[c % 2] = __fadd2_rn(sum[c % 2], v);
             w[c] = pack2(v, E());
           }
-          tensor_store32(s_at + half * 32, w);
+          tensor_store32(p_at + half * 32, w);
         }
-        l += sum.x + sum.y;
+        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         tensor_wait_store();
       }
       tensor_fence_before();
@@ -328,50 +352,33 @@ __device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const T
       if (lane == 0) barrier_arrive(&sh.p_full[s]);
     }
     // The piece's outputs: all of this stream's products are done.
-    if (ok && steps) ok = barrier_wait(&sh.o_done[s], (o_phase + steps - 1) & 1, &sh.gave_up);
-    o_phase = (o_phase + steps) & 1;
+    if (ok && steps) {
+      ok = barrier_wait(&sh.o_done[s], o_phase, &sh.gave_up);
+      o_phase ^= 1;
+    }
     float* record = plan.prefix + (uint64_t)(blockIdx.x + (uint64_t)p.at.prompt * p.inners + p.at.inner) * plan.record;
-    sh.sums[s][row] = make_float2(m == kNone ? kNone : m * scale, l);
+    float2* sums = reinterpret_cast<float2*>(record + record_sums(plan.rows, a.dim));
+    const float2 ml = make_float2(m == kNone ? kNone : m * scale, l);
+    sh.sums[s][row] = ml;
     tensor_fence_before();
     asm volatile("bar.sync 1, 256;" ::: "memory");
     tensor_fence_after();
     if (t.pair) {
       if (warp_on)
-        for (uint32_t c = 0; c < a.dim; c += 8) {
-          uint32_t o[8];
-          tensor_load8(mine + 256 + s * 128 + c, o);
-          tensor_wait_load(o);
-          if (my_row < rows) {
-            float4* to = reinterpret_cast<float4*>(record + (uint64_t)my_row * a.dim + c);
-            to[0] = *reinterpret_cast<float4*>(o);
-            to[1] = *reinterpret_cast<float4*>(o + 4);
-          }
-        }
-      if (my_row < rows) reinterpret_cast<float2*>(record + (uint64_t)plan.rows * a.dim)[my_row] = sh.sums[s][row];
+        for (uint32_t c = 0; c < a.dim; c += 32) put_outputs<false>(record, plan.rows, my_row, my_row < rows, a.dim, c, o_at, 0, 1.0f, 0.0f);
+      if (my_row < rows) sums[my_row] = ml;
     } else if (warp_on) {
-      // Both streams' sums of the same queries: each stream's threads join half of the dimensions.
+      // Both streams' outputs of the same queries: each stream's threads join every other 32 dimensions.
       const float2 s0 = sh.sums[0][row], s1 = sh.sums[1][row];
       const bool two = p.tiles > 1;
       const float most = two ? fmaxf(s0.x, s1.x) : s0.x, base = most == kNone ? 0.0f : most;
       const float w0 = exp2_of(s0.x - base), w1 = two ? exp2_of(s1.x - base) : 0.0f;
-      const uint32_t cut = (a.dim / 16 + 1) / 2 * 16 < a.dim ? (a.dim / 16 + 1) / 2 * 16 : a.dim;
-      for (uint32_t c = s ? cut : 0; c < (s ? a.dim : cut); c += 8) {
-        uint32_t o0[8], o1[8] = {};
-        tensor_load8(mine + 256 + c, o0);
-        if (two) tensor_load8(mine + 384 + c, o1);
-        tensor_wait_load(o0);
-        tensor_wait_load(o1);
-        float o[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) o[k] = fmaf(w1, __uint_as_float(o1[k]), w0 * __uint_as_float(o0[k]));
-        if (row < rows) {
-          float4* to = reinterpret_cast<float4*>(record + (uint64_t)row * a.dim + c);
-          to[0] = *reinterpret_cast<float4*>(o);
-          to[1] = *reinterpret_cast<float4*>(o + 4);
-        }
+      const uint32_t at = mine + kOutputs;
+      for (uint32_t c = 32 * s; c < a.dim; c += 64) {
+        if (two) put_outputs<true>(record, plan.rows, row, row < rows, a.dim, c, at, at + o_step, w0, w1);
+        else put_outputs<false>(record, plan.rows, row, row < rows, a.dim, c, at, 0, 1.0f, 0.0f);
       }
-      if (s == 0 && row < rows)
-        reinterpret_cast<float2*>(record + (uint64_t)plan.rows * a.dim)[row] = make_float2(most, fmaf(w1, two ? s1.y : 0.0f, w0 * s0.y));
+      if (s == 0 && row < rows) sums[row] = two ? make_float2(most, fmaf(w1, s1.y, w0 * s0.y)) : s0;
     }
     tensor_fence_before();
     // Both streams have read what the next piece writes over; all of their threads go on, or none.
@@ -384,7 +391,8 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
                                                            const __grid_constant__ TileArgs t) {
   extern __shared__ __align__(1024) unsigned char base[];  // queries, ring, barriers
   unsigned char* ring = base + (t.pair ? 2 : 1) * t.chunks * kRows * 128;
-  Shared& sh = *reinterpret_cast<Shared*>(ring + t.stages * t.chunks * kKeys * 128);
+  const uint32_t places = (t.pair ? 1 : 2) * t.stages;
+  Shared& sh = *reinterpret_cast<Shared*>(ring + places * t.chunks * kKeys * 128);
   const uint32_t warp = threadIdx.x / 32;
   let_next_start();
   if (shared_address(base) % 1024) {  // the swizzle goes by addresses
@@ -392,9 +400,9 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
     return;
   }
   if (threadIdx.x == 0) {
-    for (uint32_t i = 0; i < t.stages; ++i) {
+    for (uint32_t i = 0; i < places; ++i) {
       barrier_init(&sh.full[i], 1);
-      barrier_init(&sh.empty[i], 1);
+      barrier_init(&sh.empty[i], t.pair ? 2 : 1);
     }
     barrier_init(&sh.q_full, kSoft);
     for (uint32_t i = 0; i < 2; ++i) {
@@ -415,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
   tensor_fence_after();
   if (warp < 8) weigh_tiles<E>(a, plan, t, sh, base);
   else if (warp == 8) copy_tiles(a, plan, t, sh, ring);
-  else multiply_tiles<sizeof(E) == 2 && __is_same(E, __nv_bfloat16)>(a, plan, t, sh, shared_address(base), ring);
+  else multiply_tiles<__is_same(E, __nv_bfloat16)>(a, plan, t, sh, shared_address(base), ring, warp - 9);
   tensor_fence_before();
   __syncthreads();
   tensor_fence_after();
@@ -467,11 +475,12 @@ cudaError_t launch_tile(const AttendArgs& a, const AttendPlan& plan, cudaStream_
   t.pair = plan.rows == 2 * kRows;
   t.chunks = (a.dim + 63) / 64;
   t.columns = (a.dim + 15) / 16 * 16;
+  t.apart = a.dim <= 64;
   t.gave_up = plan.gave_up;
   const uint32_t tile = t.chunks * kKeys * 128, queries = t.pair ? 2 : 1;
-  t.stages = (227 * 1024 - sizeof(Shared)) / tile - queries;
-  if (t.stages > kMaxStages) t.stages = kMaxStages;
-  const uint32_t shared = (queries + t.stages) * tile + sizeof(Shared);
+  const uint32_t rings = t.pair ? 1 : 2, fit = (227 * 1024 - sizeof(Shared)) / tile - queries;
+  t.stages = (fit < kMaxStages ? fit : kMaxStages) / rings;
+  const uint32_t shared = (queries + rings * t.stages) * tile + sizeof(Shared);
   const auto launch = [&](auto kernel) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
     if (e != cudaSuccess) return e;

@@ -84,11 +84,19 @@ __device__ __forceinline__ void tensor_wait_load(uint32_t (&r)[N]) {
 }
 __device__ __forceinline__ void tensor_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// The barrier's phase ends when all products issued so far by this thread are done.
+// Products and their ends are issued by one thread of a whole warp, always the same.
+// The warp stays together: where only that thread ran, its operands would have to be
+// moved to the uniform registers one by one (an instruction took 125 cycles, twice
+// what the product does).
+//
+// The barrier's phase ends when all products issued so far are done.
 __device__ __forceinline__ void tensor_commit(uint64_t* barrier) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_address(barrier))
-               : "memory");
+  asm volatile(
+      "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(shared_address(barrier))
+      : "memory");
 }
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(~0u, v, 0); }
 
 // A matrix in shared memory in rows of 128 bytes whose 16-byte pieces are at their
 // place exclusive-or the row's number modulo 8, 8 rows to a kilobyte; `lead`: bytes
@@ -103,15 +111,45 @@ __device__ __forceinline__ constexpr uint32_t product_of(bool bf16, uint32_t col
 }
 __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "{\n\t.reg .pred p, e;\n\tsetp.ne.u32 p, %4, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
       "l"(a), "l"(b), "r"(what), "r"((uint32_t)add)
       : "memory");
 }
 // The same with the first operand in tensor memory.
 __device__ __forceinline__ void multiply_held(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "{\n\t.reg .pred p, e;\n\tsetp.ne.u32 p, %4, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
       "r"(a), "l"(b), "r"(what), "r"((uint32_t)add)
+      : "memory");
+}
+
+// Four products one after the other, `step` apart in both operands (16 bytes each, or columns of the held one):
+// together, because each one's choice of a thread and its branch took longer than its product.
+__device__ __forceinline__ void multiply4(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add, uint64_t step) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "add.u64 a1, %1, %5;\n\tadd.u64 a2, a1, %5;\n\tadd.u64 a3, a2, %5;\n\t"
+      "add.u64 b1, %2, %5;\n\tadd.u64 b2, b1, %5;\n\tadd.u64 b3, b2, %5;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a1, b1, %3, 1;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a2, b2, %3, 1;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a3, b3, %3, 1;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(what), "r"((uint32_t)add), "l"(step)
+      : "memory");
+}
+__device__ __forceinline__ void multiply4_held(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add, uint32_t a_step,
+                                               uint64_t b_step) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t.reg .b32 a1, a2, a3;\n\t.reg .b64 b1, b2, b3;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "add.u32 a1, %1, %5;\n\tadd.u32 a2, a1, %5;\n\tadd.u32 a3, a2, %5;\n\t"
+      "add.u64 b1, %2, %6;\n\tadd.u64 b2, b1, %6;\n\tadd.u64 b3, b2, %6;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a1], b1, %3, 1;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a2], b2, %3, 1;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a3], b3, %3, 1;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(what), "r"((uint32_t)add), "r"(a_step), "l"(b_step)
       : "memory");
 }
 

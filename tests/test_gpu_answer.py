@@ -104,6 +104,39 @@ def test_attention_lengths(dtype, dim, each):
     check_attention(x, dtype, prefix, suffix)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("each,share", [(2, 2), (40, 4), (5, 30)])
+def test_attention_many_tiles(dtype, dim, each, share):
+    """Many tiles of keys and several pieces to each block, of uneven prompts."""
+    rng = np.random.default_rng(dim + each)
+    prompts, kv_heads = 20, 8
+    x = attention_inputs(prompts, each, kv_heads * share, kv_heads, dim, 2500, None, dtype, seed=each)
+    lengths = rng.integers(0, 2501, prompts)
+    lengths[:3] = 2500, 0, 1
+    on = torch.tensor(lengths, device="cuda")
+    out, lse = bf.prefix_attention(*x[:3], prefix_lengths=on, lse=True)
+    q, k, v = (t.double() for t in x[:3])
+    s = torch.einsum("pagsd,ptgd->pagst", q.view(prompts, each, kv_heads, share, dim), k) * dim ** -0.5
+    s = s.masked_fill((torch.arange(2500, device="cuda") >= on[:, None])[:, None, None, None], -INF)
+    top = s.max(-1, keepdim=True).values.clamp(min=-1e300)
+    w = torch.exp(s - top)
+    total = w.sum(-1, keepdim=True)
+    want = torch.einsum("pagst,ptgd->pagsd", w, v) / total.clamp(min=1e-300)
+    size = torch.einsum("pagst,ptgd->pagsd", w, v.abs()) / total.clamp(min=1e-300)
+    out, lse = out.double().view(want.shape), lse.double().view(total.shape)
+    # As check_attention, with the bounds of 2,500 keys and of the largest score and value.
+    most = torch.einsum("pagsd,ptgd->pagst", q.view(prompts, each, kv_heads, share, dim).abs(), k.abs()).max().item() * dim ** -0.5
+    weight = 2 * (dim + 4) * 2.0 ** -24 * most + 2.0 ** -22 + 2.0 ** -17
+    sums = weight + 2516 * 2.0 ** -24
+    tiny = 2500 * 2.0 ** -25 * v.abs().max() + 2.0 ** -25 if dtype == "f16" else 0.0
+    bound = (weight + half(dtype) + sums) * size + tiny + half(dtype) * (1 + 2.0 ** -8) * want.abs()
+    assert ((out - want).abs() <= bound).all()
+    none = total == 0
+    assert not out[none.expand_as(out)].any() and torch.isneginf(lse[none]).all()
+    assert ((lse - top - torch.log(total))[~none].abs() <= sums + 2.0 ** -23 * (most + 20)).all()
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_attention_nothing(dtype):
     x = attention_inputs(2, 3, 4, 2, 64, 10, 4, dtype)
