@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
   const uint64_t answer = vec / heads;
   const uint32_t h = vec % heads, head = h / a.share, prompt = answer / a.per_prompt;
   const uint32_t row = (answer % a.per_prompt) * a.share + h % a.share;
-  const Owners own = owners_of(a, plan, prompt, head * plan.row_tiles + row / plan.rows);
+  const Owners own = owners_of(a, plan, standing_of(a, plan.keys, prompt), prompt, head * plan.row_tiles + row / plan.rows);
   const uint32_t c0 = own.first, c1 = own.last;
   const uint64_t segment = own.segment;
   const uint32_t splits = a.suffix_cap ? plan.suffix_splits : 0, pieces = c1 - c0 + splits;

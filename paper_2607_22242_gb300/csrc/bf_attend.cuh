@@ -113,20 +113,40 @@ cudaError_t launch_tile(const AttendArgs& a, const AttendPlan& plan, cudaStream_
 bool few_takes(const AttendArgs& a);
 cudaError_t launch_few_queries(const AttendArgs& a, const AttendPlan& plan, cudaStream_t st);
 
-// The blocks [first, last) that have a piece of a row's prefix segment; by a whole warp.
+// The blocks [first, last) that have a piece of a row's prefix segment.
 struct Owners {
   uint32_t first, last;
   uint64_t segment;
 };
-__device__ __forceinline__ Owners owners_of(const AttendArgs& a, const AttendPlan& plan, uint32_t prompt, uint32_t inner) {
+// A prompt's tiles among all, by a whole warp: how many there are, and are before it, in one segment of each prompt.
+struct Standing {
+  uint64_t total, before;
+  uint32_t tiles;
+};
+__device__ __forceinline__ Standing standing_of(const AttendArgs& a, uint32_t keys, uint32_t prompt) {
+  uint64_t total = 0, before = 0;
+  uint32_t mine = 0;
+  for (uint32_t i = threadIdx.x % 32; i < a.prompts; i += 32) {
+    const uint32_t n = (length_of(a.prefix_len, a.prefix_cap, i) + keys - 1) / keys;
+    total += n;
+    before += i < prompt ? n : 0;
+    mine += i == prompt ? n : 0;
+  }
+  return {sum_lanes(total), sum_lanes(before), __reduce_add_sync(~0u, mine)};
+}
+__device__ __forceinline__ Owners owners_of(const AttendArgs& a, const AttendPlan& plan, const Standing& s, uint32_t prompt, uint32_t inner) {
   const uint32_t inners = a.kv_heads * plan.row_tiles;
-  const uint64_t total = tiles_before(a, plan.keys, a.prompts) * inners;
-  const uint32_t tiles = (length_of(a.prefix_len, a.prefix_cap, prompt) + plan.keys - 1) / plan.keys;
+  const uint64_t total = s.total * inners;
   Owners o = {0, 0, (uint64_t)prompt * inners + inner};
-  if (tiles) {
-    const uint64_t at = tiles_before(a, plan.keys, prompt) * inners + (uint64_t)inner * tiles, parts = parts_of(plan, total);
-    o.first = (uint32_t)(((at + 1) * parts - 1) / total);
-    o.last = (uint32_t)(((at + tiles) * parts - 1) / total) + 1;
+  if (s.tiles) {
+    const uint64_t at = s.before * inners + (uint64_t)inner * s.tiles, parts = parts_of(plan, total);
+    if (total < 1u << 24 && plan.parts < 256) {
+      o.first = ((uint32_t)(at + 1) * (uint32_t)parts - 1) / (uint32_t)total;
+      o.last = ((uint32_t)(at + s.tiles) * (uint32_t)parts - 1) / (uint32_t)total + 1;
+    } else {
+      o.first = (uint32_t)(((at + 1) * parts - 1) / total);
+      o.last = (uint32_t)(((at + s.tiles) * parts - 1) / total) + 1;
+    }
   }
   return o;
 }

@@ -53,8 +53,8 @@ struct Few {
   static constexpr uint32_t kPitch = DP + 4;
   float o[kWarps][kRows][kPitch];
   float2 sums[kWarps][kRows];
-  float weight[kRows][kMostBlocks * kWarps];
-  float prefix_base[kRows], inverse[kRows];
+  float weight[kRows][kMostBlocks * kWarps + kTileParts];  // of the pieces: the cluster's warps', then the prompt's
+  float inverse[kRows];
 };
 
 template <typename E, uint32_t DP>
@@ -113,6 +113,13 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
     load_k(at);
     load_v(at);
   }
+  // Who has the prompt's pieces (while the keys are on their way); an answer's rows may lie in two tiles of queries.
+  const uint32_t row0 = (uint32_t)(answer - (uint64_t)prompt * a.per_prompt) * a.share + first;
+  const uint32_t tile0 = row0 / plan.rows, rows0 = min(rows, (tile0 + 1) * plan.rows - row0);
+  const Standing standing = standing_of(a, plan.keys, prompt);
+  const Owners own0 = owners_of(a, plan, standing, prompt, head * plan.row_tiles + tile0);
+  const Owners own1 = rows0 == rows ? own0 : owners_of(a, plan, standing, prompt, head * plan.row_tiles + tile0 + 1);
+  const bool bad = bad_answer(a, prompt, answer);
   for (; at < len; at += step) {
     float s[2][4] = {};
 #pragma unroll
@@ -201,43 +208,43 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
   else __syncthreads();
   wait_for_previous();
 
-  // All pieces of a row: of the warps of all blocks here, and of the prompt's.
-  const bool bad = bad_answer(a, prompt, answer);
-  const uint32_t near = few.blocks * kWarps, row0 = (uint32_t)(answer % a.per_prompt) * a.share + first;
+  // The weights of a row's pieces: of the warps of all blocks here, and of the prompt's.
+  const uint32_t near = few.blocks * kWarps;
   const auto peer = [&](uint32_t b) -> Few<E, DP>* { return clustered ? cluster.map_shared_rank(&sh, b) : &sh; };
+  const auto record_of = [&](const Owners& own, uint32_t i) { return plan.prefix + (own.first + i + own.segment) * plan.record; };
   for (uint32_t row = warp; row < rows; row += kWarps) {
-    const uint32_t r = row0 + row;
-    const Owners own = owners_of(a, plan, prompt, head * plan.row_tiles + r / plan.rows);
-    float most = kNone;
+    const Owners own = row < rows0 ? own0 : own1;
+    const uint32_t r = row < rows0 ? row0 - tile0 * plan.rows + row : row - rows0, far = own.last - own.first;
     bool odd = bad;
-    float2 ml = make_float2(kNone, 0.0f);
-    if (lane < near) ml = peer(lane / kWarps)->sums[lane % kWarps][row];
-    most = ml.x;
-    odd |= ml.y != ml.y;
-    const auto sums = [&](uint32_t i) {
-      return __ldcg(reinterpret_cast<const float2*>(plan.prefix + (i + own.segment) * plan.record + record_sums(plan.rows, a.dim)) + r % plan.rows);
-    };
-    for (uint32_t i = own.first + lane; i < own.last; i += 32) {
-      const float2 p = sums(i);
-      most = fmaxf(most, p.x);
-      odd |= p.y != p.y || __ldcg(plan.gave_up + i) != 0;
+    float most = kNone;
+    for (uint32_t i = lane; i < near + far; i += 32) {
+      float2 ml;
+      if (i < near) {
+        ml = peer(i / kWarps)->sums[i % kWarps][row];
+      } else {
+        ml = __ldcg(reinterpret_cast<const float2*>(record_of(own, i - near) + record_sums(plan.rows, a.dim)) + r);
+        odd |= __ldcg(plan.gave_up + own.first + i - near) != 0;
+      }
+      odd |= ml.y != ml.y;
+      most = fmaxf(most, ml.x);
+      sh.weight[row][i] = ml.x;
     }
 #pragma unroll
     for (int d = 16; d; d /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
     const float base = most == kNone ? 0.0f : most;
-    const float mine = exp2_of(ml.x - base);
-    float total = ml.y > 0.0f ? mine * ml.y : 0.0f;
-    if (lane < near) sh.weight[row][lane] = ml.y > 0.0f ? mine : 0.0f;
-    for (uint32_t i = own.first + lane; i < own.last; i += 32) {
-      const float2 p = sums(i);
-      total += p.y > 0.0f ? exp2_of(p.x - base) * p.y : 0.0f;
+    float total = 0.0f;
+    for (uint32_t i = lane; i < near + far; i += 32) {
+      const float l = i < near ? peer(i / kWarps)->sums[i % kWarps][row].y
+                               : __ldcg(reinterpret_cast<const float2*>(record_of(own, i - near) + record_sums(plan.rows, a.dim)) + r).y;
+      const float w = l > 0.0f ? exp2_of(sh.weight[row][i] - base) : 0.0f;  // 0: nothing to attend to in that piece
+      sh.weight[row][i] = w;
+      total = fmaf(w, l > 0.0f ? l : 0.0f, total);
     }
 #pragma unroll
     for (int d = 16; d; d /= 2) total += __shfl_xor_sync(~0u, total, d);
     odd = __any_sync(~0u, odd);
     const float nan = __int_as_float(0x7FC00000);
     if (lane == 0) {
-      sh.prefix_base[row] = base;
       sh.inverse[row] = odd ? nan : total > 0.0f ? 1.0f / total : 0.0f;
       if (a.lse && rank == 0)
         a.lse[answer * ((uint64_t)a.kv_heads * a.share) + head * a.share + first + row] =
@@ -245,38 +252,34 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
     }
   }
   __syncthreads();
-  // Rows of one answer may lie in two tiles of the prompt's queries.
-  const uint32_t tile0 = row0 / plan.rows, tile1 = (row0 + rows - 1) / plan.rows;
-  const Owners own0 = owners_of(a, plan, prompt, head * plan.row_tiles + tile0);
-  const Owners own1 = tile1 == tile0 ? own0 : owners_of(a, plan, prompt, head * plan.row_tiles + tile1);
   // Four dimensions of a row to a thread, neighbouring rows to neighbours; the cluster's blocks share them out.
   const uint32_t quads = a.dim / 4;
   const bool whole = ((uintptr_t)a.out.data | (uint64_t)a.out.batch * 2 | (uint64_t)a.out.head * 2) % 8 == 0;
-  for (uint32_t n = rank * kThreads + threadIdx.x; n - n % 32 < rows * quads; n += few.blocks * kThreads) {
-    const bool on = n < rows * quads;
-    const uint32_t row = on ? n % rows : 0, d = on ? n / rows * 4 : 0, r = row0 + row;
+  for (uint32_t n = rank * kThreads + threadIdx.x; n < rows * quads; n += few.blocks * kThreads) {
+    const uint32_t row = n % rows, d = n / rows * 4;
+    const Owners& own = row < rows0 ? own0 : own1;
+    const uint32_t r = row < rows0 ? row0 - tile0 * plan.rows + row : row - rows0, far = own.last - own.first;
     float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     const auto add = [&](float w, const float4& x) {
-      sum = make_float4(fmaf(w, x.x, sum.x), fmaf(w, x.y, sum.y), fmaf(w, x.z, sum.z), fmaf(w, x.w, sum.w));
+      if (w > 0.0f) sum = make_float4(fmaf(w, x.x, sum.x), fmaf(w, x.y, sum.y), fmaf(w, x.z, sum.z), fmaf(w, x.w, sum.w));
     };
-    const Owners& own = r / plan.rows == row0 / plan.rows ? own0 : own1;
-    const float base = sh.prefix_base[row];
-#pragma unroll 4
-    for (uint32_t i = own.first; i < own.last; ++i) {
-      const float* record = plan.prefix + (i + own.segment) * plan.record;
-      const float2 ml = __ldcg(reinterpret_cast<const float2*>(record + record_sums(plan.rows, a.dim)) + r % plan.rows);
-      const float4 x = __ldcg(reinterpret_cast<const float4*>(record + record_place(plan.rows, r % plan.rows, d)));
-      if (ml.y > 0.0f) add(exp2_of(ml.x - base), x);
+    const float* from = record_of(own, 0) + record_place(plan.rows, r, d);
+    constexpr uint32_t kAhead = 8;
+    for (uint32_t i = 0; i < far; i += kAhead) {
+      float4 x[kAhead];
+#pragma unroll
+      for (uint32_t k = 0; k < kAhead; ++k)
+        if (i + k < far) x[k] = __ldcg(reinterpret_cast<const float4*>(from + (uint64_t)(i + k) * plan.record));
+#pragma unroll
+      for (uint32_t k = 0; k < kAhead; ++k)
+        if (i + k < far) add(sh.weight[row][near + i + k], x[k]);
     }
     for (uint32_t b = 0; b < few.blocks; ++b) {
-      const Few<E, DP>* from = peer(b);
+      const Few<E, DP>* them = peer(b);
 #pragma unroll
-      for (uint32_t w = 0; w < kWarps; ++w) {
-        const float f = sh.weight[row][b * kWarps + w];
-        if (f > 0.0f) add(f, *reinterpret_cast<const float4*>(&from->o[w][row][d]));
-      }
+      for (uint32_t w = 0; w < kWarps; ++w) add(sh.weight[row][b * kWarps + w], *reinterpret_cast<const float4*>(&them->o[w][row][d]));
     }
-    if (on) {
+    {
       const float inv = sh.inverse[row];
       E* out = static_cast<E*>(const_cast<void*>(a.out.data)) + (int64_t)answer * a.out.batch +
                (int64_t)(head * a.share + first + row) * a.out.head + d;

@@ -46,31 +46,70 @@ struct Shared {
   float2 sums[2][kRows];  // (maximum, sum) of the streams
 };
 
-// A block's pieces, in order; the same for all its warps.
+// A block's pieces, in order; the same for all its warps.  Up to 32 prompts, whose
+// lengths a warp holds, are found by one read; divisions are of 32 bits where they can
+// be (the first version, of two reads and 64 bits, took 3,200 cycles of a block's start).
 struct Pieces {
   const AttendArgs& a;
   const AttendPlan& plan;
-  uint32_t inners;
+  uint32_t inners, my_len;
   uint64_t left;
   Place at;
   uint32_t len, tiles;  // the piece's prompt, and its tiles
+  uint32_t head, first_row;
 
   __device__ __forceinline__ Pieces(const AttendArgs& args, const AttendPlan& p)
-      : a(args), plan(p), inners(args.kv_heads * p.row_tiles), left(0), at{0, 0, 0}, len(0), tiles(0) {
-    const uint64_t total = tiles_before(a, kKeys, a.prompts) * inners, parts = parts_of(plan, total);
-    if (blockIdx.x >= parts) return;
-    const uint64_t t0 = total * blockIdx.x / parts, t1 = total * (blockIdx.x + 1) / parts;
-    at = place_of(a, kKeys, inners, t0);
-    left = t1 - t0;
+      : a(args), plan(p), inners(args.kv_heads * p.row_tiles), my_len(0), left(0), at{0, 0, 0}, len(0), tiles(0), head(0), first_row(0) {
+    const uint32_t lane = threadIdx.x % 32;
+    uint64_t t0;
+    if (a.prompts <= 32) {
+      if (lane < a.prompts) my_len = length_of(a.prefix_len, a.prefix_cap, lane);
+      const uint32_t n = (my_len + kKeys - 1) / kKeys;
+      uint32_t upto = n;
+#pragma unroll
+      for (int d = 1; d < 32; d *= 2) {
+        const uint32_t o = __shfl_up_sync(~0u, upto, d);
+        if (lane >= d) upto += o;
+      }
+      const uint64_t total = (uint64_t)__shfl_sync(~0u, upto, 31) * inners;
+      if (!share(total, &t0)) return;
+      const int prompt = __ffs(__ballot_sync(~0u, (uint64_t)upto * inners > t0)) - 1;
+      const uint64_t before = (uint64_t)__shfl_sync(~0u, upto - n, prompt) * inners;
+      const uint32_t mine = __shfl_sync(~0u, n, prompt);
+      const uint64_t in = t0 - before;
+      at.prompt = (uint32_t)prompt;
+      at.inner = in >> 32 ? (uint32_t)(in / mine) : (uint32_t)in / mine;
+      at.tile = (uint32_t)(in - (uint64_t)at.inner * mine);
+    } else {
+      if (!share(tiles_before(a, kKeys, a.prompts) * inners, &t0)) return;
+      at = place_of(a, kKeys, inners, t0);
+    }
     find();
+  }
+  // This block's run of `total` tiles: its first, and how many; false where it has none.
+  __device__ __forceinline__ bool share(uint64_t total, uint64_t* t0) {
+    const uint32_t parts = (uint32_t)parts_of(plan, total);
+    if (blockIdx.x >= parts) return false;
+    uint64_t t1;
+    if (total < 1u << 24 && plan.parts <= 256) {
+      *t0 = (uint32_t)total * blockIdx.x / parts;
+      t1 = (uint32_t)total * (blockIdx.x + 1) / parts;
+    } else {
+      *t0 = total * blockIdx.x / parts;
+      t1 = total * (blockIdx.x + 1) / parts;
+    }
+    left = t1 - *t0;
+    return true;
   }
   __device__ __forceinline__ void find() {
     for (;; ++at.prompt) {
       if (left == 0) return;
-      len = length_of(a.prefix_len, a.prefix_cap, at.prompt);
+      len = a.prompts <= 32 ? __shfl_sync(~0u, my_len, at.prompt) : length_of(a.prefix_len, a.prefix_cap, at.prompt);
       if (len) break;
     }
     tiles = (uint32_t)min((uint64_t)((len + kKeys - 1) / kKeys - at.tile), left);
+    head = plan.row_tiles == 1 ? at.inner : at.inner / plan.row_tiles;
+    first_row = (at.inner - head * plan.row_tiles) * plan.rows;
   }
   __device__ __forceinline__ bool more() const { return left != 0; }
   __device__ __forceinline__ void next() {
@@ -82,8 +121,6 @@ struct Pieces {
     }
     find();
   }
-  __device__ __forceinline__ uint32_t head() const { return at.inner / plan.row_tiles; }
-  __device__ __forceinline__ uint32_t first_row() const { return at.inner % plan.row_tiles * plan.rows; }
 };
 
 // The rings of K and V tiles: one that both streams use whole (256 queries), or one
@@ -92,42 +129,49 @@ struct Pieces {
 // every filling of that place before: a stream that passed over the other's tiles in a common ring could be a
 // round ahead of a copy that is late, and take what was there before.
 struct Ring {
-  uint32_t stage, phase;
-  // The n-th tile of a ring that begins at place `first`.
-  __device__ __forceinline__ Ring(uint32_t n, uint32_t first, uint32_t stages) : stage(first + n % stages), phase(n / stages & 1) {}
+  uint32_t stage, phase, first, end;
+  __device__ __forceinline__ Ring(uint32_t s, const TileArgs& t) : stage(s * t.stages), phase(0), first(stage), end(stage + t.stages) {}
+  __device__ __forceinline__ void step() {
+    if (++stage == end) {
+      stage = first;
+      phase ^= 1;
+    }
+  }
 };
 
 __device__ void copy_tiles(const AttendArgs& a, const AttendPlan& plan, const TileArgs& t, Shared& sh, unsigned char* ring) {
   const uint32_t bytes = t.chunks * kKeys * 128, streams = t.pair ? 1 : 2;
-  uint32_t loads[2] = {0, 0};
-  const auto load = [&](const TensorMap& map, uint32_t tile, uint32_t s, const Pieces& p) {
-    const Ring r(s ? loads[1] : loads[0], s * t.stages, t.stages);
-    if (!barrier_wait(&sh.empty[r.stage], r.phase ^ 1, &sh.gave_up)) return false;
-    if (threadIdx.x % 32 == 0) {
-      barrier_expect(&sh.full[r.stage], bytes);
-      for (uint32_t c = 0; c < t.chunks; ++c)
-        copy_box(ring + r.stage * bytes + c * kKeys * 128, &map, (int32_t)(c * 64), (int32_t)p.head(),
-                 (int32_t)((p.at.tile + tile) * kKeys), (int32_t)p.at.prompt, &sh.full[r.stage]);
-    }
-    __syncwarp();
-    if (s) ++loads[1];
-    else ++loads[0];
-    return true;
-  };
+  Ring rings[2] = {Ring(0, t), Ring(streams - 1, t)};
   bool ok = true;
   for (Pieces p(a, plan); ok && p.more(); p.next())
-    for (uint32_t i = 0; ok && i < p.tiles; i += streams) {
-      for (uint32_t s = 0; ok && s < streams && i + s < p.tiles; ++s) ok = load(t.k, i + s, s, p);
-      for (uint32_t s = 0; ok && s < streams && i + s < p.tiles; ++s) ok = load(t.v, i + s, s, p);
-    }
-  // No copy is in flight when the block ends: the last ones of each ring have arrived.
-  for (uint32_t s = 0; s < streams; ++s) {
-    const uint32_t all = s ? loads[1] : loads[0];
-    for (uint32_t i = all > t.stages ? all - t.stages : 0; i < all; ++i) {
-      const Ring r(i, s * t.stages, t.stages);
-      for (uint32_t n = 0; n < 1u << 22 && !barrier_try(&sh.full[r.stage], r.phase); ++n) {
+    for (uint32_t i = 0; ok && i < p.tiles; i += streams)
+#pragma unroll 1
+      for (uint32_t n = 0; n < 2 * streams; ++n) {  // K of the streams' next tiles, then V
+        const uint32_t s = streams == 2 ? n & 1 : 0, tile = i + s;
+        const bool value = streams == 2 ? n >= 2 : n == 1;
+        if (tile >= p.tiles) continue;
+        Ring r = s ? rings[1] : rings[0];
+        if (!(ok = barrier_wait(&sh.empty[r.stage], r.phase ^ 1, &sh.gave_up))) break;
+        if (threadIdx.x % 32 == 0) {
+          barrier_expect(&sh.full[r.stage], bytes);
+          unsigned char* to = ring + r.stage * bytes;
+          const TensorMap* map = value ? &t.v : &t.k;
+          const int32_t key = (int32_t)((p.at.tile + tile) * kKeys);
+          copy_box(to, map, 0, (int32_t)p.head, key, (int32_t)p.at.prompt, &sh.full[r.stage]);
+          if (t.chunks > 1) copy_box(to + kKeys * 128, map, 64, (int32_t)p.head, key, (int32_t)p.at.prompt, &sh.full[r.stage]);
+        }
+        __syncwarp();
+        r.step();
+        if (s) rings[1] = r;
+        else rings[0] = r;
       }
-    }
+  // No copy is in flight when the block ends: those of each place's last round have
+  // arrived (a place that was never filled is in its first phase, and has nothing to wait for).
+  for (uint32_t s = 0; s < streams; ++s) {
+    Ring r = s ? rings[1] : rings[0];
+    for (uint32_t i = 0; i < t.stages; ++i, r.step())  // the oldest filling of the ring is the next place's
+      for (uint32_t n = 0; n < 1u << 22 && !barrier_try(&sh.full[r.stage], r.phase ^ 1); ++n) {
+      }
   }
 }
 
@@ -140,8 +184,8 @@ __device__ void multiply_tiles(const AttendArgs& a, const AttendPlan& plan, cons
   const uint32_t scores = product_of(bf16, kKeys, false), outputs = product_of(bf16, t.columns, true);
   const uint32_t s_at = tensor + s * 128, o_at = tensor + kOutputs + s * (t.apart ? 64 : 128), p_at = t.apart ? tensor + kWeights + s * 64 : s_at;
   const uint64_t q = matrix_at(uniform(q_at + (t.pair ? s * t.chunks * kRows * 128 : 0)), 16);
-  uint32_t q_phase = 0, p_phase = 0, o_phase = 0, taken = 0;  // taken: tiles from the stream's ring
-  const uint32_t ring_first = t.pair ? 0 : s * t.stages;
+  uint32_t q_phase = 0, p_phase = 0, o_phase = 0;
+  Ring r(t.pair ? 0 : s, t);
   bool ok = true;
   for (Pieces p(a, plan); ok && p.more(); p.next()) {
     if (!(ok = barrier_wait(&sh.q_full, q_phase, &sh.gave_up))) break;
@@ -149,7 +193,6 @@ __device__ void multiply_tiles(const AttendArgs& a, const AttendPlan& plan, cons
     tensor_fence_after();
     const uint32_t first = t.pair ? 0 : s, step = t.pair ? 1 : 2;
     const auto score = [&](bool behind) {
-      const Ring r(taken++, ring_first, t.stages);
       const uint64_t k = matrix_at(uniform(ring_at + r.stage * bytes), 16);
       if (!barrier_wait(&sh.full[r.stage], r.phase, &sh.gave_up)) return false;
       if (behind && !t.apart) {  // the weights that lie where the scores will have been used
@@ -165,11 +208,11 @@ __device__ void multiply_tiles(const AttendArgs& a, const AttendPlan& plan, cons
       }
       tensor_commit(&sh.s_full[s]);
       tensor_commit(&sh.empty[r.stage]);
+      r.step();
       return true;
     };
     if (first < p.tiles) ok = score(false);
     for (uint32_t tile = first; ok && tile < p.tiles; tile += step) {
-      const Ring r(taken++, ring_first, t.stages);
       const uint64_t v = matrix_at(uniform(ring_at + r.stage * bytes), kKeys * 128);
       if (!(ok = barrier_wait(&sh.full[r.stage], r.phase, &sh.gave_up))) break;
       const uint32_t valid = min(kKeys, p.len - (p.at.tile + tile) * kKeys), deep = (valid + 15) / 16 * 16;
@@ -195,6 +238,7 @@ __device__ void multiply_tiles(const AttendArgs& a, const AttendPlan& plan, cons
       }
       tensor_commit(&sh.o_done[s]);
       tensor_commit(&sh.empty[r.stage]);
+      r.step();
       if (tile + step < p.tiles) ok = score(true);
       else o_phase ^= 1;  // the last outputs are the softmax threads' to wait for
     }
@@ -204,30 +248,42 @@ __device__ void multiply_tiles(const AttendArgs& a, const AttendPlan& plan, cons
     for (uint32_t n = 0; n < 1u << 16; ++n) __nanosleep(100);
 }
 
-// A query vector to a thread: rows [first, first + rows) of the prompt's, pieces of 16 bytes where they are aligned.
+// The prompt's query vectors [first_row, ...) of a key head into shared memory, 16 bytes a
+// thread and turn, eight turns' reads on their way; vectors that are not there are 0.
 template <typename E>
 __device__ __forceinline__ void stage_q(const AttendArgs& a, const Pieces& p, const TileArgs& t, unsigned char* to) {
-  const uint32_t rows_all = a.per_prompt * a.share, first = p.first_row(), tile_rows = t.pair ? 2 * kRows : kRows;
-  const uint32_t row_pieces = t.chunks * 8;
+  const uint32_t rows_all = a.per_prompt * a.share, shift = t.chunks > 1 ? 4 : 3;  // pieces of a row: 8 or 16
+  const uint32_t pieces = (t.pair ? 2 * kRows : kRows) << shift;
   const bool aligned = ((uintptr_t)a.q.data | (uint64_t)a.q.batch * 2 | (uint64_t)a.q.head * 2) % 16 == 0;
   const uint32_t flip = a.scale2 < 0.0f ? 0x80008000u : 0u;
-  for (uint32_t n = threadIdx.x; n < tile_rows * row_pieces; n += kSoft) {
-    const uint32_t row = n / row_pieces, c = n % row_pieces, at = first + row;
-    uint4 u = make_uint4(0, 0, 0, 0);
-    if (at < rows_all && c * 8 < a.dim) {
-      const E* q = static_cast<const E*>(a.q.data) + (int64_t)((uint64_t)p.at.prompt * a.per_prompt + at / a.share) * a.q.batch +
-                   (int64_t)(p.head() * a.share + at % a.share) * a.q.head + c * 8;
-      if (aligned) {
-        u = __ldg(reinterpret_cast<const uint4*>(q));
-      } else {
-        const uint16_t* h = reinterpret_cast<const uint16_t*>(q);
-        u = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16,
-                       h[6] | (uint32_t)h[7] << 16);
+  const E* base = static_cast<const E*>(a.q.data) + (int64_t)((uint64_t)p.at.prompt * a.per_prompt) * a.q.batch +
+                  (int64_t)(p.head * a.share) * a.q.head;
+#pragma unroll 1
+  for (uint32_t n0 = threadIdx.x; n0 < pieces; n0 += 8 * kSoft) {
+    uint4 u[8];
+#pragma unroll
+    for (uint32_t k = 0; k < 8; ++k) {
+      const uint32_t n = n0 + k * kSoft, row = n >> shift, c = n & ((1u << shift) - 1), at = p.first_row + row;
+      u[k] = make_uint4(0, 0, 0, 0);
+      if (n < pieces && at < rows_all && c * 8 < a.dim) {
+        const uint32_t answer = at / a.share;
+        const E* q = base + (int64_t)answer * a.q.batch + (int64_t)(at - answer * a.share) * a.q.head + c * 8;
+        if (aligned) {
+          u[k] = __ldg(reinterpret_cast<const uint4*>(q));
+        } else {
+          const uint16_t* h = reinterpret_cast<const uint16_t*>(q);
+          u[k] = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16,
+                            h[6] | (uint32_t)h[7] << 16);
+        }
       }
-      u = make_uint4(u.x ^ flip, u.y ^ flip, u.z ^ flip, u.w ^ flip);
     }
-    const uint32_t r = row % kRows;
-    *reinterpret_cast<uint4*>(to + (row / kRows * t.chunks + c / 8) * (kRows * 128) + r * 128 + (c % 8 ^ r % 8) * 16) = u;
+#pragma unroll
+    for (uint32_t k = 0; k < 8; ++k) {
+      const uint32_t n = n0 + k * kSoft, row = n >> shift, c = n & ((1u << shift) - 1), r = row % kRows;
+      if (n < pieces)
+        *reinterpret_cast<uint4*>(to + (row / kRows * t.chunks + c / 8) * (kRows * 128) + r * 128 + (c % 8 ^ r % 8) * 16) =
+            make_uint4(u[k].x ^ flip, u[k].y ^ flip, u[k].z ^ flip, u[k].w ^ flip);
+    }
   }
 }
 
@@ -242,26 +298,38 @@ __device__ __forceinline__ bool any_of_streams(bool say) {
   return any;
 }
 
-// A row's 32 columns from c on of a record, from the row's outputs in tensor memory (two parts of them, weighted).
-template <bool two>
+// A row's 32 columns from c on of a record, from the row's outputs in tensor memory, or from two weighted parts of them.
 __device__ __forceinline__ void put_outputs(float* record, uint32_t rows, uint32_t row, bool on, uint32_t dim, uint32_t c, uint32_t at0,
-                                            uint32_t at1, float w0, float w1) {
-  uint32_t o0[32], o1[two ? 32 : 1];
+                                            uint32_t at1, bool two, float w0, float w1) {
+  uint32_t o0[32];
   tensor_load32(at0 + c, o0);
-  if constexpr (two) {
+  tensor_wait_load(o0);
+  if (two) {
+    uint32_t o1[32];
     tensor_load32(at1 + c, o1);
     tensor_wait_load(o1);
+#pragma unroll
+    for (uint32_t k = 0; k < 32; ++k) o0[k] = __float_as_uint(fmaf(w1, __uint_as_float(o1[k]), w0 * __uint_as_float(o0[k])));
   }
-  tensor_wait_load(o0);
   if (!on) return;
 #pragma unroll
   for (uint32_t k = 0; k < 32; k += 4) {
     if (c + k >= dim) break;
-    float4 v = make_float4(__uint_as_float(o0[k]), __uint_as_float(o0[k + 1]), __uint_as_float(o0[k + 2]), __uint_as_float(o0[k + 3]));
-    if constexpr (two)
-      v = make_float4(fmaf(w1, __uint_as_float(o1[k]), w0 * v.x), fmaf(w1, __uint_as_float(o1[k + 1]), w0 * v.y),
-                      fmaf(w1, __uint_as_float(o1[k + 2]), w0 * v.z), fmaf(w1, __uint_as_float(o1[k + 3]), w0 * v.w));
-    *reinterpret_cast<float4*>(record + record_place(rows, row, c + k)) = v;
+    *reinterpret_cast<uint4*>(record + record_place(rows, row, c + k)) = make_uint4(o0[k], o0[k + 1], o0[k + 2], o0[k + 3]);
+  }
+}
+
+// 64 scores of a row from column c on; -inf behind the prompt's end.
+__device__ __forceinline__ void load_scores(uint32_t at, uint32_t c, uint32_t valid, float (&x)[64]) {
+  uint32_t raw[64];
+  tensor_load32(at + c, raw);
+  tensor_load32(at + c + 32, raw + 32);
+  tensor_wait_load(raw);
+#pragma unroll
+  for (uint32_t k = 0; k < 64; ++k) x[k] = __uint_as_float(raw[k]);
+  if (c + 64 > valid) {
+#pragma unroll
+    for (uint32_t k = 0; k < 64; ++k) x[k] = c + k < valid ? x[k] : kNone;
   }
 }
 
@@ -278,7 +346,7 @@ __device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const T
     fence_to_async();
     tensor_fence_before();
     barrier_arrive(&sh.q_full);
-    const uint32_t rows = min(plan.rows, rows_all - p.first_row());
+    const uint32_t rows = min(plan.rows, rows_all - p.first_row);
     const uint32_t my_row = t.pair ? s * kRows + row : row;
     const bool warp_on = my_row - lane < rows;  // some of the warp's rows are there
     const uint32_t steps = t.pair ? p.tiles : s < p.tiles ? (p.tiles - s + 1) / 2 : 0;
@@ -293,23 +361,19 @@ __device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const T
       }
       tensor_fence_after();
       if (warp_on) {
-        float x[kKeys];
         const uint32_t tile = p.at.tile + (t.pair ? i : 2 * i + s), valid = min(kKeys, p.len - tile * kKeys);
-        uint32_t raw[kKeys];
-#pragma unroll
-        for (uint32_t c = 0; c < kKeys; c += 32) tensor_load32(s_at + c, raw + c);
-        tensor_wait_load(raw);
-#pragma unroll
-        for (uint32_t c = 0; c < kKeys; ++c) x[c] = __uint_as_float(raw[c]);
-        if (valid < kKeys) {
-#pragma unroll
-          for (uint32_t c = 0; c < kKeys; ++c) x[c] = c < valid ? x[c] : kNone;
-        }
+        // Twice through the scores, 64 at a time, for their maximum and for the weights: reading them
+        // again costs less than holding 128 (spills) and code of twice the length, which a block runs cold at first.
         float top[4] = {kNone, kNone, kNone, kNone};
+#pragma unroll 1
+        for (uint32_t c = 0; c < kKeys; c += 64) {
+          float x[64];
+          load_scores(s_at, c, valid, x);
 #pragma unroll
-        for (uint32_t c = 0; c < kKeys; c += 8)
+          for (uint32_t k = 0; k < 64; k += 8)
 #pragma unroll
-          for (uint32_t k = 0; k < 4; ++k) top[k] = fmaxf(top[k], fmaxf(x[c + k], x[c + k + 4]));
+            for (uint32_t j = 0; j < 4; ++j) top[j] = fmaxf(top[j], fmaxf(x[k + j], x[k + j + 4]));
+        }
         const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
         float base = m == kNone ? 0.0f : m;
         const bool raise = (now - base) * scale > kRaise || m == kNone;
@@ -332,17 +396,19 @@ __device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const T
         base = m == kNone ? 0.0f : m;
         const float2 scale_2 = make_float2(scale, scale), less = make_float2(-base * scale, -base * scale);
         float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-#pragma unroll
-        for (uint32_t half = 0; half < 2; ++half) {
+#pragma unroll 1
+        for (uint32_t c = 0; c < kKeys; c += 64) {
+          float x[64];
           uint32_t w[32];
+          load_scores(s_at, c, valid, x);
 #pragma unroll
-          for (uint32_t c = 0; c < 32; ++c) {
-            const float2 e = __ffma2_rn(make_float2(x[half * 64 + 2 * c], x[half * 64 + 2 * c + 1]), scale_2, less);
+          for (uint32_t k = 0; k < 32; ++k) {
+            const float2 e = __ffma2_rn(make_float2(x[2 * k], x[2 * k + 1]), scale_2, less);
             const float2 v = make_float2(exp2_of(e.x), exp2_of(e.y));
-            sum[c % 2] = __fadd2_rn(sum[c % 2], v);
-            w[c] = pack2(v, E());
+            sum[k % 2] = __fadd2_rn(sum[k % 2], v);
+            w[k] = pack2(v, E());
           }
-          tensor_store32(p_at + half * 32, w);
+          tensor_store32(p_at + c / 2, w);
         }
         l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         tensor_wait_store();
@@ -365,7 +431,7 @@ __device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const T
     tensor_fence_after();
     if (t.pair) {
       if (warp_on)
-        for (uint32_t c = 0; c < a.dim; c += 32) put_outputs<false>(record, plan.rows, my_row, my_row < rows, a.dim, c, o_at, 0, 1.0f, 0.0f);
+        for (uint32_t c = 0; c < a.dim; c += 32) put_outputs(record, plan.rows, my_row, my_row < rows, a.dim, c, o_at, 0, false, 1.0f, 0.0f);
       if (my_row < rows) sums[my_row] = ml;
     } else if (warp_on) {
       // Both streams' outputs of the same queries: each stream's threads join every other 32 dimensions.
@@ -374,10 +440,8 @@ __device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const T
       const float most = two ? fmaxf(s0.x, s1.x) : s0.x, base = most == kNone ? 0.0f : most;
       const float w0 = exp2_of(s0.x - base), w1 = two ? exp2_of(s1.x - base) : 0.0f;
       const uint32_t at = mine + kOutputs;
-      for (uint32_t c = 32 * s; c < a.dim; c += 64) {
-        if (two) put_outputs<true>(record, plan.rows, row, row < rows, a.dim, c, at, at + o_step, w0, w1);
-        else put_outputs<false>(record, plan.rows, row, row < rows, a.dim, c, at, 0, 1.0f, 0.0f);
-      }
+#pragma unroll 1
+      for (uint32_t c = 32 * s; c < a.dim; c += 64) put_outputs(record, plan.rows, row, row < rows, a.dim, c, at, at + o_step, two, w0, w1);
       if (s == 0 && row < rows) sums[row] = two ? make_float2(most, fmaf(w1, s1.y, w0 * s0.y)) : s0;
     }
     tensor_fence_before();

@@ -6,9 +6,9 @@
 // largest logits are all that a group has to look at.  Rows are read once, a
 // chunk of a row to a block (row_kernel); a block leaves its chunk's maximum and
 // sum of exponentials and its `keep` largest logits.  A block per group
-// (group_kernel) joins the sums and chooses.  Ranks that decide are compared in
-// 64 bits, so a group's order is that of the real numbers up to what the 32-bit
-// sums are off by (below 1e-6), and two equal rows tie exactly wherever they lie.
+// (group_kernel) joins the sums and chooses.  Ranks are compared in two 32-bit parts, so
+// a group's order is that of the real numbers up to what the 32-bit sums are off by
+// (below 1e-6), and two equal rows tie exactly wherever they lie.
 #include "bf_answer.h"
 #include "bf_elem.cuh"
 #include "bf_launches.cuh"
@@ -31,10 +31,6 @@ __device__ __forceinline__ uint32_t order_of(float x) {
   return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float from_order(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
-__device__ __forceinline__ uint64_t order_of(double x) {
-  const uint64_t u = (uint64_t)__double_as_longlong(x + 0.0);
-  return u ^ ((uint64_t)((int64_t)u >> 63) | 0x8000000000000000ull);
-}
 constexpr uint32_t kOrderMinusInf = 0x007FFFFFu;
 
 // A continuation that may be among the best: what it is ranked by, and ties.
@@ -56,15 +52,39 @@ __device__ __forceinline__ uint32_t block_count(uint32_t mine, uint32_t* sums) {
   return *sums;
 }
 
-// A bound that at least `keep` of the threads' values reach (keep <= threads), mostly not many more; above -inf.
-__device__ __forceinline__ uint32_t bound_of(uint32_t mine, uint32_t keep) {
+// Bounds that at least `keep` of a block's threads' values reach (keep <= threads), and mostly not many more; above -inf.
+//
+// Where the warps' values are alike: each warp finds its ceil(2 keep / warps)-th
+// largest, and the one of those that enough warps reach is the bound.  One barrier.
+// `warps` holds a word for each warp.
+__device__ __forceinline__ uint32_t bound_of(uint32_t mine, uint32_t keep, uint32_t* warps) {
+  const uint32_t count = blockDim.x / 32, each = min(32u, (2 * keep + count - 1) / count), lane = threadIdx.x % 32;
+  uint32_t most = 0;
+  for (uint32_t i = 0; i < each; ++i) {
+    most = __reduce_max_sync(~0u, mine);
+    if (lane == __ffs(__ballot_sync(~0u, mine == most)) - 1u) mine = 0;
+  }
+  if (lane == 0) warps[threadIdx.x / 32] = most;
+  __syncthreads();
+  // Warps whose values are reached by `each` of theirs: the ceil(keep / each) largest are enough.
+  const uint32_t need = (keep + each - 1) / each, w = lane < count ? warps[lane] : 0;
+  uint32_t above = 0;
+  for (uint32_t i = 0; i < count; ++i) {
+    const uint32_t o = __shfl_sync(~0u, w, i);
+    above += o > w || (o == w && i < lane);
+  }
+  const uint32_t bound = __reduce_max_sync(~0u, lane < count && above == need - 1 ? w : 0);
+  return max(bound, kOrderMinusInf + 1);
+}
+// Where one warp's may be far above another's (beams of different scores): bisection.
+__device__ __forceinline__ uint32_t bound_by_halves(uint32_t mine, uint32_t keep) {
   uint32_t lo = kOrderMinusInf + 1, hi = 0xFFFFFFFFu;
   if ((uint32_t)__syncthreads_count(mine >= lo) <= keep) return lo;
   while (hi - lo > 1) {
     const uint32_t mid = lo + (hi - lo) / 2, n = __syncthreads_count(mine >= mid);
     if (n >= keep) {
       lo = mid;
-      if (n <= keep + keep / 2) break;
+      if (n <= keep + keep / 4) break;
     } else {
       hi = mid;
     }
@@ -118,20 +138,15 @@ __device__ __forceinline__ void rank_list(const Entry<Key>* list, uint32_t n, ui
 
 // ---- rows -------------------------------------------------------------------
 
-struct ChunkHead {
-  float m, s;      // maximum, sum of e^((x - m) / tau)
-  uint32_t count;  // candidates behind it
-  uint32_t pad;
-};
 struct Candidate {
-  float x;
+  float x;  // -inf: none
   uint32_t token;
 };
 
 struct Chunks {
   uint32_t per_row, elements;
-  ChunkHead* heads;   // [rows][per_row]
-  Candidate* best;    // [rows][per_row][keep]
+  float2* heads;    // [rows][per_row]: maximum, sum of e^((x - maximum) / tau)
+  Candidate* best;  // [rows][per_row][keep]
 };
 
 constexpr uint32_t kThreads = 256;
@@ -142,46 +157,43 @@ __device__ __forceinline__ bool is_alive(const BeamArgs& a, uint64_t row) {
 }
 
 // A chunk of a row: V vectors a thread, cut by the row's elements and not by
-// addresses, so that equal rows have equal sums.
-template <typename E, int V>
+// addresses, so that equal rows have equal sums.  kAligned: rows start at 16 bytes.
+template <typename E, int V, bool kAligned>
 __global__ void __launch_bounds__(kThreads) row_kernel(const __grid_constant__ BeamArgs a, const __grid_constant__ Chunks ch) {
   constexpr uint32_t kW = Vec<E>::kWidth;
   __shared__ Entry<uint32_t> list[kList];
-  __shared__ uint32_t count, sums;
+  __shared__ uint32_t count, sums, warp_bound[kThreads / 32];
   __shared__ float warp_max[kThreads / 32], warp_sum[kThreads / 32];
   let_next_start();
-  const uint64_t row = blockIdx.x / ch.per_row;
-  const uint32_t chunk = blockIdx.x % ch.per_row, t = threadIdx.x;
+  const uint32_t row = blockIdx.x / ch.per_row, chunk = blockIdx.x - row * ch.per_row, t = threadIdx.x;
   if (!is_alive(a, row)) return;
   if (t == 0) count = 0;
-  const E* x = static_cast<const E*>(a.x) + row * a.ldx;
-  const Extent matrix(static_cast<const E*>(a.x), (uint64_t)a.groups * a.beams, a.ldx, a.vocab);
-  const uint32_t first = chunk * ch.elements + t * kW;
+  const E* x = static_cast<const E*>(a.x) + (uint64_t)row * a.ldx;
+  const uint32_t cut = chunk * ch.elements, first = cut + t * kW;
   const uint32_t none = minus_inf_bits(E());
   uint4 u[V];
-  {
+  if constexpr (kAligned) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const uint32_t j = first + (uint32_t)k * kThreads * kW;
+      u[k] = make_uint4(none, none, none, none);
+      if (j + kW <= a.vocab) u[k] = __ldcs(reinterpret_cast<const uint4*>(x + j));
+      else if (j < a.vocab) u[k] = load_ends<E>(x + j, 0, (int32_t)(a.vocab - j), none);
+    }
+  } else {
+    const Extent matrix(static_cast<const E*>(a.x), (uint64_t)a.groups * a.beams, a.ldx, a.vocab);
     Unaligned<E> raw[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      const uint64_t j = (uint64_t)first + (uint64_t)k * kThreads * kW;
+      const uint32_t j = first + (uint32_t)k * kThreads * kW;
       if (j < a.vocab) raw[k].load(x, a.vocab, (int64_t)j, matrix);
     }
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      const uint64_t j = (uint64_t)first + (uint64_t)k * kThreads * kW;
+      const uint32_t j = first + (uint32_t)k * kThreads * kW;
       u[k] = make_uint4(none, none, none, none);
-      if (j < a.vocab) {
-        u[k] = raw[k].take();
-        if (j + kW > a.vocab) {  // the row's end
-          uint32_t* w = reinterpret_cast<uint32_t*>(&u[k]);
-#pragma unroll
-          for (uint32_t i = 0; i < kW; ++i)
-            if (j + i >= a.vocab) {
-              if constexpr (sizeof(E) == 4) w[i] = none;
-              else w[i / 2] = i % 2 ? (w[i / 2] & 0xFFFFu) | (none & 0xFFFF0000u) : (w[i / 2] & 0xFFFF0000u) | (none & 0xFFFFu);
-            }
-        }
-      }
+      if (j + kW <= a.vocab) u[k] = raw[k].take();
+      else if (j < a.vocab) u[k] = load_ends<E>(x + j, 0, (int32_t)(a.vocab - j), none);
     }
   }
   const float tmax = max_of<E, V>(u);
@@ -192,24 +204,29 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const __grid_constant__ B
   __syncthreads();
 #pragma unroll
   for (uint32_t w = 0; w < kThreads / 32; ++w) m = fmaxf(m, warp_max[w]);
-  const float base = m == kMinusInf ? 0.0f : m;
-  float s = 0.0f;
+  // (x - m) c2 as x c2 - r, r = m c2 rounded, where that is of ordinary size, and what r is off
+  // by put back into the sum; else (x - m) c2 (rows of the type's lowest values).
+  const bool fits = fabsf(m) * a.c2 < 1024.0f;
+  const float usable = m == kMinusInf ? 0.0f : m, r1 = fits ? -m * a.c2 : 0.0f, rest = fits ? fmaf(-m, a.c2, m * a.c2) : 0.0f;
+  const float2 base = fits ? make_float2(0.0f, 0.0f) : make_float2(-usable, -usable), r = make_float2(r1, r1), c2 = make_float2(a.c2, a.c2);
+  float2 s2 = make_float2(0.0f, 0.0f);
 #pragma unroll
   for (int k = 0; k < V; ++k) {
     float2 f[kW / 2];
     unpack<E>(u[k], f);
-    float part = 0.0f;
 #pragma unroll
-    for (uint32_t i = 0; i < kW / 2; ++i) part += exp2_of((f[i].x - base) * a.c2) + exp2_of((f[i].y - base) * a.c2);
-    s += part;
+    for (uint32_t i = 0; i < kW / 2; ++i) {
+      const float2 e = __ffma2_rn(__fadd2_rn(f[i], base), c2, r);
+      s2 = __fadd2_rn(s2, make_float2(exp2_of(e.x), exp2_of(e.y)));
+    }
   }
+  float s = s2.x + s2.y;
 #pragma unroll
   for (int d = 16; d; d /= 2) s += __shfl_xor_sync(~0u, s, d);
-  if (t % 32 == 0) warp_sum[t / 32] = s;
+  if (t % 32 == 0) warp_sum[t / 32] = fmaf(s, rest * 0.693147180559945309f, s);
   // The candidates: all that reach a bound which `keep` threads' maxima reach.
-  const uint32_t bound = bound_of(order_of(tmax), a.keep);
+  const uint32_t bound = bound_of(order_of(tmax), a.keep, warp_bound);
   const float least = from_order(bound);
-  const uint32_t cut = chunk * ch.elements;
 #pragma unroll
   for (int k = 0; k < V; ++k) {
     if (!(max_of<E, 1>(u + k) >= least)) continue;
@@ -227,16 +244,12 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const __grid_constant__ B
   __syncthreads();
   uint32_t n = count;
   if (n > kList) {
-    const auto each = [&](auto f) {
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        float2 e[kW / 2];
-        unpack<E>(u[k], e);
-#pragma unroll
-        for (uint32_t i = 0; i < kW; ++i) {
-          const float v = i % 2 ? e[i / 2].y : e[i / 2].x;
-          if (v >= least) f(order_of(v), (uint64_t)(first - cut + (uint32_t)k * kThreads * kW + i));
-        }
+    // From memory again: registers that a call takes by reference would be in memory for everybody.
+    const uint32_t some = min(ch.elements, a.vocab - cut);
+    const auto each = [=](auto f) {
+      for (uint32_t i = t; i < some; i += kThreads) {
+        const float v = to_f32(x[cut + i]);
+        if (v >= least) f(order_of(v), (uint64_t)i);
       }
     };
     uint32_t key;
@@ -251,13 +264,14 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const __grid_constant__ B
     __syncthreads();
     n = count;
   }
-  const uint64_t record = row * ch.per_row + chunk;
+  const uint64_t record = (uint64_t)row * ch.per_row + chunk;
   Candidate* best = ch.best + record * a.keep;
   rank_list(list, n, a.keep, [&](uint32_t rank, const Entry<uint32_t>& e) { best[rank] = {from_order(e.key), (uint32_t)e.tie}; });
+  for (uint32_t i = min(n, a.keep) + t; i < a.keep; i += kThreads) best[i] = {kMinusInf, 0};
   if (t == 0) {
     float total = 0.0f;
     for (uint32_t w = 0; w < kThreads / 32; ++w) total += warp_sum[w];
-    ch.heads[record] = {m, total, min(n, a.keep), 0};
+    ch.heads[record] = make_float2(m, total);
   }
 }
 
@@ -265,53 +279,94 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const __grid_constant__ B
 
 enum BeamState : uint32_t { kDead, kAlive, kFinished };
 
-// What a beam's continuations are made from.
+// Numbers in two parts, the second at most half a last place of the first: their
+// order is that of the parts, and 64-bit units are few.
+struct Two {
+  float hi, lo;
+};
+__device__ __forceinline__ Two two_sum(float a, float b) {
+  const float s = a + b, t = s - a;
+  return {s, (a - (s - t)) + (b - t)};
+}
+__device__ __forceinline__ Two quick_two(float a, float b) {  // |a| >= |b|, or either infinite
+  const float s = a + b;
+  return {s, b - (s - a)};
+}
+__device__ __forceinline__ uint64_t order_of(const Two& v) { return (uint64_t)order_of(v.hi) << 32 | order_of(v.lo); }
+// ln v of a normal v as k ln 2 + ln f, f in [3/4, 3/2): Cody and Waite's ln 2 = 355/512 - 2.12e-4.
+__device__ __forceinline__ Two log_of(float v) {
+  const int bits = __float_as_int(v), k = (bits - __float_as_int(0.75f)) >> 23;
+  return quick_two((float)k * 0.693359375f, fmaf((float)k, -2.12194440054690583e-4f, logf(__int_as_float(bits - k * (1 << 23)))));
+}
+
+// What a beam's continuations are made from: total = base + (x - most) / tau, rank = total * weight.
 struct Beam {
-  double score, log_sum, weight;  // total = score + (x - most) / tau - log_sum, rank = total / weight
-  float most;                     // the row's largest logit
-  float base, inv_weight;         // score - log_sum and 1 / weight in 32 bits, for a first choice
+  Two base, weight;  // score - ln sum (a finished beam's score); 1 / max(1, length)^penalty
+  float most;        // the row's largest logit
   uint32_t state;
 };
 
+__device__ __forceinline__ Two total_of(const Beam& b, float x, float tau, float inv_tau) {
+  const float d = x - b.most, z = d * inv_tau;
+  if (!(fabsf(z) < -kMinusInf)) return {z, 0.0f};  // the lowest values under a small temperature
+  const Two s = two_sum(b.base.hi, z);
+  return quick_two(s.hi, s.lo + fmaf(fmaf(-z, tau, d), inv_tau, b.base.lo));
+}
+__device__ __forceinline__ Two times(const Two& a, const Two& b) {
+  const float p = a.hi * b.hi;
+  if (!(fabsf(p) < -kMinusInf)) return {p, 0.0f};
+  return quick_two(p, fmaf(a.hi, b.hi, -p) + (a.hi * b.lo + a.lo * b.hi));
+}
+
+// A group's beams, its list and (kDirect) its logits, in dynamic shared memory.
+__host__ __device__ __forceinline__ uint32_t list_of(uint64_t slots) { return slots < kList ? (uint32_t)slots : kList; }
+__host__ __device__ __forceinline__ uint32_t group_bytes(uint32_t beams, uint64_t slots, uint64_t logits) {
+  return (uint32_t)((beams * sizeof(Beam) + 15) / 16 * 16 + list_of(slots) * sizeof(Entry<uint64_t>) + logits * 4);
+}
+
 template <typename E, bool kDirect>
 __global__ void __launch_bounds__(kThreads) group_kernel(const __grid_constant__ BeamArgs a, const __grid_constant__ Chunks ch) {
-  __shared__ Beam beam[BF_MAX_BEAMS];
-  __shared__ Entry<uint64_t> list[kList];
+  extern __shared__ __align__(16) unsigned char raw[];
   __shared__ uint32_t count, sums, odd;
-  extern __shared__ float logits[];  // kDirect: beams * vocab
-  const uint32_t g = blockIdx.x, t = threadIdx.x, warps = blockDim.x / 32, lane = t % 32;
+  const uint32_t g = blockIdx.x, t = threadIdx.x, warps = blockDim.x / 32, warp = t / 32, lane = t % 32;
+  const uint32_t row_slots = kDirect ? a.vocab : ch.per_row * a.keep, slots = a.beams * row_slots, most_listed = list_of(slots);
+  Beam* beam = reinterpret_cast<Beam*>(raw);
+  Entry<uint64_t>* list = reinterpret_cast<Entry<uint64_t>*>(raw + (a.beams * sizeof(Beam) + 15) / 16 * 16);
+  float* logits = reinterpret_cast<float*>(list + most_listed);
   const uint64_t row0 = (uint64_t)g * a.beams;
-  const double inv_tau = 1.0 / (double)a.tau;
+  const float inv_tau = 1.0f / a.tau;
   if (t == 0) count = odd = 0;
+  // Lanes to a row of logits: as many as a short row has.
+  const uint32_t row_lanes = row_slots >= 32 ? 32 : 1u << (31 - __clz(row_slots)), row_warps = warps * (32 / row_lanes);
+  const uint32_t my_row = t / row_lanes, my_lane = t % row_lanes;
   if constexpr (kDirect) {
-    for (uint32_t i = t; i < a.beams * a.vocab; i += blockDim.x)
-      logits[i] = to_f32(static_cast<const E*>(a.x)[(row0 + i / a.vocab) * a.ldx + i % a.vocab]);
+    for (uint32_t b = my_row; b < a.beams; b += row_warps)
+      for (uint32_t j = my_lane; j < a.vocab; j += row_lanes)
+        logits[b * a.vocab + j] = to_f32(static_cast<const E*>(a.x)[(row0 + b) * a.ldx + j]);
   } else {
     wait_for_previous();
   }
   __syncthreads();
-  // The beams' sums: a warp to a beam, or a thread where rows are short.
+  // The beams' maxima and sums: a warp to a beam, or a thread where rows are short.
   const bool by_thread = kDirect && a.vocab <= 16;
-  const uint32_t lanes = by_thread ? 1 : 32;
-  for (uint32_t b = by_thread ? t : t / 32; b < a.beams; b += by_thread ? blockDim.x : warps) {
-    const uint64_t row = row0 + b;
-    const float score = __ldg(a.scores + row);
-    const uint32_t state = score == kMinusInf ? kDead : a.finished && __ldg(a.finished + row) ? kFinished : kAlive;
+  for (uint32_t b = by_thread ? t : warp; b < a.beams; b += by_thread ? blockDim.x : warps) {
+    const float score = __ldg(a.scores + row0 + b);
+    const uint32_t state = score == kMinusInf ? kDead : a.finished && __ldg(a.finished + row0 + b) ? kFinished : kAlive;
     float m = kMinusInf, s = 0.0f;
     if (state == kAlive) {
-      const uint32_t n = kDirect ? a.vocab : ch.per_row, mine = by_thread ? 0 : lane;
-      const ChunkHead* heads = ch.heads + row * ch.per_row;
-      for (uint32_t i = mine; i < n; i += lanes) m = fmaxf(m, kDirect ? logits[b * a.vocab + i] : __ldcg(&heads[i].m));
+      const uint32_t n = kDirect ? a.vocab : ch.per_row, mine = by_thread ? 0 : lane, step = by_thread ? 1 : 32;
+      const float2* heads = ch.heads + (row0 + b) * ch.per_row;
+      for (uint32_t i = mine; i < n; i += step) m = fmaxf(m, kDirect ? logits[b * a.vocab + i] : __ldca(heads + i).x);
       if (!by_thread)
 #pragma unroll
         for (int d = 16; d; d /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
       const float base = m == kMinusInf ? 0.0f : m;
-      for (uint32_t i = mine; i < n; i += lanes) {
+      for (uint32_t i = mine; i < n; i += step) {
         if constexpr (kDirect) {
-          s += expf((logits[b * a.vocab + i] - base) * (float)inv_tau);
+          s += expf((logits[b * a.vocab + i] - base) * inv_tau);
         } else {
-          const float part = __ldcg(&heads[i].s);
-          s += part == 0.0f ? 0.0f : part * expf((__ldcg(&heads[i].m) - base) * (float)inv_tau);
+          const float2 part = __ldca(heads + i);
+          s += part.y == 0.0f ? 0.0f : part.y * expf((part.x - base) * inv_tau);
         }
       }
       if (!by_thread)
@@ -319,90 +374,80 @@ __global__ void __launch_bounds__(kThreads) group_kernel(const __grid_constant__
         for (int d = 16; d; d /= 2) s += __shfl_xor_sync(~0u, s, d);
     }
     if (by_thread || lane == 0) {
-      Beam o = {};
+      Beam o;
       o.state = state == kAlive && m == kMinusInf && s == s ? (uint32_t)kDead : state;
-      o.score = (double)score;
-      o.log_sum = o.state == kAlive ? log((double)s) : 0.0;
       o.most = o.state == kAlive ? m : 0.0f;
-      o.weight = 1.0;
-      if (a.penalty != 0.0f) {
-        const int64_t n = __ldg(a.lengths + row) + (o.state == kAlive);
-        o.weight = pow((double)(n < 1 ? 1 : n), (double)a.penalty);
+      o.base = {score, 0.0f};
+      if (o.state == kAlive) {
+        const Two l = log_of(s);
+        const Two d = two_sum(score, -l.hi);
+        o.base = quick_two(d.hi, d.lo - l.lo);
       }
-      o.base = (float)(o.score - o.log_sum);
-      o.inv_weight = (float)(1.0 / o.weight);
+      o.weight = {1.0f, 0.0f};
       beam[b] = o;
       if (score != score || score == -kMinusInf || s != s) odd = 1;
     }
   }
   __syncthreads();
+  if (a.penalty != 0.0f) {  // a thread to a beam: these are of 64 bits
+    for (uint32_t b = t; b < a.beams; b += blockDim.x) {
+      const int64_t n = __ldg(a.lengths + row0 + b) + (beam[b].state != kFinished);
+      const double w = pow((double)(n < 1 ? 1 : n), -(double)a.penalty);
+      const float hi = (float)w;
+      beam[b].weight = {hi, (float)(w - (double)hi)};
+    }
+    __syncthreads();
+  }
   // All candidates of a thread: f(beam, token, x), x the logit (0 for a finished beam).
-  const uint32_t row_slots = kDirect ? a.vocab : ch.per_row * a.keep, slots = a.beams * row_slots;
   const auto each = [&](auto f) {
-    for (uint32_t i = t; i < slots; i += blockDim.x) {
-      const uint32_t b = i / row_slots, j = i % row_slots;
+    for (uint32_t b = my_row; b < a.beams; b += row_warps) {
       const uint32_t state = beam[b].state;
       if (state == kAlive) {
-        if constexpr (kDirect) {
-          const float x = logits[i];
-          if (x > kMinusInf) f(b, j, x);
-        } else {
-          const uint64_t record = (row0 + b) * ch.per_row + j / a.keep;
-          if (j % a.keep < __ldcg(&ch.heads[record].count)) {
-            const uint2 c = __ldcg(reinterpret_cast<const uint2*>(ch.best + record * a.keep + j % a.keep));
-            f(b, c.y, __uint_as_float(c.x));
+#pragma unroll 4
+        for (uint32_t j = my_lane; j < row_slots; j += row_lanes) {
+          if constexpr (kDirect) {
+            const float x = logits[b * a.vocab + j];
+            if (x > kMinusInf) f(b, j, x);
+          } else {
+            const uint2 c = __ldca(reinterpret_cast<const uint2*>(ch.best) + (row0 + b) * row_slots + j);
+            if (__uint_as_float(c.x) > kMinusInf) f(b, c.y, __uint_as_float(c.x));
           }
         }
-      } else if (state == kFinished && j == 0) {
-        f(b, (uint32_t)0, 0.0f);
+      } else if (state == kFinished && my_lane == 0) {
+        f(b, 0u, 0.0f);
       }
     }
   };
-  // A first choice in 32 bits: a rank lies within `off` of `about`.
-  const auto near = [&](uint32_t b, float x, float& about, float& off) {
-    const Beam& o = beam[b];
-    const float z = (x - o.most) * (float)inv_tau;
-    about = (o.base + z) * o.inv_weight;
-    off = 1e-6f * (fabsf(o.base) + fabsf(z) + 1e-30f) * o.inv_weight;
-  };
   const auto key_of = [&](uint32_t b, float x) {
     const Beam& o = beam[b];
-    const double total = o.state == kFinished ? o.score : o.score + (((double)x - (double)o.most) * inv_tau - o.log_sum);
-    return order_of(total / o.weight);
+    const Two total = o.state == kFinished ? o.base : total_of(o, x, a.tau, inv_tau);
+    return order_of(a.penalty != 0.0f ? times(total, o.weight) : total);
   };
-  // Equal in 64 bits: the lower beam, in it the larger logit, then the lower token (8, 32 and 24 bits).
+  // Equal in both parts: the lower beam, in it the larger logit, then the lower token (8, 32 and 24 bits).
   const auto tie_of = [](uint32_t b, float x, uint32_t token) { return (uint64_t)b << 56 | (uint64_t)~order_of(x) << 24 | token; };
   uint32_t n = 0;
   if (!odd) {
-    float least = kMinusInf;
+    uint64_t least = 0;
     if (slots > 2 * a.keep && slots > 128 && a.keep <= blockDim.x) {
-      uint32_t most = kOrderMinusInf;
-      each([&](uint32_t b, uint32_t, float x) {
-        float about, off;
-        near(b, x, about, off);
-        const float low = about - off;
-        most = max(most, low == low ? order_of(low) : kOrderMinusInf);
-      });
-      const uint32_t bound = bound_of(most, a.keep);
-      least = bound == kOrderMinusInf + 1 ? kMinusInf : from_order(bound);
+      uint32_t most = 0;
+      each([&](uint32_t b, uint32_t, float x) { most = max(most, (uint32_t)(key_of(b, x) >> 32)); });
+      const uint32_t bound = bound_by_halves(most, a.keep);
+      least = bound == kOrderMinusInf + 1 ? 0 : (uint64_t)bound << 32;
     }
-    const auto reaches = [&](uint32_t b, float x) {
-      float about, off;
-      near(b, x, about, off);
-      return !(about + off < least);
-    };
     each([&](uint32_t b, uint32_t token, float x) {
-      if (reaches(b, x)) {
+      const uint64_t key = key_of(b, x);
+      if (key >= least) {
         const uint32_t at = atomicAdd(&count, 1u);
-        if (at < kList) list[at] = {key_of(b, x), tie_of(b, x, token)};
+        if (at < most_listed) list[at] = {key, tie_of(b, x, token)};
       }
     });
     __syncthreads();
     n = count;
-    if (n > kList) {
+    if (n > most_listed) {
       const auto each_key = [&](auto f) {
         each([&](uint32_t b, uint32_t token, float x) {
-          if (reaches(b, x)) f(key_of(b, x), tie_of(b, x, token));
+          const uint64_t key = key_of(b, x);
+          if (key >= least) f(key, tie_of(b, x, token));
         });
       };
       uint64_t key, tie;
@@ -423,9 +468,7 @@ __global__ void __launch_bounds__(kThreads) group_kernel(const __grid_constant__
     const Beam& o = beam[b];
     const bool was = o.state == kFinished;
     const int64_t token = was ? a.end_token : (int64_t)(e.tie & 0xFFFFFFu);
-    // The total back from the rank: exact where nothing is weighted.
-    const uint64_t bits = e.key & 0x8000000000000000ull ? e.key ^ 0x8000000000000000ull : ~e.key;
-    a.out_scores[out + rank] = was ? (float)o.score : (float)(__longlong_as_double((long long)bits) * o.weight);
+    a.out_scores[out + rank] = was ? o.base.hi : total_of(o, from_order(~(uint32_t)(e.tie >> 24)), a.tau, inv_tau).hi;
     a.out_tokens[out + rank] = token;
     a.out_parents[out + rank] = (int64_t)(row0 + b);
     if (a.out_finished) a.out_finished[out + rank] = was || token == a.end_token;
@@ -442,18 +485,21 @@ __global__ void __launch_bounds__(kThreads) group_kernel(const __grid_constant__
 
 constexpr uint64_t kDirectMost = 4096;  // logits of a group that one block takes as they are
 
-Chunks chunks_of(uint32_t groups, uint32_t beams, uint64_t vocab, uint32_t keep, uint32_t width, void* workspace, int* vectors,
-                 uint64_t* bytes) {
+// How rows are cut: 8 vectors a thread (4 where each is put together from two), 2
+// where there are too few blocks for two on each of 152 SMs.
+Chunks chunks_of(uint32_t groups, uint32_t beams, uint64_t vocab, uint32_t keep, uint32_t width, bool aligned, void* workspace,
+                 uint32_t* vectors, uint64_t* bytes) {
   Chunks c = {};
   *bytes = 0;
   if (beams * vocab <= kDirectMost) return c;
   const uint64_t rows = (uint64_t)groups * beams;
-  const auto per_row = [&](int v) { return (vocab + kThreads * v * width - 1) / (kThreads * v * width); };
-  *vectors = rows * per_row(8) < 304 ? 2 : 8;
+  const auto per_row = [&](uint32_t v) { return (vocab + kThreads * v * width - 1) / (kThreads * v * width); };
+  *vectors = aligned ? 8 : 4;
+  if (rows * per_row(*vectors) < 304) *vectors = 2;
   c.per_row = (uint32_t)per_row(*vectors);
   c.elements = kThreads * *vectors * width;
-  c.heads = static_cast<ChunkHead*>(workspace);
-  const uint64_t records = rows * c.per_row, heads = (records * sizeof(ChunkHead) + 255) / 256 * 256;
+  c.heads = static_cast<float2*>(workspace);
+  const uint64_t records = rows * c.per_row, heads = (records * sizeof(float2) + 255) / 256 * 256;
   c.best = reinterpret_cast<Candidate*>(static_cast<char*>(workspace) + heads);
   *bytes = heads + records * keep * sizeof(Candidate);
   return c;
@@ -461,25 +507,36 @@ Chunks chunks_of(uint32_t groups, uint32_t beams, uint64_t vocab, uint32_t keep,
 
 template <typename E>
 cudaError_t launch_step(const BeamArgs& a, void* workspace, cudaStream_t st) {
-  int vectors = 0;
+  uint32_t vectors = 0;
   uint64_t bytes = 0;
-  const Chunks c = chunks_of(a.groups, a.beams, a.vocab, a.keep, Vec<E>::kWidth, workspace, &vectors, &bytes);
-  if (!c.per_row) {
+  const bool aligned = ((uintptr_t)a.x | (a.ldx * sizeof(E))) % 16 == 0;
+  const Chunks c = chunks_of(a.groups, a.beams, a.vocab, a.keep, Vec<E>::kWidth, aligned, workspace, &vectors, &bytes);
+  const bool direct = c.per_row == 0;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute after;
+  cfg.gridDim = dim3(a.groups);
+  cfg.stream = st;
+  cfg.attrs = &after;
+  if (direct) {
     const uint32_t n = a.beams * a.vocab;
     uint32_t threads = (n / 2 + 31) / 32 * 32;
     threads = threads < 32 ? 32 : threads > kThreads ? kThreads : threads;
     if (threads < a.keep && n > 128) threads = (a.keep + 31) / 32 * 32;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(a.groups);
     cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = n * sizeof(float);
-    cfg.stream = st;
+    cfg.dynamicSmemBytes = group_bytes(a.beams, n, n);
     return cudaLaunchKernelEx(&cfg, group_kernel<E, true>, a, c);
   }
   const uint64_t blocks = (uint64_t)a.groups * a.beams * c.per_row;
-  const cudaError_t e = vectors == 8 ? launch_plain(row_kernel<E, 8>, blocks, kThreads, st, a, c)
-                                     : launch_plain(row_kernel<E, 2>, blocks, kThreads, st, a, c);
-  return e == cudaSuccess ? launch_after(group_kernel<E, false>, a.groups, kThreads, st, a, c) : e;
+  const auto rows = [&](auto kernel) { return launch_plain(kernel, blocks, kThreads, st, a, c); };
+  const cudaError_t e = aligned ? (vectors == 8 ? rows(row_kernel<E, 8, true>) : rows(row_kernel<E, 2, true>))
+                                : (vectors == 4 ? rows(row_kernel<E, 4, false>) : rows(row_kernel<E, 2, false>));
+  if (e != cudaSuccess) return e;
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = group_bytes(a.beams, (uint64_t)a.beams * c.per_row * a.keep, 0);
+  after.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  after.val.programmaticStreamSerializationAllowed = 1;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, group_kernel<E, false>, a, c);
 }
 
 // ---- states -----------------------------------------------------------------
@@ -601,10 +658,10 @@ cudaError_t launch_units(const ReorderArgs& a, bool flat, cudaStream_t st) {
 
 uint64_t beam_bytes(uint32_t groups, uint32_t beams, uint64_t vocab, uint32_t keep) {
   uint64_t most = 256;
-  for (uint32_t width = 4; width <= 8; width *= 2) {  // elements of 16 bytes
-    int vectors;
+  for (uint32_t i = 0; i < 4; ++i) {  // 4 or 8 elements in 16 bytes, aligned or not
+    uint32_t vectors;
     uint64_t bytes;
-    chunks_of(groups, beams, vocab, keep, width, nullptr, &vectors, &bytes);
+    chunks_of(groups, beams, vocab, keep, i % 2 ? 4 : 8, i / 2, nullptr, &vectors, &bytes);
     if (bytes > most) most = bytes;
   }
   return (most + 255) / 256 * 256;
