@@ -10,6 +10,7 @@
 // a group's order is that of the real numbers up to what the 32-bit sums are off by
 // (below 1e-6), and two equal rows tie exactly wherever they lie.
 #include "bf_answer.h"
+#include "bf_blackwell.cuh"
 #include "bf_elem.cuh"
 #include "bf_launches.cuh"
 
@@ -144,7 +145,7 @@ struct Candidate {
 };
 
 struct Chunks {
-  uint32_t per_row, elements;
+  uint32_t per_row, elements, tiles;
   float2* heads;    // [rows][per_row]: maximum, sum of e^((x - maximum) / tau)
   Candidate* best;  // [rows][per_row][keep]
 };
@@ -156,100 +157,156 @@ __device__ __forceinline__ bool is_alive(const BeamArgs& a, uint64_t row) {
   return !(score == kMinusInf) && !(a.finished && __ldg(a.finished + row));
 }
 
-// A chunk of a row: V vectors a thread, cut by the row's elements and not by
-// addresses, so that equal rows have equal sums.  kAligned: rows start at 16 bytes.
+// The largest element of a vector, as one word: of 32 bits, or of either half.
+__device__ __forceinline__ uint32_t most_of(const uint4& u, float) {
+  return __float_as_uint(fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w))));
+}
+template <typename E2>
+__device__ __forceinline__ uint32_t most_of_pairs(const uint4& u) {
+  const auto pair = [](uint32_t v) { return *reinterpret_cast<const E2*>(&v); };
+  const E2 m = __hmax2(__hmax2(pair(u.x), pair(u.y)), __hmax2(pair(u.z), pair(u.w)));
+  return *reinterpret_cast<const uint32_t*>(&m);
+}
+__device__ __forceinline__ uint32_t most_of(const uint4& u, __nv_bfloat16) { return most_of_pairs<__nv_bfloat162>(u); }
+__device__ __forceinline__ uint32_t most_of(const uint4& u, __half) { return most_of_pairs<__half2>(u); }
+__device__ __forceinline__ float value_of(uint32_t word, float) { return __uint_as_float(word); }
+template <typename E>
+__device__ __forceinline__ float value_of(uint32_t word, E) {
+  const float2 f = unpack2(word, E());
+  return fmaxf(f.x, f.y);
+}
+constexpr uint32_t kHits = 256;  // vectors of a chunk that have a candidate
+
+// The exponentials of V vectors against m, summed.  (x - m) c2 as x c2 - r, r = m c2
+// rounded, and what r is off by put back into the sum; where m c2 is far from ordinary
+// (nothing but the type's lowest values, a very small temperature), as it stands.
+template <typename E, int V, bool fits>
+__device__ __forceinline__ float sum_of(const uint4 (&u)[V], float m, float c2) {
+  const float r = fits ? -m * c2 : 0.0f, base = m == kMinusInf ? 0.0f : -m;
+  float2 s2 = make_float2(0.0f, 0.0f);
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    float2 f[Vec<E>::kWidth / 2];
+    unpack<E>(u[k], f);
+#pragma unroll
+    for (uint32_t i = 0; i < Vec<E>::kWidth / 2; ++i) {
+      if (!fits) f[i] = __fadd2_rn(f[i], make_float2(base, base));
+      const float2 e = __ffma2_rn(f[i], make_float2(c2, c2), make_float2(r, r));
+      s2 = __fadd2_rn(s2, make_float2(exp2_of(e.x), exp2_of(e.y)));
+    }
+  }
+  const float s = s2.x + s2.y, rest = fits ? fmaf(-m, c2, m * c2) * 0.693147180559945309f : 0.0f;
+  return fmaf(s, rest, s);
+}
+
+// A chunk of a row, `tiles` times V vectors a thread, cut by the row's elements and not
+// by addresses, so that equal rows have equal sums.  kAligned: rows start at 16 bytes.
+// What reaches a bound that `keep` of the threads' maxima in the first tile reach may be
+// among the chunk's best: a few more than `keep` in each tile.
 template <typename E, int V, bool kAligned>
-__global__ void __launch_bounds__(kThreads) row_kernel(const __grid_constant__ BeamArgs a, const __grid_constant__ Chunks ch) {
+__global__ void __launch_bounds__(kThreads, 4) row_kernel(const __grid_constant__ BeamArgs a, const __grid_constant__ Chunks ch) {
   constexpr uint32_t kW = Vec<E>::kWidth;
-  __shared__ Entry<uint32_t> list[kList];
-  __shared__ uint32_t count, sums, warp_bound[kThreads / 32];
+  __shared__ uint64_t list[kList];  // order of the logit, then of the token the other way round
+  __shared__ uint4 hit[kHits];
+  __shared__ uint32_t hit_token[kHits];
+  __shared__ uint32_t count, hits, sums, warp_bound[kThreads / 32];
   __shared__ float warp_max[kThreads / 32], warp_sum[kThreads / 32];
   let_next_start();
   const uint32_t row = blockIdx.x / ch.per_row, chunk = blockIdx.x - row * ch.per_row, t = threadIdx.x;
   if (!is_alive(a, row)) return;
-  if (t == 0) count = 0;
+  if (t == 0) count = hits = 0;
   const E* x = static_cast<const E*>(a.x) + (uint64_t)row * a.ldx;
-  const uint32_t cut = chunk * ch.elements, first = cut + t * kW;
+  const uint32_t cut = chunk * ch.elements;
   const uint32_t none = minus_inf_bits(E());
-  uint4 u[V];
-  if constexpr (kAligned) {
+  float m = kMinusInf, s = 0.0f, least = 0.0f;
+  uint32_t bound = 0;
+#pragma unroll 1
+  for (uint32_t tile = 0; tile < ch.tiles; ++tile) {
+    const uint32_t first = cut + (tile * V * kThreads + t) * kW;
+    uint4 u[V];
+    if constexpr (kAligned) {
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-      const uint32_t j = first + (uint32_t)k * kThreads * kW;
-      u[k] = make_uint4(none, none, none, none);
-      if (j + kW <= a.vocab) u[k] = __ldcs(reinterpret_cast<const uint4*>(x + j));
-      else if (j < a.vocab) u[k] = load_ends<E>(x + j, 0, (int32_t)(a.vocab - j), none);
-    }
-  } else {
-    const Extent matrix(static_cast<const E*>(a.x), (uint64_t)a.groups * a.beams, a.ldx, a.vocab);
-    Unaligned<E> raw[V];
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-      const uint32_t j = first + (uint32_t)k * kThreads * kW;
-      if (j < a.vocab) raw[k].load(x, a.vocab, (int64_t)j, matrix);
-    }
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-      const uint32_t j = first + (uint32_t)k * kThreads * kW;
-      u[k] = make_uint4(none, none, none, none);
-      if (j + kW <= a.vocab) u[k] = raw[k].take();
-      else if (j < a.vocab) u[k] = load_ends<E>(x + j, 0, (int32_t)(a.vocab - j), none);
-    }
-  }
-  const float tmax = max_of<E, V>(u);
-  float m = tmax;
-#pragma unroll
-  for (int d = 16; d; d /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
-  if (t % 32 == 0) warp_max[t / 32] = m;
-  __syncthreads();
-#pragma unroll
-  for (uint32_t w = 0; w < kThreads / 32; ++w) m = fmaxf(m, warp_max[w]);
-  // (x - m) c2 as x c2 - r, r = m c2 rounded, where that is of ordinary size, and what r is off
-  // by put back into the sum; else (x - m) c2 (rows of the type's lowest values).
-  const bool fits = fabsf(m) * a.c2 < 1024.0f;
-  const float usable = m == kMinusInf ? 0.0f : m, r1 = fits ? -m * a.c2 : 0.0f, rest = fits ? fmaf(-m, a.c2, m * a.c2) : 0.0f;
-  const float2 base = fits ? make_float2(0.0f, 0.0f) : make_float2(-usable, -usable), r = make_float2(r1, r1), c2 = make_float2(a.c2, a.c2);
-  float2 s2 = make_float2(0.0f, 0.0f);
-#pragma unroll
-  for (int k = 0; k < V; ++k) {
-    float2 f[kW / 2];
-    unpack<E>(u[k], f);
-#pragma unroll
-    for (uint32_t i = 0; i < kW / 2; ++i) {
-      const float2 e = __ffma2_rn(__fadd2_rn(f[i], base), c2, r);
-      s2 = __fadd2_rn(s2, make_float2(exp2_of(e.x), exp2_of(e.y)));
-    }
-  }
-  float s = s2.x + s2.y;
-#pragma unroll
-  for (int d = 16; d; d /= 2) s += __shfl_xor_sync(~0u, s, d);
-  if (t % 32 == 0) warp_sum[t / 32] = fmaf(s, rest * 0.693147180559945309f, s);
-  // The candidates: all that reach a bound which `keep` threads' maxima reach.
-  const uint32_t bound = bound_of(order_of(tmax), a.keep, warp_bound);
-  const float least = from_order(bound);
-#pragma unroll
-  for (int k = 0; k < V; ++k) {
-    if (!(max_of<E, 1>(u + k) >= least)) continue;
-    float2 f[kW / 2];
-    unpack<E>(u[k], f);
-#pragma unroll
-    for (uint32_t i = 0; i < kW; ++i) {
-      const float v = i % 2 ? f[i / 2].y : f[i / 2].x;
-      if (v >= least) {
-        const uint32_t at = atomicAdd(&count, 1u);
-        if (at < kList) list[at] = {order_of(v), first + (uint32_t)k * kThreads * kW + i};
+      for (int k = 0; k < V; ++k) {
+        const uint32_t j = first + (uint32_t)k * kThreads * kW;
+        u[k] = make_uint4(none, none, none, none);
+        if (j + kW <= a.vocab) u[k] = __ldcs(reinterpret_cast<const uint4*>(x + j));
+        else if (j < a.vocab) u[k] = load_ends<E>(x + j, 0, (int32_t)(a.vocab - j), none);
       }
+    } else {
+      const Extent matrix(static_cast<const E*>(a.x), (uint64_t)a.groups * a.beams, a.ldx, a.vocab);
+      Unaligned<E> raw[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const uint32_t j = first + (uint32_t)k * kThreads * kW;
+        if (j < a.vocab) raw[k].load(x, a.vocab, (int64_t)j, matrix);
+      }
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const uint32_t j = first + (uint32_t)k * kThreads * kW;
+        u[k] = make_uint4(none, none, none, none);
+        if (j + kW <= a.vocab) u[k] = raw[k].take();
+        else if (j < a.vocab) u[k] = load_ends<E>(x + j, 0, (int32_t)(a.vocab - j), none);
+      }
+    }
+    uint32_t most[V];
+    float tmax = kMinusInf;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      most[k] = most_of(u[k], E());
+      tmax = fmaxf(tmax, value_of(most[k], E()));
+    }
+    // The thread's sum, against its own maximum so far.
+    const float now = fmaxf(m, tmax);
+    if (now > m) s *= m == kMinusInf ? 1.0f : exp2_of((m - now) * a.c2);  // (s is 0, or NaN, before the first number)
+    m = now;
+    s += fabsf(m) * a.c2 < 1024.0f ? sum_of<E, V, true>(u, m, a.c2) : sum_of<E, V, false>(u, m, a.c2);
+    if (tile == 0) {
+      bound = bound_of(order_of(tmax), a.keep, warp_bound);
+      least = from_order(bound);
+    }
+    // First the vectors that have any, then their elements, one to a thread: few threads
+    // have a vector, and a warp that went through its own took twice the instructions.
+    if (tmax >= least) {
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (value_of(most[k], E()) >= least) {
+          const uint32_t at = atomicAdd(&hits, 1u);
+          if (at < kHits) {
+            hit[at] = u[k];
+            hit_token[at] = first + (uint32_t)k * kThreads * kW;
+          }
+        }
+    }
+  }
+  {
+    const float top = from_order(__reduce_max_sync(~0u, order_of(m)));
+    s *= m == top ? 1.0f : exp2_of((m - top) * a.c2);
+#pragma unroll
+    for (int d = 16; d; d /= 2) s += __shfl_xor_sync(~0u, s, d);
+    if (t % 32 == 0) {
+      warp_max[t / 32] = top;
+      warp_sum[t / 32] = s;
+    }
+  }
+  __syncthreads();
+  const uint32_t found = hits;
+  const auto entry_of = [](float v, uint32_t token) { return (uint64_t)order_of(v) << 32 | ~token; };
+  for (uint32_t i = t; i < min(found, kHits) * kW; i += kThreads) {
+    const uint32_t at = i / kW, j = i % kW;
+    const float v = to_f32(reinterpret_cast<const E*>(&hit[at])[j]);
+    if (v >= least) {
+      const uint32_t to = atomicAdd(&count, 1u);
+      if (to < kList) list[to] = entry_of(v, hit_token[at] + j);
     }
   }
   __syncthreads();
   uint32_t n = count;
-  if (n > kList) {
-    // From memory again: registers that a call takes by reference would be in memory for everybody.
+  if (n > kList || found > kHits) {
     const uint32_t some = min(ch.elements, a.vocab - cut);
     const auto each = [=](auto f) {
       for (uint32_t i = t; i < some; i += kThreads) {
         const float v = to_f32(x[cut + i]);
-        if (v >= least) f(order_of(v), (uint64_t)i);
+        if (v >= least) f(order_of(v), (uint64_t)(cut + i));
       }
     };
     uint32_t key;
@@ -259,19 +316,27 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const __grid_constant__ B
     if (t == 0) count = 0;
     __syncthreads();
     each([&](uint32_t c, uint64_t at) {
-      if (c > key || (c == key && at < tie)) list[atomicAdd(&count, 1u)] = {c, at + cut};
+      if (c > key || (c == key && at < tie)) list[atomicAdd(&count, 1u)] = (uint64_t)c << 32 | ~(uint32_t)at;
     });
     __syncthreads();
     n = count;
   }
   const uint64_t record = (uint64_t)row * ch.per_row + chunk;
   Candidate* best = ch.best + record * a.keep;
-  rank_list(list, n, a.keep, [&](uint32_t rank, const Entry<uint32_t>& e) { best[rank] = {from_order(e.key), (uint32_t)e.tie}; });
+  for (uint32_t i = t; i < n; i += kThreads) {
+    const uint64_t mine = list[i];
+    uint32_t rank = 0;
+    for (uint32_t j = 0; j < n; ++j) rank += list[j] > mine;
+    if (rank < a.keep) best[rank] = {from_order((uint32_t)(mine >> 32)), ~(uint32_t)mine};
+  }
   for (uint32_t i = min(n, a.keep) + t; i < a.keep; i += kThreads) best[i] = {kMinusInf, 0};
-  if (t == 0) {
-    float total = 0.0f;
-    for (uint32_t w = 0; w < kThreads / 32; ++w) total += warp_sum[w];
-    ch.heads[record] = make_float2(m, total);
+  if (t < 32) {
+    const float wm = t < kThreads / 32 ? warp_max[t] : kMinusInf, ws = t < kThreads / 32 ? warp_sum[t] : 0.0f;
+    const float top = from_order(__reduce_max_sync(~0u, order_of(wm)));
+    float total = wm == top ? ws : ws * exp2_of((wm - top) * a.c2);
+#pragma unroll
+    for (int d = 4; d; d /= 2) total += __shfl_xor_sync(~0u, total, d);
+    if (t == 0) ch.heads[record] = make_float2(top, total);
   }
 }
 
@@ -318,175 +383,266 @@ __device__ __forceinline__ Two times(const Two& a, const Two& b) {
   return quick_two(p, fmaf(a.hi, b.hi, -p) + (a.hi * b.lo + a.lo * b.hi));
 }
 
-// A group's beams, its list and (kDirect) its logits, in dynamic shared memory.
+// Dynamic shared memory of a group: its beams, its list, and its logits or the numbers of its lists.
 __host__ __device__ __forceinline__ uint32_t list_of(uint64_t slots) { return slots < kList ? (uint32_t)slots : kList; }
-__host__ __device__ __forceinline__ uint32_t group_bytes(uint32_t beams, uint64_t slots, uint64_t logits) {
-  return (uint32_t)((beams * sizeof(Beam) + 15) / 16 * 16 + list_of(slots) * sizeof(Entry<uint64_t>) + logits * 4);
+__host__ __device__ __forceinline__ uint64_t group_bytes(uint32_t beams, uint64_t slots, uint64_t more) {
+  return (beams * sizeof(Beam) + 15) / 16 * 16 + list_of(slots) * sizeof(Entry<uint64_t>) + more * 4;
 }
 
-template <typename E, bool kDirect>
-__global__ void __launch_bounds__(kThreads) group_kernel(const __grid_constant__ BeamArgs a, const __grid_constant__ Chunks ch) {
-  extern __shared__ __align__(16) unsigned char raw[];
-  __shared__ uint32_t count, sums, odd;
-  const uint32_t g = blockIdx.x, t = threadIdx.x, warps = blockDim.x / 32, warp = t / 32, lane = t % 32;
-  const uint32_t row_slots = kDirect ? a.vocab : ch.per_row * a.keep, slots = a.beams * row_slots, most_listed = list_of(slots);
-  Beam* beam = reinterpret_cast<Beam*>(raw);
-  Entry<uint64_t>* list = reinterpret_cast<Entry<uint64_t>*>(raw + (a.beams * sizeof(Beam) + 15) / 16 * 16);
-  float* logits = reinterpret_cast<float*>(list + most_listed);
-  const uint64_t row0 = (uint64_t)g * a.beams;
-  const float inv_tau = 1.0f / a.tau;
-  if (t == 0) count = odd = 0;
-  // Lanes to a row of logits: as many as a short row has.
-  const uint32_t row_lanes = row_slots >= 32 ? 32 : 1u << (31 - __clz(row_slots)), row_warps = warps * (32 / row_lanes);
-  const uint32_t my_row = t / row_lanes, my_lane = t % row_lanes;
-  if constexpr (kDirect) {
-    for (uint32_t b = my_row; b < a.beams; b += row_warps)
-      for (uint32_t j = my_lane; j < a.vocab; j += row_lanes)
-        logits[b * a.vocab + j] = to_f32(static_cast<const E*>(a.x)[(row0 + b) * a.ldx + j]);
-  } else {
-    wait_for_previous();
+// A group's block: beams, list and what both kernels below do with them.
+struct Group {
+  const BeamArgs& a;
+  Beam* beam;
+  Entry<uint64_t>* list;
+  uint32_t most_listed;
+  uint64_t row0;
+  float inv_tau;
+  uint32_t *count, *odd;
+
+  __device__ __forceinline__ Group(const BeamArgs& args, unsigned char* raw, uint64_t slots, uint32_t* words)
+      : a(args), beam(reinterpret_cast<Beam*>(raw)),
+        list(reinterpret_cast<Entry<uint64_t>*>(raw + (args.beams * sizeof(Beam) + 15) / 16 * 16)), most_listed(list_of(slots)),
+        row0((uint64_t)blockIdx.x * args.beams), inv_tau(1.0f / args.tau), count(words), odd(words + 1) {
+    if (threadIdx.x == 0) *count = *odd = 0;
   }
+  __device__ __forceinline__ uint32_t state_of(uint32_t b) const {
+    const float score = __ldg(a.scores + row0 + b);
+    return score == kMinusInf ? kDead : a.finished && __ldg(a.finished + row0 + b) ? kFinished : kAlive;
+  }
+  // From the maximum and sum of a row's exponentials.
+  __device__ __forceinline__ void put(uint32_t b, uint32_t state, float m, float s) {
+    const float score = __ldg(a.scores + row0 + b);
+    Beam o;
+    o.state = state == kAlive && m == kMinusInf && s == s ? (uint32_t)kDead : state;
+    o.most = o.state == kAlive ? m : 0.0f;
+    o.base = {score, 0.0f};
+    if (o.state == kAlive) {
+      const Two l = log_of(s), d = two_sum(score, -l.hi);
+      o.base = quick_two(d.hi, d.lo - l.lo);
+    }
+    o.weight = {1.0f, 0.0f};
+    if (a.penalty != 0.0f) {  // n^-penalty = e^(-penalty ln n), ln n and the product in two parts
+      const int64_t n = __ldg(a.lengths + row0 + b) + (o.state != kFinished);
+      const Two l = log_of((float)(n < 1 ? 1 : n));
+      const float p = a.penalty * l.hi, w = expf(-p);
+      o.weight = quick_two(w, -w * fmaf(a.penalty, l.lo, fmaf(a.penalty, l.hi, -p)));
+    }
+    beam[b] = o;
+    if (score != score || score == -kMinusInf || s != s) *odd = 1;
+  }
+  __device__ __forceinline__ uint64_t key_of(uint32_t b, float x) const {
+    const Beam& o = beam[b];
+    const Two total = o.state == kFinished ? o.base : total_of(o, x, a.tau, inv_tau);
+    return order_of(a.penalty != 0.0f ? times(total, o.weight) : total);
+  }
+  // Equal in both parts: the lower beam, in it the larger logit, then the lower token (8, 32 and 24 bits).
+  static __device__ __forceinline__ uint64_t tie_of(uint32_t b, float x, uint32_t token) {
+    return (uint64_t)b << 56 | (uint64_t)~order_of(x) << 24 | token;
+  }
+  __device__ __forceinline__ void push(uint64_t key, uint64_t tie) const {
+    const uint32_t at = atomicAdd(count, 1u);
+    if (at < most_listed) list[at] = {key, tie};
+  }
+  // The best of the list, of all candidates each(f) -> f(key, tie) where they did not fit in.
+  template <typename Each>
+  __device__ __forceinline__ void finish(Each each, uint32_t* sums) const {
+    __syncthreads();
+    uint32_t n = *odd ? 0 : *count;
+    if (n > most_listed) {
+      uint64_t key, tie;
+      exact_bound<uint64_t>(each, (uint64_t)0, a.keep, sums, &key, &tie);
+      __syncthreads();
+      if (threadIdx.x == 0) *count = 0;
+      __syncthreads();
+      each([&](uint64_t c, uint64_t at) {
+        if (c > key || (c == key && at < tie)) list[atomicAdd(count, 1u)] = {c, at};
+      });
+      __syncthreads();
+      n = *count;
+    }
+    const uint64_t out = (uint64_t)blockIdx.x * a.keep;
+    rank_list(list, n, a.keep, [&](uint32_t rank, const Entry<uint64_t>& e) {
+      const uint32_t b = (uint32_t)(e.tie >> 56);
+      const Beam& o = beam[b];
+      const bool was = o.state == kFinished;
+      const int64_t token = was ? a.end_token : (int64_t)(e.tie & 0xFFFFFFu);
+      a.out_scores[out + rank] = was ? o.base.hi : total_of(o, from_order(~(uint32_t)(e.tie >> 24)), a.tau, inv_tau).hi;
+      a.out_tokens[out + rank] = token;
+      a.out_parents[out + rank] = (int64_t)(row0 + b);
+      if (a.out_finished) a.out_finished[out + rank] = was || token == a.end_token;
+      if (a.out_lengths) a.out_lengths[out + rank] = __ldg(a.lengths + row0 + b) + !was;
+    });
+    for (uint32_t i = min(n, a.keep) + threadIdx.x; i < a.keep; i += blockDim.x) {
+      a.out_scores[out + i] = *odd ? __int_as_float(0x7FC00000) : kMinusInf;
+      a.out_tokens[out + i] = -1;
+      a.out_parents[out + i] = (int64_t)(row0 + i % a.beams);
+      if (a.out_finished) a.out_finished[out + i] = 0;
+      if (a.out_lengths) a.out_lengths[out + i] = 0;
+    }
+  }
+};
+
+// Few logits in a group: all of it in shared memory.
+template <typename E>
+__global__ void __launch_bounds__(kThreads) direct_kernel(const __grid_constant__ BeamArgs a) {
+  extern __shared__ __align__(16) unsigned char raw[];
+  __shared__ uint32_t words[2], sums;
+  const uint32_t t = threadIdx.x, slots = a.beams * a.vocab, warp = t / 32, lane = t % 32;
+  Group g(a, raw, slots, words);
+  float* logits = reinterpret_cast<float*>(g.list + g.most_listed);
+  // Lanes to a row of logits: as many as a short row has.
+  const uint32_t row_lanes = a.vocab >= 32 ? 32 : 1u << (31 - __clz(a.vocab)), rows = blockDim.x / row_lanes;
+  const uint32_t my_row = t / row_lanes, my_lane = t % row_lanes;
+  for (uint32_t b = my_row; b < a.beams; b += rows)
+    for (uint32_t j = my_lane; j < a.vocab; j += row_lanes)
+      logits[b * a.vocab + j] = to_f32(static_cast<const E*>(a.x)[(g.row0 + b) * a.ldx + j]);
   __syncthreads();
   // The beams' maxima and sums: a warp to a beam, or a thread where rows are short.
-  const bool by_thread = kDirect && a.vocab <= 16;
-  for (uint32_t b = by_thread ? t : warp; b < a.beams; b += by_thread ? blockDim.x : warps) {
-    const float score = __ldg(a.scores + row0 + b);
-    const uint32_t state = score == kMinusInf ? kDead : a.finished && __ldg(a.finished + row0 + b) ? kFinished : kAlive;
+  const bool by_thread = a.vocab <= 16;
+  const uint32_t mine = by_thread ? 0 : lane, step = by_thread ? 1 : 32;
+  for (uint32_t b = by_thread ? t : warp; b < a.beams; b += by_thread ? blockDim.x : blockDim.x / 32) {
+    const uint32_t state = g.state_of(b);
+    const float* x = logits + b * a.vocab;
     float m = kMinusInf, s = 0.0f;
     if (state == kAlive) {
-      const uint32_t n = kDirect ? a.vocab : ch.per_row, mine = by_thread ? 0 : lane, step = by_thread ? 1 : 32;
-      const float2* heads = ch.heads + (row0 + b) * ch.per_row;
-      for (uint32_t i = mine; i < n; i += step) m = fmaxf(m, kDirect ? logits[b * a.vocab + i] : __ldca(heads + i).x);
+      for (uint32_t i = mine; i < a.vocab; i += step) m = fmaxf(m, x[i]);
       if (!by_thread)
 #pragma unroll
         for (int d = 16; d; d /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
       const float base = m == kMinusInf ? 0.0f : m;
-      for (uint32_t i = mine; i < n; i += step) {
-        if constexpr (kDirect) {
-          s += expf((logits[b * a.vocab + i] - base) * inv_tau);
-        } else {
-          const float2 part = __ldca(heads + i);
-          s += part.y == 0.0f ? 0.0f : part.y * expf((part.x - base) * inv_tau);
-        }
-      }
+      for (uint32_t i = mine; i < a.vocab; i += step) s += expf((x[i] - base) * g.inv_tau);
       if (!by_thread)
 #pragma unroll
         for (int d = 16; d; d /= 2) s += __shfl_xor_sync(~0u, s, d);
     }
-    if (by_thread || lane == 0) {
-      Beam o;
-      o.state = state == kAlive && m == kMinusInf && s == s ? (uint32_t)kDead : state;
-      o.most = o.state == kAlive ? m : 0.0f;
-      o.base = {score, 0.0f};
-      if (o.state == kAlive) {
-        const Two l = log_of(s);
-        const Two d = two_sum(score, -l.hi);
-        o.base = quick_two(d.hi, d.lo - l.lo);
-      }
-      o.weight = {1.0f, 0.0f};
-      beam[b] = o;
-      if (score != score || score == -kMinusInf || s != s) odd = 1;
-    }
+    if (mine == 0) g.put(b, state, m, s);
   }
   __syncthreads();
-  if (a.penalty != 0.0f) {  // a thread to a beam: these are of 64 bits
-    for (uint32_t b = t; b < a.beams; b += blockDim.x) {
-      const int64_t n = __ldg(a.lengths + row0 + b) + (beam[b].state != kFinished);
-      const double w = pow((double)(n < 1 ? 1 : n), -(double)a.penalty);
-      const float hi = (float)w;
-      beam[b].weight = {hi, (float)(w - (double)hi)};
-    }
-    __syncthreads();
-  }
   // All candidates of a thread: f(beam, token, x), x the logit (0 for a finished beam).
-  const auto each = [&](auto f) {
-    for (uint32_t b = my_row; b < a.beams; b += row_warps) {
-      const uint32_t state = beam[b].state;
+  const auto each = [=](auto f) {
+    for (uint32_t b = my_row; b < a.beams; b += rows) {
+      const uint32_t state = g.beam[b].state;
       if (state == kAlive) {
-#pragma unroll 4
-        for (uint32_t j = my_lane; j < row_slots; j += row_lanes) {
-          if constexpr (kDirect) {
-            const float x = logits[b * a.vocab + j];
-            if (x > kMinusInf) f(b, j, x);
-          } else {
-            const uint2 c = __ldca(reinterpret_cast<const uint2*>(ch.best) + (row0 + b) * row_slots + j);
-            if (__uint_as_float(c.x) > kMinusInf) f(b, c.y, __uint_as_float(c.x));
-          }
+        for (uint32_t j = my_lane; j < a.vocab; j += row_lanes) {
+          const float x = logits[b * a.vocab + j];
+          if (x > kMinusInf) f(b, j, x);
         }
       } else if (state == kFinished && my_lane == 0) {
         f(b, 0u, 0.0f);
       }
     }
   };
-  const auto key_of = [&](uint32_t b, float x) {
-    const Beam& o = beam[b];
-    const Two total = o.state == kFinished ? o.base : total_of(o, x, a.tau, inv_tau);
-    return order_of(a.penalty != 0.0f ? times(total, o.weight) : total);
-  };
-  // Equal in both parts: the lower beam, in it the larger logit, then the lower token (8, 32 and 24 bits).
-  const auto tie_of = [](uint32_t b, float x, uint32_t token) { return (uint64_t)b << 56 | (uint64_t)~order_of(x) << 24 | token; };
-  uint32_t n = 0;
-  if (!odd) {
-    uint64_t least = 0;
-    if (slots > 2 * a.keep && slots > 128 && a.keep <= blockDim.x) {
-      uint32_t most = 0;
-      each([&](uint32_t b, uint32_t, float x) { most = max(most, (uint32_t)(key_of(b, x) >> 32)); });
-      const uint32_t bound = bound_by_halves(most, a.keep);
-      least = bound == kOrderMinusInf + 1 ? 0 : (uint64_t)bound << 32;
-    }
+  uint64_t least = 0;
+  if (slots > 2 * a.keep && slots > 128 && a.keep <= blockDim.x) {
+    uint32_t most = 0;
+    each([&](uint32_t b, uint32_t, float x) { most = max(most, (uint32_t)(g.key_of(b, x) >> 32)); });
+    const uint32_t bound = bound_by_halves(most, a.keep);
+    least = bound == kOrderMinusInf + 1 ? 0 : (uint64_t)bound << 32;
+  }
+  const auto each_key = [=](auto f) {
     each([&](uint32_t b, uint32_t token, float x) {
-      const uint64_t key = key_of(b, x);
-      if (key >= least) {
-        const uint32_t at = atomicAdd(&count, 1u);
-        if (at < most_listed) list[at] = {key, tie_of(b, x, token)};
-      }
+      const uint64_t key = g.key_of(b, x);
+      if (key >= least) f(key, g.tie_of(b, x, token));
     });
-    __syncthreads();
-    n = count;
-    if (n > most_listed) {
-      const auto each_key = [&](auto f) {
-        each([&](uint32_t b, uint32_t token, float x) {
-          const uint64_t key = key_of(b, x);
-          if (key >= least) f(key, tie_of(b, x, token));
-        });
-      };
-      uint64_t key, tie;
-      exact_bound<uint64_t>(each_key, (uint64_t)0, a.keep, &sums, &key, &tie);
-      __syncthreads();
-      if (t == 0) count = 0;
-      __syncthreads();
-      each_key([&](uint64_t c, uint64_t at) {
-        if (c > key || (c == key && at < tie)) list[atomicAdd(&count, 1u)] = {c, at};
-      });
-      __syncthreads();
-      n = count;
+  };
+  each_key([&](uint64_t key, uint64_t tie) { g.push(key, tie); });
+  g.finish(each_key, &sums);
+}
+
+constexpr uint32_t kLists = 4096;  // of a group that are noted as gone through
+
+// The chunks' sums and sorted lists.  A bound that `keep` continuations reach comes
+// from one of each list, the depth-th; only lists whose first reaches it are gone through,
+// eight lanes to a list, up to their first that does not.
+__global__ void __launch_bounds__(kThreads) group_kernel(const __grid_constant__ BeamArgs a, const __grid_constant__ Chunks ch) {
+  extern __shared__ __align__(16) unsigned char raw[];
+  __shared__ uint32_t words[2], sums, going;
+  const uint32_t t = threadIdx.x, chunks = a.beams * ch.per_row;
+  Group g(a, raw, (uint64_t)chunks * a.keep, words);
+  uint32_t* lists = reinterpret_cast<uint32_t*>(g.list + g.most_listed);  // those that are gone through
+  if (t == 0) going = 0;
+  wait_for_previous();
+  // The beams' sums: as many lanes to a beam as its row has chunks, up to 32.
+  uint32_t lanes = 1;
+  while (lanes < 32 && lanes < ch.per_row) lanes *= 2;
+  const uint32_t mine = t % lanes;
+  for (uint32_t b0 = 0; b0 < a.beams; b0 += kThreads / lanes) {
+    const uint32_t b = b0 + t / lanes;
+    const uint32_t state = b < a.beams ? g.state_of(b) : (uint32_t)kDead;
+    const float2* heads = ch.heads + (g.row0 + b) * ch.per_row;
+    float m = kMinusInf, s = 0.0f;
+    float2 part = make_float2(kMinusInf, 0.0f);
+    if (state == kAlive) {
+      if (mine < ch.per_row) part = __ldca(heads + mine);
+      m = part.x;
+      for (uint32_t i = mine + lanes; i < ch.per_row; i += lanes) m = fmaxf(m, __ldca(heads + i).x);
     }
+    for (uint32_t d = lanes / 2; d; d /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+    const float base = m == kMinusInf ? 0.0f : m;
+    const auto add = [&](float2 p) { s += p.y == 0.0f ? 0.0f : p.y * expf((p.x - base) * g.inv_tau); };
+    add(part);
+    if (state == kAlive)
+      for (uint32_t i = mine + lanes; i < ch.per_row; i += lanes) add(__ldca(heads + i));
+    for (uint32_t d = lanes / 2; d; d /= 2) s += __shfl_xor_sync(~0u, s, d);
+    if (mine == 0 && b < a.beams) g.put(b, state, m, s);
   }
-  const uint64_t out = (uint64_t)g * a.keep;
-  rank_list(list, n, a.keep, [&](uint32_t rank, const Entry<uint64_t>& e) {
-    const uint32_t b = (uint32_t)(e.tie >> 56);
-    const Beam& o = beam[b];
-    const bool was = o.state == kFinished;
-    const int64_t token = was ? a.end_token : (int64_t)(e.tie & 0xFFFFFFu);
-    a.out_scores[out + rank] = was ? o.base.hi : total_of(o, from_order(~(uint32_t)(e.tie >> 24)), a.tau, inv_tau).hi;
-    a.out_tokens[out + rank] = token;
-    a.out_parents[out + rank] = (int64_t)(row0 + b);
-    if (a.out_finished) a.out_finished[out + rank] = was || token == a.end_token;
-    if (a.out_lengths) a.out_lengths[out + rank] = __ldg(a.lengths + row0 + b) + !was;
-  });
-  for (uint32_t i = min(n, a.keep) + t; i < a.keep; i += blockDim.x) {
-    a.out_scores[out + i] = odd ? __int_as_float(0x7FC00000) : kMinusInf;
-    a.out_tokens[out + i] = -1;
-    a.out_parents[out + i] = (int64_t)(row0 + i % a.beams);
-    if (a.out_finished) a.out_finished[out + i] = 0;
-    if (a.out_lengths) a.out_lengths[out + i] = 0;
+  __syncthreads();
+  const uint2* best = reinterpret_cast<const uint2*>(ch.best) + g.row0 * ch.per_row * a.keep;
+  // A list's i-th continuation, as key and tie; 0: none.
+  const auto key_at = [=](uint32_t b, uint32_t list, uint32_t i, uint64_t* tie) -> uint64_t {
+    const uint32_t state = g.beam[b].state;
+    uint2 c = make_uint2(0, 0);
+    if (state == kAlive) {
+      c = __ldca(best + (uint64_t)list * a.keep + i);
+      if (!(__uint_as_float(c.x) > kMinusInf)) return 0;
+    } else if (state == kDead || i != 0 || list != b * ch.per_row) {
+      return 0;
+    }
+    *tie = g.tie_of(b, __uint_as_float(c.x), c.y);
+    return g.key_of(b, __uint_as_float(c.x));
+  };
+  const uint32_t depth = (a.keep + chunks - 1) / chunks;  // so many of each list are enough
+  uint64_t least = 0, tie;
+  if (chunks <= kThreads) {
+    uint32_t reached = 0;
+    if (t < chunks) reached = (uint32_t)(key_at(t / ch.per_row, t, depth - 1, &tie) >> 32);
+    const uint32_t bound = bound_by_halves(reached, (a.keep + depth - 1) / depth);
+    least = bound == kOrderMinusInf + 1 ? 0 : (uint64_t)bound << 32;
+  } else {  // several lists to a thread: the best of each thread's is one of a list
+    uint32_t reached = 0;
+    for (uint32_t l = t; l < chunks; l += kThreads) reached = max(reached, (uint32_t)(key_at(l / ch.per_row, l, 0, &tie) >> 32));
+    const uint32_t bound = bound_by_halves(reached, a.keep);
+    least = bound == kOrderMinusInf + 1 ? 0 : (uint64_t)bound << 32;
   }
+  for (uint32_t l = t; l < chunks; l += kThreads) {
+    const uint64_t key = key_at(l / ch.per_row, l, 0, &tie);
+    if (key == 0 || key < least) continue;
+    const uint32_t at = atomicAdd(&going, 1u);
+    if (at < kLists) lists[at] = l;
+  }
+  __syncthreads();
+  const bool some = going <= kLists;  // else equal logits all over: all lists are gone through
+  const uint32_t all = some ? going : chunks;
+  const auto each_key = [=](auto f) {
+    for (uint32_t n = t / 8; n < all; n += kThreads / 8) {
+      const uint32_t l = some ? lists[n] : n, b = l / ch.per_row;
+      uint64_t at_tie;
+      for (uint32_t i = t % 8; i < a.keep; i += 8) {
+        const uint64_t key = key_at(b, l, i, &at_tie);
+        if (key == 0 || key < least) break;  // and so are all behind it
+        f(key, at_tie);
+      }
+    }
+  };
+  each_key([&](uint64_t key, uint64_t at_tie) { g.push(key, at_tie); });
+  g.finish(each_key, &sums);
 }
 
 constexpr uint64_t kDirectMost = 4096;  // logits of a group that one block takes as they are
 
-// How rows are cut: 8 vectors a thread (4 where each is put together from two), 2
-// where there are too few blocks for two on each of 152 SMs.
+// How rows are cut: 8 vectors a thread (4 where each is put together from two), twice
+// where there are blocks enough all the same (what a block does once takes as long as a tile),
+// 2 where there would be too few for two on each of 152 SMs.
 Chunks chunks_of(uint32_t groups, uint32_t beams, uint64_t vocab, uint32_t keep, uint32_t width, bool aligned, void* workspace,
                  uint32_t* vectors, uint64_t* bytes) {
   Chunks c = {};
@@ -495,9 +651,11 @@ Chunks chunks_of(uint32_t groups, uint32_t beams, uint64_t vocab, uint32_t keep,
   const uint64_t rows = (uint64_t)groups * beams;
   const auto per_row = [&](uint32_t v) { return (vocab + kThreads * v * width - 1) / (kThreads * v * width); };
   *vectors = aligned ? 8 : 4;
+  c.tiles = 1;
   if (rows * per_row(*vectors) < 304) *vectors = 2;
-  c.per_row = (uint32_t)per_row(*vectors);
-  c.elements = kThreads * *vectors * width;
+  else if (rows * per_row(2 * *vectors) >= 1216 && per_row(*vectors) > 1) c.tiles = 2;
+  c.per_row = (uint32_t)per_row(c.tiles * *vectors);
+  c.elements = kThreads * c.tiles * *vectors * width;
   c.heads = static_cast<float2*>(workspace);
   const uint64_t records = rows * c.per_row, heads = (records * sizeof(float2) + 255) / 256 * 256;
   c.best = reinterpret_cast<Candidate*>(static_cast<char*>(workspace) + heads);
@@ -524,7 +682,7 @@ cudaError_t launch_step(const BeamArgs& a, void* workspace, cudaStream_t st) {
     if (threads < a.keep && n > 128) threads = (a.keep + 31) / 32 * 32;
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = group_bytes(a.beams, n, n);
-    return cudaLaunchKernelEx(&cfg, group_kernel<E, true>, a, c);
+    return cudaLaunchKernelEx(&cfg, direct_kernel<E>, a);
   }
   const uint64_t blocks = (uint64_t)a.groups * a.beams * c.per_row;
   const auto rows = [&](auto kernel) { return launch_plain(kernel, blocks, kThreads, st, a, c); };
@@ -532,126 +690,187 @@ cudaError_t launch_step(const BeamArgs& a, void* workspace, cudaStream_t st) {
                                 : (vectors == 4 ? rows(row_kernel<E, 4, false>) : rows(row_kernel<E, 2, false>));
   if (e != cudaSuccess) return e;
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = group_bytes(a.beams, (uint64_t)a.beams * c.per_row * a.keep, 0);
+  const uint64_t chunks = (uint64_t)a.beams * c.per_row;  // beams, list and lists fit into 48 KB
+  cfg.dynamicSmemBytes = group_bytes(a.beams, chunks * a.keep, chunks < kLists ? chunks : kLists);
   after.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   after.val.programmaticStreamSerializationAllowed = 1;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, group_kernel<E, false>, a, c);
+  return cudaLaunchKernelEx(&cfg, group_kernel, a, c);
 }
 
 // ---- states -----------------------------------------------------------------
 
 // Rows' tiles by way of shared memory: a block reads a tile of every row that is
 // somebody's parent, once, and then writes the tile of every row, so that rows
-// may change places.  U: the unit that all addresses, strides and widths are multiples
-// of.  Flat: a token's units follow the one's before.
+// may change places.
 struct Tiles {
   uint32_t units;          // of a tile and row
   uint32_t run;            // units of a token (and head, where heads are apart)
   uint32_t per_row, heads; // tiles; heads that are apart
 };
 
+// What a block's tile is made of.
+struct Moves {
+  int32_t parent[BF_MAX_BEAMS];       // of each row; -1: stays
+  uint32_t limit[BF_MAX_BEAMS];       // units of the tile that the row's parent has
+  uint32_t needed[BF_MAX_BEAMS / 32]; // rows that are parents
+  uint32_t from[BF_MAX_BEAMS];        // slot -> row
+  uint32_t have[BF_MAX_BEAMS];        // slot -> units
+  uint32_t many;
+
+  __device__ __forceinline__ uint32_t slot_of(uint32_t p) const {
+    uint32_t n = __popc(needed[p / 32] & ((1u << p % 32) - 1));
+    for (uint32_t w = 0; w < p / 32; ++w) n += __popc(needed[w]);
+    return n;
+  }
+};
+
+// Units of a tile at `first` that a row of `n` tokens has.
+__device__ __forceinline__ uint32_t units_of(int64_t n, uint64_t tokens, uint64_t first, const Tiles& tl) {
+  const uint64_t end = n <= 0 ? 0 : min((uint64_t)n, tokens) * tl.run;
+  return end > first ? (uint32_t)min(end - first, (uint64_t)tl.units) : 0;
+}
+
+// By all threads of a block.
+__device__ __forceinline__ void find_moves(const ReorderArgs& a, const Tiles& tl, uint64_t row0, uint64_t first, Moves& mv) {
+  const uint32_t t = threadIdx.x;
+  if (t < BF_MAX_BEAMS / 32) mv.needed[t] = 0;
+  __syncthreads();
+  for (uint32_t b = t; b < a.beams; b += blockDim.x) {
+    const int64_t p = __ldg(a.parents + row0 + b) - (int64_t)row0;
+    int32_t from = p >= 0 && p < (int64_t)a.beams && !(a.in_place && p == (int64_t)b) ? (int32_t)p : -1;
+    const uint32_t mine = from < 0 ? 0 : units_of(a.lengths ? __ldg(a.lengths + row0 + from) : (int64_t)a.tokens, a.tokens, first, tl);
+    if (mine == 0) from = -1;
+    mv.parent[b] = from;
+    mv.limit[b] = mine;
+    if (from >= 0) atomicOr(&mv.needed[from / 32], 1u << from % 32);
+  }
+  __syncthreads();
+  for (uint32_t b = t; b < a.beams; b += blockDim.x)
+    if (mv.parent[b] >= 0) {
+      const uint32_t s = mv.slot_of(mv.parent[b]);  // the same for all rows of a parent
+      mv.from[s] = mv.parent[b];
+      mv.have[s] = mv.limit[b];
+    }
+  if (t == 0) {
+    uint32_t many = 0;
+    for (uint32_t w = 0; w < (a.beams + 31) / 32; ++w) many += __popc(mv.needed[w]);
+    mv.many = many;
+  }
+  __syncthreads();
+}
+
+// A block's place: array, head, first row of its group, first unit of its tile.
+struct TilePlace {
+  uint32_t array, head;
+  uint64_t row0, first;
+  __device__ __forceinline__ TilePlace(const ReorderArgs& a, const Tiles& tl) {
+    uint32_t i = blockIdx.x;
+    first = (uint64_t)(i % tl.per_row) * tl.units;
+    i /= tl.per_row;
+    head = i % tl.heads;
+    i /= tl.heads;
+    array = i % a.count;
+    row0 = (uint64_t)(i / a.count) * a.beams;
+  }
+};
+
+// Rows whose valid part is one run of 16-byte units: a warp has the copying done.  (By
+// loads and stores of 256 threads, two of each on their way: 3.7 TB/s.)
+__global__ void __launch_bounds__(32) reorder_runs_kernel(const __grid_constant__ ReorderArgs a, const __grid_constant__ Tiles tl) {
+  extern __shared__ __align__(16) unsigned char held[];
+  __shared__ Moves mv;
+  __shared__ uint64_t full;
+  __shared__ uint32_t gave_up;
+  const uint32_t lane = threadIdx.x;
+  const TilePlace at(a, tl);
+  find_moves(a, tl, at.row0, at.first, mv);
+  const uint32_t many = mv.many;
+  if (many == 0) return;
+  uint32_t bytes = 0;
+  for (uint32_t s = lane; s < many; s += 32) bytes += mv.have[s] * 16;
+  bytes = __reduce_add_sync(~0u, bytes);
+  if (lane == 0) {
+    gave_up = 0;
+    barrier_init(&full, 1);
+    fence_barriers();
+    barrier_expect(&full, bytes);
+  }
+  __syncwarp();
+  for (uint32_t s = lane; s < many; s += 32)
+    copy_run(held + s * tl.units * 16, a.from[at.array] + (at.row0 + mv.from[s]) * a.from_row + at.head * a.from_head + at.first * 16,
+             mv.have[s] * 16, &full);
+  if (!barrier_wait(&full, 0, &gave_up)) return;
+  for (uint32_t b = lane; b < a.beams; b += 32)
+    if (mv.parent[b] >= 0)
+      put_run(a.to[at.array] + (at.row0 + b) * a.to_row + at.head * a.to_head + at.first * 16,
+              held + mv.slot_of(mv.parent[b]) * tl.units * 16, mv.limit[b] * 16);
+  put_runs_end();
+}
+
+// Everything else.  U: the unit that all addresses, strides and widths are multiples
+// of.  kFlat: a token's units follow the one's before.
 template <typename U, bool kFlat>
 __global__ void __launch_bounds__(kThreads) reorder_kernel(const __grid_constant__ ReorderArgs a, const __grid_constant__ Tiles tl) {
   extern __shared__ __align__(16) unsigned char raw[];
   U* held = reinterpret_cast<U*>(raw);
-  __shared__ int32_t parent[BF_MAX_BEAMS];       // of each row; -1: stays
-  __shared__ uint32_t limit[BF_MAX_BEAMS];       // units of this tile that a row's parent has
-  __shared__ uint32_t needed[BF_MAX_BEAMS / 32];
-  __shared__ uint32_t slots[BF_MAX_BEAMS];       // slot -> row
+  __shared__ Moves mv;
   const uint32_t t = threadIdx.x;
-  uint64_t i = blockIdx.x;
-  const uint32_t tile = i % tl.per_row;
-  i /= tl.per_row;
-  const uint32_t head = i % tl.heads;
-  i /= tl.heads;
-  const uint32_t k = i % a.count;
-  const uint64_t row0 = i / a.count * a.beams;
-  const uint64_t first = (uint64_t)tile * tl.units;
-  if (t < BF_MAX_BEAMS / 32) needed[t] = 0;
-  __syncthreads();
-  for (uint32_t b = t; b < a.beams; b += kThreads) {
-    const int64_t p = __ldg(a.parents + row0 + b) - (int64_t)row0;
-    int32_t from = p >= 0 && p < (int64_t)a.beams && !(a.in_place && p == (int64_t)b) ? (int32_t)p : -1;
-    uint64_t end = a.tokens * tl.run;
-    if (from >= 0 && a.lengths) {
-      const int64_t n = __ldg(a.lengths + row0 + from);
-      end = n <= 0 ? 0 : min((uint64_t)n, a.tokens) * tl.run;
-    }
-    const uint32_t mine = end > first ? (uint32_t)min(end - first, (uint64_t)tl.units) : 0;
-    if (mine == 0) from = -1;
-    parent[b] = from;
-    limit[b] = mine;
-    if (from >= 0) atomicOr(&needed[from / 32], 1u << from % 32);
-  }
-  __syncthreads();
-  uint32_t many = 0;
-  for (uint32_t w = 0; w < (a.beams + 31) / 32; ++w) many += __popc(needed[w]);
+  const TilePlace at(a, tl);
+  find_moves(a, tl, at.row0, at.first, mv);
+  const uint32_t many = mv.many;
   if (many == 0) return;
-  const auto slot_of = [&](uint32_t p) {
-    uint32_t n = __popc(needed[p / 32] & ((1u << p % 32) - 1));
-    for (uint32_t w = 0; w < p / 32; ++w) n += __popc(needed[w]);
-    return n;
-  };
-  for (uint32_t b = t; b < a.beams; b += kThreads) {
-    if (needed[b / 32] >> b % 32 & 1) slots[slot_of(b)] = b;
-  }
-  __syncthreads();
   const auto place = [&](uint64_t u, uint64_t token) -> uint64_t {  // bytes of unit u behind a row's first
     if constexpr (kFlat) return u * sizeof(U);
     const uint64_t n = u / tl.run;
     return n * token + (u - n * tl.run) * sizeof(U);
   };
-  for (uint32_t s = 0; s < many; ++s) {
-    const uint32_t p = slots[s];
-    uint32_t n = tl.units;
-    {
-      uint64_t end = a.tokens * tl.run;
-      if (a.lengths) end = min((uint64_t)__ldg(a.lengths + row0 + p), a.tokens) * tl.run;
-      n = (uint32_t)min(end - first, (uint64_t)tl.units);
-    }
-    const char* from = a.from[k] + (row0 + p) * a.from_row + head * a.from_head;
-    for (uint32_t u = t; u < n; u += kThreads)
-      held[s * tl.units + u] = *reinterpret_cast<const U*>(from + place(first + u, a.from_token));
+  const char* from = a.from[at.array] + at.head * a.from_head;
+  char* to = a.to[at.array] + at.head * a.to_head;
+#pragma unroll 4
+  for (uint32_t i = t; i < many * tl.units; i += kThreads) {
+    const uint32_t s = i / tl.units, u = i - s * tl.units;
+    if (u < mv.have[s])
+      held[i] = *reinterpret_cast<const U*>(from + (at.row0 + mv.from[s]) * a.from_row + place(at.first + u, a.from_token));
   }
   __syncthreads();
   for (uint32_t b = 0; b < a.beams; ++b) {
-    if (parent[b] < 0) continue;
-    const uint32_t s = slot_of(parent[b]), n = limit[b];
-    char* to = a.to[k] + (row0 + b) * a.to_row + head * a.to_head;
+    if (mv.parent[b] < 0) continue;
+    const uint32_t s = mv.slot_of(mv.parent[b]), n = mv.limit[b];
     for (uint32_t u = t; u < n; u += kThreads)
-      *reinterpret_cast<U*>(to + place(first + u, a.to_token)) = held[s * tl.units + u];
+      *reinterpret_cast<U*>(to + (at.row0 + b) * a.to_row + place(at.first + u, a.to_token)) = held[s * tl.units + u];
   }
 }
 
 template <typename U>
 cudaError_t launch_units(const ReorderArgs& a, bool flat, cudaStream_t st) {
+  constexpr bool kRuns = sizeof(U) == 16;
   Tiles tl = {};
   tl.run = (uint32_t)(a.width / sizeof(U));
   tl.heads = a.heads;
-  const uint32_t most = 65536 / (a.beams * sizeof(U));
-  const uint64_t row = a.tokens * tl.run;
+  const uint64_t row = a.tokens * tl.run, most = 65536 / (a.beams * sizeof(U));  // 64 KB of a tile: three blocks an SM
   uint64_t units = 8192 / sizeof(U);
   if (units > most) units = most;
   if (units > row) units = row;
   tl.units = (uint32_t)units;
   const uint64_t per_row = (row + units - 1) / units, blocks = per_row * tl.heads * a.count * a.groups;
-  if (blocks > 0x7FFFFFFFu) return cudaErrorInvalidValue;
+  if (per_row > 0x7FFFFFFFu || blocks > 0x7FFFFFFFu) return cudaErrorInvalidValue;
   tl.per_row = (uint32_t)per_row;
   const uint32_t shared = (uint32_t)(units * a.beams * sizeof(U));
-  const auto launch = [&](auto kernel) {
+  const auto launch = [&](auto kernel, uint32_t threads) {
     if (shared > 32 * 1024) {
       const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 65536);
       if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((uint32_t)blocks);
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = shared;
     cfg.stream = st;
     return cudaLaunchKernelEx(&cfg, kernel, a, tl);
   };
-  return flat ? launch(reorder_kernel<U, true>) : launch(reorder_kernel<U, false>);
+  if (flat && kRuns) return launch(reorder_runs_kernel, 32);
+  return flat ? launch(reorder_kernel<U, true>, kThreads) : launch(reorder_kernel<U, false>, kThreads);
 }
 
 }  // namespace

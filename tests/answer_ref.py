@@ -51,7 +51,8 @@ def continuations(logits, score, finished, length, end_token, penalty, tau):
 
 
 def beam_step(logits, scores, beams, keep, finished=None, lengths=None, end_token=-1, penalty=0.0, tau=1.0):
-    """For each group, all continuations in the order of rank: a list of (rank, total, token, parent, ended, length)."""
+    """For each group, its best continuations in the order of rank (20 more than are kept, at least): a list of (rank,
+    total, token, parent, ended, length)."""
     groups = []
     for first in range(0, len(scores), beams):
         rows = []
@@ -59,7 +60,8 @@ def beam_step(logits, scores, beams, keep, finished=None, lengths=None, end_toke
             done = finished is not None and bool(finished[b])
             n0 = 0 if lengths is None else int(lengths[b])
             total, rank, tokens, n = continuations(logits[b], float(scores[b]), done, n0, end_token, penalty, tau)
-            rows += [(-r, b, int(v), t, done or int(v) == end_token, n) for r, t, v in zip(rank, total, tokens)]
+            best = np.argsort(-rank, kind="stable")[:keep + 20]
+            rows += [(-rank[i], b, int(tokens[i]), total[i], done or int(tokens[i]) == end_token, n) for i in best]
         rows.sort(key=lambda x: x[:3])
         groups.append([(-r, t, v, b, e, n) for r, b, v, t, e, n in rows])
     return groups

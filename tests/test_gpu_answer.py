@@ -389,7 +389,8 @@ def beam_inputs(groups, beams, vocab, dtype, seed=0, banned=0.0):
 BEAMS = [  # groups, beams, vocabulary, keep
     (1, 1, 1, 1), (3, 4, 3, 4), (50, 16, 3, 16), (2, 3, 7, 6), (5, 8, 100, 8), (1, 4, 4096, 4), (2, 2, 2049, 5),
     (1, 4, 5003, 8), (3, 5, 16384, 10), (2, 3, 16385, 1), (2, 1, 33001, 256), (1, 2, 70001, 200), (1, 64, 300, 64),
-    (2, 256, 20, 256), (1, 256, 40, 100), (90, 4, 9001, 4), (1, 33, 129, 66),
+    (2, 256, 20, 256), (1, 256, 40, 100), (90, 4, 9001, 4), (1, 33, 129, 66), (2, 40, 70000, 33), (1, 130, 40003, 256),
+    (40, 9, 17000, 9), (1, 1, 1 << 20, 3),
 ]
 
 
@@ -421,7 +422,7 @@ def test_beams_options(shape, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("vocab", [5, 1000, 20000, 50001])
+@pytest.mark.parametrize("vocab", [5, 1000, 20000, 50001, 300000])
 def test_beams_ties(vocab, dtype):
     """Equal logits everywhere, equal rows at every alignment, a few values only: ties go to the lower beam and token."""
     same = torch.zeros(6, vocab, dtype=TYPES[dtype], device="cuda")
@@ -436,6 +437,9 @@ def test_beams_ties(vocab, dtype):
     assert got.tokens[0].tolist() == [order[0]] * 8 + [order[1]] * 8
     few = torch.tensor(rng.integers(0, 3, (4, vocab)), dtype=torch.float32, device="cuda").to(TYPES[dtype])
     check_beams(few, [-1.0, -1.5, -1.0, -1.0], 2, 40 if vocab > 5 else 10)
+    many = torch.zeros(120, vocab, dtype=TYPES[dtype], device="cuda")  # more lists than are noted
+    got = bf.beam_step(many, torch.zeros(120, device="cuda"), 120, keep=256)
+    assert got.parents[0].tolist() == [j // vocab for j in range(256)] and got.tokens[0].tolist() == [j % vocab for j in range(256)]
     signed = torch.zeros(2, vocab, dtype=TYPES[dtype], device="cuda")
     signed[:, 1::2] = -0.0
     got = bf.beam_step(signed, torch.zeros(2, device="cuda"), 2, keep=4)
