@@ -3,14 +3,11 @@
 //
 // A block to an answer and key head (and up to 16 of the query heads that share
 // it); in a cluster where there are few, so that an answer's keys are spread over
-// several SMs.  The keys are read once and by one block, so they go from memory to
-// registers in the shape in which the products take them: which dimension, or which
-// key, stands where inside a product does not matter as long as both operands agree, and
-// 16 bytes of a key's vector are eight of a thread's elements.  The products are the
-// warps' own (16 x 8 x 16): at 4 to 16 queries a key the memory is the bound, and a
-// tile of 128 queries would be empty.  A warp takes 16 keys at a time; the next keys are
-// on their way while the present ones' weights are made, the next values while the
-// scores are.
+// several SMs.  Each warp takes 16 keys at a time through a ring of its own in shared
+// memory, two steps ahead by asynchronous copies, so that the keys on their way
+// cost no registers (kept there, two blocks an SM had 64 KB on their way and stood
+// still for half of the time).  The products are the warps' own (16 x 8 x 16): at 4 to
+// 16 queries a key the memory is the bound, and a tile of 128 queries would be empty.
 //
 // Behind its own keys a block waits for the prompts' pieces and joins all of them.
 #include <cooperative_groups.h>
@@ -43,15 +40,40 @@ __device__ __forceinline__ void product(float (&d)[4], const uint32_t (&a)[4], u
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ uint4 load16(const void* p, bool on) {
-  return on ? __ldg(reinterpret_cast<const uint4*>(p)) : make_uint4(0, 0, 0, 0);
+// 16 bytes to shared memory, zeros where they are not there.
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool on) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(__cvta_generic_to_global(from)), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() {  // all but the last N groups have arrived
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+// Four 8 x 8 matrices of 16 bits; the address is of row lane % 8 of matrix lane / 8.
+__device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ void load_turned(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
 }
 
 // DP: dimensions, to a multiple of 64.
-template <typename E, uint32_t DP>
+template <uint32_t DP>
 struct Few {
-  static constexpr uint32_t kPitch = DP + 4;
-  float o[kWarps][kRows][kPitch];
+  static constexpr uint32_t kPitch = DP + 4, kStages = 3;
+  // A step's 16 keys, or values: rows of 128 bytes in columns of 64 dimensions, 16-byte
+  // pieces at their place exclusive-or the row modulo 8.
+  static constexpr uint32_t kTile = 16 * DP * 2;
+  union {
+    unsigned char ring[kWarps][kStages][2][kTile];
+    float o[kWarps][kRows][kPitch];
+  };
   float2 sums[kWarps][kRows];
   float weight[kRows][kMostBlocks * kWarps + kTileParts];  // of the pieces: the cluster's warps', then the prompt's
   float inverse[kRows];
@@ -60,76 +82,83 @@ struct Few {
 template <typename E, uint32_t DP>
 __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ AttendPlan plan,
                                                        const __grid_constant__ FewArgs few) {
-  __shared__ Few<E, DP> sh;
+  extern __shared__ __align__(128) unsigned char raw[];
+  Few<DP>& sh = *reinterpret_cast<Few<DP>*>(raw);
+  constexpr uint32_t kStages = Few<DP>::kStages, kTile = Few<DP>::kTile, kPieces = DP / 8;  // pieces of a key
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, c = lane % 4;
   const uint32_t rank = blockIdx.x % few.blocks;
-  uint64_t unit = blockIdx.x / few.blocks;
+  uint32_t unit = blockIdx.x / few.blocks;
   const uint32_t first = unit % few.row_tiles * kRows;
   unit /= few.row_tiles;
   const uint32_t head = unit % a.kv_heads, rows = min(kRows, a.share - first);
-  const uint64_t answer = unit / a.kv_heads;
-  const uint32_t prompt = (uint32_t)(answer / a.per_prompt);
+  const uint32_t answer = unit / a.kv_heads, prompt = answer / a.per_prompt;
+  const uint32_t len = length_of(a.suffix_len, a.suffix_cap, answer), step = 16 * kWarps * few.blocks;
+  uint32_t at = 16 * (rank * kWarps + warp);
 
-  // The queries, as first operands of the scores: dimensions 32 j + 8 c + (0 1 | 2 3 | 4 5 | 6 7) of rows g and g + 8.
-  uint32_t q[DP / 32][2][4];
+  // The warp's ring: a lane copies a piece of every (32 / kPieces)-th key.
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(sh.ring[warp]);
+  const uint32_t my_piece = lane % kPieces, my_key = lane / kPieces;
+  const E* k_from = static_cast<const E*>(a.sk.data) + (int64_t)answer * a.sk.batch + (int64_t)head * a.sk.head + my_piece * 8;
+  const E* v_from = static_cast<const E*>(a.sv.data) + (int64_t)answer * a.sv.batch + (int64_t)head * a.sv.head + my_piece * 8;
+  const auto copy = [&](uint32_t stage, uint32_t from) {
+#pragma unroll
+    for (uint32_t i = 0; i < 16 * kPieces / 32; ++i) {
+      const uint32_t key = my_key + i * (32 / kPieces);
+      const bool on = from + key < len && my_piece * 8 < a.dim;
+      const uint32_t to = ring + stage * 2 * kTile + my_piece / 8 * 2048 + key * 128 + (my_piece % 8 ^ key % 8) * 16;
+      const int64_t token = on ? (int64_t)(from + key) : 0;
+      copy16(to, on ? k_from + token * a.sk.token : static_cast<const E*>(a.q.data), on);
+      copy16(to + kTile, on ? v_from + token * a.sv.token : static_cast<const E*>(a.q.data), on);
+    }
+  };
+#pragma unroll
+  for (uint32_t s = 0; s < kStages - 1; ++s) {
+    if (at + s * step < len) copy(s, at + s * step);
+    copies_end();
+  }
+
+  // The queries, as first operands of the scores: dimensions 16 j + 2 c + (0 1 | 8 9) of rows g and g + 8.
+  uint32_t q[DP / 16][4];
   {
     const E* base = static_cast<const E*>(a.q.data) + (int64_t)answer * a.q.batch + (int64_t)(head * a.share + first) * a.q.head;
+    const auto two = [&](uint32_t row, uint32_t d) {
+      return row < rows && d < a.dim ? __ldg(reinterpret_cast<const uint32_t*>(base + (int64_t)row * a.q.head + d)) : 0u;
+    };
 #pragma unroll
-    for (uint32_t j = 0; j < DP / 32; ++j) {
-      const uint32_t d = 32 * j + 8 * c;
-      const uint4 lo = load16(base + (int64_t)g * a.q.head + d, g < rows && d < a.dim);
-      const uint4 hi = load16(base + (int64_t)(g + 8) * a.q.head + d, g + 8 < rows && d < a.dim);
-      q[j][0][0] = lo.x, q[j][0][2] = lo.y, q[j][1][0] = lo.z, q[j][1][2] = lo.w;
-      q[j][0][1] = hi.x, q[j][0][3] = hi.y, q[j][1][1] = hi.z, q[j][1][3] = hi.w;
+    for (uint32_t j = 0; j < DP / 16; ++j) {
+      const uint32_t d = 16 * j + 2 * c;
+      q[j][0] = two(g, d), q[j][1] = two(g + 8, d), q[j][2] = two(g, d + 8), q[j][3] = two(g + 8, d + 8);
     }
   }
-  const uint32_t len = length_of(a.suffix_len, a.suffix_cap, answer);
-  const E* keys = static_cast<const E*>(a.sk.data) + (int64_t)answer * a.sk.batch + (int64_t)head * a.sk.head;
-  const E* values = static_cast<const E*>(a.sv.data) + (int64_t)answer * a.sv.batch + (int64_t)head * a.sv.head;
-  uint4 k[2][DP / 32], v[DP / 64][4];
-  const auto load_k = [&](uint32_t at) {  // keys at + g and at + 8 + g
-#pragma unroll
-    for (uint32_t n = 0; n < 2; ++n)
-#pragma unroll
-      for (uint32_t j = 0; j < DP / 32; ++j) {
-        const uint32_t key = at + 8 * n + g, d = 32 * j + 8 * c;
-        k[n][j] = load16(keys + (int64_t)key * a.sk.token + d, key < len && d < a.dim);
-      }
-  };
-  const auto load_v = [&](uint32_t at) {  // keys at + 2c + (0, 1, 8, 9), dimensions 64 h + 8 g + (0 .. 7)
-#pragma unroll
-    for (uint32_t h = 0; h < DP / 64; ++h)
-#pragma unroll
-      for (uint32_t n = 0; n < 4; ++n) {
-        const uint32_t key = at + 2 * c + n % 2 + n / 2 * 8, d = 64 * h + 8 * g;
-        v[h][n] = load16(values + (int64_t)key * a.sv.token + d, key < len && d < a.dim);
-      }
-  };
-  float o[DP / 64][8][4] = {};
-  float m[2] = {kNone, kNone}, l[2] = {0.0f, 0.0f};  // rows g and g + 8
-  const uint32_t step = 16 * kWarps * few.blocks;
-  uint32_t at = 16 * (rank * kWarps + warp);
-  if (at < len) {
-    load_k(at);
-    load_v(at);
-  }
   // Who has the prompt's pieces (while the keys are on their way); an answer's rows may lie in two tiles of queries.
-  const uint32_t row0 = (uint32_t)(answer - (uint64_t)prompt * a.per_prompt) * a.share + first;
+  const uint32_t row0 = (answer - prompt * a.per_prompt) * a.share + first;
   const uint32_t tile0 = row0 / plan.rows, rows0 = min(rows, (tile0 + 1) * plan.rows - row0);
   const Standing standing = standing_of(a, plan.keys, prompt);
   const Owners own0 = owners_of(a, plan, standing, prompt, head * plan.row_tiles + tile0);
   const Owners own1 = rows0 == rows ? own0 : owners_of(a, plan, standing, prompt, head * plan.row_tiles + tile0 + 1);
   const bool bad = bad_answer(a, prompt, answer);
-  for (; at < len; at += step) {
+  float o[DP / 8][4] = {};
+  float m[2] = {kNone, kNone}, l[2] = {0.0f, 0.0f};  // rows g and g + 8
+  // Rows of the matrices that this lane gives the addresses of: of keys for the scores, of values for the outputs.
+  const uint32_t k_row = lane % 8, v_row = lane / 8 % 2 * 8 + lane % 8;
+  for (uint32_t stage = 0; at < len; at += step, stage = stage + 1 == kStages ? 0 : stage + 1) {
+    copies_wait<kStages - 2>();
+    __syncwarp();
+    const uint32_t ahead = at + (kStages - 1) * step;
+    if (ahead < len) copy(stage == 0 ? kStages - 1 : stage - 1, ahead);  // where the step before this one was
+    copies_end();
+    const uint32_t keys = ring + stage * 2 * kTile, values = keys + kTile;
     float s[2][4] = {};
 #pragma unroll
     for (uint32_t j = 0; j < DP / 32; ++j)
 #pragma unroll
       for (uint32_t n = 0; n < 2; ++n) {
-        product<E>(s[n], q[j][0], k[n][j].x, k[n][j].y);
-        product<E>(s[n], q[j][1], k[n][j].z, k[n][j].w);
+        const uint32_t piece = 4 * j + lane / 8, key = 8 * n + k_row;
+        uint32_t b[4];
+        load_matrices(b, keys + piece / 8 * 2048 + key * 128 + (piece % 8 ^ k_row) * 16);
+        product<E>(s[n], q[2 * j], b[0], b[1]);
+        product<E>(s[n], q[2 * j + 1], b[2], b[3]);
       }
-    if (at + step < len) load_k(at + step);
     // Scores of keys at + 8n + 2c + (0, 1): rows g (elements 0, 1) and g + 8 (2, 3).
     float top[2] = {kNone, kNone};
 #pragma unroll
@@ -153,12 +182,10 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
         m[r] = to;
         l[r] *= shrink;
 #pragma unroll
-        for (uint32_t h = 0; h < DP / 64; ++h)
-#pragma unroll
-          for (uint32_t e = 0; e < 8; ++e) {
-            o[h][e][2 * r] = shrink == 0.0f ? 0.0f : o[h][e][2 * r] * shrink;
-            o[h][e][2 * r + 1] = shrink == 0.0f ? 0.0f : o[h][e][2 * r + 1] * shrink;
-          }
+        for (uint32_t n = 0; n < DP / 8; ++n) {
+          o[n][2 * r] = shrink == 0.0f ? 0.0f : o[n][2 * r] * shrink;
+          o[n][2 * r + 1] = shrink == 0.0f ? 0.0f : o[n][2 * r + 1] * shrink;
+        }
       }
     }
     uint32_t w[4];
@@ -172,20 +199,18 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
         w[2 * n + r] = pack2(e, E());
       }
 #pragma unroll
-    for (uint32_t h = 0; h < DP / 64; ++h) {
-      const uint32_t* v0 = reinterpret_cast<const uint32_t*>(&v[h][0]);
-      const uint32_t* v1 = reinterpret_cast<const uint32_t*>(&v[h][1]);
-      const uint32_t* v2 = reinterpret_cast<const uint32_t*>(&v[h][2]);
-      const uint32_t* v3 = reinterpret_cast<const uint32_t*>(&v[h][3]);
-#pragma unroll
-      for (uint32_t e = 0; e < 8; ++e) {
-        const uint32_t pick = e % 2 ? 0x7632 : 0x5410;
-        product<E>(o[h][e], w, __byte_perm(v0[e / 2], v1[e / 2], pick), __byte_perm(v2[e / 2], v3[e / 2], pick));
-      }
+    for (uint32_t j = 0; j < DP / 16; ++j) {
+      const uint32_t piece = 2 * j + lane / 16;
+      uint32_t b[4];
+      load_turned(b, values + piece / 8 * 2048 + v_row * 128 + (piece % 8 ^ v_row % 8) * 16);
+      product<E>(o[2 * j], w, b[0], b[1]);
+      product<E>(o[2 * j + 1], w, b[2], b[3]);
     }
-    if (at + step < len) load_v(at + step);
+    __syncwarp();
   }
-  // The warp's outputs: element i of o[h][e] is of row g + i / 2 * 8 and dimension 64 h + (2 c + i % 2) 8 + e.
+  copies_wait<0>();
+  __syncthreads();  // the rings are done with: the warps' outputs take their place
+  // Element i of o[n] is of row g + i / 2 * 8 and dimension 8 n + 2 c + i % 2.
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
     l[r] += __shfl_xor_sync(~0u, l[r], 1);
@@ -194,13 +219,8 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
     if (row >= rows) continue;
     if (c == 0) sh.sums[warp][row] = make_float2(m[r], l[r]);
 #pragma unroll
-    for (uint32_t h = 0; h < DP / 64; ++h)
-#pragma unroll
-      for (uint32_t i = 0; i < 2; ++i)
-#pragma unroll
-        for (uint32_t e = 0; e < 8; e += 4)
-          *reinterpret_cast<float4*>(&sh.o[warp][row][64 * h + (2 * c + i) * 8 + e]) =
-              make_float4(o[h][e][2 * r + i], o[h][e + 1][2 * r + i], o[h][e + 2][2 * r + i], o[h][e + 3][2 * r + i]);
+    for (uint32_t n = 0; n < DP / 8; ++n)
+      *reinterpret_cast<float2*>(&sh.o[warp][row][8 * n + 2 * c]) = make_float2(o[n][2 * r], o[n][2 * r + 1]);
   }
   const bool clustered = few.blocks > 1;
   cg::cluster_group cluster = cg::this_cluster();
@@ -210,7 +230,7 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
 
   // The weights of a row's pieces: of the warps of all blocks here, and of the prompt's.
   const uint32_t near = few.blocks * kWarps;
-  const auto peer = [&](uint32_t b) -> Few<E, DP>* { return clustered ? cluster.map_shared_rank(&sh, b) : &sh; };
+  const auto peer = [&](uint32_t b) -> Few<DP>* { return clustered ? cluster.map_shared_rank(&sh, b) : &sh; };
   const auto record_of = [&](const Owners& own, uint32_t i) { return plan.prefix + (own.first + i + own.segment) * plan.record; };
   for (uint32_t row = warp; row < rows; row += kWarps) {
     const Owners own = row < rows0 ? own0 : own1;
@@ -247,7 +267,7 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
     if (lane == 0) {
       sh.inverse[row] = odd ? nan : total > 0.0f ? 1.0f / total : 0.0f;
       if (a.lse && rank == 0)
-        a.lse[answer * ((uint64_t)a.kv_heads * a.share) + head * a.share + first + row] =
+        a.lse[(uint64_t)answer * (a.kv_heads * a.share) + head * a.share + first + row] =
             odd ? nan : total > 0.0f ? (most + log2f(total)) * 0.693147180559945309f : kNone;
     }
   }
@@ -275,7 +295,7 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
         if (i + k < far) add(sh.weight[row][near + i + k], x[k]);
     }
     for (uint32_t b = 0; b < few.blocks; ++b) {
-      const Few<E, DP>* them = peer(b);
+      const Few<DP>* them = peer(b);
 #pragma unroll
       for (uint32_t w = 0; w < kWarps; ++w) add(sh.weight[row][b * kWarps + w], *reinterpret_cast<const float4*>(&them->o[w][row][d]));
     }
@@ -307,9 +327,14 @@ cudaError_t launch_few_queries(const AttendArgs& a, const AttendPlan& plan, cuda
   FewArgs f = {(a.share + kRows - 1) / kRows, 1};
   const uint64_t units = (uint64_t)a.prompts * a.per_prompt * a.kv_heads * f.row_tiles;
   while (f.blocks < kMostBlocks && units * f.blocks < 304 && a.suffix_cap > 64ull * f.blocks) f.blocks *= 2;
-  const auto launch = [&](auto kernel) { return launch_shaped(kernel, units * f.blocks, kThreads, f.blocks, true, st, a, plan, f); };
-  if (a.dtype == BF_BF16) return a.dim <= 64 ? launch(few_kernel<__nv_bfloat16, 64>) : launch(few_kernel<__nv_bfloat16, 128>);
-  return a.dim <= 64 ? launch(few_kernel<__half, 64>) : launch(few_kernel<__half, 128>);
+  const auto launch = [&](auto kernel, uint64_t shared) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+    if (e != cudaSuccess) return e;
+    return launch_shared(kernel, units * f.blocks, kThreads, f.blocks, true, shared, st, a, plan, f);
+  };
+  if (a.dtype == BF_BF16)
+    return a.dim <= 64 ? launch(few_kernel<__nv_bfloat16, 64>, sizeof(Few<64>)) : launch(few_kernel<__nv_bfloat16, 128>, sizeof(Few<128>));
+  return a.dim <= 64 ? launch(few_kernel<__half, 64>, sizeof(Few<64>)) : launch(few_kernel<__half, 128>, sizeof(Few<128>));
 }
 
 }  // namespace bfk

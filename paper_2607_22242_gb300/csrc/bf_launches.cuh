@@ -15,12 +15,13 @@ __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontr
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 template <typename K, typename... Args>
-cudaError_t launch_shaped(K kernel, uint64_t blocks, uint32_t threads, uint32_t cluster, bool follows, cudaStream_t st,
-                          const Args&... args) {
+cudaError_t launch_shared(K kernel, uint64_t blocks, uint32_t threads, uint32_t cluster, bool follows, uint64_t shared,
+                          cudaStream_t st, const Args&... args) {
   if (blocks > 0x7FFFFFFFu) return cudaErrorInvalidValue;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((uint32_t)blocks);
   cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = shared;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   cfg.attrs = attr;
@@ -35,6 +36,12 @@ cudaError_t launch_shaped(K kernel, uint64_t blocks, uint32_t threads, uint32_t 
     ++cfg.numAttrs;
   }
   return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <typename K, typename... Args>
+cudaError_t launch_shaped(K kernel, uint64_t blocks, uint32_t threads, uint32_t cluster, bool follows, cudaStream_t st,
+                          const Args&... args) {
+  return launch_shared(kernel, blocks, threads, cluster, follows, 0, st, args...);
 }
 
 template <typename K, typename... Args>
