@@ -126,13 +126,27 @@ struct Standing {
 __device__ __forceinline__ Standing standing_of(const AttendArgs& a, uint32_t keys, uint32_t prompt) {
   uint64_t total = 0, before = 0;
   uint32_t mine = 0;
-  for (uint32_t i = threadIdx.x % 32; i < a.prompts; i += 32) {
-    const uint32_t n = (length_of(a.prefix_len, a.prefix_cap, i) + keys - 1) / keys;
-    total += n;
-    before += i < prompt ? n : 0;
-    mine += i == prompt ? n : 0;
+  if (((a.prefix_cap + keys - 1) / keys) * a.prompts < 1ull << 31) {  // sums of 32 bits, an instruction each
+    uint32_t all = 0, ahead = 0;
+    for (uint32_t i = threadIdx.x % 32; i < a.prompts; i += 32) {
+      const uint32_t n = (length_of(a.prefix_len, a.prefix_cap, i) + keys - 1) / keys;
+      all += n;
+      ahead += i < prompt ? n : 0;
+      mine += i == prompt ? n : 0;
+    }
+    total = __reduce_add_sync(~0u, all);
+    before = __reduce_add_sync(~0u, ahead);
+  } else {
+    for (uint32_t i = threadIdx.x % 32; i < a.prompts; i += 32) {
+      const uint32_t n = (length_of(a.prefix_len, a.prefix_cap, i) + keys - 1) / keys;
+      total += n;
+      before += i < prompt ? n : 0;
+      mine += i == prompt ? n : 0;
+    }
+    total = sum_lanes(total);
+    before = sum_lanes(before);
   }
-  return {sum_lanes(total), sum_lanes(before), __reduce_add_sync(~0u, mine)};
+  return {total, before, __reduce_add_sync(~0u, mine)};
 }
 __device__ __forceinline__ Owners owners_of(const AttendArgs& a, const AttendPlan& plan, const Standing& s, uint32_t prompt, uint32_t inner) {
   const uint32_t inners = a.kv_heads * plan.row_tiles;

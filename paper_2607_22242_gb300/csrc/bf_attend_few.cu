@@ -10,6 +10,9 @@
 // 16 queries a key the memory is the bound, and a tile of 128 queries would be empty.
 //
 // Behind its own keys a block waits for the prompts' pieces and joins all of them.
+//
+// Where there are units enough to give every warp one of its own (kAlone), it does: what
+// a warp does once (finding its pieces, joining) was two thirds of the instructions.
 #include <cooperative_groups.h>
 
 #include "bf_attend.cuh"
@@ -21,10 +24,11 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr uint32_t kThreads = 128, kWarps = kThreads / 32, kRows = 16, kMostBlocks = 8;
+constexpr uint64_t kAloneUnits = 1216;  // eight an SM
 constexpr float kRaise = 8.0f;
 
 struct FewArgs {
-  uint32_t row_tiles, blocks;  // of a key head's query heads; of a cluster
+  uint32_t row_tiles, blocks, units;  // of a key head's query heads; of a cluster; answers times key heads times row tiles
 };
 
 // d += a b, 16 x 8 x 16.
@@ -49,6 +53,7 @@ template <int N>
 __device__ __forceinline__ void copies_wait() {  // all but the last N groups have arrived
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
+__device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch.global.L1 [%0];" ::"l"(p)); }
 // Four 8 x 8 matrices of 16 bits; the address is of row lane % 8 of matrix lane / 8.
 __device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -70,30 +75,48 @@ struct Few {
   // A step's 16 keys, or values: rows of 128 bytes in columns of 64 dimensions, 16-byte
   // pieces at their place exclusive-or the row modulo 8.
   static constexpr uint32_t kTile = 16 * DP * 2;
+  struct Joining {
+    float o[kWarps][kRows][kPitch];
+    float2 piece[kRows][kMostBlocks * kWarps + kTileParts];  // (m, l), then the weight, of the cluster's warps, then of the prompt's
+  };
   union {
     unsigned char ring[kWarps][kStages][2][kTile];
-    float o[kWarps][kRows][kPitch];
+    Joining join;
   };
   float2 sums[kWarps][kRows];
-  float weight[kRows][kMostBlocks * kWarps + kTileParts];  // of the pieces: the cluster's warps', then the prompt's
   float inverse[kRows];
+  static constexpr uint64_t kRings = kWarps * kStages * 2 * kTile;  // all that warps on their own need
 };
 
-template <typename E, uint32_t DP>
+template <typename E, uint32_t DP, bool kAlone>
 __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ AttendPlan plan,
                                                        const __grid_constant__ FewArgs few) {
   extern __shared__ __align__(128) unsigned char raw[];
   Few<DP>& sh = *reinterpret_cast<Few<DP>*>(raw);
   constexpr uint32_t kStages = Few<DP>::kStages, kTile = Few<DP>::kTile, kPieces = DP / 8;  // pieces of a key
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, c = lane % 4;
-  const uint32_t rank = blockIdx.x % few.blocks;
-  uint32_t unit = blockIdx.x / few.blocks;
+  const uint32_t rank = kAlone ? 0 : blockIdx.x % few.blocks;
+  uint32_t unit = kAlone ? blockIdx.x * kWarps + warp : blockIdx.x / few.blocks;
+  if (kAlone && unit >= few.units) return;
   const uint32_t first = unit % few.row_tiles * kRows;
   unit /= few.row_tiles;
   const uint32_t head = unit % a.kv_heads, rows = min(kRows, a.share - first);
   const uint32_t answer = unit / a.kv_heads, prompt = answer / a.per_prompt;
-  const uint32_t len = length_of(a.suffix_len, a.suffix_cap, answer), step = 16 * kWarps * few.blocks;
-  uint32_t at = 16 * (rank * kWarps + warp);
+  // The queries, as first operands of the scores: dimensions 16 j + 2 c + (0 1 | 8 9) of rows g and g + 8.
+  uint32_t q[DP / 16][4];
+  {
+    const E* base = static_cast<const E*>(a.q.data) + (int64_t)answer * a.q.batch + (int64_t)(head * a.share + first) * a.q.head;
+    const auto two = [&](uint32_t row, uint32_t d) {
+      return row < rows && d < a.dim ? __ldg(reinterpret_cast<const uint32_t*>(base + (int64_t)row * a.q.head + d)) : 0u;
+    };
+#pragma unroll
+    for (uint32_t j = 0; j < DP / 16; ++j) {
+      const uint32_t d = 16 * j + 2 * c;
+      q[j][0] = two(g, d), q[j][1] = two(g + 8, d), q[j][2] = two(g, d + 8), q[j][3] = two(g + 8, d + 8);
+    }
+  }
+  const uint32_t len = length_of(a.suffix_len, a.suffix_cap, answer), step = kAlone ? 16 : 16 * kWarps * few.blocks;
+  uint32_t at = kAlone ? 0 : 16 * (rank * kWarps + warp);
 
   // The warp's ring: a lane copies a piece of every (32 / kPieces)-th key.
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(sh.ring[warp]);
@@ -117,19 +140,8 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
     copies_end();
   }
 
-  // The queries, as first operands of the scores: dimensions 16 j + 2 c + (0 1 | 8 9) of rows g and g + 8.
-  uint32_t q[DP / 16][4];
-  {
-    const E* base = static_cast<const E*>(a.q.data) + (int64_t)answer * a.q.batch + (int64_t)(head * a.share + first) * a.q.head;
-    const auto two = [&](uint32_t row, uint32_t d) {
-      return row < rows && d < a.dim ? __ldg(reinterpret_cast<const uint32_t*>(base + (int64_t)row * a.q.head + d)) : 0u;
-    };
-#pragma unroll
-    for (uint32_t j = 0; j < DP / 16; ++j) {
-      const uint32_t d = 16 * j + 2 * c;
-      q[j][0] = two(g, d), q[j][1] = two(g + 8, d), q[j][2] = two(g, d + 8), q[j][3] = two(g + 8, d + 8);
-    }
-  }
+  // What the prompts' kernel wrote is there from here on (it takes whole SMs: blocks of this one hardly start before it ends).
+  wait_for_previous();
   // Who has the prompt's pieces (while the keys are on their way); an answer's rows may lie in two tiles of queries.
   const uint32_t row0 = (answer - prompt * a.per_prompt) * a.share + first;
   const uint32_t tile0 = row0 / plan.rows, rows0 = min(rows, (tile0 + 1) * plan.rows - row0);
@@ -137,6 +149,17 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
   const Owners own0 = owners_of(a, plan, standing, prompt, head * plan.row_tiles + tile0);
   const Owners own1 = rows0 == rows ? own0 : owners_of(a, plan, standing, prompt, head * plan.row_tiles + tile0 + 1);
   const bool bad = bad_answer(a, prompt, answer);
+  // The prompt's records of this answer's rows, on their way into this SM's cache meanwhile.
+  const auto record_of = [&](const Owners& own, uint32_t i) { return plan.prefix + (own.first + i + own.segment) * plan.record; };
+  const uint32_t quads = a.dim / 4, sums_at = record_sums(plan.rows, a.dim), r0 = row0 - tile0 * plan.rows;
+  if (!kAlone) {
+    const uint32_t far = own0.last - own0.first;
+    for (uint32_t i = warp; i < far; i += kWarps) {  // 32 bytes are four rows' sums, or two rows' quads of dimensions
+      const float* record = record_of(own0, i);
+      if (lane < rows0) prefetch(record + sums_at + 2 * (r0 + lane));
+      for (uint32_t n = 2 * lane; n < quads * rows0; n += 64) prefetch(record + record_place(plan.rows, r0 + n % rows0, n / rows0 * 4));
+    }
+  }
   float o[DP / 8][4] = {};
   float m[2] = {kNone, kNone}, l[2] = {0.0f, 0.0f};  // rows g and g + 8
   // Rows of the matrices that this lane gives the addresses of: of keys for the scores, of values for the outputs.
@@ -209,6 +232,70 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
     __syncwarp();
   }
   copies_wait<0>();
+  if constexpr (kAlone) {
+    const float nan = __int_as_float(0x7FC00000);
+    const bool pairs = ((uintptr_t)a.out.data | (uint64_t)a.out.batch * 2 | (uint64_t)a.out.head * 2) % 4 == 0;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      l[r] += __shfl_xor_sync(~0u, l[r], 1);
+      l[r] += __shfl_xor_sync(~0u, l[r], 2);
+      const uint32_t row = g + 8 * r;
+      if (row >= rows) continue;
+      const Owners& own = row < rows0 ? own0 : own1;
+      const uint32_t pr = row < rows0 ? r0 + row : row - rows0, far = own.last - own.first;
+      const float* records = record_of(own, 0);
+      bool odd = bad || l[r] != l[r];
+      float most = m[r];
+#pragma unroll 4
+      for (uint32_t i = 0; i < far; ++i) {
+        const float2 ml = __ldca(reinterpret_cast<const float2*>(records + (uint64_t)i * plan.record + sums_at) + pr);
+        odd |= ml.y != ml.y || __ldca(plan.gave_up + own.first + i) != 0;
+        most = fmaxf(most, ml.x);
+      }
+      const float base = most == kNone ? 0.0f : most, mine = l[r] > 0.0f ? exp2_of(m[r] - base) : 0.0f;
+      float total = l[r] > 0.0f ? mine * l[r] : 0.0f;
+#pragma unroll
+      for (uint32_t n = 0; n < DP / 8; ++n) {
+        o[n][2 * r] = mine > 0.0f ? o[n][2 * r] * mine : 0.0f;
+        o[n][2 * r + 1] = mine > 0.0f ? o[n][2 * r + 1] * mine : 0.0f;
+      }
+      for (uint32_t i = 0; i < far; ++i) {
+        const float* record = records + (uint64_t)i * plan.record;
+        const float2 ml = __ldca(reinterpret_cast<const float2*>(record + sums_at) + pr);
+        float2 x[DP / 8];
+#pragma unroll
+        for (uint32_t n = 0; n < DP / 8; ++n)
+          if (8 * n < a.dim) x[n] = __ldca(reinterpret_cast<const float2*>(record + record_place(plan.rows, pr, 8 * n + 2 * c)));
+        if (!(ml.y > 0.0f)) continue;  // nothing to attend to in that piece
+        const float w = exp2_of(ml.x - base);
+        total = fmaf(w, ml.y, total);
+#pragma unroll
+        for (uint32_t n = 0; n < DP / 8; ++n)
+          if (8 * n < a.dim) {
+            o[n][2 * r] = fmaf(w, x[n].x, o[n][2 * r]);
+            o[n][2 * r + 1] = fmaf(w, x[n].y, o[n][2 * r + 1]);
+          }
+      }
+      const float inv = odd ? nan : total > 0.0f ? 1.0f / total : 0.0f;
+      if (a.lse && c == 0)
+        a.lse[(uint64_t)answer * (a.kv_heads * a.share) + head * a.share + first + row] =
+            odd ? nan : total > 0.0f ? (most + log2f(total)) * 0.693147180559945309f : kNone;
+      E* out = static_cast<E*>(const_cast<void*>(a.out.data)) + (int64_t)answer * a.out.batch +
+               (int64_t)(head * a.share + first + row) * a.out.head + 2 * c;
+#pragma unroll
+      for (uint32_t n = 0; n < DP / 8; ++n)
+        if (8 * n < a.dim) {
+          const uint32_t u = pack2(make_float2(o[n][2 * r] * inv, o[n][2 * r + 1] * inv), E());
+          if (pairs) {
+            *reinterpret_cast<uint32_t*>(out + 8 * n) = u;
+          } else {
+            uint16_t* h = reinterpret_cast<uint16_t*>(out + 8 * n);
+            h[0] = (uint16_t)u, h[1] = (uint16_t)(u >> 16);
+          }
+        }
+    }
+    return;
+  }
   __syncthreads();  // the rings are done with: the warps' outputs take their place
   // Element i of o[n] is of row g + i / 2 * 8 and dimension 8 n + 2 c + i % 2.
 #pragma unroll
@@ -220,21 +307,19 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
     if (c == 0) sh.sums[warp][row] = make_float2(m[r], l[r]);
 #pragma unroll
     for (uint32_t n = 0; n < DP / 8; ++n)
-      *reinterpret_cast<float2*>(&sh.o[warp][row][8 * n + 2 * c]) = make_float2(o[n][2 * r], o[n][2 * r + 1]);
+      *reinterpret_cast<float2*>(&sh.join.o[warp][row][8 * n + 2 * c]) = make_float2(o[n][2 * r], o[n][2 * r + 1]);
   }
   const bool clustered = few.blocks > 1;
   cg::cluster_group cluster = cg::this_cluster();
   if (clustered) cluster.sync();
   else __syncthreads();
-  wait_for_previous();
 
   // The weights of a row's pieces: of the warps of all blocks here, and of the prompt's.
   const uint32_t near = few.blocks * kWarps;
   const auto peer = [&](uint32_t b) -> Few<DP>* { return clustered ? cluster.map_shared_rank(&sh, b) : &sh; };
-  const auto record_of = [&](const Owners& own, uint32_t i) { return plan.prefix + (own.first + i + own.segment) * plan.record; };
   for (uint32_t row = warp; row < rows; row += kWarps) {
     const Owners own = row < rows0 ? own0 : own1;
-    const uint32_t r = row < rows0 ? row0 - tile0 * plan.rows + row : row - rows0, far = own.last - own.first;
+    const uint32_t r = row < rows0 ? r0 + row : row - rows0, far = own.last - own.first;
     bool odd = bad;
     float most = kNone;
     for (uint32_t i = lane; i < near + far; i += 32) {
@@ -242,23 +327,22 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
       if (i < near) {
         ml = peer(i / kWarps)->sums[i % kWarps][row];
       } else {
-        ml = __ldcg(reinterpret_cast<const float2*>(record_of(own, i - near) + record_sums(plan.rows, a.dim)) + r);
-        odd |= __ldcg(plan.gave_up + own.first + i - near) != 0;
+        ml = __ldca(reinterpret_cast<const float2*>(record_of(own, i - near) + sums_at) + r);
+        odd |= __ldca(plan.gave_up + own.first + i - near) != 0;
       }
       odd |= ml.y != ml.y;
       most = fmaxf(most, ml.x);
-      sh.weight[row][i] = ml.x;
+      sh.join.piece[row][i] = ml;
     }
 #pragma unroll
     for (int d = 16; d; d /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
     const float base = most == kNone ? 0.0f : most;
     float total = 0.0f;
     for (uint32_t i = lane; i < near + far; i += 32) {
-      const float l = i < near ? peer(i / kWarps)->sums[i % kWarps][row].y
-                               : __ldcg(reinterpret_cast<const float2*>(record_of(own, i - near) + record_sums(plan.rows, a.dim)) + r).y;
-      const float w = l > 0.0f ? exp2_of(sh.weight[row][i] - base) : 0.0f;  // 0: nothing to attend to in that piece
-      sh.weight[row][i] = w;
-      total = fmaf(w, l > 0.0f ? l : 0.0f, total);
+      const float2 ml = sh.join.piece[row][i];
+      const float w = ml.y > 0.0f ? exp2_of(ml.x - base) : 0.0f;  // 0: nothing to attend to in that piece
+      sh.join.piece[row][i].x = w;
+      total = fmaf(w, ml.y > 0.0f ? ml.y : 0.0f, total);
     }
 #pragma unroll
     for (int d = 16; d; d /= 2) total += __shfl_xor_sync(~0u, total, d);
@@ -273,12 +357,11 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
   }
   __syncthreads();
   // Four dimensions of a row to a thread, neighbouring rows to neighbours; the cluster's blocks share them out.
-  const uint32_t quads = a.dim / 4;
   const bool whole = ((uintptr_t)a.out.data | (uint64_t)a.out.batch * 2 | (uint64_t)a.out.head * 2) % 8 == 0;
   for (uint32_t n = rank * kThreads + threadIdx.x; n < rows * quads; n += few.blocks * kThreads) {
     const uint32_t row = n % rows, d = n / rows * 4;
     const Owners& own = row < rows0 ? own0 : own1;
-    const uint32_t r = row < rows0 ? row0 - tile0 * plan.rows + row : row - rows0, far = own.last - own.first;
+    const uint32_t r = row < rows0 ? r0 + row : row - rows0, far = own.last - own.first;
     float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     const auto add = [&](float w, const float4& x) {
       if (w > 0.0f) sum = make_float4(fmaf(w, x.x, sum.x), fmaf(w, x.y, sum.y), fmaf(w, x.z, sum.z), fmaf(w, x.w, sum.w));
@@ -289,15 +372,15 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
       float4 x[kAhead];
 #pragma unroll
       for (uint32_t k = 0; k < kAhead; ++k)
-        if (i + k < far) x[k] = __ldcg(reinterpret_cast<const float4*>(from + (uint64_t)(i + k) * plan.record));
+        if (i + k < far) x[k] = __ldca(reinterpret_cast<const float4*>(from + (uint64_t)(i + k) * plan.record));
 #pragma unroll
       for (uint32_t k = 0; k < kAhead; ++k)
-        if (i + k < far) add(sh.weight[row][near + i + k], x[k]);
+        if (i + k < far) add(sh.join.piece[row][near + i + k].x, x[k]);
     }
     for (uint32_t b = 0; b < few.blocks; ++b) {
       const Few<DP>* them = peer(b);
 #pragma unroll
-      for (uint32_t w = 0; w < kWarps; ++w) add(sh.weight[row][b * kWarps + w], *reinterpret_cast<const float4*>(&them->o[w][row][d]));
+      for (uint32_t w = 0; w < kWarps; ++w) add(sh.join.piece[row][b * kWarps + w].x, *reinterpret_cast<const float4*>(&them->join.o[w][row][d]));
     }
     {
       const float inv = sh.inverse[row];
@@ -324,17 +407,24 @@ bool few_takes(const AttendArgs& a) {
 }
 
 cudaError_t launch_few_queries(const AttendArgs& a, const AttendPlan& plan, cudaStream_t st) {
-  FewArgs f = {(a.share + kRows - 1) / kRows, 1};
+  FewArgs f = {(a.share + kRows - 1) / kRows, 1, 0};
   const uint64_t units = (uint64_t)a.prompts * a.per_prompt * a.kv_heads * f.row_tiles;
-  while (f.blocks < kMostBlocks && units * f.blocks < 304 && a.suffix_cap > 64ull * f.blocks) f.blocks *= 2;
+  if (units > 0x7FFFFFFFu) return cudaErrorInvalidValue;
+  f.units = (uint32_t)units;
+  const bool alone = units >= kAloneUnits;
+  while (!alone && f.blocks < kMostBlocks && units * f.blocks * 2 <= 304 && a.suffix_cap > 64ull * f.blocks) f.blocks *= 2;  // two an SM
   const auto launch = [&](auto kernel, uint64_t shared) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
     if (e != cudaSuccess) return e;
-    return launch_shared(kernel, units * f.blocks, kThreads, f.blocks, true, shared, st, a, plan, f);
+    return launch_shared(kernel, alone ? (units + kWarps - 1) / kWarps : units * f.blocks, kThreads, f.blocks, true, shared, st, a, plan, f);
   };
-  if (a.dtype == BF_BF16)
-    return a.dim <= 64 ? launch(few_kernel<__nv_bfloat16, 64>, sizeof(Few<64>)) : launch(few_kernel<__nv_bfloat16, 128>, sizeof(Few<128>));
-  return a.dim <= 64 ? launch(few_kernel<__half, 64>, sizeof(Few<64>)) : launch(few_kernel<__half, 128>, sizeof(Few<128>));
+  const auto launch_type = [&](auto type) {
+    using E = decltype(type);
+    if (a.dim <= 64)
+      return alone ? launch(few_kernel<E, 64, true>, Few<64>::kRings) : launch(few_kernel<E, 64, false>, sizeof(Few<64>));
+    return alone ? launch(few_kernel<E, 128, true>, Few<128>::kRings) : launch(few_kernel<E, 128, false>, sizeof(Few<128>));
+  };
+  return a.dtype == BF_BF16 ? launch_type(__nv_bfloat16()) : launch_type(__half());
 }
 
 }  // namespace bfk
