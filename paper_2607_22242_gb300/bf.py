@@ -189,8 +189,7 @@ def load(path: str = LIB_PATH):
     lib.bf_embed.argtypes = [mat, vp, f32, mat, vp]
     lib.bf_embed_grad.argtypes = [mat, vp, f32, u32, mat, vp, u64, vp]
     cache, states, table = ctypes.POINTER(Cache), ctypes.POINTER(States), ctypes.POINTER(vp)
-    lib.bf_prefix_attention.argtypes = [cache, cache, cache, cache, cache, ctypes.POINTER(AttentionArgs), cache, vp, vp, u64,
-                                        vp]
+    lib.bf_prefix_attention.argtypes = [vp] * 9 + [u64, vp]  # bf_cache, bf_attention_args by address: prefix_attention
     lib.bf_prefix_attention_workspace.argtypes = [cache, cache, cache, ctypes.POINTER(u64)]
     lib.bf_beam_step.argtypes = [mat, ctypes.POINTER(BeamArgs), vp, vp, vp, vp, vp, vp, u64, vp]
     lib.bf_beam_step_workspace.argtypes = [u64, u32, u64, u32, ctypes.POINTER(u64)]
@@ -747,31 +746,45 @@ class BeamStep(NamedTuple):
     lengths: object
 
 
-def _cache(t, name: str, like=None) -> Cache:
-    """A CUDA tensor (batch x tokens x heads x dim, or batch x heads x dim) on the current device as ``bf_cache``."""
-    import torch
-    code, n = _dtype_code(t.dtype), t.dim()
-    if code is None or not t.is_cuda or n != (3 if like is None else 4):
-        raise ValueError(f"{name} must be a {3 if like is None else 4}-D CUDA tensor of float32, bfloat16 or float16")
-    if t.get_device() != torch._C._cuda_getDevice():
-        raise ValueError(f"{name} is on device {t.get_device()} but device {torch.cuda.current_device()} is current")
-    shape, stride = t.shape, t.stride()
-    if stride[-1] != 1 and shape[-1] > 1:
-        raise ValueError(f"{name} must have contiguous vectors")
-    if n == 3:
-        return Cache(t.data_ptr(), shape[0], 1, shape[1], shape[2], stride[0], 0, stride[1], code, 0)
-    return Cache(t.data_ptr(), *shape, *stride[:3], code, 0)
+class AttentionCall(ctypes.Structure):
+    """What a call of ``bf_prefix_attention`` reads, in one piece."""
+    _fields_ = [("caches", Cache * 6), ("args", AttentionArgs)]  # q, prefix_k, prefix_v, suffix_k, suffix_v, out
+
+
+_CACHE_AT = tuple(i * ctypes.sizeof(Cache) for i in range(6)) + (AttentionCall.args.offset,)
 
 
 @functools.lru_cache(maxsize=256)
-def _attention_bytes(answers: int, heads: int, dim: int, prompts: int, prefix: int, kv_heads: int, suffix: int,
-                     code: int) -> int:
+def _attention_call(shapes, strides, dtypes, scale: Optional[float]):
+    """The parts of a call that only shapes, strides and types decide: (AttentionCall without addresses, bytes of
+    workspace).  The last of the tensors is the output; suffixes may be missing."""
+    call = AttentionCall()
+    for c, shape, stride, dtype in zip(call.caches, shapes, strides, dtypes):
+        if shape is not None:
+            n = 3 - (len(shape) == 3)
+            c.batch, c.heads, c.dim = shape[0], shape[-2], shape[-1]
+            c.tokens, c.token_stride = (1, 0) if n == 2 else (shape[1], stride[1])
+            c.batch_stride, c.head_stride, c.dtype = stride[0], stride[-2], _dtype_code(dtype)
+    call.args.scale = max(1, shapes[0][2]) ** -0.5 if scale is None else scale
+    # Sizes that are refused have no workspace: the call itself says why.
+    probe = AttentionCall.from_buffer_copy(call)
+    for c in probe.caches:
+        c.data, c.batch_stride, c.token_stride, c.head_stride = 256, 0, 0, 0
     need = ctypes.c_uint64(0)
-    make = lambda batch, tokens, h: Cache(256, batch, tokens, h, dim, 0, 0, 0, code, 0)
-    own = None if suffix < 0 else make(answers, suffix, kv_heads)
-    _check(load().bf_prefix_attention_workspace(make(answers, 1, heads), make(prompts, prefix, kv_heads), own,
-                                                ctypes.byref(need)))
-    return need.value
+    at = probe.caches
+    ok = load().bf_prefix_attention_workspace(at[0], at[1], None if shapes[3] is None else at[3], ctypes.byref(need)) == BF_OK
+    return bytes(call), need.value if ok else 256
+
+
+def _check_vectors(t, name: str, dims: int) -> None:
+    """A CUDA tensor of contiguous vectors on the current device."""
+    import torch
+    if _dtype_code(t.dtype) is None or not t.is_cuda or t.dim() != dims:
+        raise ValueError(f"{name} must be a {dims}-D CUDA tensor of float32, bfloat16 or float16")
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} is on device {t.get_device()} but device {torch.cuda.current_device()} is current")
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{name} must have contiguous vectors")
 
 
 def prefix_attention(q, prefix_k, prefix_v, suffix_k=None, suffix_v=None, *, prefix_lengths=None, suffix_lengths=None,
@@ -783,24 +796,41 @@ def prefix_attention(q, prefix_k, prefix_v, suffix_k=None, suffix_v=None, *, pre
     Returns the outputs, of q's shape and type -- with ``lse``, the pair of them and the float32 logarithms of the sums
     of exponentials (answers x heads), by which a caller joins them with attention to other keys."""
     import torch
-    x, pk, pv = _cache(q, "q"), _cache(prefix_k, "prefix_k", q), _cache(prefix_v, "prefix_v", q)
-    sk = None if suffix_k is None else _cache(suffix_k, "suffix_k", q)
-    sv = None if suffix_v is None else _cache(suffix_v, "suffix_v", q)
+    _check_vectors(q, "q", 3)
+    _check_vectors(prefix_k, "prefix_k", 4)
+    _check_vectors(prefix_v, "prefix_v", 4)
+    if suffix_k is not None:
+        _check_vectors(suffix_k, "suffix_k", 4)
+    if suffix_v is not None:
+        _check_vectors(suffix_v, "suffix_v", 4)
+    if out is not None:
+        _check_vectors(out, "out", 3)
     i64 = torch.int64
-    pl = None if prefix_lengths is None else _vector(prefix_lengths, pk.batch, i64, q, "prefix_lengths")
-    sl = None if suffix_lengths is None else _vector(suffix_lengths, x.batch, i64, q, "suffix_lengths")
-    if sl is not None and sk is None:
+    pl = None if prefix_lengths is None else _vector(prefix_lengths, prefix_k.shape[0], i64, q, "prefix_lengths")
+    sl = None if suffix_lengths is None else _vector(suffix_lengths, q.shape[0], i64, q, "suffix_lengths")
+    if sl is not None and suffix_k is None:
         raise ValueError("suffix_lengths needs suffix_k")
-    need = _attention_bytes(x.batch, x.heads, x.dim, pk.batch, pk.tokens, pk.heads, -1 if sk is None else sk.tokens, x.dtype)
     given = out
     with _allocate(stream):
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        sums = torch.empty(x.batch, x.heads, dtype=torch.float32, device=q.device) if lse else None
+        tensors = (q, prefix_k, prefix_v, suffix_k, suffix_v, out)
+        made, need = _attention_call(tuple([None if t is None else t.shape for t in tensors]),
+                                     tuple([None if t is None else t.stride() for t in tensors]),
+                                     tuple([None if t is None else t.dtype for t in tensors]), scale)
+        sums = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse else None
         work = torch.empty(need, dtype=torch.uint8, device=q.device)
-    args = AttentionArgs(pl, sl, x.dim ** -0.5 if scale is None else scale, 0)
-    _check(load().bf_prefix_attention(x, pk, pv, sk, sv, args, _cache(out, "out"), sums.data_ptr() if lse else None,
-                                      work.data_ptr(), need, _stream_of(stream, q)))
+    call = AttentionCall.from_buffer_copy(made)
+    at = ctypes.addressof(call)
+    where = [at + i for i in _CACHE_AT]
+    for i, t in enumerate(tensors):
+        if t is None:
+            where[i] = None
+        else:
+            ctypes.c_uint64.from_address(where[i]).value = t.data_ptr()
+    call.args.prefix_lengths, call.args.suffix_lengths = pl, sl
+    _check(load().bf_prefix_attention(where[0], where[1], where[2], where[3], where[4], where[6], where[5],
+                                      sums.data_ptr() if lse else None, work.data_ptr(), need, _stream_of(stream, q)))
     _written(given)
     return (out, sums) if lse else out
 
@@ -835,12 +865,13 @@ def beam_step(logits, scores, beams: int, *, keep: Optional[int] = None, finishe
         best = torch.empty(groups, keep, dtype=torch.float32, device=device)
         whole = torch.empty(2 if lengths is None else 3, groups, keep, dtype=i64, device=device)
         ended = torch.empty(groups, keep, dtype=torch.bool, device=device)
-        work = torch.empty(need, dtype=torch.uint8, device=device)
+        work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
     at, step = whole.data_ptr(), 8 * groups * keep
     _check(load().bf_beam_step(x, args, best.data_ptr(), at, at + step, ended.data_ptr(),
-                               None if lengths is None else at + 2 * step, work.data_ptr(), need,
+                               None if lengths is None else at + 2 * step, work.data_ptr() if need else None, need,
                                _stream_of(stream, logits)))
-    return BeamStep(best, whole[0], whole[1], ended, None if lengths is None else whole[2])
+    tokens, parents, *more = whole.unbind(0)
+    return BeamStep(best, tokens, parents, ended, more[0] if more else None)
 
 
 def _addresses(tensors, name: str):

@@ -12,7 +12,8 @@ namespace {
 // A piece: R query vectors against keys [k0, k1), 64 at a time, on 256 threads.
 // Everything is staged in shared memory in 32 bits; a thread makes 4 rows by
 // R / 16 (scores) or dim / (1024 / R) (outputs) values, so that a value read from
-// shared memory is used four times or more.
+// shared memory is used four times or more.  16 rows are bound by the keys' way here, and
+// have keys and values on it at once; 64 by the sums, and have room for two blocks an SM.
 constexpr uint32_t kThreads = 256, kKeys = 64, kMaxDim = 256;
 
 template <uint32_t R>
@@ -21,12 +22,13 @@ struct Shape {
   static constexpr uint32_t kScores = kKeys / kCols;                            // scores of a thread and row
   static constexpr uint32_t kOuts = kMaxDim / kCols;                            // outputs, at most
   static constexpr uint32_t kRowThreads = kThreads / R;                         // threads of a row's softmax
+  static constexpr bool kBoth = R == 16;                                        // keys and values have places of their own
 };
 
 __host__ __device__ constexpr uint32_t pitch_of(uint32_t dim) { return (dim + 3) / 4 * 4 + 4; }
 template <uint32_t R>
 constexpr uint32_t shared_of(uint32_t dim) {
-  return 4 * ((R + kKeys) * pitch_of(dim) + R * (kKeys + 4) + 3 * R);
+  return 4 * ((R + (Shape<R>::kBoth ? 2 : 1) * kKeys) * pitch_of(dim) + R * (kKeys + 4) + 3 * R);
 }
 
 struct Piece {
@@ -36,13 +38,53 @@ struct Piece {
   float* record;
 };
 
+// Four elements of a row from d on, zeros behind its end; `whole`: addresses allow one read.
 template <typename E>
-__device__ __forceinline__ void stage(float* to, uint32_t pitch, const E* from, int64_t step, uint32_t rows, uint32_t most,
-                                      uint32_t dim) {
-  const uint32_t wide = pitch - 4;
-  for (uint32_t i = threadIdx.x; i < most * wide; i += kThreads) {
-    const uint32_t r = i / wide, d = i % wide;
-    to[r * pitch + d] = r < rows && d < dim ? to_f32(from[(int64_t)r * step + d]) : 0.0f;
+__device__ __forceinline__ float4 four(const E* row, uint32_t d, uint32_t dim, bool whole) {
+  if (whole && d + 4 <= dim) {
+    if constexpr (sizeof(E) == 4) {
+      return __ldg(reinterpret_cast<const float4*>(row + d));
+    } else {
+      const uint2 u = __ldg(reinterpret_cast<const uint2*>(row + d));
+      const float2 lo = unpack2(u.x, E()), hi = unpack2(u.y, E());
+      return make_float4(lo.x, lo.y, hi.x, hi.y);
+    }
+  }
+  float v[4];
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i) v[i] = d + i < dim ? to_f32(row[d + i]) : 0.0f;
+  return make_float4(v[0], v[1], v[2], v[3]);
+}
+template <typename E>
+__device__ __forceinline__ bool whole_quads(const E* from, int64_t step) {
+  return ((uintptr_t)from | (uint64_t)(step * (int64_t)sizeof(E))) % (4 * sizeof(E)) == 0;
+}
+
+// kKeys rows (zeros behind the first `rows`) of one or two matrices: a warp to a row, eight rows of each on their way.
+template <typename E, bool kTwo>
+__device__ __forceinline__ void stage(float* to, const E* from, int64_t step, float* to2, const E* from2, int64_t step2, uint32_t pitch,
+                                      uint32_t rows, uint32_t dim) {
+  constexpr uint32_t kWarps = kThreads / 32, kAhead = kKeys / kWarps;
+  const bool whole = whole_quads(from, step), whole2 = kTwo && whole_quads(from2, step2);
+  const uint32_t warp = threadIdx.x / 32;
+  for (uint32_t d = threadIdx.x % 32 * 4; d < pitch - 4; d += 128) {
+    float4 x[kAhead], y[kTwo ? kAhead : 1];
+#pragma unroll
+    for (uint32_t i = 0; i < kAhead; ++i) {
+      const uint32_t r = warp + i * kWarps;
+      x[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (kTwo) y[i] = x[i];
+      if (r < rows) {
+        x[i] = four(from + (int64_t)r * step, d, dim, whole);
+        if (kTwo) y[i] = four(from2 + (int64_t)r * step2, d, dim, whole2);
+      }
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kAhead; ++i) {
+      const uint32_t r = warp + i * kWarps;
+      *reinterpret_cast<float4*>(to + r * pitch + d) = x[i];
+      if (kTwo) *reinterpret_cast<float4*>(to2 + r * pitch + d) = y[i];
+    }
   }
 }
 
@@ -51,7 +93,8 @@ template <typename E, uint32_t R>
 __device__ void piece(const Piece& p, uint32_t rows, uint32_t dim, float* sm) {
   using S = Shape<R>;
   const uint32_t pitch = pitch_of(dim), t = threadIdx.x, rg = t / S::kCols, cg = t % S::kCols;
-  float *qs = sm, *kv = qs + R * pitch, *ps = kv + kKeys * pitch, *ms = ps + R * (kKeys + 4), *ls = ms + R, *as = ls + R;
+  float *qs = sm, *ks = qs + R * pitch, *vs = S::kBoth ? ks + kKeys * pitch : ks, *ps = vs + kKeys * pitch,
+        *ms = ps + R * (kKeys + 4), *ls = ms + R, *as = ls + R;
   float o[4][S::kOuts] = {};
   if (t < R) {
     ms[t] = kNone;
@@ -59,7 +102,8 @@ __device__ void piece(const Piece& p, uint32_t rows, uint32_t dim, float* sm) {
   }
   for (uint32_t k = p.k0; k < p.k1; k += kKeys) {
     const uint32_t n = min(kKeys, p.k1 - k);
-    stage<E>(kv, pitch, static_cast<const E*>(p.k) + (int64_t)k * p.k_token, p.k_token, n, kKeys, dim);
+    const E *key0 = static_cast<const E*>(p.k) + (int64_t)k * p.k_token, *value0 = static_cast<const E*>(p.v) + (int64_t)k * p.v_token;
+    stage<E, S::kBoth>(ks, key0, p.k_token, vs, value0, p.v_token, pitch, n, dim);
     __syncthreads();
     float s[4][S::kScores] = {};
     for (uint32_t d = 0; d < pitch - 4; d += 4) {
@@ -67,7 +111,7 @@ __device__ void piece(const Piece& p, uint32_t rows, uint32_t dim, float* sm) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) q[i] = *reinterpret_cast<const float4*>(qs + (rg * 4 + i) * pitch + d);
 #pragma unroll
-      for (uint32_t j = 0; j < S::kScores; ++j) c[j] = *reinterpret_cast<const float4*>(kv + (cg + j * S::kCols) * pitch + d);
+      for (uint32_t j = 0; j < S::kScores; ++j) c[j] = *reinterpret_cast<const float4*>(ks + (cg + j * S::kCols) * pitch + d);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -82,7 +126,7 @@ __device__ void piece(const Piece& p, uint32_t rows, uint32_t dim, float* sm) {
         ps[(rg * 4 + i) * (kKeys + 4) + at] = at < n ? s[i][j] : kNone;
       }
     __syncthreads();
-    stage<E>(kv, pitch, static_cast<const E*>(p.v) + (int64_t)k * p.v_token, p.v_token, n, kKeys, dim);
+    if (!S::kBoth) stage<E, false>(vs, value0, p.v_token, vs, value0, p.v_token, pitch, n, dim);
     {
       const uint32_t row = t / S::kRowThreads, mine = t % S::kRowThreads;
       float* x = ps + row * (kKeys + 4);
@@ -125,7 +169,7 @@ __device__ void piece(const Piece& p, uint32_t rows, uint32_t dim, float* sm) {
       for (uint32_t c = 0; c < S::kOuts; ++c) {
         const uint32_t d = cg + c * S::kCols;
         if (d >= dim) break;
-        const float v = kv[j * pitch + d];
+        const float v = vs[j * pitch + d];
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i][c] = fmaf(w[i], v, o[i][c]);
       }
@@ -150,24 +194,27 @@ __device__ void piece(const Piece& p, uint32_t rows, uint32_t dim, float* sm) {
   __syncthreads();
 }
 
-// Query vectors [first, first + rows) of a prompt's (or an answer's) for a key head, scaled.
+// Query vectors [first, first + rows) of a prompt's (or an answer's) for a key head, scaled; zeros up to `most`.
 template <typename E>
 __device__ __forceinline__ void stage_q(const AttendArgs& a, float* to, uint64_t answer0, uint32_t head, uint32_t first,
                                         uint32_t rows, uint32_t most) {
-  const uint32_t pitch = pitch_of(a.dim), wide = pitch - 4;
+  const uint32_t pitch = pitch_of(a.dim);
   const E* q = static_cast<const E*>(a.q.data);
-  for (uint32_t i = threadIdx.x; i < most * wide; i += kThreads) {
-    const uint32_t r = i / wide, d = i % wide, at = first + r;
-    float v = 0.0f;
-    if (r < rows && d < a.dim)
-      v = to_f32(q[(int64_t)(answer0 + at / a.share) * a.q.batch + (int64_t)(head * a.share + at % a.share) * a.q.head + d]);
-    to[r * pitch + d] = v * a.scale2;
+  const bool whole = whole_quads(q, a.q.batch) && whole_quads(q, a.q.head);
+#pragma unroll 2
+  for (uint32_t r = threadIdx.x / 32; r < most; r += kThreads / 32) {
+    const uint32_t at = first + r, answer = at / a.share;
+    const E* row = q + (int64_t)(answer0 + answer) * a.q.batch + (int64_t)(head * a.share + at - answer * a.share) * a.q.head;
+    for (uint32_t d = threadIdx.x % 32 * 4; d < pitch - 4; d += 128) {
+      const float4 v = r < rows ? four(row, d, a.dim, whole) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      *reinterpret_cast<float4*>(to + r * pitch + d) = make_float4(v.x * a.scale2, v.y * a.scale2, v.z * a.scale2, v.w * a.scale2);
+    }
   }
   __syncthreads();
 }
 
 template <typename E, uint32_t R>
-__global__ void __launch_bounds__(kThreads) general_kernel(const __grid_constant__ AttendArgs a,
+__global__ void __launch_bounds__(kThreads, 2) general_kernel(const __grid_constant__ AttendArgs a,
                                                            const __grid_constant__ AttendPlan plan) {
   extern __shared__ float sm[];
   let_next_start();
@@ -220,61 +267,68 @@ __global__ void __launch_bounds__(kThreads) general_kernel(const __grid_constant
 
 // ---- joining ----------------------------------------------------------------
 
-// A warp per query vector: its pieces' maxima and sums, then its outputs, a lane to a dimension.
+// A warp per query vector, a lane to a dimension: 32 pieces at a time, a lane to a
+// piece's maximum and sum, and eight pieces' outputs on their way.
 template <typename E>
 __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ AttendArgs a,
                                                         const __grid_constant__ AttendPlan plan) {
   const uint32_t lane = threadIdx.x % 32, heads = a.kv_heads * a.share;
   const uint64_t vec = (uint64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
   if (vec >= (uint64_t)a.prompts * a.per_prompt * heads) return;
-  const uint64_t answer = vec / heads;
-  const uint32_t h = vec % heads, head = h / a.share, prompt = answer / a.per_prompt;
-  const uint32_t row = (answer % a.per_prompt) * a.share + h % a.share;
+  const uint32_t answer = (uint32_t)(vec / heads), h = (uint32_t)vec - answer * heads, head = h / a.share, prompt = answer / a.per_prompt;
+  const uint32_t srow = h - head * a.share, row = (answer - prompt * a.per_prompt) * a.share + srow;
   const Owners own = owners_of(a, plan, standing_of(a, plan.keys, prompt), prompt, head * plan.row_tiles + row / plan.rows);
-  const uint32_t c0 = own.first, c1 = own.last;
-  const uint64_t segment = own.segment;
-  const uint32_t splits = a.suffix_cap ? plan.suffix_splits : 0, pieces = c1 - c0 + splits;
-  const uint32_t srow = h % a.share;
-  const uint64_t sslot = ((answer * a.kv_heads + head) * plan.suffix_row_tiles + srow / plan.suffix_rows) * plan.suffix_splits;
-  const auto record = [&](uint32_t i, uint32_t& rows, uint32_t& r) -> const float* {
-    if (i < c1 - c0) {
-      rows = plan.rows;
-      r = row % plan.rows;
-      return plan.prefix + (c0 + i + segment) * plan.record;
-    }
-    rows = plan.suffix_rows;
-    r = srow % plan.suffix_rows;
-    return plan.suffix + (sslot + (i - (c1 - c0))) * plan.suffix_record;
-  };
+  const uint32_t far = own.last - own.first, splits = a.suffix_cap ? plan.suffix_splits : 0, pieces = far + splits;
+  const float* prefix = plan.prefix + (own.first + own.segment) * plan.record;
+  const uint64_t sslot = (((uint64_t)answer * a.kv_heads + head) * plan.suffix_row_tiles + srow / plan.suffix_rows) * plan.suffix_splits;
+  const float* suffix = plan.suffix + sslot * plan.suffix_record;
+  const uint32_t r0 = row % plan.rows, r1 = srow % plan.suffix_rows;
+  const auto record = [&](uint32_t i) { return i < far ? prefix + (uint64_t)i * plan.record : suffix + (uint64_t)(i - far) * plan.suffix_record; };
   const bool bad = bad_answer(a, prompt, answer);
   wait_for_previous();
-  float m = kNone;
+  float m = kNone, l = 0.0f, o[kMaxDim / 32] = {};
   bool odd = bad;
-  if (plan.gave_up)
-    for (uint32_t c = c0 + lane; c < c1; c += 32) odd |= __ldcg(plan.gave_up + c) != 0;
-  for (uint32_t i = lane; i < pieces; i += 32) {
-    uint32_t rows, r;
-    const float* p = record(i, rows, r);
-    const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + record_sums(rows, a.dim)) + r);
-    m = fmaxf(m, ml.x);
+  for (uint32_t from = 0; from < pieces; from += 32) {
+    const uint32_t i = from + lane, some = min(32u, pieces - from);
+    float2 ml = make_float2(kNone, 0.0f);
+    if (i < pieces) {
+      const uint32_t rows = i < far ? plan.rows : plan.suffix_rows;
+      ml = __ldcg(reinterpret_cast<const float2*>(record(i) + record_sums(rows, a.dim)) + (i < far ? r0 : r1));
+      if (plan.gave_up && i < far) odd |= __ldcg(plan.gave_up + own.first + i) != 0;
+    }
     odd |= ml.y != ml.y;
-  }
+    float to = fmaxf(m, ml.x);
 #pragma unroll
-  for (int d = 16; d; d /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+    for (int d = 16; d; d /= 2) to = fmaxf(to, __shfl_xor_sync(~0u, to, d));
+    const float base = to == kNone ? 0.0f : to, shrink = m == kNone ? 0.0f : exp2_of(m - base);
+    m = to;
+    const float w = ml.y > 0.0f ? exp2_of(ml.x - base) : 0.0f;  // 0: nothing to attend to in that piece
+    float sum = ml.y > 0.0f ? w * ml.y : 0.0f;
+#pragma unroll
+    for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
+    l = fmaf(l, shrink, sum);
+#pragma unroll
+    for (uint32_t c = 0; c < kMaxDim / 32; ++c) o[c] = shrink == 0.0f ? 0.0f : o[c] * shrink;
+#pragma unroll
+    for (uint32_t c = 0; c < kMaxDim / 32; ++c) {
+      const uint32_t d = lane + 32 * c;
+      if (32 * c >= a.dim) break;
+      for (uint32_t k = 0; k < some; k += 8) {
+        float x[8];
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) {
+          const uint32_t p = from + k + j;
+          x[j] = k + j < some && d < a.dim ? __ldcg(record(p) + (p < far ? record_place(plan.rows, r0, d) : record_place(plan.suffix_rows, r1, d))) : 0.0f;
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) {
+          const float f = __shfl_sync(~0u, w, (k + j) % 32);
+          if (k + j < some && f > 0.0f) o[c] = fmaf(f, x[j], o[c]);
+        }
+      }
+    }
+  }
   odd = __any_sync(~0u, odd);
-  const float base = m == kNone ? 0.0f : m;
-  float l = 0.0f, o[kMaxDim / 32] = {};
-  for (uint32_t i = 0; i < pieces; ++i) {
-    uint32_t rows, r;
-    const float* p = record(i, rows, r);
-    const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + record_sums(rows, a.dim)) + r);
-    const float w = exp2_of(ml.x - base);
-    if (!(ml.y > 0.0f)) continue;  // nothing to attend to in this piece: its outputs are 0
-    l = fmaf(w, ml.y, l);
-#pragma unroll
-    for (uint32_t c = 0; c < kMaxDim / 32; ++c)
-      if (lane + 32 * c < a.dim) o[c] = fmaf(w, __ldcg(p + record_place(rows, r, lane + 32 * c)), o[c]);
-  }
   const float nan = __int_as_float(0x7FC00000), inv = odd ? nan : l > 0.0f ? 1.0f / l : 0.0f;
   E* out = static_cast<E*>(const_cast<void*>(a.out.data)) + (int64_t)answer * a.out.batch + (int64_t)h * a.out.head;
 #pragma unroll

@@ -235,17 +235,32 @@ __global__ void __launch_bounds__(kThreads, 4) row_kernel(const __grid_constant_
     } else {
       const Extent matrix(static_cast<const E*>(a.x), (uint64_t)a.groups * a.beams, a.ldx, a.vocab);
       Unaligned<E> raw[V];
+      // All rows' vectors lie alike to 16 bytes; where the block's tile is inside the matrix with what is read beside it, nothing is checked.
+      const uint32_t tile0 = cut + tile * V * kThreads * kW, tile1 = tile0 + V * kThreads * kW;
+      const uintptr_t at = (uintptr_t)x, off = at % 16;
+      if (tile1 <= a.vocab && at - off + tile0 * sizeof(E) >= matrix.begin && at - off + tile1 * sizeof(E) + 16 <= matrix.end) {
+        const uint4* p = reinterpret_cast<const uint4*>(at - off) + first / kW;
 #pragma unroll
-      for (int k = 0; k < V; ++k) {
-        const uint32_t j = first + (uint32_t)k * kThreads * kW;
-        if (j < a.vocab) raw[k].load(x, a.vocab, (int64_t)j, matrix);
-      }
+        for (int k = 0; k < V; ++k) {
+          raw[k].off = (uint32_t)off;
+          raw[k].lo = __ldg(p + k * kThreads);
+          raw[k].hi = off ? __ldg(p + k * kThreads + 1) : make_uint4(0, 0, 0, 0);
+        }
 #pragma unroll
-      for (int k = 0; k < V; ++k) {
-        const uint32_t j = first + (uint32_t)k * kThreads * kW;
-        u[k] = make_uint4(none, none, none, none);
-        if (j + kW <= a.vocab) u[k] = raw[k].take();
-        else if (j < a.vocab) u[k] = load_ends<E>(x + j, 0, (int32_t)(a.vocab - j), none);
+        for (int k = 0; k < V; ++k) u[k] = raw[k].take();
+      } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          const uint32_t j = first + (uint32_t)k * kThreads * kW;
+          if (j < a.vocab) raw[k].load(x, a.vocab, (int64_t)j, matrix);
+        }
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          const uint32_t j = first + (uint32_t)k * kThreads * kW;
+          u[k] = make_uint4(none, none, none, none);
+          if (j + kW <= a.vocab) u[k] = raw[k].take();
+          else if (j < a.vocab) u[k] = load_ends<E>(x + j, 0, (int32_t)(a.vocab - j), none);
+        }
       }
     }
     uint32_t most[V];
@@ -876,7 +891,7 @@ cudaError_t launch_units(const ReorderArgs& a, bool flat, cudaStream_t st) {
 }  // namespace
 
 uint64_t beam_bytes(uint32_t groups, uint32_t beams, uint64_t vocab, uint32_t keep) {
-  uint64_t most = 256;
+  uint64_t most = 0;
   for (uint32_t i = 0; i < 4; ++i) {  // 4 or 8 elements in 16 bytes, aligned or not
     uint32_t vectors;
     uint64_t bytes;

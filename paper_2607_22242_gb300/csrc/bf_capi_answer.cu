@@ -230,7 +230,7 @@ int bf_beam_step(const bf_matrix* logits, const bf_beam_args* args, float* d_sco
   BF_TRY(check_array(d_lengths, 0, 8, "out lengths", who));
   if (d_lengths && !args->lengths && logits->rows) return fail(BF_EINVAL, "%s: out lengths need lengths", who);
   if (args->groups == 0) return BF_OK;
-  BF_TRY(check_workspace(d_workspace, workspace_bytes, need, who));
+  if (need) BF_TRY(check_workspace(d_workspace, workspace_bytes, need, who));
   bfk::BeamArgs a = {};
   a.x = logits->data;
   a.ldx = logits->row_stride;

@@ -21,14 +21,18 @@ def cache(batch=4, tokens=1, heads=4, dim=64, dtype=1, data=SOME, **strides):
     return bf.Cache(data, batch, tokens, heads, dim, s["batch_stride"], s["token_stride"], s["head_stride"], dtype, 0)
 
 
+def at(c):
+    return None if c is None else ctypes.addressof(c)
+
+
 def attend(lib, q=None, pk=None, pv=None, sk=None, sv=None, out=None, lse=None, work=SOME, have=1 << 40, **kw):
     a = dict(prefix_lengths=None, suffix_lengths=None, scale=0.125)
     a.update(kw)
     q, pk = q or cache(), pk or cache(2, 10, 2)
     pv = pv or cache(pk.batch, pk.tokens, pk.heads, pk.dim, pk.dtype)
     out = out or cache(q.batch, 1, q.heads, q.dim, q.dtype, data=FAR)
-    return lib.bf_prefix_attention(q, pk, pv, sk, sv, bf.AttentionArgs(a["prefix_lengths"], a["suffix_lengths"], a["scale"], 0),
-                                   out, lse, work, have, None)
+    args = bf.AttentionArgs(a["prefix_lengths"], a["suffix_lengths"], a["scale"], 0)
+    return lib.bf_prefix_attention(*[at(c) for c in (q, pk, pv, sk, sv, args, out)], lse, work, have, None)
 
 
 BAD_ATTENTION = [
@@ -57,7 +61,7 @@ def test_attention_null(lib):
     args = bf.AttentionArgs(None, None, 0.1, 0)
     for call in ((None, c, c, None, None, args, far), (c, None, c, None, None, args, far), (c, c, None, None, None, args, far),
                  (c, c, c, None, None, None, far), (c, c, c, None, None, args, None)):
-        assert lib.bf_prefix_attention(*call, None, SOME, 1 << 40, None) == bf.BF_EINVAL
+        assert lib.bf_prefix_attention(*[at(v) for v in call], None, SOME, 1 << 40, None) == bf.BF_EINVAL
 
 
 def test_attention_without_answers(lib):
@@ -101,7 +105,8 @@ BAD_BEAMS = [
     dict(args=beams(length_penalty=NAN, lengths=SOME)), dict(args=beams(lengths=SOME + 4)), dict(args=beams(temperature=0.0)),
     dict(args=beams(temperature=1e19)), dict(scores=None), dict(scores=SOME + 1), dict(tokens=None), dict(tokens=SOME + 4),
     dict(parents=None), dict(parents=SOME + 4), dict(lengths=SOME), dict(lengths=SOME + 4, args=beams(lengths=SOME)),
-    dict(work=None), dict(work=SOME + 4), dict(x=mat(cols=5000, stride=5000), have=64),
+    dict(x=mat(cols=5000, stride=5000), work=None), dict(x=mat(cols=5000, stride=5000), work=SOME + 4),
+    dict(x=mat(cols=5000, stride=5000), have=64),
 ]
 
 
@@ -123,7 +128,7 @@ def test_beams_workspace(lib):
     for groups, vocab, keep in ((1, 3, 1), (1, 5000, 4), (8, 5000, 4), (8, 131072, 4), (64, 131072, 256)):
         assert lib.bf_beam_step_workspace(groups, 4, vocab, keep, ctypes.byref(n)) == bf.BF_OK
         sizes.append(n.value)
-        assert n.value % 256 == 0 and n.value > 0
+        assert n.value % 256 == 0
     assert sizes == sorted(sizes)
     for bad in ((1, 0, 10, 1), (1, 257, 10, 1), (1, 4, 10, 0), (1, 4, 10, 257), (1 << 23, 4, 10, 1), (1, 4, 0, 1), (1, 4, (1 << 24) + 1, 1)):
         assert lib.bf_beam_step_workspace(*bad, ctypes.byref(n)) == bf.BF_EINVAL
