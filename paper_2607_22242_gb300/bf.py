@@ -188,9 +188,9 @@ def load(path: str = LIB_PATH):
     lib.bf_preference_loss.argtypes = [mat, ctypes.POINTER(PreferenceArgs), vp, vp, vp, mat, vp, u64, vp]
     lib.bf_embed.argtypes = [mat, vp, f32, mat, vp]
     lib.bf_embed_grad.argtypes = [mat, vp, f32, u32, mat, vp, u64, vp]
-    cache, states, table = ctypes.POINTER(Cache), ctypes.POINTER(States), ctypes.POINTER(vp)
+    states, table = ctypes.POINTER(States), ctypes.POINTER(vp)
     lib.bf_prefix_attention.argtypes = [vp] * 9 + [u64, vp]  # bf_cache, bf_attention_args by address: prefix_attention
-    lib.bf_prefix_attention_workspace.argtypes = [cache, cache, cache, ctypes.POINTER(u64)]
+    lib.bf_prefix_attention_workspace.argtypes = [vp, vp, vp, ctypes.POINTER(u64)]
     lib.bf_beam_step.argtypes = [mat, ctypes.POINTER(BeamArgs), vp, vp, vp, vp, vp, vp, u64, vp]
     lib.bf_beam_step_workspace.argtypes = [u64, u32, u64, u32, ctypes.POINTER(u64)]
     lib.bf_beam_reorder.argtypes = [table, states, table, states, u32, vp, u32, vp, vp]
@@ -751,19 +751,34 @@ class AttentionCall(ctypes.Structure):
     _fields_ = [("caches", Cache * 6), ("args", AttentionArgs)]  # q, prefix_k, prefix_v, suffix_k, suffix_v, out
 
 
-_CACHE_AT = tuple(i * ctypes.sizeof(Cache) for i in range(6)) + (AttentionCall.args.offset,)
+# Where the caches (their addresses first) and the arguments (the lengths' first) are in it, in words.
+_DATA = tuple(i * ctypes.sizeof(Cache) // 8 for i in range(6)) + (AttentionCall.args.offset // 8,)
+
+
+def _check_vectors(shape, stride, dtype, name: str, dims: int) -> None:
+    if _dtype_code(dtype) is None or len(shape) != dims:
+        raise ValueError(f"{name} must be a {dims}-D CUDA tensor of float32, bfloat16 or float16")
+    if stride[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{name} must have contiguous vectors")
 
 
 @functools.lru_cache(maxsize=256)
 def _attention_call(shapes, strides, dtypes, scale: Optional[float]):
     """The parts of a call that only shapes, strides and types decide: (AttentionCall without addresses, bytes of
-    workspace).  The last of the tensors is the output; suffixes may be missing."""
+    workspace).  The last of the tensors is the output (None: contiguous, as the queries); suffixes may be missing."""
+    names = ("q", "prefix_k", "prefix_v", "suffix_k", "suffix_v", "out")
+    for shape, stride, dtype, name in zip(shapes, strides, dtypes, names):
+        if shape is not None:
+            _check_vectors(shape, stride, dtype, name, 3 if name in ("q", "out") else 4)
     call = AttentionCall()
+    if shapes[5] is None:
+        shapes = (*shapes[:5], shapes[0])
+        strides = (*strides[:5], (shapes[0][1] * shapes[0][2], shapes[0][2], 1))
+        dtypes = (*dtypes[:5], dtypes[0])
     for c, shape, stride, dtype in zip(call.caches, shapes, strides, dtypes):
         if shape is not None:
-            n = 3 - (len(shape) == 3)
             c.batch, c.heads, c.dim = shape[0], shape[-2], shape[-1]
-            c.tokens, c.token_stride = (1, 0) if n == 2 else (shape[1], stride[1])
+            c.tokens, c.token_stride = (1, 0) if len(shape) == 3 else (shape[1], stride[1])
             c.batch_stride, c.head_stride, c.dtype = stride[0], stride[-2], _dtype_code(dtype)
     call.args.scale = max(1, shapes[0][2]) ** -0.5 if scale is None else scale
     # Sizes that are refused have no workspace: the call itself says why.
@@ -771,20 +786,9 @@ def _attention_call(shapes, strides, dtypes, scale: Optional[float]):
     for c in probe.caches:
         c.data, c.batch_stride, c.token_stride, c.head_stride = 256, 0, 0, 0
     need = ctypes.c_uint64(0)
-    at = probe.caches
+    at = [ctypes.addressof(c) for c in probe.caches]
     ok = load().bf_prefix_attention_workspace(at[0], at[1], None if shapes[3] is None else at[3], ctypes.byref(need)) == BF_OK
     return bytes(call), need.value if ok else 256
-
-
-def _check_vectors(t, name: str, dims: int) -> None:
-    """A CUDA tensor of contiguous vectors on the current device."""
-    import torch
-    if _dtype_code(t.dtype) is None or not t.is_cuda or t.dim() != dims:
-        raise ValueError(f"{name} must be a {dims}-D CUDA tensor of float32, bfloat16 or float16")
-    if t.get_device() != torch._C._cuda_getDevice():
-        raise ValueError(f"{name} is on device {t.get_device()} but device {torch.cuda.current_device()} is current")
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
-        raise ValueError(f"{name} must have contiguous vectors")
 
 
 def prefix_attention(q, prefix_k, prefix_v, suffix_k=None, suffix_v=None, *, prefix_lengths=None, suffix_lengths=None,
@@ -796,15 +800,14 @@ def prefix_attention(q, prefix_k, prefix_v, suffix_k=None, suffix_v=None, *, pre
     Returns the outputs, of q's shape and type -- with ``lse``, the pair of them and the float32 logarithms of the sums
     of exponentials (answers x heads), by which a caller joins them with attention to other keys."""
     import torch
-    _check_vectors(q, "q", 3)
-    _check_vectors(prefix_k, "prefix_k", 4)
-    _check_vectors(prefix_v, "prefix_v", 4)
-    if suffix_k is not None:
-        _check_vectors(suffix_k, "suffix_k", 4)
-    if suffix_v is not None:
-        _check_vectors(suffix_v, "suffix_v", 4)
-    if out is not None:
-        _check_vectors(out, "out", 3)
+    tensors = (q, prefix_k, prefix_v, suffix_k, suffix_v, out)
+    made, need = _attention_call(tuple([None if t is None else t.shape for t in tensors]),
+                                 tuple([None if t is None else t.stride() for t in tensors]),
+                                 tuple([None if t is None else t.dtype for t in tensors]), scale)
+    current = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != current:
+            raise ValueError(f"a tensor is on {t.device} but device {torch.cuda.current_device()} is current")
     i64 = torch.int64
     pl = None if prefix_lengths is None else _vector(prefix_lengths, prefix_k.shape[0], i64, q, "prefix_lengths")
     sl = None if suffix_lengths is None else _vector(suffix_lengths, q.shape[0], i64, q, "suffix_lengths")
@@ -813,23 +816,21 @@ def prefix_attention(q, prefix_k, prefix_v, suffix_k=None, suffix_v=None, *, pre
     given = out
     with _allocate(stream):
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        tensors = (q, prefix_k, prefix_v, suffix_k, suffix_v, out)
-        made, need = _attention_call(tuple([None if t is None else t.shape for t in tensors]),
-                                     tuple([None if t is None else t.stride() for t in tensors]),
-                                     tuple([None if t is None else t.dtype for t in tensors]), scale)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         sums = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse else None
         work = torch.empty(need, dtype=torch.uint8, device=q.device)
-    call = AttentionCall.from_buffer_copy(made)
-    at = ctypes.addressof(call)
-    where = [at + i for i in _CACHE_AT]
-    for i, t in enumerate(tensors):
-        if t is None:
-            where[i] = None
-        else:
-            ctypes.c_uint64.from_address(where[i]).value = t.data_ptr()
-    call.args.prefix_lengths, call.args.suffix_lengths = pl, sl
-    _check(load().bf_prefix_attention(where[0], where[1], where[2], where[3], where[4], where[6], where[5],
+    call = bytearray(made)
+    words = memoryview(call).cast("Q")
+    words[_DATA[0]], words[_DATA[1]], words[_DATA[2]] = q.data_ptr(), prefix_k.data_ptr(), prefix_v.data_ptr()
+    if suffix_k is not None:
+        words[_DATA[3]] = suffix_k.data_ptr()
+    if suffix_v is not None:
+        words[_DATA[4]] = suffix_v.data_ptr()
+    words[_DATA[5]] = out.data_ptr()
+    words[_DATA[6]], words[_DATA[6] + 1] = pl or 0, sl or 0
+    at = ctypes.addressof(ctypes.c_char.from_buffer(call))
+    _check(load().bf_prefix_attention(at, at + 8 * _DATA[1], at + 8 * _DATA[2], None if suffix_k is None else at + 8 * _DATA[3],
+                                      None if suffix_v is None else at + 8 * _DATA[4], at + 8 * _DATA[6], at + 8 * _DATA[5],
                                       sums.data_ptr() if lse else None, work.data_ptr(), need, _stream_of(stream, q)))
     _written(given)
     return (out, sums) if lse else out

@@ -25,6 +25,10 @@ def at(c):
     return None if c is None else ctypes.addressof(c)
 
 
+def workspace(lib, q, pk, sk, n):
+    return lib.bf_prefix_attention_workspace(at(q), at(pk), at(sk), n)
+
+
 def attend(lib, q=None, pk=None, pv=None, sk=None, sv=None, out=None, lse=None, work=SOME, have=1 << 40, **kw):
     a = dict(prefix_lengths=None, suffix_lengths=None, scale=0.125)
     a.update(kw)
@@ -73,13 +77,13 @@ def test_attention_workspace(lib):
     n = ctypes.c_uint64(0)
     sizes = []
     for answers, tokens in ((2, 1), (4, 100), (64, 100), (256, 1000)):
-        assert lib.bf_prefix_attention_workspace(cache(answers), cache(2, tokens, 2), cache(answers, tokens, 2), ctypes.byref(n)) == bf.BF_OK
+        assert workspace(lib, cache(answers), cache(2, tokens, 2), cache(answers, tokens, 2), ctypes.byref(n)) == bf.BF_OK
         sizes.append(n.value)
         assert n.value % 256 == 0 and n.value > 0
     assert sizes == sorted(sizes)
-    assert lib.bf_prefix_attention_workspace(cache(), cache(2, 10, 2), None, ctypes.byref(n)) == bf.BF_OK
-    assert lib.bf_prefix_attention_workspace(cache(), cache(2, 10, 2), None, None) == bf.BF_EINVAL
-    assert lib.bf_prefix_attention_workspace(cache(3), cache(2, 10, 2), None, ctypes.byref(n)) == bf.BF_EINVAL
+    assert workspace(lib, cache(), cache(2, 10, 2), None, ctypes.byref(n)) == bf.BF_OK
+    assert workspace(lib, cache(), cache(2, 10, 2), None, None) == bf.BF_EINVAL
+    assert workspace(lib, cache(3), cache(2, 10, 2), None, ctypes.byref(n)) == bf.BF_EINVAL
 
 
 def mat(rows=8, cols=50, stride=50, dtype=1, data=SOME):
