@@ -191,7 +191,7 @@ def load(path: str = LIB_PATH):
     states, table = ctypes.POINTER(States), ctypes.POINTER(vp)
     lib.bf_prefix_attention.argtypes = [vp] * 9 + [u64, vp]  # bf_cache, bf_attention_args by address: prefix_attention
     lib.bf_prefix_attention_workspace.argtypes = [vp, vp, vp, ctypes.POINTER(u64)]
-    lib.bf_beam_step.argtypes = [mat, ctypes.POINTER(BeamArgs), vp, vp, vp, vp, vp, vp, u64, vp]
+    lib.bf_beam_step.argtypes = [vp] * 8 + [u64, vp]  # bf_matrix, bf_beam_args by address: beam_step
     lib.bf_beam_step_workspace.argtypes = [u64, u32, u64, u32, ctypes.POINTER(u64)]
     lib.bf_beam_reorder.argtypes = [table, states, table, states, u32, vp, u32, vp, vp]
     for name in ("bf_policy_loss_workspace", "bf_preference_loss_workspace", "bf_embed_grad_workspace"):
@@ -836,11 +836,31 @@ def prefix_attention(q, prefix_k, prefix_v, suffix_k=None, suffix_v=None, *, pre
     return (out, sums) if lse else out
 
 
+class BeamCall(ctypes.Structure):
+    """What a call of ``bf_beam_step`` reads, in one piece."""
+    _fields_ = [("logits", Matrix), ("args", BeamArgs)]
+
+
+_BEAM_ARGS = BeamCall.args.offset // 8
+
+
 @functools.lru_cache(maxsize=256)
-def _beam_bytes(groups: int, beams: int, vocab: int, keep: int) -> int:
+def _beam_call(shape, stride, dtype, beams: int, keep: int, end_token: int, penalty: float, temperature: float):
+    """The parts of a call that do not hold addresses: (BeamCall without them, groups, bytes of workspace)."""
+    code = _dtype_code(dtype)
+    if code is None or len(shape) != 2:
+        raise ValueError("logits must be a 2-D CUDA tensor of float32, bfloat16 or float16")
+    rows, cols = shape
+    if stride[1] != 1 and cols > 1 and rows:
+        raise ValueError("logits must have contiguous rows")
+    if not 1 <= beams <= MAX_BEAMS or rows % beams:
+        raise ValueError(f"beams must be 1 to {MAX_BEAMS} and a divisor of the rows")
+    groups = rows // beams
+    x = Matrix(None, rows, cols, max(stride[0], cols) if rows <= 1 else stride[0], code, 0)
     need = ctypes.c_uint64(0)
-    _check(load().bf_beam_step_workspace(groups, beams, vocab, keep, ctypes.byref(need)))
-    return need.value
+    _check(load().bf_beam_step_workspace(groups, beams, cols, keep, ctypes.byref(need)))
+    return (bytes(BeamCall(x, BeamArgs(None, None, None, groups, beams, keep, end_token, penalty, temperature))), groups,
+            need.value)
 
 
 def beam_step(logits, scores, beams: int, *, keep: Optional[int] = None, finished=None, lengths=None,
@@ -851,25 +871,27 @@ def beam_step(logits, scores, beams: int, *, keep: Optional[int] = None, finishe
     length ** length_penalty, from the beams' `lengths` (int64, one per row).  Places without a continuation have score
     -inf and token -1."""
     import torch
-    x = _matrix(logits, "logits")
-    if not 1 <= beams <= MAX_BEAMS or x.rows % beams:
-        raise ValueError(f"beams must be 1 to {MAX_BEAMS} and a divisor of the rows")
     keep = beams if keep is None else keep
-    groups = x.rows // beams
-    args = BeamArgs(_vector(scores, x.rows, torch.float32, logits, "scores"),
-                    None if finished is None else _vector(finished, x.rows, torch.bool, logits, "finished"),
-                    None if lengths is None else _vector(lengths, x.rows, torch.int64, logits, "lengths"),
-                    groups, beams, keep, end_token, length_penalty, temperature)
-    need = _beam_bytes(groups, beams, x.cols, keep)
-    device, i64 = logits.device, torch.int64
+    made, groups, need = _beam_call(logits.shape, logits.stride(), logits.dtype, beams, keep, end_token, length_penalty, temperature)
+    if logits.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"logits is on {logits.device} but device {torch.cuda.current_device()} is current")
+    rows, device, i64 = logits.shape[0], logits.device, torch.int64
+    call = bytearray(made)
+    words = memoryview(call).cast("Q")
+    words[0] = logits.data_ptr()
+    words[_BEAM_ARGS] = _vector(scores, rows, torch.float32, logits, "scores")
+    if finished is not None:
+        words[_BEAM_ARGS + 1] = _vector(finished, rows, torch.bool, logits, "finished")
+    if lengths is not None:
+        words[_BEAM_ARGS + 2] = _vector(lengths, rows, i64, logits, "lengths")
     with _allocate(stream):
         best = torch.empty(groups, keep, dtype=torch.float32, device=device)
         whole = torch.empty(2 if lengths is None else 3, groups, keep, dtype=i64, device=device)
         ended = torch.empty(groups, keep, dtype=torch.bool, device=device)
         work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    at, step = whole.data_ptr(), 8 * groups * keep
-    _check(load().bf_beam_step(x, args, best.data_ptr(), at, at + step, ended.data_ptr(),
-                               None if lengths is None else at + 2 * step, work.data_ptr() if need else None, need,
+    at, to, step = ctypes.addressof(ctypes.c_char.from_buffer(call)), whole.data_ptr(), 8 * groups * keep
+    _check(load().bf_beam_step(at, at + 8 * _BEAM_ARGS, best.data_ptr(), to, to + step, ended.data_ptr(),
+                               None if lengths is None else to + 2 * step, work.data_ptr() if need else None, need,
                                _stream_of(stream, logits)))
     tokens, parents, *more = whole.unbind(0)
     return BeamStep(best, tokens, parents, ended, more[0] if more else None)

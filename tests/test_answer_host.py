@@ -97,7 +97,8 @@ def beams(**kw):
 
 
 def step(lib, x=None, args=None, scores=SOME, tokens=SOME, parents=SOME, finished=None, lengths=None, work=SOME, have=1 << 30):
-    return lib.bf_beam_step(x or mat(), args or beams(), scores, tokens, parents, finished, lengths, work, have, None)
+    x, args = x or mat(), args or beams()
+    return lib.bf_beam_step(at(x), at(args), scores, tokens, parents, finished, lengths, work, have, None)
 
 
 BAD_BEAMS = [
@@ -121,8 +122,9 @@ def test_bad_beams(lib, i):
 
 
 def test_beams_null_and_none(lib):
-    assert lib.bf_beam_step(None, beams(), SOME, SOME, SOME, None, None, SOME, 1 << 30, None) == bf.BF_EINVAL
-    assert lib.bf_beam_step(mat(), None, SOME, SOME, SOME, None, None, SOME, 1 << 30, None) == bf.BF_EINVAL
+    x, args = mat(), beams()
+    assert lib.bf_beam_step(None, at(args), SOME, SOME, SOME, None, None, SOME, 1 << 30, None) == bf.BF_EINVAL
+    assert lib.bf_beam_step(at(x), None, SOME, SOME, SOME, None, None, SOME, 1 << 30, None) == bf.BF_EINVAL
     assert step(lib, x=mat(rows=0, data=None), args=beams(groups=0, scores=None), scores=None, tokens=None, parents=None, work=None, have=0) == bf.BF_OK
 
 
