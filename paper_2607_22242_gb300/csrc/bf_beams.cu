@@ -77,20 +77,26 @@ __device__ __forceinline__ uint32_t bound_of(uint32_t mine, uint32_t keep, uint3
   const uint32_t bound = __reduce_max_sync(~0u, lane < count && above == need - 1 ? w : 0);
   return max(bound, kOrderMinusInf + 1);
 }
-// Where one warp's may be far above another's (beams of different scores): bisection.
-__device__ __forceinline__ uint32_t bound_by_halves(uint32_t mine, uint32_t keep) {
-  uint32_t lo = kOrderMinusInf + 1, hi = 0xFFFFFFFFu;
-  if ((uint32_t)__syncthreads_count(mine >= lo) <= keep) return lo;
-  while (hi - lo > 1) {
-    const uint32_t mid = lo + (hi - lo) / 2, n = __syncthreads_count(mine >= mid);
-    if (n >= keep) {
-      lo = mid;
-      if (n <= keep + keep / 4) break;
-    } else {
-      hi = mid;
+// Where one warp's may be far above another's (beams of different scores): the keep-th
+// largest of the first `some` threads' values itself, by counting.  `all` holds a word for each thread.
+__device__ __forceinline__ uint32_t exact_of(uint32_t mine, uint32_t keep, uint32_t some, uint32_t* all, uint32_t* bound) {
+  const uint32_t t = threadIdx.x;
+  all[t] = t < some ? mine : 0;
+  if (t == 0) *bound = kOrderMinusInf + 1;
+  __syncthreads();
+  if (t < some && mine > kOrderMinusInf) {  // the bound is above -inf
+    uint32_t above = 0;
+#pragma unroll 4
+    for (uint32_t i = 0; i < some; i += 4) {
+      const uint4 o = *reinterpret_cast<const uint4*>(all + i);
+      const uint32_t least = i < t / 4 * 4 ? mine : mine + 1;  // of those ahead, equal ones are above
+      above += (o.x >= least) + (o.y >= least) + (o.z >= least) + (o.w >= least);
     }
+    for (uint32_t i = t / 4 * 4; i < t; ++i) above += all[i] == mine;
+    if (above == keep - 1) *bound = mine;
   }
-  return lo;
+  __syncthreads();
+  return *bound;
 }
 
 // Where a list would overflow (many equal values): the exact keep-th largest of
@@ -355,6 +361,8 @@ __global__ void __launch_bounds__(kThreads, 4) row_kernel(const __grid_constant_
   }
 }
 
+__device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch.global.L1 [%0];" ::"l"(p)); }
+
 // ---- groups -----------------------------------------------------------------
 
 enum BeamState : uint32_t { kDead, kAlive, kFinished };
@@ -501,7 +509,8 @@ struct Group {
 template <typename E>
 __global__ void __launch_bounds__(kThreads) direct_kernel(const __grid_constant__ BeamArgs a) {
   extern __shared__ __align__(16) unsigned char raw[];
-  __shared__ uint32_t words[2], sums;
+  __shared__ uint32_t words[2], sums, bound_word;
+  __shared__ __align__(16) uint32_t all[kThreads];
   const uint32_t t = threadIdx.x, slots = a.beams * a.vocab, warp = t / 32, lane = t % 32;
   Group g(a, raw, slots, words);
   float* logits = reinterpret_cast<float*>(g.list + g.most_listed);
@@ -551,7 +560,7 @@ __global__ void __launch_bounds__(kThreads) direct_kernel(const __grid_constant_
   if (slots > 2 * a.keep && slots > 128 && a.keep <= blockDim.x) {
     uint32_t most = 0;
     each([&](uint32_t b, uint32_t, float x) { most = max(most, (uint32_t)(g.key_of(b, x) >> 32)); });
-    const uint32_t bound = bound_by_halves(most, a.keep);
+    const uint32_t bound = exact_of(most, a.keep, blockDim.x, all, &bound_word);
     least = bound == kOrderMinusInf + 1 ? 0 : (uint64_t)bound << 32;
   }
   const auto each_key = [=](auto f) {
@@ -571,16 +580,21 @@ constexpr uint32_t kLists = 4096;  // of a group that are noted as gone through
 // eight lanes to a list, up to their first that does not.
 __global__ void __launch_bounds__(kThreads) group_kernel(const __grid_constant__ BeamArgs a, const __grid_constant__ Chunks ch) {
   extern __shared__ __align__(16) unsigned char raw[];
-  __shared__ uint32_t words[2], sums, going;
+  __shared__ uint32_t words[2], sums, going, bound_word;
+  __shared__ __align__(16) uint32_t tops[kThreads];
   const uint32_t t = threadIdx.x, chunks = a.beams * ch.per_row;
   Group g(a, raw, (uint64_t)chunks * a.keep, words);
   uint32_t* lists = reinterpret_cast<uint32_t*>(g.list + g.most_listed);  // those that are gone through
   if (t == 0) going = 0;
-  wait_for_previous();
   // The beams' sums: as many lanes to a beam as its row has chunks, up to 32.
   uint32_t lanes = 1;
   while (lanes < 32 && lanes < ch.per_row) lanes *= 2;
   const uint32_t mine = t % lanes;
+  for (uint32_t b = t / lanes; b < a.beams; b += kThreads / lanes) {  // into the cache while the rows are worked on
+    prefetch(a.scores + g.row0 + b);
+    if (a.finished) prefetch(a.finished + g.row0 + b);
+  }
+  wait_for_previous();
   for (uint32_t b0 = 0; b0 < a.beams; b0 += kThreads / lanes) {
     const uint32_t b = b0 + t / lanes;
     const uint32_t state = b < a.beams ? g.state_of(b) : (uint32_t)kDead;
@@ -621,12 +635,12 @@ __global__ void __launch_bounds__(kThreads) group_kernel(const __grid_constant__
   if (chunks <= kThreads) {
     uint32_t reached = 0;
     if (t < chunks) reached = (uint32_t)(key_at(t / ch.per_row, t, depth - 1, &tie) >> 32);
-    const uint32_t bound = bound_by_halves(reached, (a.keep + depth - 1) / depth);
+    const uint32_t bound = exact_of(reached, (a.keep + depth - 1) / depth, chunks, tops, &bound_word);
     least = bound == kOrderMinusInf + 1 ? 0 : (uint64_t)bound << 32;
   } else {  // several lists to a thread: the best of each thread's is one of a list
     uint32_t reached = 0;
     for (uint32_t l = t; l < chunks; l += kThreads) reached = max(reached, (uint32_t)(key_at(l / ch.per_row, l, 0, &tie) >> 32));
-    const uint32_t bound = bound_by_halves(reached, a.keep);
+    const uint32_t bound = exact_of(reached, a.keep, kThreads, tops, &bound_word);
     least = bound == kOrderMinusInf + 1 ? 0 : (uint64_t)bound << 32;
   }
   for (uint32_t l = t; l < chunks; l += kThreads) {
