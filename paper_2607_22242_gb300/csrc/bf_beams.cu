@@ -40,7 +40,7 @@ struct Entry {
   Key key;
   uint64_t tie;
 };
-constexpr uint32_t kList = 1024;  // entries of a block's list
+constexpr uint32_t kList = 1024, kRowList = 2048;  // entries of a group's list, and of a chunk's
 
 // The sum of a block's counts (all threads get it); `sums` has two words.
 __device__ __forceinline__ uint32_t block_count(uint32_t mine, uint32_t* sums) {
@@ -58,17 +58,12 @@ __device__ __forceinline__ uint32_t block_count(uint32_t mine, uint32_t* sums) {
 // Where the warps' values are alike: each warp finds its ceil(2 keep / warps)-th
 // largest, and the one of those that enough warps reach is the bound.  One barrier.
 // `warps` holds a word for each warp.
-__device__ __forceinline__ uint32_t bound_of(uint32_t mine, uint32_t keep, uint32_t* warps) {
-  const uint32_t count = blockDim.x / 32, each = min(32u, (2 * keep + count - 1) / count), lane = threadIdx.x % 32;
-  uint32_t most = 0;
-  for (uint32_t i = 0; i < each; ++i) {
-    most = __reduce_max_sync(~0u, mine);
-    if (lane == __ffs(__ballot_sync(~0u, mine == most)) - 1u) mine = 0;
-  }
-  if (lane == 0) warps[threadIdx.x / 32] = most;
+// The need-th largest of the warps' values (the same in all of a warp's lanes).
+__device__ __forceinline__ uint32_t bound_of_warps(uint32_t value, uint32_t need, uint32_t* warps) {
+  const uint32_t count = blockDim.x / 32, lane = threadIdx.x % 32;
+  if (lane == 0) warps[threadIdx.x / 32] = value;
   __syncthreads();
-  // Warps whose values are reached by `each` of theirs: the ceil(keep / each) largest are enough.
-  const uint32_t need = (keep + each - 1) / each, w = lane < count ? warps[lane] : 0;
+  const uint32_t w = lane < count ? warps[lane] : 0;
   uint32_t above = 0;
   for (uint32_t i = 0; i < count; ++i) {
     const uint32_t o = __shfl_sync(~0u, w, i);
@@ -76,6 +71,36 @@ __device__ __forceinline__ uint32_t bound_of(uint32_t mine, uint32_t keep, uint3
   }
   const uint32_t bound = __reduce_max_sync(~0u, lane < count && above == need - 1 ? w : 0);
   return max(bound, kOrderMinusInf + 1);
+}
+__device__ __forceinline__ uint32_t bound_of(uint32_t mine, uint32_t keep, uint32_t* warps) {
+  const uint32_t count = blockDim.x / 32, each = min(32u, (2 * keep + count - 1) / count), lane = threadIdx.x % 32;
+  uint32_t most = 0;
+  for (uint32_t i = 0; i < each; ++i) {
+    most = __reduce_max_sync(~0u, mine);
+    if (lane == __ffs(__ballot_sync(~0u, mine == most)) - 1u) mine = 0;
+  }
+  return bound_of_warps(most, (keep + each - 1) / each, warps);
+}
+// The same from N values of each thread (N times as many: for a `keep` that is large
+// beside the threads), the warps' by bisection.
+template <int N>
+__device__ __forceinline__ uint32_t bound_of_all(const uint32_t (&mine)[N], uint32_t keep, uint32_t* warps) {
+  const uint32_t count = blockDim.x / 32, each = min(32u * N, (2 * keep + count - 1) / count);
+  uint32_t lo = 0, hi = 0xFFFFFFFFu;
+  while (hi - lo > 1) {
+    const uint32_t mid = lo + (hi - lo) / 2;
+    uint32_t n = 0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) n += mine[k] >= mid;
+    n = __reduce_add_sync(~0u, n);
+    if (n >= each) {
+      lo = mid;
+      if (n <= each + each / 8) break;
+    } else {
+      hi = mid;
+    }
+  }
+  return bound_of_warps(lo, (keep + each - 1) / each, warps);
 }
 // Where one warp's may be far above another's (beams of different scores): the keep-th
 // largest of the first `some` threads' values itself, by counting.  `all` holds a word for each thread.
@@ -129,17 +154,42 @@ __device__ __noinline__ void exact_bound(Each each, Key least, uint32_t keep, ui
   *tie = upto;
 }
 
-// Calls put(rank, entry) for the best `keep` of a list of n.
-template <typename Key, typename Put>
-__device__ __forceinline__ void rank_list(const Entry<Key>* list, uint32_t n, uint32_t keep, Put put) {
-  for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) {
-    const Entry<Key> e = list[i];
-    uint32_t rank = 0;
-    for (uint32_t j = 0; j < n; ++j) {
-      const Entry<Key> o = list[j];
-      rank += o.key > e.key || (o.key == e.key && o.tie < e.tie);
+// Puts a list of n (and room for the next power of two) in order, the best first, by
+// exchanges of pairs; `none` is behind all others.
+template <typename T, typename Above>
+__device__ __forceinline__ void sort_list(T* list, uint32_t n, T none, Above above) {
+  uint32_t size = 1;
+  while (size < n) size *= 2;
+  for (uint32_t i = n + threadIdx.x; i < size; i += blockDim.x) list[i] = none;
+  __syncthreads();
+  for (uint32_t run = 2; run <= size; run *= 2)
+    for (uint32_t apart = run / 2; apart; apart /= 2) {
+      for (uint32_t i = threadIdx.x; i < size / 2; i += blockDim.x) {
+        const uint32_t lo = i / apart * 2 * apart + i % apart, hi = lo + apart;
+        const T x = list[lo], y = list[hi];
+        if (above(y, x) == ((lo & run) == 0)) {
+          list[lo] = y;
+          list[hi] = x;
+        }
+      }
+      __syncthreads();
     }
-    if (rank < keep) put(rank, e);
+}
+constexpr uint32_t kRanked = 200;  // up to so many entries are ranked by all others, which takes their square
+
+// Calls put(rank, entry) for the best `keep` of a list of n.
+template <bool kFew, typename T, typename Above, typename Put>
+__device__ __forceinline__ void best_of(T* list, uint32_t n, uint32_t keep, T none, Above above, Put put) {
+  if (kFew || n <= kRanked) {
+    for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) {
+      const T mine = list[i];
+      uint32_t rank = 0;
+      for (uint32_t j = 0; j < n; ++j) rank += above(list[j], mine);
+      if (rank < keep) put(rank, mine);
+    }
+  } else {
+    sort_list(list, n, none, above);
+    for (uint32_t i = threadIdx.x; i < min(n, keep); i += blockDim.x) put(i, list[i]);
   }
 }
 
@@ -151,7 +201,7 @@ struct Candidate {
 };
 
 struct Chunks {
-  uint32_t per_row, elements, tiles;
+  uint32_t per_row, elements, tiles, threads;
   float2* heads;    // [rows][per_row]: maximum, sum of e^((x - maximum) / tau)
   Candidate* best;  // [rows][per_row][keep]
 };
@@ -181,7 +231,7 @@ __device__ __forceinline__ float value_of(uint32_t word, E) {
   const float2 f = unpack2(word, E());
   return fmaxf(f.x, f.y);
 }
-constexpr uint32_t kHits = 256;  // vectors of a chunk that have a candidate
+constexpr uint32_t kHits = 1024;  // vectors of a chunk that have a candidate
 
 // The exponentials of V vectors against m, summed.  (x - m) c2 as x c2 - r, r = m c2
 // rounded, and what r is off by put back into the sum; where m c2 is far from ordinary
@@ -209,14 +259,15 @@ __device__ __forceinline__ float sum_of(const uint4 (&u)[V], float m, float c2) 
 // by addresses, so that equal rows have equal sums.  kAligned: rows start at 16 bytes.
 // What reaches a bound that `keep` of the threads' maxima in the first tile reach may be
 // among the chunk's best: a few more than `keep` in each tile.
-template <typename E, int V, bool kAligned>
-__global__ void __launch_bounds__(kThreads, 4) row_kernel(const __grid_constant__ BeamArgs a, const __grid_constant__ Chunks ch) {
+template <typename E, int V, bool kAligned, uint32_t T>
+__global__ void __launch_bounds__(T, 1024 / T) row_kernel(const __grid_constant__ BeamArgs a, const __grid_constant__ Chunks ch) {
   constexpr uint32_t kW = Vec<E>::kWidth;
-  __shared__ uint64_t list[kList];  // order of the logit, then of the token the other way round
+  constexpr uint32_t kRowList = T == 256 ? bfk::kRowList : 512, kHits = T == 256 ? bfk::kHits : 128;
+  __shared__ uint64_t list[kRowList];  // order of the logit, then of the token the other way round
   __shared__ uint4 hit[kHits];
   __shared__ uint32_t hit_token[kHits];
-  __shared__ uint32_t count, hits, sums, warp_bound[kThreads / 32];
-  __shared__ float warp_max[kThreads / 32], warp_sum[kThreads / 32];
+  __shared__ uint32_t count, hits, sums, warp_bound[T / 32];
+  __shared__ float warp_max[T / 32], warp_sum[T / 32];
   let_next_start();
   const uint32_t row = blockIdx.x / ch.per_row, chunk = blockIdx.x - row * ch.per_row, t = threadIdx.x;
   if (!is_alive(a, row)) return;
@@ -228,12 +279,12 @@ __global__ void __launch_bounds__(kThreads, 4) row_kernel(const __grid_constant_
   uint32_t bound = 0;
 #pragma unroll 1
   for (uint32_t tile = 0; tile < ch.tiles; ++tile) {
-    const uint32_t first = cut + (tile * V * kThreads + t) * kW;
+    const uint32_t first = cut + (tile * V * T + t) * kW;
     uint4 u[V];
     if constexpr (kAligned) {
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        const uint32_t j = first + (uint32_t)k * kThreads * kW;
+        const uint32_t j = first + (uint32_t)k * T * kW;
         u[k] = make_uint4(none, none, none, none);
         if (j + kW <= a.vocab) u[k] = __ldcs(reinterpret_cast<const uint4*>(x + j));
         else if (j < a.vocab) u[k] = load_ends<E>(x + j, 0, (int32_t)(a.vocab - j), none);
@@ -242,27 +293,27 @@ __global__ void __launch_bounds__(kThreads, 4) row_kernel(const __grid_constant_
       const Extent matrix(static_cast<const E*>(a.x), (uint64_t)a.groups * a.beams, a.ldx, a.vocab);
       Unaligned<E> raw[V];
       // All rows' vectors lie alike to 16 bytes; where the block's tile is inside the matrix with what is read beside it, nothing is checked.
-      const uint32_t tile0 = cut + tile * V * kThreads * kW, tile1 = tile0 + V * kThreads * kW;
+      const uint32_t tile0 = cut + tile * V * T * kW, tile1 = tile0 + V * T * kW;
       const uintptr_t at = (uintptr_t)x, off = at % 16;
       if (tile1 <= a.vocab && at - off + tile0 * sizeof(E) >= matrix.begin && at - off + tile1 * sizeof(E) + 16 <= matrix.end) {
         const uint4* p = reinterpret_cast<const uint4*>(at - off) + first / kW;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
           raw[k].off = (uint32_t)off;
-          raw[k].lo = __ldg(p + k * kThreads);
-          raw[k].hi = off ? __ldg(p + k * kThreads + 1) : make_uint4(0, 0, 0, 0);
+          raw[k].lo = __ldg(p + k * T);
+          raw[k].hi = off ? __ldg(p + k * T + 1) : make_uint4(0, 0, 0, 0);
         }
 #pragma unroll
         for (int k = 0; k < V; ++k) u[k] = raw[k].take();
       } else {
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-          const uint32_t j = first + (uint32_t)k * kThreads * kW;
+          const uint32_t j = first + (uint32_t)k * T * kW;
           if (j < a.vocab) raw[k].load(x, a.vocab, (int64_t)j, matrix);
         }
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-          const uint32_t j = first + (uint32_t)k * kThreads * kW;
+          const uint32_t j = first + (uint32_t)k * T * kW;
           u[k] = make_uint4(none, none, none, none);
           if (j + kW <= a.vocab) u[k] = raw[k].take();
           else if (j < a.vocab) u[k] = load_ends<E>(x + j, 0, (int32_t)(a.vocab - j), none);
@@ -282,7 +333,14 @@ __global__ void __launch_bounds__(kThreads, 4) row_kernel(const __grid_constant_
     m = now;
     s += fabsf(m) * a.c2 < 1024.0f ? sum_of<E, V, true>(u, m, a.c2) : sum_of<E, V, false>(u, m, a.c2);
     if (tile == 0) {
-      bound = bound_of(order_of(tmax), a.keep, warp_bound);
+      if (2 * a.keep <= T * 3 / 4) {
+        bound = bound_of(order_of(tmax), a.keep, warp_bound);
+      } else {
+        uint32_t keys[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) keys[k] = order_of(value_of(most[k], E()));
+        bound = bound_of_all<V>(keys, a.keep, warp_bound);
+      }
       least = from_order(bound);
     }
     // First the vectors that have any, then their elements, one to a thread: few threads
@@ -294,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, 4) row_kernel(const __grid_constant_
           const uint32_t at = atomicAdd(&hits, 1u);
           if (at < kHits) {
             hit[at] = u[k];
-            hit_token[at] = first + (uint32_t)k * kThreads * kW;
+            hit_token[at] = first + (uint32_t)k * T * kW;
           }
         }
     }
@@ -312,20 +370,20 @@ __global__ void __launch_bounds__(kThreads, 4) row_kernel(const __grid_constant_
   __syncthreads();
   const uint32_t found = hits;
   const auto entry_of = [](float v, uint32_t token) { return (uint64_t)order_of(v) << 32 | ~token; };
-  for (uint32_t i = t; i < min(found, kHits) * kW; i += kThreads) {
+  for (uint32_t i = t; i < min(found, kHits) * kW; i += T) {
     const uint32_t at = i / kW, j = i % kW;
     const float v = to_f32(reinterpret_cast<const E*>(&hit[at])[j]);
     if (v >= least) {
       const uint32_t to = atomicAdd(&count, 1u);
-      if (to < kList) list[to] = entry_of(v, hit_token[at] + j);
+      if (to < kRowList) list[to] = entry_of(v, hit_token[at] + j);
     }
   }
   __syncthreads();
   uint32_t n = count;
-  if (n > kList || found > kHits) {
+  if (n > kRowList || found > kHits) {
     const uint32_t some = min(ch.elements, a.vocab - cut);
     const auto each = [=](auto f) {
-      for (uint32_t i = t; i < some; i += kThreads) {
+      for (uint32_t i = t; i < some; i += T) {
         const float v = to_f32(x[cut + i]);
         if (v >= least) f(order_of(v), (uint64_t)(cut + i));
       }
@@ -344,19 +402,16 @@ __global__ void __launch_bounds__(kThreads, 4) row_kernel(const __grid_constant_
   }
   const uint64_t record = (uint64_t)row * ch.per_row + chunk;
   Candidate* best = ch.best + record * a.keep;
-  for (uint32_t i = t; i < n; i += kThreads) {
-    const uint64_t mine = list[i];
-    uint32_t rank = 0;
-    for (uint32_t j = 0; j < n; ++j) rank += list[j] > mine;
-    if (rank < a.keep) best[rank] = {from_order((uint32_t)(mine >> 32)), ~(uint32_t)mine};
-  }
-  for (uint32_t i = min(n, a.keep) + t; i < a.keep; i += kThreads) best[i] = {kMinusInf, 0};
+  best_of<false, uint64_t>(
+      list, n, a.keep, 0, [](uint64_t x, uint64_t y) { return x > y; },
+      [&](uint32_t rank, uint64_t e) { best[rank] = {from_order((uint32_t)(e >> 32)), ~(uint32_t)e}; });
+  for (uint32_t i = min(n, a.keep) + t; i < a.keep; i += T) best[i] = {kMinusInf, 0};
   if (t < 32) {
-    const float wm = t < kThreads / 32 ? warp_max[t] : kMinusInf, ws = t < kThreads / 32 ? warp_sum[t] : 0.0f;
+    const float wm = t < T / 32 ? warp_max[t] : kMinusInf, ws = t < T / 32 ? warp_sum[t] : 0.0f;
     const float top = from_order(__reduce_max_sync(~0u, order_of(wm)));
     float total = wm == top ? ws : ws * exp2_of((wm - top) * a.c2);
 #pragma unroll
-    for (int d = 4; d; d /= 2) total += __shfl_xor_sync(~0u, total, d);
+    for (int d = T / 64; d; d /= 2) total += __shfl_xor_sync(~0u, total, d);
     if (t == 0) ch.heads[record] = make_float2(top, total);
   }
 }
@@ -407,7 +462,11 @@ __device__ __forceinline__ Two times(const Two& a, const Two& b) {
 }
 
 // Dynamic shared memory of a group: its beams, its list, and its logits or the numbers of its lists.
-__host__ __device__ __forceinline__ uint32_t list_of(uint64_t slots) { return slots < kList ? (uint32_t)slots : kList; }
+__host__ __device__ __forceinline__ uint32_t list_of(uint64_t slots) {  // a power of two: lists are sorted
+  uint32_t n = 32;
+  while (n < slots && n < kList) n *= 2;
+  return n;
+}
 __host__ __device__ __forceinline__ uint64_t group_bytes(uint32_t beams, uint64_t slots, uint64_t more) {
   return (beams * sizeof(Beam) + 15) / 16 * 16 + list_of(slots) * sizeof(Entry<uint64_t>) + more * 4;
 }
@@ -466,12 +525,12 @@ struct Group {
     const uint32_t at = atomicAdd(count, 1u);
     if (at < most_listed) list[at] = {key, tie};
   }
-  // The best of the list, of all candidates each(f) -> f(key, tie) where they did not fit in.
-  template <typename Each>
+  // The best of the list, of all candidates each(f) -> f(key, tie) where they did not fit in (kFew: they do).
+  template <bool kFew, typename Each>
   __device__ __forceinline__ void finish(Each each, uint32_t* sums) const {
     __syncthreads();
     uint32_t n = *odd ? 0 : *count;
-    if (n > most_listed) {
+    if (!kFew && n > most_listed) {
       uint64_t key, tie;
       exact_bound<uint64_t>(each, (uint64_t)0, a.keep, sums, &key, &tie);
       __syncthreads();
@@ -484,7 +543,8 @@ struct Group {
       n = *count;
     }
     const uint64_t out = (uint64_t)blockIdx.x * a.keep;
-    rank_list(list, n, a.keep, [&](uint32_t rank, const Entry<uint64_t>& e) {
+    const auto above = [](const Entry<uint64_t>& x, const Entry<uint64_t>& y) { return x.key > y.key || (x.key == y.key && x.tie < y.tie); };
+    best_of<kFew, Entry<uint64_t>>(list, n, a.keep, Entry<uint64_t>{0, ~0ull}, above, [&](uint32_t rank, const Entry<uint64_t>& e) {
       const uint32_t b = (uint32_t)(e.tie >> 56);
       const Beam& o = beam[b];
       const bool was = o.state == kFinished;
@@ -505,8 +565,11 @@ struct Group {
   }
 };
 
-// Few logits in a group: all of it in shared memory.
-template <typename E>
+constexpr uint32_t kFewSlots = 128;
+
+// Few logits in a group: all of it in shared memory.  kFew: so few that all of them are ranked (code that is not there
+// is not fetched, which is most of the time of thousands of such groups).
+template <typename E, bool kFew>
 __global__ void __launch_bounds__(kThreads) direct_kernel(const __grid_constant__ BeamArgs a) {
   extern __shared__ __align__(16) unsigned char raw[];
   __shared__ uint32_t words[2], sums, bound_word;
@@ -557,7 +620,7 @@ __global__ void __launch_bounds__(kThreads) direct_kernel(const __grid_constant_
     }
   };
   uint64_t least = 0;
-  if (slots > 2 * a.keep && slots > 128 && a.keep <= blockDim.x) {
+  if (!kFew && slots > 2 * a.keep && a.keep <= blockDim.x) {
     uint32_t most = 0;
     each([&](uint32_t b, uint32_t, float x) { most = max(most, (uint32_t)(g.key_of(b, x) >> 32)); });
     const uint32_t bound = exact_of(most, a.keep, blockDim.x, all, &bound_word);
@@ -570,7 +633,7 @@ __global__ void __launch_bounds__(kThreads) direct_kernel(const __grid_constant_
     });
   };
   each_key([&](uint64_t key, uint64_t tie) { g.push(key, tie); });
-  g.finish(each_key, &sums);
+  g.template finish<kFew>(each_key, &sums);
 }
 
 constexpr uint32_t kLists = 4096;  // of a group that are noted as gone through
@@ -630,61 +693,76 @@ __global__ void __launch_bounds__(kThreads) group_kernel(const __grid_constant__
     *tie = g.tie_of(b, __uint_as_float(c.x), c.y);
     return g.key_of(b, __uint_as_float(c.x));
   };
-  const uint32_t depth = (a.keep + chunks - 1) / chunks;  // so many of each list are enough
+  // Of as many lists as are needed, the depth-th continuation: `keep` reach the least of them.  So deep that
+  // a quarter of the lists is enough; deeper where the list overflows, because few lists hold most of the best.
+  uint32_t depth = min(a.keep, (4 * a.keep + chunks - 1) / chunks);
   uint64_t least = 0, tie;
+  const auto raise = [&](uint32_t mine, uint32_t need) {
+    const uint32_t bound = exact_of(mine, need, min(chunks, kThreads), tops, &bound_word);
+    if (bound > kOrderMinusInf + 1) least = max(least, (uint64_t)bound << 32);
+  };
   if (chunks <= kThreads) {
-    uint32_t reached = 0;
-    if (t < chunks) reached = (uint32_t)(key_at(t / ch.per_row, t, depth - 1, &tie) >> 32);
-    const uint32_t bound = exact_of(reached, (a.keep + depth - 1) / depth, chunks, tops, &bound_word);
-    least = bound == kOrderMinusInf + 1 ? 0 : (uint64_t)bound << 32;
+    raise(t < chunks ? (uint32_t)(key_at(t / ch.per_row, t, depth - 1, &tie) >> 32) : 0, (a.keep + depth - 1) / depth);
   } else {  // several lists to a thread: the best of each thread's is one of a list
-    uint32_t reached = 0;
-    for (uint32_t l = t; l < chunks; l += kThreads) reached = max(reached, (uint32_t)(key_at(l / ch.per_row, l, 0, &tie) >> 32));
-    const uint32_t bound = exact_of(reached, a.keep, kThreads, tops, &bound_word);
-    least = bound == kOrderMinusInf + 1 ? 0 : (uint64_t)bound << 32;
+    uint32_t best_top = 0;
+    for (uint32_t l = t; l < chunks; l += kThreads) best_top = max(best_top, (uint32_t)(key_at(l / ch.per_row, l, 0, &tie) >> 32));
+    raise(best_top, a.keep);
   }
-  for (uint32_t l = t; l < chunks; l += kThreads) {
-    const uint64_t key = key_at(l / ch.per_row, l, 0, &tie);
-    if (key == 0 || key < least) continue;
-    const uint32_t at = atomicAdd(&going, 1u);
-    if (at < kLists) lists[at] = l;
-  }
-  __syncthreads();
-  const bool some = going <= kLists;  // else equal logits all over: all lists are gone through
-  const uint32_t all = some ? going : chunks;
-  const auto each_key = [=](auto f) {
+  const auto each_from = [=](uint64_t from, uint32_t all, bool some, auto f) {
     for (uint32_t n = t / 8; n < all; n += kThreads / 8) {
       const uint32_t l = some ? lists[n] : n, b = l / ch.per_row;
       uint64_t at_tie;
       for (uint32_t i = t % 8; i < a.keep; i += 8) {
         const uint64_t key = key_at(b, l, i, &at_tie);
-        if (key == 0 || key < least) break;  // and so are all behind it
+        if (key == 0 || key < from) break;  // and so are all behind it
         f(key, at_tie);
       }
     }
   };
-  each_key([&](uint64_t key, uint64_t at_tie) { g.push(key, at_tie); });
-  g.finish(each_key, &sums);
+  for (;;) {
+    for (uint32_t l = t; l < chunks; l += kThreads) {
+      const uint64_t key = key_at(l / ch.per_row, l, 0, &tie);
+      if (key == 0 || key < least) continue;
+      const uint32_t at = atomicAdd(&going, 1u);
+      if (at < kLists) lists[at] = l;
+    }
+    __syncthreads();
+    const bool some = going <= kLists;  // else equal logits all over: all lists are gone through
+    const uint32_t all = some ? going : chunks;
+    each_from(least, all, some, [&](uint64_t key, uint64_t at_tie) { g.push(key, at_tie); });
+    __syncthreads();
+    if (*g.count <= g.most_listed || depth == a.keep || *g.odd) {
+      g.finish<false>([=](auto f) { each_from(least, all, some, f); }, &sums);
+      return;
+    }
+    depth = min(a.keep, 4 * depth);
+    raise(t < chunks ? (uint32_t)(key_at(t / ch.per_row, t, depth - 1, &tie) >> 32) : 0, (a.keep + depth - 1) / depth);
+    if (t == 0) *g.count = going = 0;
+    __syncthreads();
+  }
 }
 
 constexpr uint64_t kDirectMost = 4096;  // logits of a group that one block takes as they are
 
 // How rows are cut: 8 vectors a thread (4 where each is put together from two), twice
 // where there are blocks enough all the same (what a block does once takes as long as a tile),
-// 2 where there would be too few for two on each of 152 SMs.
+// 2 where there would be too few for two on each of 152 SMs.  Rows that 64 threads hold in
+// two vectors each have blocks of 64.
+constexpr uint32_t kShort = 64;
 Chunks chunks_of(uint32_t groups, uint32_t beams, uint64_t vocab, uint32_t keep, uint32_t width, bool aligned, void* workspace,
                  uint32_t* vectors, uint64_t* bytes) {
   Chunks c = {};
   *bytes = 0;
   if (beams * vocab <= kDirectMost) return c;
   const uint64_t rows = (uint64_t)groups * beams;
-  const auto per_row = [&](uint32_t v) { return (vocab + kThreads * v * width - 1) / (kThreads * v * width); };
-  *vectors = aligned ? 8 : 4;
   c.tiles = 1;
-  if (rows * per_row(*vectors) < 304) *vectors = 2;
-  else if (rows * per_row(2 * *vectors) >= 1216 && per_row(*vectors) > 1) c.tiles = 2;
+  c.threads = vocab <= 2 * kShort * width && keep <= kShort * 3 / 8 ? kShort : kThreads;
+  const auto per_row = [&](uint32_t v) { return (vocab + c.threads * v * width - 1) / (c.threads * v * width); };
+  *vectors = aligned ? 8 : 4;
+  if (per_row(2) == 1 || rows * per_row(*vectors) < 304) *vectors = 2;
+  else if (keep <= 96 && rows * per_row(2 * *vectors) >= 1216 && per_row(*vectors) > 1) c.tiles = 2;  // (the lists would overflow)
   c.per_row = (uint32_t)per_row(c.tiles * *vectors);
-  c.elements = kThreads * c.tiles * *vectors * width;
+  c.elements = c.threads * c.tiles * *vectors * width;
   c.heads = static_cast<float2*>(workspace);
   const uint64_t records = rows * c.per_row, heads = (records * sizeof(float2) + 255) / 256 * 256;
   c.best = reinterpret_cast<Candidate*>(static_cast<char*>(workspace) + heads);
@@ -708,15 +786,17 @@ cudaError_t launch_step(const BeamArgs& a, void* workspace, cudaStream_t st) {
     const uint32_t n = a.beams * a.vocab;
     uint32_t threads = (n / 2 + 31) / 32 * 32;
     threads = threads < 32 ? 32 : threads > kThreads ? kThreads : threads;
-    if (threads < a.keep && n > 128) threads = (a.keep + 31) / 32 * 32;
+    if (threads < a.keep && n > kFewSlots) threads = (a.keep + 31) / 32 * 32;
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = group_bytes(a.beams, n, n);
-    return cudaLaunchKernelEx(&cfg, direct_kernel<E>, a);
+    return n <= kFewSlots ? cudaLaunchKernelEx(&cfg, direct_kernel<E, true>, a) : cudaLaunchKernelEx(&cfg, direct_kernel<E, false>, a);
   }
   const uint64_t blocks = (uint64_t)a.groups * a.beams * c.per_row;
-  const auto rows = [&](auto kernel) { return launch_plain(kernel, blocks, kThreads, st, a, c); };
-  const cudaError_t e = aligned ? (vectors == 8 ? rows(row_kernel<E, 8, true>) : rows(row_kernel<E, 2, true>))
-                                : (vectors == 4 ? rows(row_kernel<E, 4, false>) : rows(row_kernel<E, 2, false>));
+  const auto rows = [&](auto kernel) { return launch_plain(kernel, blocks, c.threads, st, a, c); };
+  cudaError_t e;
+  if (c.threads == kShort) e = aligned ? rows(row_kernel<E, 2, true, kShort>) : rows(row_kernel<E, 2, false, kShort>);
+  else if (aligned) e = vectors == 8 ? rows(row_kernel<E, 8, true, kThreads>) : rows(row_kernel<E, 2, true, kThreads>);
+  else e = vectors == 4 ? rows(row_kernel<E, 4, false, kThreads>) : rows(row_kernel<E, 2, false, kThreads>);
   if (e != cudaSuccess) return e;
   cfg.blockDim = dim3(kThreads);
   const uint64_t chunks = (uint64_t)a.beams * c.per_row;  // beams, list and lists fit into 48 KB

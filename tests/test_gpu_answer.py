@@ -390,7 +390,7 @@ BEAMS = [  # groups, beams, vocabulary, keep
     (1, 1, 1, 1), (3, 4, 3, 4), (50, 16, 3, 16), (2, 3, 7, 6), (5, 8, 100, 8), (1, 4, 4096, 4), (2, 2, 2049, 5),
     (1, 4, 5003, 8), (3, 5, 16384, 10), (2, 3, 16385, 1), (2, 1, 33001, 256), (1, 2, 70001, 200), (1, 64, 300, 64),
     (2, 256, 20, 256), (1, 256, 40, 100), (90, 4, 9001, 4), (1, 33, 129, 66), (2, 40, 70000, 33), (1, 130, 40003, 256),
-    (40, 9, 17000, 9), (1, 1, 1 << 20, 3),
+    (40, 9, 17000, 9), (1, 1, 1 << 20, 3), (6, 8, 30000, 128), (2, 8, 16384, 256), (3, 5, 600, 20), (3, 9, 1100, 30), (5, 3, 1500, 24),
 ]
 
 
