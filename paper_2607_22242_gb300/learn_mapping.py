@@ -10,13 +10,16 @@ Each tool card (its latencies, load-in, footprint, place in the DAG) becomes a f
 
 gives the gradient in the logits; torch carries it through the two layers between, :func:`bf.embed_grad` into the table.
 
+A fitted policy answers with a beam of mappings (:func:`beam_mappings`: :func:`bf.beam_step`, tool by tool, the histories
+following their parents by :func:`bf.beam_reorder`), of which the fastest is taken (:func:`best_of_beam`).
+
     python -m paper_2607_22242_gb300.learn_mapping [policy|preference] [steps]
 """
 from __future__ import annotations
 
 import math
 import sys
-from typing import List, Sequence
+from typing import List, Optional, Sequence
 
 from . import bf, scenarios
 from .scenarios import Scenario
@@ -97,15 +100,57 @@ def _makespans(handles, scns, modes):
     return torch.stack(out, 1)
 
 
+def beam_mappings(logits, scns: Sequence[Scenario], beams: int = 8):
+    """The `beams` likeliest mappings of every workflow under `logits` (tools of all workflows x modes), the likeliest
+    first: for each workflow (modes (beams x tools), log-probabilities (beams)).  Of fewer mappings than beams the places
+    left over have log-probability -inf and modes of -1."""
+    import torch
+    first, by_size = 0, {}
+    for i, s in enumerate(scns):
+        by_size.setdefault(s.n, []).append((i, first))
+        first += s.n
+    answers = [None] * len(scns)
+    for n, members in by_size.items():  # a group of beams for each workflow of this size
+        groups = len(members)
+        rows = torch.tensor([at for _, at in members], device=logits.device).repeat_interleave(beams)
+        scores = torch.full((groups, beams), -math.inf, device=logits.device)
+        scores[:, 0] = 0.0
+        history = torch.full((groups * beams, n), -1, dtype=torch.int64, device=logits.device)
+        for t in range(n):
+            step = bf.beam_step(logits[rows + t], scores.view(-1), beams)
+            bf.beam_reorder(history, step.parents.view(-1), beams)
+            history[:, t] = step.tokens.view(-1)
+            scores = step.scores
+        for g, (i, _) in enumerate(members):
+            answers[i] = (history[g * beams:(g + 1) * beams], scores[g])
+    return answers
+
+
+def best_of_beam(logits, scns: Sequence[Scenario], beams: int = 8) -> List[int]:
+    """The makespan (in microseconds) of the fastest of each workflow's `beams` likeliest mappings; the all-cpu mapping's
+    where all of them exceed the budget."""
+    import torch
+    found = []
+    for s, (modes, scores) in zip(scns, beam_mappings(logits, scns, beams)):
+        with bf.create_scenario(s) as h:
+            power = torch.tensor([3 ** i for i in range(s.n)], device=modes.device)
+            there = torch.isfinite(scores)
+            index = torch.where(there, (modes * power).sum(1), 0)  # 0: the all-cpu mapping, which always fits
+            ms, fe = bf.eval_indices(h, torch.cat([index, index.new_zeros(1)]))
+            best = torch.where((fe[:-1] == 1) & there, ms[:-1].long() & 0xFFFFFFFF, 1 << 40).min().item()
+            found.append(best if best < 1 << 40 else ms[-1].item() & 0xFFFFFFFF)
+    return found
+
+
 def train(scns: Sequence[Scenario], method: str = "policy", steps: int = 60, samples: int = 32, seed: int = 0,
-          progress=None) -> List[float]:
-    """Fit a policy; the mean over the workflows of (makespan of the policy's likeliest mapping / optimum), before the
+          progress=None, policy: Optional[Policy] = None) -> List[float]:
+    """Fit a policy (a new one, or `policy`); the mean over the workflows of (makespan of the policy's likeliest mapping / optimum), before the
     first step and after every one (a mapping beyond the budget counts as the all-cpu one)."""
     import torch
     if samples < 2:
         raise ValueError("samples must be at least 2: a workflow's samples are measured against each other")
     torch.manual_seed(seed)
-    policy = Policy(scns, seed=seed)
+    policy = Policy(scns, seed=seed) if policy is None else policy
     best = torch.tensor([r.makespan_us for r in bf.search_batch(list(scns))], device="cuda", dtype=torch.float64)
     sizes = [s.n for s in scns]
     tools = sum(sizes)
@@ -166,6 +211,11 @@ def train(scns: Sequence[Scenario], method: str = "policy", steps: int = 60, sam
 if __name__ == "__main__":
     how = sys.argv[1] if len(sys.argv) > 1 else "policy"
     count = int(sys.argv[2]) if len(sys.argv) > 2 else 60
-    found = train(scenarios.config4(16), how, count,
+    workflows = scenarios.config4(16)
+    fitted = Policy(workflows)
+    found = train(workflows, how, count, policy=fitted,
                   progress=lambda k, g: print(f"step {k:3d}: makespan / optimum {g:.3f}") if k % 10 == 0 else None)
     print(f"{how}: {found[0]:.3f} -> {found[-1]:.3f} of the optimum in {count} steps")
+    optima = [r.makespan_us for r in bf.search_batch(workflows)]
+    fastest = best_of_beam(fitted.logits()[0].detach(), workflows)
+    print(f"fastest of a beam of 8: {sum(f / o for f, o in zip(fastest, optima)) / len(optima):.3f} of the optimum")
