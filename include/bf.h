@@ -477,7 +477,7 @@ typedef struct bf_cache {
 typedef struct bf_attention_args {
   const int64_t* prefix_lengths;  /* device, one per prompt; NULL: prefix_k->tokens each */
   const int64_t* suffix_lengths;  /* device, one per answer; NULL: suffix_k->tokens each */
-  float scale;                    /* of the scores, 1 / sqrt(dim) as a rule; finite */
+  float scale;                    /* of the scores, 1 / sqrt(dim) as a rule; up to 1e30 in size */
   uint32_t pad;
 } bf_attention_args;
 

@@ -118,6 +118,14 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
   const uint32_t len = length_of(a.suffix_len, a.suffix_cap, answer), step = kAlone ? 16 : 16 * kWarps * few.blocks;
   uint32_t at = kAlone ? 0 : 16 * (rank * kWarps + warp);
 
+  // Who has the prompt's pieces (ahead of the copies, behind which its reads would queue); an answer's rows may lie in
+  // two tiles of queries.
+  const uint32_t row0 = (answer - prompt * a.per_prompt) * a.share + first;
+  const uint32_t tile0 = row0 / plan.rows, rows0 = min(rows, (tile0 + 1) * plan.rows - row0);
+  const Standing standing = standing_of(a, plan.keys, prompt);
+  const Owners own0 = owners_of(a, plan, standing, prompt, head * plan.row_tiles + tile0);
+  const Owners own1 = rows0 == rows ? own0 : owners_of(a, plan, standing, prompt, head * plan.row_tiles + tile0 + 1);
+  const bool bad = bad_answer(a, prompt, answer);
   // The warp's ring: a lane copies a piece of every (32 / kPieces)-th key.
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(sh.ring[warp]);
   const uint32_t my_piece = lane % kPieces, my_key = lane / kPieces;
@@ -142,13 +150,6 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
 
   // What the prompts' kernel wrote is there from here on (it takes whole SMs: blocks of this one hardly start before it ends).
   wait_for_previous();
-  // Who has the prompt's pieces (while the keys are on their way); an answer's rows may lie in two tiles of queries.
-  const uint32_t row0 = (answer - prompt * a.per_prompt) * a.share + first;
-  const uint32_t tile0 = row0 / plan.rows, rows0 = min(rows, (tile0 + 1) * plan.rows - row0);
-  const Standing standing = standing_of(a, plan.keys, prompt);
-  const Owners own0 = owners_of(a, plan, standing, prompt, head * plan.row_tiles + tile0);
-  const Owners own1 = rows0 == rows ? own0 : owners_of(a, plan, standing, prompt, head * plan.row_tiles + tile0 + 1);
-  const bool bad = bad_answer(a, prompt, answer);
   // The prompt's records of this answer's rows, on their way into this SM's cache meanwhile.
   const auto record_of = [&](const Owners& own, uint32_t i) { return plan.prefix + (own.first + i + own.segment) * plan.record; };
   const uint32_t quads = a.dim / 4, sums_at = record_sums(plan.rows, a.dim), r0 = row0 - tile0 * plan.rows;

@@ -171,7 +171,7 @@ int bf_prefix_attention(const bf_cache* q, const bf_cache* prefix_k, const bf_ca
   if (!args) return fail(BF_EINVAL, "%s: args is NULL", who);
   BF_TRY(check_array(args->prefix_lengths, 0, 8, "prefix_lengths", who));
   BF_TRY(check_array(args->suffix_lengths, 0, 8, "suffix_lengths", who));
-  BF_TRY(check_number(args->scale, true, "scale", who));
+  BF_TRY(check_number(args->scale, std::fabs(args->scale) <= 1e30f, "scale", who));
   BF_TRY(check_cache(out, "out", who));
   BF_TRY(check_like(out, q, "out", "q", who));
   if (folded(out)) return fail(BF_EINVAL, "%s: vectors of out overlap", who);

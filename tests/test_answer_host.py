@@ -49,7 +49,7 @@ BAD_ATTENTION = [
     dict(sk=cache(3, 5, 2), sv=cache(3, 5, 2)), dict(sk=cache(4, 5, 1), sv=cache(4, 5, 1)), dict(sk=cache(4, 5, 2), sv=cache(4, 6, 2)),
     dict(out=cache()), dict(out=cache(data=SOME + 128)), dict(out=cache(3, data=FAR)), dict(out=cache(dtype=2, data=FAR)),
     dict(out=cache(data=FAR, batch_stride=0)), dict(out=cache(data=FAR, head_stride=32)), dict(out=cache(data=FAR, batch_stride=200)),
-    dict(lse=SOME + 2), dict(scale=NAN), dict(scale=INF), dict(prefix_lengths=SOME + 4), dict(suffix_lengths=SOME + 4),
+    dict(lse=SOME + 2), dict(scale=NAN), dict(scale=INF), dict(scale=-1e31), dict(prefix_lengths=SOME + 4), dict(suffix_lengths=SOME + 4),
     dict(work=None), dict(work=SOME + 8), dict(have=64),
 ]
 

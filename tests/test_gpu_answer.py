@@ -216,6 +216,7 @@ def test_attention_extremes(dtype):
     x = attention_inputs(1, 9, 4, 2, 64, 700, 50, dtype, seed=5)
     check_attention(x, dtype, scale=3.0)
     check_attention(x, dtype, scale=-0.2)
+    check_attention(x, dtype, scale=0.0)
     grow = torch.linspace(0.01, 4.0, 700, device="cuda").to(TYPES[dtype])[None, :, None, None]
     check_attention((x[0], x[1] * grow, *x[2:]), dtype)
     check_attention((x[0], x[1] * grow.flip(1), *x[2:]), dtype)
@@ -695,3 +696,98 @@ def test_decoding_step_by_step():
         assert [c[0] for c in found] == history[mine].tolist()
         assert np.allclose([c[1] for c in found], d(scores[mine]), rtol=0, atol=1e-4)
         assert [c[2] for c in found] == finished[mine].tolist()
+
+
+def test_calls_of_several_threads():
+    """Calls of four threads, each on a stream of its own, on the same inputs."""
+    import threading
+    x = attention_inputs(2, 8, 8, 2, 64, 700, 50, "bf16", seed=21)
+    logits, scores, _ = beam_inputs(4, 4, 9001, "bf16", seed=21)
+    s = torch.tensor(scores, device="cuda")
+    state = random_states((16, 40, 2, 8), torch.float32, 1)[0]
+    want = bf.prefix_attention(*x)
+    step = bf.beam_step(logits, s, 4)
+    moved = bf.beam_reorder(state.clone(), step.parents, 4)
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work():
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(30):
+                a, b = bf.prefix_attention(*x), bf.beam_step(logits, s, 4)
+                c = bf.beam_reorder(state, b.parents, 4, out=torch.empty_like(state))
+                stream.synchronize()
+                if not (torch.equal(a, want) and torch.equal(b.tokens, step.tokens) and torch.equal(b.scores, step.scores)
+                        and torch.equal(c, moved)):
+                    wrong.append(1)
+
+    threads = [threading.Thread(target=work) for _ in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+
+
+def test_captured_together():
+    """A step captured as a whole, replayed over other inputs, beside another graph of the same calls."""
+    def inputs(seed):
+        x = attention_inputs(2, 4, 4, 2, 64, 300, 20, "f16", seed=seed)
+        logits, scores, _ = beam_inputs(2, 4, 5003, "f16", seed=seed)
+        return [*x, logits, torch.tensor(scores, device="cuda"), random_states((8, 20, 2, 8), torch.float16, 1, seed=seed)[0]]
+
+    def step(x):
+        out = bf.prefix_attention(*x[:5])
+        best = bf.beam_step(x[5], x[6], 4)
+        return out, best.scores, best.tokens, bf.beam_reorder(x[7], best.parents, 4, out=torch.empty_like(x[7])), \
+            bf.beam_reorder(x[7], best.parents, 4)
+
+    sets, graphs = [inputs(1), inputs(2)], []
+    for x in sets:
+        step([t.clone() for t in x])
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            held = step(x)
+        graphs.append((g, held))
+    for seed in (3, 4):
+        for k, x in enumerate(sets):
+            fresh = inputs(10 * seed + k)
+            for a, b in zip(x, fresh):
+                a.copy_(b)
+        for g, _ in graphs:
+            g.replay()
+        for k, (_, held) in enumerate(graphs):
+            want = step(inputs(10 * seed + k))
+            assert all(torch.equal(a, b) for a, b in zip(held, want))
+
+
+def test_far_offsets():
+    """Sequences, rows and states more than 2^32 elements behind each other."""
+    far = (1 << 32) + 64
+    buf = torch.empty(far + (1 << 22), dtype=torch.bfloat16, device="cuda")
+    near = attention_inputs(2, 3, 4, 2, 64, 300, 20, "bf16", seed=30)
+    shape, strides = near[1].shape, (far, *near[1].stride()[1:])
+    for which in (1, 2):  # keys, then values, of the second prompt far away
+        view = buf.as_strided(shape, strides)
+        view.copy_(near[which])
+        x = [*near]
+        x[which] = view
+        assert torch.equal(bf.prefix_attention(*x), bf.prefix_attention(*near))
+    own = buf.as_strided((2, *near[3].shape[1:]), (far, *near[3].stride()[1:]))
+    own.copy_(near[3][:2])
+    q = near[0][:2]
+    assert torch.equal(bf.prefix_attention(q, near[1], near[2], own, near[4][:2]),
+                       bf.prefix_attention(q, near[1], near[2], near[3][:2], near[4][:2]))
+    for vocab in (50, 9001):
+        x, scores, _ = beam_inputs(1, 2, vocab, "bf16", seed=31)
+        view = buf.as_strided(x.shape, (far, 1))
+        view.copy_(x)
+        check_beams(view, scores, 2, 5)
+    rows = buf.as_strided((2, 30, 2, 32), (far, 64, 32, 1))
+    rows.copy_(near[3][:1, :1, :1, :1].expand(2, 30, 2, 32))
+    rows[1] += 1
+    want = rows.flip(0).clone()
+    bf.beam_reorder(rows, torch.tensor([1, 0], device="cuda"), 2)
+    assert torch.equal(rows, want)
