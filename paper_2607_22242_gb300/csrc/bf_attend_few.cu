@@ -16,6 +16,7 @@
 #include <cooperative_groups.h>
 
 #include "bf_attend.cuh"
+#include "bf_blackwell.cuh"
 
 namespace bfk {
 
@@ -44,15 +45,6 @@ __device__ __forceinline__ void product(float (&d)[4], const uint32_t (&a)[4], u
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// 16 bytes to shared memory, zeros where they are not there.
-__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool on) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(__cvta_generic_to_global(from)), "r"(on ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() {  // all but the last N groups have arrived
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
 __device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch.global.L1 [%0];" ::"l"(p)); }
 // Four 8 x 8 matrices of 16 bits; the address is of row lane % 8 of matrix lane / 8.
 __device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t at) {
@@ -138,8 +130,8 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
       const bool on = from + key < len && my_piece * 8 < a.dim;
       const uint32_t to = ring + stage * 2 * kTile + my_piece / 8 * 2048 + key * 128 + (my_piece % 8 ^ key % 8) * 16;
       const int64_t token = on ? (int64_t)(from + key) : 0;
-      copy16(to, on ? k_from + token * a.sk.token : static_cast<const E*>(a.q.data), on);
-      copy16(to + kTile, on ? v_from + token * a.sv.token : static_cast<const E*>(a.q.data), on);
+      copy_piece(to, on ? k_from + token * a.sk.token : static_cast<const E*>(a.q.data), on);
+      copy_piece(to + kTile, on ? v_from + token * a.sv.token : static_cast<const E*>(a.q.data), on);
     }
   };
 #pragma unroll

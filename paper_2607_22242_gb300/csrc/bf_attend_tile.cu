@@ -46,26 +46,30 @@ struct Shared {
   float2 sums[2][kRows];  // (maximum, sum) of the streams
 };
 
-// A block's pieces, in order; the same for all its warps.  Up to 32 prompts, whose
-// lengths a warp holds, are found by one read; divisions are of 32 bits where they can
-// be (the first version, of two reads and 64 bits, took 3,200 cycles of a block's start).
+// A block's pieces, in order; the same for all its warps.  Up to 128 prompts, whose
+// lengths a warp holds (four to a lane), are found by one read; divisions are of 32 bits where they can
+// be (two reads and 64 bits took 3,200 to 4,000 cycles of a block's start).
 struct Pieces {
   const AttendArgs& a;
   const AttendPlan& plan;
-  uint32_t inners, my_len;
+  uint32_t inners, my_len[4];
   uint64_t left;
   Place at;
   uint32_t len, tiles;  // the piece's prompt, and its tiles
   uint32_t head, first_row;
 
   __device__ __forceinline__ Pieces(const AttendArgs& args, const AttendPlan& p)
-      : a(args), plan(p), inners(args.kv_heads * p.row_tiles), my_len(0), left(0), at{0, 0, 0}, len(0), tiles(0), head(0), first_row(0) {
+      : a(args), plan(p), inners(args.kv_heads * p.row_tiles), my_len{}, left(0), at{0, 0, 0}, len(0), tiles(0), head(0), first_row(0) {
     const uint32_t lane = threadIdx.x % 32;
     uint64_t t0;
-    if (a.prompts <= 32) {
-      if (lane < a.prompts) my_len = length_of(a.prefix_len, a.prefix_cap, lane);
-      const uint32_t n = (my_len + kKeys - 1) / kKeys;
-      uint32_t upto = n;
+    if (a.prompts <= 128) {
+      uint32_t n = 0, upto;
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j)
+        if (4 * lane + j < a.prompts) my_len[j] = length_of(a.prefix_len, a.prefix_cap, 4 * lane + j);
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j) n += tiles_of(my_len[j]);
+      upto = n;
 #pragma unroll
       for (int d = 1; d < 32; d *= 2) {
         const uint32_t o = __shfl_up_sync(~0u, upto, d);
@@ -73,11 +77,16 @@ struct Pieces {
       }
       const uint64_t total = (uint64_t)__shfl_sync(~0u, upto, 31) * inners;
       if (!share(total, &t0)) return;
-      const int prompt = __ffs(__ballot_sync(~0u, (uint64_t)upto * inners > t0)) - 1;
-      const uint64_t before = (uint64_t)__shfl_sync(~0u, upto - n, prompt) * inners;
-      const uint32_t mine = __shfl_sync(~0u, n, prompt);
+      const int owner = __ffs(__ballot_sync(~0u, (uint64_t)upto * inners > t0)) - 1;
+      uint64_t before = (uint64_t)__shfl_sync(~0u, upto - n, owner) * inners;
+      uint32_t mine = 0;
+      at.prompt = 4 * (uint32_t)owner;
+      for (;; ++at.prompt) {  // of the lane's four
+        mine = tiles_of(len_of(at.prompt));
+        if (t0 < before + (uint64_t)mine * inners) break;
+        before += (uint64_t)mine * inners;
+      }
       const uint64_t in = t0 - before;
-      at.prompt = (uint32_t)prompt;
       at.inner = in >> 32 ? (uint32_t)(in / mine) : (uint32_t)in / mine;
       at.tile = (uint32_t)(in - (uint64_t)at.inner * mine);
     } else {
@@ -85,6 +94,11 @@ struct Pieces {
       at = place_of(a, kKeys, inners, t0);
     }
     find();
+  }
+  static __device__ __forceinline__ uint32_t tiles_of(uint32_t len) { return (len + kKeys - 1) / kKeys; }
+  __device__ __forceinline__ uint32_t len_of(uint32_t prompt) const {  // by a whole warp
+    const uint32_t j = prompt % 4, mine = j == 0 ? my_len[0] : j == 1 ? my_len[1] : j == 2 ? my_len[2] : my_len[3];
+    return __shfl_sync(~0u, mine, prompt / 4);
   }
   // This block's run of `total` tiles: its first, and how many; false where it has none.
   __device__ __forceinline__ bool share(uint64_t total, uint64_t* t0) {
@@ -104,7 +118,7 @@ struct Pieces {
   __device__ __forceinline__ void find() {
     for (;; ++at.prompt) {
       if (left == 0) return;
-      len = a.prompts <= 32 ? __shfl_sync(~0u, my_len, at.prompt) : length_of(a.prefix_len, a.prefix_cap, at.prompt);
+      len = a.prompts <= 128 ? len_of(at.prompt) : length_of(a.prefix_len, a.prefix_cap, at.prompt);
       if (len) break;
     }
     tiles = (uint32_t)min((uint64_t)((len + kKeys - 1) / kKeys - at.tile), left);
@@ -139,11 +153,11 @@ struct Ring {
   }
 };
 
-__device__ void copy_tiles(const AttendArgs& a, const AttendPlan& plan, const TileArgs& t, Shared& sh, unsigned char* ring) {
+__device__ void copy_tiles(const TileArgs& t, Shared& sh, unsigned char* ring, Pieces& p) {
   const uint32_t bytes = t.chunks * kKeys * 128, streams = t.pair ? 1 : 2;
   Ring rings[2] = {Ring(0, t), Ring(streams - 1, t)};
   bool ok = true;
-  for (Pieces p(a, plan); ok && p.more(); p.next())
+  for (; ok && p.more(); p.next())
     for (uint32_t i = 0; ok && i < p.tiles; i += streams)
 #pragma unroll 1
       for (uint32_t n = 0; n < 2 * streams; ++n) {  // K of the streams' next tiles, then V
@@ -177,8 +191,7 @@ __device__ void copy_tiles(const AttendArgs& a, const AttendPlan& plan, const Ti
 
 // The products of stream s.
 template <bool bf16>
-__device__ void multiply_tiles(const AttendArgs& a, const AttendPlan& plan, const TileArgs& t, Shared& sh, uint32_t q_at,
-                               unsigned char* ring_base, uint32_t s) {
+__device__ void multiply_tiles(const TileArgs& t, Shared& sh, uint32_t q_at, unsigned char* ring_base, uint32_t s, Pieces& p) {
   const uint32_t bytes = t.chunks * kKeys * 128, tensor = uniform(sh.tensor), lane = threadIdx.x % 32;
   const uint32_t ring_at = shared_address(ring_base);
   const uint32_t scores = product_of(bf16, kKeys, false), outputs = product_of(bf16, t.columns, true);
@@ -187,7 +200,7 @@ __device__ void multiply_tiles(const AttendArgs& a, const AttendPlan& plan, cons
   uint32_t q_phase = 0, p_phase = 0, o_phase = 0;
   Ring r(t.pair ? 0 : s, t);
   bool ok = true;
-  for (Pieces p(a, plan); ok && p.more(); p.next()) {
+  for (; ok && p.more(); p.next()) {
     if (!(ok = barrier_wait(&sh.q_full, q_phase, &sh.gave_up))) break;
     q_phase ^= 1;
     tensor_fence_after();
@@ -211,7 +224,12 @@ __device__ void multiply_tiles(const AttendArgs& a, const AttendPlan& plan, cons
       r.step();
       return true;
     };
-    if (first < p.tiles) ok = score(false);
+    if (first < p.tiles) {
+      ok = score(false);
+    } else {  // a piece of one tile: nobody goes on before this warp has seen its queries' phase
+      if (lane == 0) barrier_arrive(&sh.o_done[s]);
+      o_phase ^= 1;
+    }
     for (uint32_t tile = first; ok && tile < p.tiles; tile += step) {
       const uint64_t v = matrix_at(uniform(ring_at + r.stage * bytes), kKeys * 128);
       if (!(ok = barrier_wait(&sh.full[r.stage], r.phase, &sh.gave_up))) break;
@@ -248,41 +266,39 @@ __device__ void multiply_tiles(const AttendArgs& a, const AttendPlan& plan, cons
     for (uint32_t n = 0; n < 1u << 16; ++n) __nanosleep(100);
 }
 
-// The prompt's query vectors [first_row, ...) of a key head into shared memory, 16 bytes a
-// thread and turn, eight turns' reads on their way; vectors that are not there are 0.
+// Where the streams' queries lie: both on the same rows, or, where there are at most
+// 64 (32), stream 1's on the rows 64 (32) further on, so that its softmax is on other
+// schedulers: two warps of one take 1,050 cycles for 64 exponentials, one 440 to 670.
+__device__ __forceinline__ uint32_t apart_by(const TileArgs& t, uint32_t rows) { return t.pair || rows > 64 ? 0 : rows > 32 ? 64 : 32; }
+
+// The prompt's query vectors [first_row, ...) of a key head on their way into shared
+// memory, 16 bytes a thread and turn; zeros up to a multiple of 32 vectors and in the columns behind the last dimension.
 template <typename E>
-__device__ __forceinline__ void stage_q(const AttendArgs& a, const Pieces& p, const TileArgs& t, unsigned char* to) {
-  const uint32_t rows_all = a.per_prompt * a.share, shift = t.chunks > 1 ? 4 : 3;  // pieces of a row: 8 or 16
-  const uint32_t pieces = (t.pair ? 2 * kRows : kRows) << shift;
-  const bool aligned = ((uintptr_t)a.q.data | (uint64_t)a.q.batch * 2 | (uint64_t)a.q.head * 2) % 16 == 0;
-  const uint32_t flip = a.scale2 < 0.0f ? 0x80008000u : 0u;
+__device__ __forceinline__ void request_q(const AttendArgs& a, const AttendPlan& plan, const Pieces& p, const TileArgs& t, unsigned char* to) {
+  const uint32_t rows = min(plan.rows, a.per_prompt * a.share - p.first_row), most = (rows + 31) / 32 * 32, by = apart_by(t, rows);
+  const uint32_t shift = t.chunks > 1 ? 4 : 3, pieces = (by ? 2 : 1) * most << shift;  // pieces of a row: 8 or 16
+  const bool flip = a.scale2 < 0.0f, whole = !flip && ((uintptr_t)a.q.data | (uint64_t)a.q.batch * 2 | (uint64_t)a.q.head * 2) % 16 == 0;
   const E* base = static_cast<const E*>(a.q.data) + (int64_t)((uint64_t)p.at.prompt * a.per_prompt) * a.q.batch +
                   (int64_t)(p.head * a.share) * a.q.head;
 #pragma unroll 1
-  for (uint32_t n0 = threadIdx.x; n0 < pieces; n0 += 8 * kSoft) {
-    uint4 u[8];
-#pragma unroll
-    for (uint32_t k = 0; k < 8; ++k) {
-      const uint32_t n = n0 + k * kSoft, row = n >> shift, c = n & ((1u << shift) - 1), at = p.first_row + row;
-      u[k] = make_uint4(0, 0, 0, 0);
-      if (n < pieces && at < rows_all && c * 8 < a.dim) {
-        const uint32_t answer = at / a.share;
-        const E* q = base + (int64_t)answer * a.q.batch + (int64_t)(at - answer * a.share) * a.q.head + c * 8;
-        if (aligned) {
-          u[k] = __ldg(reinterpret_cast<const uint4*>(q));
-        } else {
-          const uint16_t* h = reinterpret_cast<const uint16_t*>(q);
-          u[k] = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16,
-                            h[6] | (uint32_t)h[7] << 16);
-        }
-      }
+  for (uint32_t n = threadIdx.x; n < pieces; n += kSoft) {
+    uint32_t row = n >> shift, r = row;
+    if (row >= most && by) {
+      row -= most;
+      r = row + by;
     }
+    const uint32_t c = n & ((1u << shift) - 1), at = p.first_row + row, answer = at / a.share;
+    const bool on = row < rows && c * 8 < a.dim;
+    const E* q = on ? base + (int64_t)answer * a.q.batch + (int64_t)(at - answer * a.share) * a.q.head + c * 8 : base;
+    unsigned char* place = to + (r / kRows * t.chunks + c / 8) * (kRows * 128) + r % kRows * 128 + (c % 8 ^ r % 8) * 16;
+    if (whole) {
+      copy_piece(shared_address(place), q, on);
+    } else {
+      uint32_t u[4];
+      const uint16_t* h = reinterpret_cast<const uint16_t*>(q);
 #pragma unroll
-    for (uint32_t k = 0; k < 8; ++k) {
-      const uint32_t n = n0 + k * kSoft, row = n >> shift, c = n & ((1u << shift) - 1), r = row % kRows;
-      if (n < pieces)
-        *reinterpret_cast<uint4*>(to + (row / kRows * t.chunks + c / 8) * (kRows * 128) + r * 128 + (c % 8 ^ r % 8) * 16) =
-            make_uint4(u[k].x ^ flip, u[k].y ^ flip, u[k].z ^ flip, u[k].w ^ flip);
+      for (int k = 0; k < 4; ++k) u[k] = on ? (h[2 * k] | (uint32_t)h[2 * k + 1] << 16) ^ (flip ? 0x80008000u : 0u) : 0u;
+      *reinterpret_cast<uint4*>(place) = make_uint4(u[0], u[1], u[2], u[3]);
     }
   }
 }
@@ -298,24 +314,23 @@ __device__ __forceinline__ bool any_of_streams(bool say) {
   return any;
 }
 
-// A row's 32 columns from c on of a record, from the row's outputs in tensor memory, or from two weighted parts of them.
-__device__ __forceinline__ void put_outputs(float* record, uint32_t rows, uint32_t row, bool on, uint32_t dim, uint32_t c, uint32_t at0,
-                                            uint32_t at1, bool two, float w0, float w1) {
-  uint32_t o0[32];
-  tensor_load32(at0 + c, o0);
-  tensor_wait_load(o0);
-  if (two) {
-    uint32_t o1[32];
-    tensor_load32(at1 + c, o1);
-    tensor_wait_load(o1);
+// Columns [c0, c1) of a row, times w, into a record: as they are, or added to what is there.
+template <bool kAdd>
+__device__ __forceinline__ void put_outputs(float* record, uint32_t rows, uint32_t row, bool on, uint32_t c0, uint32_t c1, uint32_t from, float w) {
+#pragma unroll 1
+  for (uint32_t c = c0; c < c1; c += 32) {
+    uint32_t o[32];
+    tensor_load32(from + c, o);
+    tensor_wait_load(o);
+    if (!on) continue;
 #pragma unroll
-    for (uint32_t k = 0; k < 32; ++k) o0[k] = __float_as_uint(fmaf(w1, __uint_as_float(o1[k]), w0 * __uint_as_float(o0[k])));
-  }
-  if (!on) return;
-#pragma unroll
-  for (uint32_t k = 0; k < 32; k += 4) {
-    if (c + k >= dim) break;
-    *reinterpret_cast<uint4*>(record + record_place(rows, row, c + k)) = make_uint4(o0[k], o0[k + 1], o0[k + 2], o0[k + 3]);
+    for (uint32_t k = 0; k < 32; k += 4) {
+      if (c + k >= c1) break;
+      const float4 x = make_float4(w * __uint_as_float(o[k]), w * __uint_as_float(o[k + 1]), w * __uint_as_float(o[k + 2]), w * __uint_as_float(o[k + 3]));
+      float* to = record + record_place(rows, row, c + k);
+      if (kAdd) add4(to, x);
+      else *reinterpret_cast<float4*>(to) = x;
+    }
   }
 }
 
@@ -333,22 +348,23 @@ __device__ __forceinline__ void load_scores(uint32_t at, uint32_t c, uint32_t va
   }
 }
 
+// `p`: the block's first piece, whose queries are on their way.
 template <typename E>
-__device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const TileArgs& t, Shared& sh, unsigned char* q_to) {
+__device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const TileArgs& t, Shared& sh, unsigned char* q_to, Pieces& p) {
   const uint32_t s = threadIdx.x / kRows, row = threadIdx.x % kRows, lane = threadIdx.x % 32;
-  const uint32_t mine = sh.tensor + (row / 32 * 32 << 16), s_at = mine + s * 128, o_step = t.apart ? 64 : 128;
-  const uint32_t o_at = mine + kOutputs + s * o_step, p_at = t.apart ? mine + kWeights + s * 64 : s_at;
+  const uint32_t mine = sh.tensor + (row / 32 * 32 << 16), s_at = mine + s * 128;
+  const uint32_t o_at = mine + kOutputs + s * (t.apart ? 64 : 128), p_at = t.apart ? mine + kWeights + s * 64 : s_at;
   const float scale = fmaxf(fabsf(a.scale2), 1e-37f);  // 0 would make NaN of masked scores
   const uint32_t rows_all = a.per_prompt * a.share;
   uint32_t s_phase = 0, o_phase = 0;
-  for (Pieces p(a, plan); p.more(); p.next()) {
-    stage_q<E>(a, p, t, q_to);
+  while (p.more()) {
+    copies_wait_all();
     fence_to_async();
     tensor_fence_before();
     barrier_arrive(&sh.q_full);
     const uint32_t rows = min(plan.rows, rows_all - p.first_row);
-    const uint32_t my_row = t.pair ? s * kRows + row : row;
-    const bool warp_on = my_row - lane < rows;  // some of the warp's rows are there
+    const uint32_t my_row = t.pair ? s * kRows + row : row - s * apart_by(t, rows);  // (beyond 2^31 where there is none)
+    const bool warp_on = my_row - lane < rows, on = my_row < rows;  // some of the warp's rows are there; this one is
     const uint32_t steps = t.pair ? p.tiles : s < p.tiles ? (p.tiles - s + 1) / 2 : 0;
     float m = kNone, l = 0.0f;
     bool ok = true;
@@ -417,37 +433,41 @@ __device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const T
       __syncwarp();
       if (lane == 0) barrier_arrive(&sh.p_full[s]);
     }
-    // The piece's outputs: all of this stream's products are done.
-    if (ok && steps) {
+    // The piece's outputs, when all products are done.  Two streams of the same queries:
+    // each puts half of the columns there, weighted, and then adds its part to the other half.
+    const bool both = !t.pair && p.tiles > 1;
+    float* record = plan.prefix + (uint64_t)(blockIdx.x + (uint64_t)p.at.prompt * p.inners + p.at.inner) * plan.record;
+    float2* sums = reinterpret_cast<float2*>(record + record_sums(plan.rows, a.dim));
+    float2 ml = make_float2(m == kNone ? kNone : m * scale, l);
+    float w = 1.0f;
+    if (both) {
+      const uint32_t by = apart_by(t, rows);
+      sh.sums[s][row] = ml;
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      const float2 other = sh.sums[1 - s][(row + (s ? 0u - by : by)) % kRows];
+      const float most = fmaxf(ml.x, other.x), base = most == kNone ? 0.0f : most;
+      w = exp2_of(ml.x - base);
+      if (s == 0) ml = make_float2(most, fmaf(exp2_of(other.x - base), other.y, w * ml.y));
+    }
+    if (ok) {  // (without tiles, this stream's products' warp says that it has seen the piece)
       ok = barrier_wait(&sh.o_done[s], o_phase, &sh.gave_up);
       o_phase ^= 1;
     }
-    float* record = plan.prefix + (uint64_t)(blockIdx.x + (uint64_t)p.at.prompt * p.inners + p.at.inner) * plan.record;
-    float2* sums = reinterpret_cast<float2*>(record + record_sums(plan.rows, a.dim));
-    const float2 ml = make_float2(m == kNone ? kNone : m * scale, l);
-    sh.sums[s][row] = ml;
-    tensor_fence_before();
-    asm volatile("bar.sync 1, 256;" ::: "memory");
     tensor_fence_after();
-    if (t.pair) {
-      if (warp_on)
-        for (uint32_t c = 0; c < a.dim; c += 32) put_outputs(record, plan.rows, my_row, my_row < rows, a.dim, c, o_at, 0, false, 1.0f, 0.0f);
-      if (my_row < rows) sums[my_row] = ml;
-    } else if (warp_on) {
-      // Both streams' outputs of the same queries: each stream's threads join every other 32 dimensions.
-      const float2 s0 = sh.sums[0][row], s1 = sh.sums[1][row];
-      const bool two = p.tiles > 1;
-      const float most = two ? fmaxf(s0.x, s1.x) : s0.x, base = most == kNone ? 0.0f : most;
-      const float w0 = exp2_of(s0.x - base), w1 = two ? exp2_of(s1.x - base) : 0.0f;
-      const uint32_t at = mine + kOutputs;
-#pragma unroll 1
-      for (uint32_t c = 32 * s; c < a.dim; c += 64) put_outputs(record, plan.rows, row, row < rows, a.dim, c, at, at + o_step, two, w0, w1);
-      if (s == 0 && row < rows) sums[row] = two ? make_float2(most, fmaf(w1, s1.y, w0 * s0.y)) : s0;
+    const uint32_t half = both ? (a.dim / 2 + 7) / 8 * 8 : a.dim;
+    if (warp_on && (t.pair || steps)) {
+      put_outputs<false>(record, plan.rows, my_row, on, s && both ? half : 0, s && both ? a.dim : half, o_at, w);
+      if (on && (t.pair || s == 0)) sums[my_row] = ml;
     }
     tensor_fence_before();
-    // Both streams have read what the next piece writes over; all of their threads go on, or none.
-    if (any_of_streams(!ok || *static_cast<volatile uint32_t*>(&sh.gave_up))) break;
+    if (any_of_streams(!ok || *static_cast<volatile uint32_t*>(&sh.gave_up))) break;  // all go on, or none
+    tensor_fence_after();
+    p.next();
+    if (p.more()) request_q<E>(a, plan, p, t, q_to);  // neither stream has a product left that reads the queries
+    if (both && warp_on) put_outputs<true>(record, plan.rows, my_row, on, s ? 0 : half, s ? half : a.dim, o_at, w);
+    tensor_fence_before();
   }
+  copies_wait_all();
 }
 
 template <typename E>
@@ -478,6 +498,9 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
     fence_barriers();
   }
   if (warp == 9) tensor_alloc(&sh.tensor, kColumns);
+  // The first queries are asked for ahead of the rings' copies: behind them they were 7,000 to 14,000 cycles on their way.
+  Pieces p(a, plan);
+  if (warp < 8 && p.more()) request_q<E>(a, plan, p, t, base);
   if (warp == 8 && threadIdx.x % 32 == 0) {
     prefetch_map(&t.k);
     prefetch_map(&t.v);
@@ -485,9 +508,9 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
   tensor_fence_before();
   __syncthreads();
   tensor_fence_after();
-  if (warp < 8) weigh_tiles<E>(a, plan, t, sh, base);
-  else if (warp == 8) copy_tiles(a, plan, t, sh, ring);
-  else multiply_tiles<__is_same(E, __nv_bfloat16)>(a, plan, t, sh, shared_address(base), ring, warp - 9);
+  if (warp < 8) weigh_tiles<E>(a, plan, t, sh, base, p);
+  else if (warp == 8) copy_tiles(t, sh, ring, p);
+  else multiply_tiles<__is_same(E, __nv_bfloat16)>(t, sh, shared_address(base), ring, warp - 9, p);
   tensor_fence_before();
   __syncthreads();
   tensor_fence_after();

@@ -198,4 +198,20 @@ __device__ __forceinline__ void tensor_store8(uint32_t at, const uint32_t* r) {
 #undef BF_R4
 #undef BF_I4
 
+
+// 16 bytes to shared memory, zeros where they are not there.
+__device__ __forceinline__ void copy_piece(uint32_t to, const void* from, bool on) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(__cvta_generic_to_global(from)), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() {  // all but the last N groups have arrived
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void copies_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// Four values added to what is in global memory.
+__device__ __forceinline__ void add4(float* to, const float4& x) {
+  asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(__cvta_generic_to_global(to)), "f"(x.x), "f"(x.y), "f"(x.z), "f"(x.w) : "memory");
+}
+
 }  // namespace bfk

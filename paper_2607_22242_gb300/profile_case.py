@@ -7,9 +7,11 @@
   python -m paper_2607_22242_gb300.profile_case --kernel whatif --config 3 --reps 20
   python -m paper_2607_22242_gb300.profile_case --kernel tree --workload wide32 --space 3
   python -m paper_2607_22242_gb300.profile_case --kernel policy --rows 1024 --vocab 131072 --dtype bfloat16
+  python -m paper_2607_22242_gb300.profile_case --kernel attention --beams 64 --prefix 65536 --suffix 512
 
 Prints one line per repetition (CUDA-event time of the call and mappings/s; for the learning calls -- policy,
-preference, scores, embed_grad -- GB/s of the bytes they cannot do without).
+preference, scores, embed_grad -- and the answering calls -- attention, beams, reorder -- GB/s of the bytes they
+cannot do without).
 Sized so that a profiler capture of one launch stays short.
 """
 from __future__ import annotations
@@ -47,10 +49,35 @@ def learning_call(args):
     return 2 * moved, lambda: bf.policy_loss(logits, tokens, offsets, old, advantage, old, kl_coef=0.04)
 
 
+def answering_call(args):
+    """(bytes that it cannot do without, the call) of an answering entry point on random inputs."""
+    import torch
+    from paper_2607_22242_gb300 import bf
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    dtype = getattr(torch, args.dtype)
+    size = torch.empty(0, dtype=dtype).element_size()
+    randn = lambda *n: torch.randn(*n, generator=gen, device="cuda", dtype=dtype)
+    rows, heads, dim = args.groups * args.beams, args.kv_heads, args.dim
+    if args.kernel == "beams":
+        logits, scores = randn(rows, args.vocab), torch.randn(rows, generator=gen, device="cuda")
+        return rows * args.vocab * size, lambda: bf.beam_step(logits, scores, args.beams, keep=args.keep)
+    if args.kernel == "reorder":  # every second row of a group is written from the one before it
+        parents = torch.arange(rows, device="cuda") // 2 * 2
+        states = [randn(rows, args.suffix, heads, dim) for _ in range(8)]
+        moved = 8 * (rows // 2) * 2 * args.suffix * heads * dim * size
+        return moved, lambda: bf.beam_reorder(states, parents, args.beams)
+    q = randn(rows, heads * args.share, dim)
+    prefix = [randn(args.groups, args.prefix, heads, dim) for _ in range(2)]
+    suffix = [randn(rows, args.suffix, heads, dim) for _ in range(2)]
+    moved = 2 * (args.groups * args.prefix + rows * args.suffix) * heads * dim * size + 2 * q.numel() * size
+    return moved, lambda: bf.prefix_attention(q, *prefix, *suffix)
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--kernel", choices=("search", "pruned", "eval", "batch", "list", "whatif", "tree",
-                                             "policy", "preference", "scores", "embed_grad"), default="search")
+                                             "policy", "preference", "scores", "embed_grad",
+                                             "attention", "beams", "reorder"), default="search")
     ap.add_argument("--config", type=int, default=3)
     ap.add_argument("--workload", default=None, help="wide28 | wide32 | layered24 (instead of --config)")
     ap.add_argument("--space", type=int, default=3, help="tree search: 3 = full space, 2 = binary")
@@ -62,6 +89,14 @@ def main():
     ap.add_argument("--rows", type=int, default=1024, help="learning calls: tokens")
     ap.add_argument("--vocab", type=int, default=32768)
     ap.add_argument("--width", type=int, default=2048, help="embed_grad: columns of the table")
+    ap.add_argument("--groups", type=int, default=1, help="answering calls: prompts")
+    ap.add_argument("--beams", type=int, default=16, help="answers of a prompt")
+    ap.add_argument("--keep", type=int, default=16, help="beams: continuations")
+    ap.add_argument("--prefix", type=int, default=8192, help="attention: tokens of a prompt")
+    ap.add_argument("--suffix", type=int, default=256, help="attention, reorder: tokens of an answer")
+    ap.add_argument("--kv-heads", type=int, default=8)
+    ap.add_argument("--share", type=int, default=4, help="attention: query heads of a key head")
+    ap.add_argument("--dim", type=int, default=128)
     ap.add_argument("--dtype", default="bfloat16", choices=("float32", "bfloat16", "float16"))
     args = ap.parse_args()
 
@@ -76,6 +111,9 @@ def main():
     unit = "mappings/s"
     if args.kernel in ("policy", "preference", "scores", "embed_grad"):
         work, call = learning_call(args)
+        unit = "B/s"
+    elif args.kernel in ("attention", "beams", "reorder"):
+        work, call = answering_call(args)
         unit = "B/s"
     elif args.kernel == "batch":
         batch = S.config4(args.batch)
