@@ -45,7 +45,10 @@ __device__ __forceinline__ void product(float (&d)[4], const uint32_t (&a)[4], u
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch.global.L1 [%0];" ::"l"(p)); }
+// 8 bytes to shared memory.
+__device__ __forceinline__ void copy_pair(uint32_t to, const void* from) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(__cvta_generic_to_global(from)) : "memory");
+}
 // Four 8 x 8 matrices of 16 bits; the address is of row lane % 8 of matrix lane / 8.
 __device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -67,17 +70,13 @@ struct Few {
   // A step's 16 keys, or values: rows of 128 bytes in columns of 64 dimensions, 16-byte
   // pieces at their place exclusive-or the row modulo 8.
   static constexpr uint32_t kTile = 16 * DP * 2;
-  struct Joining {
-    float o[kWarps][kRows][kPitch];
-    float2 piece[kRows][kMostBlocks * kWarps + kTileParts];  // (m, l), then the weight, of the cluster's warps, then of the prompt's
-  };
-  union {
-    unsigned char ring[kWarps][kStages][2][kTile];
-    Joining join;
-  };
+  static constexpr uint64_t kRings = kWarps * kStages * 2 * kTile;  // all that warps on their own need
+  // The rings; behind the last key, in their place: the warps' outputs of the rows there are, (m, l) and then the
+  // weights of a row's pieces, and as many of the prompt's outputs as fit.
+  unsigned char ring[kRings];
+  static_assert(kWarps * kRows * kPitch * 4 + kRows * (kMostBlocks * kWarps + kTileParts) * 8 <= kRings, "16 rows and all pieces");
   float2 sums[kWarps][kRows];
   float inverse[kRows];
-  static constexpr uint64_t kRings = kWarps * kStages * 2 * kTile;  // all that warps on their own need
 };
 
 template <typename E, uint32_t DP, bool kAlone>
@@ -119,7 +118,7 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
   const Owners own1 = rows0 == rows ? own0 : owners_of(a, plan, standing, prompt, head * plan.row_tiles + tile0 + 1);
   const bool bad = bad_answer(a, prompt, answer);
   // The warp's ring: a lane copies a piece of every (32 / kPieces)-th key.
-  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(sh.ring[warp]);
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(sh.ring + warp * kStages * 2 * kTile);
   const uint32_t my_piece = lane % kPieces, my_key = lane / kPieces;
   const E* k_from = static_cast<const E*>(a.sk.data) + (int64_t)answer * a.sk.batch + (int64_t)head * a.sk.head + my_piece * 8;
   const E* v_from = static_cast<const E*>(a.sv.data) + (int64_t)answer * a.sv.batch + (int64_t)head * a.sv.head + my_piece * 8;
@@ -142,16 +141,13 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
 
   // What the prompts' kernel wrote is there from here on (it takes whole SMs: blocks of this one hardly start before it ends).
   wait_for_previous();
-  // The prompt's records of this answer's rows, on their way into this SM's cache meanwhile.
   const auto record_of = [&](const Owners& own, uint32_t i) { return plan.prefix + (own.first + i + own.segment) * plan.record; };
   const uint32_t quads = a.dim / 4, sums_at = record_sums(plan.rows, a.dim), r0 = row0 - tile0 * plan.rows;
+  uint32_t gave = 0;
   if (!kAlone) {
-    const uint32_t far = own0.last - own0.first;
-    for (uint32_t i = warp; i < far; i += kWarps) {  // 32 bytes are four rows' sums, or two rows' quads of dimensions
-      const float* record = record_of(own0, i);
-      if (lane < rows0) prefetch(record + sums_at + 2 * (r0 + lane));
-      for (uint32_t n = 2 * lane; n < quads * rows0; n += 64) prefetch(record + record_place(plan.rows, r0 + n % rows0, n / rows0 * 4));
-    }
+    const uint32_t from = own0.first, to = max(own0.last, own1.last);
+    if (from + lane < to) gave = __ldca(plan.gave_up + from + lane);
+    for (uint32_t i = from + lane + 32; i < to; i += 32) gave |= __ldca(plan.gave_up + i);
   }
   float o[DP / 8][4] = {};
   float m[2] = {kNone, kNone}, l[2] = {0.0f, 0.0f};  // rows g and g + 8
@@ -289,7 +285,49 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
     }
     return;
   }
-  __syncthreads();  // the rings are done with: the warps' outputs take their place
+  __syncthreads();  // the rings are done with
+  const uint32_t near = few.blocks * kWarps, most_pieces = near + max(own0.last - own0.first, own1.last - own1.first);
+  float* const outputs = reinterpret_cast<float*>(sh.ring);
+  float2* const pieces = reinterpret_cast<float2*>(outputs + kWarps * rows * Few<DP>::kPitch);
+  const uint32_t held_at = (kWarps * rows * Few<DP>::kPitch * 4 + rows * most_pieces * 8 + 15) / 16 * 16;
+  float4* const held = reinterpret_cast<float4*>(sh.ring + held_at) + threadIdx.x;
+  const uint32_t most_held = (uint32_t)((sizeof(sh.ring) - held_at) / (kThreads * 16));
+  const auto output_of = [&](Few<DP>* from, uint32_t w, uint32_t row, uint32_t d) {
+    return reinterpret_cast<float*>(from->ring) + (w * rows + row) * Few<DP>::kPitch + d;
+  };
+  // How the joining is shared out: four dimensions of a row to a thread, neighbouring rows to neighbours, over the
+  // cluster's blocks; where they have threads enough up to eight lanes of a warp share an item's pieces out.
+  const uint32_t items = rows * quads;
+  uint32_t parts = 1;
+  while (parts < 8 && 2 * parts * items <= few.blocks * kThreads) parts *= 2;
+  const uint32_t width = 32 / parts, part = lane / width;
+  const auto each_item = [&](auto f) {  // f(item, whether there is one, row, first dimension, its pieces' first, how many), by whole warps
+    for (uint32_t n0 = (rank * kWarps + warp) * width; n0 < items; n0 += few.blocks * kWarps * width) {
+      const uint32_t n = n0 + lane % width, row = n < items ? n % rows : 0, d = n < items ? n / rows * 4 : 0;
+      const Owners& own = row < rows0 ? own0 : own1;
+      f(n < items, row, d, record_of(own, 0) + record_place(plan.rows, row < rows0 ? r0 + row : row - rows0, d), own.last - own.first);
+    }
+  };
+  // The prompt's records of these rows, all on their way at once while the weights are found: (m, l), and what each
+  // thread will add up.  (Read where they are used, eight at a time, they were three rounds of 2,000 cycles.)
+  for (uint32_t row = warp; row < rows; row += kWarps) {
+    const Owners& own = row < rows0 ? own0 : own1;
+    const float* from = record_of(own, 0) + sums_at + 2 * (row < rows0 ? r0 + row : row - rows0);
+    for (uint32_t i = lane; i < own.last - own.first; i += 32)
+      copy_pair((uint32_t)__cvta_generic_to_shared(pieces + row * most_pieces + near + i), from + (uint64_t)i * plan.record);
+  }
+  copies_end();
+  {
+    uint32_t n = 0;
+    each_item([&](bool, uint32_t, uint32_t, const float* from, uint32_t far) {
+      const uint32_t some = min(far > part ? (far - part + parts - 1) / parts : 0u, most_held - n);
+#pragma unroll 4
+      for (uint32_t j = 0; j < some; ++j)
+        copy_piece((uint32_t)__cvta_generic_to_shared(held + (n + j) * kThreads), from + (uint64_t)(part + j * parts) * plan.record, true);
+      n += some;
+    });
+    copies_end();
+  }
   // Element i of o[n] is of row g + i / 2 * 8 and dimension 8 n + 2 c + i % 2.
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
@@ -300,41 +338,34 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
     if (c == 0) sh.sums[warp][row] = make_float2(m[r], l[r]);
 #pragma unroll
     for (uint32_t n = 0; n < DP / 8; ++n)
-      *reinterpret_cast<float2*>(&sh.join.o[warp][row][8 * n + 2 * c]) = make_float2(o[n][2 * r], o[n][2 * r + 1]);
+      *reinterpret_cast<float2*>(output_of(&sh, warp, row, 8 * n + 2 * c)) = make_float2(o[n][2 * r], o[n][2 * r + 1]);
   }
   const bool clustered = few.blocks > 1;
   cg::cluster_group cluster = cg::this_cluster();
+  copies_wait<1>();
   if (clustered) cluster.sync();
   else __syncthreads();
 
   // The weights of a row's pieces: of the warps of all blocks here, and of the prompt's.
-  const uint32_t near = few.blocks * kWarps;
   const auto peer = [&](uint32_t b) -> Few<DP>* { return clustered ? cluster.map_shared_rank(&sh, b) : &sh; };
   for (uint32_t row = warp; row < rows; row += kWarps) {
-    const Owners own = row < rows0 ? own0 : own1;
-    const uint32_t r = row < rows0 ? r0 + row : row - rows0, far = own.last - own.first;
-    bool odd = bad;
+    const uint32_t far = row < rows0 ? own0.last - own0.first : own1.last - own1.first;
+    float2* const piece = pieces + row * most_pieces;
+    bool odd = bad || gave != 0;
     float most = kNone;
     for (uint32_t i = lane; i < near + far; i += 32) {
-      float2 ml;
-      if (i < near) {
-        ml = peer(i / kWarps)->sums[i % kWarps][row];
-      } else {
-        ml = __ldca(reinterpret_cast<const float2*>(record_of(own, i - near) + sums_at) + r);
-        odd |= __ldca(plan.gave_up + own.first + i - near) != 0;
-      }
-      odd |= ml.y != ml.y;
-      most = fmaxf(most, ml.x);
-      sh.join.piece[row][i] = ml;
+      if (i < near) piece[i] = peer(i / kWarps)->sums[i % kWarps][row];
+      odd |= piece[i].y != piece[i].y;
+      most = fmaxf(most, piece[i].x);
     }
 #pragma unroll
     for (int d = 16; d; d /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
     const float base = most == kNone ? 0.0f : most;
     float total = 0.0f;
     for (uint32_t i = lane; i < near + far; i += 32) {
-      const float2 ml = sh.join.piece[row][i];
+      const float2 ml = piece[i];
       const float w = ml.y > 0.0f ? exp2_of(ml.x - base) : 0.0f;  // 0: nothing to attend to in that piece
-      sh.join.piece[row][i].x = w;
+      piece[i].x = w;
       total = fmaf(w, ml.y > 0.0f ? ml.y : 0.0f, total);
     }
 #pragma unroll
@@ -348,34 +379,32 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
             odd ? nan : total > 0.0f ? (most + log2f(total)) * 0.693147180559945309f : kNone;
     }
   }
+  copies_wait<0>();
   __syncthreads();
-  // Four dimensions of a row to a thread, neighbouring rows to neighbours; the cluster's blocks share them out.
   const bool whole = ((uintptr_t)a.out.data | (uint64_t)a.out.batch * 2 | (uint64_t)a.out.head * 2) % 8 == 0;
-  for (uint32_t n = rank * kThreads + threadIdx.x; n < rows * quads; n += few.blocks * kThreads) {
-    const uint32_t row = n % rows, d = n / rows * 4;
-    const Owners& own = row < rows0 ? own0 : own1;
-    const uint32_t r = row < rows0 ? r0 + row : row - rows0, far = own.last - own.first;
+  uint32_t next = 0;
+  each_item([&](bool on, uint32_t row, uint32_t d, const float* from, uint32_t far) {
     float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const float2* piece = pieces + row * most_pieces;
     const auto add = [&](float w, const float4& x) {
       if (w > 0.0f) sum = make_float4(fmaf(w, x.x, sum.x), fmaf(w, x.y, sum.y), fmaf(w, x.z, sum.z), fmaf(w, x.w, sum.w));
     };
-    const float* from = record_of(own, 0) + record_place(plan.rows, r, d);
-    constexpr uint32_t kAhead = 8;
-    for (uint32_t i = 0; i < far; i += kAhead) {
-      float4 x[kAhead];
-#pragma unroll
-      for (uint32_t k = 0; k < kAhead; ++k)
-        if (i + k < far) x[k] = __ldca(reinterpret_cast<const float4*>(from + (uint64_t)(i + k) * plan.record));
-#pragma unroll
-      for (uint32_t k = 0; k < kAhead; ++k)
-        if (i + k < far) add(sh.join.piece[row][near + i + k].x, x[k]);
+    const uint32_t some = min(far > part ? (far - part + parts - 1) / parts : 0u, most_held - next);
+#pragma unroll 4
+    for (uint32_t j = 0; j < some; ++j) add(piece[near + part + j * parts].x, held[(next + j) * kThreads]);
+    next += some;
+#pragma unroll 4
+    for (uint32_t i = part + some * parts; i < far; i += parts) add(piece[near + i].x, __ldca(reinterpret_cast<const float4*>(from + (uint64_t)i * plan.record)));
+#pragma unroll 4
+    for (uint32_t i = part; i < near; i += parts)
+      add(piece[i].x, *reinterpret_cast<const float4*>(output_of(peer(i / kWarps), i % kWarps, row, d)));
+    for (uint32_t apart = width; apart < 32; apart *= 2) {
+      sum.x += __shfl_xor_sync(~0u, sum.x, apart);
+      sum.y += __shfl_xor_sync(~0u, sum.y, apart);
+      sum.z += __shfl_xor_sync(~0u, sum.z, apart);
+      sum.w += __shfl_xor_sync(~0u, sum.w, apart);
     }
-    for (uint32_t b = 0; b < few.blocks; ++b) {
-      const Few<DP>* them = peer(b);
-#pragma unroll
-      for (uint32_t w = 0; w < kWarps; ++w) add(sh.join.piece[row][b * kWarps + w].x, *reinterpret_cast<const float4*>(&them->join.o[w][row][d]));
-    }
-    {
+    if (on && part == 0) {
       const float inv = sh.inverse[row];
       E* out = static_cast<E*>(const_cast<void*>(a.out.data)) + (int64_t)answer * a.out.batch +
                (int64_t)(head * a.share + first + row) * a.out.head + d;
@@ -387,7 +416,7 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
         h[0] = (uint16_t)u.x, h[1] = (uint16_t)(u.x >> 16), h[2] = (uint16_t)u.y, h[3] = (uint16_t)(u.y >> 16);
       }
     }
-  }
+  });
   if (clustered) cluster.sync();  // others may still read this block's outputs
 }
 

@@ -276,29 +276,33 @@ __device__ __forceinline__ uint32_t apart_by(const TileArgs& t, uint32_t rows) {
 template <typename E>
 __device__ __forceinline__ void request_q(const AttendArgs& a, const AttendPlan& plan, const Pieces& p, const TileArgs& t, unsigned char* to) {
   const uint32_t rows = min(plan.rows, a.per_prompt * a.share - p.first_row), most = (rows + 31) / 32 * 32, by = apart_by(t, rows);
-  const uint32_t shift = t.chunks > 1 ? 4 : 3, pieces = (by ? 2 : 1) * most << shift;  // pieces of a row: 8 or 16
+  const uint32_t shift = t.chunks > 1 ? 4 : 3, c = threadIdx.x & ((1u << shift) - 1), step = kSoft >> shift;  // pieces of a row: 8 or 16
   const bool flip = a.scale2 < 0.0f, whole = !flip && ((uintptr_t)a.q.data | (uint64_t)a.q.batch * 2 | (uint64_t)a.q.head * 2) % 16 == 0;
   const E* base = static_cast<const E*>(a.q.data) + (int64_t)((uint64_t)p.at.prompt * a.per_prompt) * a.q.batch +
-                  (int64_t)(p.head * a.share) * a.q.head;
-#pragma unroll 1
-  for (uint32_t n = threadIdx.x; n < pieces; n += kSoft) {
-    uint32_t row = n >> shift, r = row;
-    if (row >= most && by) {
-      row -= most;
-      r = row + by;
-    }
-    const uint32_t c = n & ((1u << shift) - 1), at = p.first_row + row, answer = at / a.share;
+                  (int64_t)(p.head * a.share) * a.q.head + c * 8;
+  const uint32_t step_answer = step / a.share, step_head = step - step_answer * a.share;
+  uint32_t row = threadIdx.x >> shift, answer = (p.first_row + row) / a.share, head = p.first_row + row - answer * a.share;
+#pragma unroll 2
+  for (; row < most; row += step) {
     const bool on = row < rows && c * 8 < a.dim;
-    const E* q = on ? base + (int64_t)answer * a.q.batch + (int64_t)(at - answer * a.share) * a.q.head + c * 8 : base;
-    unsigned char* place = to + (r / kRows * t.chunks + c / 8) * (kRows * 128) + r % kRows * 128 + (c % 8 ^ r % 8) * 16;
+    const E* q = on ? base + (int64_t)answer * a.q.batch + (int64_t)head * a.q.head : static_cast<const E*>(a.q.data);
+    unsigned char* place = to + (row / kRows * t.chunks + c / 8) * (kRows * 128) + row % kRows * 128 + (c % 8 ^ row % 8) * 16;
     if (whole) {
       copy_piece(shared_address(place), q, on);
+      if (by) copy_piece(shared_address(place + by * 128), q, on);
     } else {
       uint32_t u[4];
       const uint16_t* h = reinterpret_cast<const uint16_t*>(q);
 #pragma unroll
       for (int k = 0; k < 4; ++k) u[k] = on ? (h[2 * k] | (uint32_t)h[2 * k + 1] << 16) ^ (flip ? 0x80008000u : 0u) : 0u;
       *reinterpret_cast<uint4*>(place) = make_uint4(u[0], u[1], u[2], u[3]);
+      if (by) *reinterpret_cast<uint4*>(place + by * 128) = make_uint4(u[0], u[1], u[2], u[3]);
+    }
+    answer += step_answer;
+    head += step_head;
+    if (head >= a.share) {
+      head -= a.share;
+      ++answer;
     }
   }
 }
@@ -483,6 +487,7 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
     if (threadIdx.x == 0) t.gave_up[blockIdx.x] = 1;
     return;
   }
+  Pieces p(a, plan);
   if (threadIdx.x == 0) {
     for (uint32_t i = 0; i < places; ++i) {
       barrier_init(&sh.full[i], 1);
@@ -499,7 +504,6 @@ __global__ void __launch_bounds__(kThreads, 1) tile_kernel(const __grid_constant
   }
   if (warp == 9) tensor_alloc(&sh.tensor, kColumns);
   // The first queries are asked for ahead of the rings' copies: behind them they were 7,000 to 14,000 cycles on their way.
-  Pieces p(a, plan);
   if (warp < 8 && p.more()) request_q<E>(a, plan, p, t, base);
   if (warp == 8 && threadIdx.x % 32 == 0) {
     prefetch_map(&t.k);
