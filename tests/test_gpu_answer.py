@@ -137,6 +137,27 @@ def test_attention_many_tiles(dtype, dim, each, share):
     assert ((lse - top - torch.log(total))[~none].abs() <= sums + 2.0 ** -23 * (most + 20)).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("prompts,each", [(33, 3), (128, 9), (130, 17), (200, 1)])
+def test_attention_many_prompts(dtype, dim, prompts, each):
+    """More prompts than a warp has lanes, most of one tile or none, some of a few."""
+    x = attention_inputs(prompts, each, 8, 2, dim, 400, 20, dtype, seed=prompts)
+    prefix = [(0, 1, 128, 17, 0, 129, 400, 64, 127)[i % 9] for i in range(prompts)]
+    prefix[prompts // 2:prompts // 2 + 5] = [0] * 5
+    prefix[-1] = 300
+    check_attention(x, dtype, prefix, [(20, 0, 7, 16)[i % 4] for i in range(prompts * each)])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 72, 128])
+@pytest.mark.parametrize("each,share", [(1, 16), (2, 40), (9, 4)])
+def test_attention_many_pieces(dtype, dim, each, share):
+    """One prompt's keys in pieces of all blocks, more of them than an answer's joining holds at once."""
+    x = attention_inputs(1, each, share, 1, dim, 19700, 90, dtype, seed=each)
+    check_attention(x, dtype, [19650], [90 - i for i in range(each)])
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_attention_nothing(dtype):
     x = attention_inputs(2, 3, 4, 2, 64, 10, 4, dtype)
