@@ -161,17 +161,21 @@ __device__ void piece(const Piece& p, uint32_t rows, uint32_t dim, float* sm) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[i][c] *= shrink[i];
     }
-    for (uint32_t j = 0; j < n; ++j) {
-      float w[4];
+    // Four keys at a time (weights and values behind the last one are 0): one by one, each
+    // waited for its reads, 190 cycles of 16 rows.
+    for (uint32_t j = 0; j < n; j += 4) {
+      float4 w[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = ps[(rg * 4 + i) * (kKeys + 4) + j];
+      for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float4*>(ps + (rg * 4 + i) * (kKeys + 4) + j);
 #pragma unroll
       for (uint32_t c = 0; c < S::kOuts; ++c) {
         const uint32_t d = cg + c * S::kCols;
-        if (d >= dim) break;
-        const float v = vs[j * pitch + d];
+        if (c * S::kCols >= dim) break;
+        float v[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i][c] = fmaf(w[i], v, o[i][c]);
+        for (uint32_t k = 0; k < 4; ++k) v[k] = d < dim ? vs[(j + k) * pitch + d] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i][c] = fmaf(w[i].w, v[3], fmaf(w[i].z, v[2], fmaf(w[i].y, v[1], fmaf(w[i].x, v[0], o[i][c]))));
       }
     }
     __syncthreads();
@@ -267,13 +271,15 @@ __global__ void __launch_bounds__(kThreads, 2) general_kernel(const __grid_const
 
 // ---- joining ----------------------------------------------------------------
 
-// A warp per query vector, a lane to a dimension: 32 pieces at a time, a lane to a
-// piece's maximum and sum, and eight pieces' outputs on their way.
+// A warp per query vector and 32 dimensions, a lane to a dimension: 32 pieces at a time, a
+// lane to a piece's maximum and sum, and 16 pieces' outputs on their way.  (A warp to
+// all dimensions was 11 us where 120 vectors of 80 dimensions join 23 pieces.)
 template <typename E>
 __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ AttendArgs a,
                                                         const __grid_constant__ AttendPlan plan) {
-  const uint32_t lane = threadIdx.x % 32, heads = a.kv_heads * a.share;
-  const uint64_t vec = (uint64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+  const uint32_t lane = threadIdx.x % 32, heads = a.kv_heads * a.share, columns = (a.dim + 31) / 32;
+  const uint64_t warp = (uint64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32, vec = warp / columns;
+  const uint32_t d = (uint32_t)(warp - vec * columns) * 32 + lane;
   if (vec >= (uint64_t)a.prompts * a.per_prompt * heads) return;
   const uint32_t answer = (uint32_t)(vec / heads), h = (uint32_t)vec - answer * heads, head = h / a.share, prompt = answer / a.per_prompt;
   const uint32_t srow = h - head * a.share, row = (answer - prompt * a.per_prompt) * a.share + srow;
@@ -286,7 +292,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
   const auto record = [&](uint32_t i) { return i < far ? prefix + (uint64_t)i * plan.record : suffix + (uint64_t)(i - far) * plan.suffix_record; };
   const bool bad = bad_answer(a, prompt, answer);
   wait_for_previous();
-  float m = kNone, l = 0.0f, o[kMaxDim / 32] = {};
+  float m = kNone, l = 0.0f, o = 0.0f;
   bool odd = bad;
   for (uint32_t from = 0; from < pieces; from += 32) {
     const uint32_t i = from + lane, some = min(32u, pieces - from);
@@ -299,42 +305,35 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
     odd |= ml.y != ml.y;
     float to = fmaxf(m, ml.x);
 #pragma unroll
-    for (int d = 16; d; d /= 2) to = fmaxf(to, __shfl_xor_sync(~0u, to, d));
+    for (int apart = 16; apart; apart /= 2) to = fmaxf(to, __shfl_xor_sync(~0u, to, apart));
     const float base = to == kNone ? 0.0f : to, shrink = m == kNone ? 0.0f : exp2_of(m - base);
     m = to;
     const float w = ml.y > 0.0f ? exp2_of(ml.x - base) : 0.0f;  // 0: nothing to attend to in that piece
     float sum = ml.y > 0.0f ? w * ml.y : 0.0f;
 #pragma unroll
-    for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
+    for (int apart = 16; apart; apart /= 2) sum += __shfl_xor_sync(~0u, sum, apart);
     l = fmaf(l, shrink, sum);
+    o = shrink == 0.0f ? 0.0f : o * shrink;
+    constexpr uint32_t kAhead = 16;
+    for (uint32_t k = 0; k < some; k += kAhead) {
+      float x[kAhead];
 #pragma unroll
-    for (uint32_t c = 0; c < kMaxDim / 32; ++c) o[c] = shrink == 0.0f ? 0.0f : o[c] * shrink;
+      for (uint32_t j = 0; j < kAhead; ++j) {
+        const uint32_t p = from + k + j;
+        x[j] = k + j < some && d < a.dim ? __ldcg(record(p) + (p < far ? record_place(plan.rows, r0, d) : record_place(plan.suffix_rows, r1, d))) : 0.0f;
+      }
 #pragma unroll
-    for (uint32_t c = 0; c < kMaxDim / 32; ++c) {
-      const uint32_t d = lane + 32 * c;
-      if (32 * c >= a.dim) break;
-      for (uint32_t k = 0; k < some; k += 8) {
-        float x[8];
-#pragma unroll
-        for (uint32_t j = 0; j < 8; ++j) {
-          const uint32_t p = from + k + j;
-          x[j] = k + j < some && d < a.dim ? __ldcg(record(p) + (p < far ? record_place(plan.rows, r0, d) : record_place(plan.suffix_rows, r1, d))) : 0.0f;
-        }
-#pragma unroll
-        for (uint32_t j = 0; j < 8; ++j) {
-          const float f = __shfl_sync(~0u, w, (k + j) % 32);
-          if (k + j < some && f > 0.0f) o[c] = fmaf(f, x[j], o[c]);
-        }
+      for (uint32_t j = 0; j < kAhead; ++j) {
+        const float f = __shfl_sync(~0u, w, (k + j) % 32);
+        if (k + j < some && f > 0.0f) o = fmaf(f, x[j], o);
       }
     }
   }
   odd = __any_sync(~0u, odd);
   const float nan = __int_as_float(0x7FC00000), inv = odd ? nan : l > 0.0f ? 1.0f / l : 0.0f;
   E* out = static_cast<E*>(const_cast<void*>(a.out.data)) + (int64_t)answer * a.out.batch + (int64_t)h * a.out.head;
-#pragma unroll
-  for (uint32_t c = 0; c < kMaxDim / 32; ++c)
-    if (lane + 32 * c < a.dim) out[lane + 32 * c] = from_f32<E>(o[c] * inv);
-  if (a.lse && lane == 0) a.lse[vec] = odd ? nan : l > 0.0f ? (m + log2f(l)) * 0.693147180559945309f : kNone;
+  if (d < a.dim) out[d] = from_f32<E>(o * inv);
+  if (a.lse && d == 0) a.lse[vec] = odd ? nan : l > 0.0f ? (m + log2f(l)) * 0.693147180559945309f : kNone;
 }
 
 // ---- the host's part --------------------------------------------------------
@@ -353,7 +352,8 @@ AttendPlan plan_of(const AttendArgs& a, bool tile, void* workspace, uint64_t* by
   p.suffix_row_tiles = (a.share + p.suffix_rows - 1) / p.suffix_rows;
   const uint64_t pieces = (uint64_t)a.prompts * a.per_prompt * a.kv_heads * p.suffix_row_tiles;
   uint64_t splits = pieces ? kParts / pieces : 1;
-  splits = splits < a.suffix_cap / 128 ? splits : a.suffix_cap / 128;
+  const uint64_t most = (a.suffix_cap + kKeys - 1) / kKeys;  // a tile each: the first of a block takes 12 us, one more 4
+  splits = splits < most ? splits : most;
   p.suffix_splits = splits < 1 ? 1 : (uint32_t)splits;
   p.record = record_floats(p.rows, a.dim);
   p.suffix_record = record_floats(p.suffix_rows, a.dim);
@@ -404,8 +404,8 @@ cudaError_t launch_type(const AttendArgs& a, void* workspace, cudaStream_t st) {
     e = p.suffix_rows == 16 ? launch_sized(general_kernel<E, 16>, general.parts + suffix, shared_of<16>(a.dim), st, a, general)
                             : launch_sized(general_kernel<E, 64>, general.parts + suffix, shared_of<64>(a.dim), st, a, general);
   if (e != cudaSuccess) return e;
-  const uint64_t vectors = answers * a.kv_heads * a.share;
-  return launch_after(join_kernel<E>, (vectors + kThreads / 32 - 1) / (kThreads / 32), kThreads, st, a, p);
+  const uint64_t warps = answers * a.kv_heads * a.share * ((a.dim + 31) / 32);
+  return launch_after(join_kernel<E>, (warps + kThreads / 32 - 1) / (kThreads / 32), kThreads, st, a, p);
 }
 
 }  // namespace
