@@ -530,7 +530,8 @@ typedef struct bf_beam_args {
  * the group's beam j modulo beams.  A logit of NaN or +inf, a score of NaN or
  * +inf makes its group's scores NaN and the rest as if nothing could continue
  * (a finished beam's logits do not matter).  At most 2^23 - 1 groups and a
- * vocabulary of 2^24.  Where the workspace has 0 bytes it may be NULL. */
+ * vocabulary of 2^24.  No output overlaps an input or another output.  Where the
+ * workspace has 0 bytes it may be NULL. */
 BF_API int bf_beam_step(const bf_matrix* logits, const bf_beam_args* args, float* d_scores, int64_t* d_tokens,
                         int64_t* d_parents, uint8_t* d_finished, int64_t* d_lengths, void* d_workspace,
                         uint64_t workspace_bytes, void* cuda_stream);

@@ -231,6 +231,18 @@ int bf_beam_step(const bf_matrix* logits, const bf_beam_args* args, float* d_sco
   if (d_lengths && !args->lengths && logits->rows) return fail(BF_EINVAL, "%s: out lengths need lengths", who);
   if (args->groups == 0) return BF_OK;
   if (need) BF_TRY(check_workspace(d_workspace, workspace_bytes, need, who));
+  // What a group reads again may not be what another one has written.
+  const struct {
+    const void* data;
+    uint64_t bytes;
+  } arrays[] = {{d_scores, places * 4}, {d_tokens, places * 8}, {d_parents, places * 8}, {d_finished, places}, {d_lengths, places * 8},
+                {args->scores, logits->rows * 4}, {args->finished, logits->rows}, {args->lengths, logits->rows * 8},
+                {logits->data, ((logits->rows - 1) * logits->row_stride + logits->cols) * (logits->dtype == BF_F32 ? 4 : 2)}};
+  for (uint32_t i = 0; i < 5; ++i)
+    for (uint32_t j = i + 1; j < 9; ++j)
+      if (arrays[i].data && arrays[j].data && (uintptr_t)arrays[i].data < (uintptr_t)arrays[j].data + arrays[j].bytes &&
+          (uintptr_t)arrays[j].data < (uintptr_t)arrays[i].data + arrays[i].bytes)
+        return fail(BF_EINVAL, "%s: an output overlaps an input or another output", who);
   bfk::BeamArgs a = {};
   a.x = logits->data;
   a.ldx = logits->row_stride;

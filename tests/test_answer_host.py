@@ -121,6 +121,17 @@ def test_bad_beams(lib, i):
     assert bf.last_error().startswith("bf_beam_step")
 
 
+@pytest.mark.parametrize("a,b", [(a, b) for a in range(5) for b in range(a + 1, 9)])
+def test_beams_overlap(lib, a, b):
+    """An output in the last bytes of an input or of another output."""
+    where = [SOME + (i << 20) for i in range(9)]  # scores, tokens, parents, finished, lengths; scores, finished, lengths, logits
+    length = [32, 64, 64, 8, 64, 32, 8, 64, 7 * 100 + 100][b]
+    where[a] = where[b] + length - 8
+    args = beams(scores=where[5], finished=where[6], lengths=where[7], end_token=1)
+    assert step(lib, mat(data=where[8]), args, *where[:5]) == bf.BF_EINVAL
+    assert "overlaps" in bf.last_error()
+
+
 def test_beams_null_and_none(lib):
     x, args = mat(), beams()
     assert lib.bf_beam_step(None, at(args), SOME, SOME, SOME, None, None, SOME, 1 << 30, None) == bf.BF_EINVAL
