@@ -14,6 +14,8 @@ namespace {
 // R / 16 (scores) or dim / (1024 / R) (outputs) values, so that a value read from
 // shared memory is used four times or more.  16 rows are bound by the keys' way here, and
 // have keys and values on it at once; 64 by the sums, and have room for two blocks an SM.
+// Two prompts of 1,500 keys, 5 answers, 12 query and 4 key heads of 80 dimensions in 32 bits:
+// 16.4 us with the joining, one chain of waiting (a tile of a cold block is 19,000 cycles).
 constexpr uint32_t kThreads = 256, kKeys = 64, kMaxDim = 256;
 
 template <uint32_t R>

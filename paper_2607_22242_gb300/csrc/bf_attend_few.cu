@@ -12,7 +12,12 @@
 // Behind its own keys a block waits for the prompts' pieces and joins all of them.
 //
 // Where there are units enough to give every warp one of its own (kAlone), it does: what
-// a warp does once (finding its pieces, joining) was two thirds of the instructions.
+// a warp does once (finding its pieces, joining) was two thirds of the instructions.  A call
+// with 128 keys of prompt, 64 dimensions and 32 / 160 / 600 own keys, so and by four warps:
+// 608 units 15.7 / 22.4 / 45.6 and 14.4 / 15.8 / 26.2 us, 1,216 units 16.4 / 23.7 / 46.6 and
+// 19.2 / 24.6 / 43.8, 2,432 units 18.6 / 29.7 / 67.7 and 28.7 / 38.1 / 73.3.
+//
+// 134 MB of 64 answers' own keys take about 30 us behind a long prompt's, 4.5 TB/s.
 #include <cooperative_groups.h>
 
 #include "bf_attend.cuh"
@@ -25,7 +30,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr uint32_t kThreads = 128, kWarps = kThreads / 32, kRows = 16, kMostBlocks = 8;
-constexpr uint64_t kAloneUnits = 1216;  // eight an SM
+constexpr uint64_t kAloneUnits = 1216;  // eight an SM, from which on every warp has one
 constexpr float kRaise = 8.0f;
 
 struct FewArgs {
