@@ -1,8 +1,8 @@
 // bf_attend_few.cu -- an answer's own keys, and the joining of all that was attended
 // to: 16-bit types, up to 128 dimensions.
 //
-// A block to an answer and key head (and up to 16 of the query heads that share
-// it); in a cluster where there are few, so that an answer's keys are spread over
+// A unit is an answer and key head (and up to 16 of the query heads that share
+// it); in a cluster of blocks where there are few, so that an answer's keys are spread over
 // several SMs.  Each warp takes 16 keys at a time through a ring of its own in shared
 // memory, two steps ahead by asynchronous copies, so that the keys on their way
 // cost no registers (kept there, two blocks an SM had 64 KB on their way and stood
@@ -11,14 +11,19 @@
 //
 // Behind its own keys a block waits for the prompts' pieces and joins all of them.
 //
-// Where there are units enough to give every warp one of its own (kAlone), it does: what
-// a warp does once (finding its pieces, joining) was two thirds of the instructions.  A call
-// with 128 keys of prompt, 64 dimensions and 32 / 160 / 600 own keys, so and by four warps:
-// 608 units 15.7 / 22.4 / 45.6 and 14.4 / 15.8 / 26.2 us, 1,216 units 16.4 / 23.7 / 46.6 and
-// 19.2 / 24.6 / 43.8, 2,432 units 18.6 / 29.7 / 67.7 and 28.7 / 38.1 / 73.3.
+// A unit has four warps, or two where there are more units than four warps' blocks fit
+// on the GPU at once, and where there are units enough to give every warp one of its own
+// (kAlone), it has that: what a warp does once (finding its pieces, joining) was two thirds of the
+// instructions.  A call with 128 keys of prompt, 64 dimensions and 32 / 160 / 600 own keys, in us:
+//   units  four warps          two                 one
+//     608  14.4 / 15.8 / 26.2  -                   15.7 / 22.4 / 45.6
+//     912  17.8 / 21.3 / 37.5  13.7 / 17.2 / 33.2  15.8 / 22.4 / 45.9
+//   1,216  19.2 / 24.6 / 43.8  17.9 / 24.4 / 49.1  16.4 / 23.7 / 46.6
+//   2,432  28.7 / 38.1 / 73.3  23.3 / 34.2 / 76.1  18.6 / 29.7 / 67.7
 //
-// 134 MB of 64 answers' own keys take about 30 us behind a long prompt's, 4.5 TB/s.
+// 134 MB of 64 answers' own keys take about 28 us behind a long prompt's, 4.8 TB/s.
 #include <cooperative_groups.h>
+#include <type_traits>
 
 #include "bf_attend.cuh"
 #include "bf_blackwell.cuh"
@@ -29,7 +34,7 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr uint32_t kThreads = 128, kWarps = kThreads / 32, kRows = 16, kMostBlocks = 8;
+constexpr uint32_t kRows = 16, kMostBlocks = 8;
 constexpr uint64_t kAloneUnits = 1216;  // eight an SM, from which on every warp has one
 constexpr float kRaise = 8.0f;
 
@@ -69,27 +74,29 @@ __device__ __forceinline__ void load_turned(uint32_t (&r)[4], uint32_t at) {
 }
 
 // DP: dimensions, to a multiple of 64.
-template <uint32_t DP>
+template <uint32_t DP, uint32_t kWarps>
 struct Few {
   static constexpr uint32_t kPitch = DP + 4, kStages = 3;
   // A step's 16 keys, or values: rows of 128 bytes in columns of 64 dimensions, 16-byte
   // pieces at their place exclusive-or the row modulo 8.
   static constexpr uint32_t kTile = 16 * DP * 2;
   static constexpr uint64_t kRings = kWarps * kStages * 2 * kTile;  // all that warps on their own need
+  static constexpr uint64_t kJoining = kWarps * kRows * kPitch * 4 + kRows * (kMostBlocks * kWarps + kTileParts) * 8;  // 16 rows and all pieces
   // The rings; behind the last key, in their place: the warps' outputs of the rows there are, (m, l) and then the
   // weights of a row's pieces, and as many of the prompt's outputs as fit.
-  unsigned char ring[kRings];
-  static_assert(kWarps * kRows * kPitch * 4 + kRows * (kMostBlocks * kWarps + kTileParts) * 8 <= kRings, "16 rows and all pieces");
+  unsigned char ring[kRings > kJoining ? kRings : kJoining];
   float2 sums[kWarps][kRows];
   float inverse[kRows];
 };
 
-template <typename E, uint32_t DP, bool kAlone>
-__global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ AttendPlan plan,
+template <typename E, uint32_t DP, uint32_t kWarps, bool kAlone>
+__global__ void __launch_bounds__(kWarps * 32) few_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ AttendPlan plan,
                                                        const __grid_constant__ FewArgs few) {
   extern __shared__ __align__(128) unsigned char raw[];
-  Few<DP>& sh = *reinterpret_cast<Few<DP>*>(raw);
-  constexpr uint32_t kStages = Few<DP>::kStages, kTile = Few<DP>::kTile, kPieces = DP / 8;  // pieces of a key
+  using Shared = Few<DP, kWarps>;
+  constexpr uint32_t kThreads = kWarps * 32;
+  Shared& sh = *reinterpret_cast<Shared*>(raw);
+  constexpr uint32_t kStages = Shared::kStages, kTile = Shared::kTile, kPieces = DP / 8;  // pieces of a key
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, c = lane % 4;
   const uint32_t rank = kAlone ? 0 : blockIdx.x % few.blocks;
   uint32_t unit = kAlone ? blockIdx.x * kWarps + warp : blockIdx.x / few.blocks;
@@ -293,12 +300,12 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
   __syncthreads();  // the rings are done with
   const uint32_t near = few.blocks * kWarps, most_pieces = near + max(own0.last - own0.first, own1.last - own1.first);
   float* const outputs = reinterpret_cast<float*>(sh.ring);
-  float2* const pieces = reinterpret_cast<float2*>(outputs + kWarps * rows * Few<DP>::kPitch);
-  const uint32_t held_at = (kWarps * rows * Few<DP>::kPitch * 4 + rows * most_pieces * 8 + 15) / 16 * 16;
+  float2* const pieces = reinterpret_cast<float2*>(outputs + kWarps * rows * Shared::kPitch);
+  const uint32_t held_at = (kWarps * rows * Shared::kPitch * 4 + rows * most_pieces * 8 + 15) / 16 * 16;
   float4* const held = reinterpret_cast<float4*>(sh.ring + held_at) + threadIdx.x;
   const uint32_t most_held = (uint32_t)((sizeof(sh.ring) - held_at) / (kThreads * 16));
-  const auto output_of = [&](Few<DP>* from, uint32_t w, uint32_t row, uint32_t d) {
-    return reinterpret_cast<float*>(from->ring) + (w * rows + row) * Few<DP>::kPitch + d;
+  const auto output_of = [&](Shared* from, uint32_t w, uint32_t row, uint32_t d) {
+    return reinterpret_cast<float*>(from->ring) + (w * rows + row) * Shared::kPitch + d;
   };
   // How the joining is shared out: four dimensions of a row to a thread, neighbouring rows to neighbours, over the
   // cluster's blocks; where they have threads enough up to eight lanes of a warp share an item's pieces out.
@@ -352,7 +359,7 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ A
   else __syncthreads();
 
   // The weights of a row's pieces: of the warps of all blocks here, and of the prompt's.
-  const auto peer = [&](uint32_t b) -> Few<DP>* { return clustered ? cluster.map_shared_rank(&sh, b) : &sh; };
+  const auto peer = [&](uint32_t b) -> Shared* { return clustered ? cluster.map_shared_rank(&sh, b) : &sh; };
   for (uint32_t row = warp; row < rows; row += kWarps) {
     const uint32_t far = row < rows0 ? own0.last - own0.first : own1.last - own1.first;
     float2* const piece = pieces + row * most_pieces;
@@ -438,18 +445,22 @@ cudaError_t launch_few_queries(const AttendArgs& a, const AttendPlan& plan, cuda
   const uint64_t units = (uint64_t)a.prompts * a.per_prompt * a.kv_heads * f.row_tiles;
   if (units > 0x7FFFFFFFu) return cudaErrorInvalidValue;
   f.units = (uint32_t)units;
-  const bool alone = units >= kAloneUnits;
+  const bool alone = units >= kAloneUnits, two = !alone && units > (a.dim <= 64 ? 608 : 304);
   while (!alone && f.blocks < kMostBlocks && units * f.blocks * 2 <= 304 && a.suffix_cap > 64ull * f.blocks) f.blocks *= 2;  // two an SM
-  const auto launch = [&](auto kernel, uint64_t shared) {
+  const auto launch = [&](auto kernel, uint32_t warps, uint64_t shared) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
     if (e != cudaSuccess) return e;
-    return launch_shared(kernel, alone ? (units + kWarps - 1) / kWarps : units * f.blocks, kThreads, f.blocks, true, shared, st, a, plan, f);
+    return launch_shared(kernel, alone ? (units + warps - 1) / warps : units * f.blocks, warps * 32, f.blocks, true, shared, st, a, plan, f);
+  };
+  const auto launch_dim = [&](auto type, auto dim) {
+    using E = decltype(type);
+    constexpr uint32_t DP = decltype(dim)::value;
+    return alone ? launch(few_kernel<E, DP, 4, true>, 4, Few<DP, 4>::kRings)
+           : two ? launch(few_kernel<E, DP, 2, false>, 2, sizeof(Few<DP, 2>))
+                 : launch(few_kernel<E, DP, 4, false>, 4, sizeof(Few<DP, 4>));
   };
   const auto launch_type = [&](auto type) {
-    using E = decltype(type);
-    if (a.dim <= 64)
-      return alone ? launch(few_kernel<E, 64, true>, Few<64>::kRings) : launch(few_kernel<E, 64, false>, sizeof(Few<64>));
-    return alone ? launch(few_kernel<E, 128, true>, Few<128>::kRings) : launch(few_kernel<E, 128, false>, sizeof(Few<128>));
+    return a.dim <= 64 ? launch_dim(type, std::integral_constant<uint32_t, 64>()) : launch_dim(type, std::integral_constant<uint32_t, 128>());
   };
   return a.dtype == BF_BF16 ? launch_type(__nv_bfloat16()) : launch_type(__half());
 }
