@@ -158,6 +158,15 @@ def test_attention_many_pieces(dtype, dim, each, share):
     check_attention(x, dtype, [19650], [90 - i for i in range(each)])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("prompts,kv_heads", [(1, 1), (2, 2), (4, 2), (9, 2)])
+def test_attention_shared_widely(dtype, dim, prompts, kv_heads):
+    """An answer's 20 query heads of a key head in two parts, some of which lie in two tiles of a prompt's queries."""
+    x = attention_inputs(prompts, 40, 20 * kv_heads, kv_heads, dim, 700, 100, dtype, seed=prompts)
+    check_attention(x, dtype, [700 - 150 * (i % 5) for i in range(prompts)], [(100, 0, 1, 33, 64)[i % 5] for i in range(40 * prompts)])
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_attention_nothing(dtype):
     x = attention_inputs(2, 3, 4, 2, 64, 10, 4, dtype)
