@@ -55,7 +55,7 @@ __device__ __forceinline__ uint32_t block_count(uint32_t mine, uint32_t* sums) {
 
 // Bounds that at least `keep` of a block's threads' values reach (keep <= threads), and mostly not many more; above -inf.
 //
-// Where the warps' values are alike: each warp finds its ceil(2 keep / warps)-th
+// Where the values of the `full` warps that have some are alike: each finds its ceil(2 keep / full)-th
 // largest, and the one of those that enough warps reach is the bound.  One barrier.
 // `warps` holds a word for each warp.
 // The need-th largest of the warps' values (the same in all of a warp's lanes).
@@ -72,8 +72,8 @@ __device__ __forceinline__ uint32_t bound_of_warps(uint32_t value, uint32_t need
   const uint32_t bound = __reduce_max_sync(~0u, lane < count && above == need - 1 ? w : 0);
   return max(bound, kOrderMinusInf + 1);
 }
-__device__ __forceinline__ uint32_t bound_of(uint32_t mine, uint32_t keep, uint32_t* warps) {
-  const uint32_t count = blockDim.x / 32, each = min(32u, (2 * keep + count - 1) / count), lane = threadIdx.x % 32;
+__device__ __forceinline__ uint32_t bound_of(uint32_t mine, uint32_t keep, uint32_t full, uint32_t* warps) {
+  const uint32_t each = min(32u, (2 * keep + full - 1) / full), lane = threadIdx.x % 32;
   uint32_t most = 0;
   for (uint32_t i = 0; i < each; ++i) {
     most = __reduce_max_sync(~0u, mine);
@@ -84,8 +84,8 @@ __device__ __forceinline__ uint32_t bound_of(uint32_t mine, uint32_t keep, uint3
 // The same from N values of each thread (N times as many: for a `keep` that is large
 // beside the threads), the warps' by bisection.
 template <int N>
-__device__ __forceinline__ uint32_t bound_of_all(const uint32_t (&mine)[N], uint32_t keep, uint32_t* warps) {
-  const uint32_t count = blockDim.x / 32, each = min(32u * N, (2 * keep + count - 1) / count);
+__device__ __forceinline__ uint32_t bound_of_all(const uint32_t (&mine)[N], uint32_t keep, uint32_t full, uint32_t* warps) {
+  const uint32_t each = min(32u * N, (2 * keep + full - 1) / full);
   uint32_t lo = 0, hi = 0xFFFFFFFFu;
   while (hi - lo > 1) {
     const uint32_t mid = lo + (hi - lo) / 2;
@@ -291,6 +291,23 @@ __device__ __forceinline__ float sum_of(const uint4 (&u)[V], float m, float c2) 
   return fmaf(s, rest, s);
 }
 
+// V aligned vectors of each lane, which follow one another over a warp's lanes and then its turns, shifted down by
+// `off` bytes, of which W are whole words; `tail` is what follows the last one (lane 0's).  A lane has its next words from its neighbour.
+template <int V, int W>
+__device__ __forceinline__ void shift_by(uint4 (&u)[V], const uint4& tail, uint32_t off) {
+  const uint32_t lane = threadIdx.x % 32, r = off % 4 * 8;
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    const uint4 next = k + 1 < V ? u[k + 1 < V ? k + 1 : k] : tail;
+    uint32_t w[8] = {u[k].x, u[k].y, u[k].z, u[k].w, 0, 0, 0, 0};
+    const uint32_t n[4] = {next.x, next.y, next.z, next.w};
+#pragma unroll
+    for (int i = 0; i <= W; ++i) w[4 + i] = __shfl_sync(~0u, lane == 0 ? n[i] : w[i], (lane + 1) % 32);
+    u[k] = make_uint4(__funnelshift_r(w[W], w[W + 1], r), __funnelshift_r(w[W + 1], w[W + 2], r), __funnelshift_r(w[W + 2], w[W + 3], r),
+                      __funnelshift_r(w[W + 3], w[W + 4], r));
+  }
+}
+
 // A chunk of a row, `tiles` times V vectors a thread, cut by the row's elements and not
 // by addresses, so that equal rows have equal sums.  kAligned: rows start at 16 bytes.
 // What reaches a bound that `keep` of the threads' maxima in the first tile reach may be
@@ -314,50 +331,69 @@ __global__ void __launch_bounds__(T, 1024 / T) row_kernel(const __grid_constant_
   if (!is_alive(a, row)) return;
   if (t == 0) count = hits = 0;
   const E* x = static_cast<const E*>(a.x) + (uint64_t)row * a.ldx;
-  const uint32_t cut = chunk * ch.elements;
+  const uint32_t cut = chunk * ch.elements, end = min(cut + ch.elements, a.vocab);
   const uint32_t none = minus_inf_bits(E());
   float m = kMinusInf, s = 0.0f, least = 0.0f;
   uint32_t bound = 0;
 #pragma unroll 1
   for (uint32_t tile = 0; tile < ch.tiles; ++tile) {
-    const uint32_t first = cut + (tile * V * T + t) * kW;
+    // A thread's vectors are `step` elements apart.  Unaligned, a warp's vectors follow one another, up to V times 32,
+    // and all warps have some where a tile is short (44 us for 512 aligned rows of 131,072 as they are, 47 so).
+    const uint32_t tile0 = cut + tile * V * T * kW, last = min(tile0 + V * T * kW, end);
+    const uint32_t turns = tile0 < last ? (last - tile0 + T * kW - 1) / (T * kW) : 0;
+    constexpr uint32_t step = (kAligned ? T : 32) * kW;
+    const uint32_t first = tile0 + (kAligned ? t : t / 32 * turns * 32 + t % 32) * kW;
     uint4 u[V];
     if constexpr (kAligned) {
 #pragma unroll
-      for (int k = 0; k < V; ++k) {
-        const uint32_t j = first + (uint32_t)k * T * kW;
+      for (uint32_t k = 0; k < V; ++k) {
+        const uint32_t j = first + k * step;
         u[k] = make_uint4(none, none, none, none);
-        if (j + kW <= a.vocab) u[k] = __ldcs(reinterpret_cast<const uint4*>(x + j));
-        else if (j < a.vocab) u[k] = load_ends<E>(x + j, 0, (int32_t)(a.vocab - j), none);
+        if (j + kW <= last) u[k] = __ldcs(reinterpret_cast<const uint4*>(x + j));
+        else if (j < last) u[k] = load_ends<E>(x + j, 0, (int32_t)(last - j), none);
       }
     } else {
       const Extent matrix(static_cast<const E*>(a.x), (uint64_t)a.groups * a.beams, a.ldx, a.vocab);
-      Unaligned<E> raw[V];
-      // All rows' vectors lie alike to 16 bytes; where the block's tile is inside the matrix with what is read beside it, nothing is checked.
-      const uint32_t tile0 = cut + tile * V * T * kW, tile1 = tile0 + V * T * kW;
-      const uintptr_t at = (uintptr_t)x, off = at % 16;
-      if (tile1 <= a.vocab && at - off + tile0 * sizeof(E) >= matrix.begin && at - off + tile1 * sizeof(E) + 16 <= matrix.end) {
-        const uint4* p = reinterpret_cast<const uint4*>(at - off) + first / kW;
+      // Each aligned vector is read once, and those behind the row's end but one are not, where all of that lies inside the matrix.
+      const uintptr_t at = (uintptr_t)x, off = at % 16, base = at - off;
+      if (base + (uint64_t)tile0 * sizeof(E) >= matrix.begin && base + ((uint64_t)last + 2 * kW) * sizeof(E) <= matrix.end) {
+        const uint4* p = reinterpret_cast<const uint4*>(base) + first / kW;
+        uint4 tail = make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-          raw[k].off = (uint32_t)off;
-          raw[k].lo = __ldg(p + k * T);
-          raw[k].hi = off ? __ldg(p + k * T + 1) : make_uint4(0, 0, 0, 0);
+        for (uint32_t k = 0; k < V; ++k) {
+          u[k] = make_uint4(none, none, none, none);
+          if (k < turns + (t % 32 == 0) && first + k * step < last + kW) u[k] = __ldg(p + k * 32);
         }
+        if (t % 32 == 0 && turns == V && first + V * step < last + kW) tail = __ldg(p + V * 32);
+        if (off >= 12) shift_by<V, 3>(u, tail, off);
+        else if (off >= 8) shift_by<V, 2>(u, tail, off);
+        else if (off >= 4) shift_by<V, 1>(u, tail, off);
+        else if (off) shift_by<V, 0>(u, tail, off);
+        if (last == end) {  // (in all other tiles every vector is whole)
 #pragma unroll
-        for (int k = 0; k < V; ++k) u[k] = raw[k].take();
+          for (uint32_t k = 0; k < V; ++k) {
+            const uint32_t j = first + k * step;
+            if (k >= turns || j >= last) u[k] = make_uint4(none, none, none, none);
+            else if (j + kW > last) u[k] = load_ends<E>(x + j, 0, (int32_t)(last - j), none);
+          }
+        }
       } else {
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-          const uint32_t j = first + (uint32_t)k * T * kW;
-          if (j < a.vocab) raw[k].load(x, a.vocab, (int64_t)j, matrix);
-        }
+        for (int k = 0; k < V; ++k) u[k] = make_uint4(none, none, none, none);
+#pragma unroll 1
+        for (uint32_t k = 0; k < turns; ++k) {
+          const uint32_t j = first + k * step;
+          uint4 v = make_uint4(none, none, none, none);
+          if (j + kW <= last) {
+            Unaligned<E> raw;
+            raw.load(x, a.vocab, (int64_t)j, matrix);
+            v = raw.take();
+          } else if (j < last) {
+            v = load_ends<E>(x + j, 0, (int32_t)(last - j), none);
+          }
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-          const uint32_t j = first + (uint32_t)k * T * kW;
-          u[k] = make_uint4(none, none, none, none);
-          if (j + kW <= a.vocab) u[k] = raw[k].take();
-          else if (j < a.vocab) u[k] = load_ends<E>(x + j, 0, (int32_t)(a.vocab - j), none);
+          for (uint32_t i = 0; i < V; ++i)
+            if (i == k) u[i] = v;
         }
       }
     }
@@ -374,13 +410,16 @@ __global__ void __launch_bounds__(T, 1024 / T) row_kernel(const __grid_constant_
     m = now;
     s += fabsf(m) * a.c2 < 1024.0f ? sum_of<E, V, true>(u, m, a.c2) : sum_of<E, V, false>(u, m, a.c2);
     if (tile == 0) {
-      if (2 * a.keep <= T * 3 / 4) {
-        bound = bound_of(order_of(tmax), a.keep, warp_bound);
+      // Warps that have vectors; half of them are enough to count on all.
+      const uint32_t each = kAligned ? 32 : turns * 32, some = ((last - tile0 + kW - 1) / kW + each - 1) / each;
+      const uint32_t full = 2 * some >= T / 32 ? T / 32 : some;
+      if (8 * a.keep <= 3 * T && a.keep <= 16 * full) {
+        bound = bound_of(order_of(tmax), a.keep, full, warp_bound);
       } else {
         uint32_t keys[V];
 #pragma unroll
         for (int k = 0; k < V; ++k) keys[k] = order_of(value_of(most[k], E()));
-        bound = bound_of_all<V>(keys, a.keep, warp_bound);
+        bound = bound_of_all<V>(keys, a.keep, full, warp_bound);
       }
       least = from_order(bound);
     }
@@ -393,7 +432,7 @@ __global__ void __launch_bounds__(T, 1024 / T) row_kernel(const __grid_constant_
           const uint32_t at = atomicAdd(&hits, 1u);
           if (at < kHits) {
             hit[at] = u[k];
-            hit_token[at] = first + (uint32_t)k * T * kW;
+            hit_token[at] = first + (uint32_t)k * step;
           }
         }
     }
@@ -421,7 +460,7 @@ __global__ void __launch_bounds__(T, 1024 / T) row_kernel(const __grid_constant_
   __syncthreads();
   uint32_t n = count;
   if (n > kRowList || found > kHits) {
-    const uint32_t some = min(ch.elements, a.vocab - cut);
+    const uint32_t some = end - cut;
     const auto each = [=](auto f) {
       for (uint32_t i = t; i < some; i += T) {
         const float v = to_f32(x[cut + i]);
@@ -788,13 +827,13 @@ __global__ void __launch_bounds__(kThreads) group_kernel(const __grid_constant__
 // groups of 16 x 100 and 16 x 250: 84 and 120 us so, 240 and 170 by rows; 64 groups of 16 x 250: 16.4 and 13.0.)
 constexpr uint64_t kDirectMost = 4096;
 
-// How rows are cut: 8 vectors a thread (4 where each is put together from two), twice
+// How rows are cut: 8 vectors a thread, twice
 // where there are blocks enough all the same (what a block does once takes as long as a tile),
 // 2 where there would be too few for two on each of 152 SMs.  Rows that 64 threads hold in
 // two vectors each have blocks of 64.  (512 rows of 131,072 bf16, 16 kept: 45 us so, 54 with one
 // tile, 60 with 4 vectors; 16,000 rows of 300 and 1,000: 49 and 52 us, 294 and 110 with blocks of 256.)
 constexpr uint32_t kShort = 64;
-Chunks chunks_of(uint32_t groups, uint32_t beams, uint64_t vocab, uint32_t keep, uint32_t width, bool aligned, void* workspace,
+Chunks chunks_of(uint32_t groups, uint32_t beams, uint64_t vocab, uint32_t keep, uint32_t width, void* workspace,
                  uint32_t* vectors, uint64_t* bytes) {
   Chunks c = {};
   *bytes = 0;
@@ -803,11 +842,12 @@ Chunks chunks_of(uint32_t groups, uint32_t beams, uint64_t vocab, uint32_t keep,
   c.tiles = 1;
   c.threads = vocab <= 2 * kShort * width && keep <= kShort * 3 / 8 ? kShort : kThreads;
   const auto per_row = [&](uint32_t v) { return (vocab + c.threads * v * width - 1) / (c.threads * v * width); };
-  *vectors = aligned ? 8 : 4;
+  *vectors = 8;
   if (per_row(2) == 1 || rows * per_row(*vectors) < 304) *vectors = 2;
   else if (keep <= 96 && rows * per_row(2 * *vectors) >= 1216 && per_row(*vectors) > 1) c.tiles = 2;  // (the lists would overflow)
   c.per_row = (uint32_t)per_row(c.tiles * *vectors);
-  c.elements = c.threads * c.tiles * *vectors * width;
+  c.elements = (uint32_t)((vocab + (uint64_t)c.per_row * width - 1) / ((uint64_t)c.per_row * width)) * width;  // evenly
+  c.per_row = (uint32_t)((vocab + c.elements - 1) / c.elements);
   c.heads = static_cast<float2*>(workspace);
   const uint64_t records = rows * c.per_row, heads = (records * sizeof(float2) + 255) / 256 * 256;
   c.best = reinterpret_cast<Candidate*>(static_cast<char*>(workspace) + heads);
@@ -820,7 +860,7 @@ cudaError_t launch_step(const BeamArgs& a, void* workspace, cudaStream_t st) {
   uint32_t vectors = 0;
   uint64_t bytes = 0;
   const bool aligned = ((uintptr_t)a.x | (a.ldx * sizeof(E))) % 16 == 0;
-  const Chunks c = chunks_of(a.groups, a.beams, a.vocab, a.keep, Vec<E>::kWidth, aligned, workspace, &vectors, &bytes);
+  const Chunks c = chunks_of(a.groups, a.beams, a.vocab, a.keep, Vec<E>::kWidth, workspace, &vectors, &bytes);
   const bool direct = c.per_row == 0;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute after;
@@ -841,7 +881,7 @@ cudaError_t launch_step(const BeamArgs& a, void* workspace, cudaStream_t st) {
   cudaError_t e;
   if (c.threads == kShort) e = aligned ? rows(row_kernel<E, 2, true, kShort>) : rows(row_kernel<E, 2, false, kShort>);
   else if (aligned) e = vectors == 8 ? rows(row_kernel<E, 8, true, kThreads>) : rows(row_kernel<E, 2, true, kThreads>);
-  else e = vectors == 4 ? rows(row_kernel<E, 4, false, kThreads>) : rows(row_kernel<E, 2, false, kThreads>);
+  else e = vectors == 8 ? rows(row_kernel<E, 8, false, kThreads>) : rows(row_kernel<E, 2, false, kThreads>);
   if (e != cudaSuccess) return e;
   cfg.blockDim = dim3(kThreads);
   const uint64_t chunks = (uint64_t)a.beams * c.per_row;  // beams, list and lists fit into 48 KB
@@ -1032,10 +1072,10 @@ cudaError_t launch_units(const ReorderArgs& a, bool flat, cudaStream_t st) {
 
 uint64_t beam_bytes(uint32_t groups, uint32_t beams, uint64_t vocab, uint32_t keep) {
   uint64_t most = 0;
-  for (uint32_t i = 0; i < 4; ++i) {  // 4 or 8 elements in 16 bytes, aligned or not
+  for (uint32_t width = 4; width <= 8; width *= 2) {  // elements in 16 bytes
     uint32_t vectors;
     uint64_t bytes;
-    chunks_of(groups, beams, vocab, keep, i % 2 ? 4 : 8, i / 2, nullptr, &vectors, &bytes);
+    chunks_of(groups, beams, vocab, keep, width, nullptr, &vectors, &bytes);
     if (bytes > most) most = bytes;
   }
   return (most + 255) / 256 * 256;

@@ -453,6 +453,26 @@ def test_beams_options(shape, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab,beams,keep", [
+    (1025, 4, 90), (1100, 6, 64), (2049, 4, 16), (4097, 5, 100), (8193, 4, 1), (16385, 3, 40), (33000, 2, 200), (50001, 2, 32)])
+@pytest.mark.parametrize("pad", [0, 1, 2, 3, 5])
+def test_beams_cuts(vocab, beams, keep, pad, dtype):
+    """Rows a little longer than a tile or a chunk, at every alignment, groups few and many: rows cut in all ways."""
+    for groups in (1, 40 if vocab < 9000 else 3):
+        x, scores, _ = beam_inputs(groups, beams, vocab, dtype, seed=vocab + pad)
+        wide = torch.full((groups * beams, vocab + pad), 60000.0, dtype=x.dtype, device="cuda")
+        wide[:, pad // 2:pad // 2 + vocab] = x
+        check_beams(wide[:, pad // 2:pad // 2 + vocab], scores, beams, keep)
+
+
+def test_beams_long_rows():
+    """A row of many more chunks than a thread of a group's block has."""
+    for vocab in (4900000, 4900001):
+        x, scores, _ = beam_inputs(1, 1, vocab, "bf16", seed=5)
+        check_beams(x, scores, 1, 8)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("vocab", [5, 1000, 20000, 50001, 300000])
 def test_beams_ties(vocab, dtype):
     """Equal logits everywhere, equal rows at every alignment, a few values only: ties go to the lower beam and token."""
