@@ -315,7 +315,8 @@ __device__ __forceinline__ void shift_by(uint4 (&u)[V], const uint4& tail, uint3
 //
 // Bound by instruction issue (63 % of the slots; 12 instructions an element, of which the
 // exponential and its sum are 4): 107 MB of 131,072 bf16 logits a row in 31 us, 3.5 TB/s;
-// 36 MB of 50,001 f16 at any alignment in 31.5 us.
+// rows at any alignment take a quarter more (512 of 131,071: 57 us a step, 45 of 131,072),
+// and took two thirds more when each thread read both vectors that hold its elements.
 template <typename E, int V, bool kAligned, uint32_t T>
 __global__ void __launch_bounds__(T, 1024 / T) row_kernel(const __grid_constant__ BeamArgs a, const __grid_constant__ Chunks ch) {
   constexpr uint32_t kW = Vec<E>::kWidth;
@@ -832,6 +833,7 @@ constexpr uint64_t kDirectMost = 4096;
 // 2 where there would be too few for two on each of 152 SMs.  Rows that 64 threads hold in
 // two vectors each have blocks of 64.  (512 rows of 131,072 bf16, 16 kept: 45 us so, 54 with one
 // tile, 60 with 4 vectors; 16,000 rows of 300 and 1,000: 49 and 52 us, 294 and 110 with blocks of 256.)
+// A row's chunks are equally long: 512 rows of 50,000 f16, 32 kept, 40 us, and 43 with all but the last full.
 constexpr uint32_t kShort = 64;
 Chunks chunks_of(uint32_t groups, uint32_t beams, uint64_t vocab, uint32_t keep, uint32_t width, void* workspace,
                  uint32_t* vectors, uint64_t* bytes) {
