@@ -40,6 +40,16 @@ __host__ __device__ __forceinline__ uint32_t record_sums(uint32_t rows, uint32_t
 __host__ __device__ __forceinline__ uint32_t record_floats(uint32_t rows, uint32_t dim) { return record_sums(rows, dim) + 2 * rows; }
 
 constexpr float kNone = -__builtin_huge_valf();
+
+// Weights that are rounded to 16 bits for the second product are taken times 2^kLift, and the maximum less by as much.
+// bf16 has the exponents of 32 bits: a weight is off by 2^-8 of itself at most.  f16 has that (2^-11) from 2^-14 on only, and
+// nothing below 2^-25, where 100,000 keys together still weigh 0.3 % of the largest.  Weights are at most
+// 2^8 (the maximum lags by up to 8) and f16 ends at 2^16: with 2^7 what is lost is below 2^-32 of the largest each.
+template <typename E>
+constexpr float kLift = 0.0f;
+template <>
+constexpr float kLift<__half> = 7.0f;
+
 __device__ __forceinline__ float exp2_of(float t) {
   float e;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));

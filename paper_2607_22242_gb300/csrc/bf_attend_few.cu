@@ -162,7 +162,7 @@ __global__ void __launch_bounds__(kWarps * 32) few_kernel(const __grid_constant_
     for (uint32_t i = from + lane + 32; i < to; i += 32) gave |= __ldca(plan.gave_up + i);
   }
   float o[DP / 8][4] = {};
-  float m[2] = {kNone, kNone}, l[2] = {0.0f, 0.0f};  // rows g and g + 8
+  float m[2] = {kNone, kNone}, l[2] = {0.0f, 0.0f};  // rows g and g + 8; the maxima less by kLift
   // Rows of the matrices that this lane gives the addresses of: of keys for the scores, of values for the outputs.
   const uint32_t k_row = lane % 8, v_row = lane / 8 % 2 * 8 + lane % 8;
   for (uint32_t stage = 0; at < len; at += step, stage = stage + 1 == kStages ? 0 : stage + 1) {
@@ -197,12 +197,12 @@ __global__ void __launch_bounds__(kWarps * 32) few_kernel(const __grid_constant_
     for (int r = 0; r < 2; ++r) {
       top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], 1));
       top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], 2));
-      raise |= top[r] - kRaise > m[r] || (m[r] == kNone && top[r] > kNone);
+      raise |= top[r] - (kRaise + kLift<E>) > m[r] || (m[r] == kNone && top[r] > kNone);
     }
     if (__any_sync(~0u, raise)) {
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        const float to = fmaxf(m[r], top[r]), shrink = m[r] == kNone ? 0.0f : exp2_of(m[r] - to);
+        const float to = fmaxf(m[r], top[r] - kLift<E>), shrink = m[r] == kNone ? 0.0f : exp2_of(m[r] - to);
         m[r] = to;
         l[r] *= shrink;
 #pragma unroll

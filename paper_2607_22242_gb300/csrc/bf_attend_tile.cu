@@ -12,8 +12,9 @@
 // The maximum that weights are taken against is raised only where a score is above
 // it by more than 8 (in log2): weights are at most 2^8, and O in tensor memory is
 // rescaled a few times at the beginning of a piece instead of at every tile.
-// Weights are rounded to the keys' type, a relative 2^-9 (bf16) or 2^-12, as the
-// output is at the end; their sum is of the unrounded ones, in 32 bits.
+// Weights are rounded to the keys' type, which is what the products take: by at most 2^-8 of
+// themselves (bf16) or 2^-11 (f16, those below 2^-21 of the largest by up to 2^-32 of
+// it: kLift), as the output is at the end; their sum is of the unrounded ones, in 32 bits.
 //
 // 131,072 keys of 8 heads of 128 dimensions: 87 us for up to 32 queries a head (6.2 TB/s)
 // and 92 for 128: the memory.  256 queries: 121 us, 1.14 PFLOP/s, the tensor cores busy for
@@ -420,7 +421,8 @@ __device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const T
           tensor_wait_store();
         }
         base = m == kNone ? 0.0f : m;
-        const float2 scale_2 = make_float2(scale, scale), less = make_float2(-base * scale, -base * scale);
+        const float lifted = fmaf(-base, scale, kLift<E>);
+        const float2 scale_2 = make_float2(scale, scale), less = make_float2(lifted, lifted);
         float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll 1
         for (uint32_t c = 0; c < kKeys; c += 64) {
@@ -448,7 +450,7 @@ __device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const T
     const bool both = !t.pair && p.tiles > 1;
     float* record = plan.prefix + (uint64_t)(blockIdx.x + (uint64_t)p.at.prompt * p.inners + p.at.inner) * plan.record;
     float2* sums = reinterpret_cast<float2*>(record + record_sums(plan.rows, a.dim));
-    float2 ml = make_float2(m == kNone ? kNone : m * scale, l);
+    float2 ml = make_float2(m == kNone ? kNone : fmaf(m, scale, -kLift<E>), l);
     float w = 1.0f;
     if (both) {
       const uint32_t by = apart_by(t, rows);

@@ -1,0 +1,62 @@
+"""Corners of the operators of a decoding step on the GPU."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from paper_2607_22242_gb300 import bf  # noqa: E402
+from test_gpu_answer import half  # noqa: E402
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    assert torch.cuda.is_available()
+    bf.load()
+
+
+# ---- weights far below the largest ----
+
+def check_one_above_many(dtype, tokens, prompts, each, own):
+    """Two keys 25.04 above all others (in log2), which together weigh up to 0.4 % of them and have eight times their value.
+    Rounded to f16 where the largest is 1, the others' weights would be 0: below half of f16's lowest number, 2^-24."""
+    above = torch.tensor(17.359375).to(TYPES[dtype]).item()  # (17.375 in bf16)
+    value, first = 8.0, (0, 128)  # a key in each of a prompt's two streams of tiles
+    q = torch.zeros(prompts * each, 1, 8, dtype=TYPES[dtype], device="cuda")
+    q[..., 0] = 1.0
+    k = torch.zeros(prompts * each if own else prompts, tokens, 1, 8, dtype=TYPES[dtype], device="cuda")
+    v = torch.full_like(k, value)
+    for t in first:
+        k[:, t, :, 0], v[:, t] = above, 1.0
+    if own:  # behind a prompt that is empty
+        args, lengths = (q, k[:prompts, :1], v[:prompts, :1], k, v), torch.zeros(prompts, dtype=torch.int64, device="cuda")
+    else:
+        args, lengths = (q, k, v), None
+    out, lse = bf.prefix_attention(*args, prefix_lengths=lengths, scale=1.0, lse=True)
+    w = math.exp(-above)
+    total = len(first) + (tokens - len(first)) * w
+    want = (len(first) + (tokens - len(first)) * w * value) / total
+    # As in test_gpu_answer.py (one product a score, exact); the others' weights are off by half a step, or by half of
+    # f16's lowest step, 2^-25 where the largest is 2^7 or more.
+    weight = 2.0 ** -22 + 2.0 ** -17 + (tokens + 16) * 2.0 ** -24
+    rounded = 0.0 if dtype == "f32" else half(dtype) * (want - 1) * 2
+    tiny = tokens * 2.0 ** -32 * value if dtype == "f16" else 0.0
+    bound = weight * want + rounded + tiny + half(dtype) * want
+    assert dtype != "f16" or want - 1 > bound
+    assert (out.double() - want).abs().max().item() <= bound
+    assert (lse.double() - above - math.log(total)).abs().max().item() <= weight + 2.0 ** -23 * 40
+
+
+@pytest.mark.parametrize("dtype,prompts,each", [("bf16", 152, 1), ("f16", 152, 1), ("bf16", 152, 200), ("f16", 152, 200), ("f32", 19, 30)])
+def test_prompt_of_one_above_many(dtype, prompts, each):
+    """152 prompts, so that every block has a whole prompt as one piece; a tile of queries for one stream and for both."""
+    check_one_above_many(dtype, 131072, prompts, each, False)
+
+
+@pytest.mark.parametrize("dtype,answers", [("bf16", 1216), ("f16", 1216), ("bf16", 400), ("f16", 400), ("f16", 700), ("f32", 40)])
+def test_answers_of_one_above_many(dtype, answers):
+    """The answers' own keys, by a warp each, by two and by four."""
+    check_one_above_many(dtype, 131072, 1, answers, True)
