@@ -570,7 +570,6 @@ bool tile_takes(const AttendArgs& a) {
 
 cudaError_t launch_tile(const AttendArgs& a, const AttendPlan& plan, cudaStream_t st) {
   TileArgs t = {};
-  if (!make_map(&t.k, a.pk, a) || !make_map(&t.v, a.pv, a)) return cudaErrorInvalidValue;
   t.pair = plan.rows == 2 * kRows;
   t.chunks = (a.dim + 63) / 64;
   t.columns = (a.dim + 15) / 16 * 16;
@@ -583,6 +582,9 @@ cudaError_t launch_tile(const AttendArgs& a, const AttendPlan& plan, cudaStream_
   const auto launch = [&](auto kernel) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
     if (e != cudaSuccess) return e;
+    // Behind a call of the runtime, which makes the device's context current: a thread's first call has none, and the
+    // driver then refuses to make a map.
+    if (!make_map(&t.k, a.pk, a) || !make_map(&t.v, a.pv, a)) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(plan.parts);
     cfg.blockDim = dim3(kThreads);

@@ -1,5 +1,7 @@
 """Corners of the operators of a decoding step on the GPU."""
+import ctypes
 import math
+import threading
 
 import pytest
 
@@ -7,7 +9,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 from paper_2607_22242_gb300 import bf  # noqa: E402
-from test_gpu_answer import half  # noqa: E402
+from test_gpu_answer import attention_inputs, half  # noqa: E402
 
 TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
 
@@ -60,3 +62,38 @@ def test_prompt_of_one_above_many(dtype, prompts, each):
 def test_answers_of_one_above_many(dtype, answers):
     """The answers' own keys, by a warp each, by two and by four."""
     check_one_above_many(dtype, 131072, 1, answers, True)
+
+# ---- calls from threads of their own ----
+
+def plain_call(x):
+    """A call of the C entry point again and again with what it was given once: (call, its output)."""
+    lib, code = bf.load(), bf._dtype_code(x[0].dtype)
+    caches = [bf.Cache(t.data_ptr(), t.shape[0], 1 if t.dim() == 3 else t.shape[1], t.shape[-2], t.shape[-1], t.stride(0),
+                       0 if t.dim() == 3 else t.stride(1), t.stride(-2), code, 0) for t in x]
+    out, need = torch.empty_like(x[0]), ctypes.c_uint64(0)
+    caches.append(bf.Cache(out.data_ptr(), *[getattr(caches[0], f) for f in ("batch", "tokens", "heads", "dim")],
+                           out.stride(0), 0, out.stride(1), code, 0))
+    at = [ctypes.addressof(c) for c in caches]
+    args = bf.AttentionArgs(None, None, x[0].shape[2] ** -0.5, 0)
+    assert lib.bf_prefix_attention_workspace(at[0], at[1], at[3], ctypes.byref(need)) == bf.BF_OK
+    work, stream = torch.empty(need.value, dtype=torch.uint8, device="cuda"), torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    held = (caches, args, work, stream, *x)
+    where, given = ctypes.addressof(args), (work.data_ptr(), need.value, stream.cuda_stream)
+    return lambda: lib.bf_prefix_attention(*at[:5], where, at[5], None, *given) if held else None, out
+
+
+@pytest.mark.parametrize("dtype,dim,each", [("bf16", 64, 2), ("f16", 128, 70), ("f32", 64, 2), ("bf16", 30, 2)])
+def test_first_call_of_a_thread(dtype, dim, each):
+    """A call from a thread that has made no other call of CUDA: the device's context is not current there."""
+    x = attention_inputs(1, each, 4, 2, dim, 300, 20, dtype, seed=dim)
+    want = bf.prefix_attention(*x)
+    call, out = plain_call(x)
+    torch.cuda.synchronize()
+    status = []
+    thread = threading.Thread(target=lambda: status.append(call()))
+    thread.start()
+    thread.join()
+    torch.cuda.synchronize()
+    assert status == [bf.BF_OK], bf.last_error()
+    assert torch.equal(out, want)
