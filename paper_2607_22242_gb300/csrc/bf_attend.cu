@@ -373,11 +373,13 @@ AttendPlan plan_of(const AttendArgs& a, bool tile, void* workspace, uint64_t* by
   return p;
 }
 
-template <typename K>
-cudaError_t launch_sized(K kernel, uint64_t blocks, uint32_t shared, cudaStream_t st, const AttendArgs& a, const AttendPlan& p) {
+template <typename E, uint32_t R>
+cudaError_t launch_general(uint64_t blocks, cudaStream_t st, const AttendArgs& a, const AttendPlan& p) {
   if (blocks > 0x7FFFFFFFu) return cudaErrorInvalidValue;
-  if (shared > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+  const uint32_t shared = shared_of<R>(a.dim);
+  if (shared > 48 * 1024) {  // one limit for all sizes: another thread's call may come between this and the launch
+    const cudaError_t e =
+        cudaFuncSetAttribute(general_kernel<E, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared_of<R>(kMaxDim));
     if (e != cudaSuccess) return e;
   }
   cudaLaunchConfig_t cfg = {};
@@ -385,7 +387,7 @@ cudaError_t launch_sized(K kernel, uint64_t blocks, uint32_t shared, cudaStream_
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = shared;
   cfg.stream = st;
-  return cudaLaunchKernelEx(&cfg, kernel, a, p);
+  return cudaLaunchKernelEx(&cfg, general_kernel<E, R>, a, p);
 }
 
 template <typename E>
@@ -403,8 +405,8 @@ cudaError_t launch_type(const AttendArgs& a, void* workspace, cudaStream_t st) {
     general.parts = 0;
   }
   if (e == cudaSuccess && general.parts + suffix)
-    e = p.suffix_rows == 16 ? launch_sized(general_kernel<E, 16>, general.parts + suffix, shared_of<16>(a.dim), st, a, general)
-                            : launch_sized(general_kernel<E, 64>, general.parts + suffix, shared_of<64>(a.dim), st, a, general);
+    e = p.suffix_rows == 16 ? launch_general<E, 16>(general.parts + suffix, st, a, general)
+                            : launch_general<E, 64>(general.parts + suffix, st, a, general);
   if (e != cudaSuccess) return e;
   const uint64_t warps = answers * a.kv_heads * a.share * ((a.dim + 31) / 32);
   return launch_after(join_kernel<E>, (warps + kThreads / 32 - 1) / (kThreads / 32), kThreads, st, a, p);

@@ -34,7 +34,7 @@ constexpr uint32_t kKeys = 128, kRows = 128;
 constexpr uint32_t kSoft = 256, kThreads = kSoft + 96;  // softmax threads; a warp that copies, a warp of products for each stream
 // Tensor memory: S of both streams, O of both; with up to 64 dimensions P of both, which otherwise lies where S was.
 constexpr uint32_t kColumns = 512, kOutputs = 256, kWeights = 384;
-constexpr uint32_t kMaxStages = 12;
+constexpr uint32_t kMaxStages = 12, kMostShared = 227 * 1024;
 constexpr float kRaise = 8.0f;
 
 struct TileArgs {
@@ -576,11 +576,12 @@ cudaError_t launch_tile(const AttendArgs& a, const AttendPlan& plan, cudaStream_
   t.apart = a.dim <= 64;
   t.gave_up = plan.gave_up;
   const uint32_t tile = t.chunks * kKeys * 128, queries = t.pair ? 2 : 1;
-  const uint32_t rings = t.pair ? 1 : 2, fit = (227 * 1024 - sizeof(Shared)) / tile - queries;
+  const uint32_t rings = t.pair ? 1 : 2, fit = (kMostShared - sizeof(Shared)) / tile - queries;
   t.stages = (fit < kMaxStages ? fit : kMaxStages) / rings;
   const uint32_t shared = (queries + rings * t.stages) * tile + sizeof(Shared);
   const auto launch = [&](auto kernel) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+    // One limit for all sizes: another thread's call may come between this and the launch.
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
     if (e != cudaSuccess) return e;
     // Behind a call of the runtime, which makes the device's context current: a thread's first call has none, and the
     // driver then refuses to make a map.

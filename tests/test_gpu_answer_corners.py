@@ -97,3 +97,28 @@ def test_first_call_of_a_thread(dtype, dim, each):
     torch.cuda.synchronize()
     assert status == [bf.BF_OK], bf.last_error()
     assert torch.equal(out, want)
+
+
+def test_threads_of_different_shapes():
+    """Calls whose kernels are the same and whose shared memory is not, each from a thread of its own: all are valid."""
+    sets = [attention_inputs(1, 2, 4, 2, 64, 300, 20, "bf16", seed=1), attention_inputs(1, 70, 8, 2, 128, 300, 20, "bf16", seed=2),
+            attention_inputs(1, 2, 4, 2, 40, 90, 20, "f32", seed=3), attention_inputs(1, 2, 4, 2, 256, 90, 20, "f32", seed=4),
+            attention_inputs(1, 9, 4, 1, 30, 90, 20, "bf16", seed=5), attention_inputs(1, 9, 4, 1, 250, 90, 20, "bf16", seed=6)]
+    want = [bf.prefix_attention(*x) for x in sets]
+    calls = [plain_call(x) for x in sets]
+    torch.cuda.synchronize()
+    refused = [0] * len(sets)
+
+    def work(i):
+        torch.cuda.synchronize()
+        for _ in range(10000):
+            refused[i] += calls[i][0]() != bf.BF_OK
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(sets))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert refused == [0] * len(sets)
+    assert all(torch.equal(out, w) for (_, out), w in zip(calls, want))
