@@ -493,8 +493,8 @@ typedef struct bf_attention_args {
  * NULL.  What lies behind a length is not used, whatever it holds.  With nothing
  * to attend to (lengths 0, or every score -inf) out is 0 and lse -inf; a length
  * outside 0..tokens makes its answers' out and lse NaN.  For 16-bit types the
- * weights e^(s_t - max) are rounded to the type before the second product.  out
- * overlaps no input. */
+ * weights e^(s_t - max) are rounded to the type before the second product.
+ * Neither out nor lse overlaps an input (the lengths among them) or the other. */
 BF_API int bf_prefix_attention(const bf_cache* q, const bf_cache* prefix_k, const bf_cache* prefix_v,
                                const bf_cache* suffix_k, const bf_cache* suffix_v, const bf_attention_args* args,
                                const bf_cache* out, float* d_lse, void* d_workspace, uint64_t workspace_bytes,
@@ -553,8 +553,8 @@ typedef struct bf_states {
  * parent's length is negative; a length above `tokens` counts as `tokens`.
  * `from` and `to` are host arrays of `count` (at most BF_MAX_STATES) device
  * addresses; to[k] == from[k] with the same layout reorders in place (rows that
- * are their own parent cost nothing), otherwise no array overlaps another.  d_lengths is not
- * reordered. */
+ * are their own parent cost nothing), otherwise no array overlaps another.  No array of `to`
+ * overlaps d_parents or d_lengths, which are not reordered. */
 BF_API int bf_beam_reorder(void* const* from, const bf_states* from_layout, void* const* to,
                            const bf_states* to_layout, uint32_t count, const int64_t* d_parents, uint32_t beams,
                            const int64_t* d_lengths, void* cuda_stream);

@@ -39,9 +39,18 @@ int check_like(const bf_cache* c, const bf_cache* k, const char* name, const cha
   return BF_OK;
 }
 
-bool overlap(const bf_cache* a, const bf_cache* b) {
-  const uintptr_t x = (uintptr_t)a->data, y = (uintptr_t)b->data;
-  return x < y + span(b) * size_of(b->dtype) && y < x + span(a) * size_of(a->dtype);
+// Bytes of an argument; none where there is no argument.
+struct Bytes {
+  const void* data;
+  uint64_t count;
+  const char* name;
+};
+bool overlap(const Bytes& a, const Bytes& b) {
+  const uintptr_t x = (uintptr_t)a.data, y = (uintptr_t)b.data;
+  return a.data && b.data && a.count && b.count && x < y + b.count && y < x + a.count;
+}
+Bytes bytes_of(const bf_cache* c, const char* name) {
+  return c ? Bytes{c->data, span(c) * size_of(c->dtype), name} : Bytes{nullptr, 0, name};
 }
 
 // Whether two of the vectors of a one-token cache share elements.
@@ -126,10 +135,13 @@ bool folded(const bf_states* s) {
   return false;
 }
 
+// From an array's first byte to behind its last.
+uint64_t whole_extent(const bf_states* s) { return (s->rows - 1) * s->row_stride + row_extent(s); }
+
 // Whether two arrays share bytes; ones of the same layout may lie between each other's rows.
 bool overlap(const void* a, const bf_states* la, const void* b, const bf_states* lb) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  const uint64_t ea = (la->rows - 1) * la->row_stride + row_extent(la), eb = (lb->rows - 1) * lb->row_stride + row_extent(lb);
+  const uint64_t ea = whole_extent(la), eb = whole_extent(lb);
   if (x >= y + eb || y >= x + ea) return false;
   const uint64_t r = la->row_stride;
   if (la->rows < 2 || r != lb->row_stride || r == 0 || row_extent(la) > r || row_extent(lb) > r) return true;
@@ -175,10 +187,19 @@ int bf_prefix_attention(const bf_cache* q, const bf_cache* prefix_k, const bf_ca
   BF_TRY(check_cache(out, "out", who));
   BF_TRY(check_like(out, q, "out", "q", who));
   if (folded(out)) return fail(BF_EINVAL, "%s: vectors of out overlap", who);
-  if (overlap(out, q) || overlap(out, prefix_k) || overlap(out, prefix_v) || (suffix_k && overlap(out, suffix_k)) ||
-      (suffix_v && overlap(out, suffix_v)))
-    return fail(BF_EINVAL, "%s: out overlaps an input", who);
   BF_TRY(check_array(d_lse, 0, 4, "lse", who));
+  const Bytes outputs[] = {bytes_of(out, "out"), {d_lse, q->batch * q->heads * 4, "lse"}};
+  const Bytes inputs[] = {bytes_of(q, "q"),
+                          bytes_of(prefix_k, "prefix_k"),
+                          bytes_of(prefix_v, "prefix_v"),
+                          bytes_of(suffix_k, "suffix_k"),
+                          bytes_of(suffix_v, "suffix_v"),
+                          {args->prefix_lengths, prefix_k->batch * 8, "prefix_lengths"},
+                          {suffix_k ? args->suffix_lengths : nullptr, q->batch * 8, "suffix_lengths"}};
+  for (const Bytes& o : outputs)
+    for (const Bytes& i : inputs)
+      if (overlap(o, i)) return fail(BF_EINVAL, "%s: %s overlaps %s", who, o.name, i.name);
+  if (overlap(outputs[0], outputs[1])) return fail(BF_EINVAL, "%s: out overlaps lse", who);
   if (q->batch == 0) return BF_OK;
   const uint64_t need = bfk::attend_bytes(a);
   BF_TRY(check_workspace(d_workspace, workspace_bytes, need, who));
@@ -291,6 +312,11 @@ int bf_beam_reorder(void* const* from, const bf_states* from_layout, void* const
     a.from[k] = static_cast<const char*>(from[k]);
     a.to[k] = static_cast<char*>(to[k]);
   }
+  // What every block reads again may not be what another one has written.
+  const Bytes read[] = {{d_parents, f->rows * 8, "parents"}, {d_lengths, f->rows * 8, "lengths"}};
+  for (uint32_t k = 0; k < count; ++k)
+    for (const Bytes& r : read)
+      if (overlap({to[k], whole_extent(t), "to"}, r)) return fail(BF_EINVAL, "%s: array %u of to overlaps %s", who, k, r.name);
   const bool in_place = same && from[0] == to[0];
   for (uint32_t k = 0; k < count; ++k) {
     if (in_place != (same && from[k] == to[k])) return fail(BF_EINVAL, "%s: only some of the arrays are reordered in place", who);

@@ -1,0 +1,54 @@
+"""Corners of the entry points of a decoding step that need no GPU."""
+import pytest
+
+from paper_2607_22242_gb300 import _build, bf
+from test_answer_host import FAR, SOME, attend, cache, layout, reorder
+
+AWAY = 1 << 40  # aligned, behind everything else
+
+
+@pytest.fixture(scope="module")
+def lib():
+    _build.build()
+    return bf.load()
+
+
+# ---- outputs over what a call reads ----
+
+# Four answers of two prompts, four heads of 64 over two of 10 and 5 tokens; bytes of each argument.
+INPUTS = {"q": 2048, "pk": 5120, "pv": 5120, "sk": 5120, "sv": 5120, "prefix_lengths": 16, "suffix_lengths": 32}
+
+
+@pytest.mark.parametrize("end", ["first", "last"])
+@pytest.mark.parametrize("name", INPUTS)
+@pytest.mark.parametrize("output", ["out", "lse"])
+def test_attention_overlaps(lib, output, name, end):
+    """out (2,048 bytes) or lse (64) in the first or last bytes of what the call reads."""
+    where = {n: AWAY + (i << 20) for i, n in enumerate(INPUTS)}
+    size = {"out": 2048, "lse": 64}[output]
+    at = where[name] + INPUTS[name] - 8 if end == "last" else where[name] - size + 8
+    at = at // 4 * 4
+    kv = lambda n, rows, tokens: cache(rows, tokens, 2, data=where[n])
+    call = dict(q=cache(data=where["q"]), pk=kv("pk", 2, 10), pv=kv("pv", 2, 10), sk=kv("sk", 4, 5), sv=kv("sv", 4, 5),
+                prefix_lengths=where["prefix_lengths"], suffix_lengths=where["suffix_lengths"], lse=2 * AWAY)
+    call[output] = cache(data=at) if output == "out" else at
+    assert attend(lib, **call) == bf.BF_EINVAL
+    assert "overlaps" in bf.last_error()
+
+
+@pytest.mark.parametrize("off", [-60, 0, 2044])
+def test_attention_sums_over_outputs(lib, off):
+    assert attend(lib, lse=FAR + off) == bf.BF_EINVAL
+    assert "overlaps" in bf.last_error()
+
+
+@pytest.mark.parametrize("name", ["parents", "lengths"])
+@pytest.mark.parametrize("off", [-56, 0, 640, 5112])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_reorder_overlaps(lib, in_place, off, name):
+    """A second array (5,120 bytes) over the parents or the lengths (64 bytes)."""
+    to = (FAR, AWAY)
+    call = dict(frm=to if in_place else (SOME, 2 * AWAY), to=to, lengths=1 << 42)
+    call[name] = AWAY + off
+    assert reorder(lib, a=layout(), **call) == bf.BF_EINVAL
+    assert "overlaps " + name in bf.last_error()
