@@ -554,7 +554,8 @@ typedef struct bf_states {
  * `from` and `to` are host arrays of `count` (at most BF_MAX_STATES) device
  * addresses; to[k] == from[k] with the same layout reorders in place (rows that
  * are their own parent cost nothing), otherwise no array overlaps another.  No array of `to`
- * overlaps d_parents or d_lengths, which are not reordered. */
+ * overlaps d_parents or d_lengths, which are not reordered.  On a GPU whose copies no longer
+ * come in, the parts of rows that could not be moved hold bytes of 255 (NaN, or -1). */
 BF_API int bf_beam_reorder(void* const* from, const bf_states* from_layout, void* const* to,
                            const bf_states* to_layout, uint32_t count, const int64_t* d_parents, uint32_t beams,
                            const int64_t* d_lengths, void* cuda_stream);

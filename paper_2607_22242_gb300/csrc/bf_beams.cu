@@ -997,7 +997,20 @@ __global__ void __launch_bounds__(32) reorder_runs_kernel(const __grid_constant_
   for (uint32_t s = lane; s < many; s += 32)
     copy_run(held + s * tl.units * 16, a.from[at.array] + (at.row0 + mv.from[s]) * a.from_row + at.head * a.from_head + at.first * 16,
              mv.have[s] * 16, &full);
-  if (!barrier_wait(&full, 0, &gave_up)) return;
+  bool come = barrier_wait(&full, 0, &gave_up);
+  if (!come) {  // once more: no copy is on its way to this block's memory when it ends, if the GPU does anything still
+    __syncwarp();
+    if (lane == 0) gave_up = 0;
+    __syncwarp();
+    come = barrier_wait(&full, 0, &gave_up);
+  }
+  if (!come) {  // rows of two beams in one would show nowhere; bytes of 255 do: NaN, or -1
+    for (uint32_t b = 0; b < a.beams; ++b)
+      for (uint32_t u = lane; mv.parent[b] >= 0 && u < mv.limit[b]; u += 32)
+        reinterpret_cast<uint4*>(a.to[at.array] + (at.row0 + b) * a.to_row + at.head * a.to_head + at.first * 16)[u] =
+            make_uint4(~0u, ~0u, ~0u, ~0u);
+    return;
+  }
   for (uint32_t b = lane; b < a.beams; b += 32)
     if (mv.parent[b] >= 0)
       put_run(a.to[at.array] + (at.row0 + b) * a.to_row + at.head * a.to_head + at.first * 16,

@@ -1,4 +1,7 @@
 """Corners of the entry points of a decoding step that need no GPU."""
+import os
+import re
+
 import pytest
 
 from paper_2607_22242_gb300 import _build, bf
@@ -52,3 +55,18 @@ def test_reorder_overlaps(lib, in_place, off, name):
     call[name] = AWAY + off
     assert reorder(lib, a=layout(), **call) == bf.BF_EINVAL
     assert "overlaps " + name in bf.last_error()
+
+
+# ---- waits that may run out ----
+
+def test_waits_that_run_out_leave_a_sign():
+    """Rows that stay as they were because a wait ran out would be caches of two beams in one, with no sign of it: no
+    kernel just ends there."""
+    found = 0
+    for name in sorted(os.listdir(_build.CSRC)):
+        if name.endswith((".cu", ".cuh")):
+            with open(os.path.join(_build.CSRC, name), encoding="utf-8") as f:
+                code = _build._code_only(f.read())
+            found += code.count("barrier_wait(")
+            assert not re.search(r"if \(!barrier_wait\([^;]*\)\) return;", code), name
+    assert found > 5
