@@ -128,8 +128,10 @@ __device__ __forceinline__ uint32_t exact_of(uint32_t mine, uint32_t keep, uint3
 // all (key, tie), by counting.  each(f) calls f(key, tie) for all of a thread's
 // candidates.  Candidates of at least `key`, and of a tie below `tie` where they have
 // just that key, are the best; there are `keep` of them or, with fewer in all, all.
+// All ties are from `below` on, and below `upto`.
 template <typename Key, typename Each>
-__device__ __noinline__ void exact_bound(Each each, Key least, uint32_t keep, uint32_t* sums, Key* key, uint64_t* tie) {
+__device__ __noinline__ void exact_bound(Each each, Key least, uint64_t below, uint64_t upto, uint32_t keep, uint32_t* sums, Key* key,
+                                         uint64_t* tie) {
   const auto count = [&](Key k, uint64_t t) {  // candidates above (k, t): better keys, or k and a lower tie
     uint32_t n = 0;
     each([&](Key c, uint64_t at) { n += c > k || (c == k && at < t); });
@@ -144,7 +146,7 @@ __device__ __noinline__ void exact_bound(Each each, Key least, uint32_t keep, ui
     if (count(mid, ~0ull) >= keep) lo = mid;
     else hi = mid;
   }
-  uint64_t below = 0, upto = ~0ull;  // the lowest tie that makes it `keep`
+  // the lowest tie that makes it `keep`
   while (upto - below > 1) {
     const uint64_t mid = below + (upto - below) / 2;
     if (count(lo, mid) >= keep) upto = mid;
@@ -308,6 +310,34 @@ __device__ __forceinline__ void shift_by(uint4 (&u)[V], const uint4& tail, uint3
   }
 }
 
+// Lists what reaches `least` of a row's elements [cut, end).
+template <typename E, bool kAligned, uint32_t T, uint32_t kMost, typename Key>
+__device__ __forceinline__ void list_again(const E* x, uint32_t cut, uint32_t end, float least, Key* list, uint32_t* count) {
+  constexpr uint32_t kW = Vec<E>::kWidth;
+  const auto look = [=](uint32_t i) {
+    const float v = to_f32(x[i]);
+    if (v >= least) {
+      const uint32_t to = atomicAdd(count, 1u);
+      if (to < kMost) list[to] = Ranks<E>::key(v, i - cut);
+    }
+  };
+  const uint32_t whole = kAligned ? (end - cut) / kW * kW : 0;
+  if constexpr (kAligned)
+#pragma unroll 4
+    for (uint32_t j = cut + threadIdx.x * kW; j < cut + whole; j += T * kW)
+      if (value_of(most_of(__ldg(reinterpret_cast<const uint4*>(x + j)), E()), E()) >= least)
+#pragma unroll 1
+        for (uint32_t i = 0; i < kW; ++i) look(j + i);
+#pragma unroll 4
+  for (uint32_t i = cut + whole + threadIdx.x; i < end; i += T) look(i);
+}
+
+// Out of line for rows at any alignment, whose kernel has no registers for it (2 % of a step).
+template <typename E, uint32_t T, uint32_t kMost, typename Key>
+__device__ __noinline__ void list_again_apart(const E* x, uint32_t cut, uint32_t end, float least, Key* list, uint32_t* count) {
+  list_again<E, false, T, kMost>(x, cut, end, least, list, count);
+}
+
 // A chunk of a row, `tiles` times V vectors a thread, cut by the row's elements and not
 // by addresses, so that equal rows have equal sums.  kAligned: rows start at 16 bytes.
 // What reaches a bound that `keep` of the threads' maxima in the first tile reach may be
@@ -410,7 +440,7 @@ __global__ void __launch_bounds__(T, 1024 / T) row_kernel(const __grid_constant_
     if (now > m) s *= m == kMinusInf ? 1.0f : exp2_of((m - now) * a.c2);  // (s is 0, or NaN, before the first number)
     m = now;
     s += fabsf(m) * a.c2 < 1024.0f ? sum_of<E, V, true>(u, m, a.c2) : sum_of<E, V, false>(u, m, a.c2);
-    if (tile == 0) {
+    if (bound <= kOrderMinusInf + 1 && tile0 < last) {  // the first tile, or all so far are banned
       // Warps that have vectors; half of them are enough to count on all.
       const uint32_t each = kAligned ? 32 : turns * 32, some = ((last - tile0 + kW - 1) / kW + each - 1) / each;
       const uint32_t full = 2 * some >= T / 32 ? T / 32 : some;
@@ -449,7 +479,20 @@ __global__ void __launch_bounds__(T, 1024 / T) row_kernel(const __grid_constant_
     }
   }
   __syncthreads();
-  const uint32_t found = hits;
+  uint32_t found = hits;
+  // Where the first tile lies below the rest, the threads' maxima over all tiles give a better bound; the chunk is read again.
+  // (512 rows of 131,072 that ascend, or whose chunks' first tiles are banned, took 7 ms by exact bounds, and 45 us if
+  // alike all along.)
+  if (found > kHits && ch.tiles > 1) {  // (so few kept that bound_of has them)
+    const uint32_t here = bound_of(order_of(m), a.keep, T / 32, warp_bound);
+    if (here > bound) {
+      bound = here;
+      least = from_order(bound);
+      found = 0;
+      if constexpr (kAligned) list_again<E, true, T, kRowList>(x, cut, end, least, list, &count);
+      else list_again_apart<E, T, kRowList>(x, cut, end, least, list, &count);
+    }
+  }
   for (uint32_t i = t; i < min(found, kHits) * kW; i += T) {
     const uint32_t at = i / kW, j = i % kW;
     const float v = to_f32(reinterpret_cast<const E*>(&hit[at])[j]);
@@ -470,7 +513,7 @@ __global__ void __launch_bounds__(T, 1024 / T) row_kernel(const __grid_constant_
     };
     uint32_t key;
     uint64_t tie;
-    exact_bound<uint32_t>(each, bound, a.keep, &sums, &key, &tie);
+    exact_bound<uint32_t>(each, bound, cut, end, a.keep, &sums, &key, &tie);
     __syncthreads();
     if (t == 0) count = 0;
     __syncthreads();
@@ -612,7 +655,7 @@ struct Group {
     uint32_t n = *odd ? 0 : *count;
     if (!kFew && n > most_listed) {
       uint64_t key, tie;
-      exact_bound<uint64_t>(each, (uint64_t)0, a.keep, sums, &key, &tie);
+      exact_bound<uint64_t>(each, (uint64_t)0, 0, ~0ull, a.keep, sums, &key, &tie);
       __syncthreads();
       if (threadIdx.x == 0) *count = 0;
       __syncthreads();

@@ -9,9 +9,10 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 from paper_2607_22242_gb300 import bf  # noqa: E402
-from test_gpu_answer import attention_inputs, half  # noqa: E402
+from test_gpu_answer import attention_inputs, beam_inputs, check_beams, half  # noqa: E402
 
 TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+INF = float("inf")
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -122,3 +123,70 @@ def test_threads_of_different_shapes():
     torch.cuda.synchronize()
     assert refused == [0] * len(sets)
     assert all(torch.equal(out, w) for (_, out), w in zip(calls, want))
+
+
+# ---- rows whose logits are not alike all along ----
+
+def uneven(kind, x):
+    """Logits of (rows x vocab) with ranges of tokens that are banned, or in an order."""
+    vocab = x.shape[1]
+    if kind == "first":
+        x[:, :min(20000, vocab // 3)] = -INF
+    elif kind == "halves":  # of every 4,096, and so of whatever a block takes
+        on = torch.arange(vocab, device="cuda") // max(1, vocab // 8) % 2 == 0
+        x.masked_fill_(on, -INF)
+    elif kind == "few":  # a few tokens are left at the beginning
+        keep = x[:, 5:60:11].clone()
+        x[:, :vocab // 2] = -INF
+        x[:, 5:60:11] = keep
+    elif kind == "ascending":
+        x.copy_(x.sort(1).values)
+    elif kind == "lower":
+        x[:, :vocab // 2] -= 50
+    return x
+
+
+KINDS = ["first", "halves", "few", "ascending", "lower"]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("vocab,keep", [(9001, 16), (70001, 200), (131072, 32)])
+def test_beams_of_uneven_rows(vocab, keep, kind, dtype):
+    """Rows cut into one tile a block, and (310 of 131,072) two, of which the first and the last group are checked."""
+    x, scores, _ = beam_inputs(31, 10, vocab, dtype, seed=vocab)
+    x, s = uneven(kind, x), torch.tensor(scores, device="cuda")
+    for groups in (31, 1):
+        got = bf.beam_step(x[:10 * groups], s[:10 * groups], 10, keep=keep)
+        for g in (0, 30)[:groups]:
+            rows = slice(10 * g, 10 * g + 10)
+            mine = [None if t is None else t[g:g + 1] for t in got]
+            mine[2] = mine[2] - 10 * g
+            check_beams(x[rows], scores[rows], 10, keep, got=bf.BeamStep(*mine))
+
+
+def time_of(call):
+    for _ in range(3):
+        call()
+    best = INF
+    for _ in range(5):
+        a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        a.record()
+        for _ in range(5):
+            call()
+        b.record()
+        b.synchronize()
+        best = min(best, a.elapsed_time(b))
+    return best
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_beams_of_uneven_rows_take_no_longer(kind):
+    """Not many times as long as rows that are alike all along (ascending ones have the largest beside each other,
+    many of them equal in 16 bits, and are read twice)."""
+    x = torch.randn(512, 131072, device="cuda").bfloat16()
+    scores = -torch.rand(512, device="cuda")
+    alike = time_of(lambda: bf.beam_step(x, scores, 8, keep=16))
+    x = uneven(kind, x)
+    took = time_of(lambda: bf.beam_step(x, scores, 8, keep=16))
+    assert took <= 4 * alike
