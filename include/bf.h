@@ -512,7 +512,7 @@ typedef struct bf_beam_args {
   uint32_t beams;           /* per group, 1 to BF_MAX_BEAMS */
   uint32_t keep;            /* continuations kept per group, 1 to BF_MAX_BEAMS */
   int64_t end_token;        /* the token that finishes a beam; -1: none */
-  float length_penalty;     /* >= 0 */
+  float length_penalty;     /* 0 to 65536 */
   float temperature;        /* 1e-18 to 1e18 */
 } bf_beam_args;
 

@@ -565,12 +565,39 @@ __device__ __forceinline__ Two log_of(float v) {
   return quick_two((float)k * 0.693359375f, fmaf((float)k, -2.12194440054690583e-4f, logf(__int_as_float(bits - k * (1 << 23)))));
 }
 
-// What a beam's continuations are made from: total = base + (x - most) / tau, rank = total * weight.
+// What a beam's continuations are made from: total = base + (x - most) / tau, rank = total * weight / 2^down.
 struct Beam {
-  Two base, weight;  // score - ln sum (a finished beam's score); 1 / max(1, length)^penalty
+  Two base, weight;  // score - ln sum (a finished beam's score); 2^down / max(1, length)^penalty
   float most;        // the row's largest logit
-  uint32_t state;
+  uint32_t state;    // and 256 times `down`, which is not 0 where length^penalty is above e^80
 };
+
+// Ranks in 32-bit numbers are right while length^penalty is at most e^80: theirs end in steps of 2^-149, 2^-34 of a total then.
+// No length is above 2^63, so penalties up to 80 / ln 2^63 = 1.83 need nothing else, and their kernels have nothing else
+// (it took 4 % of a step of 4,096 groups of 16 x 100).
+constexpr float kNearWeights = 80.0f, kNearPenalty = 1.8f;
+// n^-penalty as weight / 2^down, weight in [0.7, 1.5); `penalty` is up to 2^16, so down is below 2^22 and the
+// 64-bit exponent off by less than 2^-30.
+__device__ __noinline__ Two far_weight(float penalty, int64_t n, uint32_t* down) {
+  const double y = (double)penalty * log2((double)n), whole = rint(y), w = exp2(whole - y);
+  *down = (uint32_t)whole;
+  const float hi = (float)w;
+  return {hi, (float)(w - (double)hi)};
+}
+// Whole numbers in the order of r / 2^down: sign, exponent (23 bits), r.hi's 23 bits and r.lo in 2^-16 of r.hi's last place; 0 is
+// none of them.
+__device__ __noinline__ uint64_t far_order_of(Two r, int32_t down) {
+  if (r.hi == 0.0f) return 1ull << 63;
+  if (!(fabsf(r.hi) < -kMinusInf)) return r.hi < 0.0f ? 1 : ~0ull;
+  if (fabsf(r.hi) < 0x1p-64f) {
+    r = {r.hi * 0x1p64f, r.lo * 0x1p64f};
+    down += 64;
+  }
+  const uint32_t u = __float_as_uint(fabsf(r.hi));
+  const int32_t e = (int32_t)(u >> 23), rest = (int32_t)rintf(ldexpf(r.hi < 0.0f ? -r.lo : r.lo, 166 - e));
+  const uint64_t size = ((uint64_t)(uint32_t)(e - down + (1 << 22)) << 40) + ((uint64_t)(u & 0x7FFFFFu) << 17) + (uint32_t)(rest + (1 << 15));
+  return r.hi < 0.0f ? (1ull << 63) - 1 - size : (1ull << 63) + 1 + size;
+}
 
 __device__ __forceinline__ Two total_of(const Beam& b, float x, float tau, float inv_tau) {
   const float d = x - b.most, z = d * inv_tau;
@@ -594,7 +621,8 @@ __host__ __device__ __forceinline__ uint64_t group_bytes(uint32_t beams, uint64_
   return (beams * sizeof(Beam) + 15) / 16 * 16 + list_of(slots) * sizeof(Entry<uint64_t>) + more * 4;
 }
 
-// A group's block: beams, list and what both kernels below do with them.
+// A group's block: beams, list and what both kernels below do with them.  kFar: weights may be beyond 32-bit numbers.
+template <bool kFar>
 struct Group {
   const BeamArgs& a;
   Beam* beam;
@@ -602,42 +630,54 @@ struct Group {
   uint32_t most_listed;
   uint64_t row0;
   float inv_tau;
-  uint32_t *count, *odd;
+  uint32_t *count, *odd, *far;  // `far`: some beam's weight is beyond
 
   __device__ __forceinline__ Group(const BeamArgs& args, unsigned char* raw, uint64_t slots, uint32_t* words)
       : a(args), beam(reinterpret_cast<Beam*>(raw)),
         list(reinterpret_cast<Entry<uint64_t>*>(raw + (args.beams * sizeof(Beam) + 15) / 16 * 16)), most_listed(list_of(slots)),
-        row0((uint64_t)blockIdx.x * args.beams), inv_tau(1.0f / args.tau), count(words), odd(words + 1) {
-    if (threadIdx.x == 0) *count = *odd = 0;
+        row0((uint64_t)blockIdx.x * args.beams), inv_tau(1.0f / args.tau), count(words), odd(words + 1), far(words + 2) {
+    if (threadIdx.x == 0) *count = *odd = *far = 0;
   }
   __device__ __forceinline__ uint32_t state_of(uint32_t b) const {
     const float score = __ldg(a.scores + row0 + b);
     return score == kMinusInf ? kDead : a.finished && __ldg(a.finished + row0 + b) ? kFinished : kAlive;
   }
+  __device__ __forceinline__ static uint32_t kind(const Beam& o) { return kFar ? o.state & 255 : o.state; }
   // From the maximum and sum of a row's exponentials.
   __device__ __forceinline__ void put(uint32_t b, uint32_t state, float m, float s) {
     const float score = __ldg(a.scores + row0 + b);
     Beam o;
-    o.state = state == kAlive && m == kMinusInf && s == s ? (uint32_t)kDead : state;
-    o.most = o.state == kAlive ? m : 0.0f;
+    if (state == kAlive && m == kMinusInf && s == s) state = kDead;
+    o.state = state;
+    o.most = state == kAlive ? m : 0.0f;
     o.base = {score, 0.0f};
-    if (o.state == kAlive) {
+    if (state == kAlive) {
       const Two l = log_of(s), d = two_sum(score, -l.hi);
       o.base = quick_two(d.hi, d.lo - l.lo);
     }
     o.weight = {1.0f, 0.0f};
     if (a.penalty != 0.0f) {  // n^-penalty = e^(-penalty ln n), ln n and the product in two parts
-      const int64_t n = __ldg(a.lengths + row0 + b) + (o.state != kFinished);
-      const Two l = log_of((float)(n < 1 ? 1 : n));
-      const float p = a.penalty * l.hi, w = expf(-p);
-      o.weight = quick_two(w, -w * fmaf(a.penalty, l.lo, fmaf(a.penalty, l.hi, -p)));
+      int64_t n = __ldg(a.lengths + row0 + b) + (state != kFinished);
+      if (n < 1) n = 1;
+      const Two l = log_of((float)n);
+      const float p = a.penalty * l.hi;
+      if (!kFar || p <= kNearWeights) {
+        const float w = expf(-p);
+        o.weight = quick_two(w, -w * fmaf(a.penalty, l.lo, fmaf(a.penalty, l.hi, -p)));
+      } else {
+        uint32_t down;
+        o.weight = far_weight(a.penalty, n, &down);
+        o.state |= down << 8;
+        *far = 1;
+      }
     }
     beam[b] = o;
     if (score != score || score == -kMinusInf || s != s) *odd = 1;
   }
   __device__ __forceinline__ uint64_t key_of(uint32_t b, float x) const {
     const Beam& o = beam[b];
-    const Two total = o.state == kFinished ? o.base : total_of(o, x, a.tau, inv_tau);
+    const Two total = kind(o) == kFinished ? o.base : total_of(o, x, a.tau, inv_tau);
+    if (kFar && *far) return far_order_of(times(total, o.weight), (int32_t)(o.state >> 8));
     return order_of(a.penalty != 0.0f ? times(total, o.weight) : total);
   }
   // Equal in both parts: the lower beam, in it the larger logit, then the lower token (8, 32 and 24 bits).
@@ -670,7 +710,7 @@ struct Group {
     best_of<kFew, Entry<uint64_t>>(list, n, a.keep, Entry<uint64_t>{0, ~0ull}, above, [&](uint32_t rank, const Entry<uint64_t>& e) {
       const uint32_t b = (uint32_t)(e.tie >> 56);
       const Beam& o = beam[b];
-      const bool was = o.state == kFinished;
+      const bool was = kind(o) == kFinished;
       const int64_t token = was ? a.end_token : (int64_t)(e.tie & 0xFFFFFFu);
       a.out_scores[out + rank] = was ? o.base.hi : total_of(o, from_order(~(uint32_t)(e.tie >> 24)), a.tau, inv_tau).hi;
       a.out_tokens[out + rank] = token;
@@ -693,13 +733,13 @@ constexpr uint32_t kFewSlots = 128;
 // Few logits in a group: all of it in shared memory.  4,096 groups of 16 x 3 are 12.6 us, of 16 x 17 42: latency and
 // the ranking of all by all.  kFew: so few that all of them are ranked (code that is not there
 // is not fetched, which is most of the time of thousands of such groups).
-template <typename E, bool kFew>
+template <typename E, bool kFew, bool kFar>
 __global__ void __launch_bounds__(kThreads) direct_kernel(const __grid_constant__ BeamArgs a) {
   extern __shared__ __align__(16) unsigned char raw[];
-  __shared__ uint32_t words[2], sums, bound_word;
+  __shared__ uint32_t words[3], sums, bound_word;
   __shared__ __align__(16) uint32_t all[kThreads];
   const uint32_t t = threadIdx.x, slots = a.beams * a.vocab, warp = t / 32, lane = t % 32;
-  Group g(a, raw, slots, words);
+  Group<kFar> g(a, raw, slots, words);
   float* logits = reinterpret_cast<float*>(g.list + g.most_listed);
   // Lanes to a row of logits: as many as a short row has.
   const uint32_t row_lanes = a.vocab >= 32 ? 32 : 1u << (31 - __clz(a.vocab)), rows = blockDim.x / row_lanes;
@@ -732,7 +772,7 @@ __global__ void __launch_bounds__(kThreads) direct_kernel(const __grid_constant_
   // All candidates of a thread: f(beam, token, x), x the logit (0 for a finished beam).
   const auto each = [=](auto f) {
     for (uint32_t b = my_row; b < a.beams; b += rows) {
-      const uint32_t state = g.beam[b].state;
+      const uint32_t state = g.kind(g.beam[b]);
       if (state == kAlive) {
         for (uint32_t j = my_lane; j < a.vocab; j += row_lanes) {
           const float x = logits[b * a.vocab + j];
@@ -766,12 +806,13 @@ constexpr uint32_t kLists = 4096;  // of a group that are noted as gone through
 // (64 groups of 8 beams, 16 kept).  A bound that `keep` continuations reach comes
 // from one of each list, the depth-th; only lists whose first reaches it are gone through,
 // eight lanes to a list, up to their first that does not.
+template <bool kFar>
 __global__ void __launch_bounds__(kThreads) group_kernel(const __grid_constant__ BeamArgs a, const __grid_constant__ Chunks ch) {
   extern __shared__ __align__(16) unsigned char raw[];
-  __shared__ uint32_t words[2], sums, going, bound_word;
+  __shared__ uint32_t words[3], sums, going, bound_word;
   __shared__ __align__(16) uint32_t tops[kThreads];
   const uint32_t t = threadIdx.x, chunks = a.beams * ch.per_row;
-  Group g(a, raw, (uint64_t)chunks * a.keep, words);
+  Group<kFar> g(a, raw, (uint64_t)chunks * a.keep, words);
   uint32_t* lists = reinterpret_cast<uint32_t*>(g.list + g.most_listed);  // those that are gone through
   if (t == 0) going = 0;
   // The beams' sums: as many lanes to a beam as its row has chunks, up to 32.
@@ -807,7 +848,7 @@ __global__ void __launch_bounds__(kThreads) group_kernel(const __grid_constant__
   const uint2* best = reinterpret_cast<const uint2*>(ch.best) + g.row0 * ch.per_row * a.keep;
   // A list's i-th continuation, as key and tie; 0: none.
   const auto key_at = [=](uint32_t b, uint32_t list, uint32_t i, uint64_t* tie) -> uint64_t {
-    const uint32_t state = g.beam[b].state;
+    const uint32_t state = g.kind(g.beam[b]);
     uint2 c = make_uint2(0, 0);
     if (state == kAlive) {
       c = __ldca(best + (uint64_t)list * a.keep + i);
@@ -906,7 +947,7 @@ cudaError_t launch_step(const BeamArgs& a, void* workspace, cudaStream_t st) {
   uint64_t bytes = 0;
   const bool aligned = ((uintptr_t)a.x | (a.ldx * sizeof(E))) % 16 == 0;
   const Chunks c = chunks_of(a.groups, a.beams, a.vocab, a.keep, Vec<E>::kWidth, workspace, &vectors, &bytes);
-  const bool direct = c.per_row == 0;
+  const bool direct = c.per_row == 0, far = a.penalty > kNearPenalty;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute after;
   cfg.gridDim = dim3(a.groups);
@@ -919,7 +960,8 @@ cudaError_t launch_step(const BeamArgs& a, void* workspace, cudaStream_t st) {
     if (threads < a.keep && n > kFewSlots) threads = (a.keep + 31) / 32 * 32;
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = group_bytes(a.beams, n, n);
-    return n <= kFewSlots ? cudaLaunchKernelEx(&cfg, direct_kernel<E, true>, a) : cudaLaunchKernelEx(&cfg, direct_kernel<E, false>, a);
+    if (far) return cudaLaunchKernelEx(&cfg, n <= kFewSlots ? direct_kernel<E, true, true> : direct_kernel<E, false, true>, a);
+    return cudaLaunchKernelEx(&cfg, n <= kFewSlots ? direct_kernel<E, true, false> : direct_kernel<E, false, false>, a);
   }
   const uint64_t blocks = (uint64_t)a.groups * a.beams * c.per_row;
   const auto rows = [&](auto kernel) { return launch_plain(kernel, blocks, c.threads, st, a, c); };
@@ -934,7 +976,7 @@ cudaError_t launch_step(const BeamArgs& a, void* workspace, cudaStream_t st) {
   after.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   after.val.programmaticStreamSerializationAllowed = 1;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, group_kernel, a, c);
+  return cudaLaunchKernelEx(&cfg, far ? group_kernel<true> : group_kernel<false>, a, c);
 }
 
 // ---- states -----------------------------------------------------------------

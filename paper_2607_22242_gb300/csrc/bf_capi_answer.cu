@@ -240,7 +240,7 @@ int bf_beam_step(const bf_matrix* logits, const bf_beam_args* args, float* d_sco
   BF_TRY(check_array(args->lengths, 0, 8, "lengths", who));
   if (args->end_token < -1) return fail(BF_EINVAL, "%s: end_token is below -1", who);
   if (args->finished && args->end_token < 0) return fail(BF_EINVAL, "%s: finished beams need an end_token", who);
-  BF_TRY(check_number(args->length_penalty, args->length_penalty >= 0.0f, "length_penalty", who));
+  BF_TRY(check_number(args->length_penalty, args->length_penalty >= 0.0f && args->length_penalty <= 65536.0f, "length_penalty", who));
   if (args->length_penalty > 0.0f && !args->lengths && logits->rows)
     return fail(BF_EINVAL, "%s: a length penalty needs lengths", who);
   BF_TRY(check_temperature(args->temperature, who));

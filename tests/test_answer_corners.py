@@ -5,7 +5,7 @@ import re
 import pytest
 
 from paper_2607_22242_gb300 import _build, bf
-from test_answer_host import FAR, SOME, attend, cache, layout, reorder
+from test_answer_host import FAR, SOME, attend, beams, cache, layout, reorder, step
 
 AWAY = 1 << 40  # aligned, behind everything else
 
@@ -70,3 +70,11 @@ def test_waits_that_run_out_leave_a_sign():
             found += code.count("barrier_wait(")
             assert not re.search(r"if \(!barrier_wait\([^;]*\)\) return;", code), name
     assert found > 5
+
+
+# ---- length penalties ----
+
+@pytest.mark.parametrize("penalty", [65537.0, 1e30, float("inf")])
+def test_beams_refuse_larger_penalties(lib, penalty):
+    assert step(lib, args=beams(length_penalty=penalty, lengths=FAR)) == bf.BF_EINVAL
+    assert "length_penalty" in bf.last_error()

@@ -3,6 +3,7 @@ import ctypes
 import math
 import threading
 
+import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -190,3 +191,56 @@ def test_beams_of_uneven_rows_take_no_longer(kind):
     x = uneven(kind, x)
     took = time_of(lambda: bf.beam_step(x, scores, 8, keep=16))
     assert took <= 4 * alike
+
+
+# ---- length penalties ----
+
+@pytest.mark.parametrize("penalty", [1.0, 1.8, 2.5, 13.0, 30.0, 200.0, 5000.0, 65536.0])
+@pytest.mark.parametrize("vocab,beams,keep", [(3, 4, 6), (3, 16, 16), (100, 16, 40), (9001, 6, 12)])
+def test_beams_of_large_penalties(vocab, beams, keep, penalty):
+    """total / n^penalty where n^penalty is beyond 32-bit numbers, for totals of both signs."""
+    groups = 8
+    x, _, rng = beam_inputs(groups, beams, vocab, "f32", seed=vocab + beams)
+    scores = np.float32(rng.uniform(-12, 12, groups * beams))
+    lengths = rng.choice([0, 1, 2, 3, 40, 41, 999, 10 ** 6, 10 ** 12], (groups, beams))
+    lengths[1] = 39  # all alike
+    lengths[2] = 39 + np.arange(beams) % 2
+    lengths = lengths.reshape(-1)
+    finished = rng.random(groups * beams) < 0.3
+    got = bf.beam_step(x, torch.tensor(scores, device="cuda"), beams, keep=keep, finished=torch.tensor(finished, device="cuda"),
+                       lengths=torch.tensor(lengths, device="cuda"), length_penalty=penalty, end_token=1)
+    z = torch.log_softmax(x.double(), 1).cpu().numpy()
+    off = 2.0 ** -22 + (64 + 13 + vocab / 4096) * 2.0 ** -24 + max(1.0, np.log2(vocab)) * 2.0 ** -23  # of a total, as check_beams
+    for g in range(groups):
+        found = []  # (sign, what orders the ranks of that sign, beam, token, total, length)
+        for b in range(g * beams, (g + 1) * beams):
+            n = int(lengths[b]) + (not finished[b])
+            for v, t in [(1, float(scores[b]))] if finished[b] else list(enumerate(scores[b] + z[b])):
+                sign = 1 if t > 0 else -1
+                found.append((sign, sign * (math.log(abs(t)) - penalty * math.log(max(1, n))), b, int(v), t, n))
+        found.sort(key=lambda c: (-c[0], -c[1], c[2], c[3]))
+        place = {c[2:4]: c for c in found}
+        seen = set()
+        for j in range(min(keep, len(found))):
+            here = (int(got.parents[g, j]), int(got.tokens[g, j]))
+            assert here in place and here not in seen
+            seen.add(here)
+            c, best = place[here], found[j]
+            near = 4 * off / min(abs(c[4]), abs(best[4])) + 1e-8 * (1 + penalty * 2.0 ** -10)
+            assert (c[0] == best[0] and abs(c[1] - best[1]) <= near) or abs(c[4]) < 4 * off or abs(best[4]) < 4 * off, (g, j, c, best)
+            assert abs(float(got.scores[g, j]) - c[4]) <= off + 2.0 ** -24 * abs(c[4])
+            assert int(got.lengths[g, j]) == c[5]
+
+
+def test_beams_of_a_penalty_over_equal_totals():
+    """Beams that differ by their lengths alone: the longer is better where totals are negative, whatever the penalty."""
+    for vocab in (1, 4099):
+        x = torch.zeros(8, vocab, device="cuda")
+        for penalty in (0.5, 20.0, 28.0, 40.0, 1000.0, 65536.0):
+            lengths = torch.tensor([9, 40, 3, 41, 7, 1 << 40, 0, 100], device="cuda")
+            got = bf.beam_step(x[:, :1] if vocab == 1 else x, torch.full((8,), -2.0, device="cuda"), 8, keep=8, lengths=lengths,
+                               length_penalty=penalty)
+            if vocab == 1:
+                assert got.parents[0].tolist() == [5, 7, 3, 1, 0, 4, 2, 6]
+            else:
+                assert got.parents[0].tolist() == [5] * 8 and got.tokens[0].tolist() == list(range(8))
