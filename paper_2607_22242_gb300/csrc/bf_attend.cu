@@ -38,6 +38,7 @@ struct Piece {
   int64_t k_token, v_token;
   uint32_t k0, k1;
   float* record;
+  uint32_t held;  // its rows
 };
 
 // Four elements of a row from d on, zeros behind its end; `whole`: addresses allow one read.
@@ -190,11 +191,11 @@ __device__ void piece(const Piece& p, uint32_t rows, uint32_t dim, float* sm) {
     for (uint32_t c = 0; c < S::kOuts; ++c) {
       const uint32_t d = cg + c * S::kCols;
       if (d >= dim) break;
-      p.record[record_place(R, row, d)] = o[i][c];
+      p.record[record_place(p.held, row, d)] = o[i][c];
     }
   }
   if (t < rows) {
-    float2* ml = reinterpret_cast<float2*>(p.record + record_sums(R, dim));
+    float2* ml = reinterpret_cast<float2*>(p.record + record_sums(p.held, dim));
     ml[t] = make_float2(ms[t], ls[t]);
   }
   __syncthreads();
@@ -243,7 +244,7 @@ __global__ void __launch_bounds__(kThreads, 2) general_kernel(const __grid_const
       const Piece p = {static_cast<const E*>(a.pk.data) + at.prompt * a.pk.batch + head * a.pk.head,
                        static_cast<const E*>(a.pv.data) + at.prompt * a.pv.batch + head * a.pv.head,
                        a.pk.token, a.pv.token, at.tile * kKeys, min(len, (at.tile + n) * kKeys),
-                       plan.prefix + (uint64_t)(blockIdx.x + (uint64_t)at.prompt * inners + at.inner) * plan.record};
+                       plan.prefix + (uint64_t)(blockIdx.x + (uint64_t)at.prompt * inners + at.inner) * plan.record, plan.held};
       piece<E, R>(p, rows, a.dim, sm);
       left -= n;
       at.tile = 0;
@@ -266,7 +267,8 @@ __global__ void __launch_bounds__(kThreads, 2) general_kernel(const __grid_const
     const Piece p = {static_cast<const E*>(a.sk.data) + answer * a.sk.batch + head * a.sk.head,
                      static_cast<const E*>(a.sv.data) + answer * a.sv.batch + head * a.sv.head, a.sk.token, a.sv.token,
                      (uint32_t)((uint64_t)len * split / plan.suffix_splits),
-                     (uint32_t)((uint64_t)len * (split + 1) / plan.suffix_splits), plan.suffix + slot * plan.suffix_record};
+                     (uint32_t)((uint64_t)len * (split + 1) / plan.suffix_splits), plan.suffix + slot * plan.suffix_record,
+                     plan.suffix_held};
     piece<E, R>(p, rows, a.dim, sm);
   }
 }
@@ -300,7 +302,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
     const uint32_t i = from + lane, some = min(32u, pieces - from);
     float2 ml = make_float2(kNone, 0.0f);
     if (i < pieces) {
-      const uint32_t rows = i < far ? plan.rows : plan.suffix_rows;
+      const uint32_t rows = i < far ? plan.held : plan.suffix_held;
       ml = __ldcg(reinterpret_cast<const float2*>(record(i) + record_sums(rows, a.dim)) + (i < far ? r0 : r1));
       if (plan.gave_up && i < far) odd |= __ldcg(plan.gave_up + own.first + i) != 0;
     }
@@ -322,7 +324,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
 #pragma unroll
       for (uint32_t j = 0; j < kAhead; ++j) {
         const uint32_t p = from + k + j;
-        x[j] = k + j < some && d < a.dim ? __ldcg(record(p) + (p < far ? record_place(plan.rows, r0, d) : record_place(plan.suffix_rows, r1, d))) : 0.0f;
+        x[j] = k + j < some && d < a.dim ? __ldcg(record(p) + (p < far ? record_place(plan.held, r0, d) : record_place(plan.suffix_held, r1, d))) : 0.0f;
       }
 #pragma unroll
       for (uint32_t j = 0; j < kAhead; ++j) {
@@ -357,8 +359,12 @@ AttendPlan plan_of(const AttendArgs& a, bool tile, void* workspace, uint64_t* by
   const uint64_t most = (a.suffix_cap + kKeys - 1) / kKeys;  // a tile each: the first of a block takes 12 us, one more 4
   splits = splits < most ? splits : most;
   p.suffix_splits = splits < 1 ? 1 : (uint32_t)splits;
-  p.record = record_floats(p.rows, a.dim);
-  p.suffix_record = record_floats(p.suffix_rows, a.dim);
+  // Records of the rows there are: with all that a tile has room for, 32,768 answers of 4 query heads a key head took 9.3 GB.
+  const auto even = [](uint64_t n) { return (uint32_t)(n + 1) / 2 * 2; };
+  p.held = even(rows < p.rows ? rows : p.rows);
+  p.suffix_held = even(a.share < p.suffix_rows ? a.share : p.suffix_rows);
+  p.record = record_floats(p.held, a.dim);
+  p.suffix_record = record_floats(p.suffix_held, a.dim);
   char* at = static_cast<char*>(workspace);
   const auto take = [&](uint64_t n) {
     char* q = at;

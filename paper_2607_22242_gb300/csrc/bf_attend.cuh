@@ -24,7 +24,8 @@ namespace bfk {
 
 // How a call is cut; chosen on the host from the sizes alone.
 struct AttendPlan {
-  uint32_t rows, row_tiles;      // query vectors of a prefix segment, segments of a prompt and key head
+  uint32_t rows, row_tiles;      // query vectors of a prefix segment at most, segments of a prompt and key head
+  uint32_t held, suffix_held;    // rows of a record: as many as a segment has, to a multiple of 2
   uint32_t keys;                 // of a tile
   uint32_t parts;                // blocks that share the prefix tiles out
   uint32_t suffix_rows, suffix_row_tiles, suffix_splits;  // the answers' own keys: pieces of an answer and key head
@@ -33,7 +34,7 @@ struct AttendPlan {
   uint32_t record, suffix_record;  // floats of a record
 };
 
-// A record: the outputs of its rows, four dimensions of all rows after four others (so
+// A record, of an even number of rows (16 bytes are read at a time): the outputs of its rows, four dimensions of all rows after four others (so
 // that a thread to a row writes, and neighbouring rows are read, whole lines), then (m, l) of each row.
 __host__ __device__ __forceinline__ uint32_t record_place(uint32_t rows, uint32_t row, uint32_t d) { return (d / 4 * rows + row) * 4 + d % 4; }
 __host__ __device__ __forceinline__ uint32_t record_sums(uint32_t rows, uint32_t dim) { return (dim + 3) / 4 * 4 * rows; }

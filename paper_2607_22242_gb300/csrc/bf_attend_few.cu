@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(kWarps * 32) few_kernel(const __grid_constant_
   // What the prompts' kernel wrote is there from here on (it takes whole SMs: blocks of this one hardly start before it ends).
   wait_for_previous();
   const auto record_of = [&](const Owners& own, uint32_t i) { return plan.prefix + (own.first + i + own.segment) * plan.record; };
-  const uint32_t quads = a.dim / 4, sums_at = record_sums(plan.rows, a.dim), r0 = row0 - tile0 * plan.rows;
+  const uint32_t quads = a.dim / 4, sums_at = record_sums(plan.held, a.dim), r0 = row0 - tile0 * plan.rows;
   uint32_t gave = 0;
   if (!kAlone) {
     const uint32_t from = own0.first, to = max(own0.last, own1.last);
@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(kWarps * 32) few_kernel(const __grid_constant_
         float2 x[DP / 8];
 #pragma unroll
         for (uint32_t n = 0; n < DP / 8; ++n)
-          if (8 * n < a.dim) x[n] = __ldca(reinterpret_cast<const float2*>(record + record_place(plan.rows, pr, 8 * n + 2 * c)));
+          if (8 * n < a.dim) x[n] = __ldca(reinterpret_cast<const float2*>(record + record_place(plan.held, pr, 8 * n + 2 * c)));
         if (!(ml.y > 0.0f)) continue;  // nothing to attend to in that piece
         const float w = exp2_of(ml.x - base);
         total = fmaf(w, ml.y, total);
@@ -317,7 +317,7 @@ __global__ void __launch_bounds__(kWarps * 32) few_kernel(const __grid_constant_
     for (uint32_t n0 = (rank * kWarps + warp) * width; n0 < items; n0 += few.blocks * kWarps * width) {
       const uint32_t n = n0 + lane % width, row = n < items ? n % rows : 0, d = n < items ? n / rows * 4 : 0;
       const Owners& own = row < rows0 ? own0 : own1;
-      f(n < items, row, d, record_of(own, 0) + record_place(plan.rows, row < rows0 ? r0 + row : row - rows0, d), own.last - own.first);
+      f(n < items, row, d, record_of(own, 0) + record_place(plan.held, row < rows0 ? r0 + row : row - rows0, d), own.last - own.first);
     }
   };
   // The prompt's records of these rows, all on their way at once while the weights are found: (m, l), and what each

@@ -449,7 +449,7 @@ __device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const T
     // each puts half of the columns there, weighted, and then adds its part to the other half.
     const bool both = !t.pair && p.tiles > 1;
     float* record = plan.prefix + (uint64_t)(blockIdx.x + (uint64_t)p.at.prompt * p.inners + p.at.inner) * plan.record;
-    float2* sums = reinterpret_cast<float2*>(record + record_sums(plan.rows, a.dim));
+    float2* sums = reinterpret_cast<float2*>(record + record_sums(plan.held, a.dim));
     float2 ml = make_float2(m == kNone ? kNone : fmaf(m, scale, -kLift<E>), l);
     float w = 1.0f;
     if (both) {
@@ -468,7 +468,7 @@ __device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const T
     tensor_fence_after();
     const uint32_t half = both ? (a.dim / 2 + 7) / 8 * 8 : a.dim;
     if (warp_on && (t.pair || steps)) {
-      put_outputs<false>(record, plan.rows, my_row, on, s && both ? half : 0, s && both ? a.dim : half, o_at, w);
+      put_outputs<false>(record, plan.held, my_row, on, s && both ? half : 0, s && both ? a.dim : half, o_at, w);
       if (on && (t.pair || s == 0)) sums[my_row] = ml;
     }
     tensor_fence_before();
@@ -476,7 +476,7 @@ __device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const T
     tensor_fence_after();
     p.next();
     if (p.more()) request_q<E>(a, plan, p, t, q_to);  // neither stream has a product left that reads the queries
-    if (both && warp_on) put_outputs<true>(record, plan.rows, my_row, on, s ? 0 : half, s ? half : a.dim, o_at, w);
+    if (both && warp_on) put_outputs<true>(record, plan.held, my_row, on, s ? 0 : half, s ? half : a.dim, o_at, w);
     tensor_fence_before();
   }
   copies_wait_all();

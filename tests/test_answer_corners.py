@@ -1,11 +1,12 @@
 """Corners of the entry points of a decoding step that need no GPU."""
+import ctypes
 import os
 import re
 
 import pytest
 
 from paper_2607_22242_gb300 import _build, bf
-from test_answer_host import FAR, SOME, attend, beams, cache, layout, reorder, step
+from test_answer_host import FAR, SOME, attend, beams, cache, layout, reorder, step, workspace
 
 AWAY = 1 << 40  # aligned, behind everything else
 
@@ -78,3 +79,24 @@ def test_waits_that_run_out_leave_a_sign():
 def test_beams_refuse_larger_penalties(lib, penalty):
     assert step(lib, args=beams(length_penalty=penalty, lengths=FAR)) == bf.BF_EINVAL
     assert "length_penalty" in bf.last_error()
+
+
+# ---- workspaces ----
+
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+@pytest.mark.parametrize("prompts,each,heads,kv_heads,dim", [(256, 16, 32, 8, 128), (4096, 1, 32, 8, 128), (2048, 16, 32, 8, 128),
+                                                             (64, 16, 16, 4, 64), (3000, 3, 8, 8, 200), (500, 40, 24, 1, 96)])
+def test_attention_workspace_is_of_what_there_is(lib, prompts, each, heads, kv_heads, dim, dtype):
+    """A prompt's and an answer's own part of each query vector's output, (dim + 2) numbers of 32 bits, with rows to a
+    multiple of 2, and a part more for each of 304 blocks."""
+    n = ctypes.c_uint64(0)
+    q, pk, sk = cache(prompts * each, 1, heads, dim, dtype), cache(prompts, 512, kv_heads, dim, dtype), cache(prompts * each, 128, kv_heads, dim, dtype)
+    assert workspace(lib, q, pk, sk, ctypes.byref(n)) == bf.BF_OK
+    even = lambda k: k + k % 2
+    share, wide = heads // kv_heads, (dim + 3) // 4 * 4 + 2
+    tiles = -(-each * share // 64)  # of 64 rows, or of up to 256
+    own = prompts * each * kv_heads * -(-share // 16) * even(min(share, 64))
+    most = 4 * wide * (own + (304 + prompts * kv_heads * tiles) * even(min(each * share, 256)))
+    assert n.value <= most + (1 << 20)
+    if each * share <= 64:  # else the last of the tiles may be part empty
+        assert n.value <= 2.2 * 4 * wide * prompts * each * heads + 4 * wide * 304 * 64 + (1 << 20) or share % 2
