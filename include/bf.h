@@ -492,7 +492,8 @@ typedef struct bf_attention_args {
  * suffix_v may both be NULL (the prompt alone); d_lse (answers x heads) may be
  * NULL.  What lies behind a length is not used, whatever it holds.  With nothing
  * to attend to (lengths 0, or every score -inf) out is 0 and lse -inf; a length
- * outside 0..tokens makes its answers' out and lse NaN.  For 16-bit types the
+ * outside 0..tokens makes its answers' out and lse NaN, and so does a score that is NaN or above
+ * 32-bit numbers.  For 16-bit types the
  * weights e^(s_t - max) are rounded to the type before the second product.
  * Neither out nor lse overlaps an input (the lengths among them) or the other. */
 BF_API int bf_prefix_attention(const bf_cache* q, const bf_cache* prefix_k, const bf_cache* prefix_v,

@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
       }
     }
   }
-  odd = __any_sync(~0u, odd);
+  odd = __any_sync(~0u, odd || m == -kNone);  // (a score above 32-bit numbers)
   const float nan = __int_as_float(0x7FC00000), inv = odd ? nan : l > 0.0f ? 1.0f / l : 0.0f;
   E* out = static_cast<E*>(const_cast<void*>(a.out.data)) + (int64_t)answer * a.out.batch + (int64_t)h * a.out.head;
   if (d < a.dim) out[d] = from_f32<E>(o * inv);

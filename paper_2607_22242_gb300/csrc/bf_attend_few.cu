@@ -253,6 +253,7 @@ __global__ void __launch_bounds__(kWarps * 32) few_kernel(const __grid_constant_
         odd |= ml.y != ml.y || __ldca(plan.gave_up + own.first + i) != 0;
         most = fmaxf(most, ml.x);
       }
+      odd |= most == -kNone;  // a score above 32-bit numbers
       const float base = most == kNone ? 0.0f : most, mine = l[r] > 0.0f ? exp2_of(m[r] - base) : 0.0f;
       float total = l[r] > 0.0f ? mine * l[r] : 0.0f;
 #pragma unroll
@@ -372,6 +373,7 @@ __global__ void __launch_bounds__(kWarps * 32) few_kernel(const __grid_constant_
     }
 #pragma unroll
     for (int d = 16; d; d /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
+    odd |= most == -kNone;  // a score above 32-bit numbers
     const float base = most == kNone ? 0.0f : most;
     float total = 0.0f;
     for (uint32_t i = lane; i < near + far; i += 32) {

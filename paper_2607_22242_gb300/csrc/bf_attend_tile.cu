@@ -421,7 +421,11 @@ __device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const T
           tensor_wait_store();
         }
         base = m == kNone ? 0.0f : m;
-        const float lifted = fmaf(-base, scale, kLift<E>);
+        // Scores so large that what the product with the scale is rounded by would show in the weights, all of them or none
+        // (beyond 2^25 it is a factor of 2): the maximum is taken off first.
+        float lifted = fmaf(-base, scale, kLift<E>);
+        const bool large = __any_sync(~0u, fabsf(lifted) > 0x1p20f);
+        if (large) lifted = kLift<E>;
         const float2 scale_2 = make_float2(scale, scale), less = make_float2(lifted, lifted);
         float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll 1
@@ -429,6 +433,10 @@ __device__ void weigh_tiles(const AttendArgs& a, const AttendPlan& plan, const T
           float x[64];
           uint32_t w[32];
           load_scores(s_at, c, valid, x);
+          if (large) {
+#pragma unroll
+            for (uint32_t k = 0; k < 64; ++k) x[k] -= base;
+          }
 #pragma unroll
           for (uint32_t k = 0; k < 32; ++k) {
             const float2 e = __ffma2_rn(make_float2(x[2 * k], x[2 * k + 1]), scale_2, less);

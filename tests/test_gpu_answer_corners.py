@@ -65,6 +65,45 @@ def test_answers_of_one_above_many(dtype, answers):
     """The answers' own keys, by a warp each, by two and by four."""
     check_one_above_many(dtype, 131072, 1, answers, True)
 
+# ---- scores of any size ----
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("scale", [1e6, -1e6, 1e8, 1e12, 1e20, 1e30, -1e30])
+@pytest.mark.parametrize("dim,each", [(64, 3), (128, 40), (128, 100), (64, 70), (40, 9)])
+def test_attention_of_large_scores(dim, each, scale, dtype):
+    """Scores far beyond what exponentials tell apart: the key of the largest has all the weight, wherever it lies."""
+    x = attention_inputs(2, each, 4, 2, dim, 700, 50, dtype, seed=each, spread=1.0)
+    q, pk, pv, sk, sv = (t.double() for t in x)
+    k, v = (torch.cat([p.repeat_interleave(each, 0), s], 1) for p, s in ((pk, sk), (pv, sv)))
+    s = torch.einsum("agsd,atgd->agst", q.view(-1, 2, 2, dim), k) * float(np.float32(scale))
+    top, at = s.topk(2, -1)
+    size = torch.einsum("agsd,atgd->agst", q.view(-1, 2, 2, dim).abs(), k.abs()).max().item() * abs(scale)
+    # A score is off by (dim + 4) 2^-24 of the sum of its products' magnitudes, scaled and rounded; two that are closer than
+    # twice that and what a weight of 2^-40 takes are not looked at.
+    off = (dim + 6) * 2.0 ** -24 * size
+    sure = top[..., 0] - top[..., 1] > 2 * off + 28
+    assert sure.double().mean() > 0.9
+    want = torch.gather(v.transpose(1, 2), 2, at[..., :1].expand(-1, -1, -1, dim))
+    out, lse = bf.prefix_attention(*x, scale=scale, lse=True)
+    got = out.double().view(want.shape)
+    near = (got - want).abs() <= half(dtype) * want.abs() + 700 * 2.0 ** -40 * 8 + (2.0 ** -25 if dtype == "f16" else 0) + 2.0 ** -22 * want.abs()
+    assert near[sure].all()
+    assert ((lse.double().view(top[..., 0].shape) - top[..., 0]).abs() <= 2 * off + 8).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("own", [False, True])
+def test_attention_of_scores_beyond_32_bits(own, dtype):
+    """A score of +inf makes its answer NaN, one of -inf has no weight."""
+    x = attention_inputs(1, 3, 4, 2, 64, 300, 50, dtype, seed=1)
+    q, pk, pv, sk, sv = (t.clone() for t in x)
+    q.fill_(3e4)
+    pk.fill_(-3e4 if own else 3e4)
+    sk.fill_(3e4 if own else -3e4)
+    out, lse = bf.prefix_attention(q, pk, pv, sk, sv, scale=1e30, lse=True)
+    assert torch.isnan(out).all() and torch.isnan(lse).all()
+
+
 # ---- calls from threads of their own ----
 
 def plain_call(x):
