@@ -825,6 +825,7 @@ __global__ void __launch_bounds__(kThreads) group_kernel(const __grid_constant__
     prefetch(a.scores + g.row0 + b);
     if (a.finished) prefetch(a.finished + g.row0 + b);
   }
+  __syncthreads();  // the group's words are 0 before any beam is found odd
   wait_for_previous();
   for (uint32_t b0 = 0; b0 < a.beams; b0 += kThreads / lanes) {
     const uint32_t b = b0 + t / lanes;
