@@ -355,7 +355,7 @@ __global__ void __launch_bounds__(T, 1024 / T) row_kernel(const __grid_constant_
   __shared__ __align__(16) Key list[kRowList];
   __shared__ uint4 hit[kHits];
   __shared__ uint32_t hit_token[kHits];
-  __shared__ uint32_t count, hits, sums, warp_bound[2][T / 32];
+  __shared__ uint32_t count, hits, sums, warp_bound[T / 32];
   __shared__ float warp_max[T / 32], warp_sum[T / 32];
   let_next_start();
   const uint32_t row = blockIdx.x / ch.per_row, chunk = blockIdx.x - row * ch.per_row, t = threadIdx.x;
@@ -440,19 +440,18 @@ __global__ void __launch_bounds__(T, 1024 / T) row_kernel(const __grid_constant_
     if (now > m) s *= m == kMinusInf ? 1.0f : exp2_of((m - now) * a.c2);  // (s is 0, or NaN, before the first number)
     m = now;
     s += fabsf(m) * a.c2 < 1024.0f ? sum_of<E, V, true>(u, m, a.c2) : sum_of<E, V, false>(u, m, a.c2);
-    // The first tile, or all so far are banned.  (The warps' words are others than those of the tile before, which some
-    // may still read.)
-    if (bound <= kOrderMinusInf + 1 && tile0 < last) {
+    if (bound <= kOrderMinusInf + 1 && tile0 < last) {  // the first tile, or all so far are banned
+      if (tile != 0) __syncthreads();  // the tile before's words of the warps have been read
       // Warps that have vectors; half of them are enough to count on all.
       const uint32_t each = kAligned ? 32 : turns * 32, some = ((last - tile0 + kW - 1) / kW + each - 1) / each;
       const uint32_t full = 2 * some >= T / 32 ? T / 32 : some;
       if (8 * a.keep <= 3 * T && a.keep <= 16 * full) {
-        bound = bound_of(order_of(tmax), a.keep, full, warp_bound[tile % 2]);
+        bound = bound_of(order_of(tmax), a.keep, full, warp_bound);
       } else {
         uint32_t keys[V];
 #pragma unroll
         for (int k = 0; k < V; ++k) keys[k] = order_of(value_of(most[k], E()));
-        bound = bound_of_all<V>(keys, a.keep, full, warp_bound[tile % 2]);
+        bound = bound_of_all<V>(keys, a.keep, full, warp_bound);
       }
       least = from_order(bound);
     }
@@ -486,7 +485,7 @@ __global__ void __launch_bounds__(T, 1024 / T) row_kernel(const __grid_constant_
   // (512 rows of 131,072 that ascend, or whose chunks' first tiles are banned, took 7 ms by exact bounds, and 45 us if
   // alike all along.)
   if (found > kHits && ch.tiles > 1) {  // (so few kept that bound_of has them)
-    const uint32_t here = bound_of(order_of(m), a.keep, T / 32, warp_bound[0]);
+    const uint32_t here = bound_of(order_of(m), a.keep, T / 32, warp_bound);
     if (here > bound) {
       bound = here;
       least = from_order(bound);
