@@ -494,8 +494,8 @@ typedef struct bf_attention_args {
  * to attend to (lengths 0, or every score -inf) out is 0 and lse -inf; a length
  * outside 0..tokens makes its answers' out and lse NaN, and so does a score that is NaN or above
  * 32-bit numbers.  For 16-bit types the
- * weights e^(s_t - max) are rounded to the type before the second product.
- * Neither out nor lse overlaps an input (the lengths among them) or the other. */
+ * weights e^(s_t - max) are rounded to the type before the second product (by at most 2^-8 of
+ * themselves for bf16; for f16 2^-11, or 2^-32 of the largest).  Neither out nor lse overlaps an input (the lengths among them) or the other. */
 BF_API int bf_prefix_attention(const bf_cache* q, const bf_cache* prefix_k, const bf_cache* prefix_v,
                                const bf_cache* suffix_k, const bf_cache* suffix_v, const bf_attention_args* args,
                                const bf_cache* out, float* d_lse, void* d_workspace, uint64_t workspace_bytes,

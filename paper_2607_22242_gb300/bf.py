@@ -867,7 +867,7 @@ def beam_step(logits, scores, beams: int, *, keep: Optional[int] = None, finishe
               length_penalty: float = 0.0, end_token: int = -1, temperature: float = 1.0, stream=None) -> BeamStep:
     """The best `keep` (by default `beams`) continuations of every group of `beams` rows of `logits` (rows x vocab),
     by the beams' `scores` (float32, one per row; -inf: not alive) plus the tokens' log-probabilities.  A beam that is
-    `finished` (bool, one per row) stays, with `end_token`.  With ``length_penalty`` continuations are ranked by score /
+    `finished` (bool, one per row) stays, with `end_token`.  With ``length_penalty`` (up to 65,536) continuations are ranked by score /
     length ** length_penalty, from the beams' `lengths` (int64, one per row).  Places without a continuation have score
     -inf and token -1."""
     import torch

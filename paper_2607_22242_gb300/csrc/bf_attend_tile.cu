@@ -18,7 +18,7 @@
 //
 // 131,072 keys of 8 heads of 128 dimensions: 87 us for up to 32 queries a head (6.2 TB/s)
 // and 92 for 128: the memory.  256 queries: 121 us, 1.14 PFLOP/s, the tensor cores busy for
-// 46 % of it: each stream's way from scores to weights takes 2,300 cycles of the 5,400 a
+// 45 % of it: each stream's way from scores to weights takes 2,300 cycles of the 5,400 a
 // tile, its products, behind the other stream's, the rest.  Handing the weights over in halves,
 // one pass over the scores and scalar exponentials were no faster.
 #include <cuda.h>

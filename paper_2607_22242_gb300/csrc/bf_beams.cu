@@ -340,11 +340,12 @@ __device__ __noinline__ void list_again_apart(const E* x, uint32_t cut, uint32_t
 
 // A chunk of a row, `tiles` times V vectors a thread, cut by the row's elements and not
 // by addresses, so that equal rows have equal sums.  kAligned: rows start at 16 bytes.
-// What reaches a bound that `keep` of the threads' maxima in the first tile reach may be
+// What reaches a bound that `keep` of the threads' maxima in the first tile (that has so many not banned) reach may be
 // among the chunk's best: a few more than `keep` in each tile.
 //
-// Bound by instruction issue (63 % of the slots; 12 instructions an element, of which the
-// exponential and its sum are 4): 107 MB of 131,072 bf16 logits a row in 31 us, 3.5 TB/s;
+// 107 MB of 131,072 bf16 logits a row in 31 us, 3.5 TB/s.  Neither the memory nor the issue slots are full (55 % of them over the
+// kernel's time, 63 % of a busy SM's cycles; 12 instructions an element, of which the exponential and its sum are 4):
+// a block's reads, bound, notes and ranks follow one another, and four blocks an SM, 3.4 waves of them, do not cover that;
 // rows at any alignment take a quarter more (512 of 131,071: 57 us a step, 45 of 131,072),
 // and took two thirds more when each thread read both vectors that hold its elements.
 template <typename E, int V, bool kAligned, uint32_t T>
