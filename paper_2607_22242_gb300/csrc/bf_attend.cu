@@ -187,11 +187,11 @@ __device__ void piece(const Piece& p, uint32_t rows, uint32_t dim, float* sm) {
   for (int i = 0; i < 4; ++i) {
     const uint32_t row = rg * 4 + i;
     if (row >= rows) break;
+    float* to = p.record + record_place(p.held, row, cg);
 #pragma unroll
-    for (uint32_t c = 0; c < S::kOuts; ++c) {
-      const uint32_t d = cg + c * S::kCols;
-      if (d >= dim) break;
-      p.record[record_place(p.held, row, d)] = o[i][c];
+    for (uint32_t c = 0; c < S::kOuts; ++c) {  // kCols dimensions further on: kCols / 4 times four of all rows
+      if (cg + c * S::kCols >= dim) break;
+      to[c * S::kCols * p.held] = o[i][c];
     }
   }
   if (t < rows) {
@@ -227,15 +227,15 @@ __global__ void __launch_bounds__(kThreads, 2) general_kernel(const __grid_const
   let_next_start();
   if (blockIdx.x < plan.parts) {
     const uint32_t inners = a.kv_heads * plan.row_tiles, rows_all = a.per_prompt * a.share;
-    const uint64_t total = tiles_before(a, kKeys, a.prompts) * inners;
+    const uint64_t total = tiles_of_all(a, plan, kKeys) * inners;
     const uint64_t parts = parts_of(plan, total);
     if (blockIdx.x >= parts) return;
     const uint64_t t0 = total * blockIdx.x / parts, t1 = total * (blockIdx.x + 1) / parts;
-    Place at = place_of(a, kKeys, inners, t0);
+    Place at = place_of(a, plan, kKeys, inners, t0);
     for (uint64_t left = t1 - t0; left;) {
       const uint32_t len = length_of(a.prefix_len, a.prefix_cap, at.prompt), tiles = (len + kKeys - 1) / kKeys;
       if (tiles == 0) {
-        ++at.prompt;
+        at.prompt = a.prompts > kFewPrompts ? not_empty_from(a, at.prompt + 1) : at.prompt + 1;
         continue;
       }
       const uint32_t n = (uint32_t)min((uint64_t)(tiles - at.tile), left);
@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
   if (vec >= (uint64_t)a.prompts * a.per_prompt * heads) return;
   const uint32_t answer = (uint32_t)(vec / heads), h = (uint32_t)vec - answer * heads, head = h / a.share, prompt = answer / a.per_prompt;
   const uint32_t srow = h - head * a.share, row = (answer - prompt * a.per_prompt) * a.share + srow;
-  const Owners own = owners_of(a, plan, standing_of(a, plan.keys, prompt), prompt, head * plan.row_tiles + row / plan.rows);
+  const Owners own = owners_of(a, plan, standing_of(a, plan, prompt), prompt, head * plan.row_tiles + row / plan.rows);
   const uint32_t far = own.last - own.first, splits = a.suffix_cap ? plan.suffix_splits : 0, pieces = far + splits;
   const float* prefix = plan.prefix + (own.first + own.segment) * plan.record;
   const uint64_t sslot = (((uint64_t)answer * a.kv_heads + head) * plan.suffix_row_tiles + srow / plan.suffix_rows) * plan.suffix_splits;
@@ -340,6 +340,42 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
   if (a.lse && d == 0) a.lse[vec] = odd ? nan : l > 0.0f ? (m + log2f(l)) * 0.693147180559945309f : kNone;
 }
 
+// The tiles ahead of each prompt, and all, where there are many: one block, eight prompts a thread and turn.
+constexpr uint32_t kCountThreads = 1024, kCounted = 8;
+__global__ void __launch_bounds__(kCountThreads) count_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ AttendPlan plan) {
+  __shared__ uint64_t warps[2][32];
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  uint64_t before = 0;
+  uint32_t turn = 0;
+  for (uint64_t first = 0; first < a.prompts; first += kCountThreads * kCounted, turn ^= 1) {
+    const uint64_t p = first + threadIdx.x * kCounted;
+    uint32_t n[kCounted];
+    uint64_t mine = 0;
+#pragma unroll
+    for (uint32_t j = 0; j < kCounted; ++j) {
+      n[j] = p + j < a.prompts ? tiles_of(a, plan.keys, p + j) : 0;
+      mine += n[j];
+    }
+    uint64_t upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const uint64_t o = __shfl_up_sync(~0u, upto, d);
+      if (lane >= d) upto += o;
+    }
+    if (lane == 31) warps[turn][warp] = upto;  // (those of the turn before may still be read)
+    __syncthreads();
+    const uint64_t w = warps[turn][lane];
+    uint64_t at = before + sum_lanes(lane < warp ? w : 0) + upto - mine;
+#pragma unroll
+    for (uint32_t j = 0; j < kCounted; ++j) {
+      if (p + j < a.prompts) plan.before[p + j] = at;
+      at += n[j];
+    }
+    before += sum_lanes(w);
+  }
+  if (threadIdx.x == 0) plan.before[a.prompts] = before;
+}
+
 // ---- the host's part --------------------------------------------------------
 
 constexpr uint32_t kParts = 304;  // two blocks of each of 152 SMs
@@ -373,6 +409,7 @@ AttendPlan plan_of(const AttendArgs& a, bool tile, void* workspace, uint64_t* by
   };
   p.gave_up = reinterpret_cast<uint32_t*>(take(4 * kTileParts));
   if (!tile) p.gave_up = nullptr;
+  p.before = reinterpret_cast<uint64_t*>(take(a.prompts > kFewPrompts ? 8 * ((uint64_t)a.prompts + 1) : 0));
   p.prefix = reinterpret_cast<float*>(take(4 * (p.parts + (uint64_t)a.prompts * a.kv_heads * p.row_tiles) * p.record));
   p.suffix = reinterpret_cast<float*>(take(a.suffix_cap ? 4 * pieces * p.suffix_splits * p.suffix_record : 0));
   *bytes = (uint64_t)(at - static_cast<char*>(workspace));
@@ -404,6 +441,8 @@ cudaError_t launch_type(const AttendArgs& a, void* workspace, cudaStream_t st) {
   const uint64_t answers = (uint64_t)a.prompts * a.per_prompt;
   const uint64_t suffix = a.suffix_cap ? answers * a.kv_heads * p.suffix_row_tiles * p.suffix_splits : 0;
   cudaError_t e = cudaSuccess;
+  if (a.prompts > kFewPrompts && a.prefix_len) e = launch_plain(count_kernel, 1, kCountThreads, st, a, p);
+  if (e != cudaSuccess) return e;
   AttendPlan general = p;
   if (tile) {
     e = launch_tile(a, p, st);

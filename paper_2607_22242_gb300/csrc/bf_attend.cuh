@@ -31,6 +31,7 @@ struct AttendPlan {
   uint32_t suffix_rows, suffix_row_tiles, suffix_splits;  // the answers' own keys: pieces of an answer and key head
   float *prefix, *suffix;        // records
   uint32_t* gave_up;             // of the tiled kernel's blocks; nullptr: it does not run
+  uint64_t* before;              // tiles ahead of each prompt, and all; of more than kFewPrompts
   uint32_t record, suffix_record;  // floats of a record
 };
 
@@ -75,10 +76,21 @@ __device__ __forceinline__ uint64_t sum_lanes(uint64_t v) {
   return v;
 }
 
-// Key tiles of prompts [0, p) in one segment each; by a whole warp.
-__device__ __forceinline__ uint64_t tiles_before(const AttendArgs& a, uint32_t keys, uint32_t p) {
+// Key tiles of a prompt in one segment, of the prompts ahead of it, and of all.  Up to kFewPrompts a warp adds up where it
+// needs to know; of more prompts `before` has the sums (every warp adding up all was 6 ms of 65,536 prompts, and minutes of millions).
+constexpr uint32_t kFewPrompts = 128;
+__device__ __forceinline__ uint32_t tiles_of(const AttendArgs& a, uint32_t keys, uint64_t p) {
+  return (length_of(a.prefix_len, a.prefix_cap, p) + keys - 1) / keys;
+}
+// Tiles ahead of prompt p (of all: p the prompts), of more than kFewPrompts.
+__device__ __forceinline__ uint64_t tiles_ahead(const AttendArgs& a, const AttendPlan& plan, uint32_t keys, uint64_t p) {
+  return a.prefix_len ? __ldg(plan.before + p) : p * (((uint32_t)a.prefix_cap + keys - 1) / keys);
+}
+// All tiles; by a whole warp.
+__device__ __forceinline__ uint64_t tiles_of_all(const AttendArgs& a, const AttendPlan& plan, uint32_t keys) {
+  if (a.prompts > kFewPrompts) return tiles_ahead(a, plan, keys, a.prompts);
   uint64_t n = 0;
-  for (uint32_t i = threadIdx.x % 32; i < p; i += 32) n += (length_of(a.prefix_len, a.prefix_cap, i) + keys - 1) / keys;
+  for (uint32_t i = threadIdx.x % 32; i < a.prompts; i += 32) n += tiles_of(a, keys, i);
   return sum_lanes(n);
 }
 
@@ -90,27 +102,56 @@ __device__ __forceinline__ uint64_t parts_of(const AttendPlan& plan, uint64_t to
 struct Place {
   uint32_t prompt, inner, tile;
 };
-// The place of tile t (below the total); by a whole warp.
-__device__ __forceinline__ Place place_of(const AttendArgs& a, uint32_t keys, uint32_t inners, uint64_t t) {
+// The place of tile t (below the total) among more than kFewPrompts; by a whole warp.
+__device__ __forceinline__ Place place_far(const AttendArgs& a, const AttendPlan& plan, uint32_t keys, uint32_t inners, uint64_t t) {
+  const uint32_t lane = threadIdx.x % 32;
+  uint64_t lo = 0, hi = a.prompts;  // the last prompt that no more than t tiles are ahead of lies in [lo, hi)
+  while (hi - lo > 1) {
+    const uint64_t step = (hi - lo + 31) / 32, p = lo + lane * step;
+    const uint32_t not_past = __popc(__ballot_sync(~0u, p < hi && tiles_ahead(a, plan, keys, p) * inners <= t));
+    lo += (not_past - 1) * step;  // (lane 0's is not)
+    hi = min(hi, lo + step);
+  }
+  const uint64_t in = t - tiles_ahead(a, plan, keys, lo) * inners;
+  const uint32_t mine = tiles_of(a, keys, lo);
+  return {(uint32_t)lo, (uint32_t)(in / mine), (uint32_t)(in % mine)};
+}
+// Out of line, for kernels that a few instructions more to fetch are long for.
+static __device__ __noinline__ Place place_far_apart(const AttendArgs& a, const AttendPlan& plan, uint32_t keys, uint32_t inners, uint64_t t) {
+  return place_far(a, plan, keys, inners, t);
+}
+// The same among any.
+__device__ __forceinline__ Place place_of(const AttendArgs& a, const AttendPlan& plan, uint32_t keys, uint32_t inners, uint64_t t) {
+  const uint32_t lane = threadIdx.x % 32;
+  if (a.prompts > kFewPrompts) return place_far_apart(a, plan, keys, inners, t);
   uint64_t before = 0;
   for (uint32_t first = 0; first < a.prompts; first += 32) {
-    const uint32_t i = first + threadIdx.x % 32;
-    const uint64_t n = i < a.prompts ? (uint64_t)((length_of(a.prefix_len, a.prefix_cap, i) + keys - 1) / keys) * inners : 0;
+    const uint32_t i = first + lane;
+    const uint64_t n = i < a.prompts ? (uint64_t)tiles_of(a, keys, i) * inners : 0;
     uint64_t upto = n;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
       const uint64_t o = __shfl_up_sync(~0u, upto, d);
-      if (threadIdx.x % 32 >= d) upto += o;
+      if (lane >= d) upto += o;
     }
     const uint32_t past = __ballot_sync(~0u, before + upto > t);
     if (past) {
-      const int lane = __ffs(past) - 1;
-      const uint64_t at = __shfl_sync(~0u, before + upto - n, lane), mine = __shfl_sync(~0u, n, lane) / inners;
-      return {first + lane, (uint32_t)((t - at) / mine), (uint32_t)((t - at) % mine)};
+      const int owner = __ffs(past) - 1;
+      const uint64_t at = __shfl_sync(~0u, before + upto - n, owner), mine = __shfl_sync(~0u, n, owner) / inners;
+      return {first + owner, (uint32_t)((t - at) / mine), (uint32_t)((t - at) % mine)};
     }
     before += __shfl_sync(~0u, upto, 31);
   }
   return {a.prompts, 0, 0};
+}
+
+// The first prompt from p on that is not empty (there is one), of more than kFewPrompts; by a whole warp.
+__device__ __forceinline__ uint32_t not_empty_from(const AttendArgs& a, uint32_t p) {
+  for (;; p += 32) {
+    const uint64_t i = (uint64_t)p + threadIdx.x % 32;
+    const uint32_t some = __ballot_sync(~0u, i < a.prompts && length_of(a.prefix_len, a.prefix_cap, i) != 0);
+    if (some) return p + __ffs(some) - 1;
+  }
 }
 
 // The prompts' keys on the tensor cores (bf_attend_tile.cu): what of a call says that it may take them, and, with
@@ -134,13 +175,15 @@ struct Standing {
   uint64_t total, before;
   uint32_t tiles;
 };
-__device__ __forceinline__ Standing standing_of(const AttendArgs& a, uint32_t keys, uint32_t prompt) {
+__device__ __forceinline__ Standing standing_of(const AttendArgs& a, const AttendPlan& plan, uint32_t prompt) {
+  const uint32_t keys = plan.keys;
+  if (a.prompts > kFewPrompts) return {tiles_ahead(a, plan, keys, a.prompts), tiles_ahead(a, plan, keys, prompt), tiles_of(a, keys, prompt)};
   uint64_t total = 0, before = 0;
   uint32_t mine = 0;
   if (((a.prefix_cap + keys - 1) / keys) * a.prompts < 1ull << 31) {  // sums of 32 bits, an instruction each
     uint32_t all = 0, ahead = 0;
     for (uint32_t i = threadIdx.x % 32; i < a.prompts; i += 32) {
-      const uint32_t n = (length_of(a.prefix_len, a.prefix_cap, i) + keys - 1) / keys;
+      const uint32_t n = tiles_of(a, keys, i);
       all += n;
       ahead += i < prompt ? n : 0;
       mine += i == prompt ? n : 0;
@@ -149,7 +192,7 @@ __device__ __forceinline__ Standing standing_of(const AttendArgs& a, uint32_t ke
     before = __reduce_add_sync(~0u, ahead);
   } else {
     for (uint32_t i = threadIdx.x % 32; i < a.prompts; i += 32) {
-      const uint32_t n = (length_of(a.prefix_len, a.prefix_cap, i) + keys - 1) / keys;
+      const uint32_t n = tiles_of(a, keys, i);
       total += n;
       before += i < prompt ? n : 0;
       mine += i == prompt ? n : 0;

@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(kWarps * 32) few_kernel(const __grid_constant_
   // two tiles of queries.
   const uint32_t row0 = (answer - prompt * a.per_prompt) * a.share + first;
   const uint32_t tile0 = row0 / plan.rows, rows0 = min(rows, (tile0 + 1) * plan.rows - row0);
-  const Standing standing = standing_of(a, plan.keys, prompt);
+  const Standing standing = standing_of(a, plan, prompt);
   const Owners own0 = owners_of(a, plan, standing, prompt, head * plan.row_tiles + tile0);
   const Owners own1 = rows0 == rows ? own0 : owners_of(a, plan, standing, prompt, head * plan.row_tiles + tile0 + 1);
   const bool bad = bad_answer(a, prompt, answer);

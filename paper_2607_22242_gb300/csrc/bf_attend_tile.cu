@@ -69,7 +69,7 @@ struct Pieces {
       : a(args), plan(p), inners(args.kv_heads * p.row_tiles), my_len{}, left(0), at{0, 0, 0}, len(0), tiles(0), head(0), first_row(0) {
     const uint32_t lane = threadIdx.x % 32;
     uint64_t t0;
-    if (a.prompts <= 128) {
+    if (a.prompts <= kFewPrompts) {
       uint32_t n = 0, upto;
 #pragma unroll
       for (uint32_t j = 0; j < 4; ++j)
@@ -97,8 +97,8 @@ struct Pieces {
       at.inner = in >> 32 ? (uint32_t)(in / mine) : (uint32_t)in / mine;
       at.tile = (uint32_t)(in - (uint64_t)at.inner * mine);
     } else {
-      if (!share(tiles_before(a, kKeys, a.prompts) * inners, &t0)) return;
-      at = place_of(a, kKeys, inners, t0);
+      if (!share(tiles_of_all(a, plan, kKeys) * inners, &t0)) return;
+      at = place_far(a, plan, kKeys, inners, t0);
     }
     find();
   }
@@ -125,7 +125,8 @@ struct Pieces {
   __device__ __forceinline__ void find() {
     for (;; ++at.prompt) {
       if (left == 0) return;
-      len = a.prompts <= 128 ? len_of(at.prompt) : length_of(a.prefix_len, a.prefix_cap, at.prompt);
+      if (a.prompts > kFewPrompts) at.prompt = not_empty_from(a, at.prompt);
+      len = a.prompts <= kFewPrompts ? len_of(at.prompt) : length_of(a.prefix_len, a.prefix_cap, at.prompt);
       if (len) break;
     }
     tiles = (uint32_t)min((uint64_t)((len + kKeys - 1) / kKeys - at.tile), left);

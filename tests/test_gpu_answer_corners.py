@@ -232,6 +232,58 @@ def test_beams_of_uneven_rows_take_no_longer(kind):
     assert took <= 4 * alike
 
 
+# ---- thousands of prompts ----
+
+def prompts_of(count, dim, tokens, own, dtype, lengths=None):
+    gen = torch.Generator(device="cuda").manual_seed(count)
+    rand = lambda *n: torch.randn(*n, generator=gen, device="cuda").to(TYPES[dtype])
+    x = (rand(count, 2, dim), rand(count, tokens, 1, dim), rand(count, tokens, 1, dim), rand(count, own, 1, dim), rand(count, own, 1, dim))
+    return x, torch.randint(0, tokens + 1, (count,), generator=gen, device="cuda") if lengths is None else lengths
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("count,dim", [(129, 64), (9000, 64), (20000, 40), (9000, 30)])
+@pytest.mark.parametrize("kind", ["any", "runs", "none", "last", "full"])
+def test_attention_of_thousands_of_prompts(count, dim, kind, dtype):
+    """Prompts of any length; thousands that are empty behind each other; none that is not; the last alone; all full."""
+    x, n = prompts_of(count, dim, 200, 5, dtype)
+    if kind == "runs":
+        n[count // 9:count // 2] = 0
+        n[-count // 4:] = 0
+    elif kind in ("none", "last"):
+        n.zero_()
+        n[-1] = 131 if kind == "last" else 0
+    given = None if kind == "full" else n
+    out, lse = bf.prefix_attention(*x, prefix_lengths=given, lse=True)
+    q, pk, pv, sk, sv = (t.double() for t in x)
+    k, v = torch.cat([pk, sk], 1)[:, :, 0], torch.cat([pv, sv], 1)[:, :, 0]
+    s = torch.einsum("phd,ptd->pht", q, k) * dim ** -0.5
+    if given is not None:
+        at = torch.arange(205, device="cuda")
+        s = s.masked_fill(((at >= n[:, None]) & (at < 200))[:, None], -INF)
+    w = torch.softmax(s, -1)
+    want, size = torch.einsum("pht,ptd->phd", w, v), torch.einsum("pht,ptd->phd", w, v.abs())
+    # As test_gpu_answer.py, with the largest score's products and 205 keys.
+    most = torch.einsum("phd,ptd->pht", q.abs(), k.abs()).max().item() * dim ** -0.5
+    weight = 2 * (dim + 4) * 2.0 ** -24 * most + 2.0 ** -22 + 2.0 ** -17
+    total = weight + 221 * 2.0 ** -24
+    rounded = 0.0 if dtype == "f32" else half(dtype)
+    bound = (weight + rounded + total) * size + (205 * 2.0 ** -32 * 6 + 2.0 ** -25 if dtype == "f16" else 0.0) + half(dtype) * (1 + 2.0 ** -8) * want.abs()
+    assert ((out.double() - want).abs() <= bound).all()
+    assert ((lse.double() - torch.logsumexp(s, -1)).abs() <= total + 2.0 ** -23 * (most + 20)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lengths", [False, True])
+def test_attention_time_is_of_the_prompts(lengths, dtype):
+    """Eight times the prompts take not much more than eight times as long (20 to 30 where every unit adds up all lengths)."""
+    took = []
+    for count in (8192, 65536):
+        x, n = prompts_of(count, 64, 64, 16, dtype)
+        took.append(time_of(lambda: bf.prefix_attention(*x, prefix_lengths=n if lengths else None)))
+    assert took[1] <= 16 * took[0], took
+
+
 # ---- length penalties ----
 
 @pytest.mark.parametrize("penalty", [1.0, 1.8, 2.5, 13.0, 30.0, 200.0, 5000.0, 65536.0])
