@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(kThreads, 2) general_kernel(const __grid_const
     if (blockIdx.x >= parts) return;
     const uint64_t t0 = total * blockIdx.x / parts, t1 = total * (blockIdx.x + 1) / parts;
     Place at = place_of(a, plan, kKeys, inners, t0);
-    for (uint64_t left = t1 - t0; left;) {
+    for (uint64_t left = t1 - t0; left && at.prompt < a.prompts;) {
       const uint32_t len = length_of(a.prefix_len, a.prefix_cap, at.prompt), tiles = (len + kKeys - 1) / kKeys;
       if (tiles == 0) {
         at.prompt = a.prompts > kFewPrompts ? not_empty_from(a, at.prompt + 1) : at.prompt + 1;

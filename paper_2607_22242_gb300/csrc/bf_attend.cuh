@@ -145,13 +145,14 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a, const AttendPlan&
   return {a.prompts, 0, 0};
 }
 
-// The first prompt from p on that is not empty (there is one), of more than kFewPrompts; by a whole warp.
+// The first prompt from p on that is not empty, of more than kFewPrompts; by a whole warp.  (There is one, unless lengths
+// change under the call: then there may be none, and nothing goes on.)
 __device__ __forceinline__ uint32_t not_empty_from(const AttendArgs& a, uint32_t p) {
-  for (;; p += 32) {
-    const uint64_t i = (uint64_t)p + threadIdx.x % 32;
-    const uint32_t some = __ballot_sync(~0u, i < a.prompts && length_of(a.prefix_len, a.prefix_cap, i) != 0);
+  for (; p < a.prompts; p += 32) {
+    const uint32_t i = p + threadIdx.x % 32, some = __ballot_sync(~0u, i < a.prompts && length_of(a.prefix_len, a.prefix_cap, i) != 0);
     if (some) return p + __ffs(some) - 1;
   }
+  return a.prompts;
 }
 
 // The prompts' keys on the tensor cores (bf_attend_tile.cu): what of a call says that it may take them, and, with

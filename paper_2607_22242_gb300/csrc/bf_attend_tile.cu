@@ -124,8 +124,9 @@ struct Pieces {
   }
   __device__ __forceinline__ void find() {
     for (;; ++at.prompt) {
+      if (left && a.prompts > kFewPrompts) at.prompt = not_empty_from(a, at.prompt);
+      if (at.prompt >= a.prompts) left = 0;
       if (left == 0) return;
-      if (a.prompts > kFewPrompts) at.prompt = not_empty_from(a, at.prompt);
       len = a.prompts <= kFewPrompts ? len_of(at.prompt) : length_of(a.prefix_len, a.prefix_cap, at.prompt);
       if (len) break;
     }
